@@ -94,8 +94,8 @@ def work(case):
         return dict(bytes=T * N * t + T * (K + -(-K // c["group"])) + 4 * N * K, flops=2 * T * N * K)
     E = c["T"] * c["V"]
     if c["kind"] == "logprob":
-        return dict(bytes=E * t + c["T"] * (16 + 8 * c["top"]), flops=6 * E)
-    return dict(bytes=2 * E * t + c["T"] * 20, flops=6 * E)
+        return dict(bytes=E * t + c["T"] * (20 + 8 * c["top"]), flops=6 * E)
+    return dict(bytes=2 * E * t + c["T"] * 24, flops=6 * E)
 
 
 # ---- inputs ------------------------------------------------------------------------------------------------
@@ -198,12 +198,12 @@ def prepare(case, seed):
             y[T // 3] = -1
             x[T // 2] = -math.inf
         s["x"], s["target"] = x.to(t)[:, :V], y.to(torch.int32)
-        s["lse"], s["entropy"], s["logprob"] = f32(T), f32(T), f32(T)
+        s["stats"], s["entropy"], s["logprob"] = f32(T, 2), f32(T), f32(T)
         if c["kind"] == "logprob":
             s["top_logprob"] = f32(T, c["top"])
             s["top_index"] = torch.empty(T, c["top"], dtype=torch.int32, device=dev)
         else:
-            s["lse"], s["entropy"] = _softmax_numbers(s["x"].float())
+            s["stats"], s["entropy"] = _softmax_numbers(s["x"].float())
             s["g_logprob"] = -torch.rand(T, generator=gen, device=dev) / T
             s["g_entropy"] = -0.01 * torch.rand(T, generator=gen, device=dev) / T
             s["dx"] = torch.empty(T, V, dtype=t, device=dev)
@@ -257,14 +257,12 @@ def run(state):
     has = y >= 0
     at = y.clamp(min=0).unsqueeze(1)
     if c["kind"] == "logprob":
-        lse, entropy = _softmax_numbers(x)
-        lp = torch.where(lse == -math.inf, lse, x.gather(1, at).squeeze(1) - lse)
+        stats, entropy = _softmax_numbers(x)
+        lp = _logp(x.gather(1, at), stats).squeeze(1)
         top, index = _top(x, c["top"])
-        top = torch.where((lse == -math.inf).unsqueeze(1), torch.full_like(top, -math.inf), top - lse.unsqueeze(1))
-        return dict(logprob=torch.where(has, lp, torch.zeros_like(lp)), entropy=entropy, lse=lse, top_logprob=top,
-                    top_index=index)
-    lse = s["lse"].unsqueeze(1)
-    lp = x - torch.where(lse == -math.inf, torch.zeros_like(lse), lse)
+        return dict(logprob=torch.where(has, lp, torch.zeros_like(lp)), entropy=entropy, stats=stats,
+                    top_logprob=_logp(top, stats), top_index=index)
+    lp = _logp(x, s["stats"])
     p = torch.exp(lp)
     a = torch.where(has, s["g_logprob"], torch.zeros_like(s["g_logprob"])).unsqueeze(1)
     lp = torch.where(p > 0, lp, torch.zeros_like(lp)) + s["entropy"].unsqueeze(1)
@@ -273,15 +271,23 @@ def run(state):
 
 
 def _softmax_numbers(x):
-    """Logarithm of the sum of exponentials and entropy per row; -inf and 0 for a row of -inf."""
+    """Largest logit and logarithm of the sum of exponentials relative to it, and entropy, per row; -inf, 0 and 0 for a
+    row of -inf."""
     m = x.amax(dim=1, keepdim=True)
     d = x - torch.where(m == -math.inf, torch.zeros_like(m), m)
     e = torch.exp(d)
     z = e.sum(dim=1)
     w = (e * torch.where(e > 0, d, torch.zeros_like(d))).sum(dim=1)
     empty = m.squeeze(1) == -math.inf
-    lse = torch.where(empty, m.squeeze(1), m.squeeze(1) + torch.log(z))
-    return lse, torch.where(empty, torch.zeros_like(z), torch.log(z) - w / z)
+    zero = torch.zeros_like(z)
+    log_sum = torch.where(empty, zero, torch.log(z))
+    return torch.stack((m.squeeze(1), log_sum), dim=1), torch.where(empty, zero, log_sum - w / z)
+
+
+def _logp(x, stats):
+    """Logarithms of probabilities; -inf in a row of -inf."""
+    m, log_sum = stats[:, :1], stats[:, 1:]
+    return torch.where(m == -math.inf, torch.full_like(x, -math.inf), (x - m) - log_sum)
 
 
 def _top(x, k):
@@ -320,9 +326,9 @@ def _call(s, c):
     x = s["x"]
     if c["kind"] == "logprob":
         qa.qa_token_logprob(t, c["T"], c["V"], x, x.stride(0), s["target"], c["top"], s["logprob"], s["entropy"],
-                            s["lse"], s["top_logprob"] if c["top"] else None, s["top_index"] if c["top"] else None, ws)
-        return {k: s[k] for k in ("logprob", "entropy", "lse", "top_logprob", "top_index")}
-    qa.qa_token_logprob_grad(t, c["T"], c["V"], x, x.stride(0), s["target"], s["lse"], s["entropy"], s["g_logprob"],
+                            s["stats"], s["top_logprob"] if c["top"] else None, s["top_index"] if c["top"] else None, ws)
+        return {k: s[k] for k in ("logprob", "entropy", "stats", "top_logprob", "top_index")}
+    qa.qa_token_logprob_grad(t, c["T"], c["V"], x, x.stride(0), s["target"], s["stats"], s["entropy"], s["g_logprob"],
                              s["g_entropy"], s["dx"], s["dx"].stride(0))
     return dict(dx=s["dx"])
 
@@ -378,7 +384,9 @@ def exact(case, seed):
         if c["kind"] == "logprob":
             given = logp.gather(1, y.clamp(min=0)[:, None])[:, 0]
             entropy = -torch.where(p > 0, p * logp, torch.zeros_like(p)).sum(dim=1)
-            got.append((torch.where(y < 0, torch.zeros_like(given), given), entropy, lse,
+            most = x.max(dim=1).values
+            got.append((torch.where(y < 0, torch.zeros_like(given), given), entropy,
+                        torch.stack((most, torch.where(torch.isinf(lse), torch.zeros_like(lse), lse - most)), dim=1),
                         logp.topk(c["top"], dim=1).values))
         else:
             a = torch.where(y < 0, torch.zeros_like(lse), s["g_logprob"][i:i + step].double())[:, None]
@@ -390,4 +398,4 @@ def exact(case, seed):
     got = [torch.cat(v) for v in zip(*got)]
     if c["kind"] == "logprob_grad":
         return dict(dx=got[0])
-    return dict(logprob=got[0], entropy=got[1], lse=got[2], top_logprob=got[3], top_index=None)
+    return dict(logprob=got[0], entropy=got[1], stats=got[2], top_logprob=got[3], top_index=None)
