@@ -452,6 +452,127 @@ int qa_step_qrda_segments(const qa_layout* layout, const qa_segment_plan* plan,
                           int64_t t, float eta, float lambda, float delta, int requant, void* ws,
                           size_t ws_bytes, void* stream);
 
+/* ---- operators of a language model's worker ----------------------------------------------------
+ *
+ * A worker whose model is a network of layers over tokens forms its local gradient from more than
+ * one loss of a linear model.  These calls are the parts of it that are read and written in few
+ * bits, or that turn answers into a gradient; what they leave, weight gradients in binary32, is what
+ * qa_quantize_pack and qa_quantize_pack_segments take.
+ *
+ * Arithmetic: inputs of any type are widened to binary32; sums, norms and softmax statistics are
+ * held in binary32 (weight gradients: products of the matrix cores, added in binary32) in an order
+ * that depends on the sizes alone, so a call repeats bit for bit; outputs are rounded once, to nearest.
+ *
+ * Rows: element (t, k) of a matrix is at t*stride + k, strides in elements.  Element buffers need the
+ * alignment of their element only, and any stride that is at least the row's length (rows of a
+ * multiple of 16 bytes that begin on 16 bytes are read fastest); codes begin on 16 bytes and their
+ * code_stride is a multiple of 16.  rows == 0 is a call without rows: it returns QA_OK, and gradients
+ * that are sums over the rows are written as zeros (kept, with accumulate).  Buffers do not overlap
+ * unless a comment says so. */
+#define QA_F32 0
+#define QA_BF16 1
+#define QA_F16 2
+
+/* Rows in 8 bits ("coded rows").  Group k of a row, its columns [k*group, (k+1)*group) up to cols, has
+ * one byte b = scales[t*scale_stride + k] and stands for the values
+ *     codes[t*code_stride + i] * 2^(b - 127),    -127 <= code <= 127.
+ * The scale is the smallest power of two by which the group's largest magnitude is at most 127, and
+ * 2^-126 at least; a code is the nearest whole multiple, ties to even: an error of at most half the
+ * scale, 1/127 of the group's largest magnitude at most.  A code times a power of two has seven significant bits: every
+ * value is exact in bfloat16 (and finite: at b = 249, the largest that a finite magnitude needs, codes end at 63).  b = 255 marks a group with an infinity or a NaN: its codes are 0, its
+ * values are read as NaN.  b = 0 is never written and is read as scale 0.  Bytes between cols and code_stride are
+ * neither written nor used. */
+typedef struct {
+  int64_t rows;         /* 0 <= rows < 2^31                                                   */
+  int64_t cols;         /* 1 <= cols < 2^24                                                   */
+  int32_t group;        /* columns per scale: 32, 64 or 128                                   */
+  int64_t code_stride;  /* bytes between rows of codes, >= cols, a multiple of 16             */
+  int64_t scale_stride; /* bytes between rows of scales, >= ceil(cols/group)                  */
+} qa_coded_rows;
+
+/* operations for qa_rows_workspace_bytes */
+#define QA_OP_NORM_GRAD 8
+#define QA_OP_WEIGHT_GRAD 9
+
+/* Bytes of device workspace that `op` needs: QA_OP_NORM_GRAD (type of dy; n is not used) or
+ * QA_OP_WEIGHT_GRAD (type of dy, n = its columns).  0 if none, or for invalid arguments. */
+size_t qa_rows_workspace_bytes(const qa_coded_rows* rows, int op, int type, int64_t n);
+
+/* Codes of x's rows, as a checkpoint for the backward pass. */
+int qa_rows_pack(const qa_coded_rows* rows, int type, const void* x, int64_t x_stride, int8_t* codes,
+                 uint8_t* scales, void* stream);
+/* The values that the codes stand for (in QA_F16 rounded, and infinite beyond its range). */
+int qa_rows_unpack(const qa_coded_rows* rows, const int8_t* codes, const uint8_t* scales, int type,
+                   void* x_out, int64_t x_stride, void* stream);
+
+/* Weight gradient of a linear layer y = W x (W of n rows and rows->cols columns) from the codes of
+ * its input and the gradient dy of its output:
+ *     dw[j*dw_stride + k] = (accumulate ? dw[j*dw_stride + k] : 0) + sum_t dy[t*dy_stride + j] * value(t, k)
+ * dy may be of any type; binary32 and binary16 elements are split into bfloat16 parts that add up to
+ * them (to 2^-24 of them, and exactly), so that no precision of theirs is lost.  Infinities and NaN in
+ * dy, and groups without values, make the sums that they enter NaN or infinite.
+ * 1 <= n < 2^24.  ws: qa_rows_workspace_bytes(rows, QA_OP_WEIGHT_GRAD, type, n) bytes, may be NULL if 0. */
+int qa_rows_weight_grad(const qa_coded_rows* rows, const int8_t* codes, const uint8_t* scales, int type,
+                        const void* dy, int64_t dy_stride, int64_t n, float* dw, int64_t dw_stride,
+                        int accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* Root-mean-square norm of a residual stream, coded in 8 bits:
+ *     h = x + residual (h = x without one);  rstd = 1 / sqrt(mean_k h_k^2 + eps)
+ *     y_k = (h_k * rstd) * weight_k  ->  codes, scales;  y_out = the values they stand for
+ * from one read of x and residual.  h_out (type `type`, may be x or residual itself, with its stride),
+ * y_out (bfloat16 whatever `type` is: the values are exact in it) and rstd (binary32, one per row) may be
+ * NULL, and residual too; so may codes and scales together, if y_out is not.  The norm is that of the
+ * unrounded h.  A linear layer that multiplies y_out and whose weight gradient reads the codes uses the
+ * same numbers in both.  eps >= 0.  A row of zeros with eps = 0 gives rstd = infinity, and NaN. */
+int qa_rms_norm(const qa_coded_rows* rows, int type, const void* x, int64_t x_stride,
+                const void* residual_or_null, int64_t residual_stride, const float* weight, float eps,
+                void* h_out_or_null, int64_t h_stride, int8_t* codes, uint8_t* scales,
+                void* y_out_or_null, int64_t y_stride, float* rstd_or_null, void* stream);
+
+/* Its backward pass.  h is the stream as qa_rms_norm wrote it (h, type `type`), or its codes (h = NULL,
+ * h_codes and h_scales with the strides of `rows`); rstd as qa_rms_norm wrote it:
+ *     n_k = h_k * rstd;  c = mean_k(dy_k weight_k n_k)
+ *     dx_k = rstd * (dy_k weight_k - n_k c) + dh_k          (dh: the gradient that reaches h past the norm)
+ *     dweight_k = (accumulate ? dweight_k : 0) + sum_t dy_k n_k
+ * dx (type `type`) is the gradient of x and of residual alike and may be dh or dy itself, with its stride.
+ * dh_or_null and dweight_or_null may be NULL.  The codes' rounding counts as part of h.
+ * ws: qa_rows_workspace_bytes(rows, QA_OP_NORM_GRAD, type, 0) bytes, may be NULL without dweight. */
+int qa_rms_norm_grad(const qa_coded_rows* rows, int type, const void* dy, int64_t dy_stride, const void* h,
+                     int64_t h_stride, const int8_t* h_codes, const uint8_t* h_scales, const float* weight,
+                     const float* rstd, const void* dh_or_null, int64_t dh_stride, void* dx,
+                     int64_t dx_stride, float* dweight_or_null, int accumulate, void* ws, size_t ws_bytes,
+                     void* stream);
+
+/* Scoring: per row of logits x (rows x vocab), with one read of it, m = max_j x_j and log_sum = log sum_j exp(x_j - m),
+ *     log p_j = (x_j - m) - log_sum        entropy = -sum_j p_j log p_j
+ *     logprob = log p_target               (0 where the target is negative or >= vocab: none)
+ *     stats[2r] = m, stats[2r + 1] = log_sum
+ *     top_logprob[r*top + i], top_index[r*top + i], i < top: the `top` largest logits, largest first, of equal
+ *     ones (-0 equals +0) the lowest index first, as log p, and where they are
+ * target (int32) and logprob are NULL together; entropy and stats may be NULL; top_logprob and top_index
+ * are not used with top = 0 (top <= vocab, top <= QA_TOP_MAX).  Logits of -infinity have probability 0
+ * and add nothing.  A row of nothing but -infinity has stats -infinity and 0, entropy 0, logprob and
+ * top_logprob -infinity and the lowest indices; one of nothing but the type's lowest value is uniform.  A NaN
+ * or +infinity in a row makes its numbers NaN, m aside (for the order of top_index a NaN counts as -infinity).
+ * Few long rows are split over the device: ws of qa_token_workspace_bytes(rows, vocab, top) bytes, may be
+ * NULL if 0.  1 <= vocab < 2^31. */
+#define QA_TOP_MAX 64
+size_t qa_token_workspace_bytes(int64_t rows, int64_t vocab, int32_t top);
+int qa_token_logprob(int type, int64_t rows, int64_t vocab, const void* logits, int64_t stride,
+                     const int32_t* target_or_null, int32_t top, float* logprob_or_null,
+                     float* entropy_or_null, float* stats_or_null, float* top_logprob, int32_t* top_index,
+                     void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient of the logits from those of logprob and entropy (binary32, one per row; NULL counts as 0):
+ *     dx_j = g_logprob ([j = target] - p_j) - g_entropy p_j (log p_j + entropy)
+ * stats and entropy as qa_token_logprob wrote them (entropy and g_entropy NULL together); a row without
+ * target gets the entropy's part alone.  Logits of -infinity get 0 (and the target's g_logprob).
+ * dlogits (type `type`) may be the logits themselves, with their stride. */
+int qa_token_logprob_grad(int type, int64_t rows, int64_t vocab, const void* logits, int64_t stride,
+                          const int32_t* target_or_null, const float* stats, const float* entropy_or_null,
+                          const float* g_logprob_or_null, const float* g_entropy_or_null, void* dlogits,
+                          int64_t dlogits_stride, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

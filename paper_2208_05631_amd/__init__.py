@@ -14,5 +14,8 @@ from .binding import (  # noqa: F401
     qa_quantize_pack_segments, qa_step_qcmd_segments, qa_step_qrda_segments, qa_select_codes, qa_segment_plan_host,
     qa_step_qcmd_selected, qa_step_qrda_selected, qa_aggregate_quantize, qa_aggregate_quantize_selected,
     qa_quantize_pack_static,
+    QA_F32, QA_BF16, QA_F16, QA_OP_NORM_GRAD, QA_OP_WEIGHT_GRAD, QA_TOP_MAX, CodedRows, qa_rows_workspace_bytes,
+    qa_rows_pack, qa_rows_unpack, qa_rows_weight_grad, qa_rms_norm, qa_rms_norm_grad,
+    qa_token_workspace_bytes, qa_token_logprob, qa_token_logprob_grad,
 )
 from . import placement  # noqa: F401,E402  (where large arrays lie in device memory)

@@ -20,6 +20,9 @@ QA_OP_QUANTIZE, QA_OP_STEP, QA_OP_GRAD_CSR, QA_OP_GRAD_DENSE = 1, 2, 3, 4
 QA_OP_SELECT, QA_OP_STEP_SELECTED, QA_OP_QUANTIZE_EXACT = 5, 6, 7
 QA_DENSE, QA_CSR = 0, 1
 QA_METHOD_QCMD, QA_METHOD_QRDA = 0, 1
+QA_F32, QA_BF16, QA_F16 = 0, 1, 2
+QA_OP_NORM_GRAD, QA_OP_WEIGHT_GRAD = 8, 9
+QA_TOP_MAX = 64
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -62,6 +65,18 @@ class Layout(C.Structure):
     @property
     def n_buckets(self):
         return (self.d + self.bucket - 1) // self.bucket if self.bucket else 1
+
+
+class CodedRows(C.Structure):
+    """Mirror of qa_coded_rows."""
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("group", C.c_int32),
+                ("code_stride", C.c_int64), ("scale_stride", C.c_int64)]
+
+    @staticmethod
+    def make(rows, cols, group=32, code_stride=None, scale_stride=None):
+        """Rows of codes padded to 16 bytes, rows of scales without padding."""
+        return CodedRows(rows, cols, group, code_stride or (cols + 15) // 16 * 16,
+                         scale_stride or (cols + group - 1) // group)
 
 
 class SegmentPlan(C.Structure):
@@ -127,6 +142,19 @@ _lib.qa_aggregate_quantize_selected.argtypes = [C.POINTER(Layout), _vp, C.c_int6
                                                 _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.qa_segment_plan_host.argtypes = [C.c_int64, C.c_int64, C.POINTER(C.c_int64), C.POINTER(C.c_int64),
                                       C.POINTER(C.c_int64), _sz, C.POINTER(C.c_int64)]
+_i64, _i32, _f32, _rows = C.c_int64, C.c_int32, C.c_float, C.POINTER(CodedRows)
+_lib.qa_rows_workspace_bytes.restype = _sz
+_lib.qa_rows_workspace_bytes.argtypes = [_rows, C.c_int, C.c_int, _i64]
+_lib.qa_rows_pack.argtypes = [_rows, C.c_int, _vp, _i64, _vp, _vp, _vp]
+_lib.qa_rows_unpack.argtypes = [_rows, _vp, _vp, C.c_int, _vp, _i64, _vp]
+_lib.qa_rows_weight_grad.argtypes = [_rows, _vp, _vp, C.c_int, _vp, _i64, _i64, _vp, _i64, C.c_int, _vp, _sz, _vp]
+_lib.qa_rms_norm.argtypes = [_rows, C.c_int, _vp, _i64, _vp, _i64, _vp, _f32, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _vp]
+_lib.qa_rms_norm_grad.argtypes = [_rows, C.c_int, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64,
+                                  _vp, C.c_int, _vp, _sz, _vp]
+_lib.qa_token_workspace_bytes.restype = _sz
+_lib.qa_token_workspace_bytes.argtypes = [_i64, _i64, _i32]
+_lib.qa_token_logprob.argtypes = [C.c_int, _i64, _i64, _vp, _i64, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.qa_token_logprob_grad.argtypes = [C.c_int, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]
 
 
 def _p(t):
@@ -327,3 +355,56 @@ def qa_segment_plan_host(d, begin, length):
                                      (C.c_int64 * max(n, 1))(*[int(v) for v in length]), table,
                                      nwords * 8, C.byref(npieces)), "qa_segment_plan_host")
     return npieces.value, list(table)
+
+
+def qa_rows_workspace_bytes(rows: CodedRows, op: int, type: int, n: int = 0) -> int:
+    return int(_lib.qa_rows_workspace_bytes(C.byref(rows), op, type, n))
+
+
+def qa_rows_pack(rows, type, x, x_stride, codes, scales, stream=None):
+    _check(_lib.qa_rows_pack(C.byref(rows), type, _p(x), x_stride, _p(codes), _p(scales), _stream(stream)),
+           "qa_rows_pack")
+
+
+def qa_rows_unpack(rows, codes, scales, type, x_out, x_stride, stream=None):
+    _check(_lib.qa_rows_unpack(C.byref(rows), _p(codes), _p(scales), type, _p(x_out), x_stride,
+                               _stream(stream)), "qa_rows_unpack")
+
+
+def qa_rows_weight_grad(rows, codes, scales, type, dy, dy_stride, n, dw, dw_stride, accumulate, ws, stream=None):
+    _check(_lib.qa_rows_weight_grad(C.byref(rows), _p(codes), _p(scales), type, _p(dy), dy_stride, n, _p(dw),
+                                    dw_stride, accumulate, _p(ws), _nbytes(ws), _stream(stream)),
+           "qa_rows_weight_grad")
+
+
+def qa_rms_norm(rows, type, x, x_stride, residual, residual_stride, weight, eps, h_out, h_stride, codes, scales,
+                y_out, y_stride, rstd, stream=None):
+    _check(_lib.qa_rms_norm(C.byref(rows), type, _p(x), x_stride, _p(residual), residual_stride, _p(weight), eps,
+                            _p(h_out), h_stride, _p(codes), _p(scales), _p(y_out), y_stride, _p(rstd),
+                            _stream(stream)), "qa_rms_norm")
+
+
+def qa_rms_norm_grad(rows, type, dy, dy_stride, h, h_stride, h_codes, h_scales, weight, rstd, dh, dh_stride, dx,
+                     dx_stride, dweight, accumulate, ws, stream=None):
+    _check(_lib.qa_rms_norm_grad(C.byref(rows), type, _p(dy), dy_stride, _p(h), h_stride, _p(h_codes),
+                                 _p(h_scales), _p(weight), _p(rstd), _p(dh), dh_stride, _p(dx), dx_stride,
+                                 _p(dweight), accumulate, _p(ws), _nbytes(ws), _stream(stream)),
+           "qa_rms_norm_grad")
+
+
+def qa_token_workspace_bytes(rows: int, vocab: int, top: int) -> int:
+    return int(_lib.qa_token_workspace_bytes(rows, vocab, top))
+
+
+def qa_token_logprob(type, rows, vocab, logits, stride, target, top, logprob, entropy, stats, top_logprob, top_index,
+                     ws, stream=None):
+    _check(_lib.qa_token_logprob(type, rows, vocab, _p(logits), stride, _p(target), top, _p(logprob), _p(entropy),
+                                 _p(stats), _p(top_logprob), _p(top_index), _p(ws), _nbytes(ws), _stream(stream)),
+           "qa_token_logprob")
+
+
+def qa_token_logprob_grad(type, rows, vocab, logits, stride, target, stats, entropy, g_logprob, g_entropy, dlogits,
+                          dlogits_stride, stream=None):
+    _check(_lib.qa_token_logprob_grad(type, rows, vocab, _p(logits), stride, _p(target), _p(stats), _p(entropy),
+                                      _p(g_logprob), _p(g_entropy), _p(dlogits), dlogits_stride,
+                                      _stream(stream)), "qa_token_logprob_grad")

@@ -1,0 +1,461 @@
+// Root-mean-square norm of a residual stream with an output in 8 bits, and its backward pass.
+#include <algorithm>
+
+#include "qa_rows.h"
+
+namespace qa {
+namespace {
+
+// A row is held in the registers of W waves, NV vectors of eight columns per lane: one read of everything.  Rows of
+// up to 1024 columns are a wave's own and need no barrier; four of them share a work-group.
+constexpr int kHeldCols = 16384;                   // 16 waves, two vectors per lane; longer rows are read twice
+
+__device__ __forceinline__ float wave_sum_f32(float v) {
+  v += as_f32((uint32_t)dpp_i32<kDppQuadXor1>((int)as_u32(v)));
+  v += as_f32((uint32_t)dpp_i32<kDppQuadXor2>((int)as_u32(v)));
+  v += as_f32((uint32_t)dpp_i32<kDppRowHalfMirror>((int)as_u32(v)));
+  v += as_f32((uint32_t)dpp_i32<kDppRowMirror>((int)as_u32(v)));
+  const int i = (int)as_u32(v);
+  return (as_f32((uint32_t)__builtin_amdgcn_readlane(i, 0)) + as_f32((uint32_t)__builtin_amdgcn_readlane(i, 16))) +
+         (as_f32((uint32_t)__builtin_amdgcn_readlane(i, 32)) + as_f32((uint32_t)__builtin_amdgcn_readlane(i, 48)));
+}
+// Sum over the W waves of a row.  `lds` holds W floats that no other call uses before the next barrier but one: the
+// callers alternate between two.
+template <int W>
+__device__ __forceinline__ float row_sum(float v, float* lds) {
+  v = wave_sum_f32(v);
+  if constexpr (W == 1) return v;
+  if ((threadIdx.x % kWave) == 0) lds[threadIdx.x / kWave] = v;
+  __syncthreads();
+  float s = lds[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) s += lds[w];
+  return s;
+}
+
+struct NormArgs {
+  qa_coded_rows R;
+  const void* x;
+  const void* residual;
+  const float* weight;
+  void* h;
+  int8_t* codes;
+  uint8_t* scales;
+  __bf16* y;
+  float* rstd;
+  int64_t x_stride, residual_stride, h_stride, y_stride;
+  float eps;
+};
+
+template <int W> constexpr int threads_of = W == 1 ? kThreads : W * kWave;
+template <int W> constexpr int rows_of = W == 1 ? kWaves : 1;
+
+// Codes and values of eight columns of y, which their lane and its neighbours of the same group hold.
+__device__ __forceinline__ void write_y(const NormArgs& A, int64_t row, int64_t col, int n, const float (&y)[kVec]) {
+  const int lanes = A.R.group / kVec;
+  const uint32_t b = scale_byte(lanes_max_u32(most_of(y), lanes));
+  if (n <= 0) return;
+  float value[kVec];
+  const u32x2 code = code8(y, b, value);
+  if (A.codes) {
+    store_codes(A.codes + row * A.R.code_stride + col, code, n);
+    if ((threadIdx.x % lanes) == 0) A.scales[row * A.R.scale_stride + col / A.R.group] = (uint8_t)b;
+  }
+  if (A.y) store_raw<QA_BF16>(A.y + row * A.y_stride + col, from_f32<QA_BF16>(value), n);
+}
+
+template <int TYPE, int W, int NV>
+__global__ __launch_bounds__(threads_of<W>) void rms_norm_kernel(NormArgs A) {
+  typedef ElemT<TYPE> T;
+  __shared__ float sums[2][W];
+  const int t = threadIdx.x % (W * kWave);
+  const int64_t step = (int64_t)gridDim.x * rows_of<W>;
+  int64_t col[NV];
+  int n[NV];
+  float w[NV][kVec];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    col[v] = ((int64_t)v * W * kWave + t) * kVec;
+    n[v] = (int)min((int64_t)kVec, A.R.cols - col[v]);
+    to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col[v], n[v]), w[v]);
+  }
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * rows_of<W> + (W == 1 ? threadIdx.x / kWave : 0); row < A.R.rows;
+       row += step) {
+    Raw8<TYPE> x[NV], r[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) x[v] = load_raw<TYPE>((const T*)A.x + row * A.x_stride + col[v], n[v]);
+    if (A.residual) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) r[v] = load_raw<TYPE>((const T*)A.residual + row * A.residual_stride + col[v], n[v]);
+    }
+    float h[NV][kVec], s = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      to_f32<TYPE>(x[v], h[v]);
+      if (A.residual) {
+        float more[kVec];
+        to_f32<TYPE>(r[v], more);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) h[v][i] += more[i];
+      }
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) s = __builtin_fmaf(h[v][i], h[v][i], s);
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<W>(s, sums[turn]) / (float)A.R.cols + A.eps);
+    turn ^= 1;
+    if (A.rstd && t == 0) A.rstd[row] = rstd;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (A.h && n[v] > 0) store_raw<TYPE>((T*)A.h + row * A.h_stride + col[v], from_f32<TYPE>(h[v]), n[v]);
+      float y[kVec];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) y[i] = (h[v][i] * rstd) * w[v][i];
+      write_y(A, row, col[v], n[v], y);
+    }
+  }
+}
+
+// Rows that registers do not hold: 16 waves per row, x and residual read twice.  A lane writes h where it has itself
+// read x and residual for the last time, so h may be either of them.
+template <int TYPE>
+__global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs A) {
+  typedef ElemT<TYPE> T;
+  __shared__ float sums[2][16];
+  int turn = 0;
+  const int64_t pieces = ceil_div(A.R.cols, (int64_t)1024 * kVec);
+  for (int64_t row = blockIdx.x; row < A.R.rows; row += gridDim.x) {
+    const T* x = (const T*)A.x + row * A.x_stride;
+    const T* r = A.residual ? (const T*)A.residual + row * A.residual_stride : nullptr;
+    auto stream = [&](int64_t col, int n, float (&h)[kVec]) {
+      to_f32<TYPE>(load_raw<TYPE>(x + col, n), h);
+      if (r) {
+        float more[kVec];
+        to_f32<TYPE>(load_raw<TYPE>(r + col, n), more);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) h[i] += more[i];
+      }
+    };
+    float s = 0.0f;
+    for (int64_t p = 0; p < pieces; ++p) {
+      const int64_t col = (p * 1024 + threadIdx.x) * kVec;
+      float h[kVec];
+      stream(col, (int)min((int64_t)kVec, A.R.cols - col), h);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) s = __builtin_fmaf(h[i], h[i], s);
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<16>(s, sums[turn]) / (float)A.R.cols + A.eps);
+    turn ^= 1;
+    if (A.rstd && threadIdx.x == 0) A.rstd[row] = rstd;
+    for (int64_t p = 0; p < pieces; ++p) {
+      const int64_t col = (p * 1024 + threadIdx.x) * kVec;
+      const int n = (int)min((int64_t)kVec, A.R.cols - col);
+      float h[kVec], w[kVec], y[kVec];
+      stream(col, n, h);
+      to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col, n), w);
+      if (A.h && n > 0) store_raw<TYPE>((T*)A.h + row * A.h_stride + col, from_f32<TYPE>(h), n);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) y[i] = (h[i] * rstd) * w[i];
+      write_y(A, row, col, n, y);
+    }
+  }
+}
+
+// ---- backward ----------------------------------------------------------------------------------------------
+
+struct NormGradArgs {
+  qa_coded_rows R;
+  const void* dy;
+  const void* h;
+  const int8_t* codes;
+  const uint8_t* scales;
+  const float* weight;
+  const float* rstd;
+  const void* dh;
+  void* dx;
+  float* parts;                                    // sums over the rows of one work-group or wave; NULL: not wanted
+  int64_t dy_stride, h_stride, dh_stride, dx_stride;
+};
+
+// Eight columns of the residual stream, from its own type or from codes.
+template <int TYPE, bool CODED>
+__device__ __forceinline__ void load_h(const NormGradArgs& A, int64_t row, int64_t col, int n, float (&h)[kVec]) {
+  if constexpr (CODED) {
+    if (n > 0) {
+      decode8(*reinterpret_cast<const u32x2*>(A.codes + row * A.R.code_stride + col),
+              A.scales[row * A.R.scale_stride + col / A.R.group], h);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) h[i] = i < n ? h[i] : 0.0f;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) h[i] = 0.0f;
+    }
+  } else {
+    to_f32<TYPE>(load_raw<TYPE>((const ElemT<TYPE>*)A.h + row * A.h_stride + col, n), h);
+  }
+}
+
+template <int TYPE, int W, int NV, bool CODED>
+__global__ __launch_bounds__(threads_of<W>) void rms_norm_grad_kernel(NormGradArgs A) {
+  typedef ElemT<TYPE> T;
+  __shared__ float sums[2][W];
+  const int t = threadIdx.x % (W * kWave);
+  const int64_t first = (int64_t)blockIdx.x * rows_of<W> + (W == 1 ? threadIdx.x / kWave : 0);
+  int64_t col[NV];
+  int n[NV];
+  float w[NV][kVec], dw[NV][kVec];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    col[v] = ((int64_t)v * W * kWave + t) * kVec;
+    n[v] = (int)min((int64_t)kVec, A.R.cols - col[v]);
+    to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col[v], n[v]), w[v]);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) dw[v][i] = 0.0f;
+  }
+  int turn = 0;
+  for (int64_t row = first; row < A.R.rows; row += (int64_t)gridDim.x * rows_of<W>) {
+    Raw8<TYPE> dy_raw[NV], dh_raw[NV];
+    float h[NV][kVec];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      dy_raw[v] = load_raw<TYPE>((const T*)A.dy + row * A.dy_stride + col[v], n[v]);
+      load_h<TYPE, CODED>(A, row, col[v], n[v], h[v]);
+    }
+    if (A.dh) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) dh_raw[v] = load_raw<TYPE>((const T*)A.dh + row * A.dh_stride + col[v], n[v]);
+    }
+    const float rstd = A.rstd[row];
+    float s = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float dy[kVec];
+      to_f32<TYPE>(dy_raw[v], dy);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        h[v][i] *= rstd;                           // n
+        s = __builtin_fmaf(dy[i] * w[v][i], h[v][i], s);
+        dw[v][i] = __builtin_fmaf(dy[i], h[v][i], dw[v][i]);
+      }
+    }
+    const float c = row_sum<W>(s, sums[turn]) / (float)A.R.cols;
+    turn ^= 1;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float dy[kVec], dx[kVec];
+      to_f32<TYPE>(dy_raw[v], dy);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) dx[i] = rstd * (dy[i] * w[v][i] - h[v][i] * c);
+      if (A.dh) {
+        float dh[kVec];
+        to_f32<TYPE>(dh_raw[v], dh);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) dx[i] += dh[i];
+      }
+      if (n[v] > 0) store_raw<TYPE>((T*)A.dx + row * A.dx_stride + col[v], from_f32<TYPE>(dx), n[v]);
+    }
+  }
+  if (A.parts && first < A.R.rows) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+      if (n[v] > 0) store_raw<QA_F32>(A.parts + first * A.R.cols + col[v], from_f32<QA_F32>(dw[v]), n[v]);
+  }
+}
+
+// Rows that registers do not hold: everything is read twice, and a work-group's sums lie in the workspace.
+template <int TYPE, bool CODED>
+__global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(NormGradArgs A) {
+  typedef ElemT<TYPE> T;
+  __shared__ float sums[2][16];
+  int turn = 0;
+  const int64_t pieces = ceil_div(A.R.cols, (int64_t)1024 * kVec);
+  for (int64_t row = blockIdx.x; row < A.R.rows; row += gridDim.x) {
+    const T* dy_row = (const T*)A.dy + row * A.dy_stride;
+    const float rstd = A.rstd[row];
+    float s = 0.0f;
+    for (int64_t p = 0; p < pieces; ++p) {
+      const int64_t col = (p * 1024 + threadIdx.x) * kVec;
+      const int n = (int)min((int64_t)kVec, A.R.cols - col);
+      float dy[kVec], h[kVec], w[kVec];
+      to_f32<TYPE>(load_raw<TYPE>(dy_row + col, n), dy);
+      load_h<TYPE, CODED>(A, row, col, n, h);
+      to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col, n), w);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) s = __builtin_fmaf(dy[i] * w[i], h[i] * rstd, s);
+    }
+    const float c = row_sum<16>(s, sums[turn]) / (float)A.R.cols;
+    turn ^= 1;
+    for (int64_t p = 0; p < pieces; ++p) {
+      const int64_t col = (p * 1024 + threadIdx.x) * kVec;
+      const int n = (int)min((int64_t)kVec, A.R.cols - col);
+      if (n <= 0) continue;
+      float dy[kVec], h[kVec], w[kVec], dw[kVec], dx[kVec];
+      to_f32<TYPE>(load_raw<TYPE>(dy_row + col, n), dy);
+      load_h<TYPE, CODED>(A, row, col, n, h);
+      to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col, n), w);
+      float* part = A.parts ? A.parts + (int64_t)blockIdx.x * A.R.cols + col : nullptr;
+      if (part && row != blockIdx.x) {
+        to_f32<QA_F32>(load_raw<QA_F32>(part, n), dw);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) dw[i] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float v = h[i] * rstd;
+        dw[i] = __builtin_fmaf(dy[i], v, dw[i]);
+        dx[i] = rstd * (dy[i] * w[i] - v * c);
+      }
+      if (part) store_raw<QA_F32>(part, from_f32<QA_F32>(dw), n);
+      if (A.dh) {
+        float dh[kVec];
+        to_f32<TYPE>(load_raw<TYPE>((const T*)A.dh + row * A.dh_stride + col, n), dh);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) dx[i] += dh[i];
+      }
+      store_raw<TYPE>((T*)A.dx + row * A.dx_stride + col, from_f32<TYPE>(dx), n);
+    }
+  }
+}
+
+// dweight from the sums of the work-groups, in their order: 64 columns per work-group, the parts split over its waves.
+__global__ __launch_bounds__(1024) void norm_weight_kernel(const float* __restrict__ parts, int64_t n_parts, int64_t cols,
+                                                           float* __restrict__ dweight, int accumulate) {
+  __shared__ float sums[16][kWave];
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int64_t col = (int64_t)blockIdx.x * kWave + lane;
+  float s = 0.0f;
+  if (col < cols) {
+    const int64_t i0 = n_parts * wave / 16, i1 = n_parts * (wave + 1) / 16;
+#pragma unroll 16
+    for (int64_t i = i0; i < i1; ++i) s += parts[i * cols + col];
+  }
+  sums[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && col < cols) {
+    s = sums[0][lane];
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += sums[w][lane];
+    dweight[col] = accumulate ? dweight[col] + s : s;
+  }
+}
+
+// ---- which form -----------------------------------------------------------------------------------------------
+
+// Waves per row (0: the row is read twice) and vectors per lane.
+struct Form { int waves, vecs; };
+Form form_of(int64_t cols) {
+  if (cols <= 512) return {1, 1};
+  if (cols <= 1024) return {1, 2};
+  if (cols <= 2048) return {4, 1};
+  if (cols <= 4096) return {4, 2};
+  if (cols <= 8192) return {8, 2};
+  if (cols <= kHeldCols) return {16, 2};
+  return {0, 0};
+}
+// Work-groups: 16 waves per compute unit.
+int64_t groups_for(int64_t rows, Form f) {
+  const int64_t per_group = f.waves == 1 ? kWaves : 1, waves = f.waves == 1 ? kWaves : f.waves ? f.waves : 16;
+  return std::min<int64_t>(ceil_div(rows, per_group), 256 * 16 / waves);
+}
+int64_t parts_for(int64_t rows, Form f) {
+  return f.waves == 1 ? std::min<int64_t>(rows, groups_for(rows, f) * kWaves) : groups_for(rows, f);
+}
+
+template <int TYPE>
+int norm_launch(const NormArgs& A, hipStream_t stream) {
+  const Form f = form_of(A.R.cols);
+  const dim3 grid((unsigned)groups_for(A.R.rows, f));
+  if (f.waves == 1 && f.vecs == 1) rms_norm_kernel<TYPE, 1, 1><<<grid, threads_of<1>, 0, stream>>>(A);
+  else if (f.waves == 1) rms_norm_kernel<TYPE, 1, 2><<<grid, threads_of<1>, 0, stream>>>(A);
+  else if (f.waves == 4 && f.vecs == 1) rms_norm_kernel<TYPE, 4, 1><<<grid, threads_of<4>, 0, stream>>>(A);
+  else if (f.waves == 4) rms_norm_kernel<TYPE, 4, 2><<<grid, threads_of<4>, 0, stream>>>(A);
+  else if (f.waves == 8) rms_norm_kernel<TYPE, 8, 2><<<grid, threads_of<8>, 0, stream>>>(A);
+  else if (f.waves == 16) rms_norm_kernel<TYPE, 16, 2><<<grid, threads_of<16>, 0, stream>>>(A);
+  else rms_norm_long_kernel<TYPE><<<grid, 1024, 0, stream>>>(A);
+  return launch_status();
+}
+
+template <int TYPE, bool CODED>
+int norm_grad_launch(const NormGradArgs& A, float* dweight, int accumulate, hipStream_t stream) {
+  const Form f = form_of(A.R.cols);
+  const dim3 grid((unsigned)groups_for(A.R.rows, f));
+  if (A.R.rows > 0) {
+    if (f.waves == 1 && f.vecs == 1) rms_norm_grad_kernel<TYPE, 1, 1, CODED><<<grid, threads_of<1>, 0, stream>>>(A);
+    else if (f.waves == 1) rms_norm_grad_kernel<TYPE, 1, 2, CODED><<<grid, threads_of<1>, 0, stream>>>(A);
+    else if (f.waves == 4 && f.vecs == 1) rms_norm_grad_kernel<TYPE, 4, 1, CODED><<<grid, threads_of<4>, 0, stream>>>(A);
+    else if (f.waves == 4) rms_norm_grad_kernel<TYPE, 4, 2, CODED><<<grid, threads_of<4>, 0, stream>>>(A);
+    else if (f.waves == 8) rms_norm_grad_kernel<TYPE, 8, 2, CODED><<<grid, threads_of<8>, 0, stream>>>(A);
+    else if (f.waves == 16) rms_norm_grad_kernel<TYPE, 16, 2, CODED><<<grid, threads_of<16>, 0, stream>>>(A);
+    else rms_norm_grad_long_kernel<TYPE, CODED><<<grid, 1024, 0, stream>>>(A);
+    if (const int rc = launch_status()) return rc;
+  }
+  if (!dweight) return QA_OK;
+  norm_weight_kernel<<<dim3((unsigned)ceil_div(A.R.cols, kWave)), 1024, 0, stream>>>(
+      A.parts, parts_for(A.R.rows, f), A.R.cols, dweight, accumulate);
+  return launch_status();
+}
+template <int TYPE>
+int norm_grad_launch(const NormGradArgs& A, float* dweight, int accumulate, hipStream_t stream) {
+  return A.codes ? norm_grad_launch<TYPE, true>(A, dweight, accumulate, stream)
+                 : norm_grad_launch<TYPE, false>(A, dweight, accumulate, stream);
+}
+
+}  // namespace
+
+size_t rms_norm_grad_workspace_bytes(const qa_coded_rows* R, int) {
+  return (size_t)parts_for(R->rows, form_of(R->cols)) * (size_t)R->cols * sizeof(float);
+}
+
+}  // namespace qa
+
+using namespace qa;
+
+extern "C" int qa_rms_norm(const qa_coded_rows* rows, int type, const void* x, int64_t x_stride,
+                           const void* residual, int64_t residual_stride, const float* weight, float eps,
+                           void* h_out, int64_t h_stride, int8_t* codes, uint8_t* scales, void* y_out,
+                           int64_t y_stride, float* rstd, void* stream) {
+  if (const int rc = check_rows(rows)) return rc;
+  if (!known_type(type) || x_stride < rows->cols || (residual && residual_stride < rows->cols) ||
+      (h_out && h_stride < rows->cols) || (y_out && y_stride < rows->cols) || !(eps >= 0.0f) || !(eps < 1e30f))
+    return QA_ERR_INVALID_ARG;
+  if (rows->rows == 0) return QA_OK;
+  if (!x || !weight || !codes != !scales || (!codes && !y_out)) return QA_ERR_INVALID_ARG;
+  if (!element_aligned(x, type) || !element_aligned(residual, type) || !element_aligned(h_out, type) ||
+      !aligned(y_out, 2) || !aligned(weight, 4) || !aligned(rstd, 4) || !aligned(codes, 16))
+    return QA_ERR_ALIGNMENT;
+  const NormArgs A{*rows, x, residual, weight, h_out, codes, scales, (__bf16*)y_out, rstd,
+                   x_stride, residual_stride, h_stride, y_stride, eps};
+  const hipStream_t s = (hipStream_t)stream;
+  if (type == QA_F32) return norm_launch<QA_F32>(A, s);
+  if (type == QA_BF16) return norm_launch<QA_BF16>(A, s);
+  return norm_launch<QA_F16>(A, s);
+}
+
+extern "C" int qa_rms_norm_grad(const qa_coded_rows* rows, int type, const void* dy, int64_t dy_stride, const void* h,
+                                int64_t h_stride, const int8_t* h_codes, const uint8_t* h_scales,
+                                const float* weight, const float* rstd, const void* dh, int64_t dh_stride, void* dx,
+                                int64_t dx_stride, float* dweight, int accumulate, void* ws, size_t ws_bytes,
+                                void* stream) {
+  if (const int rc = check_rows(rows)) return rc;
+  if (!known_type(type) || dy_stride < rows->cols || (h && h_stride < rows->cols) ||
+      (dh && dh_stride < rows->cols) || dx_stride < rows->cols || (accumulate != 0 && accumulate != 1))
+    return QA_ERR_INVALID_ARG;
+  if (!aligned(dweight, 4)) return QA_ERR_ALIGNMENT;
+  if (rows->rows > 0) {
+    if (!dy || !weight || !rstd || !dx || !h == !h_codes || !h_codes != !h_scales) return QA_ERR_INVALID_ARG;
+    if (!element_aligned(dy, type) || !element_aligned(h, type) || !element_aligned(dh, type) ||
+        !element_aligned(dx, type) || !aligned(weight, 4) || !aligned(rstd, 4) || !aligned(h_codes, 16))
+      return QA_ERR_ALIGNMENT;
+    if (dweight && (!ws || ws_bytes < rms_norm_grad_workspace_bytes(rows, type))) return QA_ERR_WORKSPACE;
+    if (dweight && !aligned(ws, 256)) return QA_ERR_ALIGNMENT;
+  } else if (!dweight || accumulate) {
+    return QA_OK;
+  }
+  const NormGradArgs A{*rows, dy, h, h_codes, h_scales, weight, rstd, dh, dx, dweight ? (float*)ws : nullptr,
+                       dy_stride, h_stride, dh_stride, dx_stride};
+  const hipStream_t s = (hipStream_t)stream;
+  if (type == QA_F32) return norm_grad_launch<QA_F32>(A, dweight, accumulate, s);
+  if (type == QA_BF16) return norm_grad_launch<QA_BF16>(A, dweight, accumulate, s);
+  return norm_grad_launch<QA_F16>(A, dweight, accumulate, s);
+}

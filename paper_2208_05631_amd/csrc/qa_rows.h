@@ -1,0 +1,216 @@
+// Rows of activations: loads and stores of eight elements of any type at any alignment, and the 8-bit code of a
+// group of columns.  Shared by the kernels on activations; not part of the public interface.
+#pragma once
+#include "qa_common.h"
+
+namespace qa {
+
+inline bool known_type(int type) { return type == QA_F32 || type == QA_BF16 || type == QA_F16; }
+inline int64_t type_bytes(int type) { return type == QA_F32 ? 4 : 2; }
+inline bool element_aligned(const void* p, int type) { return aligned(p, (size_t)type_bytes(type)); }
+inline int64_t groups_of(const qa_coded_rows* R) { return (R->cols + R->group - 1) / R->group; }
+constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+inline int check_rows(const qa_coded_rows* R) {
+  if (!R) return QA_ERR_INVALID_ARG;
+  if (R->rows < 0 || R->rows >= (int64_t(1) << 31)) return QA_ERR_INVALID_ARG;
+  if (R->cols < 1 || R->cols >= (int64_t(1) << 24)) return QA_ERR_INVALID_ARG;
+  if (R->group != 32 && R->group != 64 && R->group != 128) return QA_ERR_INVALID_ARG;
+  if (R->code_stride < R->cols || R->code_stride % 16) return QA_ERR_INVALID_ARG;
+  if (R->scale_stride < groups_of(R)) return QA_ERR_INVALID_ARG;
+  return QA_OK;
+}
+
+#if defined(__HIPCC__)
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+// The same at an element's alignment: rows of odd strides are read and written 16 bytes at a time all the same,
+// which the memory pipeline does at any byte address.
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
+
+constexpr int kVec = 8;                            // elements that a lane holds side by side
+
+template <int TYPE> struct Elem;
+template <> struct Elem<QA_F32> { typedef float T; };
+template <> struct Elem<QA_BF16> { typedef __bf16 T; };
+template <> struct Elem<QA_F16> { typedef _Float16 T; };
+template <int TYPE> using ElemT = typename Elem<TYPE>::T;
+
+__device__ __forceinline__ float as_f32(uint32_t u) { return __uint_as_float(u); }
+__device__ __forceinline__ uint32_t as_u32(float f) { return __float_as_uint(f); }
+
+// Eight elements as they lie in memory: registers of a load that is still on its way.
+template <int TYPE> struct Raw8 { u32x4 a; };
+template <> struct Raw8<QA_F32> { f32x4 a, b; };
+
+template <int TYPE>
+__device__ __forceinline__ Raw8<TYPE> load_raw(const ElemT<TYPE>* p) {
+  Raw8<TYPE> r;
+  if constexpr (TYPE == QA_F32) {
+    r.a = *reinterpret_cast<const f32x4_at4*>(p);
+    r.b = *reinterpret_cast<const f32x4_at4*>(p + 4);
+  } else {
+    r.a = *reinterpret_cast<const u32x4_at2*>(p);
+  }
+  return r;
+}
+// The first n of eight elements, the others `rest`.
+template <int TYPE>
+__device__ __forceinline__ Raw8<TYPE> load_raw(const ElemT<TYPE>* p, int n, float rest = 0.0f) {
+  if (n >= kVec) return load_raw<TYPE>(p);
+  ElemT<TYPE> v[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) v[i] = i < n ? p[i] : (ElemT<TYPE>)rest;
+  Raw8<TYPE> r;
+  __builtin_memcpy(&r, v, sizeof r);
+  return r;
+}
+template <int TYPE>
+__device__ __forceinline__ void to_f32(const Raw8<TYPE>& r, float (&v)[kVec]) {
+  if constexpr (TYPE == QA_F32) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = r.a[i]; v[4 + i] = r.b[i]; }
+  } else if constexpr (TYPE == QA_BF16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = as_f32(r.a[i] << 16); v[2 * i + 1] = as_f32(r.a[i] & 0xFFFF0000u); }
+  } else {
+    _Float16 h[kVec];
+    __builtin_memcpy(h, &r, sizeof h);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = (float)h[i];
+  }
+}
+// Rounded once, to nearest and ties to even.
+template <int TYPE>
+__device__ __forceinline__ Raw8<TYPE> from_f32(const float (&v)[kVec]) {
+  Raw8<TYPE> r;
+  if constexpr (TYPE == QA_F32) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { r.a[i] = v[i]; r.b[i] = v[4 + i]; }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x2 two = {v[2 * i], v[2 * i + 1]};
+      if constexpr (TYPE == QA_BF16)
+        r.a[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+      else
+        r.a[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, f16x2));
+    }
+  }
+  return r;
+}
+template <int TYPE>
+__device__ __forceinline__ void store_raw(ElemT<TYPE>* p, const Raw8<TYPE>& r, int n = kVec) {
+  if (n >= kVec) {
+    if constexpr (TYPE == QA_F32) {
+      *reinterpret_cast<f32x4_at4*>(p) = r.a;
+      *reinterpret_cast<f32x4_at4*>(p + 4) = r.b;
+    } else {
+      *reinterpret_cast<u32x4_at2*>(p) = r.a;
+    }
+    return;
+  }
+  ElemT<TYPE> v[kVec];
+  __builtin_memcpy(v, &r, sizeof v);
+#pragma unroll
+  for (int i = 0; i < kVec; ++i)
+    if (i < n) p[i] = v[i];
+}
+
+// ---- the 8-bit code of a group of columns -----------------------------------------------------------------
+//
+// A group has one byte b, its scale is 2^(b - 127): the smallest power of two by which the group's largest magnitude
+// is at most 127, and 2^-126 at least.  A code is the nearest whole multiple, ties to even.  The scale is a power of
+// two because a code times one has at most seven significant bits: it is exact in bfloat16, and matrix instructions
+// that read the codes multiply exactly what the forward pass used.  It costs up to one of the eight bits.  A group
+// with an infinity or a NaN has b = 255 and codes 0, and every value of it is read back as NaN.  At the largest scale
+// that a finite magnitude needs, 2^122, codes end at 63: 64 would be 2^128.
+
+constexpr uint32_t kNoScale = 255, kLargestScale = 249;
+
+// b from the bits of the largest magnitude (1.984375 = 127 / 64 is the largest mantissa that still fits 127).
+__device__ __forceinline__ uint32_t scale_byte(uint32_t most) {
+  if (most >= 0x7F800000u) return kNoScale;
+  const int b = (int)((most + 0x1FFFFu) >> 23) - 6;
+  return (uint32_t)(b > 1 ? b : 1);
+}
+// Infinity for a group without values: 0 times it is the NaN that they are read back as.
+__device__ __forceinline__ float scale_of(uint32_t b) { return as_f32(b << 23); }
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v) {
+  const uint32_t o = (uint32_t)dpp_i32<CTRL>((int)v);
+  return v > o ? v : o;
+}
+// The largest of `lanes` (4, 8 or 16) aligned neighbours' values.
+__device__ __forceinline__ uint32_t lanes_max_u32(uint32_t v, int lanes) {
+  v = dpp_max_u32<kDppQuadXor1>(v);
+  v = dpp_max_u32<kDppQuadXor2>(v);
+  if (lanes > 4) v = dpp_max_u32<kDppRowHalfMirror>(v);
+  if (lanes > 8) v = dpp_max_u32<kDppRowMirror>(v);
+  return v;
+}
+__device__ __forceinline__ uint32_t most_of(const float (&v)[kVec]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const uint32_t a = as_u32(v[i]) & 0x7FFFFFFFu;
+    m = m > a ? m : a;
+  }
+  return m;
+}
+
+// Codes of eight values as bytes of two words, and the values that they stand for.  1.5 * 2^23 added to a value
+// below 2^22 leaves its nearest whole number, ties to even, in the low bits; the product in front is exact.
+__device__ __forceinline__ u32x2 code8(const float (&v)[kVec], uint32_t b, float (&value)[kVec]) {
+  constexpr float kWhole = 12582912.0f;
+  const float inverse = as_f32((254u - b) << 23), scale = scale_of(b);
+  uint32_t w[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const float r = __builtin_fmaf(v[i], inverse, kWhole);
+    w[i] = as_u32(r);
+    value[i] = (r - kWhole) * scale;
+  }
+  u32x2 code;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t lo = __builtin_amdgcn_perm(w[4 * k + 1], w[4 * k], 0x0C0C0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(w[4 * k + 3], w[4 * k + 2], 0x04000C0Cu);
+    code[k] = lo | hi;
+  }
+  if (b >= kLargestScale) {                        // rare
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      const int whole = b == kNoScale ? 0 : max(-63, min(63, (int)(int8_t)w[i]));
+      code[i / 4] = (code[i / 4] & ~(0xFFu << (8 * (i % 4)))) | (uint32_t)(uint8_t)whole << (8 * (i % 4));
+      value[i] = b == kNoScale ? __builtin_nanf("") : (float)whole * scale;
+    }
+  }
+  return code;
+}
+__device__ __forceinline__ void decode8(u32x2 code, uint32_t b, float (&v)[kVec]) {
+  const float scale = scale_of(b);
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) v[i] = (float)(int8_t)(code[i / 4] >> (8 * (i % 4))) * scale;
+}
+// The first n of eight codes; rows begin on 16 bytes, so that eight always have their place.
+__device__ __forceinline__ void store_codes(int8_t* p, u32x2 code, int n) {
+  if (n >= kVec) {
+    *reinterpret_cast<u32x2*>(p) = code;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kVec; ++i)
+    if (i < n) p[i] = (int8_t)(code[i / 4] >> (8 * (i % 4)));
+}
+
+#endif  // __HIPCC__
+
+}  // namespace qa

@@ -1,0 +1,493 @@
+// Log probabilities of given tokens, entropy and the most likely alternatives, and the logits' gradient.
+#include <algorithm>
+#include <cfloat>
+
+#include "qa_rows.h"
+
+namespace qa {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kFar = -1e4f;                      // 2^kFar is 0
+constexpr int kTop = QA_TOP_MAX;                   // a lane for each alternative
+static_assert(kTop == kWave, "the alternatives of a row are held one per lane");
+
+__device__ __forceinline__ float wave_sum_f32(float v) {
+  v += as_f32((uint32_t)dpp_i32<kDppQuadXor1>((int)as_u32(v)));
+  v += as_f32((uint32_t)dpp_i32<kDppQuadXor2>((int)as_u32(v)));
+  v += as_f32((uint32_t)dpp_i32<kDppRowHalfMirror>((int)as_u32(v)));
+  v += as_f32((uint32_t)dpp_i32<kDppRowMirror>((int)as_u32(v)));
+  const int i = (int)as_u32(v);
+  return (as_f32((uint32_t)__builtin_amdgcn_readlane(i, 0)) + as_f32((uint32_t)__builtin_amdgcn_readlane(i, 16))) +
+         (as_f32((uint32_t)__builtin_amdgcn_readlane(i, 32)) + as_f32((uint32_t)__builtin_amdgcn_readlane(i, 48)));
+}
+__device__ __forceinline__ float wave_max_f32(float v) {
+  v = fmaxf(v, as_f32((uint32_t)dpp_i32<kDppQuadXor1>((int)as_u32(v))));
+  v = fmaxf(v, as_f32((uint32_t)dpp_i32<kDppQuadXor2>((int)as_u32(v))));
+  v = fmaxf(v, as_f32((uint32_t)dpp_i32<kDppRowHalfMirror>((int)as_u32(v))));
+  v = fmaxf(v, as_f32((uint32_t)dpp_i32<kDppRowMirror>((int)as_u32(v))));
+  const int i = (int)as_u32(v);
+  return fmaxf(fmaxf(as_f32((uint32_t)__builtin_amdgcn_readlane(i, 0)), as_f32((uint32_t)__builtin_amdgcn_readlane(i, 16))),
+               fmaxf(as_f32((uint32_t)__builtin_amdgcn_readlane(i, 32)), as_f32((uint32_t)__builtin_amdgcn_readlane(i, 48))));
+}
+
+// ---- sums of a softmax -----------------------------------------------------------------------------------------
+//
+// With m the largest logit so far: s = sum of 2^t and w = sum of 2^t t, t = (x - m) log2 e.  Then log p = (x - m) -
+// log s and entropy = log s - ln2 w / s; both terms of the entropy are >= 0, nothing cancels.
+// m is -FLT_MAX at least, so that -infinity has t = -infinity and adds nothing; in the product t is kFar at least.
+struct Sums { float m, s, w; };
+__device__ __forceinline__ Sums no_sums() { return {-FLT_MAX, 0.0f, 0.0f}; }
+
+// The same sums against another maximum.
+__device__ __forceinline__ void raise(Sums& a, float m) {
+  const float t = fmaxf((a.m - m) * kLog2e, kFar), f = __builtin_amdgcn_exp2f(t);
+  a.w = (a.w + a.s * t) * f;
+  a.s *= f;
+  a.m = m;
+}
+// Sums over the lanes of a wave, each with a maximum of its own.
+__device__ __forceinline__ Sums over_lanes(Sums a) {
+  raise(a, wave_max_f32(a.m));
+  a.s = wave_sum_f32(a.s);
+  a.w = wave_sum_f32(a.w);
+  return a;
+}
+
+// ---- alternatives ------------------------------------------------------------------------------------------------
+//
+// A logit and its place are one whole number: the logit's bits in an order that whole numbers have, above the place's
+// complement, so that the larger number is the better alternative and no two are equal.  A NaN counts as -infinity.
+__device__ __forceinline__ uint32_t ordered(float x) {
+  if (x != x) return 0x007FFFFFu;
+  const uint32_t u = as_u32(x + 0.0f);             // -0 to +0
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_ordered(uint32_t o) {
+  return as_f32(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+}
+__device__ __forceinline__ uint64_t key_of(uint32_t order, uint32_t index) { return (uint64_t)order << 32 | (uint32_t)~index; }
+
+template <typename U>
+__device__ __forceinline__ U other_lane(U v, int mask) { return __shfl_xor(v, mask, kWave); }
+template <typename U>
+__device__ __forceinline__ U merge_step(U v, int stride, bool larger) {
+  const U o = other_lane(v, stride);
+  return (v > o) == larger ? v : o;
+}
+// The wave's 64 values, the largest in lane 0.
+template <typename U>
+__device__ __forceinline__ U sort_lanes(U v) {
+  const int lane = threadIdx.x % kWave;
+#pragma unroll
+  for (int size = 2; size <= kWave; size *= 2)
+#pragma unroll
+    for (int stride = size / 2; stride >= 1; stride /= 2)
+      v = merge_step(v, stride, ((lane & stride) == 0) == ((lane & size) == 0));
+  return v;
+}
+// The 64 largest of two sorted sequences, sorted; `reversed` holds the second one's value 63 - lane.
+__device__ __forceinline__ uint64_t merge_lanes(uint64_t v, uint64_t reversed) {
+  const int lane = threadIdx.x % kWave;
+  v = v > reversed ? v : reversed;
+#pragma unroll
+  for (int stride = kWave / 2; stride >= 1; stride /= 2) v = merge_step(v, stride, (lane & stride) == 0);
+  return v;
+}
+__device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+
+// A wave's alternatives: sorted, and those that wait in LDS to be sorted in.
+struct Best {
+  uint64_t sorted = 0, last = 0;                   // last: the `top`-th, 0 while there are fewer
+  int waiting = 0;
+};
+constexpr int kWaiting = 2 * kWave;
+
+__device__ __forceinline__ void sort_in(Best& b, uint64_t* wait, int top) {
+  const int lane = threadIdx.x % kWave;
+  const uint64_t v = sort_lanes(lane < b.waiting ? wait[lane] : (uint64_t)0);
+  b.sorted = merge_lanes(b.sorted, __shfl(v, kWave - 1 - lane, kWave));
+  b.last = lane_u64(b.sorted, top - 1);
+  const int more = b.waiting - kWave;
+  if (more > 0) {
+    const uint64_t u = wait[kWave + lane];
+    __builtin_amdgcn_wave_barrier();
+    wait[lane] = u;
+    __builtin_amdgcn_wave_barrier();
+  }
+  b.waiting = more > 0 ? more : 0;
+}
+
+struct TokenArgs {
+  const void* x;
+  const int32_t* target;
+  float *logprob, *entropy, *stats, *top_logprob;
+  int32_t* top_index;
+  float* part_sums;                                // [row][split][4]: m, s, w
+  uint64_t* part_best;                             // [row][split][top]
+  int64_t rows, vocab, stride;
+  int64_t piece;                                   // logits of one split
+  int splits, top;
+};
+
+// What a row's sums and alternatives become.  `best` is lane i's alternative i; one wave writes.  Log probabilities are
+// (x - m) - log s: the difference of two logits first, which no rounding of m + log s comes into.
+template <int TYPE, bool TOP>
+__device__ __forceinline__ void write_row(const TokenArgs& A, int64_t row, const Sums& a, uint64_t best) {
+  const int lane = threadIdx.x % kWave;
+  const bool empty = a.s == 0.0f;
+  const float log_sum = empty ? 0.0f : kLn2 * __builtin_amdgcn_logf(a.s);
+  if (lane == 0) {
+    if (A.stats) {
+      A.stats[2 * row] = empty ? -INFINITY : a.m;
+      A.stats[2 * row + 1] = log_sum;
+    }
+    if (A.entropy) A.entropy[row] = empty ? 0.0f : log_sum - kLn2 * (a.w / a.s);
+    if (A.logprob) {
+      const int32_t y = A.target[row];
+      float p = 0.0f;
+      if (y >= 0 && y < A.vocab)
+        p = empty ? -INFINITY : ((float)((const ElemT<TYPE>*)A.x)[row * A.stride + y] - a.m) - log_sum;
+      A.logprob[row] = p;
+    }
+  }
+  if constexpr (TOP) {
+    if (lane < A.top) {
+      A.top_logprob[row * A.top + lane] = empty ? -INFINITY : (from_ordered((uint32_t)(best >> 32)) - a.m) - log_sum;
+      A.top_index[row * A.top + lane] = (int32_t)~(uint32_t)best;
+    }
+  }
+}
+
+// One wave's share of a row: chunks of NV vectors per lane, `chunk`, `chunk` + waves, ... of [begin, end).
+template <int TYPE, int NV, bool TOP>
+__device__ __forceinline__ void read_chunks(const ElemT<TYPE>* x, int64_t begin, int64_t end, int chunk, int waves, int top,
+                                            uint64_t* wait, uint32_t* shared, Sums& a, Best& b) {
+  const int lane = threadIdx.x % kWave;
+  constexpr int kChunk = NV * kWave * kVec;
+  bool cold = true;
+  for (int64_t at = begin + (int64_t)chunk * kChunk; at < end; at += (int64_t)waves * kChunk) {
+    float v[NV][kVec], vmax[NV], m = -INFINITY;
+    Raw8<TYPE> raw[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int64_t i = at + (k * kWave + lane) * kVec;
+      raw[k] = load_raw<TYPE>(x + i, (int)max((int64_t)0, min((int64_t)kVec, end - i)), -INFINITY);
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      to_f32<TYPE>(raw[k], v[k]);
+      vmax[k] = v[k][0];
+#pragma unroll
+      for (int i = 1; i < kVec; ++i) vmax[k] = fmaxf(vmax[k], v[k][i]);
+      m = fmaxf(m, vmax[k]);
+    }
+    const float most = wave_max_f32(m);
+    if (most > a.m) raise(a, most);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float t = (v[k][i] - a.m) * kLog2e, e = __builtin_amdgcn_exp2f(t);
+        a.s += e;
+        a.w = __builtin_fmaf(e, fmaxf(t, kFar), a.w);
+      }
+    if constexpr (TOP) {
+      // No alternative that is worse than `top` logits of any wave's can be one of the row's: in a wave's first chunk
+      // the lanes' largest are such logits, later its own alternatives, and the other waves share theirs.
+      uint32_t least = (uint32_t)(b.last >> 32);
+      if (cold) {
+        const uint32_t sorted = sort_lanes(ordered(m));
+        least = (uint32_t)__builtin_amdgcn_readlane((int)sorted, top - 1);
+      }
+      const uint32_t theirs = shared ? __hip_atomic_load(shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0u;
+      least = max(least, theirs);
+      const float bound = least ? from_ordered(least) : -INFINITY;
+      if (__any(!(m < bound))) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          if (!__any(!(vmax[k] < bound))) continue;
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) {
+            const uint32_t o = ordered(v[k][i]);
+            const uint64_t key = key_of(o, (uint32_t)(at + (k * kWave + lane) * kVec + i));
+            const bool good = o >= least && key > b.last;
+            const uint64_t mask = __ballot(good);
+            if (!mask) continue;
+            if (good) wait[b.waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key;
+            b.waiting += __popcll(mask);
+            __builtin_amdgcn_wave_barrier();
+            if (b.waiting >= kWave) sort_in(b, wait, top);
+          }
+        }
+      }
+      if (cold) {
+        cold = false;
+        sort_in(b, wait, top);
+        if (shared && lane == 0) atomicMax(shared, (uint32_t)(b.last >> 32));
+      }
+    }
+  }
+  if constexpr (TOP) {
+    if (b.waiting > 0) sort_in(b, wait, top);
+  }
+}
+
+// A wave per row, four rows per work-group.
+template <int TYPE, int NV, bool TOP>
+__global__ __launch_bounds__(kThreads) void token_narrow_kernel(TokenArgs A) {
+  __shared__ uint64_t wait[TOP ? kWaves : 1][kWaiting];
+  const int wave = threadIdx.x / kWave;
+  for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < A.rows; row += (int64_t)gridDim.x * kWaves) {
+    Sums a = no_sums();
+    Best b;
+    read_chunks<TYPE, NV, TOP>((const ElemT<TYPE>*)A.x + row * A.stride, 0, A.vocab, 0, 1, A.top, wait[TOP ? wave : 0], nullptr, a, b);
+    write_row<TYPE, TOP>(A, row, over_lanes(a), b.sorted);
+  }
+}
+
+constexpr int kTokenWaves = 8, kTokenThreads = kTokenWaves * kWave;
+
+// The row's (or the split's) sums and alternatives from its waves'; wave 0 receives them.
+template <bool TOP>
+__device__ __forceinline__ void over_waves(Sums& a, Best& b, Sums* sums, uint64_t (*lists)[kWave]) {
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  a = over_lanes(a);
+  if (lane == 0) sums[wave] = a;
+  if constexpr (TOP) {
+#pragma unroll
+    for (int w = 1; w < kTokenWaves; w *= 2) {
+      if ((wave & (2 * w - 1)) == w) lists[wave][kWave - 1 - lane] = b.sorted;
+      __syncthreads();
+      if ((wave & (2 * w - 1)) == 0) b.sorted = merge_lanes(b.sorted, lists[wave + w][lane]);
+    }
+  } else {
+    __syncthreads();
+  }
+  if (wave == 0) {
+    Sums each = no_sums();
+    if (lane < kTokenWaves) each = sums[lane];
+    a = over_lanes(each);
+  }
+  __syncthreads();
+}
+
+// A work-group per row, or per split of a row.
+template <int TYPE, int NV, bool TOP>
+__global__ __launch_bounds__(kTokenThreads) void token_wide_kernel(TokenArgs A) {
+  __shared__ uint64_t wait[TOP ? kTokenWaves : 1][kWaiting];
+  __shared__ uint64_t lists[TOP ? kTokenWaves : 1][kWave];
+  __shared__ Sums sums[kTokenWaves];
+  __shared__ uint32_t shared;
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int64_t begin = (int64_t)blockIdx.y * A.piece, end = min(A.vocab, begin + A.piece);
+  for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
+    if constexpr (TOP) {
+      if (threadIdx.x == 0) shared = 0;
+      __syncthreads();
+    }
+    Sums a = no_sums();
+    Best b;
+    read_chunks<TYPE, NV, TOP>((const ElemT<TYPE>*)A.x + row * A.stride, begin, end, wave, kTokenWaves, A.top,
+                               wait[TOP ? wave : 0], &shared, a, b);
+    over_waves<TOP>(a, b, sums, lists);
+    if (wave == 0) {
+      if (A.splits == 1) {
+        write_row<TYPE, TOP>(A, row, a, b.sorted);
+      } else {
+        const int64_t part = row * A.splits + blockIdx.y;
+        if (lane == 0) *reinterpret_cast<f32x4*>(A.part_sums + 4 * part) = f32x4{a.m, a.s, a.w, 0.0f};
+        if (TOP && lane < A.top) A.part_best[part * A.top + lane] = b.sorted;
+      }
+    }
+  }
+}
+
+// A row's splits put together.
+template <int TYPE, bool TOP>
+__global__ __launch_bounds__(kTokenThreads) void token_join_kernel(TokenArgs A) {
+  __shared__ uint64_t lists[TOP ? kTokenWaves : 1][kWave];
+  __shared__ Sums sums[kTokenWaves];
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
+    Sums a = no_sums();
+    Best b;
+    if ((int)threadIdx.x < A.splits) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(A.part_sums + 4 * (row * A.splits + threadIdx.x));
+      a.m = v[0];
+      a.s = v[1];
+      a.w = v[2];
+    }
+    if constexpr (TOP) {
+      for (int i = wave; i < A.splits; i += kTokenWaves) {
+        const int from = kWave - 1 - lane;
+        const uint64_t v = from < A.top ? A.part_best[(row * A.splits + i) * A.top + from] : 0;
+        if (__any(v > b.last)) {
+          b.sorted = merge_lanes(b.sorted, v);
+          b.last = lane_u64(b.sorted, A.top - 1);
+        }
+      }
+    }
+    over_waves<TOP>(a, b, sums, lists);
+    if (wave == 0) write_row<TYPE, TOP>(A, row, a, b.sorted);
+  }
+}
+
+// ---- gradient ----------------------------------------------------------------------------------------------------
+
+struct TokenGradArgs {
+  const void* x;
+  const int32_t* target;
+  const float *stats, *entropy, *g_logprob, *g_entropy;
+  void* dx;
+  int64_t rows, vocab, x_stride, dx_stride;
+};
+
+constexpr int kGradVecs = 4;
+constexpr int64_t kGradPiece = (int64_t)kGradVecs * kThreads * kVec;       // logits of a work-group at a time
+// dx_j = -p_j (a + e (log p_j + H)), and a more at the target.
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenGradArgs A) {
+  typedef ElemT<TYPE> T;
+  for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
+    const T* x = (const T*)A.x + row * A.x_stride;
+    T* dx = (T*)A.dx + row * A.dx_stride;
+    const int32_t y = A.target ? A.target[row] : -1;
+    const bool has = y >= 0 && y < A.vocab;
+    const float a = has && A.g_logprob ? A.g_logprob[row] : 0.0f;
+    const float e = A.g_entropy ? A.g_entropy[row] : 0.0f;
+    const float c = a + (A.g_entropy ? e * A.entropy[row] : 0.0f), e2 = e * kLn2;
+    const float m = fmaxf(A.stats[2 * row], -FLT_MAX), log_sum = A.stats[2 * row + 1];
+    for (int64_t first = (int64_t)blockIdx.y * kGradPiece; first < A.vocab; first += (int64_t)gridDim.y * kGradPiece) {
+      const int64_t lane0 = first + threadIdx.x * kVec;
+      Raw8<TYPE> raw[kGradVecs];
+#pragma unroll
+      for (int k = 0; k < kGradVecs; ++k) {
+        const int64_t i = lane0 + k * kThreads * kVec;
+        raw[k] = load_raw<TYPE>(x + i, (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i)));
+      }
+#pragma unroll
+      for (int k = 0; k < kGradVecs; ++k) {
+        const int64_t i = lane0 + k * kThreads * kVec;
+        const int n = (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i));
+        float v[kVec], d[kVec];
+        to_f32<TYPE>(raw[k], v);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+          const float t = ((v[j] - m) - log_sum) * kLog2e, p = __builtin_amdgcn_exp2f(t);
+          d[j] = -p * __builtin_fmaf(e2, fmaxf(t, kFar), c);
+        }
+        if (has && y >= i && y < i + kVec) {
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) d[j] += y - i == j ? a : 0.0f;
+        }
+        if (n > 0) store_raw<TYPE>(dx + i, from_f32<TYPE>(d), n);
+      }
+    }
+  }
+}
+
+// ---- which form ----------------------------------------------------------------------------------------------------
+
+constexpr int64_t kNarrow = 4096;                  // logits of a row that one wave reads
+constexpr int64_t kSplitLogits = kTokenThreads * kVec;       // one vector per lane
+
+int64_t splits_for(int64_t rows, int64_t vocab) {
+  if (vocab <= kNarrow || rows >= 512) return 1;
+  return std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), kTokenThreads), ceil_div(1024, rows));
+}
+
+template <int TYPE, bool TOP>
+int token_launch(TokenArgs& A, hipStream_t stream) {
+  const dim3 narrow((unsigned)std::min<int64_t>(ceil_div(A.rows, kWaves), 1 << 16));
+  if (A.vocab <= 512) {
+    token_narrow_kernel<TYPE, 1, TOP><<<narrow, kThreads, 0, stream>>>(A);
+  } else if (A.vocab <= kNarrow) {
+    token_narrow_kernel<TYPE, 4, TOP><<<narrow, kThreads, 0, stream>>>(A);
+  } else if (A.splits == 1) {
+    A.piece = A.vocab;
+    token_wide_kernel<TYPE, 4, TOP><<<dim3((unsigned)std::min<int64_t>(A.rows, 1 << 16)), kTokenThreads, 0, stream>>>(A);
+  } else {
+    A.piece = ceil_div(ceil_div(A.vocab, A.splits), kSplitLogits) * kSplitLogits;
+    const dim3 grid((unsigned)A.rows, (unsigned)A.splits);
+    token_wide_kernel<TYPE, 1, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
+    if (const int rc = launch_status()) return rc;
+    token_join_kernel<TYPE, TOP><<<dim3((unsigned)A.rows), kTokenThreads, 0, stream>>>(A);
+  }
+  return launch_status();
+}
+template <int TYPE>
+int token_launch(TokenArgs& A, hipStream_t stream) {
+  return A.top ? token_launch<TYPE, true>(A, stream) : token_launch<TYPE, false>(A, stream);
+}
+template <int TYPE>
+int token_grad_launch(const TokenGradArgs& A, hipStream_t stream) {
+  const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 22),
+                  (unsigned)std::min<int64_t>(ceil_div(A.vocab, kGradPiece), 1 << 14));
+  token_grad_kernel<TYPE><<<grid, kThreads, 0, stream>>>(A);
+  return launch_status();
+}
+
+int check_logits(int type, int64_t rows, int64_t vocab, int64_t stride) {
+  if (!known_type(type) || rows < 0 || rows >= (int64_t(1) << 31) || vocab < 1 || vocab >= (int64_t(1) << 31) ||
+      stride < vocab)
+    return QA_ERR_INVALID_ARG;
+  return QA_OK;
+}
+
+}  // namespace
+}  // namespace qa
+
+using namespace qa;
+
+extern "C" size_t qa_token_workspace_bytes(int64_t rows, int64_t vocab, int32_t top) {
+  if (check_logits(QA_F32, rows, vocab, vocab) != QA_OK || top < 0 || top > QA_TOP_MAX || top > vocab || rows == 0)
+    return 0;
+  const int64_t splits = splits_for(rows, vocab);
+  return splits == 1 ? 0 : (size_t)(rows * splits) * (16 + 8 * (size_t)top);
+}
+
+extern "C" int qa_token_logprob(int type, int64_t rows, int64_t vocab, const void* logits, int64_t stride,
+                                const int32_t* target, int32_t top, float* logprob, float* entropy, float* stats,
+                                float* top_logprob, int32_t* top_index, void* ws, size_t ws_bytes, void* stream) {
+  if (const int rc = check_logits(type, rows, vocab, stride)) return rc;
+  if (top < 0 || top > QA_TOP_MAX || top > vocab) return QA_ERR_INVALID_ARG;
+  if (rows == 0) return QA_OK;
+  if (!logits || !target != !logprob || (top && (!top_logprob || !top_index))) return QA_ERR_INVALID_ARG;
+  if (!element_aligned(logits, type) || !aligned(target, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
+      !aligned(stats, 4) || (top && (!aligned(top_logprob, 4) || !aligned(top_index, 4))))
+    return QA_ERR_ALIGNMENT;
+  TokenArgs A{logits, target, logprob, entropy, stats, top_logprob, top_index, nullptr, nullptr,
+              rows, vocab, stride, vocab, (int)splits_for(rows, vocab), top};
+  if (A.splits > 1) {
+    if (!ws || ws_bytes < qa_token_workspace_bytes(rows, vocab, top)) return QA_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return QA_ERR_ALIGNMENT;
+    A.part_sums = (float*)ws;
+    A.part_best = (uint64_t*)((char*)ws + (size_t)(rows * A.splits) * 16);
+  }
+  const hipStream_t s = (hipStream_t)stream;
+  if (type == QA_F32) return token_launch<QA_F32>(A, s);
+  if (type == QA_BF16) return token_launch<QA_BF16>(A, s);
+  return token_launch<QA_F16>(A, s);
+}
+
+extern "C" int qa_token_logprob_grad(int type, int64_t rows, int64_t vocab, const void* logits, int64_t stride,
+                                     const int32_t* target, const float* stats, const float* entropy,
+                                     const float* g_logprob, const float* g_entropy, void* dlogits,
+                                     int64_t dlogits_stride, void* stream) {
+  if (const int rc = check_logits(type, rows, vocab, stride)) return rc;
+  if (dlogits_stride < vocab) return QA_ERR_INVALID_ARG;
+  if (rows == 0) return QA_OK;
+  if (!logits || !stats || !dlogits || !entropy != !g_entropy) return QA_ERR_INVALID_ARG;
+  if (!element_aligned(logits, type) || !element_aligned(dlogits, type) || !aligned(target, 4) || !aligned(stats, 4) ||
+      !aligned(entropy, 4) || !aligned(g_logprob, 4) || !aligned(g_entropy, 4))
+    return QA_ERR_ALIGNMENT;
+  const TokenGradArgs A{logits, target, stats, entropy, g_logprob, g_entropy, dlogits, rows, vocab, stride, dlogits_stride};
+  const hipStream_t s = (hipStream_t)stream;
+  if (type == QA_F32) return token_grad_launch<QA_F32>(A, s);
+  if (type == QA_BF16) return token_grad_launch<QA_BF16>(A, s);
+  return token_grad_launch<QA_F16>(A, s);
+}
