@@ -511,7 +511,7 @@ int qa_rows_unpack(const qa_coded_rows* rows, const int8_t* codes, const uint8_t
  * dy may be of any type; binary32 and binary16 elements are split into bfloat16 parts that add up to
  * them (to 2^-24 of them, and exactly), so that no precision of theirs is lost.  Infinities and NaN in
  * dy, and groups without values, make the sums that they enter NaN or infinite.
- * 1 <= n < 2^24.  ws: qa_rows_workspace_bytes(rows, QA_OP_WEIGHT_GRAD, type, n) bytes, may be NULL if 0. */
+ * 1 <= n < 2^24; strides of what is read below 2^25.  ws: qa_rows_workspace_bytes(rows, QA_OP_WEIGHT_GRAD, type, n) bytes, may be NULL if 0. */
 int qa_rows_weight_grad(const qa_coded_rows* rows, const int8_t* codes, const uint8_t* scales, int type,
                         const void* dy, int64_t dy_stride, int64_t n, float* dw, int64_t dw_stride,
                         int accumulate, void* ws, size_t ws_bytes, void* stream);

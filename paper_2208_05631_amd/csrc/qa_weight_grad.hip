@@ -25,14 +25,15 @@ struct WeightGradArgs {
   int accumulate;
 };
 
-constexpr int kTileN = 128, kTileK = 128, kTileT = 32;      // columns of dY, columns of X, rows of both
-constexpr int kChunks = 16;                        // 16-byte chunks of a tile's row
+constexpr int kStep = 32;                          // rows of both that lie in LDS at a time
 
-// A tile lies in LDS as rows of 128 bfloat16, as in memory; matrix instructions want eight rows of one column per
-// lane, which the transposing reads give: of 16 lanes each reads four columns of one of four rows and receives four rows
-// of one column.  Chunks of 16 bytes are swapped by their row so that the four rows lie in different banks.
-__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * kTileK + (chunk ^ ((row & 3) << 2)) * kVec; }
+// A tile's rows lie in LDS as bfloat16, as in memory; matrix instructions want eight rows of one column per lane, which
+// the transposing reads give: of 16 lanes each reads four columns of one of four rows and receives four rows of one
+// column.  Chunks of 16 bytes are swapped by their row so that the four rows lie in different banks.
+template <int COLS>
+__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * COLS + (chunk ^ ((row & 3) << 2)) * kVec; }
 
+template <int COLS>
 __device__ __forceinline__ bf16x8 eight_rows(const __bf16* tile, int row0, int col0) {
   const int lane = threadIdx.x % 16, chunk = (col0 >> 3) + (lane >> 1 & 1), half = (lane & 1) * 4;
   bf16x8 v;
@@ -40,7 +41,7 @@ __device__ __forceinline__ bf16x8 eight_rows(const __bf16* tile, int row0, int c
 #pragma unroll
   for (int h = 0; h < 2; ++h)
     part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s16x4*)(tile + chunk_at(row0 + 4 * h + (lane >> 2), chunk) + half));
+        (__attribute__((address_space(3))) s16x4*)(tile + chunk_at<COLS>(row0 + 4 * h + (lane >> 2), chunk) + half));
   __builtin_memcpy(&v, part, sizeof v);
   return v;
 }
@@ -60,81 +61,192 @@ __device__ __forceinline__ void split_parts(float (&v)[kVec], u32x4 (&part)[P]) 
 }
 template <int TYPE> constexpr int parts_of = TYPE == QA_F32 ? 3 : TYPE == QA_F16 ? 2 : 1;
 
-template <int TYPE>
-__global__ __launch_bounds__(kThreads) void weight_grad_kernel(WeightGradArgs A) {
+// Four waves, F x F tiles of 32 x 32 each: a work-group has 64 F columns of dY and as many of X.  While one pair of
+// tiles is multiplied the next one's elements are on their way to registers, from where they go to LDS as bfloat16.
+template <int TYPE, int F, bool EDGE>
+struct Worker {
   typedef ElemT<TYPE> T;
-  constexpr int P = parts_of<TYPE>;
-  __shared__ __bf16 lds_dy[P][kTileT * kTileN];
-  __shared__ __bf16 lds_x[kTileT * kTileK];
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  const int64_t n0 = (int64_t)(blockIdx.x % A.tiles_n) * kTileN, k0 = (int64_t)(blockIdx.x / A.tiles_n) * kTileK;
-  const int64_t t_begin = (int64_t)blockIdx.y * A.piece, t_end = min(A.R.rows, t_begin + A.piece);
-  const int row = threadIdx.x / 8, col = (threadIdx.x % 8) * 16;       // this thread's 16 elements of each tile
-  const int wn = (wave & 1) * 64, wk = (wave >> 1) * 64;               // this wave's quarter of the output tile
-  f32x16 acc[2][2] = {};
-  const int left_n = (int)max((int64_t)0, min((int64_t)16, A.n - n0 - col));
-  const bool has_x = k0 + col < A.R.cols;
-  for (int64_t t0 = t_begin; t0 < t_end; t0 += kTileT) {
-    const int64_t t = t0 + row;
-    const bool here = t < t_end;
-    float v[2][kVec] = {};
-    if (here) {
-      const T* p = (const T*)A.dy + t * A.dy_stride + n0 + col;
-      to_f32<TYPE>(load_raw<TYPE>(p, left_n), v[0]);
-      to_f32<TYPE>(load_raw<TYPE>(p + kVec, left_n - kVec), v[1]);
+  static constexpr int P = parts_of<TYPE>, kTile = 64 * F;
+  static constexpr int kDy = kStep * kTile / kVec / kThreads, kX = kStep * kTile / 16 / kThreads;   // vectors per thread
+  static constexpr int kBuffer = (P + 1) * kStep * kTile, kBuffers = P < 3 ? 3 : 2;       // of 160 KiB
+
+  const WeightGradArgs& A;
+  int64_t n0, k0, t_end;
+  uint32_t dy_col, x_col, scale_col;               // bytes of this thread's columns from the row's begin
+  int left;                                        // columns of dY that this thread's vectors have
+  Raw8<TYPE> dy[kDy];
+  u32x4 code[kX];
+  uint32_t scale[kX];
+  f32x16 acc[F][F];
+
+  static __device__ __forceinline__ int dy_row(int v) { return (v * kThreads + (int)threadIdx.x) / (kTile / kVec); }
+  static __device__ __forceinline__ int dy_chunk() { return threadIdx.x % (kTile / kVec); }
+  static __device__ __forceinline__ int x_row(int v) { return (v * kThreads + (int)threadIdx.x) / (kTile / 16); }
+  static __device__ __forceinline__ int x_chunk() { return threadIdx.x % (kTile / 16); }
+
+  __device__ __forceinline__ Worker(const WeightGradArgs& a, int64_t n, int64_t k, int64_t end) : A(a), n0(n), k0(k), t_end(end) {
+    // A vector that the end cuts off, or that lies past it, is the last eight columns instead: write() knows.  With fewer
+    // than eight columns (EDGE) elements are read one by one.
+    const int64_t col = n0 + dy_chunk() * kVec;
+    left = (int)max((int64_t)0, min((int64_t)kVec, A.n - col));
+    dy_col = (uint32_t)(EDGE ? col : min(col, A.n - kVec)) * (uint32_t)sizeof(T);
+    x_col = (uint32_t)min(k0 + x_chunk() * 16, (A.R.cols - 1) / 16 * 16);
+    scale_col = x_col / (uint32_t)A.R.group;
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int j = 0; j < F; ++j) acc[i][j] = f32x16{};
+  }
+  // Rows past the end are read from the last one; X is 0 there.
+  __device__ __forceinline__ void load(int64_t t0) {
+    t0 = min(t0, t_end - 1);
+    const int last = (int)min((int64_t)kStep, t_end - t0) - 1;
+    const char* dy_row0 = (const char*)A.dy + t0 * A.dy_stride * (int64_t)sizeof(T);
+    const int8_t* x_row0 = A.codes + t0 * A.R.code_stride;
+    const uint8_t* scale_row0 = A.scales + t0 * A.R.scale_stride;
+#pragma unroll
+    for (int v = 0; v < kDy; ++v) {
+      const uint32_t at = (uint32_t)min(dy_row(v), last) * (uint32_t)(A.dy_stride * (int64_t)sizeof(T)) + dy_col;
+      const T* p = (const T*)(dy_row0 + at);
+      dy[v] = EDGE ? load_raw<TYPE>(p, left) : load_raw<TYPE>(p);
     }
-    u32x4 code = {0, 0, 0, 0};
-    float scale = 0.0f;
-    if (here && has_x) {
-      code = *reinterpret_cast<const u32x4*>(A.codes + t * A.R.code_stride + k0 + col);
-      scale = scale_of(A.scales[t * A.R.scale_stride + (k0 + col) / A.R.group]);
-    }
-    __syncthreads();                               // the tiles of the round before have been read
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      u32x4 part[P];
-      split_parts<P>(v[h], part);
-#pragma unroll
-      for (int p = 0; p < P; ++p) *reinterpret_cast<u32x4*>(lds_dy[p] + chunk_at(row, col / 8 + h)) = part[p];
-      u32x4 x;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t w = code[2 * h + i / 2] >> (16 * (i % 2));
-        const float lo = (float)(int8_t)w * scale, hi = (float)(int8_t)(w >> 8) * scale;
-        x[i] = __builtin_amdgcn_perm(as_u32(hi), as_u32(lo), 0x07060302u);
-      }
-      *reinterpret_cast<u32x4*>(lds_x + chunk_at(row, col / 8 + h)) = x;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int row0 = 16 * s + 8 * (lane / 32), col0 = lane & 16;
-      bf16x8 x[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) x[j] = eight_rows(lds_x, row0, wk + 32 * j + col0);
-#pragma unroll
-      for (int p = 0; p < P; ++p)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const bf16x8 d = eight_rows(lds_dy[p], row0, wn + 32 * i + col0);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d, x[j], acc[i][j], 0, 0, 0);
-        }
+    for (int v = 0; v < kX; ++v) {
+      const uint32_t row = (uint32_t)min(x_row(v), last);
+      code[v] = *reinterpret_cast<const u32x4*>(x_row0 + (row * (uint32_t)A.R.code_stride + x_col));
+      scale[v] = scale_row0[row * (uint32_t)A.R.scale_stride + scale_col];
     }
   }
-  float* out = A.out + (int64_t)blockIdx.y * A.split_stride;
+  __device__ __forceinline__ void store(__bf16* lds, int64_t t0) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int64_t n = n0 + wn + 32 * i + 8 * (e / 4) + 4 * (lane / 32) + e % 4, k = k0 + wk + 32 * j + lane % 32;
-        if (n < A.n && k < A.R.cols) {
-          float* p = out + n * A.out_stride + k;
-          *p = A.accumulate ? *p + acc[i][j][e] : acc[i][j][e];
-        }
+    for (int v = 0; v < kDy; ++v) {
+      float f[kVec];
+      u32x4 part[P];
+      if constexpr (TYPE == QA_BF16) {
+        part[0] = dy[v].a;
+      } else {
+        to_f32<TYPE>(dy[v], f);
+        split_parts<P>(f, part);
       }
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        *reinterpret_cast<u32x4*>(lds + p * kStep * kTile + chunk_at<kTile>(dy_row(v), dy_chunk())) = part[p];
+    }
+#pragma unroll
+    for (int v = 0; v < kX; ++v) {
+      asm("" : "+v"(code[v]), "+v"(scale[v]));     // or their bytes are taken apart where they are loaded, and waited for
+      const float s = t0 + x_row(v) < t_end ? scale_of(scale[v]) : 0.0f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t w = code[v][2 * h + i / 2] >> (16 * (i % 2));
+          const float lo = (float)(int8_t)w * s, hi = (float)(int8_t)(w >> 8) * s;
+          x[i] = __builtin_amdgcn_perm(as_u32(hi), as_u32(lo), 0x07060302u);
+        }
+        *reinterpret_cast<u32x4*>(lds + P * kStep * kTile + chunk_at<kTile>(x_row(v), 2 * x_chunk() + h)) = x;
+      }
+    }
+  }
+  // A step has 2 P phases of F x F matrix instructions, each for 16 rows and one part of dY.  A phase's operands are read
+  // while the one before it is multiplied, the first one's of the next step, too, where there are three buffers: the
+  // one that is read next is complete then before the step begins.
+  bf16x8 d[2][F], x[2][F];
+  __device__ __forceinline__ void operands(const __bf16* lds, int phase) {
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, s = phase / P, p = phase % P;
+    const int row0 = 16 * s + 8 * (lane / 32), col0 = lane & 16;
+    const int wn = (wave & 1) * 32 * F + col0, wk = (wave >> 1) * 32 * F + col0;
+    if (p == 0) {
+#pragma unroll
+      for (int j = 0; j < F; ++j) x[s & 1][j] = eight_rows<kTile>(lds + P * kStep * kTile, row0, wk + 32 * j);
+    }
+#pragma unroll
+    for (int i = 0; i < F; ++i) d[phase & 1][i] = eight_rows<kTile>(lds + p * kStep * kTile, row0, wn + 32 * i);
+  }
+  __device__ __forceinline__ void multiply(int phase) {
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int j = 0; j < F; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d[phase & 1][i], x[phase / P & 1][j], acc[i][j], 0, 0, 0);
+  }
+  __device__ __forceinline__ void run(int64_t t_begin, __bf16* lds) {
+    constexpr int kPhases = 2 * P;
+#pragma unroll
+    for (int b = 0; b + 1 < kBuffers; ++b) {
+      load(t_begin + b * kStep);
+      store(lds + b * kBuffer, t_begin + b * kStep);
+    }
+    load(t_begin + (kBuffers - 1) * kStep);
+    __syncthreads();
+    int now = 0, next = kBuffer, last = (kBuffers - 1) * kBuffer;          // read, read next, written
+    operands(lds, 0);
+    for (int64_t t = t_begin; t < t_end; t += kStep) {
+#pragma unroll
+      for (int phase = 0; phase < kPhases; ++phase) {
+        if (phase + 1 < kPhases) operands(lds + now, phase + 1);
+        else if (kBuffers == 3) operands(lds + next, 0);
+        if (phase == 0) {                          // what lies past the end is not used
+          store(lds + last, t + (kBuffers - 1) * kStep);
+          load(t + kBuffers * kStep);
+        }
+        multiply(phase);
+      }
+      __syncthreads();
+      if (kBuffers == 2) operands(lds + next, 0);
+      const int free = now;
+      now = next;
+      next = kBuffers == 2 ? free : last;
+      last = free;
+    }
+  }
+  // INSIDE: the whole tile is.
+  template <bool INSIDE, bool ADD>
+  __device__ __forceinline__ void write(float* out) {
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int64_t n1 = n0 + (wave & 1) * 32 * F, k1 = k0 + (wave >> 1) * 32 * F + lane % 32;
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t first = n1 + 32 * i + 8 * q;
+        const int64_t n = (INSIDE || EDGE ? first : min(first, A.n - kVec)) + 4 * (lane / 32);
+        float* p = out + n * A.out_stride + k1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e, p += A.out_stride)
+#pragma unroll
+          for (int j = 0; j < F; ++j) {
+            if (!INSIDE && (n + e < first || n + e >= A.n || k1 + 32 * j >= A.R.cols)) continue;
+            const float v = acc[i][j][4 * q + e];
+            p[32 * j] = ADD ? p[32 * j] + v : v;
+          }
+        if (ADD) __builtin_amdgcn_sched_barrier(0);          // or all that is added to is held in registers at once
+      }
+  }
+  __device__ __forceinline__ void write(float* out) {
+    if (A.accumulate) write<false, true>(out);
+    else if (n0 + kTile <= A.n && k0 + kTile <= A.R.cols) write<true, false>(out);
+    else write<false, false>(out);
+  }
+};
+
+template <int TYPE, int F, bool EDGE>
+__global__ __launch_bounds__(kThreads) void weight_grad_kernel(WeightGradArgs A) {
+  __shared__ __bf16 lds[Worker<TYPE, F, EDGE>::kBuffers * Worker<TYPE, F, EDGE>::kBuffer];
+  constexpr int kTile = 64 * F;
+  // Consecutive work-groups go to the eight dies in turn.  Each die takes tiles that lie together, eight of X beside each
+  // other, so that its cache is asked for the same rows.
+  const unsigned die = blockIdx.x % 8, each = gridDim.x / 8, more = gridDim.x % 8;
+  const unsigned tile = die * each + min(die, more) + blockIdx.x / 8;
+  const unsigned tiles_n = (unsigned)A.tiles_n, tiles_k = gridDim.x / tiles_n;
+  const unsigned band = tile / (8 * tiles_n), wide = min(8u, tiles_k - 8 * band), in_band = tile - band * 8 * tiles_n;
+  const int64_t n0 = (int64_t)(in_band / wide) * kTile, k0 = (int64_t)(8 * band + in_band % wide) * kTile;
+  const int64_t t_begin = (int64_t)blockIdx.y * A.piece, t_end = min(A.R.rows, t_begin + A.piece);
+  float* out = A.out + (int64_t)blockIdx.y * A.split_stride;
+  Worker<TYPE, F, EDGE> w(A, n0, k0, t_end);
+  if (t_begin < t_end) w.run(t_begin, lds);
+  w.write(out);
 }
 
 // dW from the splits' sums, in their order.
@@ -151,24 +263,31 @@ __global__ __launch_bounds__(kThreads) void weight_grad_join_kernel(const float*
 
 // ---- which form ----------------------------------------------------------------------------------------------
 
-// Few tiles leave compute units idle: the rows are split then, 256 at least to a split, towards four work-groups per
-// compute unit.
-int64_t splits_for(int64_t rows, int64_t cols, int64_t n) {
-  const int64_t tiles = ceil_div(n, kTileN) * ceil_div(cols, kTileK);
-  return std::max<int64_t>(1, std::min(ceil_div(1024, tiles), rows / 256));
+// Tiles of 256 x 256 where they give every compute unit one, 128 x 128 otherwise.  Few tiles leave compute units idle:
+// the rows are split then, 256 at least to a split.
+struct Plan { int f; int64_t tiles_n, tiles, splits; };
+Plan plan_for(int64_t rows, int64_t cols, int64_t n) {
+  Plan p;
+  p.f = n >= kVec && ceil_div(n, 256) * ceil_div(cols, 256) >= 256 ? 4 : 2;
+  p.tiles_n = ceil_div(n, 64 * p.f);
+  p.tiles = p.tiles_n * ceil_div(cols, 64 * p.f);
+  p.splits = p.f == 4 ? 1 : std::max<int64_t>(1, std::min(ceil_div(1024, p.tiles), rows / 256));
+  return p;
 }
 
 template <int TYPE>
-int weight_grad_launch(WeightGradArgs& A, int64_t splits, hipStream_t stream) {
-  const dim3 grid((unsigned)(A.tiles_n * ceil_div(A.R.cols, kTileK)), (unsigned)splits);
-  weight_grad_kernel<TYPE><<<grid, kThreads, 0, stream>>>(A);
+int weight_grad_launch(WeightGradArgs& A, const Plan& plan, hipStream_t stream) {
+  const dim3 grid((unsigned)plan.tiles, (unsigned)plan.splits);
+  if (A.n < kVec) weight_grad_kernel<TYPE, 2, true><<<grid, kThreads, 0, stream>>>(A);
+  else if (plan.f == 4) weight_grad_kernel<TYPE, 4, false><<<grid, kThreads, 0, stream>>>(A);
+  else weight_grad_kernel<TYPE, 2, false><<<grid, kThreads, 0, stream>>>(A);
   return launch_status();
 }
 
 }  // namespace
 
 size_t weight_grad_workspace_bytes(const qa_coded_rows* R, int, int64_t n) {
-  const int64_t splits = splits_for(R->rows, R->cols, n);
+  const int64_t splits = plan_for(R->rows, R->cols, n).splits;
   return splits == 1 ? 0 : (size_t)splits * (size_t)n * (size_t)R->cols * sizeof(float);
 }
 
@@ -180,7 +299,8 @@ extern "C" int qa_rows_weight_grad(const qa_coded_rows* rows, const int8_t* code
                                    const void* dy, int64_t dy_stride, int64_t n, float* dw, int64_t dw_stride,
                                    int accumulate, void* ws, size_t ws_bytes, void* stream) {
   if (const int rc = check_rows(rows)) return rc;
-  if (!known_type(type) || n < 1 || n >= (int64_t(1) << 24) || dy_stride < n || dw_stride < rows->cols ||
+  if (!known_type(type) || n < 1 || n >= (int64_t(1) << 24) || dy_stride < n || dy_stride >= (int64_t(1) << 25) ||
+      rows->code_stride >= (int64_t(1) << 25) || rows->scale_stride >= (int64_t(1) << 25) || dw_stride < rows->cols ||
       (accumulate != 0 && accumulate != 1) || !dw)
     return QA_ERR_INVALID_ARG;
   if (!aligned(dw, 4)) return QA_ERR_ALIGNMENT;
@@ -194,8 +314,9 @@ extern "C" int qa_rows_weight_grad(const qa_coded_rows* rows, const int8_t* code
   }
   if (!codes || !scales || !dy) return QA_ERR_INVALID_ARG;
   if (!element_aligned(dy, type) || !aligned(codes, 16)) return QA_ERR_ALIGNMENT;
-  const int64_t splits = splits_for(rows->rows, rows->cols, n);
-  WeightGradArgs A{*rows, codes, scales, dy, dw, dy_stride, dw_stride, 0, n, rows->rows, ceil_div(n, kTileN), accumulate};
+  const Plan plan = plan_for(rows->rows, rows->cols, n);
+  const int64_t splits = plan.splits;
+  WeightGradArgs A{*rows, codes, scales, dy, dw, dy_stride, dw_stride, 0, n, rows->rows, plan.tiles_n, accumulate};
   if (splits > 1) {
     if (!ws || ws_bytes < weight_grad_workspace_bytes(rows, type, n)) return QA_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return QA_ERR_ALIGNMENT;
@@ -203,11 +324,11 @@ extern "C" int qa_rows_weight_grad(const qa_coded_rows* rows, const int8_t* code
     A.out_stride = rows->cols;
     A.split_stride = all;
     A.accumulate = 0;
-    A.piece = ceil_div(ceil_div(rows->rows, splits), kTileT) * kTileT;
+    A.piece = ceil_div(ceil_div(rows->rows, splits), kStep) * kStep;
   }
-  int rc = type == QA_F32    ? weight_grad_launch<QA_F32>(A, splits, s)
-           : type == QA_BF16 ? weight_grad_launch<QA_BF16>(A, splits, s)
-                             : weight_grad_launch<QA_F16>(A, splits, s);
+  int rc = type == QA_F32    ? weight_grad_launch<QA_F32>(A, plan, s)
+           : type == QA_BF16 ? weight_grad_launch<QA_BF16>(A, plan, s)
+                             : weight_grad_launch<QA_F16>(A, plan, s);
   if (rc || splits == 1) return rc;
   weight_grad_join_kernel<<<join, kThreads, 0, s>>>((const float*)ws, (int)splits, n, rows->cols, dw, dw_stride, accumulate);
   return launch_status();
