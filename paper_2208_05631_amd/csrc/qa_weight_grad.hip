@@ -29,19 +29,15 @@ constexpr int kStep = 32;                          // rows of both that lie in L
 
 // A tile's rows lie in LDS as bfloat16, as in memory; matrix instructions want eight rows of one column per lane, which
 // the transposing reads give: of 16 lanes each reads four columns of one of four rows and receives four rows of one
-// column.  Chunks of 16 bytes are swapped by their row so that the four rows lie in different banks.
+// column.  A row is followed by 64 bytes of nothing, so that four rows lie in different banks.
+constexpr int kGap = 32;                           // elements
 template <int COLS>
-__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * COLS + (chunk ^ ((row & 3) << 2)) * kVec; }
-
-template <int COLS>
-__device__ __forceinline__ bf16x8 eight_rows(const __bf16* tile, int row0, int col0) {
-  const int lane = threadIdx.x % 16, chunk = (col0 >> 3) + (lane >> 1 & 1), half = (lane & 1) * 4;
+__device__ __forceinline__ bf16x8 eight_rows(const __bf16* lane_at) {
   bf16x8 v;
   s16x4 part[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h)
-    part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s16x4*)(tile + chunk_at<COLS>(row0 + 4 * h + (lane >> 2), chunk) + half));
+    part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lane_at + 4 * h * (COLS + kGap)));
   __builtin_memcpy(&v, part, sizeof v);
   return v;
 }
@@ -63,20 +59,52 @@ template <int TYPE> constexpr int parts_of = TYPE == QA_F32 ? 3 : TYPE == QA_F16
 
 // Four waves, F x F tiles of 32 x 32 each: a work-group has 64 F columns of dY and as many of X.  While one pair of
 // tiles is multiplied the next one's elements are on their way to registers, from where they go to LDS as bfloat16.
+// The order of a phase's instructions: everything else in the shadow of the matrix instructions.
+template <int TYPE, int F>
+__device__ __forceinline__ void interleave(int phase) {
+  constexpr int kMatrix = 8, kVector = 2, kLdsRead = 0x100, kLdsWrite = 0x200, kRead = 0x20;
+  if (TYPE == QA_BF16 && F == 4) {
+    if (phase == 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(kVector, 5, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kVector, 7, 0);
+        __builtin_amdgcn_sched_group_barrier(kLdsWrite, 1, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kVector, 3, 0);
+        if (i % 2) __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+      }
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 template <int TYPE, int F, bool EDGE>
 struct Worker {
   typedef ElemT<TYPE> T;
   static constexpr int P = parts_of<TYPE>, kTile = 64 * F;
   static constexpr int kDy = kStep * kTile / kVec / kThreads, kX = kStep * kTile / 16 / kThreads;   // vectors per thread
-  static constexpr int kBuffer = (P + 1) * kStep * kTile, kBuffers = P < 3 ? 3 : 2;       // of 160 KiB
+  static constexpr int kRow = kTile + kGap, kPart = kStep * kRow, kBuffer = (P + 1) * kPart;
+  static constexpr int kBuffers = P == 1 ? 3 : 2;  // of 160 KiB
+  static constexpr int kAhead = P < 3 ? 2 : 1;     // steps whose elements are on their way: one is as long as half a read takes, or longer
 
   const WeightGradArgs& A;
   int64_t n0, k0, t_end;
   uint32_t dy_col, x_col, scale_col;               // bytes of this thread's columns from the row's begin
   int left;                                        // columns of dY that this thread's vectors have
-  Raw8<TYPE> dy[kDy];
-  u32x4 code[kX];
-  uint32_t scale[kX];
+  int d_lane, x_lane;                              // where a lane reads in LDS
+  struct Loaded { Raw8<TYPE> dy[kDy]; u32x4 code[kX]; uint32_t scale[kX]; };
   f32x16 acc[F][F];
 
   static __device__ __forceinline__ int dy_row(int v) { return (v * kThreads + (int)threadIdx.x) / (kTile / kVec); }
@@ -92,13 +120,17 @@ struct Worker {
     dy_col = (uint32_t)(EDGE ? col : min(col, A.n - kVec)) * (uint32_t)sizeof(T);
     x_col = (uint32_t)min(k0 + x_chunk() * 16, (A.R.cols - 1) / 16 * 16);
     scale_col = x_col / (uint32_t)A.R.group;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int at = (8 * (lane / 32) + (lane % 16 >> 2)) * kRow + (lane & 16) + (lane & 3) * 4;
+    d_lane = at + (wave & 1) * 32 * F;
+    x_lane = at + (wave >> 1) * 32 * F;
 #pragma unroll
     for (int i = 0; i < F; ++i)
 #pragma unroll
       for (int j = 0; j < F; ++j) acc[i][j] = f32x16{};
   }
   // Rows past the end are read from the last one; X is 0 there.
-  __device__ __forceinline__ void load(int64_t t0) {
+  __device__ __forceinline__ void load(Loaded& to, int64_t t0) {
     t0 = min(t0, t_end - 1);
     const int last = (int)min((int64_t)kStep, t_end - t0) - 1;
     const char* dy_row0 = (const char*)A.dy + t0 * A.dy_stride * (int64_t)sizeof(T);
@@ -108,44 +140,47 @@ struct Worker {
     for (int v = 0; v < kDy; ++v) {
       const uint32_t at = (uint32_t)min(dy_row(v), last) * (uint32_t)(A.dy_stride * (int64_t)sizeof(T)) + dy_col;
       const T* p = (const T*)(dy_row0 + at);
-      dy[v] = EDGE ? load_raw<TYPE>(p, left) : load_raw<TYPE>(p);
+      to.dy[v] = EDGE ? load_raw<TYPE>(p, left) : load_raw<TYPE>(p);
     }
 #pragma unroll
     for (int v = 0; v < kX; ++v) {
       const uint32_t row = (uint32_t)min(x_row(v), last);
-      code[v] = *reinterpret_cast<const u32x4*>(x_row0 + (row * (uint32_t)A.R.code_stride + x_col));
-      scale[v] = scale_row0[row * (uint32_t)A.R.scale_stride + scale_col];
+      to.code[v] = *reinterpret_cast<const u32x4*>(x_row0 + (row * (uint32_t)A.R.code_stride + x_col));
+      to.scale[v] = scale_row0[row * (uint32_t)A.R.scale_stride + scale_col];
     }
   }
-  __device__ __forceinline__ void store(__bf16* lds, int64_t t0) {
+  __device__ __forceinline__ void store(Loaded& from, __bf16* lds, int64_t t0) {
 #pragma unroll
     for (int v = 0; v < kDy; ++v) {
       float f[kVec];
       u32x4 part[P];
       if constexpr (TYPE == QA_BF16) {
-        part[0] = dy[v].a;
+        part[0] = from.dy[v].a;
       } else {
-        to_f32<TYPE>(dy[v], f);
+        to_f32<TYPE>(from.dy[v], f);
         split_parts<P>(f, part);
       }
 #pragma unroll
       for (int p = 0; p < P; ++p)
-        *reinterpret_cast<u32x4*>(lds + p * kStep * kTile + chunk_at<kTile>(dy_row(v), dy_chunk())) = part[p];
+        *reinterpret_cast<u32x4*>(lds + p * kPart + dy_row(v) * kRow + dy_chunk() * kVec) = part[p];
     }
+    // (code + 128) scale - 128 scale, exact.  The 128's are not known to the compiler, which would take a code's bytes apart,
+    // and wait for them, where they are loaded.
+    uint32_t bias;
+    asm("s_mov_b32 %0, 0x80808080" : "=s"(bias));
 #pragma unroll
     for (int v = 0; v < kX; ++v) {
-      asm("" : "+v"(code[v]), "+v"(scale[v]));     // or their bytes are taken apart where they are loaded, and waited for
-      const float s = t0 + x_row(v) < t_end ? scale_of(scale[v]) : 0.0f;
+      const float s = t0 + x_row(v) < t_end ? scale_of(from.scale[v]) : 0.0f, s128 = -128.0f * s;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         u32x4 x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t w = code[v][2 * h + i / 2] >> (16 * (i % 2));
-          const float lo = (float)(int8_t)w * s, hi = (float)(int8_t)(w >> 8) * s;
+          const uint32_t w = (from.code[v][2 * h + i / 2] ^ bias) >> (16 * (i % 2));
+          const float lo = __builtin_fmaf((float)(w & 0xFFu), s, s128), hi = __builtin_fmaf((float)(w >> 8 & 0xFFu), s, s128);
           x[i] = __builtin_amdgcn_perm(as_u32(hi), as_u32(lo), 0x07060302u);
         }
-        *reinterpret_cast<u32x4*>(lds + P * kStep * kTile + chunk_at<kTile>(x_row(v), 2 * x_chunk() + h)) = x;
+        *reinterpret_cast<u32x4*>(lds + P * kPart + x_row(v) * kRow + x_chunk() * 16 + h * kVec) = x;
       }
     }
   }
@@ -154,15 +189,13 @@ struct Worker {
   // one that is read next is complete then before the step begins.
   bf16x8 d[2][F], x[2][F];
   __device__ __forceinline__ void operands(const __bf16* lds, int phase) {
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, s = phase / P, p = phase % P;
-    const int row0 = 16 * s + 8 * (lane / 32), col0 = lane & 16;
-    const int wn = (wave & 1) * 32 * F + col0, wk = (wave >> 1) * 32 * F + col0;
+    const int s = phase / P, p = phase % P;
     if (p == 0) {
 #pragma unroll
-      for (int j = 0; j < F; ++j) x[s & 1][j] = eight_rows<kTile>(lds + P * kStep * kTile, row0, wk + 32 * j);
+      for (int j = 0; j < F; ++j) x[s & 1][j] = eight_rows<kTile>(lds + x_lane + (P * kPart + 16 * s * kRow + 32 * j));
     }
 #pragma unroll
-    for (int i = 0; i < F; ++i) d[phase & 1][i] = eight_rows<kTile>(lds + p * kStep * kTile, row0, wn + 32 * i);
+    for (int i = 0; i < F; ++i) d[phase & 1][i] = eight_rows<kTile>(lds + d_lane + (p * kPart + 16 * s * kRow + 32 * i));
   }
   __device__ __forceinline__ void multiply(int phase) {
 #pragma unroll
@@ -173,32 +206,33 @@ struct Worker {
   }
   __device__ __forceinline__ void run(int64_t t_begin, __bf16* lds) {
     constexpr int kPhases = 2 * P;
+    Loaded loaded[kAhead];
 #pragma unroll
-    for (int b = 0; b + 1 < kBuffers; ++b) {
-      load(t_begin + b * kStep);
-      store(lds + b * kBuffer, t_begin + b * kStep);
-    }
-    load(t_begin + (kBuffers - 1) * kStep);
+    for (int b = 0; b + 1 < kBuffers; ++b) load(loaded[b % kAhead], t_begin + b * kStep), store(loaded[b % kAhead], lds + b * kBuffer, t_begin + b * kStep);
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) load(loaded[a], t_begin + (kBuffers - 1 + a) * kStep);
     __syncthreads();
     int now = 0, next = kBuffer, last = (kBuffers - 1) * kBuffer;          // read, read next, written
     operands(lds, 0);
-    for (int64_t t = t_begin; t < t_end; t += kStep) {
+    for (int64_t t = t_begin; t < t_end;) {        // X is 0 in a step past the end
 #pragma unroll
-      for (int phase = 0; phase < kPhases; ++phase) {
-        if (phase + 1 < kPhases) operands(lds + now, phase + 1);
-        else if (kBuffers == 3) operands(lds + next, 0);
-        if (phase == 0) {                          // what lies past the end is not used
-          store(lds + last, t + (kBuffers - 1) * kStep);
-          load(t + kBuffers * kStep);
+      for (int a = 0; a < kAhead; ++a, t += kStep) {
+#pragma unroll
+        for (int phase = 0; phase < kPhases; ++phase) {
+          if (phase + 1 < kPhases) operands(lds + now, phase + 1);
+          else if (kBuffers == 3) operands(lds + next, 0);
+          if (phase == 0) store(loaded[a], lds + last, t + (kBuffers - 1) * kStep);       // what lies past the end is not used
+          if (phase == 1) load(loaded[a], t + (kBuffers - 1 + kAhead) * kStep);
+          multiply(phase);
+          interleave<TYPE, F>(phase);
         }
-        multiply(phase);
+        __syncthreads();
+        if (kBuffers == 2) operands(lds + next, 0);
+        const int free = now;
+        now = next;
+        next = kBuffers == 2 ? free : last;
+        last = free;
       }
-      __syncthreads();
-      if (kBuffers == 2) operands(lds + next, 0);
-      const int free = now;
-      now = next;
-      next = kBuffers == 2 ? free : last;
-      last = free;
     }
   }
   // INSIDE: the whole tile is.
@@ -324,7 +358,7 @@ extern "C" int qa_rows_weight_grad(const qa_coded_rows* rows, const int8_t* code
     A.out_stride = rows->cols;
     A.split_stride = all;
     A.accumulate = 0;
-    A.piece = ceil_div(ceil_div(rows->rows, splits), kStep) * kStep;
+    A.piece = ceil_div(ceil_div(rows->rows, splits), 2 * kStep) * 2 * kStep;
   }
   int rc = type == QA_F32    ? weight_grad_launch<QA_F32>(A, plan, s)
            : type == QA_BF16 ? weight_grad_launch<QA_BF16>(A, plan, s)
