@@ -66,23 +66,18 @@ __device__ __forceinline__ void interleave(int phase) {
   if (TYPE == QA_BF16 && F == 4) {
     if (phase == 0) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 16; ++i) {
         __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(kVector, 5, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
         __builtin_amdgcn_sched_group_barrier(kVector, 7, 0);
-        __builtin_amdgcn_sched_group_barrier(kLdsWrite, 1, 0);
+        if (i % 2) __builtin_amdgcn_sched_group_barrier(kLdsWrite, 1, 0);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
         __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kVector, 3, 0);
+        __builtin_amdgcn_sched_group_barrier(kVector, 2, 0);
         if (i % 2) __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
       }
     }
@@ -100,8 +95,12 @@ struct Worker {
   static constexpr int kAhead = P < 3 ? 2 : 1;     // steps whose elements are on their way: one is as long as half a read takes, or longer
 
   const WeightGradArgs& A;
-  int64_t n0, k0, t_end;
-  uint32_t dy_col, x_col, scale_col;               // bytes of this thread's columns from the row's begin
+  int64_t n0, k0, t_end, t_load;
+  const char* dy_from;                             // row t_load
+  const int8_t* x_from;
+  const uint8_t* scale_from;
+  uint32_t dy_at[kDy], x_at[kX], scale_at[kX];     // bytes from there to this thread's vectors
+  uint32_t dy_tail[kDy], x_tail[kX], scale_tail[kX];       // the same in the last step
   int left;                                        // columns of dY that this thread's vectors have
   int d_lane, x_lane;                              // where a lane reads in LDS
   struct Loaded { Raw8<TYPE> dy[kDy]; u32x4 code[kX]; uint32_t scale[kX]; };
@@ -112,14 +111,32 @@ struct Worker {
   static __device__ __forceinline__ int x_row(int v) { return (v * kThreads + (int)threadIdx.x) / (kTile / 16); }
   static __device__ __forceinline__ int x_chunk() { return threadIdx.x % (kTile / 16); }
 
-  __device__ __forceinline__ Worker(const WeightGradArgs& a, int64_t n, int64_t k, int64_t end) : A(a), n0(n), k0(k), t_end(end) {
+  __device__ __forceinline__ Worker(const WeightGradArgs& a, int64_t n, int64_t k, int64_t begin, int64_t end)
+      : A(a), n0(n), k0(k), t_end(end), t_load(begin) {
     // A vector that the end cuts off, or that lies past it, is the last eight columns instead: write() knows.  With fewer
     // than eight columns (EDGE) elements are read one by one.
     const int64_t col = n0 + dy_chunk() * kVec;
     left = (int)max((int64_t)0, min((int64_t)kVec, A.n - col));
-    dy_col = (uint32_t)(EDGE ? col : min(col, A.n - kVec)) * (uint32_t)sizeof(T);
-    x_col = (uint32_t)min(k0 + x_chunk() * 16, (A.R.cols - 1) / 16 * 16);
-    scale_col = x_col / (uint32_t)A.R.group;
+    dy_from = (const char*)A.dy + begin * A.dy_stride * (int64_t)sizeof(T);
+    x_from = A.codes + begin * A.R.code_stride;
+    scale_from = A.scales + begin * A.R.scale_stride;
+    const uint32_t dy_col = (uint32_t)(EDGE ? col : min(col, A.n - kVec)) * (uint32_t)sizeof(T);
+    const uint32_t x_col = (uint32_t)min(k0 + x_chunk() * 16, (A.R.cols - 1) / 16 * 16);
+    const uint32_t scale_col = x_col / (uint32_t)A.R.group;
+    const int last = (int)((end - begin - 1) % kStep);
+#pragma unroll
+    for (int v = 0; v < kDy; ++v) {
+      const uint32_t stride = (uint32_t)(A.dy_stride * (int64_t)sizeof(T));
+      dy_at[v] = (uint32_t)dy_row(v) * stride + dy_col;
+      dy_tail[v] = (uint32_t)min(dy_row(v), last) * stride + dy_col;
+    }
+#pragma unroll
+    for (int v = 0; v < kX; ++v) {
+      x_at[v] = (uint32_t)x_row(v) * (uint32_t)A.R.code_stride + x_col;
+      x_tail[v] = (uint32_t)min(x_row(v), last) * (uint32_t)A.R.code_stride + x_col;
+      scale_at[v] = (uint32_t)x_row(v) * (uint32_t)A.R.scale_stride + scale_col;
+      scale_tail[v] = (uint32_t)min(x_row(v), last) * (uint32_t)A.R.scale_stride + scale_col;
+    }
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int at = (8 * (lane / 32) + (lane % 16 >> 2)) * kRow + (lane & 16) + (lane & 3) * 4;
     d_lane = at + (wave & 1) * 32 * F;
@@ -129,27 +146,26 @@ struct Worker {
 #pragma unroll
       for (int j = 0; j < F; ++j) acc[i][j] = f32x16{};
   }
-  // Rows past the end are read from the last one; X is 0 there.
-  __device__ __forceinline__ void load(Loaded& to, int64_t t0) {
-    t0 = min(t0, t_end - 1);
-    const int last = (int)min((int64_t)kStep, t_end - t0) - 1;
-    const char* dy_row0 = (const char*)A.dy + t0 * A.dy_stride * (int64_t)sizeof(T);
-    const int8_t* x_row0 = A.codes + t0 * A.R.code_stride;
-    const uint8_t* scale_row0 = A.scales + t0 * A.R.scale_stride;
+  // The next step's elements.  Rows past the end are read from the last one, steps past the end from the last step.
+  __device__ __forceinline__ void load(Loaded& to) {
+    const bool tail = t_load + kStep >= t_end;
 #pragma unroll
     for (int v = 0; v < kDy; ++v) {
-      const uint32_t at = (uint32_t)min(dy_row(v), last) * (uint32_t)(A.dy_stride * (int64_t)sizeof(T)) + dy_col;
-      const T* p = (const T*)(dy_row0 + at);
+      const T* p = (const T*)(dy_from + (tail ? dy_tail[v] : dy_at[v]));
       to.dy[v] = EDGE ? load_raw<TYPE>(p, left) : load_raw<TYPE>(p);
     }
 #pragma unroll
     for (int v = 0; v < kX; ++v) {
-      const uint32_t row = (uint32_t)min(x_row(v), last);
-      to.code[v] = *reinterpret_cast<const u32x4*>(x_row0 + (row * (uint32_t)A.R.code_stride + x_col));
-      to.scale[v] = scale_row0[row * (uint32_t)A.R.scale_stride + scale_col];
+      to.code[v] = *reinterpret_cast<const u32x4*>(x_from + (tail ? x_tail[v] : x_at[v]));
+      to.scale[v] = scale_from[tail ? scale_tail[v] : scale_at[v]];
     }
+    const int64_t go = tail ? 0 : -1;              // no branch: the matrix instructions around this are one block
+    t_load += kStep & go;
+    dy_from += (kStep * A.dy_stride * (int64_t)sizeof(T)) & go;
+    x_from += (kStep * A.R.code_stride) & go;
+    scale_from += (kStep * A.R.scale_stride) & go;
   }
-  __device__ __forceinline__ void store(Loaded& from, __bf16* lds, int64_t t0) {
+  __device__ __forceinline__ void store_dy(Loaded& from, __bf16* lds) {
 #pragma unroll
     for (int v = 0; v < kDy; ++v) {
       float f[kVec];
@@ -164,6 +180,9 @@ struct Worker {
       for (int p = 0; p < P; ++p)
         *reinterpret_cast<u32x4*>(lds + p * kPart + dy_row(v) * kRow + dy_chunk() * kVec) = part[p];
     }
+  }
+  // X is 0 past the end.
+  __device__ __forceinline__ void store_x(Loaded& from, __bf16* lds, int64_t t0) {
     // (code + 128) scale - 128 scale, exact.  The 128's are not known to the compiler, which would take a code's bytes apart,
     // and wait for them, where they are loaded.
     uint32_t bias;
@@ -204,30 +223,41 @@ struct Worker {
       for (int j = 0; j < F; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d[phase & 1][i], x[phase / P & 1][j], acc[i][j], 0, 0, 0);
   }
+  // One step: the buffer `now` is multiplied, what was loaded for the step that is kBuffers - 1 ahead goes to `last`.
+  static __device__ __forceinline__ void step(Worker& w, Loaded& loaded, int64_t t, const __bf16* __restrict__ now,
+                                              const __bf16* __restrict__ next, __bf16* __restrict__ last) {
+#pragma unroll
+    for (int phase = 0; phase < 2 * P; ++phase) {
+      if (phase + 1 < 2 * P) w.operands(now, phase + 1);
+      else if (kBuffers == 3) w.operands(next, 0);
+      if (phase == 0) {
+        w.store_dy(loaded, last);
+        w.store_x(loaded, last, t + (kBuffers - 1) * kStep);
+      }
+      if (phase == 1) w.load(loaded);
+      w.multiply(phase);
+      interleave<TYPE, F>(phase);
+    }
+    __syncthreads();
+    if (kBuffers == 2) w.operands(next, 0);
+  }
   __device__ __forceinline__ void run(int64_t t_begin, __bf16* lds) {
-    constexpr int kPhases = 2 * P;
     Loaded loaded[kAhead];
 #pragma unroll
-    for (int b = 0; b + 1 < kBuffers; ++b) load(loaded[b % kAhead], t_begin + b * kStep), store(loaded[b % kAhead], lds + b * kBuffer, t_begin + b * kStep);
+    for (int b = 0; b + 1 < kBuffers; ++b) {
+      load(loaded[b % kAhead]);
+      store_dy(loaded[b % kAhead], lds + b * kBuffer);
+      store_x(loaded[b % kAhead], lds + b * kBuffer, t_begin + b * kStep);
+    }
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) load(loaded[a], t_begin + (kBuffers - 1 + a) * kStep);
+    for (int a = 0; a < kAhead; ++a) load(loaded[a]);
     __syncthreads();
     int now = 0, next = kBuffer, last = (kBuffers - 1) * kBuffer;          // read, read next, written
     operands(lds, 0);
     for (int64_t t = t_begin; t < t_end;) {        // X is 0 in a step past the end
 #pragma unroll
       for (int a = 0; a < kAhead; ++a, t += kStep) {
-#pragma unroll
-        for (int phase = 0; phase < kPhases; ++phase) {
-          if (phase + 1 < kPhases) operands(lds + now, phase + 1);
-          else if (kBuffers == 3) operands(lds + next, 0);
-          if (phase == 0) store(loaded[a], lds + last, t + (kBuffers - 1) * kStep);       // what lies past the end is not used
-          if (phase == 1) load(loaded[a], t + (kBuffers - 1 + kAhead) * kStep);
-          multiply(phase);
-          interleave<TYPE, F>(phase);
-        }
-        __syncthreads();
-        if (kBuffers == 2) operands(lds + next, 0);
+        step(*this, loaded[a], t, lds + now, lds + next, lds + last);
         const int free = now;
         now = next;
         next = kBuffers == 2 ? free : last;
@@ -278,7 +308,7 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(WeightGradArgs A)
   const int64_t n0 = (int64_t)(in_band / wide) * kTile, k0 = (int64_t)(8 * band + in_band % wide) * kTile;
   const int64_t t_begin = (int64_t)blockIdx.y * A.piece, t_end = min(A.R.rows, t_begin + A.piece);
   float* out = A.out + (int64_t)blockIdx.y * A.split_stride;
-  Worker<TYPE, F, EDGE> w(A, n0, k0, t_end);
+  Worker<TYPE, F, EDGE> w(A, n0, k0, t_begin, t_end);
   if (t_begin < t_end) w.run(t_begin, lds);
   w.write(out);
 }
