@@ -57,42 +57,36 @@ __device__ __forceinline__ void split_parts(float (&v)[kVec], u32x4 (&part)[P]) 
 }
 template <int TYPE> constexpr int parts_of = TYPE == QA_F32 ? 3 : TYPE == QA_F16 ? 2 : 1;
 
-// Four waves, F x F tiles of 32 x 32 each: a work-group has 64 F columns of dY and as many of X.  While one pair of
+// WN x WK waves, FN x FK tiles of 32 x 32 each: a work-group has 32 WN FN columns of dY and 32 WK FK of X.  While one pair of
 // tiles is multiplied the next one's elements are on their way to registers, from where they go to LDS as bfloat16.
 // The order of a phase's instructions: everything else in the shadow of the matrix instructions.
-template <int TYPE, int F>
+template <int TYPE, int FN, int FK>
 __device__ __forceinline__ void interleave(int phase) {
   constexpr int kMatrix = 8, kVector = 2, kLdsRead = 0x100, kLdsWrite = 0x200, kRead = 0x20;
-  if (TYPE == QA_BF16 && F == 4) {
+  if (TYPE == QA_BF16 && FN * FK == 8) {
     if (phase == 0) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kVector, 7, 0);
-        if (i % 2) __builtin_amdgcn_sched_group_barrier(kLdsWrite, 1, 0);
-      }
+      for (int i = 0; i < 4; ++i) { __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0); __builtin_amdgcn_sched_group_barrier(kLdsRead, 3, 0); __builtin_amdgcn_sched_group_barrier(kVector, 4, 0); }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0); __builtin_amdgcn_sched_group_barrier(kVector, 10, 0); __builtin_amdgcn_sched_group_barrier(kLdsWrite, 1, 0); }
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kVector, 2, 0);
-        if (i % 2) __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
-      }
+      for (int i = 0; i < 8; ++i) { __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0); __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0); __builtin_amdgcn_sched_group_barrier(kVector, 2, 0); if (i % 2) __builtin_amdgcn_sched_group_barrier(kRead, 1, 0); }
     }
   }
   __builtin_amdgcn_sched_barrier(0);
 }
 
-template <int TYPE, int F, bool EDGE>
+template <int TYPE, int WN, int WK, int FN, int FK, bool EDGE>
 struct Worker {
   typedef ElemT<TYPE> T;
-  static constexpr int P = parts_of<TYPE>, kTile = 64 * F;
-  static constexpr int kDy = kStep * kTile / kVec / kThreads, kX = kStep * kTile / 16 / kThreads;   // vectors per thread
+  static constexpr int P = parts_of<TYPE>, kTile = 32 * WN * FN, kGroup = WN * WK * kWave;
+  static_assert(WN * FN == WK * FK, "tiles are square");
+  static constexpr int kDy = kStep * kTile / kVec / kGroup, kX = kStep * kTile / 16 / kGroup;       // vectors per thread
   static constexpr int kRow = kTile + kGap, kPart = kStep * kRow, kBuffer = (P + 1) * kPart;
   static constexpr int kBuffers = P == 1 ? 3 : 2;  // of 160 KiB
-  static constexpr int kAhead = P < 3 ? 2 : 1;     // steps whose elements are on their way: one is as long as half a read takes, or longer
+  // Steps whose elements are on their way.  A step of small tiles takes a third of the time that a read takes.
+  static constexpr int kAhead = FN * FK == 8 ? 2 : 4;
 
   const WeightGradArgs& A;
   int64_t n0, k0, t_end, t_load;
@@ -104,18 +98,19 @@ struct Worker {
   int left;                                        // columns of dY that this thread's vectors have
   int d_lane, x_lane;                              // where a lane reads in LDS
   struct Loaded { Raw8<TYPE> dy[kDy]; u32x4 code[kX]; uint32_t scale[kX]; };
-  f32x16 acc[F][F];
+  f32x16 acc[FN][FK];
 
-  static __device__ __forceinline__ int dy_row(int v) { return (v * kThreads + (int)threadIdx.x) / (kTile / kVec); }
-  static __device__ __forceinline__ int dy_chunk() { return threadIdx.x % (kTile / kVec); }
-  static __device__ __forceinline__ int x_row(int v) { return (v * kThreads + (int)threadIdx.x) / (kTile / 16); }
+  // Of both, so that a wave's 16-byte writes to LDS are side by side.
+  static __device__ __forceinline__ int row_of(int v) { return (v * kGroup + (int)threadIdx.x) / (kTile / kVec); }
+  static __device__ __forceinline__ int x_row(int v) { return (v * kGroup + (int)threadIdx.x) / (kTile / 16); }
   static __device__ __forceinline__ int x_chunk() { return threadIdx.x % (kTile / 16); }
+  static __device__ __forceinline__ int chunk() { return threadIdx.x % (kTile / kVec); }
 
   __device__ __forceinline__ Worker(const WeightGradArgs& a, int64_t n, int64_t k, int64_t begin, int64_t end)
       : A(a), n0(n), k0(k), t_end(end), t_load(begin) {
     // A vector that the end cuts off, or that lies past it, is the last eight columns instead: write() knows.  With fewer
     // than eight columns (EDGE) elements are read one by one.
-    const int64_t col = n0 + dy_chunk() * kVec;
+    const int64_t col = n0 + chunk() * kVec;
     left = (int)max((int64_t)0, min((int64_t)kVec, A.n - col));
     dy_from = (const char*)A.dy + begin * A.dy_stride * (int64_t)sizeof(T);
     x_from = A.codes + begin * A.R.code_stride;
@@ -127,8 +122,8 @@ struct Worker {
 #pragma unroll
     for (int v = 0; v < kDy; ++v) {
       const uint32_t stride = (uint32_t)(A.dy_stride * (int64_t)sizeof(T));
-      dy_at[v] = (uint32_t)dy_row(v) * stride + dy_col;
-      dy_tail[v] = (uint32_t)min(dy_row(v), last) * stride + dy_col;
+      dy_at[v] = (uint32_t)row_of(v) * stride + dy_col;
+      dy_tail[v] = (uint32_t)min(row_of(v), last) * stride + dy_col;
     }
 #pragma unroll
     for (int v = 0; v < kX; ++v) {
@@ -139,12 +134,12 @@ struct Worker {
     }
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int at = (8 * (lane / 32) + (lane % 16 >> 2)) * kRow + (lane & 16) + (lane & 3) * 4;
-    d_lane = at + (wave & 1) * 32 * F;
-    x_lane = at + (wave >> 1) * 32 * F;
+    d_lane = at + wave % WN * 32 * FN;
+    x_lane = at + wave / WN * 32 * FK;
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < FN; ++i)
 #pragma unroll
-      for (int j = 0; j < F; ++j) acc[i][j] = f32x16{};
+      for (int j = 0; j < FK; ++j) acc[i][j] = f32x16{};
   }
   // The next step's elements.  Rows past the end are read from the last one, steps past the end from the last step.
   __device__ __forceinline__ void load(Loaded& to) {
@@ -178,7 +173,7 @@ struct Worker {
       }
 #pragma unroll
       for (int p = 0; p < P; ++p)
-        *reinterpret_cast<u32x4*>(lds + p * kPart + dy_row(v) * kRow + dy_chunk() * kVec) = part[p];
+        *reinterpret_cast<u32x4*>(lds + p * kPart + row_of(v) * kRow + chunk() * kVec) = part[p];
     }
   }
   // X is 0 past the end.
@@ -203,24 +198,24 @@ struct Worker {
       }
     }
   }
-  // A step has 2 P phases of F x F matrix instructions, each for 16 rows and one part of dY.  A phase's operands are read
+  // A step has 2 P phases of FN x FK matrix instructions, each for 16 rows and one part of dY.  A phase's operands are read
   // while the one before it is multiplied, the first one's of the next step, too, where there are three buffers: the
   // one that is read next is complete then before the step begins.
-  bf16x8 d[2][F], x[2][F];
+  bf16x8 d[2][FN], x[2][FK];
   __device__ __forceinline__ void operands(const __bf16* lds, int phase) {
     const int s = phase / P, p = phase % P;
     if (p == 0) {
 #pragma unroll
-      for (int j = 0; j < F; ++j) x[s & 1][j] = eight_rows<kTile>(lds + x_lane + (P * kPart + 16 * s * kRow + 32 * j));
+      for (int j = 0; j < FK; ++j) x[s & 1][j] = eight_rows<kTile>(lds + x_lane + (P * kPart + 16 * s * kRow + 32 * j));
     }
 #pragma unroll
-    for (int i = 0; i < F; ++i) d[phase & 1][i] = eight_rows<kTile>(lds + d_lane + (p * kPart + 16 * s * kRow + 32 * i));
+    for (int i = 0; i < FN; ++i) d[phase & 1][i] = eight_rows<kTile>(lds + d_lane + (p * kPart + 16 * s * kRow + 32 * i));
   }
   __device__ __forceinline__ void multiply(int phase) {
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < FN; ++i)
 #pragma unroll
-      for (int j = 0; j < F; ++j)
+      for (int j = 0; j < FK; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d[phase & 1][i], x[phase / P & 1][j], acc[i][j], 0, 0, 0);
   }
   // One step: the buffer `now` is multiplied, what was loaded for the step that is kBuffers - 1 ahead goes to `last`.
@@ -236,28 +231,28 @@ struct Worker {
       }
       if (phase == 1) w.load(loaded);
       w.multiply(phase);
-      interleave<TYPE, F>(phase);
+      interleave<TYPE, FN, FK>(phase);
     }
     __syncthreads();
     if (kBuffers == 2) w.operands(next, 0);
   }
   __device__ __forceinline__ void run(int64_t t_begin, __bf16* lds) {
-    Loaded loaded[kAhead];
-#pragma unroll
-    for (int b = 0; b + 1 < kBuffers; ++b) {
-      load(loaded[b % kAhead]);
-      store_dy(loaded[b % kAhead], lds + b * kBuffer);
-      store_x(loaded[b % kAhead], lds + b * kBuffer, t_begin + b * kStep);
-    }
+    Loaded loaded[kAhead];                         // step i's in i % kAhead
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) load(loaded[a]);
+#pragma unroll
+    for (int b = 0; b + 1 < kBuffers; ++b) {
+      store_dy(loaded[b % kAhead], lds + b * kBuffer);
+      store_x(loaded[b % kAhead], lds + b * kBuffer, t_begin + b * kStep);
+      load(loaded[b % kAhead]);
+    }
     __syncthreads();
     int now = 0, next = kBuffer, last = (kBuffers - 1) * kBuffer;          // read, read next, written
     operands(lds, 0);
     for (int64_t t = t_begin; t < t_end;) {        // X is 0 in a step past the end
 #pragma unroll
       for (int a = 0; a < kAhead; ++a, t += kStep) {
-        step(*this, loaded[a], t, lds + now, lds + next, lds + last);
+        step(*this, loaded[(a + kBuffers - 1) % kAhead], t, lds + now, lds + next, lds + last);
         const int free = now;
         now = next;
         next = kBuffers == 2 ? free : last;
@@ -269,9 +264,9 @@ struct Worker {
   template <bool INSIDE, bool ADD>
   __device__ __forceinline__ void write(float* out) {
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int64_t n1 = n0 + (wave & 1) * 32 * F, k1 = k0 + (wave >> 1) * 32 * F + lane % 32;
+    const int64_t n1 = n0 + wave % WN * 32 * FN, k1 = k0 + wave / WN * 32 * FK + lane % 32;
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < FN; ++i)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int64_t first = n1 + 32 * i + 8 * q;
@@ -280,7 +275,7 @@ struct Worker {
 #pragma unroll
         for (int e = 0; e < 4; ++e, p += A.out_stride)
 #pragma unroll
-          for (int j = 0; j < F; ++j) {
+          for (int j = 0; j < FK; ++j) {
             if (!INSIDE && (n + e < first || n + e >= A.n || k1 + 32 * j >= A.R.cols)) continue;
             const float v = acc[i][j][4 * q + e];
             p[32 * j] = ADD ? p[32 * j] + v : v;
@@ -295,10 +290,11 @@ struct Worker {
   }
 };
 
-template <int TYPE, int F, bool EDGE>
-__global__ __launch_bounds__(kThreads) void weight_grad_kernel(WeightGradArgs A) {
-  __shared__ __bf16 lds[Worker<TYPE, F, EDGE>::kBuffers * Worker<TYPE, F, EDGE>::kBuffer];
-  constexpr int kTile = 64 * F;
+template <int TYPE, int WN, int WK, int FN, int FK, bool EDGE>
+__global__ __launch_bounds__(WN * WK * kWave) void weight_grad_kernel(WeightGradArgs A) {
+  typedef Worker<TYPE, WN, WK, FN, FK, EDGE> W;
+  __shared__ __bf16 lds[W::kBuffers * W::kBuffer];
+  constexpr int kTile = W::kTile;
   // Consecutive work-groups go to the eight dies in turn.  Each die takes tiles that lie together, eight of X beside each
   // other, so that its cache is asked for the same rows.
   const unsigned die = blockIdx.x % 8, each = gridDim.x / 8, more = gridDim.x % 8;
@@ -308,50 +304,103 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(WeightGradArgs A)
   const int64_t n0 = (int64_t)(in_band / wide) * kTile, k0 = (int64_t)(8 * band + in_band % wide) * kTile;
   const int64_t t_begin = (int64_t)blockIdx.y * A.piece, t_end = min(A.R.rows, t_begin + A.piece);
   float* out = A.out + (int64_t)blockIdx.y * A.split_stride;
-  Worker<TYPE, F, EDGE> w(A, n0, k0, t_begin, t_end);
+  W w(A, n0, k0, t_begin, t_end);
   if (t_begin < t_end) w.run(t_begin, lds);
   w.write(out);
 }
 
-// dW from the splits' sums, in their order.
+// dW from the splits' sums, in their order: a thread has four neighbouring elements, or, where there are few of them,
+// SHARE threads do, each with every SHARE-th split.
+template <int SHARE>
 __global__ __launch_bounds__(kThreads) void weight_grad_join_kernel(const float* __restrict__ parts, int splits, int64_t n, int64_t cols,
                                                                     float* dw, int64_t dw_stride, int accumulate) {
+  __shared__ f32x4 sums[SHARE][kThreads / SHARE];
   const int64_t all = n * cols;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
-    float s = splits ? parts[i] : 0.0f;
-    for (int k = 1; k < splits; ++k) s += parts[k * all + i];
-    float* p = dw + i / cols * dw_stride + i % cols;
-    *p = accumulate ? *p + s : s;
+  const int share = threadIdx.x / (kThreads / SHARE), lane = threadIdx.x % (kThreads / SHARE);
+  for (int64_t first = (int64_t)blockIdx.x * (kThreads / SHARE) * 4; first < all; first += (int64_t)gridDim.x * (kThreads / SHARE) * 4) {
+    const int64_t i = first + 4 * lane;
+    const int here = (int)max((int64_t)0, min((int64_t)4, all - i));
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (here == 4) {
+#pragma unroll 4
+      for (int k = share; k < splits; k += SHARE) s += *reinterpret_cast<const f32x4_at4*>(parts + k * all + i);
+    } else {
+      for (int k = share; k < splits; k += SHARE)
+        for (int e = 0; e < here; ++e) s[e] += parts[k * all + i + e];
+    }
+    if constexpr (SHARE > 1) {
+      __syncthreads();
+      sums[share][lane] = s;
+      __syncthreads();
+      if (share) continue;
+#pragma unroll
+      for (int k = 1; k < SHARE; ++k) s += sums[k][lane];
+    }
+    int64_t row = i / cols, col = i % cols;
+    for (int e = 0; e < here; ++e) {
+      float* p = dw + row * dw_stride + col;
+      *p = accumulate ? *p + s[e] : s[e];
+      if (++col == cols) col = 0, ++row;
+    }
   }
+}
+int join_launch(const float* parts, int64_t splits, int64_t n, int64_t cols, float* dw, int64_t dw_stride, int accumulate,
+                hipStream_t stream) {
+  constexpr int kShare = 16;
+  if (splits >= kShare && n * cols <= (int64_t)kThreads * 4 * 256) {
+    const dim3 grid((unsigned)ceil_div(n * cols, kThreads / kShare * 4));
+    weight_grad_join_kernel<kShare><<<grid, kThreads, 0, stream>>>(parts, (int)splits, n, cols, dw, dw_stride, accumulate);
+  } else {
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(n * cols, kThreads * 4), 4096));
+    weight_grad_join_kernel<1><<<grid, kThreads, 0, stream>>>(parts, (int)splits, n, cols, dw, dw_stride, accumulate);
+  }
+  return launch_status();
 }
 
 // ---- which form ----------------------------------------------------------------------------------------------
 
-// Tiles of 256 x 256 where they give every compute unit one, 128 x 128 otherwise.  Few tiles leave compute units idle:
-// the rows are split then, 256 at least to a split.
-struct Plan { int f; int64_t tiles_n, tiles, splits; };
-Plan plan_for(int64_t rows, int64_t cols, int64_t n) {
-  Plan p;
-  p.f = n >= kVec && ceil_div(n, 256) * ceil_div(cols, 256) >= 256 ? 4 : 2;
-  p.tiles_n = ceil_div(n, 64 * p.f);
-  p.tiles = p.tiles_n * ceil_div(cols, 64 * p.f);
-  p.splits = p.f == 4 ? 1 : std::max<int64_t>(1, std::min(ceil_div(1024, p.tiles), rows / 256));
-  return p;
+// Tiles of 256 x 256 or 128 x 128, and the rows whole or split: whichever is estimated to take the least time.  Measured
+// for a step of 32 rows and bfloat16: a 128-tile 0.38 us where it has its compute unit to itself, 0.65 where two share
+// one; a 256-tile 0.62 us where few run and 0.9 where all do, which the card's power bounds; times the parts of dY, but
+// for 0.1 of the small one's.  A round of work-groups takes 4 us more, and the splits' sums are written and read at
+// some 6 TB/s.  (2048 x 2048 columns, 16384 rows: 145 us with four splits of 256-tiles, 322 in one piece, 185 with two of
+// 128-tiles; 2048 rows: 40, 48 and 39, and 30 with 128-tiles in one piece.)
+struct Plan { int tile; int64_t tiles_n, tiles, splits; };
+Plan plan_for(int64_t rows, int64_t cols, int64_t n, int parts) {
+  Plan best = {};
+  double least = 0.0;
+  for (int tile = 128; tile <= 256; tile *= 2) {
+    if (tile == 256 && n < kVec) break;
+    const int64_t tiles_n = ceil_div(n, tile), tiles = tiles_n * ceil_div(cols, tile), at_once = tile == 256 ? 256 : 512;
+    for (int64_t splits = 1; splits <= 64 && (splits == 1 || splits * 64 <= rows); ++splits) {
+      const int64_t groups = tiles * splits, steps = ceil_div(ceil_div(rows, splits), kStep);
+      const double step = tile == 256 ? parts * (0.6 + 0.3 * (groups < 256 ? (double)groups / 256.0 : 1.0))
+                                      : 0.1 + parts * (groups <= 256 ? 0.28 : 0.55);
+      const double us = (double)ceil_div(groups, at_once) * ((double)steps * step + 4.0) +
+                        (splits > 1 ? 4.0 + (double)(2 * splits + 1) * (double)n * (double)cols * (4.0 / 6e6) : 0.0);
+      if (least == 0.0 || us < least) {
+        least = us;
+        best = {tile, tiles_n, tiles, splits};
+      }
+    }
+  }
+  return best;
 }
+int parts_for(int type) { return type == QA_F32 ? 3 : type == QA_F16 ? 2 : 1; }
 
 template <int TYPE>
 int weight_grad_launch(WeightGradArgs& A, const Plan& plan, hipStream_t stream) {
   const dim3 grid((unsigned)plan.tiles, (unsigned)plan.splits);
-  if (A.n < kVec) weight_grad_kernel<TYPE, 2, true><<<grid, kThreads, 0, stream>>>(A);
-  else if (plan.f == 4) weight_grad_kernel<TYPE, 4, false><<<grid, kThreads, 0, stream>>>(A);
-  else weight_grad_kernel<TYPE, 2, false><<<grid, kThreads, 0, stream>>>(A);
+  if (A.n < kVec) weight_grad_kernel<TYPE, 2, 2, 2, 2, true><<<grid, 256, 0, stream>>>(A);
+  else if (plan.tile == 256) weight_grad_kernel<TYPE, 2, 4, 4, 2, false><<<grid, 512, 0, stream>>>(A);
+  else weight_grad_kernel<TYPE, 2, 2, 2, 2, false><<<grid, 256, 0, stream>>>(A);
   return launch_status();
 }
 
 }  // namespace
 
-size_t weight_grad_workspace_bytes(const qa_coded_rows* R, int, int64_t n) {
-  const int64_t splits = plan_for(R->rows, R->cols, n).splits;
+size_t weight_grad_workspace_bytes(const qa_coded_rows* R, int type, int64_t n) {
+  const int64_t splits = plan_for(R->rows, R->cols, n, parts_for(type)).splits;
   return splits == 1 ? 0 : (size_t)splits * (size_t)n * (size_t)R->cols * sizeof(float);
 }
 
@@ -370,15 +419,13 @@ extern "C" int qa_rows_weight_grad(const qa_coded_rows* rows, const int8_t* code
   if (!aligned(dw, 4)) return QA_ERR_ALIGNMENT;
   const hipStream_t s = (hipStream_t)stream;
   const int64_t all = n * rows->cols;
-  const dim3 join((unsigned)std::min<int64_t>(ceil_div(all, kThreads), 4096));
   if (rows->rows == 0) {
     if (accumulate) return QA_OK;
-    weight_grad_join_kernel<<<join, kThreads, 0, s>>>(nullptr, 0, n, rows->cols, dw, dw_stride, 0);
-    return launch_status();
+    return join_launch(nullptr, 0, n, rows->cols, dw, dw_stride, 0, s);
   }
   if (!codes || !scales || !dy) return QA_ERR_INVALID_ARG;
   if (!element_aligned(dy, type) || !aligned(codes, 16)) return QA_ERR_ALIGNMENT;
-  const Plan plan = plan_for(rows->rows, rows->cols, n);
+  const Plan plan = plan_for(rows->rows, rows->cols, n, parts_for(type));
   const int64_t splits = plan.splits;
   WeightGradArgs A{*rows, codes, scales, dy, dw, dy_stride, dw_stride, 0, n, rows->rows, plan.tiles_n, accumulate};
   if (splits > 1) {
@@ -394,6 +441,5 @@ extern "C" int qa_rows_weight_grad(const qa_coded_rows* rows, const int8_t* code
            : type == QA_BF16 ? weight_grad_launch<QA_BF16>(A, plan, s)
                              : weight_grad_launch<QA_F16>(A, plan, s);
   if (rc || splits == 1) return rc;
-  weight_grad_join_kernel<<<join, kThreads, 0, s>>>((const float*)ws, (int)splits, n, rows->cols, dw, dw_stride, accumulate);
-  return launch_status();
+  return join_launch((const float*)ws, splits, n, rows->cols, dw, dw_stride, accumulate, s);
 }
