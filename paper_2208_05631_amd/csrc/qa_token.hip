@@ -87,7 +87,8 @@ __device__ __forceinline__ U sort_lanes(U v) {
   return v;
 }
 // The 64 largest of two sorted sequences, sorted; `reversed` holds the second one's value 63 - lane.
-__device__ __forceinline__ uint64_t merge_lanes(uint64_t v, uint64_t reversed) {
+template <typename U>
+__device__ __forceinline__ U merge_lanes(U v, U reversed) {
   const int lane = threadIdx.x % kWave;
   v = v > reversed ? v : reversed;
 #pragma unroll
@@ -162,31 +163,96 @@ __device__ __forceinline__ void write_row(const TokenArgs& A, int64_t row, const
   }
 }
 
-// One wave's share of a row: chunks of NV vectors per lane, `chunk`, `chunk` + waves, ... of [begin, end).
-template <int TYPE, int NV, bool TOP>
-__device__ __forceinline__ void read_chunks(const ElemT<TYPE>* x, int64_t begin, int64_t end, int chunk, int waves, int top,
-                                            uint64_t* wait, uint32_t* shared, Sums& a, Best& b) {
-  const int lane = threadIdx.x % kWave;
-  constexpr int kChunk = NV * kWave * kVec;
-  bool cold = true;
-  for (int64_t at = begin + (int64_t)chunk * kChunk; at < end; at += (int64_t)waves * kChunk) {
-    float v[NV][kVec], vmax[NV], m = -INFINITY;
-    Raw8<TYPE> raw[NV];
+// ---- a row, or a split of one, read by WAVES waves --------------------------------------------------------------------
+//
+// The waves take chunks of NV vectors per lane in turn.  Each lane has sums against a maximum of its own.  For the
+// alternatives it only notes a chunk's largest logit: at the row's end the `top`-th largest of the lanes' largest is a
+// bound that `top` logits reach, and the few chunks that reach it are read again.
+constexpr int kTokenWaves = 8, kTokenThreads = kTokenWaves * kWave;
+constexpr int kTokenVecs = 4;
+constexpr int64_t kTokenChunk = (int64_t)kTokenVecs * kTokenThreads * kVec;
+constexpr int kNoted = 12;                         // chunks per lane: longer rows are split
+constexpr int kFound = 256;                        // alternatives of all waves; what is more goes to the waves' own
+
+template <int WAVES, int CHUNKS, bool TOP>
+struct RowShared {
+  float most[TOP ? CHUNKS : 1][WAVES * kWave];
+  uint64_t found[TOP ? kFound : 1];
+  uint64_t wait[TOP ? WAVES : 1][kWaiting];
+  uint64_t lists[TOP ? WAVES : 1][kWave];          // also of the waves' bounds
+  Sums sums[WAVES];
+  uint32_t bounds[WAVES][2];
+  uint32_t count;
+};
+template <int WAVES>
+__device__ __forceinline__ void row_barrier() {
+  if constexpr (WAVES > 1) __syncthreads();
+  else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// The waves' sorted values merged into wave 0's.
+template <int WAVES, typename U, typename F>
+__device__ __forceinline__ U merge_waves(U v, U (*lists)[kWave], F merge) {
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int64_t i = at + (k * kWave + lane) * kVec;
-      raw[k] = load_raw<TYPE>(x + i, (int)max((int64_t)0, min((int64_t)kVec, end - i)), -INFINITY);
-    }
+  for (int w = 1; w < WAVES; w *= 2) {
+    if ((wave & (2 * w - 1)) == w) lists[wave][kWave - 1 - lane] = v;
+    row_barrier<WAVES>();
+    if ((wave & (2 * w - 1)) == 0) v = merge(v, lists[wave + w][lane]);
+  }
+  return v;
+}
+
+template <int TYPE, int NV>
+__device__ __forceinline__ void load_chunk(Raw8<TYPE> (&raw)[NV], const ElemT<TYPE>* x, int64_t at, int64_t end) {
+  const int lane = threadIdx.x % kWave;
+  const ElemT<TYPE>* p = x + at + lane * kVec;
+  if (at + NV * kWave * kVec <= end) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) raw[k] = load_raw<TYPE>(p + k * kWave * kVec);
+  } else {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      raw[k] = load_raw<TYPE>(p + k * kWave * kVec, (int)max((int64_t)0, min((int64_t)kVec, end - at - (k * kWave + lane) * kVec)), -INFINITY);
+  }
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
+__device__ __forceinline__ float most_of_eight(const float (&v)[kVec]) {
+  return max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), fmaxf(v[6], v[7]));
+}
+
+// The sums and alternatives of x[begin .. end); wave 0 receives them.  Ends with a barrier.
+template <int TYPE, int WAVES, int NV, int CHUNKS, bool TOP>
+__device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, int64_t end, int top,
+                                         RowShared<WAVES, CHUNKS, TOP>& shared, Sums& a, uint64_t& best) {
+  const int wave = WAVES > 1 ? threadIdx.x / kWave : 0, lane = threadIdx.x % kWave, me = wave * kWave + lane;
+  constexpr int64_t kChunk = NV * kWave * kVec, kStride = WAVES * kChunk;
+  a = no_sums();
+  float largest = -INFINITY;
+  const int64_t mine = begin + wave * kChunk;
+  Raw8<TYPE> raw[NV];
+  if (mine < end) load_chunk<TYPE, NV>(raw, x, mine, end);
+  int chunk = 0;
+  for (int64_t at = mine; at < end; at += kStride, ++chunk) {
+    float v[NV][kVec], most[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       to_f32<TYPE>(raw[k], v[k]);
-      vmax[k] = v[k][0];
-#pragma unroll
-      for (int i = 1; i < kVec; ++i) vmax[k] = fmaxf(vmax[k], v[k][i]);
-      m = fmaxf(m, vmax[k]);
+      most[k] = most_of_eight(v[k]);
     }
-    const float most = wave_max_f32(m);
-    if (most > a.m) raise(a, most);
+    if (at + kStride < end) load_chunk<TYPE, NV>(raw, x, at + kStride, end);
+    float m = most[0];
+#pragma unroll
+    for (int k = 1; k < NV; ++k) m = fmaxf(m, most[k]);
+    if constexpr (TOP) {
+      shared.most[chunk][me] = m;
+      largest = fmaxf(largest, m);
+    }
+    raise(a, fmaxf(a.m, m));
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -195,112 +261,125 @@ __device__ __forceinline__ void read_chunks(const ElemT<TYPE>* x, int64_t begin,
         a.s += e;
         a.w = __builtin_fmaf(e, fmaxf(t, kFar), a.w);
       }
-    if constexpr (TOP) {
-      // No alternative that is worse than `top` logits of any wave's can be one of the row's: in a wave's first chunk
-      // the lanes' largest are such logits, later its own alternatives, and the other waves share theirs.
-      uint32_t least = (uint32_t)(b.last >> 32);
-      if (cold) {
-        const uint32_t sorted = sort_lanes(ordered(m));
-        least = (uint32_t)__builtin_amdgcn_readlane((int)sorted, top - 1);
-      }
-      const uint32_t theirs = shared ? __hip_atomic_load(shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0u;
-      least = max(least, theirs);
-      const float bound = least ? from_ordered(least) : -INFINITY;
-      if (__any(!(m < bound))) {
+  }
+  a = over_lanes(a);
+  if (WAVES > 1 && lane == 0) shared.sums[wave] = a;
+  if constexpr (TOP) {
+    // The bound: `top` lanes have a logit of at least this value, and those that equal it lie before this place.  A NaN
+    // can have hidden what came before it: everything is looked at then.
+    const bool odd = __any(!(a.s == a.s));
+    const uint32_t value = ordered(largest);
+    auto merge32 = [](uint32_t v, uint32_t reversed) { return merge_lanes(v, reversed); };
+    uint32_t bound = merge_waves<WAVES, uint32_t>(sort_lanes(value), reinterpret_cast<uint32_t(*)[kWave]>(shared.lists), merge32);
+    bound = (uint32_t)__builtin_amdgcn_readlane((int)bound, top - 1);
+    if (WAVES > 1) {
+      if (threadIdx.x == 0) shared.bounds[0][0] = bound;
+      if (lane == 0) shared.bounds[wave][1] = odd;
+      row_barrier<WAVES>();
+      bound = shared.bounds[0][0];
+    }
+    bool all = WAVES > 1 ? false : odd;
+    if (WAVES > 1) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          if (!__any(!(vmax[k] < bound))) continue;
+      for (int w = 0; w < WAVES; ++w) all = all || shared.bounds[w][1];
+    }
+    if (all) bound = 0;
+    const float value_bound = bound ? from_ordered(bound) : -INFINITY;
+    Best b;
+    for (int c = 0; c < chunk; ++c) {
+      const bool here = all || !(shared.most[c][me] < value_bound);
+      if (!__any(here)) continue;
+      const int64_t at = mine + c * kStride;
+      load_chunk<TYPE, NV>(raw, x, at, end);
 #pragma unroll
-          for (int i = 0; i < kVec; ++i) {
-            const uint32_t o = ordered(v[k][i]);
-            const uint64_t key = key_of(o, (uint32_t)(at + (k * kWave + lane) * kVec + i));
-            const bool good = o >= least && key > b.last;
-            const uint64_t mask = __ballot(good);
-            if (!mask) continue;
-            if (good) wait[b.waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key;
-            b.waiting += __popcll(mask);
+      for (int k = 0; k < NV; ++k) {
+        float v[kVec];
+        to_f32<TYPE>(raw[k], v);
+        if (!__any(here && (all || !(most_of_eight(v) < value_bound)))) continue;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          const uint32_t o = ordered(v[i]);
+          const uint64_t key = key_of(o, (uint32_t)(at + (k * kWave + lane) * kVec + i));
+          const bool good = here && o >= bound && key > b.last;
+          const uint64_t mask = __ballot(good);
+          if (!mask) continue;
+          const int n = __popcll(mask);
+          const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+          uint32_t place = 0;
+          if (lane == 0) place = atomicAdd(&shared.count, (uint32_t)n);
+          place = (uint32_t)__builtin_amdgcn_readfirstlane((int)place);
+          if (place + n <= kFound) {
+            if (good) shared.found[place + rank] = key;
+          } else {
+            if (good) shared.wait[wave][b.waiting + rank] = key;
+            b.waiting += n;
             __builtin_amdgcn_wave_barrier();
-            if (b.waiting >= kWave) sort_in(b, wait, top);
+            if (b.waiting >= kWave) sort_in(b, shared.wait[wave], top);
           }
         }
       }
-      if (cold) {
-        cold = false;
-        sort_in(b, wait, top);
-        if (shared && lane == 0) atomicMax(shared, (uint32_t)(b.last >> 32));
-      }
+    }
+    if (b.waiting > 0) sort_in(b, shared.wait[wave], top);
+    row_barrier<WAVES>();
+    const uint32_t count = shared.count;
+    for (int i = wave * kWave; i < kFound && i < (int)count; i += WAVES * kWave)
+      b.sorted = merge_lanes(b.sorted, __shfl(sort_lanes(shared.found[i + lane]), kWave - 1 - lane, kWave));
+    if (count > kWave)
+      b.sorted = merge_waves<WAVES, uint64_t>(b.sorted, shared.lists, [](uint64_t v, uint64_t reversed) { return merge_lanes(v, reversed); });
+    best = b.sorted;
+  }
+  if constexpr (WAVES > 1) {
+    row_barrier<WAVES>();
+    if (wave == 0) {
+      Sums each = no_sums();
+      if (lane < WAVES) each = shared.sums[lane];
+      a = over_lanes(each);
     }
   }
+  row_barrier<WAVES>();
+}
+// What read_row() finds in LDS.
+template <int WAVES, int CHUNKS, bool TOP>
+__device__ __forceinline__ void begin_row(RowShared<WAVES, CHUNKS, TOP>& shared) {
   if constexpr (TOP) {
-    if (b.waiting > 0) sort_in(b, wait, top);
+    for (int i = threadIdx.x % (WAVES * kWave); i < kFound; i += WAVES * kWave) shared.found[i] = 0;
+    if (threadIdx.x % (WAVES * kWave) == 0) shared.count = 0;
+    row_barrier<WAVES>();
   }
 }
 
 // A wave per row, four rows per work-group.
-template <int TYPE, int NV, bool TOP>
+template <int TYPE, int NV, int CHUNKS, bool TOP>
 __global__ __launch_bounds__(kThreads) void token_narrow_kernel(TokenArgs A) {
-  __shared__ uint64_t wait[TOP ? kWaves : 1][kWaiting];
+  __shared__ RowShared<1, CHUNKS, TOP> shared[kWaves];
   const int wave = threadIdx.x / kWave;
   for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < A.rows; row += (int64_t)gridDim.x * kWaves) {
-    Sums a = no_sums();
-    Best b;
-    read_chunks<TYPE, NV, TOP>((const ElemT<TYPE>*)A.x + row * A.stride, 0, A.vocab, 0, 1, A.top, wait[TOP ? wave : 0], nullptr, a, b);
-    write_row<TYPE, TOP>(A, row, over_lanes(a), b.sorted);
+    Sums a;
+    uint64_t best = 0;
+    begin_row(shared[wave]);
+    read_row<TYPE, 1, NV, CHUNKS, TOP>((const ElemT<TYPE>*)A.x + row * A.stride, 0, A.vocab, A.top, shared[wave], a, best);
+    write_row<TYPE, TOP>(A, row, a, best);
   }
-}
-
-constexpr int kTokenWaves = 8, kTokenThreads = kTokenWaves * kWave;
-
-// The row's (or the split's) sums and alternatives from its waves'; wave 0 receives them.
-template <bool TOP>
-__device__ __forceinline__ void over_waves(Sums& a, Best& b, Sums* sums, uint64_t (*lists)[kWave]) {
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  a = over_lanes(a);
-  if (lane == 0) sums[wave] = a;
-  if constexpr (TOP) {
-#pragma unroll
-    for (int w = 1; w < kTokenWaves; w *= 2) {
-      if ((wave & (2 * w - 1)) == w) lists[wave][kWave - 1 - lane] = b.sorted;
-      __syncthreads();
-      if ((wave & (2 * w - 1)) == 0) b.sorted = merge_lanes(b.sorted, lists[wave + w][lane]);
-    }
-  } else {
-    __syncthreads();
-  }
-  if (wave == 0) {
-    Sums each = no_sums();
-    if (lane < kTokenWaves) each = sums[lane];
-    a = over_lanes(each);
-  }
-  __syncthreads();
 }
 
 // A work-group per row, or per split of a row.
 template <int TYPE, int NV, bool TOP>
 __global__ __launch_bounds__(kTokenThreads) void token_wide_kernel(TokenArgs A) {
-  __shared__ uint64_t wait[TOP ? kTokenWaves : 1][kWaiting];
-  __shared__ uint64_t lists[TOP ? kTokenWaves : 1][kWave];
-  __shared__ Sums sums[kTokenWaves];
-  __shared__ uint32_t shared;
+  __shared__ RowShared<kTokenWaves, kNoted, TOP> shared;
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
   const int64_t begin = (int64_t)blockIdx.y * A.piece, end = min(A.vocab, begin + A.piece);
   for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
-    if constexpr (TOP) {
-      if (threadIdx.x == 0) shared = 0;
-      __syncthreads();
-    }
-    Sums a = no_sums();
-    Best b;
-    read_chunks<TYPE, NV, TOP>((const ElemT<TYPE>*)A.x + row * A.stride, begin, end, wave, kTokenWaves, A.top,
-                               wait[TOP ? wave : 0], &shared, a, b);
-    over_waves<TOP>(a, b, sums, lists);
+    Sums a;
+    uint64_t best = 0;
+    begin_row(shared);
+    read_row<TYPE, kTokenWaves, NV, kNoted, TOP>((const ElemT<TYPE>*)A.x + row * A.stride, begin, end, A.top, shared, a, best);
     if (wave == 0) {
       if (A.splits == 1) {
-        write_row<TYPE, TOP>(A, row, a, b.sorted);
+        write_row<TYPE, TOP>(A, row, a, best);
       } else {
         const int64_t part = row * A.splits + blockIdx.y;
         if (lane == 0) *reinterpret_cast<f32x4*>(A.part_sums + 4 * part) = f32x4{a.m, a.s, a.w, 0.0f};
-        if (TOP && lane < A.top) A.part_best[part * A.top + lane] = b.sorted;
+        if (TOP && lane < A.top) A.part_best[part * A.top + lane] = best;
       }
     }
   }
@@ -312,27 +391,36 @@ __global__ __launch_bounds__(kTokenThreads) void token_join_kernel(TokenArgs A) 
   __shared__ uint64_t lists[TOP ? kTokenWaves : 1][kWave];
   __shared__ Sums sums[kTokenWaves];
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
-    Sums a = no_sums();
-    Best b;
-    if ((int)threadIdx.x < A.splits) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(A.part_sums + 4 * (row * A.splits + threadIdx.x));
-      a.m = v[0];
-      a.s = v[1];
-      a.w = v[2];
+  const int64_t row = blockIdx.x;
+  Sums a = no_sums();
+  for (int i = threadIdx.x; i < A.splits; i += kTokenThreads) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(A.part_sums + 4 * (row * A.splits + i));
+    Sums b{v[0], v[1], v[2]};
+    const float m = fmaxf(a.m, b.m);
+    raise(a, m);
+    raise(b, m);
+    a.s += b.s;
+    a.w += b.w;
+  }
+  a = over_lanes(a);
+  if (lane == 0) sums[wave] = a;
+  uint64_t best = 0;
+  if constexpr (TOP) {
+    uint64_t last = 0;
+    for (int i = wave; i < A.splits; i += kTokenWaves) {
+      const int from = kWave - 1 - lane;
+      const uint64_t v = from < A.top ? A.part_best[(row * A.splits + i) * A.top + from] : 0;
+      if (!__any(v > last)) continue;
+      best = merge_lanes(best, v);
+      last = lane_u64(best, A.top - 1);
     }
-    if constexpr (TOP) {
-      for (int i = wave; i < A.splits; i += kTokenWaves) {
-        const int from = kWave - 1 - lane;
-        const uint64_t v = from < A.top ? A.part_best[(row * A.splits + i) * A.top + from] : 0;
-        if (__any(v > b.last)) {
-          b.sorted = merge_lanes(b.sorted, v);
-          b.last = lane_u64(b.sorted, A.top - 1);
-        }
-      }
-    }
-    over_waves<TOP>(a, b, sums, lists);
-    if (wave == 0) write_row<TYPE, TOP>(A, row, a, b.sorted);
+    best = merge_waves<kTokenWaves, uint64_t>(best, lists, [](uint64_t v, uint64_t reversed) { return merge_lanes(v, reversed); });
+  }
+  __syncthreads();
+  if (wave == 0) {
+    Sums each = no_sums();
+    if (lane < kTokenWaves) each = sums[lane];
+    write_row<TYPE, TOP>(A, row, over_lanes(each), best);
   }
 }
 
@@ -396,24 +484,25 @@ constexpr int64_t kNarrow = 4096;                  // logits of a row that one w
 constexpr int64_t kSplitLogits = kTokenThreads * kVec;       // one vector per lane
 
 int64_t splits_for(int64_t rows, int64_t vocab) {
-  if (vocab <= kNarrow || rows >= 512) return 1;
-  return std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), kTokenThreads), ceil_div(1024, rows));
+  if (vocab <= kNarrow) return 1;
+  const int64_t least = ceil_div(vocab, kNoted * kTokenChunk);
+  if (rows >= 512) return least;
+  return std::max(least, std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), kTokenThreads), ceil_div(1024, rows)));
 }
 
 template <int TYPE, bool TOP>
 int token_launch(TokenArgs& A, hipStream_t stream) {
   const dim3 narrow((unsigned)std::min<int64_t>(ceil_div(A.rows, kWaves), 1 << 16));
   if (A.vocab <= 512) {
-    token_narrow_kernel<TYPE, 1, TOP><<<narrow, kThreads, 0, stream>>>(A);
+    token_narrow_kernel<TYPE, 1, 1, TOP><<<narrow, kThreads, 0, stream>>>(A);
   } else if (A.vocab <= kNarrow) {
-    token_narrow_kernel<TYPE, 4, TOP><<<narrow, kThreads, 0, stream>>>(A);
-  } else if (A.splits == 1) {
-    A.piece = A.vocab;
-    token_wide_kernel<TYPE, 4, TOP><<<dim3((unsigned)std::min<int64_t>(A.rows, 1 << 16)), kTokenThreads, 0, stream>>>(A);
+    token_narrow_kernel<TYPE, 4, 2, TOP><<<narrow, kThreads, 0, stream>>>(A);
   } else {
+    const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 16), (unsigned)A.splits);
     A.piece = ceil_div(ceil_div(A.vocab, A.splits), kSplitLogits) * kSplitLogits;
-    const dim3 grid((unsigned)A.rows, (unsigned)A.splits);
-    token_wide_kernel<TYPE, 1, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
+    if (A.piece <= kNoted * kSplitLogits) token_wide_kernel<TYPE, 1, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
+    else token_wide_kernel<TYPE, kTokenVecs, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
+    if (A.splits == 1) return launch_status();
     if (const int rc = launch_status()) return rc;
     token_join_kernel<TYPE, TOP><<<dim3((unsigned)A.rows), kTokenThreads, 0, stream>>>(A);
   }
