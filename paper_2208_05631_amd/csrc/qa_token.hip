@@ -9,6 +9,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kFar = -1e4f;                      // 2^kFar is 0
+constexpr int kDppQuadReverse = 0x1B;               // quad_perm:[3,2,1,0]
 constexpr int kTop = QA_TOP_MAX;                   // a lane for each alternative
 static_assert(kTop == kWave, "the alternatives of a row are held one per lane");
 
@@ -68,32 +69,48 @@ __device__ __forceinline__ float from_ordered(uint32_t o) {
 }
 __device__ __forceinline__ uint64_t key_of(uint32_t order, uint32_t index) { return (uint64_t)order << 32 | (uint32_t)~index; }
 
-template <typename U>
-__device__ __forceinline__ U other_lane(U v, int mask) { return __shfl_xor(v, mask, kWave); }
-template <typename U>
-__device__ __forceinline__ U merge_step(U v, int stride, bool larger) {
-  const U o = other_lane(v, stride);
-  return (v > o) == larger ? v : o;
+// The value of the lane whose number differs in `STRIDE` alone.  Up to 8 two moves between neighbours do it, a tenth of
+// the time that a way through LDS takes; rows of 16 lanes are swapped with their neighbours.
+template <int STRIDE>
+__device__ __forceinline__ uint32_t other_lane(uint32_t v) {
+  const int i = (int)v;
+  if constexpr (STRIDE == 1) return (uint32_t)dpp_i32<kDppQuadXor1>(i);
+  if constexpr (STRIDE == 2) return (uint32_t)dpp_i32<kDppQuadXor2>(i);
+  if constexpr (STRIDE == 4) return (uint32_t)dpp_i32<kDppQuadReverse>(dpp_i32<kDppRowHalfMirror>(i));
+  if constexpr (STRIDE == 8) return (uint32_t)dpp_i32<kDppRowHalfMirror>(dpp_i32<kDppRowMirror>(i));
+  if constexpr (STRIDE == 16) {
+    const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? both[0] : both[1];
+  }
+  if constexpr (STRIDE == 32) {
+    const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? both[0] : both[1];
+  }
+}
+template <int STRIDE>
+__device__ __forceinline__ uint64_t other_lane(uint64_t v) {
+  return (uint64_t)other_lane<STRIDE>((uint32_t)(v >> 32)) << 32 | other_lane<STRIDE>((uint32_t)v);
+}
+template <int SIZE, int STRIDE, typename U>
+__device__ __forceinline__ U merge_steps(U v) {
+  const int lane = threadIdx.x % kWave;
+  const U o = other_lane<STRIDE>(v);
+  const bool larger = ((lane & STRIDE) == 0) == ((lane & SIZE) == 0);
+  v = (v > o) == larger ? v : o;
+  if constexpr (STRIDE > 1) v = merge_steps<SIZE, STRIDE / 2>(v);
+  return v;
 }
 // The wave's 64 values, the largest in lane 0.
-template <typename U>
+template <typename U, int SIZE = 2>
 __device__ __forceinline__ U sort_lanes(U v) {
-  const int lane = threadIdx.x % kWave;
-#pragma unroll
-  for (int size = 2; size <= kWave; size *= 2)
-#pragma unroll
-    for (int stride = size / 2; stride >= 1; stride /= 2)
-      v = merge_step(v, stride, ((lane & stride) == 0) == ((lane & size) == 0));
+  v = merge_steps<SIZE, SIZE / 2>(v);
+  if constexpr (SIZE < kWave) v = sort_lanes<U, 2 * SIZE>(v);
   return v;
 }
 // The 64 largest of two sorted sequences, sorted; `reversed` holds the second one's value 63 - lane.
 template <typename U>
 __device__ __forceinline__ U merge_lanes(U v, U reversed) {
-  const int lane = threadIdx.x % kWave;
-  v = v > reversed ? v : reversed;
-#pragma unroll
-  for (int stride = kWave / 2; stride >= 1; stride /= 2) v = merge_step(v, stride, (lane & stride) == 0);
-  return v;
+  return merge_steps<kWave, kWave / 2>(v > reversed ? v : reversed);
 }
 __device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
@@ -168,10 +185,10 @@ __device__ __forceinline__ void write_row(const TokenArgs& A, int64_t row, const
 // The waves take chunks of NV vectors per lane in turn.  Each lane has sums against a maximum of its own.  For the
 // alternatives it only notes a chunk's largest logit: at the row's end the `top`-th largest of the lanes' largest is a
 // bound that `top` logits reach, and the few chunks that reach it are read again.
-constexpr int kTokenWaves = 8, kTokenThreads = kTokenWaves * kWave;
+constexpr int kTokenWaves = 4, kTokenThreads = kTokenWaves * kWave;
 constexpr int kTokenVecs = 4;
 constexpr int64_t kTokenChunk = (int64_t)kTokenVecs * kTokenThreads * kVec;
-constexpr int kNoted = 12;                         // chunks per lane: longer rows are split
+constexpr int kNoted = 24;                         // chunks per lane: longer rows are split
 constexpr int kFound = 256;                        // alternatives of all waves; what is more goes to the waves' own
 
 template <int WAVES, int CHUNKS, bool TOP>
@@ -487,7 +504,7 @@ int64_t splits_for(int64_t rows, int64_t vocab) {
   if (vocab <= kNarrow) return 1;
   const int64_t least = ceil_div(vocab, kNoted * kTokenChunk);
   if (rows >= 512) return least;
-  return std::max(least, std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), kTokenThreads), ceil_div(1024, rows)));
+  return std::max(least, std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), 512), ceil_div(1024, rows)));
 }
 
 template <int TYPE, bool TOP>
