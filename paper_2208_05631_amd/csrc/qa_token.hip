@@ -192,20 +192,20 @@ __device__ __forceinline__ void write_row(const TokenArgs& A, int64_t row, const
 // alternatives it only notes a chunk's largest logit: at the row's end the `top`-th largest of the lanes' largest is a
 // bound that `top` logits reach, and the few chunks that reach it are read again.
 constexpr int kTokenWaves = 4, kTokenThreads = kTokenWaves * kWave;
-constexpr int kTokenVecs = 4;
+constexpr int kTokenVecs = 2;
 constexpr int64_t kTokenChunk = (int64_t)kTokenVecs * kTokenThreads * kVec;
-constexpr int kNoted = 24;                         // chunks per lane: longer rows are split
+constexpr int kNoted = 48;                         // chunks per lane: longer rows are split
 constexpr int kFound = 256;                        // alternatives of all waves; what is more goes to the waves' own
 
 template <int WAVES, int CHUNKS, bool TOP>
 struct RowShared {
-  float most[TOP ? CHUNKS + 1 : 1][WAVES * kWave];  // a row that begins inside 16 bytes has one more
+  uint16_t most[TOP ? CHUNKS + 1 : 1][WAVES * kWave];      // a row that begins inside 16 bytes has one more
   uint32_t largest[WAVES][kWave];
   uint64_t found[TOP ? kFound : 1];
   uint64_t wait[TOP ? WAVES : 1][kWaiting];
   uint64_t lists[TOP ? WAVES : 1][kWave];
   Sums sums[WAVES];
-  uint32_t count;
+  uint32_t count, bound;
 };
 template <int WAVES>
 __device__ __forceinline__ void row_barrier() {
@@ -284,7 +284,7 @@ __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, in
 #pragma unroll
     for (int k = 1; k < NV; ++k) m = fmaxf(m, most[k]);
     if constexpr (TOP) {
-      shared.most[chunks][me] = m;
+      shared.most[chunks][me] = (uint16_t)(as_u32(m) >> 16);
       largest = fmaxf(largest, m);
     }
     raise(a, fmaxf(a.m, m));
@@ -311,31 +311,39 @@ __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, in
   if constexpr (TOP) {
     // `top` lanes have a logit of at least this bound, to 16 bits.  A NaN can have hidden what came before it:
     // everything is looked at then.
-    uint32_t values[WAVES], bound = 0;
+    uint32_t bound = 0;
+    if (wave == 0) {
+      uint32_t values[WAVES];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) values[w] = WAVES > 1 ? shared.largest[w][lane] : ordered(largest);
+      for (int w = 0; w < WAVES; ++w) values[w] = WAVES > 1 ? shared.largest[w][lane] : ordered(largest);
 #pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
-      const uint32_t higher = bound | 1u << bit;
-      int n = 0;
+      for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t higher = bound | 1u << bit;
+        int n = 0;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) n += __popcll(__ballot(values[w] >= higher));
-      bound = n >= top ? higher : bound;
+        for (int w = 0; w < WAVES; ++w) n += __popcll(__ballot(values[w] >= higher));
+        bound = n >= top ? higher : bound;
+      }
+      if (WAVES > 1 && lane == 0) shared.bound = bound;
+    }
+    if constexpr (WAVES > 1) {
+      row_barrier<WAVES>();
+      bound = (uint32_t)__builtin_amdgcn_readfirstlane((int)shared.bound);
     }
     if (all || bound <= 0x007FFFFFu) bound = 0;
     const float least = bound ? from_ordered(bound) : -INFINITY;
-    uint32_t chosen = 0;                           // chunks with a lane that reaches it
-    for (int c = 0; c < chunks; ++c) chosen |= (uint32_t)(__any(all || !(shared.most[c][me] < least)) != 0) << c;
+    uint64_t chosen = 0;                           // chunks with a lane that reaches it
+    for (int c = 0; c < chunks; ++c)               // 16 bits of a bound of 16 bits: the comparison is that of the whole numbers
+      chosen |= (uint64_t)(__any(all || !(as_f32((uint32_t)shared.most[c][me] << 16) < least)) != 0) << c;
     Best b;
-    if (chosen) load_chunk<TYPE, NV>(raw, x, mine + (__ffs(chosen) - 1) * kStride, begin, end);
+    if (chosen) load_chunk<TYPE, NV>(raw, x, mine + __builtin_ctzll(chosen) * kStride, begin, end);
     while (chosen) {
-      const int c = __ffs(chosen) - 1;
+      const int64_t at = mine + __builtin_ctzll(chosen) * kStride;
       chosen &= chosen - 1;
-      const int64_t at = mine + c * kStride;
       float v[NV][kVec];
 #pragma unroll
       for (int k = 0; k < NV; ++k) to_f32<TYPE>(raw[k], v[k]);
-      if (chosen) load_chunk<TYPE, NV>(raw, x, mine + (__ffs(chosen) - 1) * kStride, begin, end);
+      if (chosen) load_chunk<TYPE, NV>(raw, x, mine + __builtin_ctzll(chosen) * kStride, begin, end);
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -534,11 +542,11 @@ int token_launch(TokenArgs& A, hipStream_t stream) {
   if (A.vocab <= 512) {
     token_narrow_kernel<TYPE, 1, 1, TOP><<<narrow, kThreads, 0, stream>>>(A);
   } else if (A.vocab <= kNarrow) {
-    token_narrow_kernel<TYPE, 4, 2, TOP><<<narrow, kThreads, 0, stream>>>(A);
+    token_narrow_kernel<TYPE, kTokenVecs, 4, TOP><<<narrow, kThreads, 0, stream>>>(A);
   } else {
     const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 16), (unsigned)A.splits);
     A.piece = ceil_div(ceil_div(A.vocab, A.splits), kSplitLogits) * kSplitLogits;
-    if (A.piece <= kNoted * kSplitLogits) token_wide_kernel<TYPE, 1, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
+    if (A.splits > 1 && A.piece <= kNoted * kSplitLogits) token_wide_kernel<TYPE, 1, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
     else token_wide_kernel<TYPE, kTokenVecs, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
     if (A.splits == 1) return launch_status();
     if (const int rc = launch_status()) return rc;
