@@ -258,6 +258,67 @@ __device__ __forceinline__ float most_of_eight(const float (&v)[kVec]) {
   return max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), fmaxf(v[6], v[7]));
 }
 
+// The largest number of 16 leading bits that `top` of the wave's values reach.
+template <int N>
+__device__ __forceinline__ uint32_t bound_of(const uint32_t (&values)[N], int top) {
+  uint32_t bound = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t higher = bound | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < N; ++w) n += __popcll(__ballot(values[w] >= higher));
+    bound = n >= top ? higher : bound;
+  }
+  return bound;
+}
+// The wave's good keys join those found, or, once there is no room, its own.
+template <typename S>
+__device__ __forceinline__ void offer(S& shared, int wave, Best& b, uint64_t key, bool good, int top) {
+  const int lane = threadIdx.x % kWave;
+  const uint64_t mask = __ballot(good);
+  if (!mask) return;
+  const int n = __popcll(mask);
+  const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+  uint32_t place = 0;
+  if (lane == 0) place = atomicAdd(&shared.count, (uint32_t)n);
+  place = (uint32_t)__builtin_amdgcn_readfirstlane((int)place);
+  if (place + n <= kFound) {
+    if (good) shared.found[place + rank] = key;
+  } else {
+    if (place + lane < kFound) shared.found[place + lane] = 0;
+    if (good) shared.wait[wave][b.waiting + rank] = key;
+    b.waiting += n;
+    __builtin_amdgcn_wave_barrier();
+    if (b.waiting >= kWave) sort_in(b, shared.wait[wave], top);
+  }
+}
+// The 64 best of what was offered, for wave 0.  Begins and ends with a barrier.
+template <int WAVES, typename S>
+__device__ __forceinline__ uint64_t settle(S& shared, int wave, Best& b, int top) {
+  const int lane = threadIdx.x % kWave;
+  uint64_t best = 0;
+  if (b.waiting > 0) sort_in(b, shared.wait[wave], top);
+  row_barrier<WAVES>();
+  const int count = (int)shared.count;
+  if (count <= kWave) {
+    if (wave == 0) {                               // each goes to the place that as many better ones leave it
+      const uint64_t key = lane < count ? shared.found[lane] : 0;
+      int better = 0;
+      for (int i = 0; i < count; ++i) better += lane_u64(key, i) > key;
+      if (lane < count) shared.lists[0][better] = key;
+      row_barrier<1>();
+      best = lane < count ? shared.lists[0][lane] : 0;
+    }
+  } else {
+    for (int i = wave * kWave; i < kFound && i < count; i += WAVES * kWave)
+      b.sorted = merge_lanes(b.sorted, __shfl(sort_lanes(i + lane < count ? shared.found[i + lane] : (uint64_t)0), kWave - 1 - lane, kWave));
+    best = merge_waves<WAVES>(b.sorted, shared.lists);
+  }
+  row_barrier<WAVES>();
+  return best;
+}
+
 // The sums and alternatives of x[begin .. end); wave 0 receives them.  Ends with a barrier.
 template <int TYPE, int WAVES, int NV, int CHUNKS, bool TOP>
 __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, int64_t end, int top,
@@ -316,14 +377,7 @@ __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, in
       uint32_t values[WAVES];
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) values[w] = WAVES > 1 ? shared.largest[w][lane] : ordered(largest);
-#pragma unroll
-      for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t higher = bound | 1u << bit;
-        int n = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) n += __popcll(__ballot(values[w] >= higher));
-        bound = n >= top ? higher : bound;
-      }
+      bound = bound_of(values, top);
       if (WAVES > 1 && lane == 0) shared.bound = bound;
     }
     if constexpr (WAVES > 1) {
@@ -352,42 +406,10 @@ __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, in
           const int64_t index = at + (k * kWave + lane) * kVec + i;
           const uint64_t key = key_of(ordered(v[k][i]), (uint32_t)index);
           const bool good = !(v[k][i] < least) && key > b.last && index >= begin && index < end;
-          const uint64_t mask = __ballot(good);
-          if (!mask) continue;
-          const int n = __popcll(mask);
-          const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-          uint32_t place = 0;
-          if (lane == 0) place = atomicAdd(&shared.count, (uint32_t)n);
-          place = (uint32_t)__builtin_amdgcn_readfirstlane((int)place);
-          if (place + n <= kFound) {
-            if (good) shared.found[place + rank] = key;
-          } else {
-            if (place + lane < kFound) shared.found[place + lane] = 0;
-            if (good) shared.wait[wave][b.waiting + rank] = key;
-            b.waiting += n;
-            __builtin_amdgcn_wave_barrier();
-            if (b.waiting >= kWave) sort_in(b, shared.wait[wave], top);
-          }
+          offer(shared, wave, b, key, good, top);
         }
     }
-    if (b.waiting > 0) sort_in(b, shared.wait[wave], top);
-    row_barrier<WAVES>();
-    const int count = (int)shared.count;
-    if (count <= kWave) {
-      if (wave == 0) {                             // each goes to the place that as many better ones leave it
-        const uint64_t key = lane < count ? shared.found[lane] : 0;
-        int better = 0;
-        for (int i = 0; i < count; ++i) better += lane_u64(key, i) > key;
-        if (lane < count) shared.lists[0][better] = key;
-        row_barrier<1>();
-        best = lane < count ? shared.lists[0][lane] : 0;
-      }
-    } else {
-      for (int i = wave * kWave; i < kFound && i < count; i += WAVES * kWave)
-        b.sorted = merge_lanes(b.sorted, __shfl(sort_lanes(i + lane < count ? shared.found[i + lane] : (uint64_t)0), kWave - 1 - lane, kWave));
-      best = merge_waves<WAVES>(b.sorted, shared.lists);
-    }
-    row_barrier<WAVES>();
+    best = settle<WAVES>(shared, wave, b, top);
   }
 }
 
@@ -429,15 +451,27 @@ __global__ __launch_bounds__(kTokenThreads, 4) void token_wide_kernel(TokenArgs 
   }
 }
 
-// A row's splits put together.
+// A row's splits put together: as a row is from its chunks, with the splits' best alternatives for the lanes' largest.
+constexpr int kMostSplits = 512;
 template <int TYPE, bool TOP>
 __global__ __launch_bounds__(kTokenThreads) void token_join_kernel(TokenArgs A) {
-  __shared__ uint64_t lists[TOP ? kTokenWaves : 1][kWave];
-  __shared__ Sums sums[kTokenWaves];
+  __shared__ RowShared<kTokenWaves, 0, TOP> shared;
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
   const int64_t row = blockIdx.x;
+  const uint64_t* keys = TOP ? A.part_best + row * A.splits * A.top : nullptr;
   Given given{0.0f, false};
   if (wave == 0) given = given_of<TYPE>(A, row);
+  if (TOP && threadIdx.x == 0) shared.count = 0;
+  if (TOP && wave == 0) {
+    uint32_t values[kMostSplits / kWave];
+#pragma unroll
+    for (int i = 0; i < kMostSplits / kWave; ++i) {
+      const int split = i * kWave + lane;
+      values[i] = split < A.splits ? (uint32_t)(keys[(int64_t)split * A.top] >> 32) : 0;
+    }
+    const uint32_t bound = bound_of(values, A.top);
+    if (lane == 0) shared.bound = bound;
+  }
   Sums a = no_sums();
   for (int i = threadIdx.x; i < A.splits; i += kTokenThreads) {
     const f32x4 v = *reinterpret_cast<const f32x4*>(A.part_sums + 4 * (row * A.splits + i));
@@ -449,23 +483,23 @@ __global__ __launch_bounds__(kTokenThreads) void token_join_kernel(TokenArgs A) 
     a.w += b.w;
   }
   a = over_lanes(a);
-  if (lane == 0) sums[wave] = a;
+  if (lane == 0) shared.sums[wave] = a;
+  __syncthreads();
   uint64_t best = 0;
   if constexpr (TOP) {
-    uint64_t last = 0;
-    for (int i = wave; i < A.splits; i += kTokenWaves) {
-      const int from = kWave - 1 - lane;
-      const uint64_t v = from < A.top ? A.part_best[(row * A.splits + i) * A.top + from] : 0;
-      if (!__any(v > last)) continue;
-      best = merge_lanes(best, v);
-      last = lane_u64(best, A.top - 1);
+    const uint64_t least = (uint64_t)shared.bound << 32;
+    const int all = A.splits * A.top;
+    Best b;
+    for (int first = 0; first < all; first += kTokenThreads) {
+      const int i = first + (int)threadIdx.x;
+      const uint64_t key = i < all ? keys[i] : 0;
+      offer(shared, wave, b, key, key >= least && key > b.last, A.top);
     }
-    best = merge_waves<kTokenWaves>(best, lists);
+    best = settle<kTokenWaves>(shared, wave, b, A.top);
   }
-  __syncthreads();
   if (wave == 0) {
     Sums each = no_sums();
-    if (lane < kTokenWaves) each = sums[lane];
+    if (lane < kTokenWaves) each = shared.sums[lane];
     write_row<TOP>(A, row, given, over_lanes(each), best);
   }
 }
@@ -533,7 +567,7 @@ int64_t splits_for(int64_t rows, int64_t vocab) {
   if (vocab <= kNarrow) return 1;
   const int64_t least = ceil_div(vocab, kNoted * kTokenChunk);
   if (rows >= 512) return least;
-  return std::max(least, std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), 512), ceil_div(1024, rows)));
+  return std::max(least, std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), kMostSplits), ceil_div(1024, rows)));
 }
 
 template <int TYPE, bool TOP>
