@@ -173,7 +173,7 @@ struct NormGradArgs {
   const float* rstd;
   const void* dh;
   void* dx;
-  float* parts;                                    // sums over the rows of one work-group or wave; NULL: not wanted
+  float* parts;                                    // sums over the rows of one work-group; NULL: not wanted
   int64_t dy_stride, h_stride, dh_stride, dx_stride;
 };
 
@@ -255,11 +255,30 @@ __global__ __launch_bounds__(threads_of<W>) void rms_norm_grad_kernel(NormGradAr
       if (n[v] > 0) store_raw<TYPE>((T*)A.dx + row * A.dx_stride + col[v], from_f32<TYPE>(dx), n[v]);
     }
   }
-  if (A.parts && first < A.R.rows) {
+  if (!A.parts) return;
+  if constexpr (W == 1) {                          // the work-group's waves have the same columns
+    __shared__ f32x4 others[kWaves - 1][2 * NV][kWave];
+    const int wave = threadIdx.x / kWave;
+    if (wave > 0) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      if (n[v] > 0) store_raw<QA_F32>(A.parts + first * A.R.cols + col[v], from_f32<QA_F32>(dw[v]), n[v]);
+      for (int v = 0; v < NV; ++v) {
+        const Raw8<QA_F32> r = from_f32<QA_F32>(dw[v]);
+        others[wave - 1][2 * v][t] = r.a;
+        others[wave - 1][2 * v + 1][t] = r.b;
+      }
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < kWaves - 1; ++w)
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) dw[v][i] += others[w][2 * v + i / 4][t][i % 4];
   }
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+    if (n[v] > 0) store_raw<QA_F32>(A.parts + (int64_t)blockIdx.x * A.R.cols + col[v], from_f32<QA_F32>(dw[v]), n[v]);
 }
 
 // Rows that registers do not hold: everything is read twice, and a work-group's sums lie in the workspace.
@@ -358,10 +377,6 @@ int64_t groups_for(int64_t rows, Form f) {
   const int64_t per_group = f.waves == 1 ? kWaves : 1, waves = f.waves == 1 ? kWaves : f.waves ? f.waves : 16;
   return std::min<int64_t>(ceil_div(rows, per_group), 256 * 16 / waves);
 }
-int64_t parts_for(int64_t rows, Form f) {
-  return f.waves == 1 ? std::min<int64_t>(rows, groups_for(rows, f) * kWaves) : groups_for(rows, f);
-}
-
 template <int TYPE>
 int norm_launch(const NormArgs& A, hipStream_t stream) {
   const Form f = form_of(A.R.cols);
@@ -392,7 +407,7 @@ int norm_grad_launch(const NormGradArgs& A, float* dweight, int accumulate, hipS
   }
   if (!dweight) return QA_OK;
   norm_weight_kernel<<<dim3((unsigned)ceil_div(A.R.cols, kWave)), 1024, 0, stream>>>(
-      A.parts, parts_for(A.R.rows, f), A.R.cols, dweight, accumulate);
+      A.parts, groups_for(A.R.rows, f), A.R.cols, dweight, accumulate);
   return launch_status();
 }
 template <int TYPE>
@@ -404,7 +419,7 @@ int norm_grad_launch(const NormGradArgs& A, float* dweight, int accumulate, hipS
 }  // namespace
 
 size_t rms_norm_grad_workspace_bytes(const qa_coded_rows* R, int) {
-  return (size_t)parts_for(R->rows, form_of(R->cols)) * (size_t)R->cols * sizeof(float);
+  return (size_t)groups_for(R->rows, form_of(R->cols)) * (size_t)R->cols * sizeof(float);
 }
 
 }  // namespace qa

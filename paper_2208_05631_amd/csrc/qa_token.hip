@@ -452,7 +452,7 @@ __global__ __launch_bounds__(kTokenThreads, 4) void token_wide_kernel(TokenArgs 
 }
 
 // A row's splits put together: as a row is from its chunks, with the splits' best alternatives for the lanes' largest.
-constexpr int kMostSplits = 512;
+constexpr int kMostSplits = 512, kKeysAhead = 6;
 template <int TYPE, bool TOP>
 __global__ __launch_bounds__(kTokenThreads) void token_join_kernel(TokenArgs A) {
   __shared__ RowShared<kTokenWaves, 0, TOP> shared;
@@ -462,14 +462,26 @@ __global__ __launch_bounds__(kTokenThreads) void token_join_kernel(TokenArgs A) 
   Given given{0.0f, false};
   if (wave == 0) given = given_of<TYPE>(A, row);
   if (TOP && threadIdx.x == 0) shared.count = 0;
+  const int all = TOP ? A.splits * A.top : 0;
+  uint64_t key[kKeysAhead];                        // the first keys are on their way while the bound is sought
+#pragma unroll
+  for (int k = 0; k < kKeysAhead; ++k) {
+    const int i = k * kTokenThreads + (int)threadIdx.x;
+    key[k] = i < all ? keys[i] : 0;
+  }
   if (TOP && wave == 0) {
-    uint32_t values[kMostSplits / kWave];
+    uint32_t values[kMostSplits / kWave], bound;
 #pragma unroll
     for (int i = 0; i < kMostSplits / kWave; ++i) {
       const int split = i * kWave + lane;
       values[i] = split < A.splits ? (uint32_t)(keys[(int64_t)split * A.top] >> 32) : 0;
     }
-    const uint32_t bound = bound_of(values, A.top);
+    if (A.splits <= kWave) {
+      const uint32_t few[1] = {values[0]};
+      bound = bound_of(few, A.top);
+    } else {
+      bound = bound_of(values, A.top);
+    }
     if (lane == 0) shared.bound = bound;
   }
   Sums a = no_sums();
@@ -488,12 +500,13 @@ __global__ __launch_bounds__(kTokenThreads) void token_join_kernel(TokenArgs A) 
   uint64_t best = 0;
   if constexpr (TOP) {
     const uint64_t least = (uint64_t)shared.bound << 32;
-    const int all = A.splits * A.top;
     Best b;
-    for (int first = 0; first < all; first += kTokenThreads) {
+#pragma unroll
+    for (int k = 0; k < kKeysAhead; ++k) offer(shared, wave, b, key[k], key[k] >= least && key[k] > b.last, A.top);
+    for (int first = kKeysAhead * kTokenThreads; first < all; first += kTokenThreads) {
       const int i = first + (int)threadIdx.x;
-      const uint64_t key = i < all ? keys[i] : 0;
-      offer(shared, wave, b, key, key >= least && key > b.last, A.top);
+      const uint64_t more = i < all ? keys[i] : 0;
+      offer(shared, wave, b, more, more >= least && more > b.last, A.top);
     }
     best = settle<kTokenWaves>(shared, wave, b, A.top);
   }
@@ -567,7 +580,7 @@ int64_t splits_for(int64_t rows, int64_t vocab) {
   if (vocab <= kNarrow) return 1;
   const int64_t least = ceil_div(vocab, kNoted * kTokenChunk);
   if (rows >= 512) return least;
-  return std::max(least, std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), kMostSplits), ceil_div(1024, rows)));
+  return std::max(least, std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), kMostSplits), 1024 / rows));
 }
 
 template <int TYPE, bool TOP>
@@ -580,7 +593,7 @@ int token_launch(TokenArgs& A, hipStream_t stream) {
   } else {
     const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 16), (unsigned)A.splits);
     A.piece = ceil_div(ceil_div(A.vocab, A.splits), kSplitLogits) * kSplitLogits;
-    if (A.splits > 1 && A.piece <= kNoted * kSplitLogits) token_wide_kernel<TYPE, 1, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
+    if (A.piece <= 2 * kSplitLogits) token_wide_kernel<TYPE, 1, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
     else token_wide_kernel<TYPE, kTokenVecs, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
     if (A.splits == 1) return launch_status();
     if (const int rc = launch_status()) return rc;
