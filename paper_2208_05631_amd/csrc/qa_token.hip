@@ -255,7 +255,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 __device__ __forceinline__ float most_of_eight(const float (&v)[kVec]) {
-  return max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), fmaxf(v[6], v[7]));
+  return max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[7]));
 }
 
 // The largest number of 16 leading bits that `top` of the wave's values reach.

@@ -85,6 +85,7 @@ struct Worker {
   static constexpr int kDy = kStep * kTile / kVec / kGroup, kX = kStep * kTile / 16 / kGroup;       // vectors per thread
   static constexpr int kRow = kTile + kGap, kPart = kStep * kRow, kBuffer = (P + 1) * kPart;
   static constexpr int kBuffers = P == 1 ? 3 : 2;  // of 160 KiB
+  static_assert(P == 1 || kDy + 2 <= 2 * P, "a step has a phase for each part of its work");
   // Steps whose elements are on their way.  A step of small tiles takes a third of the time that a read takes.
   static constexpr int kAhead = FN * FK == 8 ? 2 : 4;
 
@@ -160,21 +161,18 @@ struct Worker {
     x_from += (kStep * A.R.code_stride) & go;
     scale_from += (kStep * A.R.scale_stride) & go;
   }
-  __device__ __forceinline__ void store_dy(Loaded& from, __bf16* lds) {
-#pragma unroll
-    for (int v = 0; v < kDy; ++v) {
-      float f[kVec];
-      u32x4 part[P];
-      if constexpr (TYPE == QA_BF16) {
-        part[0] = from.dy[v].a;
-      } else {
-        to_f32<TYPE>(from.dy[v], f);
-        split_parts<P>(f, part);
-      }
-#pragma unroll
-      for (int p = 0; p < P; ++p)
-        *reinterpret_cast<u32x4*>(lds + p * kPart + row_of(v) * kRow + chunk() * kVec) = part[p];
+  __device__ __forceinline__ void store_dy(Loaded& from, int v, __bf16* lds) {
+    float f[kVec];
+    u32x4 part[P];
+    if constexpr (TYPE == QA_BF16) {
+      part[0] = from.dy[v].a;
+    } else {
+      to_f32<TYPE>(from.dy[v], f);
+      split_parts<P>(f, part);
     }
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      *reinterpret_cast<u32x4*>(lds + p * kPart + row_of(v) * kRow + chunk() * kVec) = part[p];
   }
   // X is 0 past the end.
   __device__ __forceinline__ void store_x(Loaded& from, __bf16* lds, int64_t t0) {
@@ -225,11 +223,12 @@ struct Worker {
     for (int phase = 0; phase < 2 * P; ++phase) {
       if (phase + 1 < 2 * P) w.operands(now, phase + 1);
       else if (kBuffers == 3) w.operands(next, 0);
-      if (phase == 0) {
-        w.store_dy(loaded, last);
-        w.store_x(loaded, last, t + (kBuffers - 1) * kStep);
-      }
-      if (phase == 1) w.load(loaded);
+      // what is to be done beside the matrix instructions, over as many phases as there are
+#pragma unroll
+      for (int v = 0; v < kDy; ++v)
+        if (phase == (P == 1 ? 0 : v)) w.store_dy(loaded, v, last);
+      if (phase == (P == 1 ? 0 : kDy)) w.store_x(loaded, last, t + (kBuffers - 1) * kStep);
+      if (phase == (P == 1 ? 1 : kDy + 1)) w.load(loaded);
       w.multiply(phase);
       interleave<TYPE, FN, FK>(phase);
     }
@@ -242,7 +241,8 @@ struct Worker {
     for (int a = 0; a < kAhead; ++a) load(loaded[a]);
 #pragma unroll
     for (int b = 0; b + 1 < kBuffers; ++b) {
-      store_dy(loaded[b % kAhead], lds + b * kBuffer);
+#pragma unroll
+      for (int v = 0; v < kDy; ++v) store_dy(loaded[b % kAhead], v, lds + b * kBuffer);
       store_x(loaded[b % kAhead], lds + b * kBuffer, t_begin + b * kStep);
       load(loaded[b % kAhead]);
     }
