@@ -563,3 +563,79 @@ def test_calls_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_offsets_beyond_32_bits(t):
+    """Three rows, 2^31 + 24 elements apart: the last begins at 8 or 17 GB."""
+    gen, K, far = gen_of("far", t), 100, (1 << 31) + 24
+    flat = torch.empty(2 * far + K, dtype=TYPES[t], device=DEV)
+    rows = flat.as_strided((3, K), (far, 1))
+    x = torch.randn(3, K, generator=gen).to(TYPES[t])
+    rows.copy_(x)
+    L, codes, scales = coded_rows(3, K, 32)
+    qa.qa_rows_pack(L, code_of(t), flat, far, codes, scales)
+    want_s = ref.scale_bytes(x.to(F64), 32)
+    assert torch.equal(codes[:, :K].cpu().long(), ref.code(x.to(F64), want_s, 32))
+    y = torch.empty(3, K, dtype=torch.bfloat16, device=DEV)
+    rstd = torch.empty(3, device=DEV)
+    ones = torch.ones(K, device=DEV)
+    qa.qa_rms_norm(L, code_of(t), flat, far, flat, far, ones, 0.0, None, 0, codes, scales, y, K, rstd)
+    want, _ = ref.norm(2 * x.to(F64), torch.ones(K, dtype=F64), 0.0)
+    assert (rstd.cpu().to(F64) / want - 1).abs().max() < SUM
+    ws = torch.empty(qa.qa_rows_workspace_bytes(L, qa.QA_OP_NORM_GRAD, code_of(t)), dtype=torch.uint8, device=DEV)
+    dx = torch.empty(3, K, dtype=TYPES[t], device=DEV)
+    dw = torch.empty(K, device=DEV)
+    qa.qa_rms_norm_grad(L, code_of(t), flat, far, flat, far, None, None, ones, ones, flat, far, dx, K, dw, 0, ws)
+    want_dx, want_dw = ref.norm_grad(x.to(F64), x.to(F64), torch.ones(K, dtype=F64), torch.ones(3, dtype=F64), x.to(F64))
+    assert (dw.cpu().to(F64) - want_dw).abs().max() < 1e-5
+    assert ((dx.cpu().to(F64) - want_dx).abs() <= HALF_ULP[t] * 1.01 * want_dx.abs() + SUM * 40).all()
+    target = torch.tensor([1, 2, 3], dtype=torch.int32)
+    lp, entropy, stats = torch.empty(3, device=DEV), torch.empty(3, device=DEV), torch.empty(3, 2, device=DEV)
+    qa.qa_token_logprob(code_of(t), 3, K, flat, far, target.to(DEV), 0, lp, entropy, stats, None, None, None)
+    want_lp = ref.token_logprob(x.to(F64), target)[0]
+    assert (lp.cpu().to(F64) - want_lp).abs().max() < 1e-5
+    qa.qa_token_logprob_grad(code_of(t), 3, K, flat, far, target.to(DEV), stats, None, ones, None, flat, far)
+    want_dx = ref.token_logprob_grad(x.to(F64), target, torch.ones(3, dtype=F64), torch.zeros(3, dtype=F64))
+    assert ((rows.cpu().to(F64) - want_dx).abs() <= HALF_ULP[t] * 1.01 * want_dx.abs() + 1e-6).all()
+
+
+def test_more_rows_than_a_launch_has_work_groups_for():
+    """Numbers of up to seven bits come back as they are."""
+    T = (1 << 24) + 77
+    x = (torch.arange(T, device=DEV) % 255 - 127).float()[:, None]
+    L = qa.CodedRows.make(T, 1, 32)
+    codes = torch.empty(T, 16, dtype=torch.int8, device=DEV)
+    scales, back = torch.empty(T, 1, dtype=torch.uint8, device=DEV), torch.empty(T, 1, device=DEV)
+    qa.qa_rows_pack(L, qa.QA_F32, x, 1, codes, scales)
+    qa.qa_rows_unpack(L, codes, scales, qa.QA_F32, back, 1)
+    assert torch.equal(back, x)
+    T = 300_001
+    logits = torch.zeros(T, 3, device=DEV)
+    logits[:, 1] = 1.0
+    index, top = torch.full((T, 2), -1, dtype=torch.int32, device=DEV), torch.empty(T, 2, device=DEV)
+    entropy = torch.empty(T, device=DEV)
+    qa.qa_token_logprob(qa.QA_F32, T, 3, logits, 3, None, 2, None, entropy, None, top, index, None)
+    assert torch.equal(index, torch.tensor([[1, 0]], dtype=torch.int32, device=DEV).expand(T, 2))
+    assert (entropy == entropy[0]).all() and (top == top[0]).all()
+
+
+def test_tiles_that_the_whole_width_does_not_fill():
+    """A large enough gradient for the large tiles, with ends inside one in all three directions, against a product in 64 bits."""
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    T, N, K = 335, 3851, 4099
+    x = torch.randn(T, K, generator=gen, device=DEV)
+    for t in ("bf16", "f16", "f32"):
+        dy = torch.randn(T, N + 5, generator=gen, device=DEV).to(TYPES[t])[:, :N]
+        L, codes, scales = coded_rows(T, K, 64)
+        qa.qa_rows_pack(L, qa.QA_F32, x, K, codes, scales)
+        values = torch.empty(T, K, device=DEV)
+        qa.qa_rows_unpack(L, codes, scales, qa.QA_F32, values, K)
+        ws = torch.empty(max(1, qa.qa_rows_workspace_bytes(L, qa.QA_OP_WEIGHT_GRAD, code_of(t), N)), dtype=torch.uint8, device=DEV)
+        for accumulate in (0, 1):
+            dw = torch.full((N, K + 1), 0.25, device=DEV)
+            qa.qa_rows_weight_grad(L, codes, scales, code_of(t), dy, N + 5, N, dw, K + 1, accumulate, ws)
+            assert (dw[:, K] == 0.25).all()
+            want = dy.double().t().contiguous() @ values.double() + 0.25 * accumulate
+            each = dy.double().abs().t().contiguous() @ values.double().abs() + 0.25
+            assert ((dw[:, :K].double() - want).abs() <= SUM * each).all()
