@@ -527,47 +527,74 @@ struct TokenGradArgs {
   int64_t rows, vocab, x_stride, dx_stride;
 };
 
-constexpr int kGradVecs = 4;
-constexpr int64_t kGradPiece = (int64_t)kGradVecs * kThreads * kVec;       // logits of a work-group at a time
+struct GradRow {
+  float a, c, e2, m, log_sum;
+  int32_t y;
+};
+__device__ __forceinline__ GradRow grad_row(const TokenGradArgs& A, int64_t row) {
+  GradRow r;
+  r.y = A.target ? A.target[row] : -1;
+  if (r.y >= A.vocab) r.y = -1;
+  r.a = r.y >= 0 && A.g_logprob ? A.g_logprob[row] : 0.0f;
+  const float e = A.g_entropy ? A.g_entropy[row] : 0.0f;
+  r.c = r.a + (A.g_entropy ? e * A.entropy[row] : 0.0f);
+  r.e2 = e * kLn2;
+  r.m = fmaxf(A.stats[2 * row], -FLT_MAX);
+  r.log_sum = A.stats[2 * row + 1];
+  return r;
+}
 // dx_j = -p_j (a + e (log p_j + H)), and a more at the target.
 template <int TYPE>
+__device__ __forceinline__ Raw8<TYPE> grad_of(const GradRow& r, const Raw8<TYPE>& raw, int64_t i) {
+  float v[kVec], d[kVec];
+  to_f32<TYPE>(raw, v);
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) {
+    const float t = ((v[j] - r.m) - r.log_sum) * kLog2e, p = __builtin_amdgcn_exp2f(t);
+    d[j] = -p * __builtin_fmaf(r.e2, fmaxf(t, kFar), r.c);
+  }
+  if (r.y >= i && r.y < i + kVec) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) d[j] += r.y - i == j ? r.a : 0.0f;
+  }
+  return from_f32<TYPE>(d);
+}
+
+constexpr int64_t kGradPiece = (int64_t)kThreads * kVec;       // logits that a work-group has in one vector per lane
+template <int TYPE, int NV>
 __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenGradArgs A) {
   typedef ElemT<TYPE> T;
   for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
     const T* x = (const T*)A.x + row * A.x_stride;
     T* dx = (T*)A.dx + row * A.dx_stride;
-    const int32_t y = A.target ? A.target[row] : -1;
-    const bool has = y >= 0 && y < A.vocab;
-    const float a = has && A.g_logprob ? A.g_logprob[row] : 0.0f;
-    const float e = A.g_entropy ? A.g_entropy[row] : 0.0f;
-    const float c = a + (A.g_entropy ? e * A.entropy[row] : 0.0f), e2 = e * kLn2;
-    const float m = fmaxf(A.stats[2 * row], -FLT_MAX), log_sum = A.stats[2 * row + 1];
-    for (int64_t first = (int64_t)blockIdx.y * kGradPiece; first < A.vocab; first += (int64_t)gridDim.y * kGradPiece) {
+    const GradRow r = grad_row(A, row);
+    for (int64_t first = (int64_t)blockIdx.y * NV * kGradPiece; first < A.vocab; first += (int64_t)gridDim.y * NV * kGradPiece) {
       const int64_t lane0 = first + threadIdx.x * kVec;
-      Raw8<TYPE> raw[kGradVecs];
+      Raw8<TYPE> raw[NV];
 #pragma unroll
-      for (int k = 0; k < kGradVecs; ++k) {
+      for (int k = 0; k < NV; ++k) {
         const int64_t i = lane0 + k * kThreads * kVec;
         raw[k] = load_raw<TYPE>(x + i, (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i)));
       }
 #pragma unroll
-      for (int k = 0; k < kGradVecs; ++k) {
+      for (int k = 0; k < NV; ++k) {
         const int64_t i = lane0 + k * kThreads * kVec;
         const int n = (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i));
-        float v[kVec], d[kVec];
-        to_f32<TYPE>(raw[k], v);
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-          const float t = ((v[j] - m) - log_sum) * kLog2e, p = __builtin_amdgcn_exp2f(t);
-          d[j] = -p * __builtin_fmaf(e2, fmaxf(t, kFar), c);
-        }
-        if (has && y >= i && y < i + kVec) {
-#pragma unroll
-          for (int j = 0; j < kVec; ++j) d[j] += y - i == j ? a : 0.0f;
-        }
-        if (n > 0) store_raw<TYPE>(dx + i, from_f32<TYPE>(d), n);
+        if (n > 0) store_raw<TYPE>(dx + i, grad_of<TYPE>(r, raw[k], i), n);
       }
     }
+  }
+}
+// Rows of up to 2048 logits: `per_row` lanes, a power of two, have one vector each.
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void token_grad_narrow_kernel(TokenGradArgs A, int per_row) {
+  typedef ElemT<TYPE> T;
+  const int rows = kThreads / per_row, local = threadIdx.x / per_row, i = (int)threadIdx.x % per_row * kVec;
+  const int n = (int)min((int64_t)kVec, A.vocab - i);
+  if (n <= 0) return;
+  for (int64_t row = (int64_t)blockIdx.x * rows + local; row < A.rows; row += (int64_t)gridDim.x * rows) {
+    const Raw8<TYPE> raw = load_raw<TYPE>((const T*)A.x + row * A.x_stride + i, n);
+    store_raw<TYPE>((T*)A.dx + row * A.dx_stride + i, grad_of<TYPE>(grad_row(A, row), raw, i), n);
   }
 }
 
@@ -576,10 +603,13 @@ __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenGradArgs A) {
 constexpr int64_t kNarrow = 4096;                  // logits of a row that one wave reads
 constexpr int64_t kSplitLogits = kTokenThreads * kVec;       // one vector per lane
 
+// Rows longer than this are split where there are few: a second launch takes as long as it saves (one row, 20 alternatives: 16000
+// logits 10.4 us in one piece and 12.3 split, 32000 13.4 and 13.1, 64000 17.6 and 12.2; 400 rows of 64000: 23.7 and 27.7).
+constexpr int64_t kUnsplit = 16 * kSplitLogits;
 int64_t splits_for(int64_t rows, int64_t vocab) {
-  if (vocab <= kNarrow) return 1;
+  if (vocab <= kUnsplit) return 1;
   const int64_t least = ceil_div(vocab, kNoted * kTokenChunk);
-  if (rows >= 512) return least;
+  if (rows >= 256) return least;
   return std::max(least, std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), kMostSplits), 1024 / rows));
 }
 
@@ -607,9 +637,17 @@ int token_launch(TokenArgs& A, hipStream_t stream) {
 }
 template <int TYPE>
 int token_grad_launch(const TokenGradArgs& A, hipStream_t stream) {
-  const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 22),
-                  (unsigned)std::min<int64_t>(ceil_div(A.vocab, kGradPiece), 1 << 14));
-  token_grad_kernel<TYPE><<<grid, kThreads, 0, stream>>>(A);
+  if (A.vocab <= kGradPiece) {
+    int per_row = 1;
+    while (per_row * kVec < A.vocab) per_row *= 2;
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(A.rows, kThreads / per_row), 1 << 22));
+    token_grad_narrow_kernel<TYPE><<<grid, kThreads, 0, stream>>>(A, per_row);
+  } else {
+    constexpr int NV = 4;
+    const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 22),
+                    (unsigned)std::min<int64_t>(ceil_div(A.vocab, NV * kGradPiece), 1 << 14));
+    token_grad_kernel<TYPE, NV><<<grid, kThreads, 0, stream>>>(A);
+  }
   return launch_status();
 }
 
