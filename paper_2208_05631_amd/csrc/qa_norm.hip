@@ -1,36 +1,39 @@
 // Root-mean-square norm of a residual stream with an output in 8 bits, and its backward pass.
 #include <algorithm>
+#include <type_traits>
 
 #include "qa_rows.h"
 
 namespace qa {
 namespace {
 
-// A row is held in the registers of W waves, NV vectors of eight columns per lane: one read of everything.  Rows of
-// up to 1024 columns are a wave's own and need no barrier; four of them share a work-group.
+// A row is held in the registers of LANES lanes, NV vectors of eight columns each: one read of everything.  Rows of
+// up to 1024 columns lie inside a wave and need no barrier; of up to 128, the norms of attention heads, four do.
+// (524288 rows of 128 bfloat16: 115 us, and 301 with a wave for each.)
 constexpr int kHeldCols = 16384;                   // 16 waves, two vectors per lane; longer rows are read twice
 
-__device__ __forceinline__ float wave_sum_f32(float v) {
-  v += as_f32((uint32_t)dpp_i32<kDppQuadXor1>((int)as_u32(v)));
-  v += as_f32((uint32_t)dpp_i32<kDppQuadXor2>((int)as_u32(v)));
-  v += as_f32((uint32_t)dpp_i32<kDppRowHalfMirror>((int)as_u32(v)));
-  v += as_f32((uint32_t)dpp_i32<kDppRowMirror>((int)as_u32(v)));
-  const int i = (int)as_u32(v);
-  return (as_f32((uint32_t)__builtin_amdgcn_readlane(i, 0)) + as_f32((uint32_t)__builtin_amdgcn_readlane(i, 16))) +
-         (as_f32((uint32_t)__builtin_amdgcn_readlane(i, 32)) + as_f32((uint32_t)__builtin_amdgcn_readlane(i, 48)));
-}
-// Sum over the W waves of a row.  `lds` holds W floats that no other call uses before the next barrier but one: the
-// callers alternate between two.
-template <int W>
+// Sum over the LANES lanes of a row.  `lds` holds a float for each of their waves that no other call uses before the next
+// barrier but one: the callers alternate between two.
+template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
-  v = wave_sum_f32(v);
-  if constexpr (W == 1) return v;
-  if ((threadIdx.x % kWave) == 0) lds[threadIdx.x / kWave] = v;
-  __syncthreads();
-  float s = lds[0];
+  if constexpr (LANES < kWave) {
+    v += as_f32(other_lane<1>(as_u32(v)));
+    v += as_f32(other_lane<2>(as_u32(v)));
+    v += as_f32(other_lane<4>(as_u32(v)));
+    v += as_f32(other_lane<8>(as_u32(v)));
+    if constexpr (LANES == 32) v += as_f32(other_lane<16>(as_u32(v)));
+    return v;
+  } else {
+    v = wave_sum_f32(v);
+    if constexpr (LANES == kWave) return v;
+    constexpr int W = LANES / kWave;
+    if ((threadIdx.x % kWave) == 0) lds[threadIdx.x / kWave] = v;
+    __syncthreads();
+    float s = lds[0];
 #pragma unroll
-  for (int w = 1; w < W; ++w) s += lds[w];
-  return s;
+    for (int w = 1; w < W; ++w) s += lds[w];
+    return s;
+  }
 }
 
 struct NormArgs {
@@ -47,8 +50,9 @@ struct NormArgs {
   float eps;
 };
 
-template <int W> constexpr int threads_of = W == 1 ? kThreads : W * kWave;
-template <int W> constexpr int rows_of = W == 1 ? kWaves : 1;
+template <int LANES> constexpr int threads_of = LANES <= kWave ? kThreads : LANES;
+template <int LANES> constexpr int rows_of = threads_of<LANES> / LANES;
+template <int LANES> constexpr int waves_of = LANES <= kWave ? 1 : LANES / kWave;
 
 // Codes and values of eight columns of y, which their lane and its neighbours of the same group hold.
 __device__ __forceinline__ void write_y(const NormArgs& A, int64_t row, int64_t col, int n, const float (&y)[kVec]) {
@@ -64,24 +68,23 @@ __device__ __forceinline__ void write_y(const NormArgs& A, int64_t row, int64_t 
   if (A.y) store_raw<QA_BF16>(A.y + row * A.y_stride + col, from_f32<QA_BF16>(value), n);
 }
 
-template <int TYPE, int W, int NV>
-__global__ __launch_bounds__(threads_of<W>) void rms_norm_kernel(NormArgs A) {
+template <int TYPE, int LANES, int NV>
+__global__ __launch_bounds__(threads_of<LANES>) void rms_norm_kernel(NormArgs A) {
   typedef ElemT<TYPE> T;
-  __shared__ float sums[2][W];
-  const int t = threadIdx.x % (W * kWave);
-  const int64_t step = (int64_t)gridDim.x * rows_of<W>;
+  __shared__ float sums[2][waves_of<LANES>];
+  const int t = threadIdx.x % LANES;
+  const int64_t step = (int64_t)gridDim.x * rows_of<LANES>;
   int64_t col[NV];
   int n[NV];
   float w[NV][kVec];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    col[v] = ((int64_t)v * W * kWave + t) * kVec;
+    col[v] = ((int64_t)v * LANES + t) * kVec;
     n[v] = (int)min((int64_t)kVec, A.R.cols - col[v]);
     to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col[v], n[v]), w[v]);
   }
   int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * rows_of<W> + (W == 1 ? threadIdx.x / kWave : 0); row < A.R.rows;
-       row += step) {
+  for (int64_t row = (int64_t)blockIdx.x * rows_of<LANES> + threadIdx.x / LANES; row < A.R.rows; row += step) {
     Raw8<TYPE> x[NV], r[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) x[v] = load_raw<TYPE>((const T*)A.x + row * A.x_stride + col[v], n[v]);
@@ -102,7 +105,7 @@ __global__ __launch_bounds__(threads_of<W>) void rms_norm_kernel(NormArgs A) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) s = __builtin_fmaf(h[v][i], h[v][i], s);
     }
-    const float rstd = 1.0f / sqrtf(row_sum<W>(s, sums[turn]) / (float)A.R.cols + A.eps);
+    const float rstd = 1.0f / sqrtf(row_sum<LANES>(s, sums[turn]) / (float)A.R.cols + A.eps);
     turn ^= 1;
     if (A.rstd && t == 0) A.rstd[row] = rstd;
 #pragma unroll
@@ -144,7 +147,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs A) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) s = __builtin_fmaf(h[i], h[i], s);
     }
-    const float rstd = 1.0f / sqrtf(row_sum<16>(s, sums[turn]) / (float)A.R.cols + A.eps);
+    const float rstd = 1.0f / sqrtf(row_sum<1024>(s, sums[turn]) / (float)A.R.cols + A.eps);
     turn ^= 1;
     if (A.rstd && threadIdx.x == 0) A.rstd[row] = rstd;
     for (int64_t p = 0; p < pieces; ++p) {
@@ -195,25 +198,25 @@ __device__ __forceinline__ void load_h(const NormGradArgs& A, int64_t row, int64
   }
 }
 
-template <int TYPE, int W, int NV, bool CODED>
-__global__ __launch_bounds__(threads_of<W>) void rms_norm_grad_kernel(NormGradArgs A) {
+template <int TYPE, int LANES, int NV, bool CODED>
+__global__ __launch_bounds__(threads_of<LANES>) void rms_norm_grad_kernel(NormGradArgs A) {
   typedef ElemT<TYPE> T;
-  __shared__ float sums[2][W];
-  const int t = threadIdx.x % (W * kWave);
-  const int64_t first = (int64_t)blockIdx.x * rows_of<W> + (W == 1 ? threadIdx.x / kWave : 0);
+  __shared__ float sums[2][waves_of<LANES>];
+  const int t = threadIdx.x % LANES;
+  const int64_t first = (int64_t)blockIdx.x * rows_of<LANES> + threadIdx.x / LANES;
   int64_t col[NV];
   int n[NV];
   float w[NV][kVec], dw[NV][kVec];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    col[v] = ((int64_t)v * W * kWave + t) * kVec;
+    col[v] = ((int64_t)v * LANES + t) * kVec;
     n[v] = (int)min((int64_t)kVec, A.R.cols - col[v]);
     to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col[v], n[v]), w[v]);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) dw[v][i] = 0.0f;
   }
   int turn = 0;
-  for (int64_t row = first; row < A.R.rows; row += (int64_t)gridDim.x * rows_of<W>) {
+  for (int64_t row = first; row < A.R.rows; row += (int64_t)gridDim.x * rows_of<LANES>) {
     Raw8<TYPE> dy_raw[NV], dh_raw[NV];
     float h[NV][kVec];
 #pragma unroll
@@ -238,7 +241,7 @@ __global__ __launch_bounds__(threads_of<W>) void rms_norm_grad_kernel(NormGradAr
         dw[v][i] = __builtin_fmaf(dy[i], h[v][i], dw[v][i]);
       }
     }
-    const float c = row_sum<W>(s, sums[turn]) / (float)A.R.cols;
+    const float c = row_sum<LANES>(s, sums[turn]) / (float)A.R.cols;
     turn ^= 1;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -256,25 +259,32 @@ __global__ __launch_bounds__(threads_of<W>) void rms_norm_grad_kernel(NormGradAr
     }
   }
   if (!A.parts) return;
-  if constexpr (W == 1) {                          // the work-group's waves have the same columns
+  if constexpr (LANES <= kWave) {                  // the work-group's rows have the same columns
     __shared__ f32x4 others[kWaves - 1][2 * NV][kWave];
-    const int wave = threadIdx.x / kWave;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        if constexpr (LANES <= 16) dw[v][i] += as_f32(other_lane<16>(as_u32(dw[v][i])));
+        if constexpr (LANES <= 32) dw[v][i] += as_f32(other_lane<32>(as_u32(dw[v][i])));
+      }
     if (wave > 0) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const Raw8<QA_F32> r = from_f32<QA_F32>(dw[v]);
-        others[wave - 1][2 * v][t] = r.a;
-        others[wave - 1][2 * v + 1][t] = r.b;
+        others[wave - 1][2 * v][lane] = r.a;
+        others[wave - 1][2 * v + 1][lane] = r.b;
       }
     }
     __syncthreads();
-    if (wave > 0) return;
+    if (threadIdx.x >= LANES) return;
 #pragma unroll
     for (int w = 0; w < kWaves - 1; ++w)
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) dw[v][i] += others[w][2 * v + i / 4][t][i % 4];
+        for (int i = 0; i < kVec; ++i) dw[v][i] += others[w][2 * v + i / 4][lane][i % 4];
   }
 #pragma unroll
   for (int v = 0; v < NV; ++v)
@@ -302,7 +312,7 @@ __global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(NormGradArgs A
 #pragma unroll
       for (int i = 0; i < kVec; ++i) s = __builtin_fmaf(dy[i] * w[i], h[i] * rstd, s);
     }
-    const float c = row_sum<16>(s, sums[turn]) / (float)A.R.cols;
+    const float c = row_sum<1024>(s, sums[turn]) / (float)A.R.cols;
     turn ^= 1;
     for (int64_t p = 0; p < pieces; ++p) {
       const int64_t col = (p * 1024 + threadIdx.x) * kVec;
@@ -361,32 +371,49 @@ __global__ __launch_bounds__(1024) void norm_weight_kernel(const float* __restri
 
 // ---- which form -----------------------------------------------------------------------------------------------
 
-// Waves per row (0: the row is read twice) and vectors per lane.
-struct Form { int waves, vecs; };
+// Lanes per row (0: the row is read twice) and vectors per lane.
+struct Form { int lanes, vecs; };
 Form form_of(int64_t cols) {
-  if (cols <= 512) return {1, 1};
-  if (cols <= 1024) return {1, 2};
-  if (cols <= 2048) return {4, 1};
-  if (cols <= 4096) return {4, 2};
-  if (cols <= 8192) return {8, 2};
-  if (cols <= kHeldCols) return {16, 2};
+  if (cols <= 128) return {16, 1};
+  if (cols <= 256) return {32, 1};
+  if (cols <= 512) return {64, 1};
+  if (cols <= 1024) return {64, 2};
+  if (cols <= 2048) return {256, 1};
+  if (cols <= 4096) return {256, 2};
+  if (cols <= 8192) return {512, 2};
+  if (cols <= kHeldCols) return {1024, 2};
   return {0, 0};
 }
 // Work-groups: 16 waves per compute unit.
 int64_t groups_for(int64_t rows, Form f) {
-  const int64_t per_group = f.waves == 1 ? kWaves : 1, waves = f.waves == 1 ? kWaves : f.waves ? f.waves : 16;
-  return std::min<int64_t>(ceil_div(rows, per_group), 256 * 16 / waves);
+  const int64_t threads = f.lanes == 0 ? 1024 : f.lanes <= kWave ? kThreads : f.lanes;
+  return std::min<int64_t>(ceil_div(rows, f.lanes && f.lanes <= kWave ? kThreads / f.lanes : 1), 256 * 1024 / threads);
 }
+
+// Calls `launch` with the lanes and vectors of a form as constants.
+template <typename F>
+void with_form(Form f, F launch) {
+  using std::integral_constant;
+#define QA_FORM(LANES, VECS) if (f.lanes == LANES && f.vecs == VECS) launch(integral_constant<int, LANES>{}, integral_constant<int, VECS>{})
+  QA_FORM(16, 1);
+  QA_FORM(32, 1);
+  QA_FORM(64, 1);
+  QA_FORM(64, 2);
+  QA_FORM(256, 1);
+  QA_FORM(256, 2);
+  QA_FORM(512, 2);
+  QA_FORM(1024, 2);
+#undef QA_FORM
+}
+
 template <int TYPE>
 int norm_launch(const NormArgs& A, hipStream_t stream) {
   const Form f = form_of(A.R.cols);
   const dim3 grid((unsigned)groups_for(A.R.rows, f));
-  if (f.waves == 1 && f.vecs == 1) rms_norm_kernel<TYPE, 1, 1><<<grid, threads_of<1>, 0, stream>>>(A);
-  else if (f.waves == 1) rms_norm_kernel<TYPE, 1, 2><<<grid, threads_of<1>, 0, stream>>>(A);
-  else if (f.waves == 4 && f.vecs == 1) rms_norm_kernel<TYPE, 4, 1><<<grid, threads_of<4>, 0, stream>>>(A);
-  else if (f.waves == 4) rms_norm_kernel<TYPE, 4, 2><<<grid, threads_of<4>, 0, stream>>>(A);
-  else if (f.waves == 8) rms_norm_kernel<TYPE, 8, 2><<<grid, threads_of<8>, 0, stream>>>(A);
-  else if (f.waves == 16) rms_norm_kernel<TYPE, 16, 2><<<grid, threads_of<16>, 0, stream>>>(A);
+  if (f.lanes)
+    with_form(f, [&](auto lanes, auto vecs) {
+      rms_norm_kernel<TYPE, lanes, vecs><<<grid, threads_of<lanes>, 0, stream>>>(A);
+    });
   else rms_norm_long_kernel<TYPE><<<grid, 1024, 0, stream>>>(A);
   return launch_status();
 }
@@ -396,12 +423,10 @@ int norm_grad_launch(const NormGradArgs& A, float* dweight, int accumulate, hipS
   const Form f = form_of(A.R.cols);
   const dim3 grid((unsigned)groups_for(A.R.rows, f));
   if (A.R.rows > 0) {
-    if (f.waves == 1 && f.vecs == 1) rms_norm_grad_kernel<TYPE, 1, 1, CODED><<<grid, threads_of<1>, 0, stream>>>(A);
-    else if (f.waves == 1) rms_norm_grad_kernel<TYPE, 1, 2, CODED><<<grid, threads_of<1>, 0, stream>>>(A);
-    else if (f.waves == 4 && f.vecs == 1) rms_norm_grad_kernel<TYPE, 4, 1, CODED><<<grid, threads_of<4>, 0, stream>>>(A);
-    else if (f.waves == 4) rms_norm_grad_kernel<TYPE, 4, 2, CODED><<<grid, threads_of<4>, 0, stream>>>(A);
-    else if (f.waves == 8) rms_norm_grad_kernel<TYPE, 8, 2, CODED><<<grid, threads_of<8>, 0, stream>>>(A);
-    else if (f.waves == 16) rms_norm_grad_kernel<TYPE, 16, 2, CODED><<<grid, threads_of<16>, 0, stream>>>(A);
+    if (f.lanes)
+      with_form(f, [&](auto lanes, auto vecs) {
+        rms_norm_grad_kernel<TYPE, lanes, vecs, CODED><<<grid, threads_of<lanes>, 0, stream>>>(A);
+      });
     else rms_norm_grad_long_kernel<TYPE, CODED><<<grid, 1024, 0, stream>>>(A);
     if (const int rc = launch_status()) return rc;
   }

@@ -123,6 +123,41 @@ __device__ __forceinline__ void store_raw(ElemT<TYPE>* p, const Raw8<TYPE>& r, i
     if (i < n) p[i] = v[i];
 }
 
+// ---- between lanes ---------------------------------------------------------------------------------------
+
+__device__ __forceinline__ float wave_sum_f32(float v) {
+  v += as_f32((uint32_t)dpp_i32<kDppQuadXor1>((int)as_u32(v)));
+  v += as_f32((uint32_t)dpp_i32<kDppQuadXor2>((int)as_u32(v)));
+  v += as_f32((uint32_t)dpp_i32<kDppRowHalfMirror>((int)as_u32(v)));
+  v += as_f32((uint32_t)dpp_i32<kDppRowMirror>((int)as_u32(v)));
+  const int i = (int)as_u32(v);
+  return (as_f32((uint32_t)__builtin_amdgcn_readlane(i, 0)) + as_f32((uint32_t)__builtin_amdgcn_readlane(i, 16))) +
+         (as_f32((uint32_t)__builtin_amdgcn_readlane(i, 32)) + as_f32((uint32_t)__builtin_amdgcn_readlane(i, 48)));
+}
+constexpr int kDppQuadReverse = 0x1B;               // quad_perm:[3,2,1,0]
+// The value of the lane whose number differs in `STRIDE` alone.  Up to 8 two moves between neighbours do it, a tenth of
+// the time that a way through LDS takes; rows of 16 lanes are swapped with their neighbours.
+template <int STRIDE>
+__device__ __forceinline__ uint32_t other_lane(uint32_t v) {
+  const int i = (int)v;
+  if constexpr (STRIDE == 1) return (uint32_t)dpp_i32<kDppQuadXor1>(i);
+  if constexpr (STRIDE == 2) return (uint32_t)dpp_i32<kDppQuadXor2>(i);
+  if constexpr (STRIDE == 4) return (uint32_t)dpp_i32<kDppQuadReverse>(dpp_i32<kDppRowHalfMirror>(i));
+  if constexpr (STRIDE == 8) return (uint32_t)dpp_i32<kDppRowHalfMirror>(dpp_i32<kDppRowMirror>(i));
+  if constexpr (STRIDE == 16) {
+    const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? both[0] : both[1];
+  }
+  if constexpr (STRIDE == 32) {
+    const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? both[0] : both[1];
+  }
+}
+template <int STRIDE>
+__device__ __forceinline__ uint64_t other_lane(uint64_t v) {
+  return (uint64_t)other_lane<STRIDE>((uint32_t)(v >> 32)) << 32 | other_lane<STRIDE>((uint32_t)v);
+}
+
 // ---- the 8-bit code of a group of columns -----------------------------------------------------------------
 //
 // A group has one byte b, its scale is 2^(b - 127): the smallest power of two by which the group's largest magnitude

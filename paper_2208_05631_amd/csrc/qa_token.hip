@@ -9,19 +9,9 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kFar = -1e4f;                      // 2^kFar is 0
-constexpr int kDppQuadReverse = 0x1B;               // quad_perm:[3,2,1,0]
 constexpr int kTop = QA_TOP_MAX;                   // a lane for each alternative
 static_assert(kTop == kWave, "the alternatives of a row are held one per lane");
 
-__device__ __forceinline__ float wave_sum_f32(float v) {
-  v += as_f32((uint32_t)dpp_i32<kDppQuadXor1>((int)as_u32(v)));
-  v += as_f32((uint32_t)dpp_i32<kDppQuadXor2>((int)as_u32(v)));
-  v += as_f32((uint32_t)dpp_i32<kDppRowHalfMirror>((int)as_u32(v)));
-  v += as_f32((uint32_t)dpp_i32<kDppRowMirror>((int)as_u32(v)));
-  const int i = (int)as_u32(v);
-  return (as_f32((uint32_t)__builtin_amdgcn_readlane(i, 0)) + as_f32((uint32_t)__builtin_amdgcn_readlane(i, 16))) +
-         (as_f32((uint32_t)__builtin_amdgcn_readlane(i, 32)) + as_f32((uint32_t)__builtin_amdgcn_readlane(i, 48)));
-}
 __device__ __forceinline__ float wave_max_f32(float v) {
   v = fmaxf(v, as_f32((uint32_t)dpp_i32<kDppQuadXor1>((int)as_u32(v))));
   v = fmaxf(v, as_f32((uint32_t)dpp_i32<kDppQuadXor2>((int)as_u32(v))));
@@ -69,28 +59,6 @@ __device__ __forceinline__ float from_ordered(uint32_t o) {
 }
 __device__ __forceinline__ uint64_t key_of(uint32_t order, uint32_t index) { return (uint64_t)order << 32 | (uint32_t)~index; }
 
-// The value of the lane whose number differs in `STRIDE` alone.  Up to 8 two moves between neighbours do it, a tenth of
-// the time that a way through LDS takes; rows of 16 lanes are swapped with their neighbours.
-template <int STRIDE>
-__device__ __forceinline__ uint32_t other_lane(uint32_t v) {
-  const int i = (int)v;
-  if constexpr (STRIDE == 1) return (uint32_t)dpp_i32<kDppQuadXor1>(i);
-  if constexpr (STRIDE == 2) return (uint32_t)dpp_i32<kDppQuadXor2>(i);
-  if constexpr (STRIDE == 4) return (uint32_t)dpp_i32<kDppQuadReverse>(dpp_i32<kDppRowHalfMirror>(i));
-  if constexpr (STRIDE == 8) return (uint32_t)dpp_i32<kDppRowHalfMirror>(dpp_i32<kDppRowMirror>(i));
-  if constexpr (STRIDE == 16) {
-    const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    return threadIdx.x & 16 ? both[0] : both[1];
-  }
-  if constexpr (STRIDE == 32) {
-    const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    return threadIdx.x & 32 ? both[0] : both[1];
-  }
-}
-template <int STRIDE>
-__device__ __forceinline__ uint64_t other_lane(uint64_t v) {
-  return (uint64_t)other_lane<STRIDE>((uint32_t)(v >> 32)) << 32 | other_lane<STRIDE>((uint32_t)v);
-}
 template <int SIZE, int STRIDE, typename U>
 __device__ __forceinline__ U merge_steps(U v) {
   const int lane = threadIdx.x % kWave;
@@ -410,6 +378,8 @@ __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, in
         }
     }
     best = settle<WAVES>(shared, wave, b, top);
+  } else {
+    row_barrier<WAVES>();                          // the next row's sums come to the same place
   }
 }
 

@@ -19,7 +19,7 @@ def waves(kernels, part):
 def test_norm_kernels():
     """Rows of 8193 to 16384 columns from codes use what registers sixteen waves leave each other, and a few words of scratch
     before their loop."""
-    kernels = without_spills("qa_norm.hip", ("rms_norm_grad_kernelILi0ELi16ELi2ELb1E", "rms_norm_grad_kernelILi1ELi16ELi2ELb1E"))
+    kernels = without_spills("qa_norm.hip", ("rms_norm_grad_kernelILi0ELi1024ELi2ELb1E", "rms_norm_grad_kernelILi1ELi1024ELi2ELb1E"))
     assert all(v["scratch"] <= 32 for v in kernels.values())
     assert waves(kernels, "15rms_norm_kernel") >= 5 and waves(kernels, "rms_norm_grad_kernel") >= 3
 
