@@ -48,6 +48,7 @@ struct NormArgs {
   float* rstd;
   int64_t x_stride, residual_stride, h_stride, y_stride;
   float eps;
+  bool stream;
 };
 
 template <int LANES> constexpr int threads_of = LANES <= kWave ? kThreads : LANES;
@@ -55,6 +56,7 @@ template <int LANES> constexpr int rows_of = threads_of<LANES> / LANES;
 template <int LANES> constexpr int waves_of = LANES <= kWave ? 1 : LANES / kWave;
 
 // Codes and values of eight columns of y, which their lane and its neighbours of the same group hold.
+template <bool STREAM>
 __device__ __forceinline__ void write_y(const NormArgs& A, int64_t row, int64_t col, int n, const float (&y)[kVec]) {
   const int lanes = A.R.group / kVec;
   const uint32_t b = scale_byte(lanes_max_u32(most_of(y), lanes));
@@ -62,13 +64,13 @@ __device__ __forceinline__ void write_y(const NormArgs& A, int64_t row, int64_t 
   float value[kVec];
   const u32x2 code = code8(y, b, value);
   if (A.codes) {
-    store_codes(A.codes + row * A.R.code_stride + col, code, n);
+    store_codes<STREAM>(A.codes + row * A.R.code_stride + col, code, n);
     if ((threadIdx.x % lanes) == 0) A.scales[row * A.R.scale_stride + col / A.R.group] = (uint8_t)b;
   }
-  if (A.y) store_raw<QA_BF16>(A.y + row * A.y_stride + col, from_f32<QA_BF16>(value), n);
+  if (A.y) store_raw<QA_BF16, STREAM>(A.y + row * A.y_stride + col, from_f32<QA_BF16>(value), n);
 }
 
-template <int TYPE, int LANES, int NV>
+template <int TYPE, int LANES, int NV, bool STREAM>
 __global__ __launch_bounds__(threads_of<LANES>) void rms_norm_kernel(NormArgs A) {
   typedef ElemT<TYPE> T;
   __shared__ float sums[2][waves_of<LANES>];
@@ -110,11 +112,11 @@ __global__ __launch_bounds__(threads_of<LANES>) void rms_norm_kernel(NormArgs A)
     if (A.rstd && t == 0) A.rstd[row] = rstd;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      if (A.h && n[v] > 0) store_raw<TYPE>((T*)A.h + row * A.h_stride + col[v], from_f32<TYPE>(h[v]), n[v]);
+      if (A.h && n[v] > 0) store_raw<TYPE, STREAM>((T*)A.h + row * A.h_stride + col[v], from_f32<TYPE>(h[v]), n[v]);
       float y[kVec];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) y[i] = (h[v][i] * rstd) * w[v][i];
-      write_y(A, row, col[v], n[v], y);
+      write_y<STREAM>(A, row, col[v], n[v], y);
     }
   }
 }
@@ -159,7 +161,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs A) {
       if (A.h && n > 0) store_raw<TYPE>((T*)A.h + row * A.h_stride + col, from_f32<TYPE>(h), n);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) y[i] = (h[i] * rstd) * w[i];
-      write_y(A, row, col, n, y);
+      write_y<false>(A, row, col, n, y);
     }
   }
 }
@@ -178,10 +180,11 @@ struct NormGradArgs {
   void* dx;
   float* parts;                                    // sums over the rows of one work-group; NULL: not wanted
   int64_t dy_stride, h_stride, dh_stride, dx_stride;
+  bool stream;
 };
 
 // Eight columns of the residual stream, from its own type or from codes.
-template <int TYPE, bool CODED>
+template <int TYPE, bool CODED, bool STREAM>
 __device__ __forceinline__ void load_h(const NormGradArgs& A, int64_t row, int64_t col, int n, float (&h)[kVec]) {
   if constexpr (CODED) {
     if (n > 0) {
@@ -194,11 +197,11 @@ __device__ __forceinline__ void load_h(const NormGradArgs& A, int64_t row, int64
       for (int i = 0; i < kVec; ++i) h[i] = 0.0f;
     }
   } else {
-    to_f32<TYPE>(load_raw<TYPE>((const ElemT<TYPE>*)A.h + row * A.h_stride + col, n), h);
+    to_f32<TYPE>(load_raw<TYPE, STREAM>((const ElemT<TYPE>*)A.h + row * A.h_stride + col, n), h);
   }
 }
 
-template <int TYPE, int LANES, int NV, bool CODED>
+template <int TYPE, int LANES, int NV, bool CODED, bool STREAM>
 __global__ __launch_bounds__(threads_of<LANES>) void rms_norm_grad_kernel(NormGradArgs A) {
   typedef ElemT<TYPE> T;
   __shared__ float sums[2][waves_of<LANES>];
@@ -221,12 +224,12 @@ __global__ __launch_bounds__(threads_of<LANES>) void rms_norm_grad_kernel(NormGr
     float h[NV][kVec];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      dy_raw[v] = load_raw<TYPE>((const T*)A.dy + row * A.dy_stride + col[v], n[v]);
-      load_h<TYPE, CODED>(A, row, col[v], n[v], h[v]);
+      dy_raw[v] = load_raw<TYPE, STREAM>((const T*)A.dy + row * A.dy_stride + col[v], n[v]);
+      load_h<TYPE, CODED, STREAM>(A, row, col[v], n[v], h[v]);
     }
     if (A.dh) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) dh_raw[v] = load_raw<TYPE>((const T*)A.dh + row * A.dh_stride + col[v], n[v]);
+      for (int v = 0; v < NV; ++v) dh_raw[v] = load_raw<TYPE, STREAM>((const T*)A.dh + row * A.dh_stride + col[v], n[v]);
     }
     const float rstd = A.rstd[row];
     float s = 0.0f;
@@ -307,7 +310,7 @@ __global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(NormGradArgs A
       const int n = (int)min((int64_t)kVec, A.R.cols - col);
       float dy[kVec], h[kVec], w[kVec];
       to_f32<TYPE>(load_raw<TYPE>(dy_row + col, n), dy);
-      load_h<TYPE, CODED>(A, row, col, n, h);
+      load_h<TYPE, CODED, false>(A, row, col, n, h);
       to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col, n), w);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) s = __builtin_fmaf(dy[i] * w[i], h[i] * rstd, s);
@@ -320,7 +323,7 @@ __global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(NormGradArgs A
       if (n <= 0) continue;
       float dy[kVec], h[kVec], w[kVec], dw[kVec], dx[kVec];
       to_f32<TYPE>(load_raw<TYPE>(dy_row + col, n), dy);
-      load_h<TYPE, CODED>(A, row, col, n, h);
+      load_h<TYPE, CODED, false>(A, row, col, n, h);
       to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col, n), w);
       float* part = A.parts ? A.parts + (int64_t)blockIdx.x * A.R.cols + col : nullptr;
       if (part && row != blockIdx.x) {
@@ -412,7 +415,8 @@ int norm_launch(const NormArgs& A, hipStream_t stream) {
   const dim3 grid((unsigned)groups_for(A.R.rows, f));
   if (f.lanes)
     with_form(f, [&](auto lanes, auto vecs) {
-      rms_norm_kernel<TYPE, lanes, vecs><<<grid, threads_of<lanes>, 0, stream>>>(A);
+      if (A.stream) rms_norm_kernel<TYPE, lanes, vecs, true><<<grid, threads_of<lanes>, 0, stream>>>(A);
+      else rms_norm_kernel<TYPE, lanes, vecs, false><<<grid, threads_of<lanes>, 0, stream>>>(A);
     });
   else rms_norm_long_kernel<TYPE><<<grid, 1024, 0, stream>>>(A);
   return launch_status();
@@ -425,7 +429,8 @@ int norm_grad_launch(const NormGradArgs& A, float* dweight, int accumulate, hipS
   if (A.R.rows > 0) {
     if (f.lanes)
       with_form(f, [&](auto lanes, auto vecs) {
-        rms_norm_grad_kernel<TYPE, lanes, vecs, CODED><<<grid, threads_of<lanes>, 0, stream>>>(A);
+        if (A.stream) rms_norm_grad_kernel<TYPE, lanes, vecs, CODED, true><<<grid, threads_of<lanes>, 0, stream>>>(A);
+        else rms_norm_grad_kernel<TYPE, lanes, vecs, CODED, false><<<grid, threads_of<lanes>, 0, stream>>>(A);
       });
     else rms_norm_grad_long_kernel<TYPE, CODED><<<grid, 1024, 0, stream>>>(A);
     if (const int rc = launch_status()) return rc;
@@ -465,7 +470,9 @@ extern "C" int qa_rms_norm(const qa_coded_rows* rows, int type, const void* x, i
       !aligned(y_out, 2) || !aligned(weight, 4) || !aligned(rstd, 4) || !aligned(codes, 16))
     return QA_ERR_ALIGNMENT;
   const NormArgs A{*rows, x, residual, weight, h_out, codes, scales, (__bf16*)y_out, rstd,
-                   x_stride, residual_stride, h_stride, y_stride, eps};
+                   x_stride, residual_stride, h_stride, y_stride, eps,
+                   streams((double)rows->rows * (double)rows->cols *
+                           (double)(type_bytes(type) * (1 + (residual != nullptr) + (h_out != nullptr)) + (codes != nullptr) + 2 * (y_out != nullptr)))};
   const hipStream_t s = (hipStream_t)stream;
   if (type == QA_F32) return norm_launch<QA_F32>(A, s);
   if (type == QA_BF16) return norm_launch<QA_BF16>(A, s);
@@ -493,7 +500,9 @@ extern "C" int qa_rms_norm_grad(const qa_coded_rows* rows, int type, const void*
     return QA_OK;
   }
   const NormGradArgs A{*rows, dy, h, h_codes, h_scales, weight, rstd, dh, dx, dweight ? (float*)ws : nullptr,
-                       dy_stride, h_stride, dh_stride, dx_stride};
+                       dy_stride, h_stride, dh_stride, dx_stride,
+                       streams((double)rows->rows * (double)rows->cols *
+                               (double)(type_bytes(type) * (2 + (dh != nullptr)) + (h ? type_bytes(type) : 1)))};
   const hipStream_t s = (hipStream_t)stream;
   if (type == QA_F32) return norm_grad_launch<QA_F32>(A, dweight, accumulate, s);
   if (type == QA_BF16) return norm_grad_launch<QA_BF16>(A, dweight, accumulate, s);

@@ -27,7 +27,7 @@ RowGrid row_grid(int64_t rows, int64_t cols) {
   return g;
 }
 
-template <int TYPE>
+template <int TYPE, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rows_pack_kernel(qa_coded_rows R, int per_row, int rows_per_group,
                                                              const ElemT<TYPE>* __restrict__ x, int64_t x_stride,
                                                              int8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
@@ -42,13 +42,13 @@ __global__ __launch_bounds__(kThreads) void rows_pack_kernel(qa_coded_rows R, in
     if (here) to_f32<TYPE>(load_raw<TYPE>(x + row * x_stride + col, n), v);
     const uint32_t b = scale_byte(lanes_max_u32(most_of(v), lanes));
     if (here) {
-      store_codes(codes + row * R.code_stride + col, code8(v, b, value), n);
+      store_codes<STREAM>(codes + row * R.code_stride + col, code8(v, b, value), n);
       if ((threadIdx.x % lanes) == 0) scales[row * R.scale_stride + col / R.group] = (uint8_t)b;
     }
   }
 }
 
-template <int TYPE>
+template <int TYPE, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rows_unpack_kernel(qa_coded_rows R, int per_row, int rows_per_group,
                                                                const int8_t* __restrict__ codes,
                                                                const uint8_t* __restrict__ scales,
@@ -62,24 +62,28 @@ __global__ __launch_bounds__(kThreads) void rows_unpack_kernel(qa_coded_rows R, 
     float v[kVec];
     decode8(*reinterpret_cast<const u32x2*>(codes + row * R.code_stride + col),
             scales[row * R.scale_stride + col / R.group], v);
-    store_raw<TYPE>(x + row * x_stride + col, from_f32<TYPE>(v), n);
+    store_raw<TYPE, STREAM>(x + row * x_stride + col, from_f32<TYPE>(v), n);
   }
+}
+
+bool streams(const qa_coded_rows* R, int type) {
+  return qa::streams((double)R->rows * (double)R->cols * (double)(type_bytes(type) + 1));
 }
 
 template <int TYPE>
 int pack_launch(const qa_coded_rows* R, const void* x, int64_t x_stride, int8_t* codes, uint8_t* scales,
                 hipStream_t stream) {
   const RowGrid g = row_grid(R->rows, R->cols);
-  rows_pack_kernel<TYPE><<<g.grid, kThreads, 0, stream>>>(*R, g.per_row, g.rows, (const ElemT<TYPE>*)x, x_stride, codes,
-                                                          scales);
+  const auto kernel = streams(R, TYPE) ? rows_pack_kernel<TYPE, true> : rows_pack_kernel<TYPE, false>;
+  kernel<<<g.grid, kThreads, 0, stream>>>(*R, g.per_row, g.rows, (const ElemT<TYPE>*)x, x_stride, codes, scales);
   return launch_status();
 }
 template <int TYPE>
 int unpack_launch(const qa_coded_rows* R, const int8_t* codes, const uint8_t* scales, void* x, int64_t x_stride,
                   hipStream_t stream) {
   const RowGrid g = row_grid(R->rows, R->cols);
-  rows_unpack_kernel<TYPE><<<g.grid, kThreads, 0, stream>>>(*R, g.per_row, g.rows, codes, scales, (ElemT<TYPE>*)x,
-                                                            x_stride);
+  const auto kernel = streams(R, TYPE) ? rows_unpack_kernel<TYPE, true> : rows_unpack_kernel<TYPE, false>;
+  kernel<<<g.grid, kThreads, 0, stream>>>(*R, g.per_row, g.rows, codes, scales, (ElemT<TYPE>*)x, x_stride);
   return launch_status();
 }
 

@@ -117,6 +117,7 @@ struct TokenArgs {
   int64_t rows, vocab, stride;
   int64_t piece;                                   // logits of one split
   int splits, top;
+  bool stream;
 };
 
 // What a row's sums and alternatives become.  `best` is lane i's alternative i; one wave writes.  Log probabilities are
@@ -195,13 +196,13 @@ __device__ __forceinline__ uint64_t merge_waves(uint64_t v, uint64_t (*lists)[kW
 }
 
 // x[at ..) of a chunk; what lies outside [begin, end) is -infinity.
-template <int TYPE, int NV>
+template <int TYPE, int NV, bool STREAM>
 __device__ __forceinline__ void load_chunk(Raw8<TYPE> (&raw)[NV], const ElemT<TYPE>* x, int64_t at, int64_t begin, int64_t end) {
   const int lane = threadIdx.x % kWave;
   const ElemT<TYPE>* p = x + at + lane * kVec;
   if (at >= begin && at + NV * kWave * kVec <= end) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) raw[k] = load_raw<TYPE>(p + k * kWave * kVec);
+    for (int k = 0; k < NV; ++k) raw[k] = load_raw<TYPE, STREAM>(p + k * kWave * kVec);
   } else {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -288,7 +289,7 @@ __device__ __forceinline__ uint64_t settle(S& shared, int wave, Best& b, int top
 }
 
 // The sums and alternatives of x[begin .. end); wave 0 receives them.  Ends with a barrier.
-template <int TYPE, int WAVES, int NV, int CHUNKS, bool TOP>
+template <int TYPE, int WAVES, int NV, int CHUNKS, bool TOP, bool STREAM>
 __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, int64_t end, int top,
                                          RowShared<WAVES, CHUNKS, TOP>& shared, Sums& a, uint64_t& best) {
   const int wave = WAVES > 1 ? threadIdx.x / kWave : 0, lane = threadIdx.x % kWave, me = wave * kWave + lane;
@@ -299,7 +300,7 @@ __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, in
   // Chunks begin on 16 bytes, wherever the row does: 2.9 -> 2.4 us for 100003 bfloat16 logits of an odd row.
   const int64_t mine = begin - (int64_t)((uintptr_t)(x + begin) % 16 / sizeof(ElemT<TYPE>)) + wave * kChunk;
   Raw8<TYPE> raw[NV];
-  if (mine < end) load_chunk<TYPE, NV>(raw, x, mine, begin, end);
+  if (mine < end) load_chunk<TYPE, NV, STREAM>(raw, x, mine, begin, end);
   int chunks = 0;
   for (int64_t at = mine; at < end; at += kStride, ++chunks) {
     float v[NV][kVec], most[NV];
@@ -308,7 +309,7 @@ __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, in
       to_f32<TYPE>(raw[k], v[k]);
       most[k] = most_of_eight(v[k]);
     }
-    if (at + kStride < end) load_chunk<TYPE, NV>(raw, x, at + kStride, begin, end);
+    if (at + kStride < end) load_chunk<TYPE, NV, STREAM>(raw, x, at + kStride, begin, end);
     float m = most[0];
 #pragma unroll
     for (int k = 1; k < NV; ++k) m = fmaxf(m, most[k]);
@@ -358,14 +359,14 @@ __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, in
     for (int c = 0; c < chunks; ++c)               // 16 bits of a bound of 16 bits: the comparison is that of the whole numbers
       chosen |= (uint64_t)(__any(all || !(as_f32((uint32_t)shared.most[c][me] << 16) < least)) != 0) << c;
     Best b;
-    if (chosen) load_chunk<TYPE, NV>(raw, x, mine + __builtin_ctzll(chosen) * kStride, begin, end);
+    if (chosen) load_chunk<TYPE, NV, false>(raw, x, mine + __builtin_ctzll(chosen) * kStride, begin, end);
     while (chosen) {
       const int64_t at = mine + __builtin_ctzll(chosen) * kStride;
       chosen &= chosen - 1;
       float v[NV][kVec];
 #pragma unroll
       for (int k = 0; k < NV; ++k) to_f32<TYPE>(raw[k], v[k]);
-      if (chosen) load_chunk<TYPE, NV>(raw, x, mine + __builtin_ctzll(chosen) * kStride, begin, end);
+      if (chosen) load_chunk<TYPE, NV, false>(raw, x, mine + __builtin_ctzll(chosen) * kStride, begin, end);
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -392,13 +393,13 @@ __global__ __launch_bounds__(kThreads) void token_narrow_kernel(TokenArgs A) {
     const Given given = given_of<TYPE>(A, row);
     Sums a;
     uint64_t best = 0;
-    read_row<TYPE, 1, NV, CHUNKS, TOP>((const ElemT<TYPE>*)A.x + row * A.stride, 0, A.vocab, A.top, shared[wave], a, best);
+    read_row<TYPE, 1, NV, CHUNKS, TOP, false>((const ElemT<TYPE>*)A.x + row * A.stride, 0, A.vocab, A.top, shared[wave], a, best);
     write_row<TOP>(A, row, given, a, best);
   }
 }
 
 // A work-group per row, or per split of a row.
-template <int TYPE, int NV, bool TOP>
+template <int TYPE, int NV, bool TOP, bool STREAM>
 __global__ __launch_bounds__(kTokenThreads, 4) void token_wide_kernel(TokenArgs A) {
   __shared__ RowShared<kTokenWaves, kNoted, TOP> shared;
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
@@ -408,7 +409,7 @@ __global__ __launch_bounds__(kTokenThreads, 4) void token_wide_kernel(TokenArgs 
     if (A.splits == 1 && wave == 0) given = given_of<TYPE>(A, row);
     Sums a;
     uint64_t best = 0;
-    read_row<TYPE, kTokenWaves, NV, kNoted, TOP>((const ElemT<TYPE>*)A.x + row * A.stride, begin, end, A.top, shared, a, best);
+    read_row<TYPE, kTokenWaves, NV, kNoted, TOP, STREAM>((const ElemT<TYPE>*)A.x + row * A.stride, begin, end, A.top, shared, a, best);
     if (wave == 0) {
       if (A.splits == 1) {
         write_row<TOP>(A, row, given, a, best);
@@ -495,6 +496,7 @@ struct TokenGradArgs {
   const float *stats, *entropy, *g_logprob, *g_entropy;
   void* dx;
   int64_t rows, vocab, x_stride, dx_stride;
+  bool stream;
 };
 
 struct GradRow {
@@ -531,7 +533,7 @@ __device__ __forceinline__ Raw8<TYPE> grad_of(const GradRow& r, const Raw8<TYPE>
 }
 
 constexpr int64_t kGradPiece = (int64_t)kThreads * kVec;       // logits that a work-group has in one vector per lane
-template <int TYPE, int NV>
+template <int TYPE, int NV, bool STREAM>
 __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenGradArgs A) {
   typedef ElemT<TYPE> T;
   for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
@@ -544,27 +546,27 @@ __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenGradArgs A) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int64_t i = lane0 + k * kThreads * kVec;
-        raw[k] = load_raw<TYPE>(x + i, (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i)));
+        raw[k] = load_raw<TYPE, STREAM>(x + i, (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i)));
       }
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int64_t i = lane0 + k * kThreads * kVec;
         const int n = (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i));
-        if (n > 0) store_raw<TYPE>(dx + i, grad_of<TYPE>(r, raw[k], i), n);
+        if (n > 0) store_raw<TYPE, STREAM>(dx + i, grad_of<TYPE>(r, raw[k], i), n);
       }
     }
   }
 }
 // Rows of up to 2048 logits: `per_row` lanes, a power of two, have one vector each.
-template <int TYPE>
+template <int TYPE, bool STREAM>
 __global__ __launch_bounds__(kThreads) void token_grad_narrow_kernel(TokenGradArgs A, int per_row) {
   typedef ElemT<TYPE> T;
   const int rows = kThreads / per_row, local = threadIdx.x / per_row, i = (int)threadIdx.x % per_row * kVec;
   const int n = (int)min((int64_t)kVec, A.vocab - i);
   if (n <= 0) return;
   for (int64_t row = (int64_t)blockIdx.x * rows + local; row < A.rows; row += (int64_t)gridDim.x * rows) {
-    const Raw8<TYPE> raw = load_raw<TYPE>((const T*)A.x + row * A.x_stride + i, n);
-    store_raw<TYPE>((T*)A.dx + row * A.dx_stride + i, grad_of<TYPE>(grad_row(A, row), raw, i), n);
+    const Raw8<TYPE> raw = load_raw<TYPE, STREAM>((const T*)A.x + row * A.x_stride + i, n);
+    store_raw<TYPE, STREAM>((T*)A.dx + row * A.dx_stride + i, grad_of<TYPE>(grad_row(A, row), raw, i), n);
   }
 }
 
@@ -593,8 +595,9 @@ int token_launch(TokenArgs& A, hipStream_t stream) {
   } else {
     const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 16), (unsigned)A.splits);
     A.piece = ceil_div(ceil_div(A.vocab, A.splits), kSplitLogits) * kSplitLogits;
-    if (A.piece <= 2 * kSplitLogits) token_wide_kernel<TYPE, 1, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
-    else token_wide_kernel<TYPE, kTokenVecs, TOP><<<grid, kTokenThreads, 0, stream>>>(A);
+    if (A.piece <= 2 * kSplitLogits) token_wide_kernel<TYPE, 1, TOP, false><<<grid, kTokenThreads, 0, stream>>>(A);
+    else if (A.stream) token_wide_kernel<TYPE, kTokenVecs, TOP, true><<<grid, kTokenThreads, 0, stream>>>(A);
+    else token_wide_kernel<TYPE, kTokenVecs, TOP, false><<<grid, kTokenThreads, 0, stream>>>(A);
     if (A.splits == 1) return launch_status();
     if (const int rc = launch_status()) return rc;
     token_join_kernel<TYPE, TOP><<<dim3((unsigned)A.rows), kTokenThreads, 0, stream>>>(A);
@@ -611,12 +614,14 @@ int token_grad_launch(const TokenGradArgs& A, hipStream_t stream) {
     int per_row = 1;
     while (per_row * kVec < A.vocab) per_row *= 2;
     const dim3 grid((unsigned)std::min<int64_t>(ceil_div(A.rows, kThreads / per_row), 1 << 22));
-    token_grad_narrow_kernel<TYPE><<<grid, kThreads, 0, stream>>>(A, per_row);
+    const auto kernel = A.stream ? token_grad_narrow_kernel<TYPE, true> : token_grad_narrow_kernel<TYPE, false>;
+    kernel<<<grid, kThreads, 0, stream>>>(A, per_row);
   } else {
     constexpr int NV = 4;
     const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 22),
                     (unsigned)std::min<int64_t>(ceil_div(A.vocab, NV * kGradPiece), 1 << 14));
-    token_grad_kernel<TYPE, NV><<<grid, kThreads, 0, stream>>>(A);
+    const auto kernel = A.stream ? token_grad_kernel<TYPE, NV, true> : token_grad_kernel<TYPE, NV, false>;
+    kernel<<<grid, kThreads, 0, stream>>>(A);
   }
   return launch_status();
 }
@@ -651,7 +656,7 @@ extern "C" int qa_token_logprob(int type, int64_t rows, int64_t vocab, const voi
       !aligned(stats, 4) || (top && (!aligned(top_logprob, 4) || !aligned(top_index, 4))))
     return QA_ERR_ALIGNMENT;
   TokenArgs A{logits, target, logprob, entropy, stats, top_logprob, top_index, nullptr, nullptr,
-              rows, vocab, stride, vocab, (int)splits_for(rows, vocab), top};
+              rows, vocab, stride, vocab, (int)splits_for(rows, vocab), top, streams((double)rows * (double)vocab * (double)type_bytes(type))};
   if (A.splits > 1) {
     if (!ws || ws_bytes < qa_token_workspace_bytes(rows, vocab, top)) return QA_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return QA_ERR_ALIGNMENT;
@@ -675,7 +680,8 @@ extern "C" int qa_token_logprob_grad(int type, int64_t rows, int64_t vocab, cons
   if (!element_aligned(logits, type) || !element_aligned(dlogits, type) || !aligned(target, 4) || !aligned(stats, 4) ||
       !aligned(entropy, 4) || !aligned(g_logprob, 4) || !aligned(g_entropy, 4))
     return QA_ERR_ALIGNMENT;
-  const TokenGradArgs A{logits, target, stats, entropy, g_logprob, g_entropy, dlogits, rows, vocab, stride, dlogits_stride};
+  const TokenGradArgs A{logits, target, stats, entropy, g_logprob, g_entropy, dlogits, rows, vocab, stride, dlogits_stride,
+                        streams((double)rows * (double)vocab * (double)(2 * type_bytes(type)))};
   const hipStream_t s = (hipStream_t)stream;
   if (type == QA_F32) return token_grad_launch<QA_F32>(A, s);
   if (type == QA_BF16) return token_grad_launch<QA_BF16>(A, s);
