@@ -1,4 +1,9 @@
 // Log probabilities of given tokens, entropy and the most likely alternatives, and the logits' gradient.
+//
+// Scoring reads every logit once.  4096 x 100003 bfloat16: without alternatives 146 us, 5.6 TB/s, bound by memory; with 8 alternatives
+// 157, with 64 some 205, bound by instructions: some nine per logit, one of them an exponential that takes four times as long,
+// and a few thousand per row for the alternatives.  One row of 128000 with 20 alternatives: 12 us, two launches of some 4 us each and
+// a chain of dependent reads.
 #include <algorithm>
 #include <cfloat>
 
@@ -159,7 +164,8 @@ __device__ __forceinline__ void write_row(const TokenArgs& A, int64_t row, const
 //
 // The waves take chunks of NV vectors per lane in turn.  Each lane has sums against a maximum of its own.  For the
 // alternatives it only notes a chunk's largest logit: at the row's end the `top`-th largest of the lanes' largest is a
-// bound that `top` logits reach, and the few chunks that reach it are read again.
+// bound that `top` logits reach, and the few chunks that reach it are read again.  (A sorted list that each wave keeps while it
+// reads: 278 us for 4096 x 100003 with 8 alternatives; eight waves per row instead of four, sorts through LDS: 221.)
 constexpr int kTokenWaves = 4, kTokenThreads = kTokenWaves * kWave;
 constexpr int kTokenVecs = 2;
 constexpr int64_t kTokenChunk = (int64_t)kTokenVecs * kTokenThreads * kVec;
@@ -218,6 +224,8 @@ __device__ __forceinline__ void load_chunk(Raw8<TYPE> (&raw)[NV], const ElemT<TY
     }
   }
 }
+// The compiler's own maximum takes each operand through one more instruction, for the sake of signaling NaN.  Here such a one can hide
+// what is beside it; read_row() knows then from the sum of exponentials.
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
@@ -297,7 +305,7 @@ __device__ __forceinline__ void read_row(const ElemT<TYPE>* x, int64_t begin, in
   if (TOP && lane == 0 && wave == 0) shared.count = 0;
   a = no_sums();
   float largest = -INFINITY;
-  // Chunks begin on 16 bytes, wherever the row does: 2.9 -> 2.4 us for 100003 bfloat16 logits of an odd row.
+  // Chunks begin on 16 bytes, wherever the row does (4096 rows of 100003 bfloat16 logits without alternatives: 171 -> 146 us).
   const int64_t mine = begin - (int64_t)((uintptr_t)(x + begin) % 16 / sizeof(ElemT<TYPE>)) + wave * kChunk;
   Raw8<TYPE> raw[NV];
   if (mine < end) load_chunk<TYPE, NV, STREAM>(raw, x, mine, begin, end);
@@ -515,7 +523,8 @@ __device__ __forceinline__ GradRow grad_row(const TokenGradArgs& A, int64_t row)
   r.log_sum = A.stats[2 * row + 1];
   return r;
 }
-// dx_j = -p_j (a + e (log p_j + H)), and a more at the target.
+// dx_j = -p_j (a + e (log p_j + H)), and a more at the target.  Bound by memory: 8192 x 32768 bfloat16 183 us, 5.9 TB/s; 509 x 47236
+// binary32 in rows of 47239: 43 us, 4.5 TB/s.
 template <int TYPE>
 __device__ __forceinline__ Raw8<TYPE> grad_of(const GradRow& r, const Raw8<TYPE>& raw, int64_t i) {
   float v[kVec], d[kVec];
@@ -557,7 +566,8 @@ __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenGradArgs A) {
     }
   }
 }
-// Rows of up to 2048 logits: `per_row` lanes, a power of two, have one vector each.
+// Rows of up to 2048 logits: `per_row` lanes, a power of two, have one vector each (a work-group for each row: 16384 x 8 logits 61 us
+// instead of 6, 8192 x 2000 36 instead of 14).
 template <int TYPE, bool STREAM>
 __global__ __launch_bounds__(kThreads) void token_grad_narrow_kernel(TokenGradArgs A, int per_row) {
   typedef ElemT<TYPE> T;
