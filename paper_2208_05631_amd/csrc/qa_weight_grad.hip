@@ -62,36 +62,18 @@ __device__ __forceinline__ void split_parts(float (&v)[kVec], u32x4 (&part)[P]) 
 }
 template <int TYPE> constexpr int parts_of = TYPE == QA_F32 ? 3 : TYPE == QA_F16 ? 2 : 1;
 
-// The order of a phase's instructions in the large bfloat16 tile: everything else in the shadow of the matrix instructions
-// (left to the compiler the reads of LDS and the decoding stand together in front of them: 1.04 ms instead of 0.94).
-template <int TYPE, int FN, int FK>
-__device__ __forceinline__ void interleave(int phase) {
-  constexpr int kMatrix = 8, kVector = 2, kLdsRead = 0x100, kLdsWrite = 0x200, kRead = 0x20;
-  if (TYPE == QA_BF16 && FN * FK == 8) {
-    if (phase == 0) {
+// The order of a phase's instructions: N times a matrix instruction and in its shadow READS reads of LDS, VECTOR vector instructions,
+// WRITES writes to LDS and LOADS reads of memory.
+template <int N, int READS, int VECTOR, int WRITES, int LOADS>
+__device__ __forceinline__ void interleave() {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kLdsRead, 3, 0);
-        __builtin_amdgcn_sched_group_barrier(kVector, 4, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kVector, 10, 0);
-        __builtin_amdgcn_sched_group_barrier(kLdsWrite, 1, 0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(kVector, 2, 0);
-        if (i % 2) __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
-      }
-    }
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);
+    __builtin_amdgcn_sched_group_barrier(0x200, WRITES, 0);
+    __builtin_amdgcn_sched_group_barrier(0x020, LOADS, 0);
   }
-  __builtin_amdgcn_sched_barrier(0);
 }
 
 // WN x WK waves, FN x FK tiles of 32 x 32 each: a work-group has 32 WN FN columns of dY and 32 WK FK of X.  While one step's
@@ -107,9 +89,10 @@ struct Worker {
   static constexpr int kRow = kTile + kGap, kPart = kStep * kRow, kBuffer = (P + 1) * kPart;
   static constexpr int kBuffers = P == 1 ? 3 : 2;  // of 160 KiB
   static_assert(P == 1 || kDy + 2 <= 2 * P, "a step has a phase for each part of its work");
-  // Steps whose elements are on their way (one in the large tile: 0.99 ms).  A step of small tiles takes a third of the time that a
-  // read takes.
-  static constexpr int kAhead = FN * FK == 8 ? 2 : 4;
+  // Steps whose elements are on their way (one in the large tile: 0.99 ms).  A step of a small tile takes a third of the time that a
+  // read takes, unless dY has several parts: bfloat16, 4096 rows, 2048 x 2048: 53 us (with two 57), and binary16, 2048 rows: 45 (44).
+  // Rows are taken kAhead steps at a time, so that one row costs 1.6 us more with four than with two.
+  static constexpr int kAhead = FN * FK == 8 || P > 1 ? 2 : 4;
 
   const WeightGradArgs& A;
   int64_t n0, k0, t_end, t_load;
@@ -238,22 +221,44 @@ struct Worker {
       for (int j = 0; j < FK; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d[phase & 1][i], x[phase / P & 1][j], acc[i][j], 0, 0, 0);
   }
-  // One step: the buffer `now` is multiplied, what was loaded for the step that is kBuffers - 1 ahead goes to `last`.
+  // One step: the buffer `now` is multiplied, what was loaded for the step that is kBuffers - 1 ahead goes to `last`.  What is to be
+  // done beside the matrix instructions is laid out over as many phases as there are, and inside a phase it stands in their
+  // shadow: left to the compiler the reads of LDS and the decoding stand together in front of them (large bfloat16 tiles: 1.04 ms
+  // instead of 0.94).
+  template <int PHASE>
+  static __device__ __forceinline__ void phases(Worker& w, Loaded& loaded, int64_t t, const __bf16* __restrict__ now,
+                                                const __bf16* __restrict__ next, __bf16* __restrict__ last) {
+    constexpr int kAll = FN * FK, kXPhase = P == 1 ? 0 : kDy, kLoadPhase = kXPhase + 1;
+    if constexpr (PHASE + 1 < 2 * P) w.operands(now, PHASE + 1);
+    else if constexpr (kBuffers == 3) w.operands(next, 0);
+#pragma unroll
+    for (int v = 0; v < kDy; ++v)
+      if (PHASE == (P == 1 ? 0 : v)) w.store_dy(loaded, v, last);
+    if constexpr (PHASE == kXPhase) w.store_x(loaded, last, t + (kBuffers - 1) * kStep);
+    if constexpr (PHASE == kLoadPhase) w.load(loaded);
+    w.multiply(PHASE);
+    if constexpr (P == 1 && kAll == 8 && PHASE == 0) {
+      interleave<4, 3, 4, 0, 0>();
+      interleave<4, 0, 10, 1, 0>();
+    } else if constexpr (P == 1 && kAll == 8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        interleave<1, 2, 2, 0, 0>();
+        interleave<1, 2, 2, 0, 1>();
+      }
+    } else if constexpr (P > 1 && PHASE < kDy) {
+      interleave<kAll, 8 / kAll, (P == 3 ? 64 : 36) / kAll, 1, 0>();
+    } else if constexpr (P > 1 && PHASE == kXPhase) {
+      interleave<kAll, 8 / kAll, 48 * kX / kAll, 1, 0>();
+    } else if constexpr (P > 1) {
+      interleave<kAll, 8 / kAll, 16 / kAll, 0, 8 / kAll>();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (PHASE + 1 < 2 * P) phases<PHASE + 1>(w, loaded, t, now, next, last);
+  }
   static __device__ __forceinline__ void step(Worker& w, Loaded& loaded, int64_t t, const __bf16* __restrict__ now,
                                               const __bf16* __restrict__ next, __bf16* __restrict__ last) {
-#pragma unroll
-    for (int phase = 0; phase < 2 * P; ++phase) {
-      if (phase + 1 < 2 * P) w.operands(now, phase + 1);
-      else if (kBuffers == 3) w.operands(next, 0);
-      // what is to be done beside the matrix instructions, over as many phases as there are
-#pragma unroll
-      for (int v = 0; v < kDy; ++v)
-        if (phase == (P == 1 ? 0 : v)) w.store_dy(loaded, v, last);
-      if (phase == (P == 1 ? 0 : kDy)) w.store_x(loaded, last, t + (kBuffers - 1) * kStep);
-      if (phase == (P == 1 ? 1 : kDy + 1)) w.load(loaded);
-      w.multiply(phase);
-      interleave<TYPE, FN, FK>(phase);
-    }
+    phases<0>(w, loaded, t, now, next, last);
     __syncthreads();
     if (kBuffers == 2) w.operands(next, 0);
   }
