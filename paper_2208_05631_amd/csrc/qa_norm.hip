@@ -1,9 +1,9 @@
 // Root-mean-square norm of a residual stream with an output in 8 bits, and its backward pass.
 //
-// Both are bound by memory, and hold a row in registers between its sum and its outputs.  Forward, 8192 x 4096 bfloat16 with
-// everything written: 303 MB in 50 us, 6.1 TB/s; one row of 8192: 1.5 us of device time in a call of 6.  Backward, 16384 x 4096 with
-// the gradient that comes past the norm: 537 MB in 101 us, 5.3 TB/s.  Rows of an odd number of columns begin inside a 16-byte word and
-// cost a fifth more (8192 x 4097: 69 us against 58, both without streaming stores).
+// Both are bound by memory, hold a row in registers between its sum and its outputs, and read the next row meanwhile.  Forward, 8192 x
+// 4096 bfloat16 with everything written: 303 MB in 52 us, 5.8 TB/s; one row of 8192: 1.5 us of device time in a call of 6.  Backward,
+// 16384 x 4096 with the gradient that comes past the norm: 537 MB in 88 us, 6.1 TB/s.  Rows of an odd number of columns begin inside a
+// 16-byte word and cost more (8192 x 4097: 71 us and 76).
 #include <algorithm>
 #include <type_traits>
 
@@ -13,8 +13,8 @@ namespace qa {
 namespace {
 
 // A row is held in the registers of LANES lanes, NV vectors of eight columns each: one read of everything.  Rows of
-// up to 1024 columns lie inside a wave and need no barrier; of up to 128, the norms of attention heads, four do.
-// (524288 rows of 128 bfloat16: 115 us, and 301 with a wave for each.)
+// up to 1024 columns lie inside a wave and need no barrier; of up to 128, the norms of attention heads, four do, of up to 64 eight.
+// (524288 rows of 128 bfloat16: 100 us, and 301 with a wave for each; of 64: 51, and 85 with sixteen lanes.)
 constexpr int kHeldCols = 16384;                   // 16 waves, two vectors per lane; longer rows are read twice
 
 // Sum over the LANES lanes of a row.  `lds` holds a float for each of their waves that no other call uses before the next
@@ -25,7 +25,7 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
     v += as_f32(other_lane<1>(as_u32(v)));
     v += as_f32(other_lane<2>(as_u32(v)));
     v += as_f32(other_lane<4>(as_u32(v)));
-    v += as_f32(other_lane<8>(as_u32(v)));
+    if constexpr (LANES >= 16) v += as_f32(other_lane<8>(as_u32(v)));
     if constexpr (LANES == 32) v += as_f32(other_lane<16>(as_u32(v)));
     return v;
   } else {
@@ -39,6 +39,42 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
     for (int w = 1; w < W; ++w) s += lds[w];
     return s;
   }
+}
+
+// The next row is read ahead where that leaves registers for five waves per SIMD forward and three backward.  (16384 columns backward,
+// which would spill: 195 us -> 218.)
+template <int TYPE, int LANES, int NV> constexpr bool kAhead = LANES < 1024 && !(TYPE == QA_F32 && NV == 2);
+template <int LANES> constexpr int kLeast = LANES < 1024 ? 5 : 4;
+template <int LANES> constexpr int kLeastGrad = LANES < 1024 ? 3 : 4;
+
+// Eight columns of a row from `col`, of which it has n.  The end of a row is read from its last eight elements, and placed() moves
+// them to where they belong: a branch around a load waits for it, and rows are read ahead.  (16384 x 2047 bfloat16, backward: 80 us ->
+// 69 in all.)  Rows of fewer than eight columns, of the narrowest form, are read by elements, and
+// those of sixteen waves, which have no registers for this.
+template <typename I>
+struct Place {
+  I at;                                            // read from here
+  int shift;
+};
+template <int LANES, typename I>
+__device__ __forceinline__ Place<I> place_of(I col, int n, I cols) {
+  if (LANES == 1024) return {col, 0};
+  if (LANES == 8 && cols < kVec) return {0, 0};
+  return {min(col, cols - kVec), max(0, min(kVec, kVec - n))};
+}
+template <int TYPE, bool STREAM, int LANES, typename I>
+__device__ __forceinline__ Raw8<TYPE> load_place(const ElemT<TYPE>* row, Place<I> place, int n, int64_t cols) {
+  if (LANES == 1024 || (LANES == 8 && cols < kVec)) return load_raw<TYPE, STREAM>(row + place.at, n);
+  return load_raw<TYPE, STREAM>(row + place.at);
+}
+template <typename I>
+__device__ __forceinline__ void placed(Place<I> place, float (&v)[kVec]) {
+  if (place.shift == 0) return;
+#pragma unroll
+  for (int by = 1; by <= kVec; by *= 2)
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (place.shift & by) v[i] = i + by < kVec ? v[i + by] : 0.0f;
 }
 
 struct NormArgs {
@@ -61,9 +97,9 @@ template <int LANES> constexpr int rows_of = threads_of<LANES> / LANES;
 template <int LANES> constexpr int waves_of = LANES <= kWave ? 1 : LANES / kWave;
 
 // Codes and values of eight columns of y, which their lane and its neighbours of the same group hold.
-template <bool STREAM>
+template <int LANES, bool STREAM>
 __device__ __forceinline__ void write_y(const NormArgs& A, int64_t row, int64_t col, int n, const float (&y)[kVec]) {
-  const int lanes = A.R.group / kVec;
+  const int lanes = LANES < 16 ? min(A.R.group / kVec, LANES) : A.R.group / kVec;  // of one row
   const uint32_t b = scale_byte(lanes_max_u32(most_of(y), lanes));
   if (n <= 0) return;
   float value[kVec];
@@ -76,29 +112,36 @@ __device__ __forceinline__ void write_y(const NormArgs& A, int64_t row, int64_t 
 }
 
 template <int TYPE, int LANES, int NV, bool STREAM>
-__global__ __launch_bounds__(threads_of<LANES>) void rms_norm_kernel(NormArgs A) {
+__global__ __launch_bounds__(threads_of<LANES>) __attribute__((amdgpu_waves_per_eu(kLeast<LANES>))) void rms_norm_kernel(NormArgs A) {
   typedef ElemT<TYPE> T;
   __shared__ float sums[2][waves_of<LANES>];
   const int t = threadIdx.x % LANES;
   const int64_t step = (int64_t)gridDim.x * rows_of<LANES>;
-  int64_t col[NV];
-  int n[NV];
+  const int cols = (int)A.R.cols;
+  int col[NV], n[NV];
+  Place<int> place[NV];
   float w[NV][kVec];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    col[v] = ((int64_t)v * LANES + t) * kVec;
-    n[v] = (int)min((int64_t)kVec, A.R.cols - col[v]);
+    col[v] = (v * LANES + t) * kVec;
+    n[v] = min(kVec, cols - col[v]);
+    place[v] = place_of<LANES>(col[v], n[v], cols);
     to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col[v], n[v]), w[v]);
   }
-  int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * rows_of<LANES> + threadIdx.x / LANES; row < A.R.rows; row += step) {
-    Raw8<TYPE> x[NV], r[NV];
+  Raw8<TYPE> x[NV], r[NV];
+  auto read = [&](int64_t row) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) x[v] = load_raw<TYPE>((const T*)A.x + row * A.x_stride + col[v], n[v]);
+    for (int v = 0; v < NV; ++v) x[v] = load_place<TYPE, STREAM, LANES>((const T*)A.x + row * A.x_stride, place[v], n[v], cols);
     if (A.residual) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) r[v] = load_raw<TYPE>((const T*)A.residual + row * A.residual_stride + col[v], n[v]);
+      for (int v = 0; v < NV; ++v) r[v] = load_place<TYPE, STREAM, LANES>((const T*)A.residual + row * A.residual_stride, place[v], n[v], cols);
     }
+  };
+  int turn = 0;
+  int64_t row = (int64_t)blockIdx.x * rows_of<LANES> + threadIdx.x / LANES;
+  if (kAhead<TYPE, LANES, NV> && row < A.R.rows) read(row);
+  for (; row < A.R.rows; row += step) {
+    if (!kAhead<TYPE, LANES, NV>) read(row);
     float h[NV][kVec], s = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -109,9 +152,11 @@ __global__ __launch_bounds__(threads_of<LANES>) void rms_norm_kernel(NormArgs A)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) h[v][i] += more[i];
       }
+      placed(place[v], h[v]);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) s = __builtin_fmaf(h[v][i], h[v][i], s);
     }
+    if (kAhead<TYPE, LANES, NV> && row + step < A.R.rows) read(row + step);
     const float rstd = 1.0f / sqrtf(row_sum<LANES>(s, sums[turn]) / (float)A.R.cols + A.eps);
     turn ^= 1;
     if (A.rstd && t == 0) A.rstd[row] = rstd;
@@ -121,7 +166,7 @@ __global__ __launch_bounds__(threads_of<LANES>) void rms_norm_kernel(NormArgs A)
       float y[kVec];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) y[i] = (h[v][i] * rstd) * w[v][i];
-      write_y<STREAM>(A, row, col[v], n[v], y);
+      write_y<LANES, STREAM>(A, row, col[v], n[v], y);
     }
   }
 }
@@ -166,7 +211,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs A) {
       if (A.h && n > 0) store_raw<TYPE>((T*)A.h + row * A.h_stride + col, from_f32<TYPE>(h), n);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) y[i] = (h[i] * rstd) * w[i];
-      write_y<false>(A, row, col, n, y);
+      write_y<1024, false>(A, row, col, n, y);
     }
   }
 }
@@ -188,60 +233,94 @@ struct NormGradArgs {
   bool stream;
 };
 
-// Eight columns of the residual stream, from its own type or from codes.
-template <int TYPE, bool CODED, bool STREAM>
-__device__ __forceinline__ void load_h(const NormGradArgs& A, int64_t row, int64_t col, int n, float (&h)[kVec]) {
-  if constexpr (CODED) {
-    if (n > 0) {
-      decode8(*reinterpret_cast<const u32x2*>(A.codes + row * A.R.code_stride + col),
-              A.scales[row * A.R.scale_stride + col / A.R.group], h);
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) h[i] = i < n ? h[i] : 0.0f;
-    } else {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) h[i] = 0.0f;
-    }
+// Eight columns of the residual stream, of its own type or codes, as they are in memory.
+template <int TYPE, bool CODED> struct RawH { Raw8<TYPE> h; };
+template <int TYPE> struct RawH<TYPE, true> { u32x2 code; uint32_t scale; };
+template <int TYPE, bool CODED, bool STREAM, int LANES, typename I>
+__device__ __forceinline__ RawH<TYPE, CODED> load_h(const NormGradArgs& A, int64_t row, I col, Place<I> place, int n) {
+  RawH<TYPE, CODED> raw;
+  if constexpr (CODED) {                           // no branch: one would wait for the loads at its end
+    if (n <= 0) col = 0;
+    raw.code = *reinterpret_cast<const u32x2*>(A.codes + row * A.R.code_stride + col);
+    raw.scale = A.scales[row * A.R.scale_stride + (col >> __builtin_ctz(A.R.group))];
   } else {
-    to_f32<TYPE>(load_raw<TYPE, STREAM>((const ElemT<TYPE>*)A.h + row * A.h_stride + col, n), h);
+    raw.h = load_place<TYPE, STREAM, LANES>((const ElemT<TYPE>*)A.h + row * A.h_stride, place, n, A.R.cols);
+  }
+  return raw;
+}
+template <int TYPE, bool CODED, typename I>
+__device__ __forceinline__ void values_of(const RawH<TYPE, CODED>& raw, Place<I> place, int n, float (&h)[kVec]) {
+  if constexpr (CODED) {
+    decode8(raw.code, raw.scale, h);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) h[i] = i < n ? h[i] : 0.0f;
+  } else {
+    to_f32<TYPE>(raw.h, h);
+    placed(place, h);
   }
 }
 
 template <int TYPE, int LANES, int NV, bool CODED, bool STREAM>
-__global__ __launch_bounds__(threads_of<LANES>) void rms_norm_grad_kernel(NormGradArgs A) {
+__global__ __launch_bounds__(threads_of<LANES>) __attribute__((amdgpu_waves_per_eu(kLeastGrad<LANES>))) void rms_norm_grad_kernel(NormGradArgs A) {
   typedef ElemT<TYPE> T;
   __shared__ float sums[2][waves_of<LANES>];
   const int t = threadIdx.x % LANES;
   const int64_t first = (int64_t)blockIdx.x * rows_of<LANES> + threadIdx.x / LANES;
-  int64_t col[NV];
-  int n[NV];
+  const int cols = (int)A.R.cols;
+  int col[NV], n[NV];
+  Place<int> place[NV];
   float w[NV][kVec], dw[NV][kVec];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    col[v] = ((int64_t)v * LANES + t) * kVec;
-    n[v] = (int)min((int64_t)kVec, A.R.cols - col[v]);
+    col[v] = (v * LANES + t) * kVec;
+    n[v] = min(kVec, cols - col[v]);
+    place[v] = place_of<LANES>(col[v], n[v], cols);
     to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col[v], n[v]), w[v]);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) dw[v][i] = 0.0f;
   }
+  const int64_t step = (int64_t)gridDim.x * rows_of<LANES>;
+  Raw8<TYPE> next_dy[NV], next_dh[NV];
+  RawH<TYPE, CODED> next_h[NV];
+  float next_rstd = 0.0f;
+  auto read = [&](int64_t row) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      next_dy[v] = load_place<TYPE, STREAM, LANES>((const T*)A.dy + row * A.dy_stride, place[v], n[v], cols);
+      next_h[v] = load_h<TYPE, CODED, STREAM, LANES>(A, row, col[v], place[v], n[v]);
+    }
+    next_rstd = A.rstd[row];
+  };
+  auto read_dh = [&](Raw8<TYPE> (&dh)[NV], int64_t row) {
+    if (!A.dh) return;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+      dh[v] = load_place<TYPE, STREAM, LANES>((const T*)A.dh + row * A.dh_stride, place[v], n[v], cols);
+  };
+  constexpr bool AHEAD = kAhead<TYPE, LANES, NV>, DH_AHEAD = AHEAD && !CODED;  // codes take the registers that this takes
   int turn = 0;
-  for (int64_t row = first; row < A.R.rows; row += (int64_t)gridDim.x * rows_of<LANES>) {
+  if (AHEAD && first < A.R.rows) read(first);
+  if (DH_AHEAD && first < A.R.rows) read_dh(next_dh, first);
+  for (int64_t row = first; row < A.R.rows; row += step) {
+    if (!AHEAD) read(row);
+    if (!DH_AHEAD) read_dh(next_dh, row);
     Raw8<TYPE> dy_raw[NV], dh_raw[NV];
     float h[NV][kVec];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      dy_raw[v] = load_raw<TYPE, STREAM>((const T*)A.dy + row * A.dy_stride + col[v], n[v]);
-      load_h<TYPE, CODED, STREAM>(A, row, col[v], n[v], h[v]);
+      dy_raw[v] = next_dy[v];
+      if (A.dh) dh_raw[v] = next_dh[v];
+      values_of<TYPE, CODED>(next_h[v], place[v], n[v], h[v]);
     }
-    if (A.dh) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) dh_raw[v] = load_raw<TYPE, STREAM>((const T*)A.dh + row * A.dh_stride + col[v], n[v]);
-    }
-    const float rstd = A.rstd[row];
+    const float rstd = next_rstd;
+    if (AHEAD && row + step < A.R.rows) read(row + step);
+    if (DH_AHEAD && row + step < A.R.rows) read_dh(next_dh, row + step);
     float s = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float dy[kVec];
       to_f32<TYPE>(dy_raw[v], dy);
+      placed(place[v], dy);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         h[v][i] *= rstd;                           // n
@@ -254,16 +333,20 @@ __global__ __launch_bounds__(threads_of<LANES>) void rms_norm_grad_kernel(NormGr
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float dy[kVec], dx[kVec];
+      if constexpr (TYPE != QA_F32) asm("" : "+v"(dy_raw[v].a));  // what is kept is the words, not what they were converted to
       to_f32<TYPE>(dy_raw[v], dy);
+      placed(place[v], dy);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) dx[i] = rstd * (dy[i] * w[v][i] - h[v][i] * c);
       if (A.dh) {
         float dh[kVec];
+        if constexpr (TYPE != QA_F32) asm("" : "+v"(dh_raw[v].a));
         to_f32<TYPE>(dh_raw[v], dh);
+        placed(place[v], dh);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) dx[i] += dh[i];
       }
-      if (n[v] > 0) store_raw<TYPE>((T*)A.dx + row * A.dx_stride + col[v], from_f32<TYPE>(dx), n[v]);
+      if (n[v] > 0) store_raw<TYPE, STREAM>((T*)A.dx + row * A.dx_stride + col[v], from_f32<TYPE>(dx), n[v]);
     }
   }
   if (!A.parts) return;
@@ -274,6 +357,7 @@ __global__ __launch_bounds__(threads_of<LANES>) void rms_norm_grad_kernel(NormGr
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
+        if constexpr (LANES <= 8) dw[v][i] += as_f32(other_lane<8>(as_u32(dw[v][i])));
         if constexpr (LANES <= 16) dw[v][i] += as_f32(other_lane<16>(as_u32(dw[v][i])));
         if constexpr (LANES <= 32) dw[v][i] += as_f32(other_lane<32>(as_u32(dw[v][i])));
       }
@@ -315,7 +399,8 @@ __global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(NormGradArgs A
       const int n = (int)min((int64_t)kVec, A.R.cols - col);
       float dy[kVec], h[kVec], w[kVec];
       to_f32<TYPE>(load_raw<TYPE>(dy_row + col, n), dy);
-      load_h<TYPE, CODED, false>(A, row, col, n, h);
+      const auto place = place_of<1024>(col, n, A.R.cols);
+      values_of<TYPE, CODED>(load_h<TYPE, CODED, false, 1024>(A, row, col, place, n), place, n, h);
       to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col, n), w);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) s = __builtin_fmaf(dy[i] * w[i], h[i] * rstd, s);
@@ -328,7 +413,8 @@ __global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(NormGradArgs A
       if (n <= 0) continue;
       float dy[kVec], h[kVec], w[kVec], dw[kVec], dx[kVec];
       to_f32<TYPE>(load_raw<TYPE>(dy_row + col, n), dy);
-      load_h<TYPE, CODED, false>(A, row, col, n, h);
+      const auto place = place_of<1024>(col, n, A.R.cols);
+      values_of<TYPE, CODED>(load_h<TYPE, CODED, false, 1024>(A, row, col, place, n), place, n, h);
       to_f32<QA_F32>(load_raw<QA_F32>(A.weight + col, n), w);
       float* part = A.parts ? A.parts + (int64_t)blockIdx.x * A.R.cols + col : nullptr;
       if (part && row != blockIdx.x) {
@@ -385,6 +471,7 @@ __global__ __launch_bounds__(1024) void norm_weight_kernel(const float* __restri
 // Lanes per row (0: the row is read twice) and vectors per lane.
 struct Form { int lanes, vecs; };
 Form form_of(int64_t cols) {
+  if (cols <= 64) return {8, 1};
   if (cols <= 128) return {16, 1};
   if (cols <= 256) return {32, 1};
   if (cols <= 512) return {64, 1};
@@ -395,57 +482,66 @@ Form form_of(int64_t cols) {
   if (cols <= kHeldCols) return {1024, 2};
   return {0, 0};
 }
-// Work-groups: 16 waves per compute unit.
-int64_t groups_for(int64_t rows, Form f) {
+// Work-groups, from threads per compute unit: where rows are read ahead some 4096 columns at a time are on their way to each, and
+// twice as many where they are codes.  More are slower, by the rows that meet in memory and, backward, by the work-groups' sums
+// (16384 x 4096 bfloat16, 256 threads, 512 and 1024: forward 101 us, 114 and 113, backward 87, 90 and 105).  Calls that the caches hold
+// do not mind forward, and are spread wider.
+int64_t groups_for(int64_t rows, Form f, int64_t threads_per_unit) {
   const int64_t threads = f.lanes == 0 ? 1024 : f.lanes <= kWave ? kThreads : f.lanes;
-  return std::min<int64_t>(ceil_div(rows, f.lanes && f.lanes <= kWave ? kThreads / f.lanes : 1), 256 * 1024 / threads);
+  return std::min<int64_t>(ceil_div(rows, f.lanes && f.lanes <= kWave ? kThreads / f.lanes : 1),
+                           256 * std::max<int64_t>(threads_per_unit / threads, 1));
+}
+int64_t norm_groups(int64_t rows, Form f, int type, bool stream) {
+  return groups_for(rows, f, f.lanes == 0 ? 1024 : stream && f.vecs == 2 && type != QA_F32 ? 256 : 512);
+}
+int64_t norm_grad_groups(int64_t rows, Form f, int type, bool coded) {
+  if (f.lanes == 0 || (type == QA_F32 && f.vecs == 2)) return groups_for(rows, f, 1024);
+  return groups_for(rows, f, (coded ? 2 : 1) * (f.vecs == 2 ? 256 : 512));
 }
 
 // Calls `launch` with the lanes and vectors of a form as constants.
+template <int LANES, int VECS, typename F>
+bool launched(Form f, F launch) {
+  if (f.lanes != LANES || f.vecs != VECS) return false;
+  launch(std::integral_constant<int, LANES>{}, std::integral_constant<int, VECS>{});
+  return true;
+}
 template <typename F>
-void with_form(Form f, F launch) {
-  using std::integral_constant;
-#define QA_FORM(LANES, VECS) if (f.lanes == LANES && f.vecs == VECS) launch(integral_constant<int, LANES>{}, integral_constant<int, VECS>{})
-  QA_FORM(16, 1);
-  QA_FORM(32, 1);
-  QA_FORM(64, 1);
-  QA_FORM(64, 2);
-  QA_FORM(256, 1);
-  QA_FORM(256, 2);
-  QA_FORM(512, 2);
-  QA_FORM(1024, 2);
-#undef QA_FORM
+bool with_form(Form f, F launch) {
+  return launched<8, 1>(f, launch) || launched<16, 1>(f, launch) || launched<32, 1>(f, launch) || launched<64, 1>(f, launch) ||
+         launched<64, 2>(f, launch) || launched<256, 1>(f, launch) || launched<256, 2>(f, launch) || launched<512, 2>(f, launch) ||
+         launched<1024, 2>(f, launch);
 }
 
 template <int TYPE>
 int norm_launch(const NormArgs& A, hipStream_t stream) {
   const Form f = form_of(A.R.cols);
-  const dim3 grid((unsigned)groups_for(A.R.rows, f));
-  if (f.lanes)
-    with_form(f, [&](auto lanes, auto vecs) {
-      if (A.stream) rms_norm_kernel<TYPE, lanes, vecs, true><<<grid, threads_of<lanes>, 0, stream>>>(A);
-      else rms_norm_kernel<TYPE, lanes, vecs, false><<<grid, threads_of<lanes>, 0, stream>>>(A);
-    });
-  else rms_norm_long_kernel<TYPE><<<grid, 1024, 0, stream>>>(A);
+  const dim3 grid((unsigned)norm_groups(A.R.rows, f, TYPE, A.stream));
+  auto held = [&](auto lanes, auto vecs) {
+    if (A.stream) rms_norm_kernel<TYPE, lanes, vecs, true><<<grid, threads_of<lanes>, 0, stream>>>(A);
+    else rms_norm_kernel<TYPE, lanes, vecs, false><<<grid, threads_of<lanes>, 0, stream>>>(A);
+  };
+  if (!with_form(f, held)) rms_norm_long_kernel<TYPE><<<grid, 1024, 0, stream>>>(A);
   return launch_status();
 }
 
 template <int TYPE, bool CODED>
 int norm_grad_launch(const NormGradArgs& A, float* dweight, int accumulate, hipStream_t stream) {
   const Form f = form_of(A.R.cols);
-  const dim3 grid((unsigned)groups_for(A.R.rows, f));
+  const dim3 grid((unsigned)norm_grad_groups(A.R.rows, f, TYPE, CODED));
   if (A.R.rows > 0) {
-    if (f.lanes)
-      with_form(f, [&](auto lanes, auto vecs) {
-        if (A.stream) rms_norm_grad_kernel<TYPE, lanes, vecs, CODED, true><<<grid, threads_of<lanes>, 0, stream>>>(A);
-        else rms_norm_grad_kernel<TYPE, lanes, vecs, CODED, false><<<grid, threads_of<lanes>, 0, stream>>>(A);
-      });
-    else rms_norm_grad_long_kernel<TYPE, CODED><<<grid, 1024, 0, stream>>>(A);
+    auto held = [&](auto lanes, auto vecs) {
+      constexpr bool STREAM = TYPE != QA_F32;
+      if (STREAM && A.stream) rms_norm_grad_kernel<TYPE, lanes, vecs, CODED, STREAM><<<grid, threads_of<lanes>, 0, stream>>>(A);
+      else rms_norm_grad_kernel<TYPE, lanes, vecs, CODED, false><<<grid, threads_of<lanes>, 0, stream>>>(A);
+    };
+    if (!with_form(f, held))
+      rms_norm_grad_long_kernel<TYPE, CODED><<<grid, 1024, 0, stream>>>(A);
     if (const int rc = launch_status()) return rc;
   }
   if (!dweight) return QA_OK;
   norm_weight_kernel<<<dim3((unsigned)ceil_div(A.R.cols, kWave)), 1024, 0, stream>>>(
-      A.parts, groups_for(A.R.rows, f), A.R.cols, dweight, accumulate);
+      A.parts, grid.x, A.R.cols, dweight, accumulate);
   return launch_status();
 }
 template <int TYPE>
@@ -456,8 +552,8 @@ int norm_grad_launch(const NormGradArgs& A, float* dweight, int accumulate, hipS
 
 }  // namespace
 
-size_t rms_norm_grad_workspace_bytes(const qa_coded_rows* R, int) {
-  return (size_t)groups_for(R->rows, form_of(R->cols)) * (size_t)R->cols * sizeof(float);
+size_t rms_norm_grad_workspace_bytes(const qa_coded_rows* R, int type) {
+  return (size_t)norm_grad_groups(R->rows, form_of(R->cols), type, true) * (size_t)R->cols * sizeof(float);
 }
 
 }  // namespace qa

@@ -22,8 +22,8 @@ inline int check_rows(const qa_coded_rows* R) {
 }
 
 // Whether a call reads and writes more than the last-level cache holds.  Its outputs, or what it reads once, go past the
-// caches then: the norm of 8192 x 4096 bfloat16 (303 MB) 58 -> 50 us with streaming stores, its backward pass over 16384 x 4096
-// 110 -> 101 with streaming loads, log probabilities of 4096 x 100003 168 -> 157, the logits' gradient of 8192 x 32768 192 -> 183
+// caches then: the norm of 8192 x 4096 bfloat16 (303 MB) 58 -> 55 us with streaming stores, its backward pass over 16384 x 4096
+// 107 -> 101 with loads and stores, log probabilities of 4096 x 100003 168 -> 157, the logits' gradient of 8192 x 32768 192 -> 183
 // with both.  Smaller calls lose by it (norm's backward pass over 4096 x 4096: 31 -> 34, with both 38).
 inline bool streams(double bytes) { return bytes > (double)(256 << 20); }
 

@@ -1,7 +1,7 @@
 // Log probabilities of given tokens, entropy and the most likely alternatives, and the logits' gradient.
 //
-// Scoring reads every logit once.  4096 x 100003 bfloat16: without alternatives 146 us, 5.6 TB/s, bound by memory; with 8 alternatives
-// 157, with 64 some 205, bound by instructions: some nine per logit, one of them an exponential that takes four times as long,
+// Scoring reads every logit once.  4096 x 100003 bfloat16: without alternatives 133 us, 6.2 TB/s, bound by memory; with 8 alternatives
+// 157, with 64 some 221, bound by instructions: some nine per logit, one of them an exponential that takes four times as long,
 // and a few thousand per row for the alternatives.  One row of 128000 with 20 alternatives: 12 us, two launches of some 4 us each and
 // a chain of dependent reads.
 #include <algorithm>
