@@ -523,8 +523,8 @@ __device__ __forceinline__ GradRow grad_row(const TokenGradArgs& A, int64_t row)
   r.log_sum = A.stats[2 * row + 1];
   return r;
 }
-// dx_j = -p_j (a + e (log p_j + H)), and a more at the target.  Bound by memory: 8192 x 32768 bfloat16 183 us, 5.9 TB/s; 509 x 47236
-// binary32 in rows of 47239: 43 us, 4.5 TB/s.
+// dx_j = -p_j (a + e (log p_j + H)), and a more at the target.  Bound by memory: 8192 x 32768 bfloat16 178 us, 6.0 TB/s; 509 x 47236
+// binary32 in rows of 47239: 44 us, 4.4 TB/s.
 template <int TYPE>
 __device__ __forceinline__ Raw8<TYPE> grad_of(const GradRow& r, const Raw8<TYPE>& raw, int64_t i) {
   float v[kVec], d[kVec];
@@ -542,26 +542,60 @@ __device__ __forceinline__ Raw8<TYPE> grad_of(const GradRow& r, const Raw8<TYPE>
 }
 
 constexpr int64_t kGradPiece = (int64_t)kThreads * kVec;       // logits that a work-group has in one vector per lane
+// Pieces inside a row have no branch.  Past the caches they begin on 16 bytes of dx, wherever the row does: 4096 x 100003 bfloat16 395
+// us -> 337 (not in calls that the caches hold, 8192 x 2049 22 us and 27, nor in rows of few pieces, 32768 x 4099 118 and 145).
 template <int TYPE, int NV, bool STREAM>
 __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenGradArgs A) {
   typedef ElemT<TYPE> T;
+  constexpr int64_t kPiece = NV * kGradPiece;
   for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
     const T* x = (const T*)A.x + row * A.x_stride;
     T* dx = (T*)A.dx + row * A.dx_stride;
     const GradRow r = grad_row(A, row);
-    for (int64_t first = (int64_t)blockIdx.y * NV * kGradPiece; first < A.vocab; first += (int64_t)gridDim.y * NV * kGradPiece) {
+    const int64_t lead = STREAM && A.vocab > 2 * kPiece ? (int64_t)((uintptr_t)dx % 16 / sizeof(T)) : 0;
+    for (int64_t first = (int64_t)blockIdx.y * kPiece - lead; first < A.vocab; first += (int64_t)gridDim.y * kPiece) {
       const int64_t lane0 = first + threadIdx.x * kVec;
       Raw8<TYPE> raw[NV];
+      if (first >= 0 && first + kPiece <= A.vocab) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int64_t i = lane0 + k * kThreads * kVec;
-        raw[k] = load_raw<TYPE, STREAM>(x + i, (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i)));
-      }
+        for (int k = 0; k < NV; ++k) raw[k] = load_raw<TYPE, STREAM>(x + lane0 + k * kGradPiece);
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int64_t i = lane0 + k * kThreads * kVec;
-        const int n = (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i));
-        if (n > 0) store_raw<TYPE, STREAM>(dx + i, grad_of<TYPE>(r, raw[k], i), n);
+        for (int k = 0; k < NV; ++k) {
+          const int64_t i = lane0 + k * kGradPiece;
+          store_raw<TYPE, STREAM>(dx + i, grad_of<TYPE>(r, raw[k], i), kVec);
+        }
+      } else {
+        auto elements = [&](int64_t i, auto each) {
+#pragma unroll
+          for (int j = 0; j < kVec; ++j)
+            if (i + j >= 0 && i + j < A.vocab) each(i + j, j);
+        };
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int64_t i = lane0 + k * kGradPiece;
+          const int n = (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i));
+          if (STREAM && i < 0) {
+            T v[kVec] = {};
+            elements(i, [&](int64_t at, int j) { v[j] = x[at]; });
+            __builtin_memcpy(&raw[k], v, sizeof raw[k]);
+          } else {
+            raw[k] = load_raw<TYPE, STREAM>(x + i, n);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int64_t i = lane0 + k * kGradPiece;
+          const int n = (int)max((int64_t)0, min((int64_t)kVec, A.vocab - i));
+          if (n == 0) continue;
+          const Raw8<TYPE> d = grad_of<TYPE>(r, raw[k], i);
+          if (STREAM && i < 0) {
+            T v[kVec];
+            __builtin_memcpy(v, &d, sizeof d);
+            elements(i, [&](int64_t at, int j) { dx[at] = v[j]; });
+          } else {
+            store_raw<TYPE, STREAM>(dx + i, d, n);
+          }
+        }
       }
     }
   }

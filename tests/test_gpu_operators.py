@@ -639,3 +639,56 @@ def test_tiles_that_the_whole_width_does_not_fill():
             want = dy.double().t().contiguous() @ values.double() + 0.25 * accumulate
             each = dy.double().abs().t().contiguous() @ values.double().abs() + 0.25
             assert ((dw[:, :K].double() - want).abs() <= SUM * each).all()
+
+
+# ---- many rows ---------------------------------------------------------------------------------------------------
+
+# Rows that a work-group goes over, one read ahead, in every form; the last are more than the caches hold.
+MANY = [(40000, 5, 32, 0), (20000, 8, 64, 1), (18000, 43, 32, 0), (17001, 64, 128, 3), (9000, 120, 64, 1), (5000, 200, 32, 0), (2300, 511, 32, 0),
+        (2100, 1003, 64, 1), (1100, 2047, 32, 0), (700, 3001, 32, 2), (600, 4097, 128, 0), (300, 9001, 32, 0)]
+MANY_TYPES = [(*shape, t) for shape in MANY for t in ("f32", "bf16")] + [(9400, 4099, 32, 0, "bf16")]
+
+
+@pytest.mark.parametrize("T,K,group,pad,t", MANY_TYPES)
+def test_norm_of_many_rows(T, K, group, pad, t):
+    test_norm(t, T, K, group, pad, True)
+
+
+@pytest.mark.parametrize("T,K,group,pad,t", MANY_TYPES)
+@pytest.mark.parametrize("coded", [False, True])
+def test_norm_grad_of_many_rows(T, K, group, pad, t, coded):
+    run_norm_grad(t, T, K, group, pad, True, coded)
+
+
+@pytest.mark.parametrize("T,V,t", [(4200, 16500, "bf16"), (2100, 16500, "f32"), (4200, 8200, "f32")])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_token_logprob_grad_of_many_rows(T, V, t, in_place):
+    """More than the caches hold, rows at every offset inside 16 bytes; all rows against each other's bits, some against 64 bits."""
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    x = torch.full((T, V + 1), 5.0, dtype=TYPES[t], device=DEV)
+    x[:, :V] = 3 * torch.randn(T, V, generator=gen, device=DEV)
+    x[T // 2:, :V] = x[:T - T // 2, :V]                                          # at other offsets
+    target = torch.randint(0, V, (T,), generator=gen, device=DEV, dtype=torch.int32)
+    target[0], target[1] = 0, V - 1
+    target[T // 2:] = target[:T - T // 2].clone()
+    a, e = (torch.randn(T, generator=gen, device=DEV) for _ in range(2))
+    a[T // 2:], e[T // 2:] = a[:T - T // 2].clone(), e[:T - T // 2].clone()
+    rows = torch.tensor([0, 1, 2, 3, 5, T // 3, T // 2 - 1, T // 2, T - 1])
+    x64, some = x[rows.to(DEV), :V].cpu().to(F64), target[rows.to(DEV)].cpu()
+    entropy, stats = torch.empty(T, device=DEV), torch.empty(T, 2, device=DEV)
+    logprob = torch.empty(T, device=DEV)
+    qa.qa_token_logprob(code_of(t), T, V, x, V + 1, target, 0, logprob, entropy, stats, None, None, None)
+    entropy[T // 2:], stats[T // 2:] = entropy[:T - T // 2].clone(), stats[:T - T // 2].clone()
+    out = x if in_place else torch.full((T, V + 1), 5.0, dtype=TYPES[t], device=DEV)
+    qa.qa_token_logprob_grad(code_of(t), T, V, x, V + 1, target, stats, entropy, a, e, out, V + 1)
+    assert (out[:, V] == 5.0).all()
+    assert torch.equal(out[T // 2:, :V], out[:T - T // 2, :V])
+    _, entropy64, stats64, logp = ref.token_logprob(x64, some)
+    a64, e64 = a[rows.to(DEV)].cpu().to(F64), e[rows.to(DEV)].cpu().to(F64)
+    want = ref.token_logprob_grad(x64, some, a64, e64)
+    p = torch.exp(logp)
+    reach = (logp - entropy64[:, None]).abs() + 1
+    units = logp.abs() + stats64[:, 1:] + 4
+    # stats and entropy are the call's own, good to SUM of the largest |log p| that enters them
+    off = p * (a64.abs()[:, None] + e64.abs()[:, None] * reach) * (2.0 ** -21 * units + 4 * SUM * units) + 2.0 ** -23 * a64.abs()[:, None]
+    assert ((out[rows.to(DEV), :V].cpu().to(F64) - want).abs() <= HALF_ULP[t] * 1.01 * want.abs() + off).all()
