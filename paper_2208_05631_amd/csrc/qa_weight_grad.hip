@@ -181,20 +181,21 @@ struct Worker {
   }
   // X is 0 past the end.
   __device__ __forceinline__ void store_x(Loaded& from, __bf16* lds, int64_t t0) {
-    // (code + 128) scale - 128 scale, exact.  The 128's are not known to the compiler, which would take a code's bytes apart,
-    // and wait for them, where they are loaded.
-    uint32_t bias;
-    asm("s_mov_b32 %0, 0x80808080" : "=s"(bias));
+    // A signed byte times its scale: exact, and finite for every scale that a finite group has (a bias taken off behind the scaling
+    // would be infinite from 2^121 on).  The zeros are not known to the compiler, which would take a code's bytes apart, and wait
+    // for them, where they are loaded.
+    uint32_t none;
+    asm("s_mov_b32 %0, 0" : "=s"(none));
 #pragma unroll
     for (int v = 0; v < kX; ++v) {
-      const float s = t0 + x_row(v) < t_end ? scale_of(from.scale[v]) : 0.0f, s128 = -128.0f * s;
+      const float s = t0 + x_row(v) < t_end ? scale_of(from.scale[v]) : 0.0f;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         u32x4 x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t w = (from.code[v][2 * h + i / 2] ^ bias) >> (16 * (i % 2));
-          const float lo = __builtin_fmaf((float)(w & 0xFFu), s, s128), hi = __builtin_fmaf((float)(w >> 8 & 0xFFu), s, s128);
+          const uint32_t w = from.code[v][2 * h + i / 2] ^ none;
+          const float lo = (float)(int8_t)(w >> (16 * (i % 2))) * s, hi = (float)(int8_t)(w >> (16 * (i % 2) + 8)) * s;
           x[i] = __builtin_amdgcn_perm(as_u32(hi), as_u32(lo), 0x07060302u);
         }
         *reinterpret_cast<u32x4*>(lds + P * kPart + x_row(v) * kRow + x_chunk() * 16 + h * kVec) = x;
