@@ -225,7 +225,8 @@ struct Worker {
   // One step: the buffer `now` is multiplied, what was loaded for the step that is kBuffers - 1 ahead goes to `last`.  What is to be
   // done beside the matrix instructions is laid out over as many phases as there are, and inside a phase it stands in their
   // shadow: left to the compiler the reads of LDS and the decoding stand together in front of them (large bfloat16 tiles: 1.04 ms
-  // instead of 0.94).
+  // instead of 0.94).  It is told that the three lie apart.  With two buffers the next one is the one that is written: it is
+  // read behind the step only, and `now` stands in its place here.
   template <int PHASE>
   static __device__ __forceinline__ void phases(Worker& w, Loaded& loaded, int64_t t, const __bf16* __restrict__ now,
                                                 const __bf16* __restrict__ next, __bf16* __restrict__ last) {
@@ -261,7 +262,6 @@ struct Worker {
                                               const __bf16* __restrict__ next, __bf16* __restrict__ last) {
     phases<0>(w, loaded, t, now, next, last);
     __syncthreads();
-    if (kBuffers == 2) w.operands(next, 0);
   }
   __device__ __forceinline__ void run(int64_t t_begin, __bf16* lds) {
     Loaded loaded[kAhead];                         // step i's in i % kAhead
@@ -280,7 +280,8 @@ struct Worker {
     for (int64_t t = t_begin; t < t_end;) {        // X is 0 in a step past the end
 #pragma unroll
       for (int a = 0; a < kAhead; ++a, t += kStep) {
-        step(*this, loaded[(a + kBuffers - 1) % kAhead], t, lds + now, lds + next, lds + last);
+        step(*this, loaded[(a + kBuffers - 1) % kAhead], t, lds + now, lds + (kBuffers == 2 ? now : next), lds + last);
+        if (kBuffers == 2) operands(lds + last, 0);
         const int free = now;
         now = next;
         next = kBuffers == 2 ? free : last;
