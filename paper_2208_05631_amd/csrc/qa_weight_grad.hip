@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "qa_rows.h"
+#include "qa_weight_plan.h"
 
 namespace qa {
 namespace {
@@ -30,7 +31,7 @@ struct WeightGradArgs {
   int accumulate;
 };
 
-constexpr int kStep = 32;                          // rows of both that lie in LDS at a time
+constexpr int kStep = kWeightStep;                 // rows of both that lie in LDS at a time
 
 // A tile's rows lie in LDS as bfloat16, as in memory; matrix instructions want eight rows of one column per lane, which
 // the transposing reads give: of 16 lanes each reads four columns of one of four rows and receives four rows of one
@@ -388,37 +389,10 @@ int join_launch(const float* parts, int64_t splits, int64_t n, int64_t cols, flo
 
 // ---- which form ----------------------------------------------------------------------------------------------
 
-// Tiles of 256 x 256 or 128 x 128, and the rows whole or split: whichever is estimated to take the least time.  Measured
-// for a step of 32 rows and bfloat16: a 128-tile 0.38 us where it has its compute unit to itself, 0.65 where two share
-// one; a 256-tile 0.62 us where few run and 0.9 where all do, which the card's power bounds; times the parts of dY, but
-// for 0.1 of the small one's.  A round of work-groups takes 4 us more, and the splits' sums are written and read at
-// some 6 TB/s.  (2048 x 2048 columns, 16384 rows: 145 us with four splits of 256-tiles, 322 in one piece, 185 with two of
-// 128-tiles; 2048 rows: 40, 48 and 39, and 30 with 128-tiles in one piece.)
-struct Plan { int tile; int64_t tiles_n, tiles, splits; };
-Plan plan_for(int64_t rows, int64_t cols, int64_t n, int parts) {
-  Plan best = {};
-  double least = 0.0;
-  for (int tile = 128; tile <= 256; tile *= 2) {
-    if (tile == 256 && n < kVec) break;
-    const int64_t tiles_n = ceil_div(n, tile), tiles = tiles_n * ceil_div(cols, tile), at_once = tile == 256 ? 256 : 512;
-    for (int64_t splits = 1; splits <= 64 && (splits == 1 || splits * 64 <= rows); ++splits) {
-      const int64_t groups = tiles * splits, steps = ceil_div(ceil_div(rows, splits), kStep);
-      const double step = tile == 256 ? parts * (0.6 + 0.3 * (groups < 256 ? (double)groups / 256.0 : 1.0))
-                                      : 0.1 + parts * (groups <= 256 ? 0.28 : 0.55);
-      const double us = (double)ceil_div(groups, at_once) * ((double)steps * step + 4.0) +
-                        (splits > 1 ? 4.0 + (double)(2 * splits + 1) * (double)n * (double)cols * (4.0 / 6e6) : 0.0);
-      if (least == 0.0 || us < least) {
-        least = us;
-        best = {tile, tiles_n, tiles, splits};
-      }
-    }
-  }
-  return best;
-}
 int parts_for(int type) { return type == QA_F32 ? 3 : type == QA_F16 ? 2 : 1; }
 
 template <int TYPE>
-int weight_grad_launch(WeightGradArgs& A, const Plan& plan, hipStream_t stream) {
+int weight_grad_launch(WeightGradArgs& A, const WeightPlan& plan, hipStream_t stream) {
   const dim3 grid((unsigned)plan.tiles, (unsigned)plan.splits);
   if (A.n < kVec) weight_grad_kernel<TYPE, 2, 2, 2, 2, true><<<grid, 256, 0, stream>>>(A);
   else if (plan.tile == 256) weight_grad_kernel<TYPE, 2, 4, 4, 2, false><<<grid, 512, 0, stream>>>(A);
@@ -429,7 +403,7 @@ int weight_grad_launch(WeightGradArgs& A, const Plan& plan, hipStream_t stream) 
 }  // namespace
 
 size_t weight_grad_workspace_bytes(const qa_coded_rows* R, int type, int64_t n) {
-  const int64_t splits = plan_for(R->rows, R->cols, n, parts_for(type)).splits;
+  const int64_t splits = weight_plan(R->rows, R->cols, n, parts_for(type)).splits;
   return splits == 1 ? 0 : (size_t)splits * (size_t)n * (size_t)R->cols * sizeof(float);
 }
 
@@ -454,7 +428,7 @@ extern "C" int qa_rows_weight_grad(const qa_coded_rows* rows, const int8_t* code
   }
   if (!codes || !scales || !dy) return QA_ERR_INVALID_ARG;
   if (!element_aligned(dy, type) || !aligned(codes, 16)) return QA_ERR_ALIGNMENT;
-  const Plan plan = plan_for(rows->rows, rows->cols, n, parts_for(type));
+  const WeightPlan plan = weight_plan(rows->rows, rows->cols, n, parts_for(type));
   const int64_t splits = plan.splits;
   WeightGradArgs A{*rows, codes, scales, dy, dw, dy_stride, dw_stride, 0, n, rows->rows, plan.tiles_n, accumulate};
   if (splits > 1) {

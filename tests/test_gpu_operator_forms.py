@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import operator_reference as ref
+from weight_grad_shapes import FEW, LARGE, LARGE_SPLIT, SMALL
 
 pytestmark = pytest.mark.gpu
 
@@ -19,12 +20,8 @@ if torch.cuda.is_available():
 
 # ---- weight gradient ---------------------------------------------------------------------------------------------
 
-# Small tiles, and large ones.
-SMALL, LARGE = (70, 40, 200), (70, 4099, 4100)
-
-
 @pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("T,N,K", [SMALL, (70, 5, 200), LARGE])
+@pytest.mark.parametrize("T,N,K", [SMALL, FEW, LARGE[1]])
 def test_weight_grad_of_groups_with_the_largest_scales(t, T, N, K):
     """Groups whose largest magnitude is up to binary32's largest number, with zeros beside it: their codes stand for finite
     values, and dY is small enough that every sum is finite.  An infinity makes its group's columns NaN and no others."""
@@ -52,3 +49,47 @@ def test_weight_grad_of_groups_with_the_largest_scales(t, T, N, K):
     want, each = dy.t().contiguous() @ values, dy.abs().t().contiguous() @ values.abs()
     ok = (dw.to(F64) - want).abs() <= SUM * each
     assert ok[:, ~bad.to(DEV)].all()
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,N,K", LARGE + LARGE_SPLIT)
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_weight_grad_of_large_tiles(t, T, N, K, accumulate):
+    """Rows, columns of dY and of X that end inside a tile, in one piece and split, against a product in 64 bits; one row to
+    the last bit, where a product of dY's 8 or 11 bits and a code's 7 is a binary32 number."""
+    gen = torch.Generator(device=DEV).manual_seed(T + N)
+    x = 2 * torch.randn(T, K, generator=gen, device=DEV)
+    pad = N % 3
+    dy = (0.1 * torch.randn(T, N + pad, generator=gen, device=DEV)).to(TYPES[t])[:, :N]
+    L, codes, scales = coded_rows(T, K, 64)
+    qa.qa_rows_pack(L, qa.QA_F32, x, K, codes, scales)
+    values = torch.empty(T, K, device=DEV)
+    qa.qa_rows_unpack(L, codes, scales, qa.QA_F32, values, K)
+    need = qa.qa_rows_workspace_bytes(L, qa.QA_OP_WEIGHT_GRAD, code_of(t), N)
+    assert (need > 0) == ((T, N, K) in LARGE_SPLIT)
+    ws = torch.full((need,), 0xA5, dtype=torch.uint8, device=DEV) if need else None
+    got = []
+    for _ in range(2):
+        dw = torch.full((N, K + 1), 0.25, device=DEV)
+        qa.qa_rows_weight_grad(L, codes, scales, code_of(t), dy, N + pad, N, dw, K + 1, accumulate, ws)
+        got.append(dw)
+    assert torch.equal(*got) and (dw[:, K] == 0.25).all()
+    want = dy.double().t().contiguous() @ values.double() + 0.25 * accumulate
+    each = dy.double().abs().t().contiguous() @ values.double().abs() + 0.25 * accumulate
+    assert ((dw[:, :K].double() - want).abs() <= SUM * each).all()
+    if T == 1 and not accumulate and t != "f32":
+        assert torch.equal(dw[:, :K], want.float())
+
+
+def test_weight_grad_of_large_tiles_keeps_every_bit_of_dy():
+    """One row of codes that are powers of two: each product has the 24 bits of a binary32 number."""
+    _, N, K = LARGE[0]
+    gen = gen_of("bits of large tiles")
+    dy = torch.randn(1, N, generator=gen) * torch.exp2(torch.randint(-60, 60, (1, N), generator=gen).float())
+    x = torch.exp2(torch.randint(-6, 1, (1, K), generator=gen).float())
+    x[:, ::32] = 1.0
+    L, codes, scales = coded_rows(1, K, 32)
+    qa.qa_rows_pack(L, qa.QA_F32, x.to(DEV), K, codes, scales)
+    dw = torch.empty(N, K, device=DEV)
+    qa.qa_rows_weight_grad(L, codes, scales, qa.QA_F32, dy.to(DEV), N, N, dw, K, 0, None)
+    assert torch.equal(dw.cpu(), dy.t() @ x)
