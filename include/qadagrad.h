@@ -477,10 +477,13 @@ int qa_step_qrda_segments(const qa_layout* layout, const qa_segment_plan* plan,
  * one byte b = scales[t*scale_stride + k] and stands for the values
  *     codes[t*code_stride + i] * 2^(b - 127),    -127 <= code <= 127.
  * The scale is the smallest power of two by which the group's largest magnitude is at most 127, and
- * 2^-126 at least; a code is the nearest whole multiple, ties to even: an error of at most half the
- * scale, 1/127 of the group's largest magnitude at most.  A code times a power of two has seven significant bits: every
- * value is exact in bfloat16 (and finite: at b = 249, the largest that a finite magnitude needs, codes end at 63).  b = 255 marks a group with an infinity or a NaN: its codes are 0, its
- * values are read as NaN.  b = 0 is never written and is read as scale 0.  Bytes between cols and code_stride are
+ * 2^-126 at least; a code is the nearest whole multiple, ties to even.  The error is at most half the
+ * scale, which is 1/127 of the group's largest magnitude at most, but for both ends of the range: a
+ * scale of 2^-126 may be more than that, and at b = 249, the largest that a finite magnitude needs,
+ * codes end at 63, as 64 would stand for 2^128: the error is below one scale there, 1/64 of that
+ * magnitude.  A code times a power of two has seven significant bits: every value is finite and exact
+ * in bfloat16.  b = 255 marks a group with an infinity or a NaN: its codes are 0, its values are read
+ * as NaN.  b = 0 is never written and is read as scale 0.  Bytes between cols and code_stride are
  * neither written nor used. */
 typedef struct {
   int64_t rows;         /* 0 <= rows < 2^31                                                   */
@@ -509,8 +512,9 @@ int qa_rows_unpack(const qa_coded_rows* rows, const int8_t* codes, const uint8_t
  * its input and the gradient dy of its output:
  *     dw[j*dw_stride + k] = (accumulate ? dw[j*dw_stride + k] : 0) + sum_t dy[t*dy_stride + j] * value(t, k)
  * dy may be of any type; binary32 and binary16 elements are split into bfloat16 parts that add up to
- * them (to 2^-24 of them, and exactly), so that no precision of theirs is lost.  Infinities and NaN in
- * dy, and groups without values, make the sums that they enter NaN or infinite.
+ * them, so that no precision of theirs is lost, but for what a binary32 element has below 2^-133, where
+ * bfloat16 ends (elements under 2^-109 do).  Infinities and NaN in dy, and groups without values, make
+ * the sums that they enter NaN or infinite.
  * 1 <= n < 2^24; strides of what is read below 2^25.  ws: qa_rows_workspace_bytes(rows, QA_OP_WEIGHT_GRAD, type, n) bytes, may be NULL if 0. */
 int qa_rows_weight_grad(const qa_coded_rows* rows, const int8_t* codes, const uint8_t* scales, int type,
                         const void* dy, int64_t dy_stride, int64_t n, float* dw, int64_t dw_stride,

@@ -48,7 +48,8 @@ __device__ __forceinline__ bf16x8 eight_rows(const __bf16* lane_at) {
   return v;
 }
 
-// v as `P` bfloat16 parts, each the leading eight bits of what is left: exact for 8 P bits.
+// v as `P` bfloat16 parts, each the leading eight bits of what is left: exact for 8 P bits, but for what lies below 2^-133,
+// bfloat16's last bit (matrix instructions take numbers under 2^-126 as they are).
 template <int P>
 __device__ __forceinline__ void split_parts(float (&v)[kVec], u32x4 (&part)[P]) {
 #pragma unroll

@@ -18,6 +18,26 @@ if torch.cuda.is_available():
     DEV = torch.device("cuda:0")
 
 
+# ---- rows in 8 bits ------------------------------------------------------------------------------------------------
+
+
+def test_error_of_a_code():
+    """Half a scale, and 1/127 of the group's largest magnitude; at the largest scale less than a whole one, and 1/64."""
+    gen = gen_of("error")
+    most = torch.exp2(torch.randint(-115, 128, (3000, 1), generator=gen).double()) * (1 + torch.rand(3000, 1, generator=gen).double())
+    most[-600:] = 2.0 ** 127 * (1.9 + 0.1 * torch.rand(600, 1, generator=gen).double())
+    x = (most.clamp(max=torch.finfo(torch.float32).max) * (2 * torch.rand(3000, 32, generator=gen) - 1).double()).float()
+    x[:, 7] = most.clamp(max=torch.finfo(torch.float32).max)[:, 0].float()
+    L, codes, scales = coded_rows(3000, 32, 32)
+    qa.qa_rows_pack(L, qa.QA_F32, x.to(DEV), 32, codes, scales)
+    s = scales[:, :1].cpu().long()
+    off = (ref.decode(codes[:, :32].cpu(), s, 32) - x.to(F64)).abs() / torch.exp2((s - 127).to(F64))
+    share = (ref.decode(codes[:, :32].cpu(), s, 32) - x.to(F64)).abs() / x.to(F64).abs().amax(dim=1, keepdim=True)
+    last = (s == 249)[:, 0]
+    assert last.sum() > 50 and (off[last] < 1).all() and (share[last] < 1 / 64).all()
+    assert (off[~last] <= 0.5).all() and (share[~last] <= 1 / 127).all()
+
+
 # ---- weight gradient ---------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
@@ -93,3 +113,20 @@ def test_weight_grad_of_large_tiles_keeps_every_bit_of_dy():
     dw = torch.empty(N, K, device=DEV)
     qa.qa_rows_weight_grad(L, codes, scales, qa.QA_F32, dy.to(DEV), N, N, dw, K, 0, None)
     assert torch.equal(dw.cpu(), dy.t() @ x)
+
+
+@pytest.mark.parametrize("T,N,K", [SMALL, LARGE[1]])
+def test_weight_grad_of_the_smallest_numbers(T, N, K):
+    """binary32 elements of dY lose what lies below 2^-133, and bfloat16 ones nothing."""
+    gen = gen_of("smallest", T, N, K)
+    dy = torch.zeros(T, N)
+    dy[0] = torch.randn(N, generator=gen) * torch.exp2(torch.randint(-140, -100, (N,), generator=gen).double()).float()
+    L, codes, scales = coded_rows(T, K, 32)
+    qa.qa_rows_pack(L, qa.QA_F32, torch.full((T, K), 2.0 ** 100, device=DEV), K, codes, scales)
+    for t, lost in (("f32", 2.0 ** -133), ("bf16", 0.0)):
+        d = dy.to(TYPES[t])
+        dw = torch.empty(N, K, device=DEV)
+        ws = torch.empty(max(1, qa.qa_rows_workspace_bytes(L, qa.QA_OP_WEIGHT_GRAD, code_of(t), N)), dtype=torch.uint8, device=DEV)
+        qa.qa_rows_weight_grad(L, codes, scales, code_of(t), d.to(DEV), N, N, dw, K, 0, ws)
+        assert ((dw[:, 0].cpu().to(F64) * 2.0 ** -100 - d[0].to(F64)).abs() <= lost).all()
+        assert (dw == dw[:, :1]).all()
