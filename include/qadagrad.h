@@ -461,7 +461,8 @@ int qa_step_qrda_segments(const qa_layout* layout, const qa_segment_plan* plan,
  *
  * Arithmetic: inputs of any type are widened to binary32; sums, norms and softmax statistics are
  * held in binary32 (weight gradients: products of the matrix cores, added in binary32) in an order
- * that depends on the sizes alone, so a call repeats bit for bit; outputs are rounded once, to nearest.
+ * that depends on the sizes alone, and for log probabilities on where a row begins inside 16 bytes, so
+ * a call repeats bit for bit; outputs are rounded once, to nearest.
  *
  * Rows: element (t, k) of a matrix is at t*stride + k, strides in elements.  Element buffers need the
  * alignment of their element only, and any stride that is at least the row's length (rows of a

@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 
 if torch.cuda.is_available():
     import paper_2208_05631_amd as qa
-    from test_gpu_operators import F64, SUM, TYPES, code_of, coded_rows, gen_of
+    from test_gpu_operators import F64, SUM, TYPES, check_token, code_of, coded_rows, gen_of
     DEV = torch.device("cuda:0")
 
 
@@ -130,3 +130,85 @@ def test_weight_grad_of_the_smallest_numbers(T, N, K):
         qa.qa_rows_weight_grad(L, codes, scales, code_of(t), d.to(DEV), N, N, dw, K, 0, ws)
         assert ((dw[:, 0].cpu().to(F64) * 2.0 ** -100 - d[0].to(F64)).abs() <= lost).all()
         assert (dw == dw[:, :1]).all()
+
+
+# ---- log probabilities of long rows ----------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(1, 131073), (1, 199999), (3, 200001), (2, 1_100_003)])
+@pytest.mark.parametrize("top", [0, 1, 64])
+def test_token_logprob_of_more_splits_than_lanes(t, T, V, top):
+    """65 to 512 splits of a row: the join's bound comes from several of them per lane."""
+    gen = gen_of("splits", t, T, V, top)
+    x = (3 * torch.randn(T, V, generator=gen)).to(TYPES[t])
+    target = torch.randint(0, V, (T,), generator=gen, dtype=torch.int32)
+    need = qa.qa_token_workspace_bytes(T, V, top)
+    assert 64 < need // (T * (16 + 8 * top)) <= 512
+    check_token(t, x, target, top, pad=V % 2, lead=V % 3)
+    if T > 1:                                          # all of one row's best in one split, ties, a mask that leaves nothing
+        x[0] = -math.inf
+        x[1, : V // 2] = 1.0
+        x[1, V // 2:] = -2.0
+        x[T - 1, 5000:5100] = 30.0 + torch.arange(100) % 7
+        check_token(t, x, target, top)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [196_609, 200_000])
+@pytest.mark.parametrize("top", [0, 20])
+def test_token_logprob_of_many_rows_that_are_too_long_for_one_piece(t, V, top):
+    """More chunks than a work-group notes: split although there are rows enough.  Rows against their copies' bits, at the same place
+    inside 16 bytes, and some in 64 bits."""
+    T, stride = 260, -(-V // 8) * 8
+    gen = torch.Generator(device=DEV).manual_seed(V)
+    x = torch.full((T, stride), 50.0, dtype=TYPES[t], device=DEV)[:, :V]
+    x.copy_(3 * torch.randn(T, V, generator=gen, device=DEV))
+    x[T // 2:] = x[:T // 2].clone()
+    x[7] = -math.inf
+    x[9, : V - 40] = -math.inf
+    x[11] = 2.0
+    target = torch.randint(0, V, (T,), generator=gen, device=DEV, dtype=torch.int32)
+    target[T // 2:] = target[:T // 2].clone()
+    need = qa.qa_token_workspace_bytes(T, V, top)
+    assert need == T * 2 * (16 + 8 * top)
+    ws = torch.full((need,), 0xA5, dtype=torch.uint8, device=DEV)
+    logprob, entropy, stats = torch.empty(T, device=DEV), torch.empty(T, device=DEV), torch.empty(T, 2, device=DEV)
+    best, index = torch.empty(T, top, device=DEV), torch.empty(T, top, dtype=torch.int32, device=DEV)
+    qa.qa_token_logprob(code_of(t), T, V, x, stride, target, top, logprob, entropy, stats, best if top else None, index if top else None, ws)
+    keep = [i for i in range(T // 2) if i not in (7, 9, 11)]
+    for v in (logprob, entropy, stats, best, index):
+        assert torch.equal(v[:T // 2][keep], v[T // 2:][keep])
+    some = torch.tensor([0, 1, 7, 9, 11, T - 1])
+    x64, y = x[some.to(DEV)].cpu().to(F64), target[some.to(DEV)].cpu()
+    lp, want_h, want_s, logp = ref.token_logprob(x64, y)
+    logprob, entropy, stats, best, index = (v[some.to(DEV)].cpu().to(F64) for v in (logprob, entropy, stats, best, index))
+    near = lambda a, b: ((a - b).abs() <= 2 * SUM + 2.0 ** -22 * (b.abs() + 20)) | (a == b)  # noqa: E731
+    assert torch.equal(stats[:, 0], want_s[:, 0]) and near(stats[:, 1], want_s[:, 1]).all() and near(logprob, lp).all()
+    assert ((entropy - want_h).abs() <= SUM * (8 + 2 * want_h)).all()
+    assert torch.equal(index.long(), ref.top(x64, top)) and near(best, logp.gather(1, index.long())).all()
+
+
+def test_token_logprob_of_more_splits_than_the_bound_looks_at():
+    """A row of more than 512 pieces: the bound comes from the first 512, and the best may lie in the others."""
+    V, top = 512 * 196_608 + 12_345, 20
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn(1, V, generator=gen, device=DEV)
+    places = torch.tensor([5, 196_608, 100_000_000, V - 12_000, V - 1, V // 2])
+    x[0, places.to(DEV)] = torch.tensor([9.0, 9.0, 11.0, 10.0, 12.0, 8.5], device=DEV)
+    need = qa.qa_token_workspace_bytes(1, V, top)
+    assert need == 513 * (16 + 8 * top)
+    ws = torch.full((need,), 0xA5, dtype=torch.uint8, device=DEV)
+    target = torch.tensor([V - 1], dtype=torch.int32, device=DEV)
+    logprob, entropy, stats = torch.empty(1, device=DEV), torch.empty(1, device=DEV), torch.empty(1, 2, device=DEV)
+    best, index = torch.empty(1, top, device=DEV), torch.empty(1, top, dtype=torch.int32, device=DEV)
+    qa.qa_token_logprob(qa.QA_F32, 1, V, x, V, target, top, logprob, entropy, stats, best, index, ws)
+    x64 = x.double()
+    log_sum = torch.log(torch.exp(x64 - 12.0).sum())
+    logp = x64 - 12.0 - log_sum
+    want_h = -(torch.exp(logp) * logp).sum()
+    order = torch.sort(x64[0], descending=True, stable=True).indices[:top]
+    assert torch.equal(index[0].long(), order) and float(stats[0, 0]) == 12.0
+    slack = 2 * SUM + 2.0 ** -22 * 40
+    assert abs(float(stats[0, 1] - log_sum)) <= slack and abs(float(logprob[0] - logp[0, V - 1])) <= slack
+    assert (best[0] - logp[0, order]).abs().max() <= slack and abs(float(entropy[0] - want_h)) <= SUM * (8 + 2 * float(want_h))
