@@ -484,19 +484,28 @@ Form form_of(int64_t cols) {
 }
 // Work-groups, from threads per compute unit: where rows are read ahead some 4096 columns at a time are on their way to each, and
 // twice as many where they are codes.  More are slower, by the rows that meet in memory and, backward, by the work-groups' sums
-// (16384 x 4096 bfloat16, 256 threads, 512 and 1024: forward 101 us, 114 and 113, backward 87, 90 and 105).  Calls that the caches hold
-// do not mind forward, and are spread wider.
+// (16384 x 4096 bfloat16, 256 threads, 512 and 1024: forward 101 us, 114 and 113, backward 87, 90 and 105).  Rows that leave lanes
+// empty bring fewer columns, and those whose last vector is not full hold their work-group up, by stores of single elements: they get 512
+// threads for 256 (forward 20000 x 2051: 180 us -> 103, 10000 x 4095: 109 -> 84, 16000 x 2560: 84 -> 65, but 10000 x 4000: 65 -> 69,
+// and, of rows inside a wave, 40000 x 1003: 74 -> 77; backward 20000 x 2051: 116 -> 93, 16000 x 3000: 85 -> 72, 10000 x 4000: 64 -> 61, but
+// 10000 x 4096: 57 -> 59; from codes they lose, 10000 x 4095: 73 -> 82).  Calls that the caches hold do not mind forward, and are spread
+// wider; backward they stay as they are (2000 x 4095: 21 us -> 23).
 int64_t groups_for(int64_t rows, Form f, int64_t threads_per_unit) {
   const int64_t threads = f.lanes == 0 ? 1024 : f.lanes <= kWave ? kThreads : f.lanes;
   return std::min<int64_t>(ceil_div(rows, f.lanes && f.lanes <= kWave ? kThreads / f.lanes : 1),
                            256 * std::max<int64_t>(threads_per_unit / threads, 1));
 }
-int64_t norm_groups(int64_t rows, Form f, int type, bool stream) {
-  return groups_for(rows, f, f.lanes == 0 ? 1024 : stream && f.vecs == 2 && type != QA_F32 ? 256 : 512);
+int64_t norm_groups(int64_t rows, int64_t cols, int type, bool stream) {
+  const Form f = form_of(cols);
+  if (f.lanes == 0) return groups_for(rows, f, 1024);
+  const bool filled = (cols % kVec == 0 || f.lanes <= kWave) && 4 * cols > 3 * f.lanes * f.vecs * kVec;
+  return groups_for(rows, f, stream && f.vecs == 2 && type != QA_F32 && filled ? 256 : 512);
 }
-int64_t norm_grad_groups(int64_t rows, Form f, int type, bool coded) {
+int64_t norm_grad_groups(int64_t rows, int64_t cols, int type, bool coded, bool stream) {
+  const Form f = form_of(cols);
   if (f.lanes == 0 || (type == QA_F32 && f.vecs == 2)) return groups_for(rows, f, 1024);
-  return groups_for(rows, f, (coded ? 2 : 1) * (f.vecs == 2 ? 256 : 512));
+  if (coded) return groups_for(rows, f, f.vecs == 2 ? 512 : 1024);
+  return groups_for(rows, f, f.vecs == 2 && !(stream && cols < f.lanes * f.vecs * kVec) ? 256 : 512);
 }
 
 // Calls `launch` with the lanes and vectors of a form as constants.
@@ -516,7 +525,7 @@ bool with_form(Form f, F launch) {
 template <int TYPE>
 int norm_launch(const NormArgs& A, hipStream_t stream) {
   const Form f = form_of(A.R.cols);
-  const dim3 grid((unsigned)norm_groups(A.R.rows, f, TYPE, A.stream));
+  const dim3 grid((unsigned)norm_groups(A.R.rows, A.R.cols, TYPE, A.stream));
   auto held = [&](auto lanes, auto vecs) {
     if (A.stream) rms_norm_kernel<TYPE, lanes, vecs, true><<<grid, threads_of<lanes>, 0, stream>>>(A);
     else rms_norm_kernel<TYPE, lanes, vecs, false><<<grid, threads_of<lanes>, 0, stream>>>(A);
@@ -528,7 +537,7 @@ int norm_launch(const NormArgs& A, hipStream_t stream) {
 template <int TYPE, bool CODED>
 int norm_grad_launch(const NormGradArgs& A, float* dweight, int accumulate, hipStream_t stream) {
   const Form f = form_of(A.R.cols);
-  const dim3 grid((unsigned)norm_grad_groups(A.R.rows, f, TYPE, CODED));
+  const dim3 grid((unsigned)norm_grad_groups(A.R.rows, A.R.cols, TYPE, CODED, A.stream));
   if (A.R.rows > 0) {
     auto held = [&](auto lanes, auto vecs) {
       constexpr bool STREAM = TYPE != QA_F32;
@@ -553,7 +562,7 @@ int norm_grad_launch(const NormGradArgs& A, float* dweight, int accumulate, hipS
 }  // namespace
 
 size_t rms_norm_grad_workspace_bytes(const qa_coded_rows* R, int type) {
-  return (size_t)norm_grad_groups(R->rows, form_of(R->cols), type, true) * (size_t)R->cols * sizeof(float);
+  return (size_t)norm_grad_groups(R->rows, R->cols, type, true, true) * (size_t)R->cols * sizeof(float);
 }
 
 }  // namespace qa
