@@ -527,7 +527,8 @@ int norm_launch(const NormArgs& A, hipStream_t stream) {
   const Form f = form_of(A.R.cols);
   const dim3 grid((unsigned)norm_groups(A.R.rows, A.R.cols, TYPE, A.stream));
   auto held = [&](auto lanes, auto vecs) {
-    if (A.stream) rms_norm_kernel<TYPE, lanes, vecs, true><<<grid, threads_of<lanes>, 0, stream>>>(A);
+    constexpr bool STREAM = TYPE != QA_F32;
+    if (STREAM && A.stream) rms_norm_kernel<TYPE, lanes, vecs, STREAM><<<grid, threads_of<lanes>, 0, stream>>>(A);
     else rms_norm_kernel<TYPE, lanes, vecs, false><<<grid, threads_of<lanes>, 0, stream>>>(A);
   };
   if (!with_form(f, held)) rms_norm_long_kernel<TYPE><<<grid, 1024, 0, stream>>>(A);

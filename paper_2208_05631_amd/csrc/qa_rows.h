@@ -22,9 +22,13 @@ inline int check_rows(const qa_coded_rows* R) {
 }
 
 // Whether a call reads and writes more than the last-level cache holds.  Its outputs, or what it reads once, go past the
-// caches then: the norm of 8192 x 4096 bfloat16 (303 MB) 58 -> 55 us with streaming stores, its backward pass over 16384 x 4096
-// 107 -> 101 with loads and stores, log probabilities of 4096 x 100003 168 -> 157, the logits' gradient of 8192 x 32768 192 -> 183
-// with both.  Smaller calls lose by it (norm's backward pass over 4096 x 4096: 31 -> 34, with both 38).
+// caches then, where its kernel has such a form and gains by it: the norm of 8192 x 4096 bfloat16 59 -> 52 us, its backward pass over
+// 16384 x 4096 95 -> 88, codes of 16384 x 8192 and their values again 158 -> 144, log probabilities of 4096 x 100003 with 8 alternatives
+// 169 -> 161, the logits' gradient of 8192 x 32768 198 -> 178.  Smaller calls lose by it if the caches hold what they read and
+// write (norm of 4096 x 4096 23 -> 27, backward 24 -> 27) and gain if they do not (30 -> 28, 29 -> 28): their inputs are what the step
+// before has just written.  The norm and log probabilities in binary32, rows that registers do not hold and weight gradients keep to the
+// caches: a lane's eight binary32 elements are two words with another lane's between them, and a line is asked for twice
+// (binary32, norm of 16384 x 4096: 181 us, and 194 past the caches, 30000 x 2047: 170 and 196; backward 206 both).
 inline bool streams(double bytes) { return bytes > (double)(256 << 20); }
 
 #if defined(__HIPCC__)

@@ -629,8 +629,27 @@ int64_t splits_for(int64_t rows, int64_t vocab) {
   return std::max(least, std::min<int64_t>(std::min<int64_t>(ceil_div(vocab, kSplitLogits), kMostSplits), 1024 / rows));
 }
 
+// Whether a row is read past the caches.  With alternatives parts of it are read again, which pays for long rows only (8 of them, bfloat16:
+// 40000 x 4100 344 us, and 365 past the caches, 16000 x 16384 166 and 177, 6000 x 50021 146 both, 4000 x 65536 114 and 108; without:
+// 136 and 133, 92 and 90, 95 and 84); in binary32 without alternatives it pays in rows that begin on 16 bytes (8000 x 16384 89 and 85,
+// but 1500 x 100003 104 and 112, 20000 x 4100 66 and 72), with 8 it does not (4000 x 32768 105 and 110).
+bool token_streams(int type, int64_t rows, int64_t vocab, const void* logits, int64_t stride, int32_t top) {
+  if (!streams((double)rows * (double)vocab * (double)type_bytes(type))) return false;
+  if (top) return type != QA_F32 && vocab >= 1 << 16;
+  return type != QA_F32 || (vocab >= 1 << 14 && aligned(logits, 16) && stride % 4 == 0);
+}
+// Whether the logits' gradient goes past the caches: not in binary32 (4000 x 32768: 204 us, and 218 if it did), and not where a row
+// is a part of one piece (bfloat16, 40000 x 2049: 109 and 126, 32768 x 4096: 100 and 118, 20000 x 6144: 87 and 88, 16000 x 8191: 110 and 105;
+// 100000 x 1001, several rows to a work-group: 100 and 95).
+constexpr int kGradVecs = 4;
+bool token_grad_streams(int type, int64_t rows, int64_t vocab) {
+  return type != QA_F32 && (vocab <= kGradPiece || 4 * vocab > 3 * kGradVecs * kGradPiece) &&
+         streams((double)rows * (double)vocab * (double)(2 * type_bytes(type)));
+}
+
 template <int TYPE, bool TOP>
 int token_launch(TokenArgs& A, hipStream_t stream) {
+  constexpr bool STREAM = !(TOP && TYPE == QA_F32);
   const dim3 narrow((unsigned)std::min<int64_t>(ceil_div(A.rows, kWaves), 1 << 16));
   if (A.vocab <= 512) {
     token_narrow_kernel<TYPE, 1, 1, TOP><<<narrow, kThreads, 0, stream>>>(A);
@@ -640,7 +659,7 @@ int token_launch(TokenArgs& A, hipStream_t stream) {
     const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 16), (unsigned)A.splits);
     A.piece = ceil_div(ceil_div(A.vocab, A.splits), kSplitLogits) * kSplitLogits;
     if (A.piece <= 2 * kSplitLogits) token_wide_kernel<TYPE, 1, TOP, false><<<grid, kTokenThreads, 0, stream>>>(A);
-    else if (A.stream) token_wide_kernel<TYPE, kTokenVecs, TOP, true><<<grid, kTokenThreads, 0, stream>>>(A);
+    else if (STREAM && A.stream) token_wide_kernel<TYPE, kTokenVecs, TOP, STREAM><<<grid, kTokenThreads, 0, stream>>>(A);
     else token_wide_kernel<TYPE, kTokenVecs, TOP, false><<<grid, kTokenThreads, 0, stream>>>(A);
     if (A.splits == 1) return launch_status();
     if (const int rc = launch_status()) return rc;
@@ -654,17 +673,17 @@ int token_launch(TokenArgs& A, hipStream_t stream) {
 }
 template <int TYPE>
 int token_grad_launch(const TokenGradArgs& A, hipStream_t stream) {
+  constexpr bool STREAM = TYPE != QA_F32;
   if (A.vocab <= kGradPiece) {
     int per_row = 1;
     while (per_row * kVec < A.vocab) per_row *= 2;
     const dim3 grid((unsigned)std::min<int64_t>(ceil_div(A.rows, kThreads / per_row), 1 << 22));
-    const auto kernel = A.stream ? token_grad_narrow_kernel<TYPE, true> : token_grad_narrow_kernel<TYPE, false>;
+    const auto kernel = A.stream ? token_grad_narrow_kernel<TYPE, STREAM> : token_grad_narrow_kernel<TYPE, false>;
     kernel<<<grid, kThreads, 0, stream>>>(A, per_row);
   } else {
-    constexpr int NV = 4;
     const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 22),
-                    (unsigned)std::min<int64_t>(ceil_div(A.vocab, NV * kGradPiece), 1 << 14));
-    const auto kernel = A.stream ? token_grad_kernel<TYPE, NV, true> : token_grad_kernel<TYPE, NV, false>;
+                    (unsigned)std::min<int64_t>(ceil_div(A.vocab, kGradVecs * kGradPiece), 1 << 14));
+    const auto kernel = A.stream ? token_grad_kernel<TYPE, kGradVecs, STREAM> : token_grad_kernel<TYPE, kGradVecs, false>;
     kernel<<<grid, kThreads, 0, stream>>>(A);
   }
   return launch_status();
@@ -700,7 +719,7 @@ extern "C" int qa_token_logprob(int type, int64_t rows, int64_t vocab, const voi
       !aligned(stats, 4) || (top && (!aligned(top_logprob, 4) || !aligned(top_index, 4))))
     return QA_ERR_ALIGNMENT;
   TokenArgs A{logits, target, logprob, entropy, stats, top_logprob, top_index, nullptr, nullptr,
-              rows, vocab, stride, vocab, (int)splits_for(rows, vocab), top, streams((double)rows * (double)vocab * (double)type_bytes(type))};
+              rows, vocab, stride, vocab, (int)splits_for(rows, vocab), top, token_streams(type, rows, vocab, logits, stride, top)};
   if (A.splits > 1) {
     if (!ws || ws_bytes < qa_token_workspace_bytes(rows, vocab, top)) return QA_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return QA_ERR_ALIGNMENT;
@@ -725,7 +744,7 @@ extern "C" int qa_token_logprob_grad(int type, int64_t rows, int64_t vocab, cons
       !aligned(entropy, 4) || !aligned(g_logprob, 4) || !aligned(g_entropy, 4))
     return QA_ERR_ALIGNMENT;
   const TokenGradArgs A{logits, target, stats, entropy, g_logprob, g_entropy, dlogits, rows, vocab, stride, dlogits_stride,
-                        streams((double)rows * (double)vocab * (double)(2 * type_bytes(type)))};
+                        token_grad_streams(type, rows, vocab)};
   const hipStream_t s = (hipStream_t)stream;
   if (type == QA_F32) return token_grad_launch<QA_F32>(A, s);
   if (type == QA_BF16) return token_grad_launch<QA_BF16>(A, s);

@@ -181,7 +181,8 @@ def logits(gen, T, V, t, pad):
     return x, target
 
 
-@pytest.mark.parametrize("t,V,pad", [("bf16", 50021, 0), ("f32", 70001, 1), ("f16", 4097, 2), ("bf16", 32768, 0)])
+@pytest.mark.parametrize("t,V,pad", [("bf16", 50021, 0), ("f32", 70001, 1), ("f16", 4097, 2), ("bf16", 32768, 0), ("bf16", 70001, 0),
+                                     ("f32", 32768, 0), ("f16", 131072, 0)])
 @pytest.mark.parametrize("top", [0, 8, 64])
 def test_token_logprob(t, V, pad, top):
     T = rows_for(V * BYTES[t])
@@ -214,7 +215,8 @@ def test_token_logprob(t, V, pad, top):
     assert torch.isnan(got[1][T - 2]) and torch.isnan(got[2][T - 2, 1])
 
 
-@pytest.mark.parametrize("t,V,pad", [("bf16", 2048, 0), ("f32", 1001, 0), ("f16", 7, 0), ("bf16", 2049, 1), ("f16", 8193, 0), ("f32", 47236, 3)])
+@pytest.mark.parametrize("t,V,pad", [("bf16", 2048, 0), ("f32", 1001, 0), ("f16", 7, 0), ("bf16", 2049, 1), ("f16", 8193, 0), ("f32", 47236, 3),
+                                     ("bf16", 16387, 0), ("f16", 7001, 1)])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_token_logprob_grad(t, V, pad, in_place):
     T = rows_for(2 * V * BYTES[t])
