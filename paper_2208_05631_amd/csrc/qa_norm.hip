@@ -297,7 +297,9 @@ __global__ __launch_bounds__(threads_of<LANES>) __attribute__((amdgpu_waves_per_
     for (int v = 0; v < NV; ++v)
       dh[v] = load_place<TYPE, STREAM, LANES>((const T*)A.dh + row * A.dh_stride, place[v], n[v], cols);
   };
-  constexpr bool AHEAD = kAhead<TYPE, LANES, NV>, DH_AHEAD = AHEAD && !CODED;  // codes take the registers that this takes
+  // Codes take the registers that reading dh ahead takes, and those of two vectors per lane inside a wave lose by any reading ahead
+  // (42744 x 785 bfloat16: 54 us, and 71).
+  constexpr bool AHEAD = kAhead<TYPE, LANES, NV> && !(CODED && LANES == kWave && NV == 2), DH_AHEAD = AHEAD && !CODED;
   int turn = 0;
   if (AHEAD && first < A.R.rows) read(first);
   if (DH_AHEAD && first < A.R.rows) read_dh(next_dh, first);
@@ -482,30 +484,41 @@ Form form_of(int64_t cols) {
   if (cols <= kHeldCols) return {1024, 2};
   return {0, 0};
 }
-// Work-groups, from threads per compute unit: where rows are read ahead some 4096 columns at a time are on their way to each, and
-// twice as many where they are codes.  More are slower, by the rows that meet in memory and, backward, by the work-groups' sums
-// (16384 x 4096 bfloat16, 256 threads, 512 and 1024: forward 101 us, 114 and 113, backward 87, 90 and 105).  Rows that leave lanes
-// empty bring fewer columns, and those whose last vector is not full hold their work-group up, by stores of single elements: they get 512
-// threads for 256 (forward 20000 x 2051: 180 us -> 103, 10000 x 4095: 109 -> 84, 16000 x 2560: 84 -> 65, but 10000 x 4000: 65 -> 69,
-// and, of rows inside a wave, 40000 x 1003: 74 -> 77; backward 20000 x 2051: 116 -> 93, 16000 x 3000: 85 -> 72, 10000 x 4000: 64 -> 61, but
-// 10000 x 4096: 57 -> 59; from codes they lose, 10000 x 4095: 73 -> 82).  Calls that the caches hold do not mind forward, and are spread
-// wider; backward they stay as they are (2000 x 4095: 21 us -> 23).
+// Work-groups, from threads per compute unit.  Some 4096 columns at a time are to be on their way to each where rows are read ahead, and
+// twice as many where they are codes; more are slower, by the rows that meet in memory and, backward, by the work-groups' sums
+// (16384 x 4096 bfloat16, 256 threads, 512 and 1024: forward 101 us, 114 and 113, backward 87, 90 and 105).
 int64_t groups_for(int64_t rows, Form f, int64_t threads_per_unit) {
   const int64_t threads = f.lanes == 0 ? 1024 : f.lanes <= kWave ? kThreads : f.lanes;
   return std::min<int64_t>(ceil_div(rows, f.lanes && f.lanes <= kWave ? kThreads / f.lanes : 1),
                            256 * std::max<int64_t>(threads_per_unit / threads, 1));
 }
-int64_t norm_groups(int64_t rows, int64_t cols, int type, bool stream) {
+// Rows bring less where they leave lanes empty, where they come without a residual, and where a row of several waves ends inside a vector,
+// whose elements are stored one by one while the others wait: twice the threads, and twice again for two of these with two vectors.  With
+// one vector per lane (1024 threads and 512): 32263 x 1040 63 us and 91, 63550 x 272 33 and 41, but 20164 x 1664 56 and 55, 93206 x 360 68 and
+// 62; without residual 16384 x 2048 45 and 46, 123361 x 272 58 and 81.  With two (512 and 256): 20000 x 2051 103 and 180, 10000 x 4095 84 and
+// 109, but 10000 x 4000 69 and 65, 40000 x 1003, in one wave, 77 and 74; without residual 8192 x 4096 45 and 47, and (1024 and 512)
+// 15307 x 2192 50 and 58, 8190 x 4097 54 and 60.  Calls that the caches hold are not slower with 512.
+int64_t norm_groups(int64_t rows, int64_t cols, int type, bool residual, bool stream) {
   const Form f = form_of(cols);
+  const int64_t full = f.lanes * f.vecs * kVec;
+  const bool in_wave = f.lanes <= kWave;
   if (f.lanes == 0) return groups_for(rows, f, 1024);
-  const bool filled = (cols % kVec == 0 || f.lanes <= kWave) && 4 * cols > 3 * f.lanes * f.vecs * kVec;
-  return groups_for(rows, f, stream && f.vecs == 2 && type != QA_F32 && filled ? 256 : 512);
+  if (f.vecs == 1) return groups_for(rows, f, !residual || 8 * cols <= (in_wave ? 5 : 6) * full ? 1024 : 512);
+  if (type == QA_F32) return groups_for(rows, f, 512);
+  const bool filled = (cols % kVec == 0 || in_wave) && 4 * cols > 3 * full;
+  if (residual) return groups_for(rows, f, filled && stream ? 256 : 512);
+  return groups_for(rows, f, filled ? 512 : 1024);
 }
+// Backward the sums make small calls dearer: 30840 x 272 20.8 us with 512 threads, 19.4 with 1024, 10459 x 401 13.7 and 15.0, but 61680 x 272 37 and
+// 32, 123361 x 272 73 and 62, 9847 x 1761 33 and 36; two vectors, 256 and 512: 16000 x 3000 85 and 72, 1913 x 2192 15.9 and 14.1, 10000 x 4095 81 and
+// 77, but 2000 x 4095 21 and 23, 10000 x 4096 57 and 59.  Binary32 rows of one vector lose with 1024 (32263 x 1040: 105 and 111).
 int64_t norm_grad_groups(int64_t rows, int64_t cols, int type, bool coded, bool stream) {
   const Form f = form_of(cols);
+  const int64_t full = f.lanes * f.vecs * kVec;
   if (f.lanes == 0 || (type == QA_F32 && f.vecs == 2)) return groups_for(rows, f, 1024);
   if (coded) return groups_for(rows, f, f.vecs == 2 ? 512 : 1024);
-  return groups_for(rows, f, f.vecs == 2 && !(stream && cols < f.lanes * f.vecs * kVec) ? 256 : 512);
+  if (f.vecs == 1) return groups_for(rows, f, 6 * cols < 5 * full && type != QA_F32 && rows * cols >= 1 << 24 ? 1024 : 512);
+  return groups_for(rows, f, 8 * cols < 7 * full || (stream && cols < full) ? 512 : 256);
 }
 
 // Calls `launch` with the lanes and vectors of a form as constants.
@@ -525,7 +538,7 @@ bool with_form(Form f, F launch) {
 template <int TYPE>
 int norm_launch(const NormArgs& A, hipStream_t stream) {
   const Form f = form_of(A.R.cols);
-  const dim3 grid((unsigned)norm_groups(A.R.rows, A.R.cols, TYPE, A.stream));
+  const dim3 grid((unsigned)norm_groups(A.R.rows, A.R.cols, TYPE, A.residual != nullptr, A.stream));
   auto held = [&](auto lanes, auto vecs) {
     constexpr bool STREAM = TYPE != QA_F32;
     if (STREAM && A.stream) rms_norm_kernel<TYPE, lanes, vecs, STREAM><<<grid, threads_of<lanes>, 0, stream>>>(A);
