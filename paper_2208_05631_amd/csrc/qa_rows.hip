@@ -14,20 +14,22 @@ namespace {
 // 16, cover a row; narrow rows share a work-group, wide ones are split over blockIdx.y.
 //
 // Eight work-groups per compute unit go over the rows: 144 us for the two calls of 16384 x 8192 bfloat16, and 155 with a work-group
-// for each 2048 columns of a row.
-constexpr int64_t kGroups = 2048;
+// for each 2048 columns of a row.  Calls beyond the caches whose rows one work-group covers have 32 (262144 x 512: 137 us, with
+// eight 144, without an end 154; 137096 x 979 180, 201 and 174; 994205 x 135 334, 350 and 320), others lose by as many (16384 x 8192: 165,
+// 211060 x 64 25.5 and 21.9).
 struct RowGrid {
   int per_row;      // lanes of a row that one work-group covers
   int rows;         // rows of one work-group
   dim3 grid;
 };
-RowGrid row_grid(int64_t rows, int64_t cols) {
+RowGrid row_grid(int64_t rows, int64_t cols, bool beyond) {
   RowGrid g;
   const int64_t lanes = ceil_div(ceil_div(cols, kVec), 16) * 16;
   g.per_row = (int)(lanes < kThreads ? lanes : kThreads);
   g.rows = kThreads / g.per_row;
   const int64_t across = ceil_div(lanes, g.per_row);
-  g.grid = dim3((unsigned)std::min<int64_t>(ceil_div(rows, g.rows), std::max<int64_t>(kGroups / across, 1)), (unsigned)across);
+  const int64_t most = across == 1 && beyond ? 8192 : std::max<int64_t>(2048 / across, 1);
+  g.grid = dim3((unsigned)std::min<int64_t>(ceil_div(rows, g.rows), most), (unsigned)across);
   return g;
 }
 
@@ -73,23 +75,26 @@ __global__ __launch_bounds__(kThreads) void rows_unpack_kernel(qa_coded_rows R, 
   }
 }
 
-bool streams(const qa_coded_rows* R, int type) {
-  return qa::streams((double)R->rows * (double)R->cols * (double)(type_bytes(type) + 1));
+bool beyond_caches(const qa_coded_rows* R, int type) {
+  return streams((double)R->rows * (double)R->cols * (double)(type_bytes(type) + 1));
 }
 
 template <int TYPE>
 int pack_launch(const qa_coded_rows* R, const void* x, int64_t x_stride, int8_t* codes, uint8_t* scales,
                 hipStream_t stream) {
-  const RowGrid g = row_grid(R->rows, R->cols);
-  const auto kernel = streams(R, TYPE) ? rows_pack_kernel<TYPE, true> : rows_pack_kernel<TYPE, false>;
+  // Narrow rows of binary32 that begin inside 16 bytes are not read past the caches (497102 x 135: the two calls 168 us, and 195 if so).
+  const bool beyond = beyond_caches(R, TYPE), past = beyond && !(TYPE == QA_F32 && R->cols <= 512 && x_stride % 4);
+  const RowGrid g = row_grid(R->rows, R->cols, beyond);
+  const auto kernel = past ? rows_pack_kernel<TYPE, true> : rows_pack_kernel<TYPE, false>;
   kernel<<<g.grid, kThreads, 0, stream>>>(*R, g.per_row, g.rows, (const ElemT<TYPE>*)x, x_stride, codes, scales);
   return launch_status();
 }
 template <int TYPE>
 int unpack_launch(const qa_coded_rows* R, const int8_t* codes, const uint8_t* scales, void* x, int64_t x_stride,
                   hipStream_t stream) {
-  const RowGrid g = row_grid(R->rows, R->cols);
-  const auto kernel = streams(R, TYPE) ? rows_unpack_kernel<TYPE, true> : rows_unpack_kernel<TYPE, false>;
+  const bool beyond = beyond_caches(R, TYPE);
+  const RowGrid g = row_grid(R->rows, R->cols, beyond);
+  const auto kernel = beyond ? rows_unpack_kernel<TYPE, true> : rows_unpack_kernel<TYPE, false>;
   kernel<<<g.grid, kThreads, 0, stream>>>(*R, g.per_row, g.rows, codes, scales, (ElemT<TYPE>*)x, x_stride);
   return launch_status();
 }
