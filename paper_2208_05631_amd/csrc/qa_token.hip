@@ -638,13 +638,15 @@ bool token_streams(int type, int64_t rows, int64_t vocab, const void* logits, in
   if (top) return type != QA_F32 && vocab >= 1 << 16;
   return type != QA_F32 || (vocab >= 1 << 14 && aligned(logits, 16) && stride % 4 == 0);
 }
-// Whether the logits' gradient goes past the caches: not in binary32 (4000 x 32768: 204 us, and 218 if it did), and not where a row
-// is a part of one piece (bfloat16, 40000 x 2049: 109 and 126, 32768 x 4096: 100 and 118, 20000 x 6144: 87 and 88, 16000 x 8191: 110 and 105;
-// 100000 x 1001, several rows to a work-group: 100 and 95).
+// Whether the logits' gradient goes past the caches: not where a row is a part of one piece (bfloat16, 40000 x 2049: 109 us, and 126 if it did,
+// 32768 x 4096: 100 and 118, 20000 x 6144: 87 and 88, 16000 x 8191: 110 and 105; 100000 x 1001, several rows to a work-group: 100 and 95), and
+// in binary32 only for rows of a quarter of a work-group or an aligned half (180000 x 217: 66 and 63, 80000 x 512: 67 and 63, but 80000 x 511:
+// 69 and 77, 4000 x 32768: 204 and 218).
 constexpr int kGradVecs = 4;
-bool token_grad_streams(int type, int64_t rows, int64_t vocab) {
-  return type != QA_F32 && (vocab <= kGradPiece || 4 * vocab > 3 * kGradVecs * kGradPiece) &&
-         streams((double)rows * (double)vocab * (double)(2 * type_bytes(type)));
+bool token_grad_streams(int type, int64_t rows, int64_t vocab, int64_t x_stride, int64_t dx_stride) {
+  if (!streams((double)rows * (double)vocab * (double)(2 * type_bytes(type)))) return false;
+  if (type == QA_F32) return vocab <= 256 || (vocab <= 512 && x_stride % 4 == 0 && dx_stride % 4 == 0);
+  return vocab <= kGradPiece || 4 * vocab > 3 * kGradVecs * kGradPiece;
 }
 
 template <int TYPE, bool TOP>
@@ -673,16 +675,16 @@ int token_launch(TokenArgs& A, hipStream_t stream) {
 }
 template <int TYPE>
 int token_grad_launch(const TokenGradArgs& A, hipStream_t stream) {
-  constexpr bool STREAM = TYPE != QA_F32;
   if (A.vocab <= kGradPiece) {
     int per_row = 1;
     while (per_row * kVec < A.vocab) per_row *= 2;
     const dim3 grid((unsigned)std::min<int64_t>(ceil_div(A.rows, kThreads / per_row), 1 << 22));
-    const auto kernel = A.stream ? token_grad_narrow_kernel<TYPE, STREAM> : token_grad_narrow_kernel<TYPE, false>;
+    const auto kernel = A.stream ? token_grad_narrow_kernel<TYPE, true> : token_grad_narrow_kernel<TYPE, false>;
     kernel<<<grid, kThreads, 0, stream>>>(A, per_row);
   } else {
     const dim3 grid((unsigned)std::min<int64_t>(A.rows, 1 << 22),
                     (unsigned)std::min<int64_t>(ceil_div(A.vocab, kGradVecs * kGradPiece), 1 << 14));
+    constexpr bool STREAM = TYPE != QA_F32;
     const auto kernel = A.stream ? token_grad_kernel<TYPE, kGradVecs, STREAM> : token_grad_kernel<TYPE, kGradVecs, false>;
     kernel<<<grid, kThreads, 0, stream>>>(A);
   }
@@ -744,7 +746,7 @@ extern "C" int qa_token_logprob_grad(int type, int64_t rows, int64_t vocab, cons
       !aligned(entropy, 4) || !aligned(g_logprob, 4) || !aligned(g_entropy, 4))
     return QA_ERR_ALIGNMENT;
   const TokenGradArgs A{logits, target, stats, entropy, g_logprob, g_entropy, dlogits, rows, vocab, stride, dlogits_stride,
-                        token_grad_streams(type, rows, vocab)};
+                        token_grad_streams(type, rows, vocab, stride, dlogits_stride)};
   const hipStream_t s = (hipStream_t)stream;
   if (type == QA_F32) return token_grad_launch<QA_F32>(A, s);
   if (type == QA_BF16) return token_grad_launch<QA_BF16>(A, s);

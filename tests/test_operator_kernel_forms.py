@@ -32,4 +32,4 @@ def test_token(forms):
     past = {(f[0], f[2]) for f in forms["token_wide_kernel"] if f[3]}                # type, alternatives
     assert past == {(F32, False), (BF16, False), (F16, False), (BF16, True), (F16, True)}
     assert {f[0] for f in forms["token_grad_kernel"] if f[2]} == {BF16, F16}
-    assert {f[0] for f in forms["token_grad_narrow_kernel"] if f[1]} == {BF16, F16}
+    assert {f[0] for f in forms["token_grad_narrow_kernel"] if f[1]} == {F32, BF16, F16}
