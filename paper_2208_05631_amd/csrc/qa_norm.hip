@@ -2,8 +2,9 @@
 //
 // Both are bound by memory, hold a row in registers between its sum and its outputs, and read the next row meanwhile.  Forward, 8192 x
 // 4096 bfloat16 with everything written: 303 MB in 52 us, 5.8 TB/s; one row of 8192: 1.5 us of device time in a call of 6.  Backward,
-// 16384 x 4096 with the gradient that comes past the norm: 537 MB in 88 us, 6.1 TB/s.  Rows of an odd number of columns begin inside a
-// 16-byte word and cost more (8192 x 4097: 71 us and 76).
+// 16384 x 4096 with the gradient that comes past the norm: 537 MB in 88 us, 6.1 TB/s.  Rows that end inside a vector cost more: 8192 x
+// 4097 71 us and 76, 8192 x 4104 59 and 62.  That is neither where they begin (4097 columns in rows of 4104 elements take as long) nor the
+// stores of their last elements (69 without these).
 #include <algorithm>
 #include <type_traits>
 
@@ -492,9 +493,8 @@ int64_t groups_for(int64_t rows, Form f, int64_t threads_per_unit) {
   return std::min<int64_t>(ceil_div(rows, f.lanes && f.lanes <= kWave ? kThreads / f.lanes : 1),
                            256 * std::max<int64_t>(threads_per_unit / threads, 1));
 }
-// Rows bring less where they leave lanes empty, where they come without a residual, and where a row of several waves ends inside a vector,
-// whose elements are stored one by one while the others wait: twice the threads, and twice again for two of these with two vectors.  With
-// one vector per lane (1024 threads and 512): 32263 x 1040 63 us and 91, 63550 x 272 33 and 41, but 20164 x 1664 56 and 55, 93206 x 360 68 and
+// Rows bring less where they leave lanes empty, where they come without a residual, and, measured, where a row of several waves ends inside
+// a vector: twice the threads, and twice again for two of these with two vectors.  With one vector per lane (1024 threads and 512): 32263 x 1040 63 us and 91, 63550 x 272 33 and 41, but 20164 x 1664 56 and 55, 93206 x 360 68 and
 // 62; without residual 16384 x 2048 45 and 46, 123361 x 272 58 and 81.  With two (512 and 256): 20000 x 2051 103 and 180, 10000 x 4095 84 and
 // 109, but 10000 x 4000 69 and 65, 40000 x 1003, in one wave, 77 and 74; without residual 8192 x 4096 45 and 47, and (1024 and 512)
 // 15307 x 2192 50 and 58, 8190 x 4097 54 and 60.  Calls that the caches hold are not slower with 512.

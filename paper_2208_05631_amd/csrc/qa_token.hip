@@ -524,7 +524,8 @@ __device__ __forceinline__ GradRow grad_row(const TokenGradArgs& A, int64_t row)
   return r;
 }
 // dx_j = -p_j (a + e (log p_j + H)), and a more at the target.  Bound by memory: 8192 x 32768 bfloat16 178 us, 6.0 TB/s; 509 x 47236
-// binary32 in rows of 47239: 44 us, 4.4 TB/s.
+// binary32 44 us, 4.4 TB/s, whether rows begin on 16 bytes or not: rows of several pieces are read by work-groups that run together, each
+// elsewhere (as much in rows of one piece: 38, of six whole ones: 42).
 template <int TYPE>
 __device__ __forceinline__ Raw8<TYPE> grad_of(const GradRow& r, const Raw8<TYPE>& raw, int64_t i) {
   float v[kVec], d[kVec];
@@ -542,8 +543,9 @@ __device__ __forceinline__ Raw8<TYPE> grad_of(const GradRow& r, const Raw8<TYPE>
 }
 
 constexpr int64_t kGradPiece = (int64_t)kThreads * kVec;       // logits that a work-group has in one vector per lane
-// Pieces inside a row have no branch.  Past the caches they begin on 16 bytes of dx, wherever the row does: 4096 x 100003 bfloat16 395
-// us -> 337 (not in calls that the caches hold, 8192 x 2049 22 us and 27, nor in rows of few pieces, 32768 x 4099 118 and 145).
+// Pieces inside a row have no branch; a row's last piece has one around each load, which costs rows of a part of one piece most (8192 x
+// 2049: 22 us, 8192 x 2048 in the form below: 15).  Past the caches pieces begin on 16 bytes of dx, wherever the row does, where there are
+// more than two: 4096 x 100003 bfloat16 395 us -> 337.
 template <int TYPE, int NV, bool STREAM>
 __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenGradArgs A) {
   typedef ElemT<TYPE> T;

@@ -3,10 +3,11 @@
 // A code times its power of two is exact in bfloat16, and so are dY's elements, or two (binary16) or three (binary32)
 // bfloat16 parts of them, so every product of the matrix cores is exact and the sums are held in binary32.
 //
-// 16384 rows, 8192 x 4096: 0.92-0.94 ms, 1.17-1.20 PFLOP/s; a bfloat16 product of the same shape by the library, from
-// operands that are bfloat16 already, takes 1.06 ms, its largest square ones reach 1.35.  Bound by the card's power: the matrix cores are
-// busy for two thirds of the cycles, at 1.7 of 2.4 GHz (four waves of 128 x 128 instead of eight of 128 x 64: half of the cycles at
-// 2.0 GHz, 1.00 ms).  8192 rows, 4096 x 4096: bfloat16 0.24 ms, binary16 0.43, binary32 0.63.
+// 16384 rows, 8192 x 4096: 0.88-0.93 ms from card to card, 1.18-1.25 PFLOP/s; a bfloat16 product of the same shape by the library, from
+// operands that are bfloat16 already, takes 1.06 ms, its largest square ones reach 1.35.  Bound by the card's power: it takes 1.57 million
+// cycles, two thirds of which the matrix cores are busy, at 1.75 GHz of 2.4, and at 1.4 for some launches soon after a pause, which take 1.1 ms
+// (four waves of 128 x 128 instead of eight of 128 x 64: half of the cycles at 2.0 GHz, 1.00 ms).  8192 rows, 4096 x 4096: bfloat16 0.23 ms,
+// binary16 0.41, binary32 0.61.
 #include <algorithm>
 
 #include "qa_rows.h"
