@@ -524,8 +524,7 @@ __device__ __forceinline__ GradRow grad_row(const TokenGradArgs& A, int64_t row)
   return r;
 }
 // dx_j = -p_j (a + e (log p_j + H)), and a more at the target.  Bound by memory: 8192 x 32768 bfloat16 178 us, 6.0 TB/s; 509 x 47236
-// binary32 44 us, 4.4 TB/s, whether rows begin on 16 bytes or not: rows of several pieces are read by work-groups that run together, each
-// elsewhere (as much in rows of one piece: 38, of six whole ones: 42).
+// binary32 44 us, 4.4 TB/s, whether rows begin on 16 bytes or not (as much in rows of one piece 38, of six whole ones 42, copied by torch 37).
 template <int TYPE>
 __device__ __forceinline__ Raw8<TYPE> grad_of(const GradRow& r, const Raw8<TYPE>& raw, int64_t i) {
   float v[kVec], d[kVec];
