@@ -578,6 +578,85 @@ int qa_token_logprob_grad(int type, int64_t rows, int64_t vocab, const void* log
                           const float* g_logprob_or_null, const float* g_entropy_or_null, void* dlogits,
                           int64_t dlogits_stride, void* stream);
 
+/* Log probabilities of targets under an output layer, logits = x w^T (x: rows x features, w: vocab x features), without
+ * the logits being kept: they are multiplied tile by tile, with sums in binary32, and what is left of a tile is the
+ * largest logit and two sums per row.  Numbers and conventions are those of qa_token_logprob, of unrounded logits. */
+typedef struct {
+  int64_t rows;      /* 0 <= rows < 2^24                               */
+  int64_t vocab;     /* 1 <= vocab < 2^24                              */
+  int64_t features;  /* 1 <= features < 2^20                           */
+  int64_t x_stride;  /* elements between rows of x, >= features, < 2^40 */
+  int64_t w_stride;  /* elements between rows of w, >= features, < 2^40 */
+} qa_output_layer;
+
+#define QA_OP_LOGPROB 10
+#define QA_OP_LOGPROB_GRAD 11
+
+/* Bytes of device workspace that `op` (QA_OP_LOGPROB or QA_OP_LOGPROB_GRAD) needs, a multiple of 256; 0 for invalid
+ * arguments, other operations and rows == 0.  Every call of one layer at a time has its own. */
+size_t qa_output_workspace_bytes(const qa_output_layer* layer, int op, int type);
+
+/* logprob, entropy and stats of each row as qa_token_logprob gives them.  target and logprob are NULL together, entropy and
+ * stats may be NULL.  16-bit elements are multiplied as they are; binary32 ones as two binary16 parts each, scaled by a power of two
+ * per row (22 bits and a sign; what is below 2^-39 of a row's largest magnitude is lost).  Rows that begin on 16 bytes,
+ * with strides of a multiple of 8 below 2^22 and features a multiple of 32, are read where they lie (16-bit types); others are copied
+ * into the workspace first. */
+int qa_output_logprob(const qa_output_layer* layer, int type, const void* x, const void* w,
+                      const int32_t* target_or_null, float* logprob_or_null, float* entropy_or_null,
+                      float* stats_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of x and w from those of logprob and entropy (binary32, one per row; NULL counts as 0):
+ *     c_tj = g_logprob_t ([j = target_t] - p_tj) - g_entropy_t p_tj (log p_tj + entropy_t)
+ *     dx = c w (type `type`);   dw_jk = (accumulate ? dw_jk : 0) + sum_t c_tj x_tk (binary32)
+ * with the logits multiplied again, a piece of the vocabulary at a time.  stats and entropy as qa_output_logprob wrote them
+ * (entropy and g_entropy NULL together).  A row without target has the entropy's part alone.  A row whose g_logprob (or
+ * target) and g_entropy are both none or 0 gets dx = 0 and adds nothing to dw, whatever x holds there: padding.
+ * Numbers are multiplied as binary16 with one power of two per matrix as scale: c in two parts, but in one for dx of a 16-bit
+ * type (a rounding by 2^-11, an eighth of a bfloat16's), binary32 x and w in two, bfloat16 ones exactly, but for magnitudes below 2^-32 of
+ * their matrix's largest, which lose bits below 2^-39 of it.  dx_or_null and dw_or_null may be NULL (not both); dx does not overlap x.
+ * rows == 0 writes dw = 0 (kept, with accumulate). */
+int qa_output_logprob_grad(const qa_output_layer* layer, int type, const void* x, const void* w,
+                           const int32_t* target_or_null, const float* stats, const float* entropy_or_null,
+                           const float* g_logprob_or_null, const float* g_entropy_or_null, void* dx_or_null,
+                           int64_t dx_stride, float* dw_or_null, int64_t dw_stride, int accumulate, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* ---- a matrix's update, orthogonalised ----------------------------------------------------------------------------
+ *
+ * The steps above treat a parameter vector one coordinate at a time.  A matrix's gradient can be stepped as a whole: its
+ * singular vectors kept, its singular values brought near 1 by odd polynomials, which need products only:
+ *     X_0 = G / |G| (the root of the sum of squares),   X_{i+1} = a_i X_i + b_i (X_i X_i^T) X_i + c_i (X_i X_i^T)^2 X_i
+ * (for more rows than columns with X_i^T X_i on the other side, which is the same).  Element (r, k) of matrix i is at
+ * i*matrix_stride + r*stride + k of every buffer of a call. */
+typedef struct {
+  int64_t count;          /* matrices of one shape, 0 <= count < 2^16                                */
+  int64_t rows, cols;     /* 1 <= rows, cols < 2^20                                                 */
+  int64_t stride;         /* elements between rows, >= cols, < 2^40                                 */
+  int64_t matrix_stride;  /* elements between matrices, >= (rows-1)*stride + cols; unused for count 1 */
+} qa_matrices;
+
+#define QA_ORTHOGONAL_STEPS_MAX 32
+
+/* Bytes of device workspace that the calls below need for matrices of `type` (QA_F32 for qa_step_orthogonal): some 16 to 24
+ * per element; 0 for invalid arguments and count == 0. */
+size_t qa_orthogonal_workspace_bytes(const qa_matrices* matrices, int type);
+
+/* out = X_steps, 1 <= steps <= QA_ORTHOGONAL_STEPS_MAX.  coefficients: HOST array of 3*steps floats, a, b, c of each
+ * step in turn, magnitudes below 64; NULL: 3.4445, -4.7750, 2.0315 in every step, by which all but the smallest singular values end
+ * between 0.7 and 1.2 after five.  A matrix of zeros gives zeros; one with an infinity or a NaN gives NaN.  Numbers
+ * are held in two binary16 parts, 22 bits and a sign, in fixed point below 2^-24 (X_i of a magnitude of 64 and more, which no
+ * polynomial of this use has, are infinite, and NaN from there on); norms in binary64, sums in binary32.  out may be g. */
+int qa_orthogonalize(const qa_matrices* matrices, int type, const void* g, int steps, const float* coefficients_or_null,
+                     void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* One step of parameters x along it, all in binary32:
+ *     momentum = mu momentum + g;   u = nesterov ? g + mu momentum : momentum   (u = g with momentum NULL)
+ *     x = shrink x - eta X_steps(u)
+ * 0 <= mu <= 1, nesterov 0 or 1, 0 <= eta < 1e30, 0 <= shrink <= 1 (1 - eta times a weight decay). */
+int qa_step_orthogonal(const qa_matrices* matrices, const float* g, float* momentum_or_null, float* x, float mu,
+                       int nesterov, int steps, const float* coefficients_or_null, float eta, float shrink, void* ws,
+                       size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

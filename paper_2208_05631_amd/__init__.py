@@ -17,5 +17,7 @@ from .binding import (  # noqa: F401
     QA_F32, QA_BF16, QA_F16, QA_OP_NORM_GRAD, QA_OP_WEIGHT_GRAD, QA_TOP_MAX, CodedRows, qa_rows_workspace_bytes,
     qa_rows_pack, qa_rows_unpack, qa_rows_weight_grad, qa_rms_norm, qa_rms_norm_grad,
     qa_token_workspace_bytes, qa_token_logprob, qa_token_logprob_grad,
+    QA_OP_LOGPROB, QA_OP_LOGPROB_GRAD, QA_ORTHOGONAL_STEPS_MAX, OutputLayer, Matrices, qa_output_workspace_bytes,
+    qa_output_logprob, qa_output_logprob_grad, qa_orthogonal_workspace_bytes, qa_orthogonalize, qa_step_orthogonal,
 )
 from . import placement  # noqa: F401,E402  (where large arrays lie in device memory)

@@ -22,7 +22,9 @@ QA_DENSE, QA_CSR = 0, 1
 QA_METHOD_QCMD, QA_METHOD_QRDA = 0, 1
 QA_F32, QA_BF16, QA_F16 = 0, 1, 2
 QA_OP_NORM_GRAD, QA_OP_WEIGHT_GRAD = 8, 9
+QA_OP_LOGPROB, QA_OP_LOGPROB_GRAD = 10, 11
 QA_TOP_MAX = 64
+QA_ORTHOGONAL_STEPS_MAX = 32
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -77,6 +79,28 @@ class CodedRows(C.Structure):
         """Rows of codes padded to 16 bytes, rows of scales without padding."""
         return CodedRows(rows, cols, group, code_stride or (cols + 15) // 16 * 16,
                          scale_stride or (cols + group - 1) // group)
+
+
+class OutputLayer(C.Structure):
+    """Mirror of qa_output_layer."""
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int64), ("features", C.c_int64), ("x_stride", C.c_int64),
+                ("w_stride", C.c_int64)]
+
+    @staticmethod
+    def make(rows, vocab, features, x_stride=None, w_stride=None):
+        return OutputLayer(rows, vocab, features, features if x_stride is None else x_stride,
+                           features if w_stride is None else w_stride)
+
+
+class Matrices(C.Structure):
+    """Mirror of qa_matrices."""
+    _fields_ = [("count", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64), ("stride", C.c_int64),
+                ("matrix_stride", C.c_int64)]
+
+    @staticmethod
+    def make(count, rows, cols, stride=None, matrix_stride=None):
+        stride = cols if stride is None else stride
+        return Matrices(count, rows, cols, stride, rows * stride if matrix_stride is None else matrix_stride)
 
 
 class SegmentPlan(C.Structure):
@@ -155,6 +179,17 @@ _lib.qa_token_workspace_bytes.restype = _sz
 _lib.qa_token_workspace_bytes.argtypes = [_i64, _i64, _i32]
 _lib.qa_token_logprob.argtypes = [C.c_int, _i64, _i64, _vp, _i64, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.qa_token_logprob_grad.argtypes = [C.c_int, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]
+
+_layer, _matrices = C.POINTER(OutputLayer), C.POINTER(Matrices)
+_lib.qa_output_workspace_bytes.restype = _sz
+_lib.qa_output_workspace_bytes.argtypes = [_layer, C.c_int, C.c_int]
+_lib.qa_output_logprob.argtypes = [_layer, C.c_int, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.qa_output_logprob_grad.argtypes = [_layer, C.c_int, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64, C.c_int,
+                                        _vp, _sz, _vp]
+_lib.qa_orthogonal_workspace_bytes.restype = _sz
+_lib.qa_orthogonal_workspace_bytes.argtypes = [_matrices, C.c_int]
+_lib.qa_orthogonalize.argtypes = [_matrices, C.c_int, _vp, C.c_int, C.POINTER(_f32), _vp, _vp, _sz, _vp]
+_lib.qa_step_orthogonal.argtypes = [_matrices, _vp, _vp, _vp, _f32, C.c_int, C.c_int, C.POINTER(_f32), _f32, _f32, _vp, _sz, _vp]
 
 
 def _p(t):
@@ -408,3 +443,44 @@ def qa_token_logprob_grad(type, rows, vocab, logits, stride, target, stats, entr
     _check(_lib.qa_token_logprob_grad(type, rows, vocab, _p(logits), stride, _p(target), _p(stats), _p(entropy),
                                       _p(g_logprob), _p(g_entropy), _p(dlogits), dlogits_stride,
                                       _stream(stream)), "qa_token_logprob_grad")
+
+
+def qa_output_workspace_bytes(layer: OutputLayer, op: int, type: int) -> int:
+    return int(_lib.qa_output_workspace_bytes(C.byref(layer), op, type))
+
+
+def qa_output_logprob(layer, type, x, w, target, logprob, entropy, stats, ws, stream=None):
+    _check(_lib.qa_output_logprob(C.byref(layer), type, _p(x), _p(w), _p(target), _p(logprob), _p(entropy), _p(stats),
+                                  _p(ws), _nbytes(ws), _stream(stream)), "qa_output_logprob")
+
+
+def qa_output_logprob_grad(layer, type, x, w, target, stats, entropy, g_logprob, g_entropy, dx, dx_stride, dw, dw_stride,
+                           accumulate, ws, stream=None):
+    _check(_lib.qa_output_logprob_grad(C.byref(layer), type, _p(x), _p(w), _p(target), _p(stats), _p(entropy),
+                                       _p(g_logprob), _p(g_entropy), _p(dx), dx_stride, _p(dw), dw_stride, accumulate,
+                                       _p(ws), _nbytes(ws), _stream(stream)), "qa_output_logprob_grad")
+
+
+def qa_orthogonal_workspace_bytes(matrices: Matrices, type: int) -> int:
+    return int(_lib.qa_orthogonal_workspace_bytes(C.byref(matrices), type))
+
+
+def _coefficients(steps, coefficients):
+    """coefficients: (a, b, c) of each step, host numbers, or None."""
+    if coefficients is None:
+        return None
+    flat = [float(v) for abc in coefficients for v in abc]
+    if len(flat) != 3 * steps:
+        raise ValueError(f"coefficients: three numbers for each of {steps} steps are wanted")
+    return (C.c_float * len(flat))(*flat)
+
+
+def qa_orthogonalize(matrices, type, g, steps, coefficients, out, ws, stream=None):
+    _check(_lib.qa_orthogonalize(C.byref(matrices), type, _p(g), steps, _coefficients(steps, coefficients), _p(out), _p(ws),
+                                 _nbytes(ws), _stream(stream)), "qa_orthogonalize")
+
+
+def qa_step_orthogonal(matrices, g, momentum, x, mu, nesterov, steps, coefficients, eta, shrink, ws, stream=None):
+    _check(_lib.qa_step_orthogonal(C.byref(matrices), _p(g), _p(momentum), _p(x), mu, nesterov, steps,
+                                   _coefficients(steps, coefficients), eta, shrink, _p(ws), _nbytes(ws), _stream(stream)),
+           "qa_step_orthogonal")

@@ -8,12 +8,11 @@
 #include <cfloat>
 
 #include "qa_rows.h"
+#include "qa_softmax.h"
 
 namespace qa {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr float kFar = -1e4f;                      // 2^kFar is 0
 constexpr int kTop = QA_TOP_MAX;                   // a lane for each alternative
 static_assert(kTop == kWave, "the alternatives of a row are held one per lane");
 
@@ -27,22 +26,9 @@ __device__ __forceinline__ float wave_max_f32(float v) {
                fmaxf(as_f32((uint32_t)__builtin_amdgcn_readlane(i, 32)), as_f32((uint32_t)__builtin_amdgcn_readlane(i, 48))));
 }
 
-// ---- sums of a softmax -----------------------------------------------------------------------------------------
-//
-// With m the largest logit so far: s = sum of 2^t and w = sum of 2^t t, t = (x - m) log2 e.  Then log p = (x - m) -
-// log s and entropy = log s - ln2 w / s; both terms of the entropy are >= 0, nothing cancels.
-// m is -FLT_MAX at least, so that -infinity has t = -infinity and adds nothing; in the product t is kFar at least.
-struct Sums { float m, s, w; };
-__device__ __forceinline__ Sums no_sums() { return {-FLT_MAX, 0.0f, 0.0f}; }
+// ---- sums of a softmax, over the lanes of a wave --------------------------------------------------------------
 
-// The same sums against another maximum.
-__device__ __forceinline__ void raise(Sums& a, float m) {
-  const float t = fmaxf((a.m - m) * kLog2e, kFar), f = __builtin_amdgcn_exp2f(t);
-  a.w = (a.w + a.s * t) * f;
-  a.s *= f;
-  a.m = m;
-}
-// Sums over the lanes of a wave, each with a maximum of its own.
+// Each lane has a maximum of its own.
 __device__ __forceinline__ Sums over_lanes(Sums a) {
   raise(a, wave_max_f32(a.m));
   a.s = wave_sum_f32(a.s);

@@ -1,0 +1,264 @@
+"""Log probabilities under an output layer and their gradient against the formulas in 64 bits.
+
+Tolerances.  u = 2^-24.  A logit of 16-bit operands is a sum of exact products in binary32, k taken sixteen at a time: at most (K / 16 + 16)
+roundings of partial sums, each at most u sum|x w|.  Binary32 operands are two parts of 22 bits and a sign: 2^-23 of each factor,
+2^-22 for the product of the two small parts that is left out, and three times the sums.  So a logit is off by at most
+    dz = ((P K / 16 + 16) u + (P == 3) 2^-21) max_v sum|x w|          (P: products, 1 or 3),
+log p by 2 dz and the statistics' own errors (SUM as in the other operators' tests), the entropy by dz sum p |log p + H| <= dz (2 H + 2)."""
+import math
+import zlib
+
+import pytest
+import torch
+
+import layer_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    import paper_2208_05631_amd as qa
+    DEV = torch.device("cuda:0")
+
+F64 = torch.float64
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF_ULP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+U = 2.0 ** -24
+SUM = 64 * U
+
+
+def code_of(t):
+    return {"f32": qa.QA_F32, "bf16": qa.QA_BF16, "f16": qa.QA_F16}[t]
+
+
+def gen_of(*what):
+    return torch.Generator().manual_seed(zlib.crc32(repr(what).encode()))
+
+
+def inside(v, t, pad=0, lead=0):
+    """v rounded to the type, and on the device as rows of a wider buffer of NaN that begins `lead` elements after an aligned place."""
+    v = v.to(TYPES[t])
+    T, K = v.shape
+    flat = torch.full((lead + T * (K + pad) + 8,), math.nan, dtype=TYPES[t])
+    flat[lead:lead + T * (K + pad)].view(T, K + pad)[:, :K] = v
+    return v.to(F64), flat.to(DEV)[lead:lead + T * (K + pad)].view(T, K + pad)[:, :K]
+
+
+def layer_of(gen, T, V, H, t, pad=0, lead=0, scale=2.0):
+    w = torch.randn(V, H, generator=gen) * (scale / math.sqrt(H))
+    y = torch.randint(0, V, (T,), generator=gen)
+    x = torch.randn(T, H, generator=gen) + 1.5 * (torch.rand(T, 1, generator=gen) < 0.5) * w[y] / scale
+    x64, xd = inside(x, t, pad, lead)
+    w64, wd = inside(w, t, pad, lead)
+    return qa.OutputLayer.make(T, V, H, H + pad, H + pad), x64, xd, w64, wd, y
+
+
+def room(layer, op, t):
+    """Filled with NaN: nothing that a call reads there may be older than the call."""
+    return torch.full((qa.qa_output_workspace_bytes(layer, op, code_of(t)) // 4,), math.nan, device=DEV)
+
+
+def dz_of(x, w, t):
+    P = 3 if t == "f32" else 1
+    most = (x.abs() @ w.abs().t()).amax(dim=1)
+    return ((P * x.shape[1] / 16 + 16) * U + (2.0 ** -21 if P == 3 else 0.0)) * most
+
+
+def score(layer, xd, wd, y, t):
+    T = layer.rows
+    lp, h, st = (torch.full(s, 5.0, device=DEV) for s in ((T + 1,), (T + 1,), (T + 1, 2)))
+    qa.qa_output_logprob(layer, code_of(t), xd, wd, y.to(torch.int32).to(DEV), lp, h, st, room(layer, qa.QA_OP_LOGPROB, t))
+    assert (lp[T:] == 5.0).all() and (h[T:] == 5.0).all() and (st[T:] == 5.0).all()
+    return lp[:T].cpu().to(F64), h[:T].cpu().to(F64), st[:T].cpu().to(F64)
+
+
+def check_score(t, x, w, y, got):
+    z, lp, h, st = ref.score(x, w, y)
+    dz = dz_of(x, w, t)
+    assert ((got[2][:, 0] - st[:, 0]).abs() <= dz + U * st[:, 0].abs()).all()
+    assert ((got[2][:, 1] - st[:, 1]).abs() <= 2 * dz + SUM * (1 + st[:, 1])).all()
+    assert ((got[0] - lp).abs() <= 2 * dz + SUM * (1 + lp.abs())).all()
+    assert ((got[1] - h).abs() <= dz * (2 * h + 2) + SUM * (1 + 4 * st[:, 1])).all()
+
+
+SHAPES = [(1, 1, 1, 0), (1, 1000, 64, 0), (1, 333, 100, 0), (3, 129, 32, 0), (16, 64, 96, 8), (17, 257, 33, 0), (64, 500, 128, 0), (65, 511, 160, 0),
+          (100, 65, 257, 1), (130, 1030, 64, 8), (300, 700, 72, 0), (1, 70000, 32, 0), (513, 130, 515, 3), (48, 4097, 320, 0)]
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,V,H,pad", SHAPES)
+def test_logprob(t, T, V, H, pad):
+    gen = gen_of(t, T, V, H)
+    layer, x, xd, w, wd, y = layer_of(gen, T, V, H, t, pad)
+    y[T // 2] = -1 if T > 2 else y[T // 2]
+    check_score(t, x, w, y, score(layer, xd, wd, y, t))
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_logprob_in_large_tiles(t):
+    """Enough tiles for those of 256 x 256, ends inside a tile on both sides."""
+    gen = gen_of("large", t)
+    layer, x, xd, w, wd, y = layer_of(gen, 2101, 6101, 64, t)
+    check_score(t, x, w, y, score(layer, xd, wd, y, t))
+
+
+def check_grad(t, T, V, H, pad=0, lead=0, entropy=False, ignored=0.0, wants="xw", accumulate=False, seed=0):
+    gen = gen_of(t, T, V, H, entropy, ignored, seed)
+    layer, x, xd, w, wd, y = layer_of(gen, T, V, H, t, pad, lead)
+    if ignored:
+        y = torch.where(torch.rand(T, generator=gen) < ignored, torch.full_like(y, -1), y)
+    z, _, h, st = ref.score(x, w, y)
+    st32, h32 = st.float(), h.float()
+    a = -torch.rand(T, generator=gen) - 0.5
+    e = 0.3 * torch.randn(T, generator=gen) if entropy else None
+    dx = torch.full((T, H + 1), 5.0, dtype=TYPES[t], device=DEV) if "x" in wants else None
+    dw = torch.full((V, H + 2), 3.0, device=DEV) if "w" in wants else None
+    qa.qa_output_logprob_grad(layer, code_of(t), xd, wd, y.to(torch.int32).to(DEV), st32.to(DEV), h32.to(DEV) if entropy else None, a.to(DEV),
+                              e.to(DEV) if entropy else None, dx, H + 1, dw, H + 2, int(accumulate), room(layer, qa.QA_OP_LOGPROB_GRAD, t))
+    c, none = ref.logits_grad(z, y, st32.to(F64), h32.to(F64), a.to(F64), e.to(F64) if entropy else None)
+    # c: log p is off by dz and the roundings of z, m and log_sum; p relatively by as much and the exponential's 2^-21
+    lp = z - st32.to(F64)[:, :1] - st32.to(F64)[:, 1:]
+    off = dz_of(x, w, t)[:, None] + 8 * U * (z.abs() + st[:, :1].abs() + st[:, 1:]) + 2.0 ** -21
+    size = a.abs().to(F64)[:, None] * torch.exp(lp) * off
+    if entropy:
+        size = size + e.abs().to(F64)[:, None] * torch.exp(lp) * (lp.abs() + h[:, None] + 1) * off
+    size = torch.where(none[:, None], torch.zeros_like(c), size + 4 * U * c.abs())
+    most = float((a.abs() + (18 * e.abs() if entropy else 0)).max())
+    part = 2.0 ** -11 if t != "f32" else 2.0 ** -21               # of c, and of w where it has two parts
+    small = 2.0 ** -38 * most                                     # what binary16 has no bits for, of the scaled c
+    sums = (3 * max(T, V) / 16 + 64) * U
+    if dx is not None:
+        assert (dx[:, H:] == 5.0).all()
+        want = c @ w
+        tol = (size + (part + sums) * c.abs() + small) @ w.abs() + HALF_ULP[t] * 1.01 * want.abs() + (2.0 ** -24 if t == "f16" else 0.0)
+        got = dx[:, :H].cpu().to(F64)
+        assert ((got - want).abs() <= tol).all(), float(((got - want).abs() / tol).max())
+        assert (got[none] == 0).all()
+    if dw is not None:
+        assert (dw[:, H:] == 3.0).all()
+        want = c.t() @ x + (3.0 if accumulate else 0.0)
+        tol = (size + (2.0 ** -21 + sums) * c.abs() + small).t() @ x.abs() + 2 * U * want.abs()
+        got = dw[:, :H].cpu().to(F64)
+        assert ((got - want).abs() <= tol).all(), float(((got - want).abs() / tol).max())
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,V,H,pad", SHAPES)
+@pytest.mark.parametrize("entropy", [False, True])
+def test_grad(t, T, V, H, pad, entropy):
+    check_grad(t, T, V, H, pad, entropy=entropy, ignored=0.3 if T > 2 else 0.0)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("wants", ["x", "w"])
+def test_grad_of_one_side(t, wants):
+    check_grad(t, 77, 301, 96, wants=wants, accumulate=wants == "w", entropy=True)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_grad_accumulates_and_begins_anywhere(t):
+    check_grad(t, 70, 200, 96, lead=1, accumulate=True)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_grad_in_large_tiles(t):
+    check_grad(t, 2101, 6101, 64, ignored=0.1)
+
+
+def test_rows_of_padding_hold_anything():
+    """Rows without target and without weight: NaN and infinities in x, statistics of NaN; every other number is as without them."""
+    gen = gen_of("padding")
+    T, V, H = 200, 600, 96
+    layer, x, xd, w, wd, y = layer_of(gen, T, V, H, "bf16")
+    st, h = (v.float().to(DEV) for v in ref.score(x, w, y)[3:1:-1])
+    a, e = torch.rand(T, device=DEV), torch.rand(T, device=DEV)
+    none = torch.arange(T) % 3 == 0
+    y[none], e[none.to(DEV)] = -1, 0.0
+    got = []
+    for junk in (0.0, math.nan, math.inf, 3e38):
+        xj, stj = xd.clone(), st.clone()
+        xj[none.to(DEV)] = junk
+        stj[none.to(DEV)] = math.nan if junk else 0.0
+        dx, dw = torch.full((T, H), 5.0, dtype=torch.bfloat16, device=DEV), torch.full((V, H), 5.0, device=DEV)
+        qa.qa_output_logprob_grad(layer, qa.QA_BF16, xj, wd, y.to(torch.int32).to(DEV), stj, h, a, e, dx, H, dw, H, 0, room(layer, qa.QA_OP_LOGPROB_GRAD, "bf16"))
+        assert (dx[none.to(DEV)] == 0).all()
+        got.append((dx, dw))
+    assert bool(torch.isfinite(got[0][1]).all())
+    for dx, dw in got[1:]:
+        assert torch.equal(dx, got[0][0]) and torch.equal(dw, got[0][1])
+
+
+def test_a_row_that_is_not_finite_spoils_its_own_numbers_alone():
+    gen = gen_of("nan")
+    layer, x, xd, w, wd, y = layer_of(gen, 70, 300, 64, "bf16")
+    clean = score(layer, xd, wd, y, "bf16")
+    for bad in (math.nan, math.inf):
+        xb = xd.clone()
+        xb[33, 5] = bad
+        lp, h, st = score(layer, xb, wd, y, "bf16")
+        others = torch.arange(70) != 33
+        assert math.isnan(float(lp[33])) and math.isnan(float(h[33])) and math.isnan(float(st[33, 1]))
+        for a, b in zip((lp, h, st), clean):
+            assert torch.equal(a[others], b[others])
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** 60])
+def test_binary32_of_any_size(scale):
+    """x small by as much as w is large: the logits are the same to the bit, as scales are powers of two."""
+    gen = gen_of("sizes")
+    layer, x, xd, w, wd, y = layer_of(gen, 40, 200, 50, "f32")
+    a, b = score(layer, xd, wd, y, "f32"), score(layer, xd * scale, wd / scale, y, "f32")
+    assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_targets_outside_the_vocabulary_and_outputs_left_out():
+    gen = gen_of("outside")
+    layer, x, xd, w, wd, y = layer_of(gen, 20, 100, 32, "f16")
+    full = score(layer, xd, wd, y, "f16")
+    y2 = y.clone()
+    y2[3], y2[4], y2[5] = 100, -7, 2 ** 31 - 1
+    lp, h, st = score(layer, xd, wd, y2, "f16")
+    assert (lp[3:6] == 0).all() and torch.equal(h, full[1]) and torch.equal(st, full[2])
+    only = torch.empty(20, device=DEV)
+    ws = room(layer, qa.QA_OP_LOGPROB, "f16")
+    qa.qa_output_logprob(layer, qa.QA_F16, xd, wd, None, None, only, None, ws)
+    assert torch.equal(only.cpu().to(F64), h)
+    qa.qa_output_logprob(layer, qa.QA_F16, xd, wd, y.to(torch.int32).to(DEV), only, None, None, ws)
+    assert torch.equal(only.cpu().to(F64), full[0])
+
+
+def test_no_rows():
+    layer = qa.OutputLayer.make(0, 50, 32)
+    w = torch.zeros(50, 32, device=DEV)
+    dw = torch.full((50, 40), 3.0, device=DEV)
+    qa.qa_output_logprob(layer, qa.QA_F32, None, w, None, None, None, None, None)
+    qa.qa_output_logprob_grad(layer, qa.QA_F32, None, w, None, None, None, None, None, None, 32, dw, 40, 1, None)
+    assert (dw == 3.0).all()
+    qa.qa_output_logprob_grad(layer, qa.QA_F32, None, w, None, None, None, None, None, None, 32, dw, 40, 0, None)
+    assert (dw[:, :32] == 0).all() and (dw[:, 32:] == 3.0).all()
+
+
+def test_the_gradient_is_the_slope_of_the_loss():
+    """Central differences in 64 bits of sum(a log p + e H) over single elements, step d: off by d^2 / 6 of a third derivative of the
+    gradient's own order, plus the gradient's rounding (dz and parts of 2^-21, of numbers below 3)."""
+    gen = gen_of("slope")
+    T, V, H, d = 4, 9, 6, 1e-4
+    layer, x, xd, w, wd, y = layer_of(gen, T, V, H, "f32")
+    y[2] = -1
+    a, e = torch.randn(T, generator=gen), 0.5 * torch.randn(T, generator=gen)
+    _, _, h, st = ref.score(x, w, y)
+    dx, dw = torch.empty(T, H, device=DEV), torch.empty(V, H, device=DEV)
+    qa.qa_output_logprob_grad(layer, qa.QA_F32, xd, wd, y.to(torch.int32).to(DEV), st.float().to(DEV), h.float().to(DEV), a.to(DEV), e.to(DEV), dx, H, dw, H, 0,
+                              room(layer, qa.QA_OP_LOGPROB_GRAD, "f32"))
+
+    def loss(x, w):
+        _, lp, h, _ = ref.score(x, w, y)
+        return float((a.to(F64) * lp + e.to(F64) * h).sum())
+    for v, got in ((x, dx), (w, dw)):
+        for i in range(v.numel()):
+            keep = float(v.view(-1)[i])
+            v.view(-1)[i] = keep + d
+            up = loss(x, w)
+            v.view(-1)[i] = keep - d
+            down = loss(x, w)
+            v.view(-1)[i] = keep
+            assert abs((up - down) / (2 * d) - float(got.view(-1)[i])) < 3e-5
