@@ -26,8 +26,8 @@ struct SourceArgs {
   const void* g;
   float* momentum;                                 // NULL: none
   double* partial;                                 // [matrix][norm_blocks]: sums of squares
-  _Float16 *rm, *tr;                               // hi of the matrix as it lies, and of its transpose
-  int64_t rm_ld, tr_ld, rm_part, tr_part, rm_batch, tr_batch;
+  _Float16* x;                                     // X in parts
+  int64_t ld, batch;
   float mu;
   int nesterov, norm_blocks, lanes;                // lanes: threads side by side along a row, a power of two
 };
@@ -68,11 +68,12 @@ __global__ __launch_bounds__(kThreads) void orthogonal_norm_kernel(SourceArgs A)
   if (threadIdx.x == 0) A.partial[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-// Tiles of 64 x 64, as they lie and transposed by way of LDS; rows are filled with zeros up to a whole step of k.
-template <int TYPE>
+// X = u / |u| in parts, the shorter side along its rows: tiles of 64 x 64, turned by way of LDS for a TALL matrix.  Rows and columns are
+// filled with zeros up to a whole step.
+template <int TYPE, bool TALL>
 __global__ __launch_bounds__(kThreads) void orthogonal_parts_kernel(SourceArgs A) {
   constexpr int kSide = 64;
-  __shared__ uint32_t tile[kSide][kSide + 1];
+  __shared__ float tile[TALL ? kSide : 1][kSide + 1];
   __shared__ double sums[kWaves];
   const int64_t z = blockIdx.z, r0 = (int64_t)blockIdx.y * kSide, c0 = (int64_t)blockIdx.x * kSide, base = z * A.M.matrix_stride;
   const double part = wave_sum_f64((int)threadIdx.x < A.norm_blocks ? A.partial[z * A.norm_blocks + threadIdx.x] : 0.0);
@@ -81,6 +82,7 @@ __global__ __launch_bounds__(kThreads) void orthogonal_parts_kernel(SourceArgs A
   const double all = (sums[0] + sums[1]) + (sums[2] + sums[3]);
   // A matrix of zeros stays one; one with an infinity or a NaN has no direction.
   const double scale = all == 0.0 ? 0.0 : __builtin_isfinite(all) ? (double)kUnit / __builtin_sqrt(all) : (double)__builtin_nanf("");
+  const int64_t x_rows = whole(TALL ? A.M.cols : A.M.rows, kPartsStep), x_cols = A.ld / 2;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int row = h * 32 + (int)threadIdx.x / 8, col = (int)threadIdx.x % 8 * kVec;
@@ -88,154 +90,116 @@ __global__ __launch_bounds__(kThreads) void orthogonal_parts_kernel(SourceArgs A
     const int n = r < A.M.rows ? (int)max((int64_t)0, min((int64_t)kVec, A.M.cols - c)) : 0;
     float v[kVec] = {};
     if (n) source8<TYPE, false>(A, base + r * A.M.stride + c, n, v);
-    _Float16 hi[kVec], lo[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      split_f16(i < n ? (float)((double)v[i] * scale) : 0.0f, hi[i], lo[i]);
-      tile[row][col + i] = (uint32_t)__builtin_bit_cast(uint16_t, hi[i]) | (uint32_t)__builtin_bit_cast(uint16_t, lo[i]) << 16;
+      v[i] = i < n ? (float)((double)v[i] * scale) : 0.0f;
+      if (TALL) tile[row][col + i] = v[i];
     }
-    if (r < A.M.rows && c < A.rm_ld) {
-      _Float16* p = A.rm + z * A.rm_batch + r * A.rm_ld + c;
-      __builtin_memcpy(__builtin_assume_aligned(p, 16), hi, sizeof hi);
-      __builtin_memcpy(__builtin_assume_aligned(p + A.rm_part, 16), lo, sizeof lo);
-    }
+    if (!TALL && r < x_rows && c < x_cols) put_parts(A.x + z * A.batch + r * A.ld + 2 * c, v);
   }
-  __syncthreads();
+  if constexpr (TALL) {
+    __syncthreads();
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int col = h * 32 + (int)threadIdx.x / 8, row = (int)threadIdx.x % 8 * kVec;
-    const int64_t c = c0 + col, r = r0 + row;
-    if (c >= A.M.cols || r >= A.tr_ld) continue;
-    u32x4 hi, lo;
+    for (int h = 0; h < 2; ++h) {
+      const int col = h * 32 + (int)threadIdx.x / 8, row = (int)threadIdx.x % 8 * kVec;
+      const int64_t c = c0 + col, r = r0 + row;
+      float v[kVec];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t u = tile[row + 2 * i][col], v = tile[row + 2 * i + 1][col];
-      hi[i] = __builtin_amdgcn_perm(v, u, 0x05040100u);
-      lo[i] = __builtin_amdgcn_perm(v, u, 0x07060302u);
+      for (int i = 0; i < kVec; ++i) v[i] = tile[row + i][col];
+      if (c < x_rows && r < x_cols) put_parts(A.x + z * A.batch + c * A.ld + 2 * r, v);
     }
-    _Float16* p = A.tr + z * A.tr_batch + c * A.tr_ld + r;
-    *reinterpret_cast<u32x4*>(p) = hi;
-    *reinterpret_cast<u32x4*>(p + A.tr_part) = lo;
   }
 }
 
 // ---- what becomes of a product's sums ------------------------------------------------------------------------------------
 
-// A matrix in parts: rows of `ld` elements, zeros behind `cols`.
+// A matrix in parts; rows of `ld` elements, two per number.
 struct Parts {
   _Float16* p;
-  int64_t ld, part, batch, rows, cols;
-  __device__ __forceinline__ _Float16* at(int64_t row, int64_t col) const { return p + (int64_t)blockIdx.z * batch + row * ld + col; }
-  // Four numbers of a row.
-  __device__ __forceinline__ void get4(int64_t row, int64_t col, float (&v)[4]) const {
-    const f16x4 hi = *reinterpret_cast<const f16x4*>(at(row, col)), lo = *reinterpret_cast<const f16x4*>(at(row, col) + part);
+  int64_t ld, batch, rows, cols;
+  __device__ __forceinline__ _Float16* at(int64_t row, int64_t col) const { return p + (int64_t)blockIdx.z * batch + row * ld + 2 * col; }
+  // Eight numbers of a row; zeros behind its end.
+  __device__ __forceinline__ void put(int64_t row, int64_t col, const float (&v)[kVec]) const {
+    float w[kVec];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)hi[e] + (float)lo[e];
+    for (int e = 0; e < kVec; ++e) w[e] = col + e < cols ? v[e] : 0.0f;
+    put_parts(at(row, col), w);
   }
+  __device__ __forceinline__ bool holds(int64_t row, int64_t col) const { return row < rows && 2 * col < ld; }
 };
 
-// Calls each(row, column, sums of four rows) for all that a lane holds.
-template <class P, class Each>
-__device__ __forceinline__ void for_all(P& p, int64_t m0, int64_t n0, const Each& each) {
-  const int lane = threadIdx.x % kWave;
-#pragma unroll
-  for (int i = 0; i < (int)(sizeof p.acc / sizeof p.acc[0]); ++i)
-#pragma unroll
-    for (int j = 0; j < (int)(sizeof p.acc[0] / sizeof p.acc[0][0]); ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = p.acc[i][j][4 * q + e];
-        each(m0 + 32 * i + 8 * q + 4 * (lane / 32), n0 + 32 * j + lane % 32, v);
-      }
-}
-
-// C and its transpose: t's row is C's column.  c.p NULL: the transpose alone.
-__device__ __forceinline__ void put_parts(const Parts& c, const Parts& t, int64_t row, int64_t col, float (&v)[4], bool both) {
-  if (col >= t.rows && col >= c.ld) return;
-  f16x4 hi, lo;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    _Float16 h, l;
-    split_f16(row + e < t.cols && col < t.rows ? v[e] : 0.0f, h, l);
-    hi[e] = h;
-    lo[e] = l;
-  }
-  if (col < t.rows && row < t.ld) {
-    *reinterpret_cast<f16x4*>(t.at(col, row)) = hi;
-    *reinterpret_cast<f16x4*>(t.at(col, row) + t.part) = lo;
-  }
-  if (both && col < c.ld) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (row + e < c.rows) {
-        *c.at(row + e, col) = hi[e];
-        c.at(row + e, col)[c.part] = lo[e];
-      }
-  }
-}
-
-// A = X X^T, tiles on and below the diagonal; the others are their transposes.
-struct GramOut {
-  Parts a;
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0) const {
-    const bool both = m0 / P::kM != n0 / P::kN;
-    for_all(p, m0, n0, [&](int64_t row, int64_t col, float (&v)[4]) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = v[e] * (1.0f / kUnit);
-      put_parts(a, a, row, col, v, both);
-    });
-  }
-};
-// B = b A + c A A, the same way.
-struct SquareOut {
-  Parts a, b;
+// A = X X^T or B = b A + c A A, tiles on and below the diagonal; the others are their transposes.  p's rows are the products' columns:
+// a lane has eight numbers of one row, and the transpose goes by way of LDS.
+template <bool SQUARE>
+struct SymmetricOut {
+  Parts to, a;
   float cb, cc;
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0) const {
+  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
     const bool both = m0 / P::kM != n0 / P::kN;
-    for_all(p, m0, n0, [&](int64_t row, int64_t col, float (&v)[4]) {
-      float x[4] = {};
-      if (col < a.rows && row < a.ld) a.get4(col, row, x);
+    const Turned turned = {(float*)lds};
+    p.for_eights(m0, n0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
+      float x[kVec] = {};
+      if (SQUARE && a.holds(j, i)) get_parts(a.at(j, i), x);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = cb * x[e] + (cc / kUnit) * v[e];
-      put_parts(b, b, row, col, v, both);
+      for (int e = 0; e < kVec; ++e) v[e] = SQUARE ? cb * x[e] + (cc / kUnit) * v[e] : v[e] * (1.0f / kUnit);
+      if (to.holds(j, i)) to.put(j, i, v);
+      if (both) turned.put(i, v);
+    }, [&](int64_t i0, int64_t j0) {
+      if (both) turned.take(i0, j0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
+        if (to.holds(i, j)) to.put(i, j, v);
+      });
     });
   }
 };
-// X' = a X + B X and its transpose.
+// X' = a X + B X, with rows of zeros up to a whole step.
 struct NextOut {
-  Parts x_t, c, t;                                 // X^T; X' and X'^T
+  Parts x, to;
   float ca;
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0) const {
-    for_all(p, m0, n0, [&](int64_t row, int64_t col, float (&v)[4]) {
-      float x[4] = {};
-      if (col < x_t.rows && row < x_t.ld) x_t.get4(col, row, x);
+  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char*) const {
+    p.for_eights(m0, n0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
+      if (j >= whole(to.rows, kPartsStep) || 2 * i >= to.ld) return;
+      float o[kVec] = {};
+      if (j < to.rows) get_parts(x.at(j, i), o);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = ca * x[e] + v[e] * (1.0f / kUnit);
-      put_parts(c, t, row, col, v, true);
+      for (int e = 0; e < kVec; ++e) o[e] = j < to.rows ? ca * o[e] + v[e] * (1.0f / kUnit) : 0.0f;
+      to.put(j, i, o);
     });
   }
 };
-// The last X', rounded once, or the parameters stepped with it: rows are those of the caller's matrix.
-template <int TYPE, bool STEP>
+// The last X', rounded once, or the parameters stepped with it.
+template <int TYPE, bool STEP, bool TALL>
 struct LastOut {
-  Parts x_t;                                       // transpose of X in the caller's rows
+  Parts x;
   ElemT<TYPE>* out;
   int64_t stride, matrix_stride;
   float ca, eta, shrink;
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0) const {
-    for_all(p, m0, n0, [&](int64_t row, int64_t col, float (&v)[4]) {
-      if (col >= x_t.rows || row >= x_t.cols) return;
-      float x[4];
-      x_t.get4(col, row, x);
-      ElemT<TYPE>* at = out + (int64_t)blockIdx.z * matrix_stride + row * stride + col;
+  __device__ __forceinline__ void put(int64_t row, int64_t col, int64_t cols, const float (&o)[kVec]) const {
+    ElemT<TYPE>* at = out + (int64_t)blockIdx.z * matrix_stride + row * stride + col;
+    const int n = (int)min((int64_t)kVec, cols - col);
+    if constexpr (STEP) {
+      float w[kVec];
+      to_f32<TYPE>(load_raw<TYPE>(at, n), w);
 #pragma unroll
-      for (int e = 0; e < 4; ++e, at += stride) {
-        if (row + e >= x_t.cols) break;
-        const float o = (ca * x[e] + v[e] * (1.0f / kUnit)) * (1.0f / kUnit);
-        *at = STEP ? (ElemT<TYPE>)(shrink * (float)*at - eta * o) : (ElemT<TYPE>)o;
-      }
+      for (int e = 0; e < kVec; ++e) w[e] = shrink * w[e] - eta * o[e];
+      store_raw<TYPE>(at, from_f32<TYPE>(w), n);
+    } else {
+      store_raw<TYPE>(at, from_f32<TYPE>(o), n);
+    }
+  }
+  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
+    const Turned turned = {(float*)lds};
+    p.for_eights(m0, n0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
+      float o[kVec] = {};
+      const bool holds = j < x.rows && i < x.cols;
+      if (holds) get_parts(x.at(j, i), o);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) o[e] = (ca * o[e] + v[e] * (1.0f / kUnit)) * (1.0f / kUnit);
+      if (TALL) turned.put(i, o);
+      else if (holds) put(j, i, x.cols, o);
+    }, [&](int64_t i0, int64_t j0) {
+      if (TALL) turned.take(i0, j0, [&](int64_t i, int64_t j, float (&o)[kVec]) {
+        if (i < x.cols && j < x.rows) put(i, j, x.rows, o);
+      });
     });
   }
 };
@@ -243,102 +207,82 @@ struct LastOut {
 // ---- the steps ---------------------------------------------------------------------------------------------------------------
 
 struct Plan {
-  int64_t n, m, np, mp;                            // sides, and their rows' lengths: whole steps of k
-  bool tall;                                       // the caller's rows are the longer side
-  size_t x, xt, a, norms, bytes;                   // of one buffer (both parts, all matrices), and of everything
+  int64_t n, m, np, mp;                            // sides, and with whole steps
+  size_t x, a, norms, bytes;                       // of one buffer for all matrices, and of everything
 };
 Plan plan_of(const qa_matrices& M) {
   Plan P;
-  P.tall = M.rows > M.cols;
   P.n = std::min(M.rows, M.cols);
   P.m = std::max(M.rows, M.cols);
-  P.np = ceil_div(P.n, kProductStep) * kProductStep;
-  P.mp = ceil_div(P.m, kProductStep) * kProductStep;
-  const auto room = [&](int64_t elements) { return ((size_t)(M.count * elements) * 2 + 255) / 256 * 256; };
-  P.x = room(2 * P.n * P.mp);
-  P.xt = room(2 * P.m * P.np);
-  P.a = room(2 * P.n * P.np);
-  P.norms = ((size_t)M.count * kNormBlocks * 8 + 255) / 256 * 256;
-  P.bytes = 2 * P.x + 2 * P.xt + 2 * P.a + P.norms;
+  P.np = whole(P.n, kPartsStep);
+  P.mp = whole(P.m, kPartsStep);
+  P.x = (size_t)whole(M.count * P.np * 2 * P.mp * 2, 256);
+  P.a = (size_t)whole(M.count * P.n * 2 * P.np * 2, 256);
+  P.norms = (size_t)whole(M.count * kNormBlocks * 8, 256);
+  P.bytes = 2 * P.x + 2 * P.a + P.norms;
   return P;
 }
 
-template <bool LOWER, class Epilogue>
+template <Lies LA, Lies LB, bool LOWER, class Epilogue>
 int multiply(const Parts& a, const Parts& b, int64_t k, int64_t count, const Epilogue& out, hipStream_t stream) {
-  ProductArgs A = {};
-  A.a = (const uint16_t*)a.p;
-  A.b = (const uint16_t*)b.p;
-  A.lda = a.ld;
-  A.ldb = b.ld;
-  A.a_part = a.part;
-  A.b_part = b.part;
-  A.a_batch = a.batch;
-  A.b_batch = b.batch;
-  A.m = a.rows;
-  A.n = b.rows;
-  A.steps = (int)(k / kProductStep);
+  const Operand oa = {a.p, a.ld, a.batch, in_rows(LA) ? a.rows : a.cols}, ob = {b.p, b.ld, b.batch, in_rows(LB) ? b.rows : b.cols};
   const auto tiles = [&](int64_t side) {
-    const int64_t tm = ceil_div(A.m, side), tn = ceil_div(A.n, side);
+    const int64_t tm = ceil_div(oa.n, side), tn = ceil_div(ob.n, side);
     return count * (LOWER ? tm * (tm + 1) / 2 : tm * tn);
   };
-  if (tiles(256) >= 192) return product_launch<false, 3, 2, 4, 4, 2, LOWER>(A, out, 1, (unsigned)count, stream);
-  if (tiles(128) >= 128) return product_launch<false, 3, 2, 2, 2, 2, LOWER>(A, out, 1, (unsigned)count, stream);
-  return product_launch<false, 3, 2, 2, 1, 1, LOWER>(A, out, 1, (unsigned)count, stream);
+  if (tiles(256) >= 192) return product_launch<Product256<false, LA, LB>, LOWER>(oa, ob, k, out, (unsigned)count, stream);
+  if (tiles(128) >= 128) return product_launch<Product128<false, LA, LB>, LOWER>(oa, ob, k, out, (unsigned)count, stream);
+  return product_launch<Product64<false, LA, LB>, LOWER>(oa, ob, k, out, (unsigned)count, stream);
 }
 
-template <int TYPE, bool STEP>
+template <int TYPE, bool STEP, bool TALL>
 int orthogonal_launch(const qa_matrices& M, const void* g, float* momentum, void* out, float mu, int nesterov, int steps,
                       const float* coefficients, float eta, float shrink, char* ws, hipStream_t stream) {
   const Plan P = plan_of(M);
-  const auto parts = [&](size_t at, int64_t rows, int64_t cols, int64_t ld) {
-    return Parts{(_Float16*)(ws + at), ld, M.count * rows * ld, rows * ld, rows, cols};
-  };
-  Parts x[2], xt[2];
+  Parts x[2], ab[2];
   for (int i = 0; i < 2; ++i) {
-    x[i] = parts((size_t)i * P.x, P.n, P.m, P.mp);
-    xt[i] = parts(2 * P.x + (size_t)i * P.xt, P.m, P.n, P.np);
+    x[i] = {(_Float16*)(ws + i * P.x), 2 * P.mp, P.np * 2 * P.mp, P.n, P.m};
+    ab[i] = {(_Float16*)(ws + 2 * P.x + i * P.a), 2 * P.np, P.n * 2 * P.np, P.n, P.n};
   }
-  const Parts a = parts(2 * (P.x + P.xt), P.n, P.n, P.np), b = parts(2 * (P.x + P.xt) + P.a, P.n, P.n, P.np);
-  const Parts &rm = P.tall ? xt[0] : x[0], &tr = P.tall ? x[0] : xt[0];
+  const Parts &a = ab[0], &b = ab[1];
 
   SourceArgs S = {};
   S.M = M;
   S.g = g;
   S.momentum = momentum;
-  S.partial = (double*)(ws + 2 * (P.x + P.xt + P.a));
-  S.rm = rm.p;
-  S.tr = tr.p;
-  S.rm_ld = rm.ld;
-  S.tr_ld = tr.ld;
-  S.rm_part = rm.part;
-  S.tr_part = tr.part;
-  S.rm_batch = rm.batch;
-  S.tr_batch = tr.batch;
+  S.partial = (double*)(ws + 2 * P.x + 2 * P.a);
+  S.x = x[0].p;
+  S.ld = x[0].ld;
+  S.batch = x[0].batch;
   S.mu = mu;
   S.nesterov = nesterov;
   S.lanes = 1;
   while (S.lanes < kThreads && S.lanes * kVec < M.cols) S.lanes *= 2;
   S.norm_blocks = (int)std::min<int64_t>(kNormBlocks, ceil_div(M.rows * S.lanes, kThreads));
   orthogonal_norm_kernel<TYPE><<<dim3(S.norm_blocks, (unsigned)M.count), kThreads, 0, stream>>>(S);
-  orthogonal_parts_kernel<TYPE><<<dim3((unsigned)ceil_div(M.cols, 64), (unsigned)ceil_div(M.rows, 64), (unsigned)M.count), kThreads, 0, stream>>>(S);
+  orthogonal_parts_kernel<TYPE, TALL><<<dim3((unsigned)ceil_div(M.cols, 64), (unsigned)ceil_div(M.rows, 64), (unsigned)M.count), kThreads, 0, stream>>>(S);
   if (const int rc = launch_status()) return rc;
 
   constexpr float usual[3] = {3.4445f, -4.7750f, 2.0315f};
   for (int s = 0, now = 0; s < steps; ++s, now ^= 1) {
     const float* c = coefficients ? coefficients + 3 * s : usual;
-    if (const int rc = multiply<true>(x[now], x[now], P.mp, M.count, GramOut{a}, stream)) return rc;
-    if (const int rc = multiply<true>(a, a, P.np, M.count, SquareOut{a, b, c[1], c[2]}, stream)) return rc;
+    if (const int rc = multiply<kRowsOfParts, kRowsOfParts, true>(x[now], x[now], P.m, M.count, SymmetricOut<false>{a, a, 0.0f, 0.0f}, stream)) return rc;
+    if (const int rc = multiply<kRowsOfParts, kRowsOfParts, true>(a, a, P.n, M.count, SymmetricOut<true>{b, a, c[1], c[2]}, stream)) return rc;
     int rc;
-    if (s + 1 < steps) {
-      rc = multiply<false>(b, xt[now], P.np, M.count, NextOut{xt[now], x[now ^ 1], xt[now ^ 1], c[0]}, stream);
-    } else {
-      const Parts& back = P.tall ? x[now] : xt[now];
-      const LastOut<TYPE, STEP> last{back, (ElemT<TYPE>*)out, M.stride, M.matrix_stride, c[0], eta, shrink};
-      rc = P.tall ? multiply<false>(xt[now], b, P.np, M.count, last, stream) : multiply<false>(b, xt[now], P.np, M.count, last, stream);
-    }
+    if (s + 1 < steps)
+      rc = multiply<kColumnsOfParts, kRowsOfParts, false>(x[now], b, P.n, M.count, NextOut{x[now], x[now ^ 1], c[0]}, stream);
+    else
+      rc = multiply<kColumnsOfParts, kRowsOfParts, false>(
+          x[now], b, P.n, M.count, LastOut<TYPE, STEP, TALL>{x[now], (ElemT<TYPE>*)out, M.stride, M.matrix_stride, c[0], eta, shrink}, stream);
     if (rc) return rc;
   }
   return QA_OK;
+}
+template <int TYPE, bool STEP>
+int orthogonal(const qa_matrices& M, const void* g, float* momentum, void* out, float mu, int nesterov, int steps, const float* coefficients,
+               float eta, float shrink, void* ws, void* stream) {
+  const auto launch = M.rows > M.cols ? orthogonal_launch<TYPE, STEP, true> : orthogonal_launch<TYPE, STEP, false>;
+  return launch(M, g, momentum, out, mu, nesterov, steps, coefficients, eta, shrink, (char*)ws, (hipStream_t)stream);
 }
 
 int check_matrices(const qa_matrices* M) {
@@ -379,8 +323,8 @@ extern "C" int qa_orthogonalize(const qa_matrices* matrices, int type, const voi
   if (!g || !out) return QA_ERR_INVALID_ARG;
   if (!element_aligned(g, type) || !element_aligned(out, type)) return QA_ERR_ALIGNMENT;
   if (const int rc = check_workspace(matrices, ws, ws_bytes)) return rc;
-  const auto launch = type == QA_F32 ? orthogonal_launch<QA_F32, false> : type == QA_BF16 ? orthogonal_launch<QA_BF16, false> : orthogonal_launch<QA_F16, false>;
-  return launch(*matrices, g, nullptr, out, 0.0f, 0, steps, coefficients, 0.0f, 0.0f, (char*)ws, (hipStream_t)stream);
+  const auto launch = type == QA_F32 ? orthogonal<QA_F32, false> : type == QA_BF16 ? orthogonal<QA_BF16, false> : orthogonal<QA_F16, false>;
+  return launch(*matrices, g, nullptr, out, 0.0f, 0, steps, coefficients, 0.0f, 0.0f, ws, stream);
 }
 
 extern "C" int qa_step_orthogonal(const qa_matrices* matrices, const float* g, float* momentum, float* x, float mu, int nesterov,
@@ -393,5 +337,5 @@ extern "C" int qa_step_orthogonal(const qa_matrices* matrices, const float* g, f
   if (!g || !x) return QA_ERR_INVALID_ARG;
   if (!aligned(g, 4) || !aligned(momentum, 4) || !aligned(x, 4)) return QA_ERR_ALIGNMENT;
   if (const int rc = check_workspace(matrices, ws, ws_bytes)) return rc;
-  return orthogonal_launch<QA_F32, true>(*matrices, g, momentum, x, mu, nesterov, steps, coefficients, eta, shrink, (char*)ws, (hipStream_t)stream);
+  return orthogonal<QA_F32, true>(*matrices, g, momentum, x, mu, nesterov, steps, coefficients, eta, shrink, ws, stream);
 }

@@ -3,8 +3,7 @@
 // Logits are products of the matrix cores with rows of w along the tile's height and rows of x along its width, so that a lane holds
 // many logits of one row: a tile's maximum and sums are formed in registers, and a row's numbers are joined from one triple per
 // chunk of the vocabulary.  The backward pass multiplies the logits again, a piece of the vocabulary at a time, turns them into
-// c, the gradient of the logits, which is written in binary16 parts along the vocabulary (for dx = c w) and along the rows
-// (for dw = c^T x), and multiplies those with transposes of w's piece and of x.
+// c, the gradient of the logits, which is written once, as rows of binary16 parts, and multiplies that from both sides: dx = c w, dw = c^T x.
 #include <algorithm>
 
 #include "qa_product.h"
@@ -35,40 +34,77 @@ __device__ __forceinline__ int exponent_for(uint32_t most) {
   return most == 0 ? 0 : min(126, max(-126, 14 - ((int)(max(most, 0x00800000u) >> 23) - 127)));
 }
 
-// Rows copied to whole steps of k: 16-bit elements as they are, binary32 ones in two parts times a power of two per row.  A wave per row.
-template <int TYPE>
-__global__ __launch_bounds__(kThreads) void output_rows_kernel(const void* from, int64_t stride, int64_t rows, int64_t cols, uint16_t* to,
-                                                               int64_t ld, int64_t part, int* exps) {
-  const int64_t row = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+struct RowArgs {
+  const int32_t* target;
+  const float *stats, *entropy, *g_logprob, *g_entropy;
+  int64_t vocab;
+};
+struct Row { float m, log_sum, h, a, e; int64_t at; };
+__device__ __forceinline__ Row row_of(const RowArgs& A, int64_t t) {
+  Row r;
+  r.m = fmaxf(A.stats[2 * t], -FLT_MAX);
+  r.log_sum = A.stats[2 * t + 1];
+  const int64_t y = A.target ? A.target[t] : -1;
+  r.at = y < 0 || y >= A.vocab ? -1 : y;
+  r.a = A.g_logprob && r.at >= 0 ? A.g_logprob[t] : 0.0f;
+  r.e = A.g_entropy ? A.g_entropy[t] : 0.0f;
+  r.h = A.g_entropy ? A.entropy[t] : 0.0f;
+  return r;
+}
+__device__ __forceinline__ bool counts(const Row& r) { return r.a != 0.0f || r.e != 0.0f; }
+
+// Largest magnitudes (bits) that the powers of two follow by which the gradient's operands are scaled.
+struct Scales { uint32_t most[4]; };
+enum { kOfC, kOfX, kOfW };
+
+struct CopyArgs {
+  const void* from;
+  int64_t stride, rows, cols;
+  void* to;
+  int64_t ld, to_rows;                             // zeros up to ld / parts columns, and in rows from `rows` on
+  int* exps;                                       // kOwnScale: written
+  const Scales* scales;                            // kOneScale
+  int which;
+  bool masked;                                     // zeros in rows that do not count
+  RowArgs R;
+};
+// Rows copied, a wave per row: 16-bit elements as they are, or binary16 (binary32 elements: in two parts) times a power of two per row
+// or per matrix.
+enum Copies { kAsTheyAre, kOwnScale, kOneScale };
+template <int TYPE, Copies HOW>
+__global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
+  constexpr int kParts = TYPE == QA_F32 ? 2 : 1;
   const int lane = threadIdx.x % kWave;
-  if (row >= rows) return;
-  const ElemT<TYPE>* p = (const ElemT<TYPE>*)from + row * stride;
-  uint16_t* q = to + row * ld;
-  if constexpr (TYPE != QA_F32) {
-    for (int64_t c = lane * kVec; c < ld; c += kWave * kVec) {
-      const int n = (int)max((int64_t)0, min((int64_t)kVec, cols - c));
-      *reinterpret_cast<u32x4*>(q + c) = n ? load_raw<TYPE>(p + c, n).a : u32x4{};
-    }
-  } else {
-    uint32_t most = 0;
-    for (int64_t c = lane * kVec; c < cols; c += kWave * kVec) {
-      float v[kVec];
-      to_f32<TYPE>(load_raw<TYPE>(p + c, (int)min((int64_t)kVec, cols - c)), v);
-      most = max(most, finite_most(v));
-    }
+  for (int64_t row = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; row < A.to_rows; row += (int64_t)gridDim.x * kWaves) {
+    const ElemT<TYPE>* p = (const ElemT<TYPE>*)A.from + row * A.stride;
+    _Float16* q = (_Float16*)A.to + row * A.ld;
+    const int64_t cols = row < A.rows && !(A.masked && !counts(row_of(A.R, row))) ? A.cols : 0;
+    int exp = 0;
+    if constexpr (HOW == kOwnScale) {
+      uint32_t most = 0;
+      for (int64_t c = lane * kVec; c < cols; c += kWave * kVec) {
+        float v[kVec];
+        to_f32<TYPE>(load_raw<TYPE>(p + c, (int)min((int64_t)kVec, cols - c)), v);
+        most = max(most, finite_most(v));
+      }
 #pragma unroll
-    for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
-    const int exp = exponent_for(most);
-    if (lane == 0) exps[row] = exp;
-    for (int64_t c = lane * kVec; c < ld; c += kWave * kVec) {
+      for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
+      exp = exponent_for(most);
+      if (lane == 0) A.exps[row] = exp;
+    }
+    if constexpr (HOW == kOneScale && TYPE != QA_F16) exp = exponent_for(A.scales->most[A.which]);
+    for (int64_t c = lane * kVec; c < A.ld / kParts; c += kWave * kVec) {
       const int n = (int)max((int64_t)0, min((int64_t)kVec, cols - c));
-      float v[kVec] = {};
-      if (n) to_f32<TYPE>(load_raw<TYPE>(p + c, n), v);
-      _Float16 hi[kVec], lo[kVec];
+      if constexpr (HOW == kAsTheyAre || TYPE == QA_F16) {
+        *reinterpret_cast<u32x4*>(q + c) = n ? load_raw<TYPE>(p + c, n).a : u32x4{};
+      } else {
+        float v[kVec] = {};
+        if (n) to_f32<TYPE>(load_raw<TYPE>(p + c, n), v);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) split_f16(i < n ? ldexpf(v[i], exp) : 0.0f, hi[i], lo[i]);
-      __builtin_memcpy(__builtin_assume_aligned(q + c, 16), hi, sizeof hi);
-      __builtin_memcpy(__builtin_assume_aligned(q + part + c, 16), lo, sizeof lo);
+        for (int i = 0; i < kVec; ++i) v[i] = ldexpf(v[i], exp);
+        if constexpr (kParts == 2) put_parts(q + 2 * c, v);
+        else *reinterpret_cast<u32x4*>(q + c) = from_f32<QA_F16>(v).a;
+      }
     }
   }
 }
@@ -106,7 +142,7 @@ template <bool SCALED>
 struct ScoreOut {
   LayerArgs L;                                     // vocab: of this launch
   ScoreArgs A;
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0) const {
+  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0, char*) const {
     constexpr int kChunk = 32 * (int)(sizeof p.acc / sizeof p.acc[0]);
     if (v0 >= L.vocab) return;
 #pragma unroll
@@ -199,30 +235,7 @@ __global__ __launch_bounds__(kThreads) void output_join_kernel(ScoreArgs A, int6
 
 // ---- the gradient of the logits -------------------------------------------------------------------------------------------
 
-// Exponents of the powers of two that the gradient's operands are scaled by, and largest magnitudes (bits) before them.
-struct Scales { uint32_t most[4]; };
-enum { kOfC, kOfX, kOfW };
-
 __global__ void output_clear_kernel(Scales* s) { s->most[threadIdx.x] = 0; }
-
-struct RowArgs {
-  const int32_t* target;
-  const float *stats, *entropy, *g_logprob, *g_entropy;
-  int64_t vocab;
-};
-struct Row { float m, log_sum, h, a, e; int64_t at; };
-__device__ __forceinline__ Row row_of(const RowArgs& A, int64_t t) {
-  Row r;
-  r.m = fmaxf(A.stats[2 * t], -FLT_MAX);
-  r.log_sum = A.stats[2 * t + 1];
-  const int64_t y = A.target ? A.target[t] : -1;
-  r.at = y < 0 || y >= A.vocab ? -1 : y;
-  r.a = A.g_logprob && r.at >= 0 ? A.g_logprob[t] : 0.0f;
-  r.e = A.g_entropy ? A.g_entropy[t] : 0.0f;
-  r.h = A.g_entropy ? A.entropy[t] : 0.0f;
-  return r;
-}
-__device__ __forceinline__ bool counts(const Row& r) { return r.a != 0.0f || r.e != 0.0f; }
 
 // The largest |c| that a row can have: p <= 1, p |log p| <= 1 / e, and an entropy of at most log 2^24 < 17.
 __global__ __launch_bounds__(kThreads) void output_weights_kernel(RowArgs A, int64_t rows, Scales* scales) {
@@ -257,133 +270,76 @@ __global__ __launch_bounds__(kThreads) void output_most_kernel(const void* from,
   if (lane == 0) atomicMax(&scales->most[which], most);
 }
 
-// Transpose of rows [0, rows) in one or two binary16 parts, scaled, with zeros up to a whole step of k and in rows that do not count.
-template <int TYPE, int PARTS>
-__global__ __launch_bounds__(kThreads) void output_transpose_kernel(const void* from, int64_t stride, int64_t rows, int64_t cols, RowArgs A, bool masked,
-                                                                    const Scales* scales, int which, _Float16* to, int64_t ld, int64_t part) {
-  constexpr int kSide = 64;
-  __shared__ uint32_t tile[kSide][kSide + 1];
-  const int64_t r0 = (int64_t)blockIdx.x * kSide, c0 = (int64_t)blockIdx.y * kSide;
-  const int exp = TYPE == QA_F16 ? 0 : exponent_for(scales->most[which]);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int row = h * 32 + (int)threadIdx.x / 8, col = (int)threadIdx.x % 8 * kVec;
-    const int64_t r = r0 + row, c = c0 + col;
-    int n = r < rows ? (int)max((int64_t)0, min((int64_t)kVec, cols - c)) : 0;
-    if (n && masked && !counts(row_of(A, r))) n = 0;
-    float v[kVec] = {};
-    if (n) to_f32<TYPE>(load_raw<TYPE>((const ElemT<TYPE>*)from + r * stride + c, n), v);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      _Float16 hi, lo;
-      split_f16(i < n ? ldexpf(v[i], exp) : 0.0f, hi, lo);
-      tile[row][col + i] = (uint32_t)__builtin_bit_cast(uint16_t, hi) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int col = h * 32 + (int)threadIdx.x / 8, row = (int)threadIdx.x % 8 * kVec;
-    const int64_t c = c0 + col, r = r0 + row;
-    if (c >= cols || r >= ld) continue;
-    u32x4 hi, lo;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t u = tile[row + 2 * i][col], v = tile[row + 2 * i + 1][col];
-      hi[i] = __builtin_amdgcn_perm(v, u, 0x05040100u);
-      lo[i] = __builtin_amdgcn_perm(v, u, 0x07060302u);
-    }
-    _Float16* p = to + c * ld + r;
-    *reinterpret_cast<u32x4*>(p) = hi;
-    if (PARTS == 2) *reinterpret_cast<u32x4*>(p + part) = lo;
-  }
-}
-
-// c of a piece of the vocabulary, scaled: along the vocabulary (C_PARTS parts, none: not wanted) and along the rows (two parts).
-template <bool SCALED, int C_PARTS, bool DW>
+// c of a piece of the vocabulary, scaled, in rows of parts: zeros behind the piece, in rows that do not count, and in rows up to a whole step.
+template <bool SCALED>
 struct LogitsGradOut {
   LayerArgs L;                                     // vocab: of this piece
   RowArgs R;
   int64_t first;                                   // of the piece
   const Scales* scales;
-  _Float16 *c, *ct;
-  int64_t c_ld, c_part, ct_ld, ct_part;            // whole steps of k: zeros behind the piece and behind the rows
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0) const {
-    const int exp = exponent_for(scales->most[kOfC]);
+  _Float16* c;
+  int64_t ld, to_rows;
+  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0, char*) const {
+    const int exp = exponent_for(scales->most[kOfC]), lane = threadIdx.x % kWave;
+    constexpr int FN = (int)(sizeof p.acc[0] / sizeof p.acc[0][0]);
+    Row r[FN];
+    int x_exp[FN], here[FN];
+    bool none[FN];
 #pragma unroll
-    for (int j = 0; j < (int)(sizeof p.acc[0] / sizeof p.acc[0][0]); ++j) {
-      const int64_t t = t0 + 32 * j + threadIdx.x % 32;
-      const int x_exp = SCALED ? L.x_exp[min(t, L.rows - 1)] : 0;
-      const Row r = row_of(R, min(t, L.rows - 1));
-      const bool none = t >= L.rows || !counts(r);
-      const int64_t at = r.at - first - v0;
-      const int here = at >= 0 && at < P::kM ? (int)at : -1, left = (int)max((int64_t)0, min((int64_t)P::kM, L.vocab - v0));
-      const int wide = (int)max((int64_t)0, min((int64_t)P::kM, c_ld - v0));
-      _Float16 *const c_row = c + t * c_ld + v0, *const ct_row = ct + v0 * ct_ld + t;
-      for_logits<SCALED>(p, L, v0, j, x_exp, [&](int v, int, int, float (&z)[4]) {
-        f16x4 hi, lo;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float lp = (z[e] - r.m) - r.log_sum, q = __builtin_amdgcn_exp2f(lp * kLog2e);
-          float g = -q * (r.a + r.e * (fmaxf(lp, kFar) + r.h));
-          if (v + e == here) g += r.a;
-          _Float16 a, b;
-          split_f16(none || v + e >= left ? 0.0f : ldexpf(g, exp), a, b);
-          hi[e] = a;
-          lo[e] = b;
-        }
-        if (C_PARTS && t < L.rows && v < wide) {
-          *reinterpret_cast<f16x4*>(c_row + v) = hi;
-          if (C_PARTS == 2) *reinterpret_cast<f16x4*>(c_row + c_part + v) = lo;
-        }
-        if (DW && t < ct_ld) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (v + e < left) {
-              ct_row[(v + e) * ct_ld] = hi[e];
-              ct_row[(v + e) * ct_ld + ct_part] = lo[e];
-            }
-        }
-      });
+    for (int j = 0; j < FN; ++j) {
+      const int64_t t = t0 + 32 * j + lane % 32;
+      r[j] = row_of(R, min(t, L.rows - 1));
+      x_exp[j] = SCALED ? L.x_exp[min(t, L.rows - 1)] : 0;
+      none[j] = t >= L.rows || !counts(r[j]);
+      const int64_t at = r[j].at - first - v0;
+      here[j] = at >= 0 && at < P::kM ? (int)at : -1;
     }
+    const int left = (int)max((int64_t)0, min((int64_t)P::kM, L.vocab - v0)), wide = (int)max((int64_t)0, min((int64_t)P::kM, ld / 2 - v0));
+    p.for_eights(0, 0, [&](int64_t i, int64_t col, float (&z)[kVec]) {
+      const int v = (int)i, j = (int)col / 32;
+      float g[kVec];
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        if (SCALED) z[e] = ldexpf(z[e], -(x_exp[j] + L.w_exp[min(v0 + v + e, L.vocab - 1)]));
+        const float lp = (z[e] - r[j].m) - r[j].log_sum, q = __builtin_amdgcn_exp2f(lp * kLog2e);
+        g[e] = -q * (r[j].a + r[j].e * (fmaxf(lp, kFar) + r[j].h));
+        if (v + e == here[j]) g[e] += r[j].a;
+        g[e] = none[j] || v + e >= left ? 0.0f : ldexpf(g[e], exp);
+      }
+      const int64_t t = t0 + col;
+      if (t < to_rows && v < wide) put_parts(c + t * ld + 2 * (v0 + v), g);
+      __builtin_amdgcn_sched_barrier(0);           // or all exponents and addresses are held in registers at once
+    });
   }
 };
 
-// Sums of a product, unscaled, rounded to the type or added in binary32.
+// Sums of a product, unscaled, rounded to the type or added in binary32; the product's columns are the rows that are written.
 template <int TYPE>
 struct GradOut {
   ElemT<TYPE>* out;
   float* sums;                                     // NULL: none before this piece, and this is the last
   const Scales* scales;
   int64_t stride, rows, cols;
-  int which;
+  int which;                                       // the scale of the other operand, -1: none
   bool add, last;                                  // to what is in sums (or, of binary32, in out); the last piece writes out
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0) const {
-    const int lane = threadIdx.x % kWave, x = which == kOfX || which == kOfW ? (int)scales->most[which] : 0;
-    const int exp = -(exponent_for(scales->most[kOfC]) + exponent_for((uint32_t)x));
+  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char*) const {
+    const int exp = -(exponent_for(scales->most[kOfC]) + (which < 0 ? 0 : exponent_for(scales->most[which])));
+    p.for_eights(m0, n0, [&](int64_t col, int64_t row, float (&v)[kVec]) {
+      if (row >= rows || col >= cols) return;
+      const int n = (int)min((int64_t)kVec, cols - col);
+      ElemT<TYPE>* const at = out + row * stride + col;
+      float* const s = sums + row * cols + col;
+      float before[kVec] = {};
+      if (add) {
+        if (sums) to_f32<QA_F32>(load_raw<QA_F32>(s, n), before);
+        else to_f32<TYPE>(load_raw<TYPE>(at, n), before);
+      }
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof p.acc / sizeof p.acc[0]); ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int64_t row = m0 + 32 * i + 8 * q + 4 * (lane / 32) + e;
-          if (row >= rows) continue;
-#pragma unroll
-          for (int j = 0; j < (int)(sizeof p.acc[0] / sizeof p.acc[0][0]); ++j) {
-            const int64_t col = n0 + 32 * j + lane % 32;
-            if (col >= cols) continue;
-            float v = ldexpf(p.acc[i][j][4 * q + e], exp);
-            if (sums) {
-              float* s = sums + row * cols + col;
-              if (add) v += *s;
-              if (!last) *s = v;
-            } else if (add) {
-              v += (float)out[row * stride + col];
-            }
-            if (last) out[row * stride + col] = (ElemT<TYPE>)v;
-          }
-        }
+      for (int e = 0; e < kVec; ++e) v[e] = before[e] + ldexpf(v[e], exp);
+      if (last) store_raw<TYPE>(at, from_f32<TYPE>(v), n);
+      else store_raw<QA_F32>(s, from_f32<QA_F32>(v), n);
+      __builtin_amdgcn_sched_barrier(0);           // or all that is added to is held in registers at once
+    });
   }
 };
 __global__ __launch_bounds__(kThreads) void output_zero_kernel(float* p, int64_t stride, int64_t rows, int64_t cols) {
@@ -393,16 +349,13 @@ __global__ __launch_bounds__(kThreads) void output_zero_kernel(float* p, int64_t
 
 // ---- what a call does ------------------------------------------------------------------------------------------------------------
 
-constexpr int64_t kPieceBytes = int64_t(256) << 20;
-
-int64_t whole_steps(int64_t k) { return ceil_div(k, kProductStep) * kProductStep; }
-int parts_for(int type) { return type == QA_F32 ? 2 : 1; }
+constexpr int64_t kPieceBytes = int64_t(512) << 20;
 
 struct Room {
   size_t bytes = 0;
   size_t take(int64_t n) {
     const size_t at = bytes;
-    bytes += ((size_t)n + 255) / 256 * 256;
+    bytes += (size_t)whole(n, 256);
     return at;
   }
 };
@@ -415,89 +368,91 @@ int logits_tiles(int64_t rows, int64_t vocab) {
 }
 constexpr int64_t chunk_of(int tiles) { return tiles == kTiles256 ? 128 : 64; }
 
+// Equal pieces of n, whole tiles each, of at most `most`.
+int64_t piece_of(int64_t n, int64_t most) { return std::min(whole(n, kWholeStep), whole(ceil_div(n, ceil_div(n, most)), 256)); }
+int64_t power_of_two_within(int64_t n, int64_t least) {
+  while (2 * least <= n) least *= 2;
+  return least;
+}
+
 struct Plan {
-  bool copy_x, copy_w;
-  int64_t hp, piece, pieces;                       // copied rows' length; vocabulary of a launch
+  bool copy_x, copy_w;                             // for the logits
+  int64_t parts, hp, piece, pieces;                // a copied row's columns; vocabulary of a launch
   int tiles;
-  size_t xs, ws, x_exp, w_exp;                     // copies and exponents
-  size_t m, s, w, given;                           // scoring
+  size_t x, w, x_exp, w_exp;                       // copies and exponents
+  size_t m, s, sw, given;                          // scoring
   int64_t chunks;
-  size_t scales, xt, wt, c, ct, sums;              // gradient
-  int64_t tp, vp;
+  size_t scales, xc, wc, c, sums;                  // gradient: x and w as the products with c take them
+  int64_t hc, tp, vp;
   size_t bytes;
 };
 
-bool in_place(int type, const void* p, int64_t stride, int64_t features) {
-  return type != QA_F32 && features % kProductStep == 0 && stride % 8 == 0 && stride < (int64_t(1) << 22) && aligned(p, 16);
-}
-// p NULL: a place of any alignment.
+bool in_place(const void* p, int64_t stride) { return stride % 8 == 0 && stride < (int64_t(1) << 22) && aligned(p, 16); }
+
+// x and w NULL: at places of any alignment.
 Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const void* w) {
   Plan P = {};
   Room room;
-  const int parts = parts_for(type);
-  P.copy_x = !x || !in_place(type, x, L.x_stride, L.features);
-  P.copy_w = !w || !in_place(type, w, L.w_stride, L.features);
-  P.hp = whole_steps(L.features);
+  P.parts = type == QA_F32 ? 2 : 1;
+  const bool rows_as_they_are = type != QA_F32 && L.features % kWholeStep == 0;
+  P.copy_x = !x || !rows_as_they_are || !in_place(x, L.x_stride);
+  P.copy_w = !w || !rows_as_they_are || !in_place(w, L.w_stride);
+  P.hp = whole(L.features, kWholeStep);
   if (op == QA_OP_LOGPROB) {
     P.tiles = logits_tiles(L.rows, L.vocab);
-    const int64_t most = std::max<int64_t>(16384, kPieceBytes / (P.hp * 2 * parts) / 256 * 256);
-    P.piece = P.copy_w ? std::min(L.vocab, most) : L.vocab;
+    P.piece = P.copy_w ? piece_of(L.vocab, power_of_two_within(kPieceBytes / (P.hp * 2 * P.parts), 16384)) : L.vocab;
     P.pieces = ceil_div(L.vocab, P.piece);
     P.chunks = ceil_div(L.vocab, chunk_of(P.tiles));
     P.m = room.take(4 * P.chunks * L.rows);
     P.s = room.take(4 * P.chunks * L.rows);
-    P.w = room.take(4 * P.chunks * L.rows);
+    P.sw = room.take(4 * P.chunks * L.rows);
     P.given = room.take(4 * L.rows);
   } else {
-    const int64_t each = L.rows * 2 * (parts + 2) + L.features * 2 * parts;
-    P.piece = std::min(whole_steps(L.vocab), std::max<int64_t>(1024, 2 * kPieceBytes / each / 256 * 256));
+    P.tp = whole(L.rows, kPartsStep);
+    P.hc = whole(L.features, 8);
+    P.piece = piece_of(L.vocab, std::min(power_of_two_within(kPieceBytes / (4 * P.tp), 1024), power_of_two_within(kPieceBytes / (P.hp * 2 * P.parts), 1024)));
     P.pieces = ceil_div(L.vocab, P.piece);
     P.tiles = logits_tiles(L.rows, P.piece);
-    P.tp = whole_steps(L.rows);
-    P.vp = P.piece;
+    P.vp = whole(P.piece, kWholeStep);
     P.scales = room.take(sizeof(Scales));
-    P.xt = room.take(2 * parts * L.features * P.tp);
-    P.wt = room.take(2 * parts * L.features * P.vp);
-    P.c = room.take(2 * parts * L.rows * P.vp);
-    P.ct = room.take(2 * 2 * P.piece * P.tp);
+    P.xc = room.take(2 * P.parts * P.tp * P.hc);
+    P.wc = room.take(2 * P.parts * P.vp * P.hc);
+    P.c = room.take(2 * 2 * P.tp * P.vp);
     P.sums = room.take(P.pieces > 1 ? 4 * L.rows * L.features : 0);
   }
   P.x_exp = room.take(type == QA_F32 ? 4 * L.rows : 0);
   P.w_exp = room.take(type == QA_F32 ? 4 * P.piece : 0);
-  P.xs = room.take(P.copy_x ? 2 * parts * L.rows * P.hp : 0);
-  P.ws = room.take(P.copy_w ? 2 * parts * P.piece * P.hp : 0);
+  P.x = room.take(P.copy_x ? 2 * P.parts * L.rows * P.hp : 0);
+  P.w = room.take(P.copy_w ? 2 * P.parts * P.piece * P.hp : 0);
   P.bytes = room.bytes;
   return P;
 }
-// Any alignment of x and w: the most that a call may take.
+// At most, whatever the alignment of x and w: in place, the scored vocabulary is one piece, which needs less.
 size_t bytes_of(const qa_output_layer& L, int op, int type) { return plan_of(L, op, type, nullptr, nullptr).bytes; }
 
-struct Operand { const uint16_t* p; int64_t ld, part; };
-
-template <int TYPE>
-int copy_rows(const void* from, int64_t stride, int64_t rows, int64_t cols, uint16_t* to, int64_t ld, int* exps, hipStream_t stream) {
-  output_rows_kernel<TYPE><<<(unsigned)ceil_div(rows, kWaves), kThreads, 0, stream>>>(from, stride, rows, cols, to, ld, rows * ld, exps);
+template <int TYPE, Copies HOW>
+int copy_launch(const CopyArgs& A, hipStream_t stream) {
+  output_copy_kernel<TYPE, HOW><<<(unsigned)std::min<int64_t>(ceil_div(A.to_rows, kWaves), 1 << 14), kThreads, 0, stream>>>(A);
   return launch_status();
 }
-
+// Rows for the logits: where they lie, or copied.
+template <int TYPE>
+int logits_operand(const void* from, int64_t stride, int64_t rows, const qa_output_layer& L, const Plan& P, bool copy, char* to, int* exps, Operand& O,
+                   hipStream_t stream) {
+  O = {from, stride, 0, rows};
+  if (!copy) return QA_OK;
+  O = {to, P.parts * P.hp, 0, rows};
+  CopyArgs A = {from, stride, rows, L.features, to, O.ld, rows, exps, nullptr, 0, false, {}};
+  return copy_launch<TYPE, TYPE == QA_F32 ? kOwnScale : kAsTheyAre>(A, stream);
+}
 // Logits of a piece of the vocabulary: w's rows by x's.
 template <int TYPE, class Epilogue>
-int logits_launch(const Operand& w, const Operand& x, int64_t vocab, int64_t rows, int64_t hp, int tiles, const Epilogue& out, hipStream_t stream) {
-  ProductArgs A = {};
-  A.a = w.p;
-  A.b = x.p;
-  A.lda = w.ld;
-  A.ldb = x.ld;
-  A.a_part = w.part;
-  A.b_part = x.part;
-  A.m = vocab;
-  A.n = rows;
-  A.steps = (int)(hp / kProductStep);
+int logits_launch(const Operand& w, const Operand& x, int64_t features, int tiles, const Epilogue& out, hipStream_t stream) {
   constexpr bool kBf16 = TYPE == QA_BF16;
-  constexpr int kPasses = TYPE == QA_F32 ? 3 : 1;
-  if (tiles == kTiles256) return product_launch<kBf16, kPasses, 2, 4, 4, 2>(A, out, 1, 1, stream);
-  if (tiles == kTiles128) return product_launch<kBf16, kPasses, 2, 2, 2, 2>(A, out, 1, 1, stream);
-  return product_launch<kBf16, kPasses, 4, 1, 2, 2>(A, out, 1, 1, stream);
+  constexpr Lies kLie = TYPE == QA_F32 ? kRowsOfParts : kRows;
+  if (tiles == kTiles256) return product_launch<Product256<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
+  if (tiles == kTiles128) return product_launch<Product128<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
+  return product_launch<Product<kBf16, kLie, kLie, 4, 1, 2, 2>>(w, x, features, out, 1, stream);
 }
 
 template <int TYPE>
@@ -506,24 +461,16 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
   const Plan P = plan_of(L, QA_OP_LOGPROB, TYPE, x, w);
   int* const x_exp = (int*)(ws + P.x_exp);
   int* const w_exp = (int*)(ws + P.w_exp);
-  Operand xo = {(const uint16_t*)x, L.x_stride, 0};
-  if (P.copy_x) {
-    xo = {(const uint16_t*)(ws + P.xs), P.hp, L.rows * P.hp};
-    if (const int rc = copy_rows<TYPE>(x, L.x_stride, L.rows, L.features, (uint16_t*)(ws + P.xs), P.hp, x_exp, stream)) return rc;
-  }
-  ScoreArgs A = {(float*)(ws + P.m), (float*)(ws + P.s), (float*)(ws + P.w), (float*)(ws + P.given), 0, 0};
+  Operand xo, wo;
+  if (const int rc = logits_operand<TYPE>(x, L.x_stride, L.rows, L, P, P.copy_x, ws + P.x, x_exp, xo, stream)) return rc;
+  ScoreArgs A = {(float*)(ws + P.m), (float*)(ws + P.s), (float*)(ws + P.sw), (float*)(ws + P.given), 0, 0};
   for (int64_t first = 0; first < L.vocab; first += P.piece) {
     const int64_t vocab = std::min(P.piece, L.vocab - first);
-    const void* const from = (const ElemT<TYPE>*)w + first * L.w_stride;
-    Operand wo = {(const uint16_t*)from, L.w_stride, 0};
-    if (P.copy_w) {
-      wo = {(const uint16_t*)(ws + P.ws), P.hp, vocab * P.hp};
-      if (const int rc = copy_rows<TYPE>(from, L.w_stride, vocab, L.features, (uint16_t*)(ws + P.ws), P.hp, w_exp, stream)) return rc;
-    }
+    if (const int rc = logits_operand<TYPE>((const ElemT<TYPE>*)w + first * L.w_stride, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp, wo, stream)) return rc;
     A.first = first;
     A.first_chunk = first / chunk_of(P.tiles);
     const ScoreOut<TYPE == QA_F32> out{LayerArgs{L.rows, vocab, x_exp, w_exp, target}, A};
-    if (const int rc = logits_launch<TYPE>(wo, xo, vocab, L.rows, P.hp, P.tiles, out, stream)) return rc;
+    if (const int rc = logits_launch<TYPE>(wo, xo, L.features, P.tiles, out, stream)) return rc;
   }
   if (L.rows < 256)
     output_join_kernel<1><<<(unsigned)L.rows, kThreads, 0, stream>>>(A, L.rows, P.chunks, L.vocab, target, logprob, entropy, stats);
@@ -532,20 +479,10 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
   return launch_status();
 }
 
-template <int PASSES, class Epilogue>
-int grad_product(const Operand& a, const Operand& b, int64_t m, int64_t n, int64_t k, const Epilogue& out, hipStream_t stream) {
-  ProductArgs A = {};
-  A.a = a.p;
-  A.b = b.p;
-  A.lda = a.ld;
-  A.ldb = b.ld;
-  A.a_part = a.part;
-  A.b_part = b.part;
-  A.m = m;
-  A.n = n;
-  A.steps = (int)(k / kProductStep);
-  if (ceil_div(m, 256) * ceil_div(n, 256) >= 192) return product_launch<false, PASSES, 2, 4, 4, 2>(A, out, 1, 1, stream);
-  return product_launch<false, PASSES, 2, 2, 2, 2>(A, out, 1, 1, stream);
+template <Lies LA, Lies LB, class Epilogue>
+int grad_product(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, hipStream_t stream) {
+  if (ceil_div(a.n, 256) * ceil_div(b.n, 256) >= 192) return product_launch<Product256<false, LA, LB>>(a, b, k, out, 1, stream);
+  return product_launch<Product128<false, LA, LB>>(a, b, k, out, 1, stream);
 }
 
 struct GradCall {
@@ -557,17 +494,10 @@ struct GradCall {
   int64_t dw_stride;
   int accumulate;
 };
-template <int TYPE, int C_PARTS, bool DW>
-int logits_grad(const Operand& w, const Operand& x, const LayerArgs& L, const RowArgs& R, int64_t hp, int64_t first, const Scales* scales, const Operand& c,
-                const Operand& ct, int tiles, hipStream_t stream) {
-  const LogitsGradOut<TYPE == QA_F32, C_PARTS, DW> out{L, R, first, scales, (_Float16*)c.p, (_Float16*)ct.p, c.ld, c.part, ct.ld, ct.part};
-  return logits_launch<TYPE>(w, x, L.vocab, L.rows, hp, tiles, out, stream);
-}
 
 template <int TYPE>
 int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream_t stream) {
   const Plan P = plan_of(L, QA_OP_LOGPROB_GRAD, TYPE, G.x, G.w);
-  constexpr int kParts = TYPE == QA_F32 ? 2 : 1;
   int* const x_exp = (int*)(ws + P.x_exp);
   int* const w_exp = (int*)(ws + P.w_exp);
   Scales* const scales = (Scales*)(ws + P.scales);
@@ -576,41 +506,39 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
   output_weights_kernel<<<(unsigned)std::min<int64_t>(256, ceil_div(L.rows, kThreads)), kThreads, 0, stream>>>(G.rows, L.rows, scales);
   if (TYPE != QA_F16 && G.dw) output_most_kernel<TYPE><<<most_blocks(L.rows), kThreads, 0, stream>>>(G.x, L.x_stride, L.rows, L.features, G.rows, true, scales, kOfX);
   if (TYPE != QA_F16 && G.dx) output_most_kernel<TYPE><<<most_blocks(L.vocab), kThreads, 0, stream>>>(G.w, L.w_stride, L.vocab, L.features, G.rows, false, scales, kOfW);
-  const Operand xt = {(const uint16_t*)(ws + P.xt), P.tp, L.features * P.tp}, wt = {(const uint16_t*)(ws + P.wt), P.vp, L.features * P.vp};
-  if (G.dw)
-    output_transpose_kernel<TYPE, kParts><<<dim3((unsigned)ceil_div(P.tp, 64), (unsigned)ceil_div(L.features, 64)), kThreads, 0, stream>>>(
-        G.x, L.x_stride, L.rows, L.features, G.rows, true, scales, kOfX, (_Float16*)xt.p, xt.ld, xt.part);
   if (const int rc = launch_status()) return rc;
-  Operand xo = {(const uint16_t*)G.x, L.x_stride, 0};
-  if (P.copy_x) {
-    xo = {(const uint16_t*)(ws + P.xs), P.hp, L.rows * P.hp};
-    if (const int rc = copy_rows<TYPE>(G.x, L.x_stride, L.rows, L.features, (uint16_t*)(ws + P.xs), P.hp, x_exp, stream)) return rc;
+
+  const int64_t copied = P.parts * P.hc;
+  if (G.dw) {                                      // always copied: rows that do not count may hold anything
+    const CopyArgs A = {G.x, L.x_stride, L.rows, L.features, ws + P.xc, copied, P.tp, nullptr, scales, kOfX, true, G.rows};
+    if (const int rc = copy_launch<TYPE, kOneScale>(A, stream)) return rc;
   }
-  const Operand c = {(const uint16_t*)(ws + P.c), P.vp, L.rows * P.vp}, ct = {(const uint16_t*)(ws + P.ct), P.tp, P.piece * P.tp};
+  Operand xo, wo;
+  if (const int rc = logits_operand<TYPE>(G.x, L.x_stride, L.rows, L, P, P.copy_x, ws + P.x, x_exp, xo, stream)) return rc;
+  constexpr Lies kColumnsOf = TYPE == QA_F32 ? kColumnsOfParts : kColumns;
   for (int64_t first = 0; first < L.vocab; first += P.piece) {
-    const int64_t vocab = std::min(P.piece, L.vocab - first), vp = whole_steps(vocab);
+    const int64_t vocab = std::min(P.piece, L.vocab - first);
     const void* const from = (const ElemT<TYPE>*)G.w + first * L.w_stride;
-    Operand wo = {(const uint16_t*)from, L.w_stride, 0};
-    if (P.copy_w) {
-      wo = {(const uint16_t*)(ws + P.ws), P.hp, vocab * P.hp};
-      if (const int rc = copy_rows<TYPE>(from, L.w_stride, vocab, L.features, (uint16_t*)(ws + P.ws), P.hp, w_exp, stream)) return rc;
-    }
-    const LayerArgs piece = {L.rows, vocab, x_exp, w_exp, nullptr};
-    const auto form = G.dx && G.dw ? logits_grad<TYPE, kParts, true> : G.dx ? logits_grad<TYPE, kParts, false> : logits_grad<TYPE, 0, true>;
-    if (const int rc = form(wo, xo, piece, G.rows, P.hp, first, scales, c, ct, P.tiles, stream)) return rc;
+    if (const int rc = logits_operand<TYPE>(from, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp, wo, stream)) return rc;
+    _Float16* const c = (_Float16*)(ws + P.c);
+    const LogitsGradOut<TYPE == QA_F32> grad{LayerArgs{L.rows, vocab, x_exp, w_exp, nullptr}, G.rows, first, scales, c, 2 * P.vp, P.tp};
+    if (const int rc = logits_launch<TYPE>(wo, xo, L.features, P.tiles, grad, stream)) return rc;
     if (G.dx) {
-      output_transpose_kernel<TYPE, kParts><<<dim3((unsigned)ceil_div(vp, 64), (unsigned)ceil_div(L.features, 64)), kThreads, 0, stream>>>(
-          from, L.w_stride, vocab, L.features, G.rows, false, scales, kOfW, (_Float16*)wt.p, wt.ld, wt.part);
-      if (const int rc = launch_status()) return rc;
-      const bool last = first + P.piece >= L.vocab;
+      Operand wc = {from, L.w_stride, 0, L.features};
+      if (TYPE != QA_F16 || !in_place(from, L.w_stride) || L.features % 8 || vocab % kWholeStep) {
+        wc = {ws + P.wc, copied, 0, L.features};
+        const CopyArgs A = {from, L.w_stride, vocab, L.features, ws + P.wc, copied, whole(vocab, kWholeStep), nullptr, scales, kOfW, false, G.rows};
+        if (const int rc = copy_launch<TYPE, kOneScale>(A, stream)) return rc;
+      }
       const GradOut<TYPE> out{(ElemT<TYPE>*)G.dx, P.pieces > 1 ? (float*)(ws + P.sums) : nullptr, scales, G.dx_stride, L.rows, L.features,
-                              TYPE == QA_F16 ? -1 : kOfW, first > 0, last};
-      if (const int rc = grad_product<TYPE == QA_F32 ? 3 : 1>(c, wt, L.rows, L.features, vp, out, stream)) return rc;
+                              TYPE == QA_F16 ? -1 : kOfW, first > 0, first + P.piece >= L.vocab};
+      // One part of c has 11 bits, which is little beside bfloat16's 8, but as much as binary16's own.
+      constexpr Lies kC = TYPE == QA_BF16 ? kHiOfRows : kRowsOfParts;
+      if (const int rc = grad_product<kColumnsOf, kC>(wc, Operand{c, 2 * P.vp, 0, L.rows}, vocab, out, stream)) return rc;
     }
     if (G.dw) {
-      const GradOut<QA_F32> out{G.dw + first * G.dw_stride, nullptr, scales, G.dw_stride, vocab, L.features, TYPE == QA_F16 ? -1 : kOfX,
-                                G.accumulate != 0, true};
-      if (const int rc = grad_product<TYPE == QA_F32 ? 3 : 2>(ct, xt, vocab, L.features, P.tp, out, stream)) return rc;
+      const GradOut<QA_F32> out{G.dw + first * G.dw_stride, nullptr, scales, G.dw_stride, vocab, L.features, TYPE == QA_F16 ? -1 : kOfX, G.accumulate != 0, true};
+      if (const int rc = grad_product<kColumnsOf, kColumnsOfParts>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, stream)) return rc;
     }
   }
   return QA_OK;

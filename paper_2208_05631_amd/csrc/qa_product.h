@@ -1,88 +1,170 @@
-// Products of the matrix cores over rows of 16-bit elements: C[i][j] = sum_k A[i][k] B[j][k], both operands with k along
-// their rows, sums in binary32.  Shared by the kernels that multiply; not part of the public interface.
+// Products of the matrix cores over matrices of 16-bit elements: C[i][j] = sum_k A(i, k) B(j, k), sums in binary32.  Shared by
+// the kernels that multiply; not part of the public interface.
 #pragma once
 #include "qa_rows.h"
 
-#if defined(__HIPCC__)
-
 namespace qa {
 
+// A number of more bits than an element has is two elements ("parts"), hi + lo.  A row of parts is eight hi, the eight lo
+// that belong to them, and so on: 16 bytes each.  Products are hi hi, hi lo and lo hi; the fourth is below binary32's rounding.
+constexpr int64_t kPartsStep = 16, kWholeStep = 32;        // elements of k per step, of products with parts and without
+constexpr int64_t whole(int64_t n, int64_t step) { return (n + step - 1) / step * step; }
+
+#if defined(__HIPCC__)
+
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kProductStep = 32;                   // elements of k that lie in LDS per step: 64 bytes of a row
+// How an operand lies in memory.
+enum Lies {
+  kRows,                                           // k along its rows
+  kRowsOfParts,
+  kHiOfRows,                                       // the hi of rows of parts
+  kColumns,                                        // i along its rows: row k holds all i
+  kColumnsOfParts
+};
+constexpr int parts_in(Lies l) { return l == kRowsOfParts || l == kColumnsOfParts ? 2 : 1; }
+constexpr bool in_rows(Lies l) { return l <= kHiOfRows; }
 
-// A number of more bits than an element has is two elements ("parts"), hi + lo; their products are hi hi, lo hi and hi lo
-// (the fourth is below binary32's rounding), one after the other for each step of k.
+struct Operand {
+  const void* p;                                   // 16-byte aligned
+  int64_t ld;                                      // elements between rows, a multiple of 8, < 2^22
+  int64_t batch;                                   // elements between matrices (gridDim.z)
+  int64_t n;                                       // how many i there are; past them the last ones are read again
+};
 struct ProductArgs {
-  const uint16_t *a, *b;                           // 16-byte aligned, as are all strides
-  int64_t lda, ldb;                                // elements between rows, < 2^22
-  int64_t a_part, b_part;                          // elements from an operand's hi to its lo
-  int64_t a_batch, b_batch;                        // elements between matrices (gridDim.z)
-  int64_t m, n;                                    // rows of a and of b; past them the last one is read again
-  int steps, split_steps;                          // steps of k, and those of one split (gridDim.y)
+  Operand a, b;
+  int steps, split_steps;                          // of k in all, and of one split (gridDim.y)
   unsigned tiles_m, tiles_n;
 };
 
-// WM x WN waves, FM x FN blocks of 32 x 32 each.
+// Brings SIDE values of i and STEP of k to LDS, straight from memory, 16 bytes per lane.
 //
-// Rows come straight from memory to LDS, 16 bytes per lane: a wave's instruction brings 64 bytes of sixteen rows.  In LDS
-// a row's four octets stand at octet ^ (row / 4 % 4), which the lanes' addresses in memory see to, so that the sixteen
-// rows that are read at a time lie in different banks.  Four buffers: while step s is multiplied, s + 1 is there and
-// s + 2 and s + 3 are on their way, into the buffer that step s - 1 had.
-template <bool BF16, int PASSES, int WM, int WN, int FM, int FN>
-struct Product {
-  static constexpr int kM = 32 * WM * FM, kN = 32 * WN * FN, kGroup = WM * WN * kWave;
-  static constexpr int kBuffer = (kM + kN) * kProductStep, kBuffers = 4;
-  static constexpr int kA = kM / 16 / (WM * WN), kB = kN / 16 / (WM * WN), kLoads = kA + kB;      // instructions per wave and step
-  static_assert(kA * 16 * WM * WN == kM && kB * 16 * WM * WN == kN, "a wave brings rows of one operand at a time");
-
-  f32x16 acc[FM][FN];
-  u32x4 a[2][FM], b[2][FN];                        // operands of the two halves of a step
-  const char *a_from, *b_from;                     // k = 0 of the tile's first row
-  const char *a_at, *b_at;                         // what is loaded next
-  int64_t a_part, b_part, k_at;                    // bytes
-  int to_load, pass;
+// k along the rows: 64 bytes of each row, which are four octets of k, or the two octets' hi and then their lo.  An octet stands at
+// octet ^ (row / 4 % 4), so that the sixteen rows that are read at a time lie in different banks.
+// i along the rows: row k is SIDE elements (and then their lo); the eight elements c of it stand at c ^ 4 (k % 4), so that
+// the four rows that a transposing read takes lie in different banks.
+// The lanes' addresses in memory see to that: in LDS a wave's 64 lanes lie side by side.
+template <Lies LIES, int SIDE, int STEP, int WAVES>
+struct Bringer {
+  static constexpr int kParts = parts_in(LIES);
+  static constexpr int kBytes = in_rows(LIES) ? SIDE * 64 : STEP * SIDE * 2 * kParts;
+  static constexpr int kLoads = kBytes / 1024 / WAVES;
+  static constexpr int kPitch = in_rows(LIES) ? 64 : SIDE * 2 * kParts;        // bytes between rows in LDS
+  static_assert(kLoads * 1024 * WAVES == kBytes && (in_rows(LIES) || SIDE >= 128 || kParts == 2), "whole instructions, 16 chunks a row");
+  const char* at;
+  int64_t advance;
   uint32_t off[kLoads];
-  int a_lane, b_lane, half[2], wave;
 
-  __device__ __forceinline__ void next() {
-    if (to_load > 1) {
-      if constexpr (PASSES == 1) {
-        a_at += 2 * kProductStep;
-        b_at += 2 * kProductStep;
-      } else {
-        if (++pass == PASSES) pass = 0, k_at += 2 * kProductStep;
-        a_at = a_from + k_at + (pass == 1 ? a_part : 0);
-        b_at = b_from + k_at + (pass == 2 ? b_part : 0);
+  __device__ __forceinline__ void begin(const Operand& O, int64_t i0, int first_step, int wave) {
+    const int lane = threadIdx.x % kWave;
+    const char* p = (const char*)O.p + (int64_t)blockIdx.z * O.batch * 2;
+    if constexpr (in_rows(LIES)) {
+      advance = LIES == kHiOfRows ? 128 : 64;
+      at = p + i0 * O.ld * 2 + first_step * advance;
+      const int slot = (lane & 3) ^ (lane >> 4 & 3);
+      const uint32_t octet = (uint32_t)(LIES == kRows ? slot : LIES == kHiOfRows ? 2 * slot : 2 * (slot & 1) + (slot >> 1)) * 16;
+#pragma unroll
+      for (int v = 0; v < kLoads; ++v)
+        off[v] = (uint32_t)min((int64_t)((v * WAVES + wave) * 16 + lane / 4), O.n - 1 - i0) * (uint32_t)(2 * O.ld) + octet;
+    } else {
+      advance = STEP * O.ld * 2;
+      at = p + i0 * 2 * kParts + first_step * advance;
+      const int last = (int)min((int64_t)SIDE, (O.n - i0 + 7) / 8 * 8) / 8 - 1;
+#pragma unroll
+      for (int v = 0; v < kLoads; ++v) {
+        const int chunk = (v * WAVES + wave) * 64 + lane, k = chunk / (kPitch / 16), slot = (chunk % (kPitch / 16)) ^ 4 * (k & 3);
+        const int part = slot / (SIDE / 8), c = slot % (SIDE / 8);
+        off[v] = (uint32_t)k * (uint32_t)(2 * O.ld) + (uint32_t)((min(c, last) * kParts + part) * 16);
       }
     }
-    --to_load;
   }
-  __device__ __forceinline__ void load(uint16_t* lds) {
+  __device__ __forceinline__ void bring(char* lds, int wave) const {
 #pragma unroll
     for (int v = 0; v < kLoads; ++v)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((v < kA ? a_at : b_at) + off[v]),
-                                       (__attribute__((address_space(3))) void*)(lds + (v * WM * WN + wave) * 16 * kProductStep), 16, 0, 0);
-    next();
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(at + off[v]),
+                                       (__attribute__((address_space(3))) void*)(lds + (v * WAVES + wave) * 1024), 16, 0, 0);
   }
-  __device__ __forceinline__ void read(const uint16_t* lds, int h) {
+};
+
+// What a lane of a matrix instruction reads of it: i = lane % 32 of block f, k = 8 (lane / 32) ... + 7 of half h (or of part h).
+// Of 16 lanes that read transposed each addresses four i of one of four k, and receives four k of one i.
+template <Lies LIES, int SIDE, int STEP, int BLOCKS>
+struct Reader {
+  static constexpr int kPitch = Bringer<LIES, SIDE, STEP, 1>::kPitch;
+  static constexpr bool kMixed = !in_rows(LIES) && SIDE < 128;       // lo lies among hi: of 16 chunks eight are hi
+  int lane_at[in_rows(LIES) || kMixed ? 2 * BLOCKS : BLOCKS];
+  __device__ __forceinline__ void begin(int block0) {
+    const int lane = threadIdx.x % kWave;
+    if constexpr (in_rows(LIES)) {
 #pragma unroll
-    for (int j = 0; j < FN; ++j) b[h][j] = *reinterpret_cast<const u32x4*>(lds + b_lane + half[h] + 32 * j * kProductStep);
+      for (int h = 0; h < 2; ++h) lane_at[h] = (32 * block0 + lane % 32) * 64 + ((2 * h + lane / 32) ^ (lane >> 2 & 3)) * 16;
+    } else {
+      const int k = 8 * (lane / 32) + (lane % 16 >> 2);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) a[h][i] = *reinterpret_cast<const u32x4*>(lds + a_lane + half[h] + 32 * i * kProductStep);
+      for (int f = 0; f < BLOCKS; ++f) {
+        const int i = 32 * (block0 + f) + (lane & 16) + 4 * (lane & 3);
+        lane_at[f] = k * kPitch + ((i / 8) ^ 4 * (k & 3)) * 16 + (lane & 1) * 8;
+        if constexpr (kMixed) lane_at[BLOCKS + f] = k * kPitch + ((SIDE / 8 + i / 8) ^ 4 * (k & 3)) * 16 + (lane & 1) * 8;
+      }
+    }
   }
-  __device__ __forceinline__ void multiply(int h) {
+  __device__ __forceinline__ void read(const char* lds, int h, u32x4 (&v)[BLOCKS]) const {
+#pragma unroll
+    for (int f = 0; f < BLOCKS; ++f) {
+      if constexpr (in_rows(LIES)) {
+        v[f] = *reinterpret_cast<const u32x4*>(lds + lane_at[h] + f * 32 * 64);
+      } else {
+        const char* p = lds + (kMixed ? lane_at[h * BLOCKS + f] : lane_at[f] + h * (parts_in(LIES) == 2 ? 2 * SIDE : 16 * kPitch));
+        s16x4 half[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          half[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 4 * e * kPitch));
+        __builtin_memcpy(&v[f], half, sizeof half);
+      }
+    }
+  }
+};
+
+// WM x WN waves, FM x FN blocks of 32 x 32 each.  Four buffers: while step s is multiplied, s + 1 is there and s + 2 and
+// s + 3 are on their way, into the buffer that step s - 1 had.
+template <bool BF16, Lies LA, Lies LB, int WM, int WN, int FM, int FN>
+struct Product {
+  static constexpr int kM = 32 * WM * FM, kN = 32 * WN * FN, kWavesHere = WM * WN, kGroup = kWavesHere * kWave;
+  static constexpr int kPA = parts_in(LA), kPB = parts_in(LB);
+  static constexpr int kStep = kPA * kPB == 1 ? kWholeStep : kPartsStep;
+  static_assert(kPA <= kPB && !(kStep == kPartsStep && (LA == kRows || LA == kHiOfRows || LB == kRows || LB == kHiOfRows)), "forms that there are");
+  typedef Bringer<LA, kM, kStep, kWavesHere> BringA;
+  typedef Bringer<LB, kN, kStep, kWavesHere> BringB;
+  static constexpr int kBuffer = BringA::kBytes + BringB::kBytes, kBuffers = 4, kLoads = BringA::kLoads + BringB::kLoads;
+
+  f32x16 acc[FM][FN];
+  u32x4 a[2][FM], b[2][FN];
+  BringA bring_a;
+  BringB bring_b;
+  Reader<LA, kM, kStep, FM> read_a;
+  Reader<LB, kN, kStep, FN> read_b;
+  int to_load, wave;
+
+  // Past the last step the last one is read again.
+  __device__ __forceinline__ void load(char* lds) {
+    bring_a.bring(lds, wave);
+    bring_b.bring(lds + BringA::kBytes, wave);
+    const int64_t go = --to_load > 0 ? -1 : 0;     // no branch: the matrix instructions around this are one block
+    bring_a.at += bring_a.advance & go;
+    bring_b.at += bring_b.advance & go;
+  }
+  __device__ __forceinline__ void multiply(const u32x4 (&x)[FM], const u32x4 (&y)[FN]) {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
         if constexpr (BF16)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[h][i]), __builtin_bit_cast(bf16x8, b[h][j]), acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[i]), __builtin_bit_cast(bf16x8, y[j]), acc[i][j], 0, 0, 0);
         else
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a[h][i]), __builtin_bit_cast(f16x8, b[h][j]), acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x[i]), __builtin_bit_cast(f16x8, y[j]), acc[i][j], 0, 0, 0);
       }
   }
   // Waits until at most LEFT of this wave's loads are on their way, then for the other waves.  Loads into LDS are the only
@@ -92,53 +174,47 @@ struct Product {
     static_assert(LEFT < 64, "the counter's bits");
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LEFT) : "memory");
   }
-  // The three buffers lie apart, as the compiler is told: it would wait for all loads before each read otherwise.
-  static __device__ __forceinline__ void step(Product& p, const uint16_t* __restrict__ now, const uint16_t* __restrict__ then,
-                                              uint16_t* __restrict__ last) {
-    p.read(now, 1);
-    p.multiply(0);
+  // The first operands of a step are read beside the last products of the one before.  The three buffers lie apart, as the
+  // compiler is told: it would wait for all loads before each read otherwise.
+  static __device__ __forceinline__ void step(Product& p, const char* __restrict__ now, const char* __restrict__ then, char* __restrict__ last) {
+    if constexpr (kPA == kPB) p.read_a.read(now, 1, p.a[1]);
+    p.read_b.read(now + BringA::kBytes, 1, p.b[1]);
+    p.multiply(p.a[0], p.b[0]);
+    if constexpr (kPA == 2) p.multiply(p.a[0], p.b[1]);
     arrive<kLoads>();                              // `then` is there, and nobody reads `last` any more
     p.load(last);
-    p.read(then, 0);
-    p.multiply(1);
+    u32x4 a_next[FM], b_next[FN];
+    p.read_a.read(then, 0, a_next);
+    p.read_b.read(then + BringA::kBytes, 0, b_next);
+    if constexpr (kPA == 2) p.multiply(p.a[1], p.b[0]);
+    else if constexpr (kPB == 2) p.multiply(p.a[0], p.b[1]);
+    else p.multiply(p.a[1], p.b[1]);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) p.a[0][i] = a_next[i];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) p.b[0][j] = b_next[j];
   }
   // Sums of split blockIdx.y, 0 where it has no steps.
-  __device__ __forceinline__ void run(const ProductArgs& A, int64_t m0, int64_t n0, uint16_t* lds) {
-    const int lane = threadIdx.x % kWave;
+  __device__ __forceinline__ void run(const ProductArgs& A, int64_t m0, int64_t n0, char* lds) {
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
-    const int first = (int)blockIdx.y * A.split_steps, steps = min(A.steps - first, A.split_steps) * PASSES;
+    const int first = (int)blockIdx.y * A.split_steps, steps = min(A.steps - first, A.split_steps);
     if (steps <= 0) return;
-    a_from = (const char*)(A.a + (int64_t)blockIdx.z * A.a_batch + m0 * A.lda + (int64_t)first * kProductStep);
-    b_from = (const char*)(A.b + (int64_t)blockIdx.z * A.b_batch + n0 * A.ldb + (int64_t)first * kProductStep);
-    a_at = a_from;
-    b_at = b_from;
-    a_part = 2 * A.a_part;
-    b_part = 2 * A.b_part;
-    k_at = 0;
+    bring_a.begin(A.a, m0, first, wave);
+    bring_b.begin(A.b, n0, first, wave);
+    read_a.begin(wave % WM * FM);
+    read_b.begin(wave / WM * FN);
     to_load = steps;
-    pass = 0;
-    const uint32_t octet = (uint32_t)((lane & 3) ^ (lane >> 4 & 3)) * 16;
-#pragma unroll
-    for (int v = 0; v < kLoads; ++v) {
-      const int row = (v < kA ? v : v - kA) * 16 * WM * WN + wave * 16 + lane / 4;
-      const int64_t most = (v < kA ? A.m - m0 : A.n - n0) - 1;
-      off[v] = (uint32_t)min((int64_t)row, most) * (uint32_t)(2 * (v < kA ? A.lda : A.ldb)) + octet;
-    }
-    a_lane = (wave % WM * 32 * FM + lane % 32) * kProductStep;
-    b_lane = (kM + wave / WM * 32 * FN + lane % 32) * kProductStep;
-    half[0] = ((lane / 32) ^ (lane >> 2 & 3)) * 8;
-    half[1] = ((2 + lane / 32) ^ (lane >> 2 & 3)) * 8;
-
     int now = 0, then = kBuffer, later = 2 * kBuffer, last = 3 * kBuffer;
     load(lds + now);
     load(lds + then);
     load(lds + later);
     arrive<2 * kLoads>();
-    read(lds + now, 0);
+    read_a.read(lds, 0, a[0]);
+    read_b.read(lds + BringA::kBytes, 0, b[0]);
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
       step(*this, lds + now, lds + then, lds + last);
@@ -152,9 +228,60 @@ struct Product {
   }
   __device__ __forceinline__ int64_t wave_m(int64_t m0) const { return m0 + wave % WM * 32 * FM; }
   __device__ __forceinline__ int64_t wave_n(int64_t n0) const { return n0 + wave / WM * 32 * FN; }
+
+  // A lane holds of block (i, j) rows 8 q + 4 (lane / 32) + e, e < 4, of column lane % 32.  With its counterpart of the other half it changes
+  // four rows for four, so that it has eight that follow each other: each(i0, j, eight sums), i0 .. i0 + 7 and j within C.
+  // block(i0, j0): behind the 32 x 32 that begin there.
+  template <class Each, class Block>
+  __device__ __forceinline__ void for_eights(int64_t m0, int64_t n0, const Each& each, const Block& block) {
+    const int lane = threadIdx.x % kWave;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          float v[kVec];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const auto both = __builtin_amdgcn_permlane32_swap(as_u32(acc[i][j][8 * q + e]), as_u32(acc[i][j][8 * q + 4 + e]), false, false);
+            v[e] = as_f32(both[0]);
+            v[4 + e] = as_f32(both[1]);
+          }
+          each(m0 + 32 * i + 16 * q + 8 * (lane / 32), n0 + 32 * j + lane % 32, v);
+        }
+        block(m0 + 32 * i, n0 + 32 * j);
+      }
+  }
+  template <class Each>
+  __device__ __forceinline__ void for_eights(int64_t m0, int64_t n0, const Each& each) {
+    for_eights(m0, n0, each, [](int64_t, int64_t) {});
+  }
 };
 
-// The numbers that a lane has of block (i, j): rows 8 q + 4 (lane / 32) + e, e < 4, of column lane % 32.
+// 32 x 32 numbers of a wave, put in by rows of C's columns and taken out by its rows, by way of LDS.
+struct Turned {
+  float* at;                                       // 32 rows of 33
+  __device__ __forceinline__ void put(int64_t i0, const float (&v)[kVec]) const {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) at[((int)i0 % 32 + e) * 33 + (int)threadIdx.x % 32] = v[e];
+  }
+  // each(i, j0, eight numbers of row i)
+  template <class Each>
+  __device__ __forceinline__ void take(int64_t i0, int64_t j0, const Each& each) const {
+    __builtin_amdgcn_wave_barrier();
+    const int row = (int)threadIdx.x % kWave / 2;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int col = 16 * ((int)threadIdx.x % 2) + kVec * h;
+      float v[kVec];
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v[e] = at[row * 33 + col + e];
+      each(i0 + row, j0 + col, v);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+};
 
 // Consecutive work-groups go to the eight dies in turn.  Each die takes tiles that lie together, in bands eight tiles wide,
 // so that its cache is asked for the same rows.  LOWER: tiles on and below the diagonal only.
@@ -175,36 +302,50 @@ __device__ __forceinline__ void tile_of(const ProductArgs& A, unsigned& tm, unsi
   }
 }
 
-template <bool BF16, int PASSES, int WM, int WN, int FM, int FN, bool LOWER, class Epilogue>
-__global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(ProductArgs A, Epilogue out) {
-  typedef Product<BF16, PASSES, WM, WN, FM, FN> P;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[P::kBuffers * P::kBuffer];
+template <class P, bool LOWER, class Epilogue>
+__global__ __launch_bounds__(P::kGroup, 2) void product_kernel(ProductArgs A, Epilogue out) {
+  __shared__ __attribute__((aligned(1024))) char lds[P::kBuffers * P::kBuffer];
   unsigned tm, tn;
   tile_of<LOWER>(A, tm, tn);
   const int64_t m0 = (int64_t)tm * P::kM, n0 = (int64_t)tn * P::kN;
   P p;
   p.run(A, m0, n0, lds);
-  out(p, p.wave_m(m0), p.wave_n(n0));
+  out(p, p.wave_m(m0), p.wave_n(n0), lds + p.wave * (P::kBuffers * P::kBuffer / P::kWavesHere));
 }
 
-// Launches tiles of the given form over all of A, splits and batches as they are set.
-template <bool BF16, int PASSES, int WM, int WN, int FM, int FN, bool LOWER = false, class Epilogue>
-int product_launch(ProductArgs A, const Epilogue& out, unsigned splits, unsigned batch, hipStream_t stream) {
-  typedef Product<BF16, PASSES, WM, WN, FM, FN> P;
-  A.tiles_m = (unsigned)ceil_div(A.m, P::kM);
-  A.tiles_n = (unsigned)ceil_div(A.n, P::kN);
-  A.split_steps = (int)ceil_div(A.steps, splits);
+// Launches tiles of the given form over all of A and B; k: how many there are, zeros up to a whole step.
+template <class P, bool LOWER = false, class Epilogue>
+int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream) {
+  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), (int)ceil_div(k, P::kStep), (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN)};
   const unsigned tiles = LOWER ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n;
-  product_kernel<BF16, PASSES, WM, WN, FM, FN, LOWER><<<dim3(tiles, splits, batch), P::kGroup, 0, stream>>>(A, out);
+  product_kernel<P, LOWER><<<dim3(tiles, 1, batch), P::kGroup, 0, stream>>>(A, out);
   return launch_status();
 }
+template <bool BF16, Lies LA, Lies LB> using Product256 = Product<BF16, LA, LB, 2, 4, 4, 2>;
+template <bool BF16, Lies LA, Lies LB> using Product128 = Product<BF16, LA, LB, 2, 2, 2, 2>;
+template <bool BF16, Lies LA, Lies LB> using Product64 = Product<BF16, LA, LB, 2, 2, 1, 1>;
 
 // v as hi + lo of binary16: 22 bits and a sign between them, as long as v is at least 2^-13; what is lost below is 2^-25 at most.
 __device__ __forceinline__ void split_f16(float v, _Float16& hi, _Float16& lo) {
   hi = (_Float16)v;
   lo = (_Float16)(v - (float)hi);
 }
-
-}  // namespace qa
+// Eight numbers to their place in a row of parts, and back.
+__device__ __forceinline__ void put_parts(_Float16* p, const float (&v)[kVec]) {
+  _Float16 hi[kVec], lo[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) split_f16(v[i], hi[i], lo[i]);
+  __builtin_memcpy(__builtin_assume_aligned(p, 16), hi, sizeof hi);
+  __builtin_memcpy(__builtin_assume_aligned(p + kVec, 16), lo, sizeof lo);
+}
+__device__ __forceinline__ void get_parts(const _Float16* p, float (&v)[kVec]) {
+  _Float16 hi[kVec], lo[kVec];
+  __builtin_memcpy(hi, __builtin_assume_aligned(p, 16), sizeof hi);
+  __builtin_memcpy(lo, __builtin_assume_aligned(p + kVec, 16), sizeof lo);
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) v[i] = (float)hi[i] + (float)lo[i];
+}
 
 #endif  // __HIPCC__
+
+}  // namespace qa
