@@ -81,9 +81,11 @@ struct Bringer {
       }
     }
   }
+  // Instructions [FROM, TO) of them.
+  template <int FROM, int TO>
   __device__ __forceinline__ void bring(char* lds, int wave) const {
 #pragma unroll
-    for (int v = 0; v < kLoads; ++v)
+    for (int v = FROM < 0 ? 0 : FROM; v < (TO < kLoads ? TO : kLoads); ++v)
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(at + off[v]),
                                        (__attribute__((address_space(3))) void*)(lds + (v * WAVES + wave) * 1024), 16, 0, 0);
   }
@@ -128,17 +130,19 @@ struct Reader {
   }
 };
 
-// WM x WN waves, FM x FN blocks of 32 x 32 each.  Four buffers: while step s is multiplied, s + 1 is there and s + 2 and
-// s + 3 are on their way, into the buffer that step s - 1 had.
+// WM x WN waves, FM x FN blocks of 32 x 32 each.  Four buffers: while step s is multiplied, s + 1 is there, s + 2 on its way, and s + 3
+// sets out for the buffer that step s - 1 had.
 template <bool BF16, Lies LA, Lies LB, int WM, int WN, int FM, int FN>
 struct Product {
   static constexpr int kM = 32 * WM * FM, kN = 32 * WN * FN, kWavesHere = WM * WN, kGroup = kWavesHere * kWave;
+  static constexpr int kWavesPerSimd = FM * FN == 16 ? 1 : 2;        // of registers
   static constexpr int kPA = parts_in(LA), kPB = parts_in(LB);
   static constexpr int kStep = kPA * kPB == 1 ? kWholeStep : kPartsStep;
   static_assert(kPA <= kPB && !(kStep == kPartsStep && (LA == kRows || LA == kHiOfRows || LB == kRows || LB == kHiOfRows)), "forms that there are");
   typedef Bringer<LA, kM, kStep, kWavesHere> BringA;
   typedef Bringer<LB, kN, kStep, kWavesHere> BringB;
   static constexpr int kBuffer = BringA::kBytes + BringB::kBytes, kBuffers = 4, kLoads = BringA::kLoads + BringB::kLoads;
+  static constexpr int kLate = (kLoads + 1) / (kPA + 1);       // a step's loads behind the barrier; the others follow in the next step
 
   f32x16 acc[FM][FN];
   u32x4 a[2][FM], b[2][FN];
@@ -148,13 +152,16 @@ struct Product {
   Reader<LB, kN, kStep, FN> read_b;
   int to_load, wave;
 
-  // Past the last step the last one is read again.
+  // Instructions [FROM, TO) of a step's; behind the last one go on, past the last step to itself.
+  template <int FROM, int TO>
   __device__ __forceinline__ void load(char* lds) {
-    bring_a.bring(lds, wave);
-    bring_b.bring(lds + BringA::kBytes, wave);
-    const int64_t go = --to_load > 0 ? -1 : 0;     // no branch: the matrix instructions around this are one block
-    bring_a.at += bring_a.advance & go;
-    bring_b.at += bring_b.advance & go;
+    bring_a.template bring<FROM, TO>(lds, wave);
+    bring_b.template bring<FROM - BringA::kLoads, TO - BringA::kLoads>(lds + BringA::kBytes, wave);
+    if constexpr (TO == kLoads) {
+      const int64_t go = --to_load > 0 ? -1 : 0;   // no branch: the matrix instructions around this are one block
+      bring_a.at += bring_a.advance & go;
+      bring_b.at += bring_b.advance & go;
+    }
   }
   __device__ __forceinline__ void multiply(const u32x4 (&x)[FM], const u32x4 (&y)[FN]) {
 #pragma unroll
@@ -174,21 +181,41 @@ struct Product {
     static_assert(LEFT < 64, "the counter's bits");
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LEFT) : "memory");
   }
-  // The first operands of a step are read beside the last products of the one before.  The three buffers lie apart, as the
+  // The order of a phase's instructions: MULTIPLIES matrix instructions, with READS reads of LDS in the shadow of the first ones, two each,
+  // as they have to be there when the next phase begins, and LOADS reads of memory spread over all.
+  template <int MULTIPLIES, int READS, int LOADS, int I = 0>
+  static __device__ __forceinline__ void interleave() {
+    if constexpr (I < MULTIPLIES) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      constexpr int kReads = 2 * I >= READS ? 0 : READS - 2 * I < 2 ? 1 : 2, kHere = (I + 1) * LOADS / MULTIPLIES - I * LOADS / MULTIPLIES;
+      if constexpr (kReads > 0) __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+      if constexpr (kHere > 0) __builtin_amdgcn_sched_group_barrier(0x020, kHere, 0);
+      interleave<MULTIPLIES, READS, LOADS, I + 1>();
+    } else {
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // The first operands of a step are read beside the last products of the one before.  Half of the loads stand in front of the
+  // barrier, half behind it: all at once, they wait for each other, and the products for them.  The buffers lie apart, as the
   // compiler is told: it would wait for all loads before each read otherwise.
-  static __device__ __forceinline__ void step(Product& p, const char* __restrict__ now, const char* __restrict__ then, char* __restrict__ last) {
+  static __device__ __forceinline__ void step(Product& p, const char* __restrict__ now, const char* __restrict__ then, char* __restrict__ late,
+                                              char* __restrict__ last) {
+    constexpr int kAll = FM * FN, kReadA = FM * (in_rows(LA) ? 1 : 2), kReadB = FN * (in_rows(LB) ? 1 : 2);
     if constexpr (kPA == kPB) p.read_a.read(now, 1, p.a[1]);
     p.read_b.read(now + BringA::kBytes, 1, p.b[1]);
+    p.template load<kLate, kLoads>(late);
     p.multiply(p.a[0], p.b[0]);
     if constexpr (kPA == 2) p.multiply(p.a[0], p.b[1]);
+    interleave<kPA == 2 ? 2 * kAll : kAll, (kPA == kPB ? kReadA : 0) + kReadB, kLoads - kLate>();
     arrive<kLoads>();                              // `then` is there, and nobody reads `last` any more
-    p.load(last);
     u32x4 a_next[FM], b_next[FN];
     p.read_a.read(then, 0, a_next);
     p.read_b.read(then + BringA::kBytes, 0, b_next);
+    p.template load<0, kLate>(last);
     if constexpr (kPA == 2) p.multiply(p.a[1], p.b[0]);
     else if constexpr (kPB == 2) p.multiply(p.a[0], p.b[1]);
     else p.multiply(p.a[1], p.b[1]);
+    interleave<kAll, kReadA + kReadB, kLate>();
 #pragma unroll
     for (int i = 0; i < FM; ++i) p.a[0][i] = a_next[i];
 #pragma unroll
@@ -208,20 +235,20 @@ struct Product {
     read_a.begin(wave % WM * FM);
     read_b.begin(wave / WM * FN);
     to_load = steps;
-    int now = 0, then = kBuffer, later = 2 * kBuffer, last = 3 * kBuffer;
-    load(lds + now);
-    load(lds + then);
-    load(lds + later);
-    arrive<2 * kLoads>();
+    int now = 0, then = kBuffer, late = 2 * kBuffer, last = 3 * kBuffer;
+    load<0, kLoads>(lds + now);
+    load<0, kLoads>(lds + then);
+    load<0, kLate>(lds + late);
+    arrive<kLoads + kLate>();
     read_a.read(lds, 0, a[0]);
     read_b.read(lds + BringA::kBytes, 0, b[0]);
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
-      step(*this, lds + now, lds + then, lds + last);
+      step(*this, lds + now, lds + then, lds + late, lds + last);
       const int free = now;
       now = then;
-      then = later;
-      later = last;
+      then = late;
+      late = last;
       last = free;
     }
     arrive<0>();                                   // loads past the last step, before LDS is used for something else
@@ -303,7 +330,7 @@ __device__ __forceinline__ void tile_of(const ProductArgs& A, unsigned& tm, unsi
 }
 
 template <class P, bool LOWER, class Epilogue>
-__global__ __launch_bounds__(P::kGroup, 2) void product_kernel(ProductArgs A, Epilogue out) {
+__global__ __launch_bounds__(P::kGroup, P::kWavesPerSimd) void product_kernel(ProductArgs A, Epilogue out) {
   __shared__ __attribute__((aligned(1024))) char lds[P::kBuffers * P::kBuffer];
   unsigned tm, tn;
   tile_of<LOWER>(A, tm, tn);
@@ -321,7 +348,7 @@ int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue
   product_kernel<P, LOWER><<<dim3(tiles, 1, batch), P::kGroup, 0, stream>>>(A, out);
   return launch_status();
 }
-template <bool BF16, Lies LA, Lies LB> using Product256 = Product<BF16, LA, LB, 2, 4, 4, 2>;
+template <bool BF16, Lies LA, Lies LB> using Product256 = Product<BF16, LA, LB, 2, 2, 4, 4>;
 template <bool BF16, Lies LA, Lies LB> using Product128 = Product<BF16, LA, LB, 2, 2, 2, 2>;
 template <bool BF16, Lies LA, Lies LB> using Product64 = Product<BF16, LA, LB, 2, 2, 1, 1>;
 
