@@ -47,6 +47,12 @@ __device__ __forceinline__ void source8(const SourceArgs& A, int64_t at, int n, 
   if (UPDATE) store_raw<QA_F32>(A.momentum + at, from_f32<QA_F32>(m), n);
 }
 
+// What the numbers are multiplied by, from the sum of their squares.  A matrix of zeros stays one; one with an infinity or a NaN has
+// no direction.
+__device__ __forceinline__ double scale_for(double all) {
+  return all == 0.0 ? 0.0 : __builtin_isfinite(all) ? (double)kUnit / __builtin_sqrt(all) : (double)__builtin_nanf("");
+}
+
 // Squares are added in binary64: those of any finite numbers are finite there, and none is lost.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void orthogonal_norm_kernel(SourceArgs A) {
@@ -80,8 +86,7 @@ __global__ __launch_bounds__(kThreads) void orthogonal_parts_kernel(SourceArgs A
   if (threadIdx.x % kWave == 0) sums[threadIdx.x / kWave] = part;
   __syncthreads();
   const double all = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-  // A matrix of zeros stays one; one with an infinity or a NaN has no direction.
-  const double scale = all == 0.0 ? 0.0 : __builtin_isfinite(all) ? (double)kUnit / __builtin_sqrt(all) : (double)__builtin_nanf("");
+  const double scale = scale_for(all);
   const int64_t x_rows = whole(TALL ? A.M.cols : A.M.rows, kPartsStep), x_cols = A.ld / 2;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -117,13 +122,13 @@ __global__ __launch_bounds__(kThreads) void orthogonal_parts_kernel(SourceArgs A
 struct Parts {
   _Float16* p;
   int64_t ld, batch, rows, cols;
-  __device__ __forceinline__ _Float16* at(int64_t row, int64_t col) const { return p + (int64_t)blockIdx.z * batch + row * ld + 2 * col; }
+  __device__ __forceinline__ _Float16* at(int64_t matrix, int64_t row, int64_t col) const { return p + matrix * batch + row * ld + 2 * col; }
   // Eight numbers of a row; zeros behind its end.
-  __device__ __forceinline__ void put(int64_t row, int64_t col, const float (&v)[kVec]) const {
+  __device__ __forceinline__ void put(int64_t matrix, int64_t row, int64_t col, const float (&v)[kVec]) const {
     float w[kVec];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) w[e] = col + e < cols ? v[e] : 0.0f;
-    put_parts(at(row, col), w);
+    put_parts(at(matrix, row, col), w);
   }
   __device__ __forceinline__ bool holds(int64_t row, int64_t col) const { return row < rows && 2 * col < ld; }
 };
@@ -139,14 +144,14 @@ struct SymmetricOut {
     const Turned turned = {(float*)lds};
     p.for_eights(m0, n0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
       float x[kVec] = {};
-      if (SQUARE && a.holds(j, i)) get_parts(a.at(j, i), x);
+      if (SQUARE && a.holds(j, i)) get_parts(a.at(p.matrix, j, i), x);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) v[e] = SQUARE ? cb * x[e] + (cc / kUnit) * v[e] : v[e] * (1.0f / kUnit);
-      if (to.holds(j, i)) to.put(j, i, v);
+      if (to.holds(j, i)) to.put(p.matrix, j, i, v);
       if (both) turned.put(i, v);
     }, [&](int64_t i0, int64_t j0) {
       if (both) turned.take(i0, j0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
-        if (to.holds(i, j)) to.put(i, j, v);
+        if (to.holds(i, j)) to.put(p.matrix, i, j, v);
       });
     });
   }
@@ -159,50 +164,283 @@ struct NextOut {
     p.for_eights(m0, n0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
       if (j >= whole(to.rows, kPartsStep) || 2 * i >= to.ld) return;
       float o[kVec] = {};
-      if (j < to.rows) get_parts(x.at(j, i), o);
+      if (j < to.rows) get_parts(x.at(p.matrix, j, i), o);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) o[e] = j < to.rows ? ca * o[e] + v[e] * (1.0f / kUnit) : 0.0f;
-      to.put(j, i, o);
+      to.put(p.matrix, j, i, o);
     });
   }
 };
 // The last X', rounded once, or the parameters stepped with it.
+template <int TYPE, bool STEP>
+__device__ __forceinline__ void put_last(ElemT<TYPE>* at, int n, const float (&o)[kVec], float eta, float shrink) {
+  if constexpr (STEP) {
+    float w[kVec];
+    to_f32<TYPE>(load_raw<TYPE>(at, n), w);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) w[e] = shrink * w[e] - eta * o[e];
+    store_raw<TYPE>(at, from_f32<TYPE>(w), n);
+  } else {
+    store_raw<TYPE>(at, from_f32<TYPE>(o), n);
+  }
+}
 template <int TYPE, bool STEP, bool TALL>
 struct LastOut {
   Parts x;
   ElemT<TYPE>* out;
   int64_t stride, matrix_stride;
   float ca, eta, shrink;
-  __device__ __forceinline__ void put(int64_t row, int64_t col, int64_t cols, const float (&o)[kVec]) const {
-    ElemT<TYPE>* at = out + (int64_t)blockIdx.z * matrix_stride + row * stride + col;
-    const int n = (int)min((int64_t)kVec, cols - col);
-    if constexpr (STEP) {
-      float w[kVec];
-      to_f32<TYPE>(load_raw<TYPE>(at, n), w);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) w[e] = shrink * w[e] - eta * o[e];
-      store_raw<TYPE>(at, from_f32<TYPE>(w), n);
-    } else {
-      store_raw<TYPE>(at, from_f32<TYPE>(o), n);
-    }
+  __device__ __forceinline__ void put(int64_t matrix, int64_t row, int64_t col, int64_t cols, const float (&o)[kVec]) const {
+    put_last<TYPE, STEP>(out + matrix * matrix_stride + row * stride + col, (int)min((int64_t)kVec, cols - col), o, eta, shrink);
   }
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
     const Turned turned = {(float*)lds};
     p.for_eights(m0, n0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
       float o[kVec] = {};
       const bool holds = j < x.rows && i < x.cols;
-      if (holds) get_parts(x.at(j, i), o);
+      if (holds) get_parts(x.at(p.matrix, j, i), o);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) o[e] = (ca * o[e] + v[e] * (1.0f / kUnit)) * (1.0f / kUnit);
       if (TALL) turned.put(i, o);
-      else if (holds) put(j, i, x.cols, o);
+      else if (holds) put(p.matrix, j, i, x.cols, o);
     }, [&](int64_t i0, int64_t j0) {
       if (TALL) turned.take(i0, j0, [&](int64_t i, int64_t j, float (&o)[kVec]) {
-        if (i < x.cols && j < x.rows) put(i, j, x.rows, o);
+        if (i < x.cols && j < x.rows) put(p.matrix, i, j, x.rows, o);
       });
     });
   }
 };
+
+// ---- small matrices ------------------------------------------------------------------------------------------------------------
+
+// A matrix that fits LDS beside its A: one work-group takes all steps, without a launch between the products.  X and A lie there as
+// rows of parts; B takes A's place.  Sides are whole blocks of 32, zeros behind the matrix, and a wave has a block of 32 x 32 of each product
+// (kSmallBlocks of X').  What bounds it is LDS: a block reads 4 KiB for three matrix instructions.
+//
+// 16 bytes behind each row, so that sixteen rows that are read side by side lie in different banks.
+constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / kWave, kSmallBlocks = 2, kSmallVecs = 4;
+constexpr int64_t kSmallLds = 156 << 10;
+constexpr int64_t small_row(int64_t cols) { return whole(cols, 32) * 4 + 16; }
+inline int64_t small_bytes(int64_t n, int64_t m) { return whole(n, 32) * (small_row(m) + small_row(n)); }
+inline bool is_small(int64_t n, int64_t m) {
+  return n <= 128 && m <= 512 && small_bytes(n, m) <= kSmallLds && whole(n, 32) / 32 * (whole(m, 32) / 32) <= kSmallWaves * kSmallBlocks &&
+         std::max(n * ceil_div(m, kVec), m * ceil_div(n, kVec)) <= kSmallThreads * kSmallVecs;
+}
+
+template <int TYPE>
+struct SmallArgs {
+  SourceArgs S;                                    // g, momentum
+  ElemT<TYPE>* out;
+  int n, m, steps;
+  float eta, shrink;
+  float coefficients[3 * QA_ORTHOGONAL_STEPS_MAX];
+};
+
+__device__ __forceinline__ char* small_at(char* p, int pitch, int row, int byte) { return p + row * pitch + byte; }
+__device__ __forceinline__ void small_put(char* p, int pitch, int row, int col, const float (&v)[kVec]) {
+  _Float16 hi[kVec], lo[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) split_f16(v[i], hi[i], lo[i]);
+  __builtin_memcpy(__builtin_assume_aligned(small_at(p, pitch, row, 4 * col), 16), hi, sizeof hi);
+  __builtin_memcpy(__builtin_assume_aligned(small_at(p, pitch, row, 4 * col + 16), 16), lo, sizeof lo);
+}
+__device__ __forceinline__ void small_put(char* p, int pitch, int row, int col, float v) {
+  _Float16 hi, lo;
+  split_f16(v, hi, lo);
+  *(_Float16*)small_at(p, pitch, row, col / kVec * 32 + col % kVec * 2) = hi;
+  *(_Float16*)small_at(p, pitch, row, col / kVec * 32 + col % kVec * 2 + 16) = lo;
+}
+__device__ __forceinline__ void small_get(char* p, int pitch, int row, int col, float (&v)[kVec]) {
+  _Float16 hi[kVec], lo[kVec];
+  __builtin_memcpy(hi, __builtin_assume_aligned(small_at(p, pitch, row, 4 * col), 16), sizeof hi);
+  __builtin_memcpy(lo, __builtin_assume_aligned(small_at(p, pitch, row, 4 * col + 16), 16), sizeof lo);
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) v[i] = (float)hi[i] + (float)lo[i];
+}
+
+// One block of sums over k, a multiple of 32: rows a0 ... of A and b0 ... of B, or (COLUMNS) columns a0 ... of A, whose rows k are.
+template <bool COLUMNS>
+__device__ __forceinline__ f32x16 small_block(char* a, int a_pitch, int a0, char* b, int b_pitch, int b0, int k) {
+  const int lane = threadIdx.x % kWave, half = lane / 32;
+  f32x16 acc = {}, more = {};                      // two, as a sum waits for the one before
+  const char *a_at[2][2], *b_at[2][2];             // k = 0 and 16 of a row, or four k and the next four; hi and lo
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      b_at[h][p] = small_at(b, b_pitch, b0 + lane % 32, h * 64 + half * 32 + p * 16);
+      a_at[h][p] = COLUMNS ? small_at(a, a_pitch, 8 * half + 4 * h + (lane % 16 >> 2), (a0 + (lane & 16) + 4 * (lane & 3)) / 8 * 32 + p * 16) + (lane & 1) * 8
+                           : small_at(a, a_pitch, a0 + lane % 32, h * 64 + half * 32 + p * 16);
+    }
+#pragma unroll 1
+  for (int s = 0; s < k / 32; ++s) {
+    u32x4 x[2][2], y[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        y[h][p] = *reinterpret_cast<const u32x4*>(b_at[h][p] + s * 128);
+        if constexpr (COLUMNS) {
+          s16x4 part[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(a_at[e][p] + (2 * s + h) * 16 * a_pitch));
+          __builtin_memcpy(&x[h][p], part, sizeof part);
+        } else {
+          x[h][p] = *reinterpret_cast<const u32x4*>(a_at[h][p] + s * 128);
+        }
+      }
+    const auto times = [&](const u32x4& i, const u32x4& j, f32x16& c) {
+      c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, i), __builtin_bit_cast(f16x8, j), c, 0, 0, 0);
+    };
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      times(x[h][0], y[h][0], acc);
+      times(x[h][0], y[h][1], more);
+      times(x[h][1], y[h][0], more);
+    }
+  }
+  return acc + more;
+}
+// each(quarter, first of eight i within the block, j, sums)
+template <class Each>
+__device__ __forceinline__ void small_eights(const f32x16& acc, const Each& each) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    float v[kVec];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const auto both = __builtin_amdgcn_permlane32_swap(as_u32(acc[8 * q + e]), as_u32(acc[8 * q + 4 + e]), false, false);
+      v[e] = as_f32(both[0]);
+      v[4 + e] = as_f32(both[1]);
+    }
+    each(q, 16 * q + 8 * ((int)threadIdx.x % kWave / 32), (int)threadIdx.x % 32, v);
+  }
+}
+
+// BYTES: half of a compute unit's LDS, or all of it.
+template <int TYPE, bool STEP, bool TALL, int BYTES>
+__global__ __launch_bounds__(kSmallThreads) void orthogonal_small_kernel(SmallArgs<TYPE> A) {
+  __shared__ __attribute__((aligned(16))) char lds[BYTES];
+  __shared__ double sums[kSmallWaves];
+  const int np = (A.n + 31) / 32 * 32, mp = (A.m + 31) / 32 * 32, x_pitch = mp * 4 + 16, a_pitch = np * 4 + 16;
+  char* const x = lds;
+  char* const a = lds + np * x_pitch;
+  const int wave = threadIdx.x / kWave, across = (A.S.M.cols + kVec - 1) / kVec, vecs = (int)A.S.M.rows * across;
+  const int64_t base = (int64_t)blockIdx.x * A.S.M.matrix_stride;
+  float u[kSmallVecs][kVec];
+  double s = 0.0;
+#pragma unroll
+  for (int k = 0; k < kSmallVecs; ++k) {
+    const int i = k * kSmallThreads + threadIdx.x, r = i / across, c = i % across * kVec;
+    if (i >= vecs) continue;
+    const int n = min(kVec, (int)A.S.M.cols - c);
+    source8<TYPE, true>(A.S, base + r * A.S.M.stride + c, n, u[k]);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      u[k][e] = e < n ? u[k][e] : 0.0f;
+      s += (double)u[k][e] * (double)u[k][e];
+    }
+  }
+  s = wave_sum_f64(s);
+  if (threadIdx.x % kWave == 0) sums[wave] = s;
+  for (int i = threadIdx.x; i < np * x_pitch / 16; i += kSmallThreads) reinterpret_cast<u32x4*>(x)[i] = u32x4{};
+  __syncthreads();
+  double all = 0.0;
+#pragma unroll
+  for (int w = 0; w < kSmallWaves; ++w) all += sums[w];
+  const double scale = scale_for(all);
+#pragma unroll
+  for (int k = 0; k < kSmallVecs; ++k) {
+    const int i = k * kSmallThreads + threadIdx.x, r = i / across, c = i % across * kVec;
+    if (i >= vecs) continue;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) u[k][e] = (float)((double)u[k][e] * scale);
+    if constexpr (!TALL) {
+      small_put(x, x_pitch, r, c, u[k]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        if (c + e < A.n) small_put(x, x_pitch, c + e, r, u[k][e]);
+    }
+  }
+  __syncthreads();
+
+  // All blocks of A are computed, those that mirror others too: there is a wave for each, and a mirrored write takes longer.
+  const int nb = np / 32, mb = mp / 32, br = wave / nb, bc = wave % nb;
+  const bool has = br < nb;
+  const auto put_a = [&](int i, int j, const float (&v)[kVec]) { small_put(a, a_pitch, 32 * bc + j, 32 * br + i, v); };
+  for (int step = 0; step < A.steps; ++step) {
+    const float ca = A.coefficients[3 * step], cb = A.coefficients[3 * step + 1], cc = A.coefficients[3 * step + 2];
+    if (has) {
+      const f32x16 acc = small_block<false>(x, x_pitch, 32 * br, x, x_pitch, 32 * bc, mp);
+      small_eights(acc, [&](int, int i, int j, float (&v)[kVec]) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = v[e] * (1.0f / kUnit);
+        put_a(i, j, v);
+      });
+    }
+    __syncthreads();
+    f32x16 square = {};
+    if (has) square = small_block<false>(a, a_pitch, 32 * br, a, a_pitch, 32 * bc, np);
+    float b[2][kVec];
+    if (has)
+      small_eights(square, [&](int q, int i, int j, float (&v)[kVec]) {
+        float w[kVec];
+        small_get(a, a_pitch, 32 * bc + j, 32 * br + i, w);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) b[q][e] = cb * w[e] + (cc / kUnit) * v[e];
+      });
+    __syncthreads();
+    if (has) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) put_a(16 * q + 8 * ((int)threadIdx.x % kWave / 32), (int)threadIdx.x % 32, b[q]);
+    }
+    __syncthreads();
+    const bool last = step + 1 == A.steps;
+    float next[kSmallBlocks][2][kVec];
+#pragma unroll
+    for (int k = 0; k < kSmallBlocks; ++k) {
+      const int block = k * kSmallWaves + wave, bm = block / nb, bn = block % nb;
+      if (block >= nb * mb) continue;
+      const f32x16 acc = small_block<true>(x, x_pitch, 32 * bm, a, a_pitch, 32 * bn, np);
+      small_eights(acc, [&](int q, int i, int j, float (&v)[kVec]) {
+        float w[kVec];
+        small_get(x, x_pitch, 32 * bn + j, 32 * bm + i, w);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) next[k][q][e] = ca * w[e] + v[e] * (1.0f / kUnit);
+      });
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSmallBlocks; ++k) {
+      const int block = k * kSmallWaves + wave, bm = block / nb, bn = block % nb;
+      if (block >= nb * mb) continue;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int i = 32 * bm + 16 * q + 8 * ((int)threadIdx.x % kWave / 32), j = 32 * bn + (int)threadIdx.x % 32;
+        // Behind the last step X' is wanted as it is: binary32 in the place of the parts.
+        if (last) {
+          __builtin_memcpy(__builtin_assume_aligned(small_at(x, x_pitch, j, 4 * i), 16), next[k][q], 16);
+          __builtin_memcpy(__builtin_assume_aligned(small_at(x, x_pitch, j, 4 * i + 16), 16), next[k][q] + 4, 16);
+        } else {
+          small_put(x, x_pitch, j, i, next[k][q]);
+        }
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int k = 0; k < kSmallVecs; ++k) {
+    const int i = k * kSmallThreads + threadIdx.x, r = i / across, c = i % across * kVec;
+    if (i >= vecs) continue;
+    float o[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e)
+      o[e] = *reinterpret_cast<const float*>(TALL ? small_at(x, x_pitch, min(c + e, A.n - 1), r * 4) : small_at(x, x_pitch, r, (c + e) * 4)) * (1.0f / kUnit);
+    put_last<TYPE, STEP>(A.out + base + r * A.S.M.stride + c, min(kVec, (int)A.S.M.cols - c), o, A.eta, A.shrink);
+  }
+}
 
 // ---- the steps ---------------------------------------------------------------------------------------------------------------
 
@@ -239,6 +477,25 @@ template <int TYPE, bool STEP, bool TALL>
 int orthogonal_launch(const qa_matrices& M, const void* g, float* momentum, void* out, float mu, int nesterov, int steps,
                       const float* coefficients, float eta, float shrink, char* ws, hipStream_t stream) {
   const Plan P = plan_of(M);
+  constexpr float usual[3] = {3.4445f, -4.7750f, 2.0315f};
+  if (is_small(P.n, P.m)) {
+    SmallArgs<TYPE> A = {};
+    A.S.M = M;
+    A.S.g = g;
+    A.S.momentum = momentum;
+    A.S.mu = mu;
+    A.S.nesterov = nesterov;
+    A.out = (ElemT<TYPE>*)out;
+    A.n = (int)P.n;
+    A.m = (int)P.m;
+    A.steps = steps;
+    A.eta = eta;
+    A.shrink = shrink;
+    for (int i = 0; i < 3 * steps; ++i) A.coefficients[i] = coefficients ? coefficients[i] : usual[i % 3];
+    const auto kernel = small_bytes(P.n, P.m) <= kSmallLds / 2 ? orthogonal_small_kernel<TYPE, STEP, TALL, kSmallLds / 2> : orthogonal_small_kernel<TYPE, STEP, TALL, kSmallLds>;
+    kernel<<<(unsigned)M.count, kSmallThreads, 0, stream>>>(A);
+    return launch_status();
+  }
   Parts x[2], ab[2];
   for (int i = 0; i < 2; ++i) {
     x[i] = {(_Float16*)(ws + i * P.x), 2 * P.mp, P.np * 2 * P.mp, P.n, P.m};
@@ -263,7 +520,6 @@ int orthogonal_launch(const qa_matrices& M, const void* g, float* momentum, void
   orthogonal_parts_kernel<TYPE, TALL><<<dim3((unsigned)ceil_div(M.cols, 64), (unsigned)ceil_div(M.rows, 64), (unsigned)M.count), kThreads, 0, stream>>>(S);
   if (const int rc = launch_status()) return rc;
 
-  constexpr float usual[3] = {3.4445f, -4.7750f, 2.0315f};
   for (int s = 0, now = 0; s < steps; ++s, now ^= 1) {
     const float* c = coefficients ? coefficients + 3 * s : usual;
     if (const int rc = multiply<kRowsOfParts, kRowsOfParts, true>(x[now], x[now], P.m, M.count, SymmetricOut<false>{a, a, 0.0f, 0.0f}, stream)) return rc;

@@ -31,13 +31,13 @@ constexpr bool in_rows(Lies l) { return l <= kHiOfRows; }
 struct Operand {
   const void* p;                                   // 16-byte aligned
   int64_t ld;                                      // elements between rows, a multiple of 8, < 2^22
-  int64_t batch;                                   // elements between matrices (gridDim.z)
+  int64_t batch;                                   // elements between matrices
   int64_t n;                                       // how many i there are; past them the last ones are read again
 };
 struct ProductArgs {
   Operand a, b;
-  int steps, split_steps;                          // of k in all, and of one split (gridDim.y)
-  unsigned tiles_m, tiles_n;
+  int steps;                                       // of k
+  unsigned tiles_m, tiles_n, tiles;                // tiles: of one matrix
 };
 
 // Brings SIDE values of i and STEP of k to LDS, straight from memory, 16 bytes per lane.
@@ -58,9 +58,9 @@ struct Bringer {
   int64_t advance;
   uint32_t off[kLoads];
 
-  __device__ __forceinline__ void begin(const Operand& O, int64_t i0, int first_step, int wave) {
+  __device__ __forceinline__ void begin(const Operand& O, int64_t matrix, int64_t i0, int first_step, int wave) {
     const int lane = threadIdx.x % kWave;
-    const char* p = (const char*)O.p + (int64_t)blockIdx.z * O.batch * 2;
+    const char* p = (const char*)O.p + matrix * O.batch * 2;
     if constexpr (in_rows(LIES)) {
       advance = LIES == kHiOfRows ? 128 : 64;
       at = p + i0 * O.ld * 2 + first_step * advance;
@@ -151,6 +151,7 @@ struct Product {
   Reader<LA, kM, kStep, FM> read_a;
   Reader<LB, kN, kStep, FN> read_b;
   int to_load, wave;
+  int64_t matrix;                                  // which of the batch
 
   // Instructions [FROM, TO) of a step's; behind the last one go on, past the last step to itself.
   template <int FROM, int TO>
@@ -221,17 +222,16 @@ struct Product {
 #pragma unroll
     for (int j = 0; j < FN; ++j) p.b[0][j] = b_next[j];
   }
-  // Sums of split blockIdx.y, 0 where it has no steps.
-  __device__ __forceinline__ void run(const ProductArgs& A, int64_t m0, int64_t n0, char* lds) {
+  // Sums over `steps` steps of k, 1 at least, from step `first` on.
+  __device__ __forceinline__ void run(const ProductArgs& A, int64_t matrix_, int64_t m0, int64_t n0, int first, int steps, char* lds) {
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    matrix = matrix_;
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
-    const int first = (int)blockIdx.y * A.split_steps, steps = min(A.steps - first, A.split_steps);
-    if (steps <= 0) return;
-    bring_a.begin(A.a, m0, first, wave);
-    bring_b.begin(A.b, n0, first, wave);
+    bring_a.begin(A.a, matrix, m0, first, wave);
+    bring_b.begin(A.b, matrix, n0, first, wave);
     read_a.begin(wave % WM * FM);
     read_b.begin(wave / WM * FN);
     to_load = steps;
@@ -311,11 +311,14 @@ struct Turned {
 };
 
 // Consecutive work-groups go to the eight dies in turn.  Each die takes tiles that lie together, in bands eight tiles wide,
-// so that its cache is asked for the same rows.  LOWER: tiles on and below the diagonal only.
-template <bool LOWER>
-__device__ __forceinline__ void tile_of(const ProductArgs& A, unsigned& tm, unsigned& tn) {
+// so that its cache is asked for the same rows.
+__device__ __forceinline__ unsigned on_its_die() {
   const unsigned die = blockIdx.x % 8, each = gridDim.x / 8, more = gridDim.x % 8;
-  const unsigned tile = die * each + min(die, more) + blockIdx.x / 8;
+  return die * each + min(die, more) + blockIdx.x / 8;
+}
+// LOWER: tiles on and below the diagonal only.
+template <bool LOWER>
+__device__ __forceinline__ void tile_of(const ProductArgs& A, unsigned tile, unsigned& tm, unsigned& tn) {
   if constexpr (LOWER) {
     unsigned r = (unsigned)((__builtin_sqrtf(8.0f * (float)tile + 1.0f) - 1.0f) * 0.5f);
     while ((r + 1) * (r + 2) / 2 <= tile) ++r;
@@ -329,23 +332,29 @@ __device__ __forceinline__ void tile_of(const ProductArgs& A, unsigned& tm, unsi
   }
 }
 
+// A work-group per tile.
 template <class P, bool LOWER, class Epilogue>
 __global__ __launch_bounds__(P::kGroup, P::kWavesPerSimd) void product_kernel(ProductArgs A, Epilogue out) {
   __shared__ __attribute__((aligned(1024))) char lds[P::kBuffers * P::kBuffer];
   unsigned tm, tn;
-  tile_of<LOWER>(A, tm, tn);
+  tile_of<LOWER>(A, on_its_die(), tm, tn);
   const int64_t m0 = (int64_t)tm * P::kM, n0 = (int64_t)tn * P::kN;
   P p;
-  p.run(A, m0, n0, lds);
+  p.run(A, blockIdx.y, m0, n0, 0, A.steps, lds);
   out(p, p.wave_m(m0), p.wave_n(n0), lds + p.wave * (P::kBuffers * P::kBuffer / P::kWavesHere));
 }
 
 // Launches tiles of the given form over all of A and B; k: how many there are, zeros up to a whole step.
+template <class P, bool LOWER>
+ProductArgs product_args(const Operand& a, const Operand& b, int64_t k) {
+  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN), 0};
+  A.tiles = LOWER ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n;
+  return A;
+}
 template <class P, bool LOWER = false, class Epilogue>
 int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream) {
-  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), (int)ceil_div(k, P::kStep), (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN)};
-  const unsigned tiles = LOWER ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n;
-  product_kernel<P, LOWER><<<dim3(tiles, 1, batch), P::kGroup, 0, stream>>>(A, out);
+  const ProductArgs A = product_args<P, LOWER>(a, b, k);
+  product_kernel<P, LOWER><<<dim3(A.tiles, batch), P::kGroup, 0, stream>>>(A, out);
   return launch_status();
 }
 template <bool BF16, Lies LA, Lies LB> using Product256 = Product<BF16, LA, LB, 2, 2, 4, 4>;
