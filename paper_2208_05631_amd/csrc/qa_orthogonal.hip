@@ -12,12 +12,13 @@
 #include <algorithm>
 
 #include "qa_product.h"
+#include "qa_product_plan.h"
 
 namespace qa {
 namespace {
 
 constexpr float kUnit = 1024.0f;                   // a stored number is so many times the number it stands for
-constexpr int kNormBlocks = 128;
+constexpr int kNormBlocks = 1024;                 // work-groups that add one matrix's squares
 
 // ---- the matrix's norm, and its parts ---------------------------------------------------------------------------------
 
@@ -82,7 +83,11 @@ __global__ __launch_bounds__(kThreads) void orthogonal_parts_kernel(SourceArgs A
   __shared__ float tile[TALL ? kSide : 1][kSide + 1];
   __shared__ double sums[kWaves];
   const int64_t z = blockIdx.z, r0 = (int64_t)blockIdx.y * kSide, c0 = (int64_t)blockIdx.x * kSide, base = z * A.M.matrix_stride;
-  const double part = wave_sum_f64((int)threadIdx.x < A.norm_blocks ? A.partial[z * A.norm_blocks + threadIdx.x] : 0.0);
+  double part = 0.0;
+#pragma unroll
+  for (int b = 0; b < kNormBlocks; b += kThreads)
+    if (b + (int)threadIdx.x < A.norm_blocks) part += A.partial[z * A.norm_blocks + b + threadIdx.x];
+  part = wave_sum_f64(part);
   if (threadIdx.x % kWave == 0) sums[threadIdx.x / kWave] = part;
   __syncthreads();
   const double all = (sums[0] + sums[1]) + (sums[2] + sums[3]);
@@ -446,6 +451,7 @@ __global__ __launch_bounds__(kSmallThreads) void orthogonal_small_kernel(SmallAr
 
 struct Plan {
   int64_t n, m, np, mp;                            // sides, and with whole steps
+  int lanes, norm_blocks;                          // of the squares' sums
   size_t x, a, norms, bytes;                       // of one buffer for all matrices, and of everything
 };
 Plan plan_of(const qa_matrices& M) {
@@ -456,7 +462,10 @@ Plan plan_of(const qa_matrices& M) {
   P.mp = whole(P.m, kPartsStep);
   P.x = (size_t)whole(M.count * P.np * 2 * P.mp * 2, 256);
   P.a = (size_t)whole(M.count * P.n * 2 * P.np * 2, 256);
-  P.norms = (size_t)whole(M.count * kNormBlocks * 8, 256);
+  P.lanes = 1;
+  while (P.lanes < kThreads && P.lanes * kVec < M.cols) P.lanes *= 2;
+  P.norm_blocks = (int)std::min<int64_t>(std::max<int64_t>(kNormBlocks / std::max<int64_t>(M.count, 1), 16), ceil_div(M.rows * P.lanes, kThreads));
+  P.norms = (size_t)whole(M.count * P.norm_blocks * 8, 256);
   P.bytes = 2 * P.x + 2 * P.a + P.norms;
   return P;
 }
@@ -464,13 +473,23 @@ Plan plan_of(const qa_matrices& M) {
 template <Lies LA, Lies LB, bool LOWER, class Epilogue>
 int multiply(const Parts& a, const Parts& b, int64_t k, int64_t count, const Epilogue& out, hipStream_t stream) {
   const Operand oa = {a.p, a.ld, a.batch, in_rows(LA) ? a.rows : a.cols}, ob = {b.p, b.ld, b.batch, in_rows(LB) ? b.rows : b.cols};
-  const auto tiles = [&](int64_t side) {
-    const int64_t tm = ceil_div(oa.n, side), tn = ceil_div(ob.n, side);
-    return count * (LOWER ? tm * (tm + 1) / 2 : tm * tn);
-  };
-  if (tiles(256) >= 192) return product_launch<Product256<false, LA, LB>, LOWER>(oa, ob, k, out, (unsigned)count, stream);
-  if (tiles(128) >= 128) return product_launch<Product128<false, LA, LB>, LOWER>(oa, ob, k, out, (unsigned)count, stream);
-  return product_launch<Product64<false, LA, LB>, LOWER>(oa, ob, k, out, (unsigned)count, stream);
+  // X' has many tiles, A and B have few.
+  constexpr unsigned kAllowed = LOWER ? ~0u : 1u << kTiles256 | 1u << kTiles128 | 1u << kTiles64Two;
+  const unsigned batch = (unsigned)count;
+  switch (tiles_for(kAllowed, oa.n, ob.n, ceil_div(k, kPartsStep), count, LOWER)) {
+    case kTiles256: return product_launch<Product<false, LA, LB, 2, 2, 4, 4>, LOWER>(oa, ob, k, out, batch, stream);
+    case kTiles128: return product_launch<Product<false, LA, LB, 2, 2, 2, 2>, LOWER>(oa, ob, k, out, batch, stream);
+    case kTiles64Two: return product_launch<Product<false, LA, LB, 2, 2, 1, 1, 2>, LOWER>(oa, ob, k, out, batch, stream);
+    default: break;
+  }
+  if constexpr (LOWER) {
+    switch (tiles_for(kAllowed, oa.n, ob.n, ceil_div(k, kPartsStep), count, LOWER)) {
+      case kTiles192: return product_launch<Product<false, LA, LB, 2, 2, 3, 3>, LOWER>(oa, ob, k, out, batch, stream);
+      case kTiles128Two: return product_launch<Product<false, LA, LB, 2, 2, 2, 2, 2>, LOWER>(oa, ob, k, out, batch, stream);
+      default: return product_launch<Product<false, LA, LB, 1, 1, 2, 2, 4>, LOWER>(oa, ob, k, out, batch, stream);
+    }
+  }
+  return QA_ERR_INVALID_ARG;                       // not reached: all that is allowed is above
 }
 
 template <int TYPE, bool STEP, bool TALL>
@@ -513,9 +532,8 @@ int orthogonal_launch(const qa_matrices& M, const void* g, float* momentum, void
   S.batch = x[0].batch;
   S.mu = mu;
   S.nesterov = nesterov;
-  S.lanes = 1;
-  while (S.lanes < kThreads && S.lanes * kVec < M.cols) S.lanes *= 2;
-  S.norm_blocks = (int)std::min<int64_t>(kNormBlocks, ceil_div(M.rows * S.lanes, kThreads));
+  S.lanes = P.lanes;
+  S.norm_blocks = P.norm_blocks;
   orthogonal_norm_kernel<TYPE><<<dim3(S.norm_blocks, (unsigned)M.count), kThreads, 0, stream>>>(S);
   orthogonal_parts_kernel<TYPE, TALL><<<dim3((unsigned)ceil_div(M.cols, 64), (unsigned)ceil_div(M.rows, 64), (unsigned)M.count), kThreads, 0, stream>>>(S);
   if (const int rc = launch_status()) return rc;

@@ -5,6 +5,7 @@
 // chunk of the vocabulary.  The backward pass multiplies the logits again, a piece of the vocabulary at a time, turns them into
 // c, the gradient of the logits, which is written once, as rows of binary16 parts, and multiplies that from both sides: dx = c w, dw = c^T x.
 #include <algorithm>
+#include <type_traits>
 
 #include "qa_product.h"
 #include "qa_softmax.h"
@@ -237,6 +238,16 @@ __global__ __launch_bounds__(kThreads) void output_join_kernel(ScoreArgs A, int6
 
 __global__ void output_clear_kernel(Scales* s) { s->most[threadIdx.x] = 0; }
 
+// One atomic per work-group (8192 of them, from all dies to one word, took 100 us).
+__device__ __forceinline__ void raise_most(uint32_t* to, uint32_t most) {
+  __shared__ uint32_t waves[kWaves];
+#pragma unroll
+  for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
+  if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) atomicMax(to, max(max(waves[0], waves[1]), max(waves[2], waves[3])));
+}
+
 // The largest |c| that a row can have: p <= 1, p |log p| <= 1 / e, and an entropy of at most log 2^24 < 17.
 __global__ __launch_bounds__(kThreads) void output_weights_kernel(RowArgs A, int64_t rows, Scales* scales) {
   uint32_t most = 0;
@@ -245,9 +256,7 @@ __global__ __launch_bounds__(kThreads) void output_weights_kernel(RowArgs A, int
     const uint32_t c = as_u32(fabsf(r.a) + 18.0f * fabsf(r.e));
     if (c < 0x7F800000u) most = max(most, c);
   }
-#pragma unroll
-  for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
-  if (threadIdx.x % kWave == 0) atomicMax(&scales->most[kOfC], most);
+  raise_most(&scales->most[kOfC], most);
 }
 
 // The largest finite magnitude of rows that count.
@@ -259,19 +268,30 @@ __global__ __launch_bounds__(kThreads) void output_most_kernel(const void* from,
   for (int64_t row = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; row < rows; row += (int64_t)gridDim.x * kWaves) {
     if (masked && !counts(row_of(A, row))) continue;
     const ElemT<TYPE>* p = (const ElemT<TYPE>*)from + row * stride;
-    for (int64_t c = lane * kVec; c < cols; c += kWave * kVec) {
+    constexpr int kAtOnce = 4;                     // reads that are on their way
+    int64_t c = lane * kVec;
+    for (; c + (kAtOnce - 1) * kWave * kVec + kVec <= cols; c += kAtOnce * kWave * kVec) {
+      Raw8<TYPE> raw[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) raw[k] = load_raw<TYPE>(p + c + k * kWave * kVec);
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        float v[kVec];
+        to_f32<TYPE>(raw[k], v);
+        most = max(most, finite_most(v));
+      }
+    }
+    for (; c < cols; c += kWave * kVec) {
       float v[kVec];
       to_f32<TYPE>(load_raw<TYPE>(p + c, (int)min((int64_t)kVec, cols - c)), v);
       most = max(most, finite_most(v));
     }
   }
-#pragma unroll
-  for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
-  if (lane == 0) atomicMax(&scales->most[which], most);
+  raise_most(&scales->most[which], most);
 }
 
 // c of a piece of the vocabulary, scaled, in rows of parts: zeros behind the piece, in rows that do not count, and in rows up to a whole step.
-template <bool SCALED>
+template <bool SCALED, bool ENTROPY>
 struct LogitsGradOut {
   LayerArgs L;                                     // vocab: of this piece
   RowArgs R;
@@ -282,30 +302,40 @@ struct LogitsGradOut {
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0, char*) const {
     const int exp = exponent_for(scales->most[kOfC]), lane = threadIdx.x % kWave;
     constexpr int FN = (int)(sizeof p.acc[0] / sizeof p.acc[0][0]);
-    Row r[FN];
+    float m[FN], log_sum[FN], a[FN], e[FN], h[FN];
     int x_exp[FN], here[FN];
     bool none[FN];
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t t = t0 + 32 * j + lane % 32;
-      r[j] = row_of(R, min(t, L.rows - 1));
+      const Row r = row_of(R, min(t, L.rows - 1));
+      m[j] = r.m;
+      log_sum[j] = r.log_sum * kLog2e;
+      a[j] = ldexpf(r.a, exp);
+      e[j] = ldexpf(r.e, exp) * kLn2;
+      h[j] = r.h * kLog2e;
       x_exp[j] = SCALED ? L.x_exp[min(t, L.rows - 1)] : 0;
-      none[j] = t >= L.rows || !counts(r[j]);
-      const int64_t at = r[j].at - first - v0;
-      here[j] = at >= 0 && at < P::kM ? (int)at : -1;
+      none[j] = t >= L.rows || !counts(r);
+      const int64_t at = r.at - first - v0;
+      here[j] = at >= 0 && at < P::kM ? (int)at : -kVec;
     }
     const int left = (int)max((int64_t)0, min((int64_t)P::kM, L.vocab - v0)), wide = (int)max((int64_t)0, min((int64_t)P::kM, ld / 2 - v0));
     p.for_eights(0, 0, [&](int64_t i, int64_t col, float (&z)[kVec]) {
       const int v = (int)i, j = (int)col / 32;
       float g[kVec];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        if (SCALED) z[e] = ldexpf(z[e], -(x_exp[j] + L.w_exp[min(v0 + v + e, L.vocab - 1)]));
-        const float lp = (z[e] - r[j].m) - r[j].log_sum, q = __builtin_amdgcn_exp2f(lp * kLog2e);
-        g[e] = -q * (r[j].a + r[j].e * (fmaxf(lp, kFar) + r[j].h));
-        if (v + e == here[j]) g[e] += r[j].a;
-        g[e] = none[j] || v + e >= left ? 0.0f : ldexpf(g[e], exp);
+      for (int k = 0; k < kVec; ++k) {
+        if (SCALED) z[k] = ldexpf(z[k], -(x_exp[j] + L.w_exp[min(v0 + v + k, L.vocab - 1)]));
+        const float lp = __builtin_fmaf(z[k] - m[j], kLog2e, -log_sum[j]), q = __builtin_amdgcn_exp2f(lp);      // in powers of two
+        g[k] = ENTROPY ? -q * (a[j] + e[j] * (fmaxf(lp, kFar) + h[j])) : -q * a[j];
       }
+      if (__any((unsigned)(here[j] - v) < kVec)) {           // few eights have a target
+#pragma unroll
+        for (int k = 0; k < kVec; ++k)
+          if (v + k == here[j]) g[k] += a[j];
+      }
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) g[k] = none[j] || v + k >= left ? 0.0f : g[k];
       const int64_t t = t0 + col;
       if (t < to_rows && v < wide) put_parts(c + t * ld + 2 * (v0 + v), g);
       __builtin_amdgcn_sched_barrier(0);           // or all exponents and addresses are held in registers at once
@@ -317,7 +347,7 @@ struct LogitsGradOut {
 template <int TYPE>
 struct GradOut {
   ElemT<TYPE>* out;
-  float* sums;                                     // NULL: none before this piece, and this is the last
+  float* sums;                                     // [split][rows][cols]; NULL: none before this piece, and this is the last
   const Scales* scales;
   int64_t stride, rows, cols;
   int which;                                       // the scale of the other operand, -1: none
@@ -328,7 +358,7 @@ struct GradOut {
       if (row >= rows || col >= cols) return;
       const int n = (int)min((int64_t)kVec, cols - col);
       ElemT<TYPE>* const at = out + row * stride + col;
-      float* const s = sums + row * cols + col;
+      float* const s = sums + (p.split * rows + row) * cols + col;
       float before[kVec] = {};
       if (add) {
         if (sums) to_f32<QA_F32>(load_raw<QA_F32>(s, n), before);
@@ -342,6 +372,24 @@ struct GradOut {
     });
   }
 };
+// dx from the splits' sums, in their order.
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void output_sum_kernel(const float* sums, int splits, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride) {
+  const int64_t across = ceil_div(cols, kVec), all = rows * across;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t row = i / across, col = i % across * kVec;
+    const int n = (int)min((int64_t)kVec, cols - col);
+    float v[kVec] = {};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      float w[kVec];
+      to_f32<QA_F32>(load_raw<QA_F32>(sums + (s * rows + row) * cols + col, n), w);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v[e] += w[e];
+    }
+    store_raw<TYPE>(out + row * stride + col, from_f32<TYPE>(v), n);
+  }
+}
 __global__ __launch_bounds__(kThreads) void output_zero_kernel(float* p, int64_t stride, int64_t rows, int64_t cols) {
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
     for (int64_t c = threadIdx.x; c < cols; c += kThreads) p[r * stride + c] = 0.0f;
@@ -361,12 +409,12 @@ struct Room {
 };
 
 // Which tiles multiply the logits: heights (vocabulary) of chunks, and widths (rows).
-enum { kTiles256, kTiles128, kTiles64 };
+enum { kTall256, kTall128, kTall64 };
 int logits_tiles(int64_t rows, int64_t vocab) {
-  if (rows <= 64) return kTiles64;
-  return ceil_div(rows, 256) * ceil_div(vocab, 256) >= 192 ? kTiles256 : kTiles128;
+  if (rows <= 64) return kTall64;
+  return ceil_div(rows, 256) * ceil_div(vocab, 256) >= 192 ? kTall256 : kTall128;
 }
-constexpr int64_t chunk_of(int tiles) { return tiles == kTiles256 ? 128 : 64; }
+constexpr int64_t chunk_of(int tiles) { return tiles == kTall256 ? 128 : 64; }
 
 // Equal pieces of n, whole tiles each, of at most `most`.
 int64_t piece_of(int64_t n, int64_t most) { return std::min(whole(n, kWholeStep), whole(ceil_div(n, ceil_div(n, most)), 256)); }
@@ -383,9 +431,10 @@ struct Plan {
   size_t m, s, sw, given;                          // scoring
   int64_t chunks;
   size_t scales, xc, wc, c, sums;                  // gradient: x and w as the products with c take them
-  int64_t hc, tp, vp;
+  int64_t hc, tp, vp, splits;
   size_t bytes;
 };
+bool has_large_tiles(int64_t m, int64_t n) { return ceil_div(m, 256) * ceil_div(n, 256) >= 192; }
 
 bool in_place(const void* p, int64_t stride) { return stride % 8 == 0 && stride < (int64_t(1) << 22) && aligned(p, 16); }
 
@@ -418,7 +467,12 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.xc = room.take(2 * P.parts * P.tp * P.hc);
     P.wc = room.take(2 * P.parts * P.vp * P.hc);
     P.c = room.take(2 * 2 * P.tp * P.vp);
-    P.sums = room.take(P.pieces > 1 ? 4 * L.rows * L.features : 0);
+    // dx has few tiles and sums over the vocabulary: splits of it, until every compute unit has two, of eight steps at least.
+    const int64_t tiles = ceil_div(L.rows, 128) * ceil_div(L.features, 128), step = type == QA_BF16 ? kWholeStep : kPartsStep;
+    const int64_t steps = ceil_div(std::min(P.piece, L.vocab), step);
+    P.splits = has_large_tiles(L.features, L.rows) ? 1 : std::max<int64_t>(1, std::min(512 / tiles, steps / 8));
+    P.splits = ceil_div(steps, ceil_div(steps, P.splits));       // none without steps in the first piece
+    P.sums = room.take(P.pieces > 1 || P.splits > 1 ? 4 * P.splits * L.rows * L.features : 0);
   }
   P.x_exp = room.take(type == QA_F32 ? 4 * L.rows : 0);
   P.w_exp = room.take(type == QA_F32 ? 4 * P.piece : 0);
@@ -450,8 +504,8 @@ template <int TYPE, class Epilogue>
 int logits_launch(const Operand& w, const Operand& x, int64_t features, int tiles, const Epilogue& out, hipStream_t stream) {
   constexpr bool kBf16 = TYPE == QA_BF16;
   constexpr Lies kLie = TYPE == QA_F32 ? kRowsOfParts : kRows;
-  if (tiles == kTiles256) return product_launch<Product256<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
-  if (tiles == kTiles128) return product_launch<Product128<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
+  if (tiles == kTall256) return product_launch<Product256<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
+  if (tiles == kTall128) return product_launch<Product128<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
   return product_launch<Product<kBf16, kLie, kLie, 4, 1, 2, 2>>(w, x, features, out, 1, stream);
 }
 
@@ -480,9 +534,9 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
 }
 
 template <Lies LA, Lies LB, class Epilogue>
-int grad_product(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, hipStream_t stream) {
-  if (ceil_div(a.n, 256) * ceil_div(b.n, 256) >= 192) return product_launch<Product256<false, LA, LB>>(a, b, k, out, 1, stream);
-  return product_launch<Product128<false, LA, LB>>(a, b, k, out, 1, stream);
+int grad_product(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, hipStream_t stream, int64_t splits = 1) {
+  if (has_large_tiles(a.n, b.n)) return product_launch<Product256<false, LA, LB>>(a, b, k, out, 1, stream);
+  return product_launch<Product128<false, LA, LB>>(a, b, k, out, 1, stream, splits);
 }
 
 struct GradCall {
@@ -501,7 +555,7 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
   int* const x_exp = (int*)(ws + P.x_exp);
   int* const w_exp = (int*)(ws + P.w_exp);
   Scales* const scales = (Scales*)(ws + P.scales);
-  const auto most_blocks = [](int64_t rows) { return (unsigned)std::min<int64_t>(2048, ceil_div(rows, kWaves)); };
+  const auto most_blocks = [](int64_t rows) { return (unsigned)std::min<int64_t>(1024, ceil_div(rows, kWaves)); };
   output_clear_kernel<<<1, 4, 0, stream>>>(scales);
   output_weights_kernel<<<(unsigned)std::min<int64_t>(256, ceil_div(L.rows, kThreads)), kThreads, 0, stream>>>(G.rows, L.rows, scales);
   if (TYPE != QA_F16 && G.dw) output_most_kernel<TYPE><<<most_blocks(L.rows), kThreads, 0, stream>>>(G.x, L.x_stride, L.rows, L.features, G.rows, true, scales, kOfX);
@@ -521,8 +575,11 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     const void* const from = (const ElemT<TYPE>*)G.w + first * L.w_stride;
     if (const int rc = logits_operand<TYPE>(from, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp, wo, stream)) return rc;
     _Float16* const c = (_Float16*)(ws + P.c);
-    const LogitsGradOut<TYPE == QA_F32> grad{LayerArgs{L.rows, vocab, x_exp, w_exp, nullptr}, G.rows, first, scales, c, 2 * P.vp, P.tp};
-    if (const int rc = logits_launch<TYPE>(wo, xo, L.features, P.tiles, grad, stream)) return rc;
+    const auto logits = [&](auto entropy) {
+      const LogitsGradOut<TYPE == QA_F32, decltype(entropy)::value> grad{LayerArgs{L.rows, vocab, x_exp, w_exp, nullptr}, G.rows, first, scales, c, 2 * P.vp, P.tp};
+      return logits_launch<TYPE>(wo, xo, L.features, P.tiles, grad, stream);
+    };
+    if (const int rc = G.rows.g_entropy ? logits(std::true_type()) : logits(std::false_type())) return rc;
     if (G.dx) {
       Operand wc = {from, L.w_stride, 0, L.features};
       if (TYPE != QA_F16 || !in_place(from, L.w_stride) || L.features % 8 || vocab % kWholeStep) {
@@ -530,11 +587,17 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
         const CopyArgs A = {from, L.w_stride, vocab, L.features, ws + P.wc, copied, whole(vocab, kWholeStep), nullptr, scales, kOfW, false, G.rows};
         if (const int rc = copy_launch<TYPE, kOneScale>(A, stream)) return rc;
       }
-      const GradOut<TYPE> out{(ElemT<TYPE>*)G.dx, P.pieces > 1 ? (float*)(ws + P.sums) : nullptr, scales, G.dx_stride, L.rows, L.features,
-                              TYPE == QA_F16 ? -1 : kOfW, first > 0, first + P.piece >= L.vocab};
+      const bool last = first + P.piece >= L.vocab;
+      const GradOut<TYPE> out{(ElemT<TYPE>*)G.dx, P.pieces > 1 || P.splits > 1 ? (float*)(ws + P.sums) : nullptr, scales, G.dx_stride, L.rows, L.features,
+                              TYPE == QA_F16 ? -1 : kOfW, first > 0, last && P.splits == 1};
       // One part of c has 11 bits, which is little beside bfloat16's 8, but as much as binary16's own.
       constexpr Lies kC = TYPE == QA_BF16 ? kHiOfRows : kRowsOfParts;
-      if (const int rc = grad_product<kColumnsOf, kC>(wc, Operand{c, 2 * P.vp, 0, L.rows}, vocab, out, stream)) return rc;
+      if (const int rc = grad_product<kColumnsOf, kC>(wc, Operand{c, 2 * P.vp, 0, L.rows}, vocab, out, stream, P.splits)) return rc;
+      if (last && P.splits > 1) {
+        output_sum_kernel<TYPE><<<(unsigned)std::min<int64_t>(ceil_div(L.rows * ceil_div(L.features, kVec), kThreads), 4096), kThreads, 0, stream>>>(
+            (const float*)(ws + P.sums), P.splits, L.rows, L.features, (ElemT<TYPE>*)G.dx, G.dx_stride);
+        if (const int rc = launch_status()) return rc;
+      }
     }
     if (G.dw) {
       const GradOut<QA_F32> out{G.dw + first * G.dw_stride, nullptr, scales, G.dw_stride, vocab, L.features, TYPE == QA_F16 ? -1 : kOfX, G.accumulate != 0, true};

@@ -36,8 +36,8 @@ struct Operand {
 };
 struct ProductArgs {
   Operand a, b;
-  int steps;                                       // of k
-  unsigned tiles_m, tiles_n, tiles;                // tiles: of one matrix
+  int steps, split_steps;                          // of k, and of one split of them
+  unsigned splits, tiles_m, tiles_n, tiles;        // tiles: of one matrix
 };
 
 // Brings SIDE values of i and STEP of k to LDS, straight from memory, 16 bytes per lane.
@@ -96,7 +96,7 @@ struct Bringer {
 template <Lies LIES, int SIDE, int STEP, int BLOCKS>
 struct Reader {
   static constexpr int kPitch = Bringer<LIES, SIDE, STEP, 1>::kPitch;
-  static constexpr bool kMixed = !in_rows(LIES) && SIDE < 128;       // lo lies among hi: of 16 chunks eight are hi
+  static constexpr bool kMixed = !in_rows(LIES) && SIDE / 8 % 16 != 0;       // lo lies among hi in groups of 16 chunks
   int lane_at[in_rows(LIES) || kMixed ? 2 * BLOCKS : BLOCKS];
   __device__ __forceinline__ void begin(int block0) {
     const int lane = threadIdx.x % kWave;
@@ -130,18 +130,19 @@ struct Reader {
   }
 };
 
-// WM x WN waves, FM x FN blocks of 32 x 32 each.  Four buffers: while step s is multiplied, s + 1 is there, s + 2 on its way, and s + 3
+// WM x WN waves, FM x FN blocks of 32 x 32 each.  SHARE > 1: so many times the waves, each lot with every SHARE-th step and buffers of its own;
+// the first lot gets all sums.  Four buffers: while step s is multiplied, s + 1 is there, s + 2 on its way, and s + 3
 // sets out for the buffer that step s - 1 had.
-template <bool BF16, Lies LA, Lies LB, int WM, int WN, int FM, int FN>
+template <bool BF16, Lies LA, Lies LB, int WM, int WN, int FM, int FN, int SHARE = 1>
 struct Product {
-  static constexpr int kM = 32 * WM * FM, kN = 32 * WN * FN, kWavesHere = WM * WN, kGroup = kWavesHere * kWave;
-  static constexpr int kWavesPerSimd = FM * FN == 16 ? 1 : 2;        // of registers
+  static constexpr int kM = 32 * WM * FM, kN = 32 * WN * FN, kWavesHere = WM * WN, kGroup = SHARE * kWavesHere * kWave;
+  static constexpr int kWavesPerSimd = FM * FN == 16 ? 1 : SHARE > 1 ? SHARE : 2;        // of registers
   static constexpr int kPA = parts_in(LA), kPB = parts_in(LB);
   static constexpr int kStep = kPA * kPB == 1 ? kWholeStep : kPartsStep;
   static_assert(kPA <= kPB && !(kStep == kPartsStep && (LA == kRows || LA == kHiOfRows || LB == kRows || LB == kHiOfRows)), "forms that there are");
   typedef Bringer<LA, kM, kStep, kWavesHere> BringA;
   typedef Bringer<LB, kN, kStep, kWavesHere> BringB;
-  static constexpr int kBuffer = BringA::kBytes + BringB::kBytes, kBuffers = 4, kLoads = BringA::kLoads + BringB::kLoads;
+  static constexpr int kBuffer = BringA::kBytes + BringB::kBytes, kBuffers = 4, kLds = SHARE * kBuffers * kBuffer, kLoads = BringA::kLoads + BringB::kLoads;
   static constexpr int kLate = (kLoads + 1) / (kPA + 1);       // a step's loads behind the barrier; the others follow in the next step
 
   f32x16 acc[FM][FN];
@@ -151,7 +152,8 @@ struct Product {
   Reader<LA, kM, kStep, FM> read_a;
   Reader<LB, kN, kStep, FN> read_b;
   int to_load, wave;
-  int64_t matrix;                                  // which of the batch
+  int64_t matrix, split;                           // which of the batch, and of the splits of k
+  bool owns;                                       // whether this wave has the sums
 
   // Instructions [FROM, TO) of a step's; behind the last one go on, past the last step to itself.
   template <int FROM, int TO>
@@ -222,19 +224,28 @@ struct Product {
 #pragma unroll
     for (int j = 0; j < FN; ++j) p.b[0][j] = b_next[j];
   }
-  // Sums over `steps` steps of k, 1 at least, from step `first` on.
-  __device__ __forceinline__ void run(const ProductArgs& A, int64_t matrix_, int64_t m0, int64_t n0, int first, int steps, char* lds) {
+  // All steps of a tile's split, one at least.
+  __device__ __forceinline__ void run(const ProductArgs& A, int64_t matrix_, int64_t split_, int64_t m0, int64_t n0, char* all_lds) {
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int share = SHARE == 1 ? 0 : wave / kWavesHere;
+    wave -= share * kWavesHere;
+    owns = share == 0;
     matrix = matrix_;
+    split = split_;
+    const int begin = (int)split * A.split_steps, in_split = min(A.split_steps, A.steps - begin);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
-    bring_a.begin(A.a, matrix, m0, first, wave);
-    bring_b.begin(A.b, matrix, n0, first, wave);
+    bring_a.begin(A.a, matrix, m0, begin + min(share, in_split - 1), wave);
+    bring_b.begin(A.b, matrix, n0, begin + min(share, in_split - 1), wave);
+    bring_a.advance *= SHARE;
+    bring_b.advance *= SHARE;
+    char* const lds = all_lds + share * kBuffers * kBuffer;
+    const int steps = (in_split - share + SHARE - 1) / SHARE, all_steps = (in_split + SHARE - 1) / SHARE;       // this lot's, and the first one's
     read_a.begin(wave % WM * FM);
     read_b.begin(wave / WM * FN);
-    to_load = steps;
+    to_load = steps;                               // a lot without any brings the last one and leaves it
     int now = 0, then = kBuffer, late = 2 * kBuffer, last = 3 * kBuffer;
     load<0, kLoads>(lds + now);
     load<0, kLoads>(lds + then);
@@ -251,7 +262,29 @@ struct Product {
       late = last;
       last = free;
     }
+    if constexpr (SHARE > 1)
+      for (int s = max(steps, 0); s < all_steps; ++s) arrive<0>();
     arrive<0>();                                   // loads past the last step, before LDS is used for something else
+    if constexpr (SHARE > 1) {
+      constexpr int kPieces = (int)(sizeof acc / sizeof(f32x4));
+      f32x4 v[kPieces];
+      __builtin_memcpy(v, &acc, sizeof v);
+      f32x4* const at = (f32x4*)all_lds + threadIdx.x % (kWavesHere * kWave);
+      constexpr int kLot = kWavesHere * kWave * kPieces;
+      static_assert(SHARE * kLot * 16 <= kLds, "sums fit the buffers");
+      if (!owns) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) at[share * kLot + i * kWavesHere * kWave] = v[i];
+      }
+      __syncthreads();
+      if (owns) {
+#pragma unroll 1
+        for (int g = 1; g < SHARE; ++g)
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) v[i] += at[g * kLot + i * kWavesHere * kWave];
+        __builtin_memcpy(&acc, v, sizeof v);
+      }
+    }
   }
   __device__ __forceinline__ int64_t wave_m(int64_t m0) const { return m0 + wave % WM * 32 * FM; }
   __device__ __forceinline__ int64_t wave_n(int64_t n0) const { return n0 + wave / WM * 32 * FN; }
@@ -332,35 +365,31 @@ __device__ __forceinline__ void tile_of(const ProductArgs& A, unsigned tile, uns
   }
 }
 
-// A work-group per tile.
+// A work-group per tile and split.
 template <class P, bool LOWER, class Epilogue>
 __global__ __launch_bounds__(P::kGroup, P::kWavesPerSimd) void product_kernel(ProductArgs A, Epilogue out) {
-  __shared__ __attribute__((aligned(1024))) char lds[P::kBuffers * P::kBuffer];
+  __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
+  const unsigned tile = on_its_die(), which = tile / A.tiles, matrix = which / A.splits;
   unsigned tm, tn;
-  tile_of<LOWER>(A, on_its_die(), tm, tn);
+  tile_of<LOWER>(A, tile - which * A.tiles, tm, tn);
   const int64_t m0 = (int64_t)tm * P::kM, n0 = (int64_t)tn * P::kN;
   P p;
-  p.run(A, blockIdx.y, m0, n0, 0, A.steps, lds);
-  out(p, p.wave_m(m0), p.wave_n(n0), lds + p.wave * (P::kBuffers * P::kBuffer / P::kWavesHere));
+  p.run(A, matrix, which - matrix * A.splits, m0, n0, lds);
+  if (p.owns) out(p, p.wave_m(m0), p.wave_n(n0), lds + p.wave * (P::kBuffers * P::kBuffer / P::kWavesHere));
 }
 
 // Launches tiles of the given form over all of A and B; k: how many there are, zeros up to a whole step.
-template <class P, bool LOWER>
-ProductArgs product_args(const Operand& a, const Operand& b, int64_t k) {
-  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN), 0};
-  A.tiles = LOWER ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n;
-  return A;
-}
 template <class P, bool LOWER = false, class Epilogue>
-int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream) {
-  const ProductArgs A = product_args<P, LOWER>(a, b, k);
-  product_kernel<P, LOWER><<<dim3(A.tiles, batch), P::kGroup, 0, stream>>>(A, out);
+int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream, int64_t splits = 1) {
+  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), 0, 0, (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN), 0};
+  A.split_steps = (int)ceil_div(A.steps, splits);
+  A.splits = (unsigned)ceil_div(A.steps, A.split_steps);       // none is empty
+  A.tiles = LOWER ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n;
+  product_kernel<P, LOWER><<<A.tiles * batch * A.splits, P::kGroup, 0, stream>>>(A, out);
   return launch_status();
 }
 template <bool BF16, Lies LA, Lies LB> using Product256 = Product<BF16, LA, LB, 2, 2, 4, 4>;
 template <bool BF16, Lies LA, Lies LB> using Product128 = Product<BF16, LA, LB, 2, 2, 2, 2>;
-template <bool BF16, Lies LA, Lies LB> using Product64 = Product<BF16, LA, LB, 2, 2, 1, 1>;
-
 // v as hi + lo of binary16: 22 bits and a sign between them, as long as v is at least 2^-13; what is lost below is 2^-25 at most.
 __device__ __forceinline__ void split_f16(float v, _Float16& hi, _Float16& lo) {
   hi = (_Float16)v;
