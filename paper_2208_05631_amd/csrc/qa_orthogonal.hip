@@ -138,35 +138,34 @@ struct Parts {
   __device__ __forceinline__ bool holds(int64_t row, int64_t col) const { return row < rows && 2 * col < ld; }
 };
 
-// A = X X^T or B = b A + c A A, tiles on and below the diagonal; the others are their transposes.  p's rows are the products' columns:
-// a lane has eight numbers of one row, and the transpose goes by way of LDS.
+// A = X X^T or B = b A + c A A, tiles on and below the diagonal; the others are their transposes.
 template <bool SQUARE>
 struct SymmetricOut {
   Parts to, a;
   float cb, cc;
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
-    const bool both = m0 / P::kM != n0 / P::kN;
-    const Turned turned = {(float*)lds};
-    p.for_eights(m0, n0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
-      float x[kVec] = {};
-      if (SQUARE && a.holds(j, i)) get_parts(a.at(p.matrix, j, i), x);
+  // Eight numbers of a row.
+  __device__ __forceinline__ void put(int64_t matrix, int64_t row, int64_t col, float (&v)[kVec]) const {
+    if (!to.holds(row, col)) return;
+    float x[kVec] = {};
+    if (SQUARE) get_parts(a.at(matrix, row, col), x);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) v[e] = SQUARE ? cb * x[e] + (cc / kUnit) * v[e] : v[e] * (1.0f / kUnit);
-      if (to.holds(j, i)) to.put(p.matrix, j, i, v);
-      if (both) turned.put(i, v);
-    }, [&](int64_t i0, int64_t j0) {
-      if (both) turned.take(i0, j0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
-        if (to.holds(i, j)) to.put(p.matrix, i, j, v);
-      });
-    });
+    for (int e = 0; e < kVec; ++e) v[e] = SQUARE ? cb * x[e] + (cc / kUnit) * v[e] : v[e] * (1.0f / kUnit);
+    to.put(matrix, row, col, v);
+  }
+  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
+    const auto same = [](int, int, float (&)[kVec]) {};
+    const auto run = [&](int64_t i, int64_t j, float (&v)[kVec]) { put(p.matrix, j, i, v); };
+    const auto turned = [&](int64_t i, int64_t j, float (&v)[kVec]) { put(p.matrix, i, j, v); };
+    if (m0 / P::kM == n0 / P::kN) p.template for_runs<false>(m0, n0, lds, same, run, turned);
+    else p.template for_runs<true>(m0, n0, lds, same, run, turned);
   }
 };
 // X' = a X + B X, with rows of zeros up to a whole step.
 struct NextOut {
   Parts x, to;
   float ca;
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char*) const {
-    p.for_eights(m0, n0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
+  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
+    p.for_runs(m0, n0, lds, [&](int64_t i, int64_t j, float (&v)[kVec]) {
       if (j >= whole(to.rows, kPartsStep) || 2 * i >= to.ld) return;
       float o[kVec] = {};
       if (j < to.rows) get_parts(x.at(p.matrix, j, i), o);
@@ -198,21 +197,26 @@ struct LastOut {
   __device__ __forceinline__ void put(int64_t matrix, int64_t row, int64_t col, int64_t cols, const float (&o)[kVec]) const {
     put_last<TYPE, STEP>(out + matrix * matrix_stride + row * stride + col, (int)min((int64_t)kVec, cols - col), o, eta, shrink);
   }
+  // X' goes to LDS complete where its rows are the caller's columns, and straight to memory where they are rows.
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
-    const Turned turned = {(float*)lds};
-    p.for_eights(m0, n0, [&](int64_t i, int64_t j, float (&v)[kVec]) {
+    const auto complete = [&](int64_t i, int64_t j, float (&v)[kVec]) {
       float o[kVec] = {};
-      const bool holds = j < x.rows && i < x.cols;
-      if (holds) get_parts(x.at(p.matrix, j, i), o);
+      if (j < x.rows && i < x.cols) get_parts(x.at(p.matrix, j, i), o);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) o[e] = (ca * o[e] + v[e] * (1.0f / kUnit)) * (1.0f / kUnit);
-      if (TALL) turned.put(i, o);
-      else if (holds) put(p.matrix, j, i, x.cols, o);
-    }, [&](int64_t i0, int64_t j0) {
-      if (TALL) turned.take(i0, j0, [&](int64_t i, int64_t j, float (&o)[kVec]) {
+      for (int e = 0; e < kVec; ++e) v[e] = (ca * o[e] + v[e] * (1.0f / kUnit)) * (1.0f / kUnit);
+    };
+    if constexpr (TALL) {
+      p.template for_runs<true>(m0, n0, lds, [&](int i, int j, float (&v)[kVec]) { complete(m0 + i, n0 + j, v); }, [](int64_t, int64_t, float (&)[kVec]) {},
+                                [&](int64_t i, int64_t j, float (&o)[kVec]) {
         if (i < x.cols && j < x.rows) put(p.matrix, i, j, x.rows, o);
       });
-    });
+    } else {
+      p.for_runs(m0, n0, lds, [&](int64_t i, int64_t j, float (&v)[kVec]) {
+        if (j >= x.rows || i >= x.cols) return;
+        complete(i, j, v);
+        put(p.matrix, j, i, x.cols, v);
+      });
+    }
   }
 };
 
@@ -474,16 +478,17 @@ template <Lies LA, Lies LB, bool LOWER, class Epilogue>
 int multiply(const Parts& a, const Parts& b, int64_t k, int64_t count, const Epilogue& out, hipStream_t stream) {
   const Operand oa = {a.p, a.ld, a.batch, in_rows(LA) ? a.rows : a.cols}, ob = {b.p, b.ld, b.batch, in_rows(LB) ? b.rows : b.cols};
   // X' has many tiles, A and B have few.
-  constexpr unsigned kAllowed = LOWER ? ~0u : 1u << kTiles256 | 1u << kTiles128 | 1u << kTiles64Two;
+  constexpr unsigned kAllowed = LOWER ? ~0u : tiles_bit(kTiles256) | tiles_bit(kTiles128) | tiles_bit(kTiles64Two);
   const unsigned batch = (unsigned)count;
-  switch (tiles_for(kAllowed, oa.n, ob.n, ceil_div(k, kPartsStep), count, LOWER)) {
+  const Tiles tiles = product_plan(kAllowed, ProductShape{oa.n, ob.n, ceil_div(k, kPartsStep), count, LOWER, 1.0}, 1).tiles;
+  switch (tiles) {
     case kTiles256: return product_launch<Product<false, LA, LB, 2, 2, 4, 4>, LOWER>(oa, ob, k, out, batch, stream);
     case kTiles128: return product_launch<Product<false, LA, LB, 2, 2, 2, 2>, LOWER>(oa, ob, k, out, batch, stream);
     case kTiles64Two: return product_launch<Product<false, LA, LB, 2, 2, 1, 1, 2>, LOWER>(oa, ob, k, out, batch, stream);
     default: break;
   }
   if constexpr (LOWER) {
-    switch (tiles_for(kAllowed, oa.n, ob.n, ceil_div(k, kPartsStep), count, LOWER)) {
+    switch (tiles) {
       case kTiles192: return product_launch<Product<false, LA, LB, 2, 2, 3, 3>, LOWER>(oa, ob, k, out, batch, stream);
       case kTiles128Two: return product_launch<Product<false, LA, LB, 2, 2, 2, 2, 2>, LOWER>(oa, ob, k, out, batch, stream);
       default: return product_launch<Product<false, LA, LB, 1, 1, 2, 2, 4>, LOWER>(oa, ob, k, out, batch, stream);

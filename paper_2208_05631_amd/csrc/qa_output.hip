@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "qa_product.h"
+#include "qa_product_plan.h"
 #include "qa_softmax.h"
 
 namespace qa {
@@ -299,7 +300,7 @@ struct LogitsGradOut {
   const Scales* scales;
   _Float16* c;
   int64_t ld, to_rows;
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0, char*) const {
+  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0, char* lds) const {
     const int exp = exponent_for(scales->most[kOfC]), lane = threadIdx.x % kWave;
     constexpr int FN = (int)(sizeof p.acc[0] / sizeof p.acc[0][0]);
     float m[FN], log_sum[FN], a[FN], e[FN], h[FN];
@@ -320,8 +321,8 @@ struct LogitsGradOut {
       here[j] = at >= 0 && at < P::kM ? (int)at : -kVec;
     }
     const int left = (int)max((int64_t)0, min((int64_t)P::kM, L.vocab - v0)), wide = (int)max((int64_t)0, min((int64_t)P::kM, ld / 2 - v0));
-    p.for_eights(0, 0, [&](int64_t i, int64_t col, float (&z)[kVec]) {
-      const int v = (int)i, j = (int)col / 32;
+    p.template for_runs<false>(0, 0, lds, [&](int v, int col, float (&z)[kVec]) {
+      const int j = col / 32;
       float g[kVec];
 #pragma unroll
       for (int k = 0; k < kVec; ++k) {
@@ -335,11 +336,11 @@ struct LogitsGradOut {
           if (v + k == here[j]) g[k] += a[j];
       }
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) g[k] = none[j] || v + k >= left ? 0.0f : g[k];
-      const int64_t t = t0 + col;
-      if (t < to_rows && v < wide) put_parts(c + t * ld + 2 * (v0 + v), g);
+      for (int k = 0; k < kVec; ++k) z[k] = none[j] || v + k >= left ? 0.0f : g[k];
       __builtin_amdgcn_sched_barrier(0);           // or all exponents and addresses are held in registers at once
-    });
+    }, [&](int64_t v, int64_t col, float (&g)[kVec]) {
+      if (t0 + col < to_rows && v < wide) put_parts(c + (t0 + col) * ld + 2 * (v0 + v), g);
+    }, 0);
   }
 };
 
@@ -352,9 +353,9 @@ struct GradOut {
   int64_t stride, rows, cols;
   int which;                                       // the scale of the other operand, -1: none
   bool add, last;                                  // to what is in sums (or, of binary32, in out); the last piece writes out
-  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char*) const {
+  template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
     const int exp = -(exponent_for(scales->most[kOfC]) + (which < 0 ? 0 : exponent_for(scales->most[which])));
-    p.for_eights(m0, n0, [&](int64_t col, int64_t row, float (&v)[kVec]) {
+    p.for_runs(m0, n0, lds, [&](int64_t col, int64_t row, float (&v)[kVec]) {
       if (row >= rows || col >= cols) return;
       const int n = (int)min((int64_t)kVec, cols - col);
       ElemT<TYPE>* const at = out + row * stride + col;
@@ -368,13 +369,13 @@ struct GradOut {
       for (int e = 0; e < kVec; ++e) v[e] = before[e] + ldexpf(v[e], exp);
       if (last) store_raw<TYPE>(at, from_f32<TYPE>(v), n);
       else store_raw<QA_F32>(s, from_f32<QA_F32>(v), n);
-      __builtin_amdgcn_sched_barrier(0);           // or all that is added to is held in registers at once
     });
   }
 };
-// dx from the splits' sums, in their order.
+// A gradient from the splits' sums, in their order.
 template <int TYPE>
-__global__ __launch_bounds__(kThreads) void output_sum_kernel(const float* sums, int splits, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride) {
+__global__ __launch_bounds__(kThreads) void output_sum_kernel(const float* sums, int splits, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride,
+                                                              int accumulate) {
   const int64_t across = ceil_div(cols, kVec), all = rows * across;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
     const int64_t row = i / across, col = i % across * kVec;
@@ -384,6 +385,12 @@ __global__ __launch_bounds__(kThreads) void output_sum_kernel(const float* sums,
     for (int s = 0; s < splits; ++s) {
       float w[kVec];
       to_f32<QA_F32>(load_raw<QA_F32>(sums + (s * rows + row) * cols + col, n), w);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v[e] += w[e];
+    }
+    if (accumulate) {
+      float w[kVec];
+      to_f32<TYPE>(load_raw<TYPE>(out + row * stride + col, n), w);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) v[e] += w[e];
     }
@@ -408,16 +415,33 @@ struct Room {
   }
 };
 
+// Time of a step of k beside one of three products of 16: 32 k and one product bring as much for two thirds of the matrix instructions.
+constexpr double kOneProduct = 0.75, kTwoProducts = 0.65, kThreeProducts = 1.0;
+
 // Which tiles multiply the logits: heights (vocabulary) of chunks, and widths (rows).
 enum { kTall256, kTall128, kTall64 };
-int logits_tiles(int64_t rows, int64_t vocab) {
+int logits_tiles(int64_t rows, int64_t vocab, int64_t features, int type) {
   if (rows <= 64) return kTall64;
-  return ceil_div(rows, 256) * ceil_div(vocab, 256) >= 192 ? kTall256 : kTall128;
+  const ProductShape S = {vocab, rows, ceil_div(features, type == QA_F32 ? kPartsStep : kWholeStep), 1, false, type == QA_F32 ? kThreeProducts : kOneProduct};
+  return product_plan(tiles_bit(kTiles256) | tiles_bit(kTiles128), S, 1).tiles == kTiles256 ? kTall256 : kTall128;
 }
 constexpr int64_t chunk_of(int tiles) { return tiles == kTall256 ? 128 : 64; }
 
 // Equal pieces of n, whole tiles each, of at most `most`.
 int64_t piece_of(int64_t n, int64_t most) { return std::min(whole(n, kWholeStep), whole(ceil_div(n, ceil_div(n, most)), 256)); }
+// Pieces of the vocabulary whose tiles of 256 x 256 leave the fewest compute units without one at the end of each piece.
+int64_t even_piece_of(int64_t n, int64_t most, int64_t rows) {
+  int64_t best = piece_of(n, most), least = 0;
+  for (int64_t piece = whole(std::min(n, most), 256); piece >= 256 && 2 * piece >= std::min(n, most); piece -= 256) {
+    int64_t rounds = 0;
+    for (int64_t first = 0; first < n; first += piece) rounds += ceil_div(ceil_div(std::min(piece, n - first), 256) * ceil_div(rows, 256), 256);
+    if (least == 0 || rounds < least) {
+      least = rounds;
+      best = piece;
+    }
+  }
+  return std::min(whole(n, kWholeStep), best);
+}
 int64_t power_of_two_within(int64_t n, int64_t least) {
   while (2 * least <= n) least *= 2;
   return least;
@@ -431,10 +455,12 @@ struct Plan {
   size_t m, s, sw, given;                          // scoring
   int64_t chunks;
   size_t scales, xc, wc, c, sums;                  // gradient: x and w as the products with c take them
-  int64_t hc, tp, vp, splits;
+  size_t dw_sums;
+  int64_t hc, tp, vp;
+  ProductPlan dx, dw;
   size_t bytes;
 };
-bool has_large_tiles(int64_t m, int64_t n) { return ceil_div(m, 256) * ceil_div(n, 256) >= 192; }
+ProductPlan grad_plan(const ProductShape& S, int64_t most) { return product_plan(tiles_bit(kTiles256) | tiles_bit(kTiles128) | tiles_bit(kTiles128Two), S, most); }
 
 bool in_place(const void* p, int64_t stride) { return stride % 8 == 0 && stride < (int64_t(1) << 22) && aligned(p, 16); }
 
@@ -448,7 +474,7 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
   P.copy_w = !w || !rows_as_they_are || !in_place(w, L.w_stride);
   P.hp = whole(L.features, kWholeStep);
   if (op == QA_OP_LOGPROB) {
-    P.tiles = logits_tiles(L.rows, L.vocab);
+    P.tiles = logits_tiles(L.rows, L.vocab, L.features, type);
     P.piece = P.copy_w ? piece_of(L.vocab, power_of_two_within(kPieceBytes / (P.hp * 2 * P.parts), 16384)) : L.vocab;
     P.pieces = ceil_div(L.vocab, P.piece);
     P.chunks = ceil_div(L.vocab, chunk_of(P.tiles));
@@ -459,20 +485,22 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
   } else {
     P.tp = whole(L.rows, kPartsStep);
     P.hc = whole(L.features, 8);
-    P.piece = piece_of(L.vocab, std::min(power_of_two_within(kPieceBytes / (4 * P.tp), 1024), power_of_two_within(kPieceBytes / (P.hp * 2 * P.parts), 1024)));
+    P.piece = even_piece_of(L.vocab, std::min(power_of_two_within(kPieceBytes / (4 * P.tp), 1024), power_of_two_within(kPieceBytes / (P.hp * 2 * P.parts), 1024)), L.rows);
     P.pieces = ceil_div(L.vocab, P.piece);
-    P.tiles = logits_tiles(L.rows, P.piece);
+    P.tiles = logits_tiles(L.rows, std::min(P.piece, L.vocab), L.features, type);
     P.vp = whole(P.piece, kWholeStep);
     P.scales = room.take(sizeof(Scales));
     P.xc = room.take(2 * P.parts * P.tp * P.hc);
     P.wc = room.take(2 * P.parts * P.vp * P.hc);
     P.c = room.take(2 * 2 * P.tp * P.vp);
-    // dx has few tiles and sums over the vocabulary: splits of it, until every compute unit has two, of eight steps at least.
-    const int64_t tiles = ceil_div(L.rows, 128) * ceil_div(L.features, 128), step = type == QA_BF16 ? kWholeStep : kPartsStep;
-    const int64_t steps = ceil_div(std::min(P.piece, L.vocab), step);
-    P.splits = has_large_tiles(L.features, L.rows) ? 1 : std::max<int64_t>(1, std::min(512 / tiles, steps / 8));
-    P.splits = ceil_div(steps, ceil_div(steps, P.splits));       // none without steps in the first piece
-    P.sums = room.take(P.pieces > 1 || P.splits > 1 ? 4 * P.splits * L.rows * L.features : 0);
+    // dx has few tiles and sums over the vocabulary, dw few where both sides are small.
+    const bool one = type == QA_BF16;
+    const int64_t vocab = std::min(P.piece, L.vocab), fit = std::max<int64_t>(1, kPieceBytes / (4 * L.rows * L.features));
+    P.dx = grad_plan({L.features, L.rows, ceil_div(vocab, one ? kWholeStep : kPartsStep), 1, false, one ? kOneProduct : type == QA_F32 ? kThreeProducts : kTwoProducts}, std::min<int64_t>(64, fit));
+    P.dw = grad_plan({L.features, vocab, ceil_div(L.rows, kPartsStep), 1, false, type == QA_F32 ? kThreeProducts : kTwoProducts},
+                     std::min(std::max<int64_t>(1, kPieceBytes / (4 * vocab * L.features)), int64_t(64)));
+    P.sums = room.take(P.pieces > 1 || P.dx.splits > 1 ? 4 * P.dx.splits * L.rows * L.features : 0);
+    P.dw_sums = room.take(P.dw.splits > 1 ? 4 * P.dw.splits * vocab * L.features : 0);
   }
   P.x_exp = room.take(type == QA_F32 ? 4 * L.rows : 0);
   P.w_exp = room.take(type == QA_F32 ? 4 * P.piece : 0);
@@ -533,10 +561,17 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
   return launch_status();
 }
 
+template <int TYPE>
+int sum_launch(const float* sums, int64_t splits, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride, int accumulate, hipStream_t stream) {
+  const int64_t vecs = rows * ceil_div(cols, kVec);
+  output_sum_kernel<TYPE><<<(unsigned)std::min<int64_t>(ceil_div(vecs, kThreads), 4096), kThreads, 0, stream>>>(sums, (int)splits, rows, cols, out, stride, accumulate);
+  return launch_status();
+}
 template <Lies LA, Lies LB, class Epilogue>
-int grad_product(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, hipStream_t stream, int64_t splits = 1) {
-  if (has_large_tiles(a.n, b.n)) return product_launch<Product256<false, LA, LB>>(a, b, k, out, 1, stream);
-  return product_launch<Product128<false, LA, LB>>(a, b, k, out, 1, stream, splits);
+int grad_product(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, const ProductPlan& plan, hipStream_t stream) {
+  if (plan.tiles == kTiles256) return product_launch<Product256<false, LA, LB>>(a, b, k, out, 1, stream, plan.splits);
+  if (plan.tiles == kTiles128) return product_launch<Product128<false, LA, LB>>(a, b, k, out, 1, stream, plan.splits);
+  return product_launch<Product<false, LA, LB, 2, 2, 2, 2, 2>>(a, b, k, out, 1, stream, plan.splits);
 }
 
 struct GradCall {
@@ -588,20 +623,21 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
         if (const int rc = copy_launch<TYPE, kOneScale>(A, stream)) return rc;
       }
       const bool last = first + P.piece >= L.vocab;
-      const GradOut<TYPE> out{(ElemT<TYPE>*)G.dx, P.pieces > 1 || P.splits > 1 ? (float*)(ws + P.sums) : nullptr, scales, G.dx_stride, L.rows, L.features,
-                              TYPE == QA_F16 ? -1 : kOfW, first > 0, last && P.splits == 1};
+      const GradOut<TYPE> out{(ElemT<TYPE>*)G.dx, P.pieces > 1 || P.dx.splits > 1 ? (float*)(ws + P.sums) : nullptr, scales, G.dx_stride, L.rows, L.features,
+                              TYPE == QA_F16 ? -1 : kOfW, first > 0, last && P.dx.splits == 1};
       // One part of c has 11 bits, which is little beside bfloat16's 8, but as much as binary16's own.
       constexpr Lies kC = TYPE == QA_BF16 ? kHiOfRows : kRowsOfParts;
-      if (const int rc = grad_product<kColumnsOf, kC>(wc, Operand{c, 2 * P.vp, 0, L.rows}, vocab, out, stream, P.splits)) return rc;
-      if (last && P.splits > 1) {
-        output_sum_kernel<TYPE><<<(unsigned)std::min<int64_t>(ceil_div(L.rows * ceil_div(L.features, kVec), kThreads), 4096), kThreads, 0, stream>>>(
-            (const float*)(ws + P.sums), P.splits, L.rows, L.features, (ElemT<TYPE>*)G.dx, G.dx_stride);
-        if (const int rc = launch_status()) return rc;
-      }
+      if (const int rc = grad_product<kColumnsOf, kC>(wc, Operand{c, 2 * P.vp, 0, L.rows}, vocab, out, P.dx, stream)) return rc;
+      if (last && P.dx.splits > 1)
+        if (const int rc = sum_launch<TYPE>((const float*)(ws + P.sums), P.dx.splits, L.rows, L.features, (ElemT<TYPE>*)G.dx, G.dx_stride, 0, stream)) return rc;
     }
     if (G.dw) {
-      const GradOut<QA_F32> out{G.dw + first * G.dw_stride, nullptr, scales, G.dw_stride, vocab, L.features, TYPE == QA_F16 ? -1 : kOfX, G.accumulate != 0, true};
-      if (const int rc = grad_product<kColumnsOf, kColumnsOfParts>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, stream)) return rc;
+      float* const dw = G.dw + first * G.dw_stride;
+      float* const sums = P.dw.splits > 1 ? (float*)(ws + P.dw_sums) : nullptr;
+      const GradOut<QA_F32> out{dw, sums, scales, G.dw_stride, vocab, L.features, TYPE == QA_F16 ? -1 : kOfX, !sums && G.accumulate, !sums};
+      if (const int rc = grad_product<kColumnsOf, kColumnsOfParts>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, P.dw, stream)) return rc;
+      if (sums)
+        if (const int rc = sum_launch<QA_F32>(sums, P.dw.splits, vocab, L.features, dw, G.dw_stride, G.accumulate, stream)) return rc;
     }
   }
   return QA_OK;

@@ -142,8 +142,12 @@ struct Product {
   static_assert(kPA <= kPB && !(kStep == kPartsStep && (LA == kRows || LA == kHiOfRows || LB == kRows || LB == kHiOfRows)), "forms that there are");
   typedef Bringer<LA, kM, kStep, kWavesHere> BringA;
   typedef Bringer<LB, kN, kStep, kWavesHere> BringB;
-  static constexpr int kBuffer = BringA::kBytes + BringB::kBytes, kBuffers = 4, kLds = SHARE * kBuffers * kBuffer, kLoads = BringA::kLoads + BringB::kLoads;
+  static constexpr int kBuffer = BringA::kBytes + BringB::kBytes, kBuffers = 4, kLoads = BringA::kLoads + BringB::kLoads;
   static constexpr int kLate = (kLoads + 1) / (kPA + 1);       // a step's loads behind the barrier; the others follow in the next step
+
+  // The other lots' sums stand behind the first lot's buffers, which its epilogue uses.
+  static constexpr int kLotBytes = kWavesHere * kWave * FM * FN * 64, kShared = kBuffers * kBuffer + (SHARE - 1) * kLotBytes;
+  static constexpr int kLds = SHARE * kBuffers * kBuffer > kShared ? SHARE * kBuffers * kBuffer : kShared;
 
   f32x16 acc[FM][FN];
   u32x4 a[2][FM], b[2][FN];
@@ -269,19 +273,18 @@ struct Product {
       constexpr int kPieces = (int)(sizeof acc / sizeof(f32x4));
       f32x4 v[kPieces];
       __builtin_memcpy(v, &acc, sizeof v);
-      f32x4* const at = (f32x4*)all_lds + threadIdx.x % (kWavesHere * kWave);
-      constexpr int kLot = kWavesHere * kWave * kPieces;
-      static_assert(SHARE * kLot * 16 <= kLds, "sums fit the buffers");
+      f32x4* const at = (f32x4*)(all_lds + kBuffers * kBuffer) + threadIdx.x % (kWavesHere * kWave);
+      constexpr int kLot = kLotBytes / 16;
       if (!owns) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) at[share * kLot + i * kWavesHere * kWave] = v[i];
+        for (int i = 0; i < kPieces; ++i) at[(share - 1) * kLot + i * kWavesHere * kWave] = v[i];
       }
       __syncthreads();
       if (owns) {
 #pragma unroll 1
         for (int g = 1; g < SHARE; ++g)
 #pragma unroll
-          for (int i = 0; i < kPieces; ++i) v[i] += at[g * kLot + i * kWavesHere * kWave];
+          for (int i = 0; i < kPieces; ++i) v[i] += at[(g - 1) * kLot + i * kWavesHere * kWave];
         __builtin_memcpy(&acc, v, sizeof v);
       }
     }
@@ -290,15 +293,21 @@ struct Product {
   __device__ __forceinline__ int64_t wave_n(int64_t n0) const { return n0 + wave / WM * 32 * FN; }
 
   // A lane holds of block (i, j) rows 8 q + 4 (lane / 32) + e, e < 4, of column lane % 32.  With its counterpart of the other half it changes
-  // four rows for four, so that it has eight that follow each other: each(i0, j, eight sums), i0 .. i0 + 7 and j within C.
-  // block(i0, j0): behind the 32 x 32 that begin there.
-  template <class Each, class Block>
-  __device__ __forceinline__ void for_eights(int64_t m0, int64_t n0, const Each& each, const Block& block) {
+  // four rows for four, so that it has eight that follow each other, which it may change: change(i, j, eight sums), i and j
+  // from the wave's first on.  By way of LDS they come to lanes that lie side by side along i, as they do in memory where C's columns are
+  // rows: run(i, j, eight numbers), i .. i + 7 and j within C.  TURN: then side by side along j: turned(i, j, eight numbers), j .. j + 7.
+  // (Eight at a time from where they are, every lane to a row of its own, took 25 us beside the 30 of 32 steps.)
+  static constexpr int kRunPitch = FM == 1 ? 128 : FM == 2 ? 256 : 512;
+  static_assert(32 * kRunPitch <= kBuffers * kBuffer / kWavesHere, "32 columns of a wave fit its share of the buffers");
+  // Sixteen rows at one place, and one row, lie in different banks.
+  static __device__ __forceinline__ int run_at(int row, int chunk) { return row * kRunPitch + (chunk ^ (FM == 1 ? row >> 1 & 7 : row & 15)) * 16; }
+  template <bool TURN, class Change, class Run, class Turned>
+  __device__ __forceinline__ void for_runs(int64_t m0, int64_t n0, char* lds, const Change& change, const Run& run, const Turned& turned) {
     const int lane = threadIdx.x % kWave;
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int j = 0; j < FN; ++j) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
+      for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           float v[kVec];
@@ -308,38 +317,36 @@ struct Product {
             v[e] = as_f32(both[0]);
             v[4 + e] = as_f32(both[1]);
           }
-          each(m0 + 32 * i + 16 * q + 8 * (lane / 32), n0 + 32 * j + lane % 32, v);
+          change(32 * i + 16 * q + 8 * (lane / 32), 32 * j + lane % 32, v);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            __builtin_memcpy(__builtin_assume_aligned(lds + run_at(lane % 32, 8 * i + 4 * q + 2 * (lane / 32) + h), 16), v + 4 * h, 16);
         }
-        block(m0 + 32 * i, n0 + 32 * j);
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll 2
+      for (int r = lane; r < 32 * 4 * FM; r += kWave) {
+        const int row = r / (4 * FM), at = r % (4 * FM);
+        float v[kVec];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) __builtin_memcpy(v + 4 * h, __builtin_assume_aligned(lds + run_at(row, 2 * at + h), 16), 16);
+        run(m0 + 8 * at, n0 + 32 * j + row, v);
       }
-  }
-  template <class Each>
-  __device__ __forceinline__ void for_eights(int64_t m0, int64_t n0, const Each& each) {
-    for_eights(m0, n0, each, [](int64_t, int64_t) {});
-  }
-};
-
-// 32 x 32 numbers of a wave, put in by rows of C's columns and taken out by its rows, by way of LDS.
-struct Turned {
-  float* at;                                       // 32 rows of 33
-  __device__ __forceinline__ void put(int64_t i0, const float (&v)[kVec]) const {
+      if constexpr (TURN) {
+#pragma unroll 2
+        for (int r = lane; r < 32 * 4 * FM; r += kWave) {
+          const int i = r / 4, at = r % 4 * kVec;
+          float v[kVec];
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) at[((int)i0 % 32 + e) * 33 + (int)threadIdx.x % 32] = v[e];
-  }
-  // each(i, j0, eight numbers of row i)
-  template <class Each>
-  __device__ __forceinline__ void take(int64_t i0, int64_t j0, const Each& each) const {
-    __builtin_amdgcn_wave_barrier();
-    const int row = (int)threadIdx.x % kWave / 2;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int col = 16 * ((int)threadIdx.x % 2) + kVec * h;
-      float v[kVec];
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) v[e] = at[row * 33 + col + e];
-      each(i0 + row, j0 + col, v);
+          for (int e = 0; e < kVec; ++e) __builtin_memcpy(v + e, lds + run_at(at + e, i / 4) + i % 4 * 4, 4);
+          turned(m0 + i, n0 + 32 * j + at, v);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();
+  }
+  template <class Run>
+  __device__ __forceinline__ void for_runs(int64_t m0, int64_t n0, char* lds, const Run& run) {
+    for_runs<false>(m0, n0, lds, [](int, int, float (&)[kVec]) {}, run, 0);
   }
 };
 

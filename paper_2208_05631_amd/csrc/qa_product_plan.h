@@ -1,4 +1,4 @@
-// Which tiles a product of parts takes.  Host code without a GPU in it, so that a test can ask it.
+// Which tiles a product takes, and into how many splits its sums go.  Host code without a GPU in it, so that a test can ask it.
 #pragma once
 #include <cstdint>
 
@@ -6,11 +6,12 @@ namespace qa {
 
 // Tiles of a work-group, in columns and rows; with k shared by two or four lots of its waves.
 enum Tiles { kTiles256, kTiles192, kTiles128, kTiles128Two, kTiles64Two, kTiles64Four };
+constexpr unsigned tiles_bit(Tiles t) { return 1u << t; }
 
 struct TileForm {
   int side;
   int at_once;                                     // tiles that run at a time
-  double alone, full;                              // us per step of 16: where few tiles run, and where all do
+  double alone, full;                              // us per step of three products of 16: where few tiles run, and where all do
   double round;                                    // us per round beside the steps
 };
 // Measured with products of 1 x 1 to 4096 x 4096 numbers in two parts; a step of a large tile takes longer where all run, which the
@@ -19,24 +20,38 @@ struct TileForm {
 constexpr TileForm kTileForms[] = {{256, 256, 0.70, 1.24, 9.0}, {192, 256, 0.38, 0.75, 6.5}, {128, 512, 0.20, 0.71, 4.5},
                                    {128, 256, 0.19, 0.37, 5.0}, {64, 512, 0.11, 0.24, 3.6}, {64, 256, 0.07, 0.115, 4.6}};
 
-// The form out of `allowed` (bits) that is estimated to take the least time for `count` products of m x n over `steps` steps; lower: tiles on and below
-// the diagonal only (m = n).
-inline Tiles tiles_for(unsigned allowed, int64_t m, int64_t n, int64_t steps, int64_t count, bool lower) {
-  int best = -1;
+struct ProductShape {
+  int64_t m, n, steps, count;                      // count: products side by side
+  bool lower;                                      // tiles on and below the diagonal only (m = n)
+  double step;                                     // time of a step beside one of three products of 16
+};
+inline double product_us(Tiles form, const ProductShape& S, int64_t splits) {
+  const auto over = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  const TileForm& F = kTileForms[form];
+  const int64_t tm = over(S.m, F.side), tn = over(S.n, F.side), tiles = S.count * splits * (S.lower ? tm * (tm + 1) / 2 : tm * tn);
+  const int64_t rounds = tiles / F.at_once, rest = tiles % F.at_once;
+  const double step = (double)rounds * F.full + (rest ? F.alone + (F.full - F.alone) * (double)rest / F.at_once : 0.0);
+  return (double)over(S.steps, splits) * S.step * step + F.round * (double)(rounds + (rest != 0)) +
+         (splits > 1 ? 5.0 + (double)(2 * splits + 1) * (double)S.m * (double)S.n * (4.0 / 5e6) : 0.0);       // written, read and joined at 5 TB/s
+}
+
+struct ProductPlan { Tiles tiles; int64_t splits; };
+// What is estimated to take the least time, of the forms in `allowed` and up to `most` splits, each of eight steps at least and none without any.
+inline ProductPlan product_plan(unsigned allowed, const ProductShape& S, int64_t most) {
+  ProductPlan best = {kTiles256, 0};
   double least = 0.0;
   for (int f = 0; f < (int)(sizeof kTileForms / sizeof *kTileForms); ++f) {
     if (!(allowed >> f & 1)) continue;
-    const TileForm& F = kTileForms[f];
-    const int64_t tm = (m + F.side - 1) / F.side, tn = (n + F.side - 1) / F.side, tiles = count * (lower ? tm * (tm + 1) / 2 : tm * tn);
-    const int64_t rounds = tiles / F.at_once, rest = tiles % F.at_once;
-    const double step = (double)rounds * F.full + (rest ? F.alone + (F.full - F.alone) * (double)rest / F.at_once : 0.0);
-    const double us = (double)steps * step + F.round * (double)(rounds + (rest != 0));
-    if (best < 0 || us < least) {
+    for (int64_t s = 1; s <= most && (s == 1 || s * 8 <= S.steps); ++s) {
+      const double us = product_us((Tiles)f, S, s);
+      if (best.splits && us >= least) continue;
       least = us;
-      best = f;
+      best = {(Tiles)f, s};
     }
   }
-  return (Tiles)best;
+  const int64_t each = (S.steps + best.splits - 1) / best.splits;
+  best.splits = (S.steps + each - 1) / each;
+  return best;
 }
 
 }  // namespace qa
