@@ -135,9 +135,10 @@ __device__ __forceinline__ void for_logits(P& p, const LayerArgs& L, int64_t v0,
 }
 
 struct ScoreArgs {
-  float *m, *s, *w;                                // [chunk][rows]
+  float *m, *s, *w;                                // [chunk][rows]: a wave's part of a tile
   float* given;                                    // the targets' logits
   int64_t first, first_chunk;                      // of this launch's vocabulary
+  int64_t pitch;                                   // of the tiles
 };
 
 template <bool SCALED>
@@ -145,14 +146,15 @@ struct ScoreOut {
   LayerArgs L;                                     // vocab: of this launch
   ScoreArgs A;
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0, char*) const {
-    constexpr int kChunk = 32 * (int)(sizeof p.acc / sizeof p.acc[0]);
-    if (v0 >= L.vocab) return;
+    constexpr int kChunk = 32 * (int)(sizeof p.acc / sizeof p.acc[0]), kChunks = P::kM / kChunk;
+    const int64_t tile = p.tile_m, in_tile = v0 - tile * A.pitch;
+    const int left = (int)max((int64_t)0, min(min((int64_t)kChunk, A.pitch - in_tile), L.vocab - v0));       // of this wave's logits there are
 #pragma unroll
     for (int j = 0; j < (int)(sizeof p.acc[0] / sizeof p.acc[0][0]); ++j) {
       const int64_t t = t0 + 32 * j + threadIdx.x % 32;
       const int x_exp = SCALED ? L.x_exp[min(t, L.rows - 1)] : 0;
       const int64_t at = L.target && t < L.rows ? (int64_t)L.target[t] - A.first - v0 : -1;
-      const int here = at >= 0 && at < kChunk ? (int)at : -1, left = (int)min((int64_t)kChunk, L.vocab - v0);
+      const int here = at >= 0 && at < left ? (int)at : -1;
       Sums a = no_sums();
       float given = 0.0f;
       for_logits<SCALED>(p, L, v0, j, x_exp, [&](int v, int i, int q, float (&z)[4]) {
@@ -164,7 +166,7 @@ struct ScoreOut {
           a.m = fmaxf(a.m, z[e]);
         }
       });
-      if (here >= 0 && here < left && here / 4 % 2 == (int)threadIdx.x % kWave / 32) A.given[t] = given;
+      if (here >= 0 && here / 4 % 2 == (int)threadIdx.x % kWave / 32) A.given[t] = given;
       a.m = fmaxf(a.m, as_f32(other_lane<32>(as_u32(a.m))));
 #pragma unroll
       for (int i = 0; i < kChunk / 32; ++i)
@@ -177,7 +179,7 @@ struct ScoreOut {
       a.s += as_f32(other_lane<32>(as_u32(a.s)));
       a.w += as_f32(other_lane<32>(as_u32(a.w)));
       if (threadIdx.x % kWave < 32 && t < L.rows) {
-        const int64_t to = (A.first_chunk + v0 / kChunk) * L.rows + t;
+        const int64_t to = (A.first_chunk + tile * kChunks + in_tile / kChunk) * L.rows + t;
         A.m[to] = a.m;
         A.s[to] = a.s;
         A.w[to] = a.w;
@@ -425,7 +427,13 @@ int logits_tiles(int64_t rows, int64_t vocab, int64_t features, int type) {
   const ProductShape S = {vocab, rows, ceil_div(features, type == QA_F32 ? kPartsStep : kWholeStep), 1, false, type == QA_F32 ? kThreeProducts : kOneProduct};
   return product_plan(tiles_bit(kTiles256) | tiles_bit(kTiles128), S, 1).tiles == kTiles256 ? kTall256 : kTall128;
 }
-constexpr int64_t chunk_of(int tiles) { return tiles == kTall256 ? 128 : 64; }
+constexpr int64_t chunks_of(int tiles) { return tiles == kTall64 ? 4 : 2; }       // waves along a tile's vocabulary
+// Few rows: reading w is all that takes time, and each of the 512 tiles that run at a time gets as much of it, though that leaves it
+// a part empty (48 rows, 100003 x 2048: 107 us with 391 tiles of 256, %d with 512 of 196).
+int64_t pitch_of(int tiles, int64_t vocab) {
+  if (tiles == kTall64) return whole(ceil_div(vocab, 512 * ceil_div(vocab, 512 * 256)), 16);
+  return tiles == kTall256 ? 256 : 128;
+}
 
 // Equal pieces of n, whole tiles each, of at most `most`.
 int64_t piece_of(int64_t n, int64_t most) { return std::min(whole(n, kWholeStep), whole(ceil_div(n, ceil_div(n, most)), 256)); }
@@ -451,6 +459,7 @@ struct Plan {
   bool copy_x, copy_w;                             // for the logits
   int64_t parts, hp, piece, pieces;                // a copied row's columns; vocabulary of a launch
   int tiles;
+  int64_t pitch;
   size_t x, w, x_exp, w_exp;                       // copies and exponents
   size_t m, s, sw, given;                          // scoring
   int64_t chunks;
@@ -473,11 +482,13 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
   P.copy_x = !x || !rows_as_they_are || !in_place(x, L.x_stride);
   P.copy_w = !w || !rows_as_they_are || !in_place(w, L.w_stride);
   P.hp = whole(L.features, kWholeStep);
+  P.pitch = 256;
   if (op == QA_OP_LOGPROB) {
     P.tiles = logits_tiles(L.rows, L.vocab, L.features, type);
     P.piece = P.copy_w ? piece_of(L.vocab, power_of_two_within(kPieceBytes / (P.hp * 2 * P.parts), 16384)) : L.vocab;
     P.pieces = ceil_div(L.vocab, P.piece);
-    P.chunks = ceil_div(L.vocab, chunk_of(P.tiles));
+    P.pitch = pitch_of(P.tiles, std::min(P.piece, L.vocab));
+    P.chunks = ((P.pieces - 1) * ceil_div(P.piece, P.pitch) + ceil_div(L.vocab - (P.pieces - 1) * P.piece, P.pitch)) * chunks_of(P.tiles);
     P.m = room.take(4 * P.chunks * L.rows);
     P.s = room.take(4 * P.chunks * L.rows);
     P.sw = room.take(4 * P.chunks * L.rows);
@@ -529,12 +540,12 @@ int logits_operand(const void* from, int64_t stride, int64_t rows, const qa_outp
 }
 // Logits of a piece of the vocabulary: w's rows by x's.
 template <int TYPE, class Epilogue>
-int logits_launch(const Operand& w, const Operand& x, int64_t features, int tiles, const Epilogue& out, hipStream_t stream) {
+int logits_launch(const Operand& w, const Operand& x, int64_t features, int tiles, const Epilogue& out, hipStream_t stream, int64_t pitch = 256) {
   constexpr bool kBf16 = TYPE == QA_BF16;
   constexpr Lies kLie = TYPE == QA_F32 ? kRowsOfParts : kRows;
   if (tiles == kTall256) return product_launch<Product256<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
   if (tiles == kTall128) return product_launch<Product128<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
-  return product_launch<Product<kBf16, kLie, kLie, 4, 1, 2, 2>>(w, x, features, out, 1, stream);
+  return product_launch<Product<kBf16, kLie, kLie, 4, 1, 2, 2>>(w, x, features, out, 1, stream, 1, pitch);
 }
 
 template <int TYPE>
@@ -550,9 +561,10 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
     const int64_t vocab = std::min(P.piece, L.vocab - first);
     if (const int rc = logits_operand<TYPE>((const ElemT<TYPE>*)w + first * L.w_stride, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp, wo, stream)) return rc;
     A.first = first;
-    A.first_chunk = first / chunk_of(P.tiles);
+    A.first_chunk = first / P.piece * ceil_div(P.piece, P.pitch) * chunks_of(P.tiles);
+    A.pitch = P.pitch;
     const ScoreOut<TYPE == QA_F32> out{LayerArgs{L.rows, vocab, x_exp, w_exp, target}, A};
-    if (const int rc = logits_launch<TYPE>(wo, xo, L.features, P.tiles, out, stream)) return rc;
+    if (const int rc = logits_launch<TYPE>(wo, xo, L.features, P.tiles, out, stream, P.pitch)) return rc;
   }
   if (L.rows < 256)
     output_join_kernel<1><<<(unsigned)L.rows, kThreads, 0, stream>>>(A, L.rows, P.chunks, L.vocab, target, logprob, entropy, stats);

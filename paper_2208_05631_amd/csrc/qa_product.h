@@ -32,12 +32,13 @@ struct Operand {
   const void* p;                                   // 16-byte aligned
   int64_t ld;                                      // elements between rows, a multiple of 8, < 2^22
   int64_t batch;                                   // elements between matrices
-  int64_t n;                                       // how many i there are; past them the last ones are read again
+  int64_t n;                                       // how many i there are
 };
 struct ProductArgs {
   Operand a, b;
   int steps, split_steps;                          // of k, and of one split of them
   unsigned splits, tiles_m, tiles_n, tiles;        // tiles: of one matrix
+  int64_t pitch;                                   // values of a's i from tile to tile, a tile's side at most
 };
 
 // Brings SIDE values of i and STEP of k to LDS, straight from memory, 16 bytes per lane.
@@ -58,7 +59,8 @@ struct Bringer {
   int64_t advance;
   uint32_t off[kLoads];
 
-  __device__ __forceinline__ void begin(const Operand& O, int64_t matrix, int64_t i0, int first_step, int wave) {
+  // Values of i from i0 up to `end`; past them the last ones are read again.
+  __device__ __forceinline__ void begin(const Operand& O, int64_t matrix, int64_t i0, int64_t end, int first_step, int wave) {
     const int lane = threadIdx.x % kWave;
     const char* p = (const char*)O.p + matrix * O.batch * 2;
     if constexpr (in_rows(LIES)) {
@@ -68,11 +70,11 @@ struct Bringer {
       const uint32_t octet = (uint32_t)(LIES == kRows ? slot : LIES == kHiOfRows ? 2 * slot : 2 * (slot & 1) + (slot >> 1)) * 16;
 #pragma unroll
       for (int v = 0; v < kLoads; ++v)
-        off[v] = (uint32_t)min((int64_t)((v * WAVES + wave) * 16 + lane / 4), O.n - 1 - i0) * (uint32_t)(2 * O.ld) + octet;
+        off[v] = (uint32_t)min((int64_t)((v * WAVES + wave) * 16 + lane / 4), end - 1 - i0) * (uint32_t)(2 * O.ld) + octet;
     } else {
       advance = STEP * O.ld * 2;
       at = p + i0 * 2 * kParts + first_step * advance;
-      const int last = (int)min((int64_t)SIDE, (O.n - i0 + 7) / 8 * 8) / 8 - 1;
+      const int last = (int)min((int64_t)SIDE, (end - i0 + 7) / 8 * 8) / 8 - 1;
 #pragma unroll
       for (int v = 0; v < kLoads; ++v) {
         const int chunk = (v * WAVES + wave) * 64 + lane, k = chunk / (kPitch / 16), slot = (chunk % (kPitch / 16)) ^ 4 * (k & 3);
@@ -157,6 +159,7 @@ struct Product {
   Reader<LB, kN, kStep, FN> read_b;
   int to_load, wave;
   int64_t matrix, split;                           // which of the batch, and of the splits of k
+  int64_t tile_m;                                  // which tile along a
   bool owns;                                       // whether this wave has the sums
 
   // Instructions [FROM, TO) of a step's; behind the last one go on, past the last step to itself.
@@ -241,8 +244,8 @@ struct Product {
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
-    bring_a.begin(A.a, matrix, m0, begin + min(share, in_split - 1), wave);
-    bring_b.begin(A.b, matrix, n0, begin + min(share, in_split - 1), wave);
+    bring_a.begin(A.a, matrix, m0, min(A.a.n, m0 + A.pitch), begin + min(share, in_split - 1), wave);
+    bring_b.begin(A.b, matrix, n0, A.b.n, begin + min(share, in_split - 1), wave);
     bring_a.advance *= SHARE;
     bring_b.advance *= SHARE;
     char* const lds = all_lds + share * kBuffers * kBuffer;
@@ -379,16 +382,18 @@ __global__ __launch_bounds__(P::kGroup, P::kWavesPerSimd) void product_kernel(Pr
   const unsigned tile = on_its_die(), which = tile / A.tiles, matrix = which / A.splits;
   unsigned tm, tn;
   tile_of<LOWER>(A, tile - which * A.tiles, tm, tn);
-  const int64_t m0 = (int64_t)tm * P::kM, n0 = (int64_t)tn * P::kN;
+  const int64_t m0 = (int64_t)tm * A.pitch, n0 = (int64_t)tn * P::kN;
   P p;
+  p.tile_m = tm;
   p.run(A, matrix, which - matrix * A.splits, m0, n0, lds);
   if (p.owns) out(p, p.wave_m(m0), p.wave_n(n0), lds + p.wave * (P::kBuffers * P::kBuffer / P::kWavesHere));
 }
 
 // Launches tiles of the given form over all of A and B; k: how many there are, zeros up to a whole step.
 template <class P, bool LOWER = false, class Epilogue>
-int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream, int64_t splits = 1) {
-  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), 0, 0, (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN), 0};
+int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream, int64_t splits = 1,
+                   int64_t pitch = P::kM) {
+  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), 0, 0, (unsigned)ceil_div(a.n, pitch), (unsigned)ceil_div(b.n, P::kN), 0, pitch};
   A.split_steps = (int)ceil_div(A.steps, splits);
   A.splits = (unsigned)ceil_div(A.steps, A.split_steps);       // none is empty
   A.tiles = LOWER ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n;
