@@ -138,7 +138,6 @@ struct ScoreArgs {
   float *m, *s, *w;                                // [chunk][rows]: a wave's part of a tile
   float* given;                                    // the targets' logits
   int64_t first, first_chunk;                      // of this launch's vocabulary
-  int64_t pitch;                                   // of the tiles
 };
 
 template <bool SCALED>
@@ -146,9 +145,8 @@ struct ScoreOut {
   LayerArgs L;                                     // vocab: of this launch
   ScoreArgs A;
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0, char*) const {
-    constexpr int kChunk = 32 * (int)(sizeof p.acc / sizeof p.acc[0]), kChunks = P::kM / kChunk;
-    const int64_t tile = p.tile_m, in_tile = v0 - tile * A.pitch;
-    const int left = (int)max((int64_t)0, min(min((int64_t)kChunk, A.pitch - in_tile), L.vocab - v0));       // of this wave's logits there are
+    constexpr int kChunk = 32 * (int)(sizeof p.acc / sizeof p.acc[0]);
+    const int left = (int)max((int64_t)0, min((int64_t)kChunk, L.vocab - v0));       // of this wave's logits there are
 #pragma unroll
     for (int j = 0; j < (int)(sizeof p.acc[0] / sizeof p.acc[0][0]); ++j) {
       const int64_t t = t0 + 32 * j + threadIdx.x % 32;
@@ -179,7 +177,7 @@ struct ScoreOut {
       a.s += as_f32(other_lane<32>(as_u32(a.s)));
       a.w += as_f32(other_lane<32>(as_u32(a.w)));
       if (threadIdx.x % kWave < 32 && t < L.rows) {
-        const int64_t to = (A.first_chunk + tile * kChunks + in_tile / kChunk) * L.rows + t;
+        const int64_t to = (A.first_chunk + v0 / kChunk) * L.rows + t;
         A.m[to] = a.m;
         A.s[to] = a.s;
         A.w[to] = a.w;
@@ -187,6 +185,179 @@ struct ScoreOut {
     }
   }
 };
+
+// ---- scoring of few rows --------------------------------------------------------------------------------------------------------
+//
+// Up to 64 rows: reading w is all that takes time.  It goes from memory to registers, from any place and in any type, and each of its elements
+// is multiplied at once with all rows of x, which lie in LDS, a piece of k at a time: binary32 in three bfloat16 parts (six products, what is
+// left out is below 2^-24).  A wave has sixteen rows of w twice, eight waves go over the work-group's share of the vocabulary, and a lane keeps
+// the maximum and the sums of its logits all along.
+
+typedef float f32x4m __attribute__((ext_vector_type(4)));
+constexpr int kStreamGroup = 512, kStreamWaves = kStreamGroup / kWave, kStreamRows = 2 * 16 * kStreamWaves;
+template <int TYPE> constexpr int stream_parts = TYPE == QA_F32 ? 3 : 1;
+// Columns of k of x in LDS, in steps of 32: 64 KiB.
+template <int TYPE, int NB> constexpr int stream_k = 2048 / NB / stream_parts<TYPE> / 128 * 128;
+
+struct StreamArgs {
+  LayerArgs L;                                     // without exponents
+  ScoreArgs A;
+  const void *x, *w;
+  int64_t x_stride, w_stride;
+  int features;
+  int64_t each;                                    // of the vocabulary per work-group, a multiple of 16
+};
+
+template <int TYPE, int NB>
+__global__ __launch_bounds__(kStreamGroup, 4) void output_stream_kernel(StreamArgs S) {
+  typedef ElemT<TYPE> T;
+  constexpr int P = stream_parts<TYPE>, KC = stream_k<TYPE, NB>, kPitch = KC + 8, kPlane = 16 * NB * kPitch;
+  constexpr int U = TYPE == QA_F32 ? 1 : NB == 1 ? 4 : 2;      // steps of w that are on their way, twice: what registers hold
+  static_assert(KC % (64 * U) == 0, "whole blocks, two by two");
+  __shared__ __attribute__((aligned(16))) uint16_t lds[P * kPlane];
+  __shared__ Sums joined[kStreamWaves][16 * NB];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, K = S.features;
+  const int64_t r0 = (int64_t)blockIdx.x * S.each, r1 = min(S.L.vocab, r0 + S.each);
+  Sums sums[NB];
+  int64_t at[NB];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    sums[n] = no_sums();
+    const int64_t t = 16 * n + lane % 16;
+    at[n] = S.L.target && t < S.L.rows ? S.L.target[t] : -1;
+  }
+
+  for (int64_t base = r0; base < r1; base += kStreamRows) {
+    const T* from[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) from[g] = (const T*)S.w + min(base + (2 * wave + g) * 16 + lane % 16, S.L.vocab - 1) * S.w_stride;
+    f32x4m acc[2][NB] = {};
+    Raw8<TYPE> raw[2][2][U];
+    const auto load = [&](Raw8<TYPE> (&to)[2][U], int k) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          // No branch, which would wait for what is on its way: past the end the last eight, and nobody uses them.
+          to[g][u] = load_raw<TYPE>(from[g] + min(k + 32 * u + 8 * (lane / 16), K - kVec));
+    };
+    const auto multiply = [&](const auto& of, int k, auto steps) {
+#pragma unroll
+      for (int u = 0; u < decltype(steps)::value; ++u) {
+        u32x4 a[2][P];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          if constexpr (TYPE == QA_F32) {
+            float v[kVec];
+            to_f32<TYPE>(of[g][u], v);
+            split_parts<P>(v, a[g]);
+          } else {
+            a[g][0] = of[g][u].a;
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int q = 0; q < P; ++q) {
+            const u32x4 b = *reinterpret_cast<const u32x4*>(lds + q * kPlane + (16 * n + lane % 16) * kPitch + k + 32 * u + 8 * (lane / 16));
+#pragma unroll
+            for (int p = 0; p + q < P; ++p)
+#pragma unroll
+              for (int g = 0; g < 2; ++g) {
+                if constexpr (TYPE == QA_F16)
+                  acc[g][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a[g][p]), __builtin_bit_cast(f16x8, b), acc[g][n], 0, 0, 0);
+                else
+                  acc[g][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[g][p]), __builtin_bit_cast(bf16x8, b), acc[g][n], 0, 0, 0);
+              }
+          }
+      }
+    };
+    load(raw[0], 0);
+    for (int k0 = 0; k0 < K; k0 += KC) {
+      if (K > KC || base == r0) {                  // or all of x lies there already
+        __syncthreads();
+        for (int i = threadIdx.x; i < 16 * NB * (KC / kVec); i += kStreamGroup) {
+          const int row = i / (KC / kVec), col = i % (KC / kVec) * kVec;
+          const int n = row < S.L.rows ? max(0, min(kVec, K - k0 - col)) : 0;
+          float v[kVec] = {};
+          u32x4 part[P] = {};
+          if constexpr (TYPE == QA_F32) {
+            if (n) to_f32<TYPE>(load_raw<TYPE>((const T*)S.x + row * S.x_stride + k0 + col, n), v);
+            split_parts<P>(v, part);
+          } else if (n) {
+            part[0] = load_raw<TYPE>((const T*)S.x + row * S.x_stride + k0 + col, n).a;
+          }
+#pragma unroll
+          for (int p = 0; p < P; ++p) *reinterpret_cast<u32x4*>(lds + p * kPlane + row * kPitch + col) = part[p];
+        }
+        __syncthreads();
+      }
+      typedef std::integral_constant<int, U> All;
+      const int end = min(KC, K - k0), blocks = end / (64 * U) * (64 * U);
+#pragma unroll 1
+      for (int k = 0; k < blocks; k += 64 * U) {
+        load(raw[1], k0 + k + 32 * U);
+        multiply(raw[0], k, All());
+        load(raw[0], k0 + k + 64 * U);
+        multiply(raw[1], k + 32 * U, All());
+      }
+#pragma unroll 1
+      for (int k = blocks; k < end; k += 32) {     // the end of the rows
+        Raw8<TYPE> one[2][1];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) one[g][0] = load_raw<TYPE>(from[g] + k0 + k + 8 * (lane / 16), K - (k0 + k + 8 * (lane / 16)));
+        multiply(one, k, std::integral_constant<int, 1>());
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      float most = sums[n].m;
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int64_t v = base + (2 * wave + g) * 16 + 4 * (lane / 16) + e;
+          if (v == at[n] && v < r1) S.A.given[16 * n + lane % 16] = acc[g][n][e];
+          acc[g][n][e] = v < r1 ? acc[g][n][e] : -__builtin_inff();
+          most = fmaxf(most, acc[g][n][e]);
+        }
+      raise(sums[n], most);
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float y = (acc[g][n][e] - most) * kLog2e, q = __builtin_amdgcn_exp2f(y);
+          sums[n].s += q;
+          sums[n].w = __builtin_fmaf(q, fmaxf(y, kFar), sums[n].w);
+        }
+    }
+  }
+  const auto join = [](Sums& a, Sums b) {
+    const float m = fmaxf(a.m, b.m);
+    raise(a, m);
+    raise(b, m);
+    a.s += b.s;
+    a.w += b.w;
+  };
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+#pragma unroll
+    for (int s = 16; s < kWave; s *= 2) join(sums[n], Sums{__shfl_xor(sums[n].m, s, kWave), __shfl_xor(sums[n].s, s, kWave), __shfl_xor(sums[n].w, s, kWave)});
+    if (lane < 16) joined[wave][16 * n + lane] = sums[n];
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < S.L.rows) {
+    Sums a = joined[0][threadIdx.x];
+#pragma unroll 1
+    for (int i = 1; i < kStreamWaves; ++i) join(a, joined[i][threadIdx.x]);
+    const int64_t to = (int64_t)blockIdx.x * S.L.rows + threadIdx.x;
+    S.A.m[to] = a.m;
+    S.A.s[to] = a.s;
+    S.A.w[to] = a.w;
+  }
+}
+
+// ---- a row's numbers -------------------------------------------------------------------------------------------------------------
 
 // A row's numbers from its chunks': ROWS rows per work-group, the other threads along the chunks.
 template <int ROWS>
@@ -417,23 +588,20 @@ struct Room {
   }
 };
 
+constexpr int64_t kFewRows = 64;
+
 // Time of a step of k beside one of three products of 16: 32 k and one product bring as much for two thirds of the matrix instructions.
 constexpr double kOneProduct = 0.75, kTwoProducts = 0.65, kThreeProducts = 1.0;
 
-// Which tiles multiply the logits: heights (vocabulary) of chunks, and widths (rows).
-enum { kTall256, kTall128, kTall64 };
+// Which tiles multiply the logits, in vocabulary by rows: 256 x 64 for few rows, 256 x 256 or 128 x 128.
+enum { kTall256, kTall128, kFlat };
 int logits_tiles(int64_t rows, int64_t vocab, int64_t features, int type) {
-  if (rows <= 64) return kTall64;
+  if (rows <= kFewRows) return kFlat;
   const ProductShape S = {vocab, rows, ceil_div(features, type == QA_F32 ? kPartsStep : kWholeStep), 1, false, type == QA_F32 ? kThreeProducts : kOneProduct};
   return product_plan(tiles_bit(kTiles256) | tiles_bit(kTiles128), S, 1).tiles == kTiles256 ? kTall256 : kTall128;
 }
-constexpr int64_t chunks_of(int tiles) { return tiles == kTall64 ? 4 : 2; }       // waves along a tile's vocabulary
-// Few rows: reading w is all that takes time, and each of the 512 tiles that run at a time gets as much of it, though that leaves it
-// a part empty (48 rows, 100003 x 2048: 107 us with 391 tiles of 256, %d with 512 of 196).
-int64_t pitch_of(int tiles, int64_t vocab) {
-  if (tiles == kTall64) return whole(ceil_div(vocab, 512 * ceil_div(vocab, 512 * 256)), 16);
-  return tiles == kTall256 ? 256 : 128;
-}
+constexpr int64_t height_of(int tiles) { return tiles == kTall128 ? 128 : 256; }
+constexpr int64_t chunks_of(int tiles) { return tiles == kFlat ? 4 : 2; }         // of a tile
 
 // Equal pieces of n, whole tiles each, of at most `most`.
 int64_t piece_of(int64_t n, int64_t most) { return std::min(whole(n, kWholeStep), whole(ceil_div(n, ceil_div(n, most)), 256)); }
@@ -458,11 +626,11 @@ int64_t power_of_two_within(int64_t n, int64_t least) {
 struct Plan {
   bool copy_x, copy_w;                             // for the logits
   int64_t parts, hp, piece, pieces;                // a copied row's columns; vocabulary of a launch
+  bool streams;                                    // w, for few rows that would have to be copied
   int tiles;
-  int64_t pitch;
   size_t x, w, x_exp, w_exp;                       // copies and exponents
   size_t m, s, sw, given;                          // scoring
-  int64_t chunks;
+  int64_t chunks, each;                            // each: of the vocabulary per work-group, where w is streamed
   size_t scales, xc, wc, c, sums;                  // gradient: x and w as the products with c take them
   size_t dw_sums;
   int64_t hc, tp, vp;
@@ -482,17 +650,18 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
   P.copy_x = !x || !rows_as_they_are || !in_place(x, L.x_stride);
   P.copy_w = !w || !rows_as_they_are || !in_place(w, L.w_stride);
   P.hp = whole(L.features, kWholeStep);
-  P.pitch = 256;
-  if (op == QA_OP_LOGPROB) {
+  // Copying w takes longer than the products of few rows with it (48 rows, 100003 x 2049 binary16: 294 us, 220 from where it lies; one row,
+  // 47236 x 515 binary32: 76, 57), but where it can be brought straight to LDS, that is faster (100003 x 2048: 107, 123).
+  P.streams = op == QA_OP_LOGPROB && L.rows <= kFewRows && L.features >= kVec && (P.copy_x || P.copy_w);
+  if (P.streams) {
+    P.copy_x = P.copy_w = false;
+    P.each = whole(ceil_div(L.vocab, 512), 16);
+    P.chunks = ceil_div(L.vocab, P.each);
+  } else if (op == QA_OP_LOGPROB) {
     P.tiles = logits_tiles(L.rows, L.vocab, L.features, type);
     P.piece = P.copy_w ? piece_of(L.vocab, power_of_two_within(kPieceBytes / (P.hp * 2 * P.parts), 16384)) : L.vocab;
     P.pieces = ceil_div(L.vocab, P.piece);
-    P.pitch = pitch_of(P.tiles, std::min(P.piece, L.vocab));
-    P.chunks = ((P.pieces - 1) * ceil_div(P.piece, P.pitch) + ceil_div(L.vocab - (P.pieces - 1) * P.piece, P.pitch)) * chunks_of(P.tiles);
-    P.m = room.take(4 * P.chunks * L.rows);
-    P.s = room.take(4 * P.chunks * L.rows);
-    P.sw = room.take(4 * P.chunks * L.rows);
-    P.given = room.take(4 * L.rows);
+    P.chunks = chunks_of(P.tiles) * ((P.pieces - 1) * ceil_div(P.piece, height_of(P.tiles)) + ceil_div(L.vocab - (P.pieces - 1) * P.piece, height_of(P.tiles)));
   } else {
     P.tp = whole(L.rows, kPartsStep);
     P.hc = whole(L.features, 8);
@@ -513,6 +682,12 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.sums = room.take(P.pieces > 1 || P.dx.splits > 1 ? 4 * P.dx.splits * L.rows * L.features : 0);
     P.dw_sums = room.take(P.dw.splits > 1 ? 4 * P.dw.splits * vocab * L.features : 0);
   }
+  if (op == QA_OP_LOGPROB) {
+    P.m = room.take(4 * P.chunks * L.rows);
+    P.s = room.take(4 * P.chunks * L.rows);
+    P.sw = room.take(4 * P.chunks * L.rows);
+    P.given = room.take(4 * L.rows);
+  }
   P.x_exp = room.take(type == QA_F32 ? 4 * L.rows : 0);
   P.w_exp = room.take(type == QA_F32 ? 4 * P.piece : 0);
   P.x = room.take(P.copy_x ? 2 * P.parts * L.rows * P.hp : 0);
@@ -520,8 +695,11 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
   P.bytes = room.bytes;
   return P;
 }
-// At most, whatever the alignment of x and w: in place, the scored vocabulary is one piece, which needs less.
-size_t bytes_of(const qa_output_layer& L, int op, int type) { return plan_of(L, op, type, nullptr, nullptr).bytes; }
+// At most, whatever the alignment of x and w.
+size_t bytes_of(const qa_output_layer& L, int op, int type) {
+  alignas(16) static const char aligned_place[16] = {};
+  return std::max(plan_of(L, op, type, nullptr, nullptr).bytes, plan_of(L, op, type, aligned_place, aligned_place).bytes);
+}
 
 template <int TYPE, Copies HOW>
 int copy_launch(const CopyArgs& A, hipStream_t stream) {
@@ -540,12 +718,12 @@ int logits_operand(const void* from, int64_t stride, int64_t rows, const qa_outp
 }
 // Logits of a piece of the vocabulary: w's rows by x's.
 template <int TYPE, class Epilogue>
-int logits_launch(const Operand& w, const Operand& x, int64_t features, int tiles, const Epilogue& out, hipStream_t stream, int64_t pitch = 256) {
+int logits_launch(const Operand& w, const Operand& x, int64_t features, int tiles, const Epilogue& out, hipStream_t stream) {
   constexpr bool kBf16 = TYPE == QA_BF16;
   constexpr Lies kLie = TYPE == QA_F32 ? kRowsOfParts : kRows;
   if (tiles == kTall256) return product_launch<Product256<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
-  if (tiles == kTall128) return product_launch<Product128<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
-  return product_launch<Product<kBf16, kLie, kLie, 4, 1, 2, 2>>(w, x, features, out, 1, stream, 1, pitch);
+  if (tiles == kFlat) return product_launch<Product<kBf16, kLie, kLie, 4, 1, 2, 2>>(w, x, features, out, 1, stream);
+  return product_launch<Product128<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
 }
 
 template <int TYPE>
@@ -554,17 +732,23 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
   const Plan P = plan_of(L, QA_OP_LOGPROB, TYPE, x, w);
   int* const x_exp = (int*)(ws + P.x_exp);
   int* const w_exp = (int*)(ws + P.w_exp);
+  ScoreArgs A = {(float*)(ws + P.m), (float*)(ws + P.s), (float*)(ws + P.sw), (float*)(ws + P.given), 0, 0};
+  if (P.streams) {
+    const StreamArgs S = {LayerArgs{L.rows, L.vocab, nullptr, nullptr, target}, A, x, w, L.x_stride, L.w_stride, (int)L.features, P.each};
+    const auto kernel = L.rows <= 16 ? output_stream_kernel<TYPE, 1> : L.rows <= 32 ? output_stream_kernel<TYPE, 2> : output_stream_kernel<TYPE, 4>;
+    kernel<<<(unsigned)P.chunks, kStreamGroup, 0, stream>>>(S);
+    output_join_kernel<1><<<(unsigned)L.rows, kThreads, 0, stream>>>(A, L.rows, P.chunks, L.vocab, target, logprob, entropy, stats);
+    return launch_status();
+  }
   Operand xo, wo;
   if (const int rc = logits_operand<TYPE>(x, L.x_stride, L.rows, L, P, P.copy_x, ws + P.x, x_exp, xo, stream)) return rc;
-  ScoreArgs A = {(float*)(ws + P.m), (float*)(ws + P.s), (float*)(ws + P.sw), (float*)(ws + P.given), 0, 0};
   for (int64_t first = 0; first < L.vocab; first += P.piece) {
     const int64_t vocab = std::min(P.piece, L.vocab - first);
     if (const int rc = logits_operand<TYPE>((const ElemT<TYPE>*)w + first * L.w_stride, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp, wo, stream)) return rc;
     A.first = first;
-    A.first_chunk = first / P.piece * ceil_div(P.piece, P.pitch) * chunks_of(P.tiles);
-    A.pitch = P.pitch;
+    A.first_chunk = first / P.piece * chunks_of(P.tiles) * ceil_div(P.piece, height_of(P.tiles));
     const ScoreOut<TYPE == QA_F32> out{LayerArgs{L.rows, vocab, x_exp, w_exp, target}, A};
-    if (const int rc = logits_launch<TYPE>(wo, xo, L.features, P.tiles, out, stream, P.pitch)) return rc;
+    if (const int rc = logits_launch<TYPE>(wo, xo, L.features, P.tiles, out, stream)) return rc;
   }
   if (L.rows < 256)
     output_join_kernel<1><<<(unsigned)L.rows, kThreads, 0, stream>>>(A, L.rows, P.chunks, L.vocab, target, logprob, entropy, stats);

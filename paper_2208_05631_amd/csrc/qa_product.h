@@ -38,7 +38,6 @@ struct ProductArgs {
   Operand a, b;
   int steps, split_steps;                          // of k, and of one split of them
   unsigned splits, tiles_m, tiles_n, tiles;        // tiles: of one matrix
-  int64_t pitch;                                   // values of a's i from tile to tile, a tile's side at most
 };
 
 // Brings SIDE values of i and STEP of k to LDS, straight from memory, 16 bytes per lane.
@@ -159,7 +158,6 @@ struct Product {
   Reader<LB, kN, kStep, FN> read_b;
   int to_load, wave;
   int64_t matrix, split;                           // which of the batch, and of the splits of k
-  int64_t tile_m;                                  // which tile along a
   bool owns;                                       // whether this wave has the sums
 
   // Instructions [FROM, TO) of a step's; behind the last one go on, past the last step to itself.
@@ -244,7 +242,7 @@ struct Product {
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
-    bring_a.begin(A.a, matrix, m0, min(A.a.n, m0 + A.pitch), begin + min(share, in_split - 1), wave);
+    bring_a.begin(A.a, matrix, m0, A.a.n, begin + min(share, in_split - 1), wave);
     bring_b.begin(A.b, matrix, n0, A.b.n, begin + min(share, in_split - 1), wave);
     bring_a.advance *= SHARE;
     bring_b.advance *= SHARE;
@@ -382,18 +380,16 @@ __global__ __launch_bounds__(P::kGroup, P::kWavesPerSimd) void product_kernel(Pr
   const unsigned tile = on_its_die(), which = tile / A.tiles, matrix = which / A.splits;
   unsigned tm, tn;
   tile_of<LOWER>(A, tile - which * A.tiles, tm, tn);
-  const int64_t m0 = (int64_t)tm * A.pitch, n0 = (int64_t)tn * P::kN;
+  const int64_t m0 = (int64_t)tm * P::kM, n0 = (int64_t)tn * P::kN;
   P p;
-  p.tile_m = tm;
   p.run(A, matrix, which - matrix * A.splits, m0, n0, lds);
   if (p.owns) out(p, p.wave_m(m0), p.wave_n(n0), lds + p.wave * (P::kBuffers * P::kBuffer / P::kWavesHere));
 }
 
 // Launches tiles of the given form over all of A and B; k: how many there are, zeros up to a whole step.
 template <class P, bool LOWER = false, class Epilogue>
-int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream, int64_t splits = 1,
-                   int64_t pitch = P::kM) {
-  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), 0, 0, (unsigned)ceil_div(a.n, pitch), (unsigned)ceil_div(b.n, P::kN), 0, pitch};
+int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream, int64_t splits = 1) {
+  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), 0, 0, (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN), 0};
   A.split_steps = (int)ceil_div(A.steps, splits);
   A.splits = (unsigned)ceil_div(A.steps, A.split_steps);       // none is empty
   A.tiles = LOWER ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n;

@@ -144,6 +144,21 @@ __device__ __forceinline__ void store_raw(ElemT<TYPE>* p, const Raw8<TYPE>& r, i
     if (i < n) p[i] = v[i];
 }
 
+// v as `P` bfloat16 parts, each the leading eight bits of what is left: exact for 8 P bits, but for what lies below 2^-133,
+// bfloat16's last bit (matrix instructions take numbers under 2^-126 as they are).
+template <int P>
+__device__ __forceinline__ void split_parts(float (&v)[kVec], u32x4 (&part)[P]) {
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[p][i] = __builtin_amdgcn_perm(as_u32(v[2 * i + 1]), as_u32(v[2 * i]), 0x07060302u);
+    if (p + 1 < P) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[i] = v[i] - as_f32(as_u32(v[i]) & 0xFFFF0000u);
+    }
+  }
+}
+
 // ---- between lanes ---------------------------------------------------------------------------------------
 
 __device__ __forceinline__ float wave_sum_f32(float v) {
