@@ -12,7 +12,11 @@ parameters lie in one flat binary32 vector with a list of tensors.  A worker's s
   message   qa_quantize_pack_segments, one threshold and scale per tensor
   update    qa_step_qcmd_segments on the average of all workers' messages
 
-Run: python examples/next_token.py [steps]
+Two of these have another form.  Without kept logits (`keep_logits=False`) the loss is qa_output_logprob and its gradient
+qa_output_logprob_grad, which multiply the output matrix themselves.  With `orthogonal` the blocks' square matrices are stepped by
+qa_step_orthogonal on the average of their messages (qa_aggregate_unpack), the other tensors by QCMD.
+
+Run: python examples/next_token.py [steps] [--no-logits] [--orthogonal]
 """
 import math
 import os
@@ -30,8 +34,8 @@ EPS = 1e-6
 class Model:
     """The list of tensors, and one worker's forward and backward pass on the flat vector."""
 
-    def __init__(self, vocab, width, layers, rows, device="cuda:0", group=32):
-        self.vocab, self.width, self.layers, self.rows, self.dev = vocab, width, layers, rows, device
+    def __init__(self, vocab, width, layers, rows, device="cuda:0", group=32, keep_logits=True):
+        self.vocab, self.width, self.layers, self.rows, self.dev, self.keep_logits = vocab, width, layers, rows, device, keep_logits
         shapes = [("embedding", (vocab, width))]
         for i in range(layers):
             shapes += [(f"norm{i}", (width,)), (f"w{i}", (width, width))]
@@ -44,11 +48,13 @@ class Model:
             at += -(-self.length[-1] // 16) * 16
         self.d = at
         self.codes = qa.CodedRows.make(rows, width, group)
+        self.output = qa.OutputLayer.make(rows, vocab, width)
         room = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, device=device)  # noqa: E731
         self.ws = room(max(qa.qa_rows_workspace_bytes(self.codes, qa.QA_OP_WEIGHT_GRAD, qa.QA_BF16, vocab),
                            qa.qa_rows_workspace_bytes(self.codes, qa.QA_OP_WEIGHT_GRAD, qa.QA_BF16, width),
                            qa.qa_rows_workspace_bytes(self.codes, qa.QA_OP_NORM_GRAD, qa.QA_BF16),
-                           qa.qa_token_workspace_bytes(rows, vocab, 1)))
+                           qa.qa_token_workspace_bytes(rows, vocab, 1),
+                           *(qa.qa_output_workspace_bytes(self.output, op, qa.QA_BF16) for op in (qa.QA_OP_LOGPROB, qa.QA_OP_LOGPROB_GRAD) if not keep_logits)))
         new = lambda *shape, dtype=BF16: torch.empty(*shape, dtype=dtype, device=device)  # noqa: E731
         n = layers + 1
         self.stream = [new(rows, width) for _ in range(n)]                        # h after each addition
@@ -88,7 +94,7 @@ class Model:
 
     def gradient(self, x, g, before, after):
         """Gradient of the mean loss -log p(after | before) at the flat parameters x, into the flat g.  Returns nothing and waits for
-        nothing: logprob, entropy and top_index hold the batch's numbers."""
+        nothing: logprob, entropy and, with kept logits, top_index hold the batch's numbers."""
         T, V, out = self.rows, self.vocab, self.layers
         w = {n: self.view(x, n).to(BF16) for n in self.shape if n.startswith("w")}
         h, add = self.view(x, "embedding")[before].to(BF16), None
@@ -96,12 +102,18 @@ class Model:
             y = self._norm(i, h, add, self.view(x, f"norm{i}"))
             h, add = self.stream[i], y @ w[f"w{i}"].t()
         y = self._norm(out, h, add, self.view(x, "norm_out"))
-        logits = y @ w["w_out"].t()
-        qa.qa_token_logprob(qa.QA_BF16, T, V, logits, V, after, 1, self.logprob, self.entropy, self.stats, self.top, self.top_index, self.ws)
-
-        qa.qa_token_logprob_grad(qa.QA_BF16, T, V, logits, V, after, self.stats, None, self.weight_of_row, None, logits, V)     # in place
-        self._weight_grad(out, logits, self.view(g, "w_out"))
-        dh = self._norm_grad(out, logits @ w["w_out"], None, self.view(x, "norm_out"), self.view(g, "norm_out"))
+        if self.keep_logits:
+            logits = y @ w["w_out"].t()
+            qa.qa_token_logprob(qa.QA_BF16, T, V, logits, V, after, 1, self.logprob, self.entropy, self.stats, self.top, self.top_index, self.ws)
+            qa.qa_token_logprob_grad(qa.QA_BF16, T, V, logits, V, after, self.stats, None, self.weight_of_row, None, logits, V)     # in place
+            self._weight_grad(out, logits, self.view(g, "w_out"))
+            dy = logits @ w["w_out"]
+        else:
+            dy = torch.empty_like(y)
+            qa.qa_output_logprob(self.output, qa.QA_BF16, y, w["w_out"], after, self.logprob, self.entropy, self.stats, self.ws)
+            qa.qa_output_logprob_grad(self.output, qa.QA_BF16, y, w["w_out"], after, self.stats, None, self.weight_of_row, None, dy, self.width,
+                                      self.view(g, "w_out"), self.width, 0, self.ws)
+        dh = self._norm_grad(out, dy, None, self.view(x, "norm_out"), self.view(g, "norm_out"))
         for i in reversed(range(self.layers)):
             self._weight_grad(i, dh, self.view(g, f"w{i}"))
             dh = self._norm_grad(i, dh @ w[f"w{i}"], dh, self.view(x, f"norm{i}"), self.view(g, f"norm{i}"))
@@ -114,14 +126,38 @@ def source(vocab, seed=1):
     return torch.softmax(3.0 * torch.randn(vocab, vocab, generator=gen), dim=1)
 
 
-def train(steps=200, workers=4, rows=2048, vocab=257, width=96, layers=2, eta=0.02, lam=1e-7, say=print):
+class MatrixSteps:
+    """qa_step_orthogonal for some of a model's matrices, from all workers' messages: a matrix's code words and scale lie in them where its
+    components do."""
+
+    def __init__(self, model, names, workers, layout):
+        self.at = []
+        for name in names:
+            begin, shape = model.shape[name]
+            L = qa.Layout.make(math.prod(shape), workers, 0, code_stride=layout.code_stride, scale_stride=layout.scale_stride)
+            M = qa.Matrices.make(1, *shape)
+            need = qa.qa_orthogonal_workspace_bytes(M, qa.QA_F32)
+            mean = torch.empty(shape, device=model.dev)
+            self.at.append((begin, list(model.shape).index(name), L, M, mean, torch.zeros_like(mean), torch.empty(need, dtype=torch.uint8, device=model.dev) if need else None))
+
+    def step(self, codes, scales, x, eta):
+        for begin, tensor, L, M, mean, momentum, ws in self.at:
+            qa.qa_aggregate_unpack(L, codes[:, begin // 16:], scales[:, tensor:], mean)
+            qa.qa_step_orthogonal(M, mean, momentum, x[begin:], 0.9, 1, 5, None, eta, 1.0, ws)
+
+
+def train(steps=200, workers=4, rows=2048, vocab=257, width=96, layers=2, eta=0.02, lam=1e-7, say=print, keep_logits=True, orthogonal=False):
     dev = torch.device("cuda:0")
-    model = Model(vocab, width, layers, rows, dev)
+    model = Model(vocab, width, layers, rows, dev, keep_logits=keep_logits)
     x = model.initial()
     G, z = torch.zeros_like(x), None
+    square = [f"w{i}" for i in range(layers)] if orthogonal else []
+    length = [0 if name in square else n for name, n in zip(model.shape, model.length)]      # what QCMD steps
     table = qa.qa_segment_plan_bytes(model.d, len(model.begin))
     plan = qa.qa_segment_plan_init(model.d, model.begin, model.length, torch.empty(table, dtype=torch.uint8, device=dev))
+    rest = plan if not square else qa.qa_segment_plan_init(model.d, model.begin, length, torch.empty(table, dtype=torch.uint8, device=dev))
     L = qa.Layout.make(model.d, workers, 0, scale_stride=len(model.begin))
+    matrices = MatrixSteps(model, square, workers, L)
     g = torch.zeros(workers, model.d, device=dev)
     codes = torch.empty(workers, L.code_stride, dtype=torch.int32, device=dev)
     scales = torch.empty(workers, L.scale_stride, device=dev)
@@ -137,11 +173,12 @@ def train(steps=200, workers=4, rows=2048, vocab=257, width=96, layers=2, eta=0.
             model.gradient(x, g[m], before, after)
             loss -= model.logprob.mean() / workers
         qa.qa_quantize_pack_segments(L, plan, g, model.d, codes, scales, None, ws)
-        qa.qa_step_qcmd_segments(L, plan, codes, scales, x, G, z, eta, lam, 1e-8, qa.QA_REQUANT_NONE, None)
+        matrices.step(codes, scales, x, eta)
+        qa.qa_step_qcmd_segments(L, rest, codes, scales, x, G, z, eta, lam, 1e-8, qa.QA_REQUANT_NONE, None)
         losses.append(loss)
         if say and (step % 20 == 0 or step == steps - 1):
-            hit = float((model.top_index[:, 0] == after).float().mean())
-            say(f"step {step:4d}  loss {float(loss):.4f}  entropy {float(model.entropy.mean()):.4f}  most likely token right {hit:.3f}")
+            hit = f"  most likely token right {float((model.top_index[:, 0] == after).float().mean()):.3f}" if keep_logits else ""
+            say(f"step {step:4d}  loss {float(loss):.4f}  entropy {float(model.entropy.mean()):.4f}{hit}")
     least = float(-(p * torch.log(p)).sum(dim=1).mean())
     if say:
         say(f"loss of the source itself: {least:.4f}, of a guess: {math.log(vocab):.4f}")
@@ -149,4 +186,5 @@ def train(steps=200, workers=4, rows=2048, vocab=257, width=96, layers=2, eta=0.
 
 
 if __name__ == "__main__":
-    train(int(sys.argv[1]) if len(sys.argv) > 1 else 200)
+    numbers = [int(v) for v in sys.argv[1:] if not v.startswith("--")]
+    train(*numbers[:1] or [200], keep_logits="--no-logits" not in sys.argv, orthogonal="--orthogonal" in sys.argv)

@@ -637,13 +637,14 @@ typedef struct {
 
 #define QA_ORTHOGONAL_STEPS_MAX 32
 
-/* Bytes of device workspace that the calls below need for matrices of `type` (QA_F32 for qa_step_orthogonal): some 16 to 24
- * per element; 0 for invalid arguments and count == 0. */
+/* Bytes of device workspace that the calls below need for matrices of `type` (QA_F32 for qa_step_orthogonal): 8 to 16 per
+ * element; 0 for matrices that a compute unit holds (sides of up to some 128 x 128, 96 x 288 or 64 x 512), for
+ * invalid arguments and for count == 0. */
 size_t qa_orthogonal_workspace_bytes(const qa_matrices* matrices, int type);
 
 /* out = X_steps, 1 <= steps <= QA_ORTHOGONAL_STEPS_MAX.  coefficients: HOST array of 3*steps floats, a, b, c of each
  * step in turn, magnitudes below 64; NULL: 3.4445, -4.7750, 2.0315 in every step, by which all but the smallest singular values end
- * between 0.7 and 1.2 after five.  A matrix of zeros gives zeros; one with an infinity or a NaN gives NaN.  Numbers
+ * between 0.7 and 1.2 after five.  A matrix of zeros gives zeros; one with an infinity or a NaN gives NaN.  ws may be NULL if 0 bytes are needed.  Numbers
  * are held in two binary16 parts, 22 bits and a sign, in fixed point below 2^-24 (X_i of a magnitude of 64 and more, which no
  * polynomial of this use has, are infinite, and NaN from there on); norms in binary64, sums in binary32.  out may be g. */
 int qa_orthogonalize(const qa_matrices* matrices, int type, const void* g, int steps, const float* coefficients_or_null,

@@ -470,7 +470,7 @@ Plan plan_of(const qa_matrices& M) {
   while (P.lanes < kThreads && P.lanes * kVec < M.cols) P.lanes *= 2;
   P.norm_blocks = (int)std::min<int64_t>(std::max<int64_t>(kNormBlocks / std::max<int64_t>(M.count, 1), 16), ceil_div(M.rows * P.lanes, kThreads));
   P.norms = (size_t)whole(M.count * P.norm_blocks * 8, 256);
-  P.bytes = 2 * P.x + 2 * P.a + P.norms;
+  P.bytes = is_small(P.n, P.m) ? 0 : 2 * P.x + 2 * P.a + P.norms;
   return P;
 }
 
@@ -579,7 +579,9 @@ int check_steps(int steps, const float* coefficients) {
   return QA_OK;
 }
 int check_workspace(const qa_matrices* M, const void* ws, size_t ws_bytes) {
-  if (!ws || ws_bytes < plan_of(*M).bytes) return QA_ERR_WORKSPACE;
+  const size_t need = plan_of(*M).bytes;
+  if (need == 0) return QA_OK;
+  if (!ws || ws_bytes < need) return QA_ERR_WORKSPACE;
   return aligned(ws, 256) ? QA_OK : QA_ERR_ALIGNMENT;
 }
 

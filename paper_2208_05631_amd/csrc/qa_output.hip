@@ -360,10 +360,10 @@ __global__ __launch_bounds__(kStreamGroup, 4) void output_stream_kernel(StreamAr
 // ---- a row's numbers -------------------------------------------------------------------------------------------------------------
 
 // A row's numbers from its chunks': ROWS rows per work-group, the other threads along the chunks.
-template <int ROWS>
-__global__ __launch_bounds__(kThreads) void output_join_kernel(ScoreArgs A, int64_t rows, int64_t chunks, int64_t vocab, const int32_t* target,
+template <int ROWS, int THREADS>
+__global__ __launch_bounds__(THREADS) void output_join_kernel(ScoreArgs A, int64_t rows, int64_t chunks, int64_t vocab, const int32_t* target,
                                                                float* logprob, float* entropy, float* stats) {
-  constexpr int kShare = kThreads / ROWS;
+  constexpr int kShare = THREADS / ROWS;
   __shared__ Sums part[kShare][ROWS];
   const int r = threadIdx.x % ROWS, share = threadIdx.x / ROWS;
   const int64_t t = (int64_t)blockIdx.x * ROWS + r;
@@ -726,6 +726,15 @@ int logits_launch(const Operand& w, const Operand& x, int64_t features, int tile
   return product_launch<Product128<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
 }
 
+int join_launch(const ScoreArgs& A, const qa_output_layer& L, int64_t chunks, const int32_t* target, float* logprob, float* entropy, float* stats, hipStream_t stream) {
+  const auto launch = [&](auto kernel, int rows, int threads) {
+    kernel<<<(unsigned)ceil_div(L.rows, rows), threads, 0, stream>>>(A, L.rows, chunks, L.vocab, target, logprob, entropy, stats);
+    return launch_status();
+  };
+  if (L.rows <= kFewRows) return launch(output_join_kernel<1, 1024>, 1, 1024);
+  if (L.rows <= 2048) return launch(output_join_kernel<4, kThreads>, 4, kThreads);
+  return launch(output_join_kernel<16, kThreads>, 16, kThreads);
+}
 template <int TYPE>
 int score_launch(const qa_output_layer& L, const void* x, const void* w, const int32_t* target, float* logprob, float* entropy, float* stats,
                  char* ws, hipStream_t stream) {
@@ -737,8 +746,7 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
     const StreamArgs S = {LayerArgs{L.rows, L.vocab, nullptr, nullptr, target}, A, x, w, L.x_stride, L.w_stride, (int)L.features, P.each};
     const auto kernel = L.rows <= 16 ? output_stream_kernel<TYPE, 1> : L.rows <= 32 ? output_stream_kernel<TYPE, 2> : output_stream_kernel<TYPE, 4>;
     kernel<<<(unsigned)P.chunks, kStreamGroup, 0, stream>>>(S);
-    output_join_kernel<1><<<(unsigned)L.rows, kThreads, 0, stream>>>(A, L.rows, P.chunks, L.vocab, target, logprob, entropy, stats);
-    return launch_status();
+    return join_launch(A, L, P.chunks, target, logprob, entropy, stats, stream);
   }
   Operand xo, wo;
   if (const int rc = logits_operand<TYPE>(x, L.x_stride, L.rows, L, P, P.copy_x, ws + P.x, x_exp, xo, stream)) return rc;
@@ -750,11 +758,7 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
     const ScoreOut<TYPE == QA_F32> out{LayerArgs{L.rows, vocab, x_exp, w_exp, target}, A};
     if (const int rc = logits_launch<TYPE>(wo, xo, L.features, P.tiles, out, stream)) return rc;
   }
-  if (L.rows < 256)
-    output_join_kernel<1><<<(unsigned)L.rows, kThreads, 0, stream>>>(A, L.rows, P.chunks, L.vocab, target, logprob, entropy, stats);
-  else
-    output_join_kernel<16><<<(unsigned)ceil_div(L.rows, 16), kThreads, 0, stream>>>(A, L.rows, P.chunks, L.vocab, target, logprob, entropy, stats);
-  return launch_status();
+  return join_launch(A, L, P.chunks, target, logprob, entropy, stats, stream);
 }
 
 template <int TYPE>

@@ -43,7 +43,9 @@ def matrices_of(gen, N, R, C, t, pad=0, lead=0, scale=1.0):
 
 
 def room(M, t):
-    return torch.full((qa.qa_orthogonal_workspace_bytes(M, code_of(t)) // 4,), math.nan, device=DEV)
+    """Filled with NaN: nothing that a call reads there may be older than the call."""
+    need = qa.qa_orthogonal_workspace_bytes(M, code_of(t))
+    return torch.full((need // 4,), math.nan, device=DEV) if need else None
 
 
 def run(M, t, d, steps, coefficients, out=None):
@@ -187,3 +189,66 @@ def test_repeats_bit_for_bit():
 
 def test_no_matrices():
     qa.qa_orthogonalize(qa.Matrices.make(0, 4, 4), qa.QA_F32, None, 5, None, None, None)
+
+
+@pytest.mark.parametrize("N,R,C", [(2, 90, 70), (1, 300, 200)])
+def test_captured_and_replayed_among_eager_steps(N, R, C):
+    gen = gen_of("graph", R)
+    g, gd = matrices_of(gen, N, R, C, "f32", 0, 0, 1e-2)
+    _, x0 = matrices_of(gen, N, R, C, "f32", 0, 0, 0.1)
+    M = qa.Matrices.make(N, R, C)
+    ws = room(M, "f32")
+
+    def step(g, m, x):
+        qa.qa_step_orthogonal(M, g, m, x, 0.9, 1, 5, None, 0.02, 0.99, ws)
+    m, x = torch.zeros_like(gd), x0.clone()
+    want_m, want_x = torch.zeros_like(gd), x0.clone()
+    other_m, other_x = torch.zeros_like(gd), x0.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(gd, other_m, other_x)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(gd, m, x)
+    for i in range(5):
+        step(gd, want_m, want_x)
+        step(-gd, other_m, other_x)                               # the same workspace, other numbers
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(m, want_m) and torch.equal(x, want_x), i
+
+
+def test_offsets_beyond_32_bits():
+    """Rows 40000 elements apart, matrices 2^31 elements apart, at the end of the buffer."""
+    gen = gen_of("far")
+    R, C, stride, apart = 200, 150, 40000, (1 << 31) + 8
+    v = torch.randn(2, R, C, generator=gen)
+    flat = torch.empty(apart + R * stride, device=DEV)
+    for i in range(2):
+        flat[i * apart:i * apart + R * stride].view(R, stride)[:, :C] = v[i].to(DEV)
+    M = qa.Matrices(2, R, C, stride, apart)
+    run(M, "f32", flat, 3, None, out=flat)
+    near = run(qa.Matrices.make(2, R, C), "f32", v.to(DEV), 3, None)
+    for i in range(2):
+        assert torch.equal(flat[i * apart:i * apart + R * stride].view(R, stride)[:, :C], near[i])
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("N,R,C", [(3, 128, 128), (2, 288, 96), (1, 64, 512), (1, 512, 64), (1, 129, 129), (1, 64, 513), (300, 17, 23)])
+def test_sides_of_what_a_compute_unit_holds(t, N, R, C):
+    gen = gen_of("held", t, N, R, C)
+    v, d = matrices_of(gen, N, R, C, t)
+    out = run(qa.Matrices.make(N, R, C), t, d, 5, None)
+    for i in {0, N // 2, N - 1}:
+        assert off(out[i].cpu().to(F64), ref.orthogonal(v[i], 5)) <= 341 * 8 * U + HALF_ULP[t]
+
+
+def test_many_matrices_side_by_side():
+    gen = gen_of("many")
+    v, d = matrices_of(gen, 700, 40, 600, "bf16")
+    out = run(qa.Matrices.make(700, 40, 600), "bf16", d, 5, None)
+    for i in (0, 1, 350, 699):
+        assert off(out[i].cpu().to(F64), ref.orthogonal(v[i], 5)) <= 341 * 8 * U + 2.0 ** -8

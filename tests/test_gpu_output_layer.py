@@ -262,3 +262,133 @@ def test_the_gradient_is_the_slope_of_the_loss():
             down = loss(x, w)
             v.view(-1)[i] = keep
             assert abs((up - down) / (2 * d) - float(got.view(-1)[i])) < 3e-5
+
+
+# ---- calls as programs make them ------------------------------------------------------------------------------------------------
+
+
+def buffers(T, V, H, t):
+    return dict(lp=torch.empty(T, device=DEV), h=torch.empty(T, device=DEV), st=torch.empty(T, 2, device=DEV), dx=torch.empty(T, H, dtype=TYPES[t], device=DEV),
+                dw=torch.empty(V, H, device=DEV))
+
+
+def forward_and_back(layer, t, x, w, y, a, b, ws, ws2, stream=None):
+    c, H = code_of(t), layer.features
+    qa.qa_output_logprob(layer, c, x, w, y, b["lp"], b["h"], b["st"], ws, stream)
+    qa.qa_output_logprob_grad(layer, c, x, w, y, b["st"], b["h"], a, a, b["dx"], H, b["dw"], H, 0, ws2, stream)
+
+
+@pytest.mark.parametrize("t,T,V,H", [("bf16", 40, 3000, 96), ("f16", 300, 2500, 128), ("f32", 70, 900, 50)])
+def test_captured_and_replayed_among_eager_calls(t, T, V, H):
+    """Replays give what eager calls give, bit for bit, with eager calls of the same buffers and other inputs between them; two graphs
+    share a workspace, one after the other."""
+    gen = gen_of("graph", t)
+    layer, _, xd, _, wd, y = layer_of(gen, T, V, H, t)
+    y, a = y.to(torch.int32).to(DEV), torch.randn(T, generator=gen).to(DEV)
+    ws, ws2 = room(layer, qa.QA_OP_LOGPROB, t), room(layer, qa.QA_OP_LOGPROB_GRAD, t)
+    x, b = xd.clone(), buffers(T, V, H, t)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        forward_and_back(layer, t, x, wd, y, a, b, ws, ws2)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            forward_and_back(layer, t, x, wd, y, a, b, ws, ws2)
+        graphs.append(g)
+    for i in range(6):
+        fresh = (xd * (1 + 0.1 * i)).clone()
+        want = buffers(T, V, H, t)
+        forward_and_back(layer, t, fresh, wd, y, a, want, ws, ws2)
+        torch.cuda.synchronize()
+        x.copy_(fresh)
+        for v in b.values():
+            v.fill_(7.0)
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        for k in b:
+            assert torch.equal(b[k], want[k]), (i, k)
+
+
+def test_on_another_stream():
+    gen = gen_of("stream")
+    T, V, H, t = 130, 4000, 64, "bf16"
+    layer, _, xd, _, wd, y = layer_of(gen, T, V, H, t)
+    y, a = y.to(torch.int32).to(DEV), torch.randn(T, generator=gen).to(DEV)
+    want, got = buffers(T, V, H, t), buffers(T, V, H, t)
+    forward_and_back(layer, t, xd, wd, y, a, want, room(layer, qa.QA_OP_LOGPROB, t), room(layer, qa.QA_OP_LOGPROB_GRAD, t))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    both = [(buffers(T, V, H, t), room(layer, qa.QA_OP_LOGPROB, t), room(layer, qa.QA_OP_LOGPROB_GRAD, t)) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):                                            # two calls at once, each with its own workspace
+        for s, (b, ws, ws2) in zip(streams, both):
+            forward_and_back(layer, t, xd, wd, y, a, b, ws, ws2, s)
+    torch.cuda.synchronize()
+    for b, _, _ in both:
+        assert all(torch.equal(b[k], want[k]) for k in want)
+    del got
+
+
+@pytest.mark.parametrize("t,T", [("bf16", 20), ("bf16", 100), ("f32", 3)])
+def test_offsets_beyond_32_bits(t, T):
+    """Rows of w 150000 and more elements apart, 20000 of them: offsets of 6 GB and more, strides that are read in place and ones that are not."""
+    gen = gen_of("far", t)
+    V, H = 20000, 64
+    for stride in (150000, 150001):
+        wide = torch.zeros(V, stride, dtype=TYPES[t], device=DEV)
+        wide[:, :H] = (torch.randn(V, H, generator=gen) / 4).to(TYPES[t]).to(DEV)
+        w = wide[:, :H]
+        x = torch.randn(T, H, generator=gen).to(TYPES[t]).to(DEV)
+        y = torch.randint(0, V, (T,), generator=gen)
+        y[0] = V - 1
+        layer = qa.OutputLayer.make(T, V, H, H, stride)
+        check_score(t, x.cpu().to(F64), w.cpu().to(F64), y, score(layer, x, w, y, t))
+        del wide, w
+        torch.cuda.empty_cache()
+
+
+def test_dw_of_far_rows():
+    """dw rows a few hundred thousand elements apart, past 2^31 elements."""
+    gen = gen_of("far dw")
+    T, V, H, stride = 33, 9000, 48, 250000
+    layer, x, xd, w, wd, y = layer_of(gen, T, V, H, "bf16")
+    _, _, h, st = ref.score(x, w, y)
+    a = torch.rand(T, generator=gen) + 0.5
+    dw, near = torch.zeros(V, stride, device=DEV), torch.empty(V, H, device=DEV)
+    ws = room(layer, qa.QA_OP_LOGPROB_GRAD, "bf16")
+    for to, s in ((dw, stride), (near, H)):
+        qa.qa_output_logprob_grad(layer, qa.QA_BF16, xd, wd, y.to(torch.int32).to(DEV), st.float().to(DEV), None, a.to(DEV), None, None, H, to, s, 0, ws)
+    assert torch.equal(dw[:, :H], near) and bool((dw[:, H:H + 100] == 0).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_pieces_of_the_vocabulary(t):
+    """So many rows that the vocabulary is taken in pieces: the sums of dx go on from piece to piece."""
+    T, V, H = (20000, 20011, 32) if t == "bf16" else (9000, 20011, 20)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    w = (torch.randn(V, H, generator=gen, device=DEV) * (2 / math.sqrt(H))).to(TYPES[t])
+    x = torch.randn(T, H, generator=gen, device=DEV).to(TYPES[t])
+    y = torch.randint(0, V, (T,), generator=gen, device=DEV)
+    layer = qa.OutputLayer.make(T, V, H)
+    b = buffers(T, V, H, t)
+    qa.qa_output_logprob(layer, code_of(t), x, w, y.to(torch.int32), b["lp"], b["h"], b["st"], room(layer, qa.QA_OP_LOGPROB, t))
+    a = -torch.rand(T, generator=gen, device=DEV) - 0.5
+    qa.qa_output_logprob_grad(layer, code_of(t), x, w, y.to(torch.int32), b["st"], None, a, None, b["dx"], H, b["dw"], H, 0, room(layer, qa.QA_OP_LOGPROB_GRAD, t))
+    x64, w64, dx, dw, sizes = x.to(F64), w.to(F64), [], torch.zeros(V, H, dtype=F64, device=DEV), torch.zeros(V, H, dtype=F64, device=DEV)
+    off_x = []
+    for i in range(0, T, 2000):
+        z, lp, h, st = ref.score(x64[i:i + 2000], w64, y[i:i + 2000])
+        dz = dz_of(x64[i:i + 2000], w64, t)
+        assert ((b["lp"][i:i + 2000] - lp).abs() <= 2 * dz + SUM * (1 + lp.abs())).all()
+        c, _ = ref.logits_grad(z, y[i:i + 2000], b["st"][i:i + 2000].to(F64), None, a[i:i + 2000].to(F64), None)
+        off = c.abs() * (dz[:, None] + 8 * U * (z.abs() + 30) + 2.0 ** -21 + (3 * T / 16 + 64) * U)
+        dx.append(c @ w64)
+        off_x.append((off + c.abs() * (2.0 ** -11 if t != "f32" else 2.0 ** -21) + 2.0 ** -38 * 1.5) @ w64.abs())
+        dw += c.t() @ x64[i:i + 2000]
+        sizes += (off + c.abs() * 2.0 ** -21 + 2.0 ** -38 * 1.5).t() @ x64[i:i + 2000].abs()
+    dx, off_x = torch.cat(dx), torch.cat(off_x)
+    assert ((b["dx"].to(F64) - dx).abs() <= off_x + 1.01 * HALF_ULP[t] * dx.abs()).all()
+    assert ((b["dw"].to(F64) - dw).abs() <= sizes + 2 * U * dw.abs()).all()
