@@ -55,51 +55,141 @@ __device__ __forceinline__ Row row_of(const RowArgs& A, int64_t t) {
 }
 __device__ __forceinline__ bool counts(const Row& r) { return r.a != 0.0f || r.e != 0.0f; }
 
-// Largest magnitudes (bits) that the powers of two follow by which the gradient's operands are scaled.
-struct Scales { uint32_t most[4]; };
+// The gradient's operands are scaled by powers of two that follow from their largest magnitudes.  Work-groups leave theirs (bits) side by
+// side, the next kernel's find the largest of them, and its first one leaves that for the kernels behind it: no atomics, nothing to clear.
 enum { kOfC, kOfX, kOfW };
+constexpr int kMostBlocks = 1024;
+struct Scales {
+  uint32_t most[3];
+  uint32_t found[3][kMostBlocks];
+};
+__device__ __forceinline__ uint32_t most_in_block(uint32_t most) {
+  __shared__ uint32_t waves[kWaves];
+#pragma unroll
+  for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = most;
+  __syncthreads();
+  return max(max(waves[0], waves[1]), max(waves[2], waves[3]));
+}
 
-struct CopyArgs {
+struct MostArgs {
+  RowArgs R;
+  int64_t rows, vocab, features;
+  const void *x, *w;
+  int64_t x_stride, w_stride;
+  Scales* scales;
+  int blocks[3];                                   // work-groups for c, for x and for w; 0: not wanted
+};
+template <int TYPE>
+__device__ __forceinline__ uint32_t most_of_row(const ElemT<TYPE>* p, int64_t cols) {
+  constexpr int kAtOnce = 4;                       // reads that are on their way
+  const int lane = threadIdx.x % kWave;
+  uint32_t most = 0;
+  int64_t c = lane * kVec;
+  for (; c + (kAtOnce - 1) * kWave * kVec + kVec <= cols; c += kAtOnce * kWave * kVec) {
+    Raw8<TYPE> raw[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) raw[k] = load_raw<TYPE>(p + c + k * kWave * kVec);
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      float v[kVec];
+      to_f32<TYPE>(raw[k], v);
+      most = max(most, finite_most(v));
+    }
+  }
+  for (; c < cols; c += kWave * kVec) {
+    float v[kVec];
+    to_f32<TYPE>(load_raw<TYPE>(p + c, (int)min((int64_t)kVec, cols - c)), v);
+    most = max(most, finite_most(v));
+  }
+  return most;
+}
+// The largest |c| that a row can have: p <= 1, p |log p| <= 1 / e, and an entropy of at most log 2^24 < 17; the largest finite magnitudes of
+// rows of x that count, and of w.
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void output_most_kernel(MostArgs A) {
+  int block = blockIdx.x, which = 0;
+  while (block >= A.blocks[which]) block -= A.blocks[which++];
+  uint32_t most = 0;
+  if (which == kOfC) {
+    for (int64_t t = (int64_t)block * kThreads + threadIdx.x; t < A.rows; t += (int64_t)A.blocks[which] * kThreads) {
+      const Row r = row_of(A.R, t);
+      const uint32_t c = as_u32(fabsf(r.a) + 18.0f * fabsf(r.e));
+      if (c < 0x7F800000u) most = max(most, c);
+    }
+  } else {
+    const int64_t rows = which == kOfX ? A.rows : A.vocab, stride = which == kOfX ? A.x_stride : A.w_stride;
+    const ElemT<TYPE>* const p = (const ElemT<TYPE>*)(which == kOfX ? A.x : A.w);
+    for (int64_t row = (int64_t)block * kWaves + threadIdx.x / kWave; row < rows; row += (int64_t)A.blocks[which] * kWaves)
+      if (which == kOfW || counts(row_of(A.R, row))) most = max(most, most_of_row<TYPE>(p + row * stride, A.features));
+  }
+  most = most_in_block(most);
+  if (threadIdx.x == 0) A.scales->found[which][block] = most;
+}
+
+// Rows copied, a wave per row: 16-bit elements as they are, or binary16 (binary32 elements: in two parts) times a power of two per row
+// or per matrix.
+enum Copies { kAsTheyAre, kOwnScale, kOneScale };
+struct Copy {
+  int how;
   const void* from;
   int64_t stride, rows, cols;
   void* to;
   int64_t ld, to_rows;                             // zeros up to ld / parts columns, and in rows from `rows` on
   int* exps;                                       // kOwnScale: written
-  const Scales* scales;                            // kOneScale
-  int which;
+  int which;                                       // kOneScale
   bool masked;                                     // zeros in rows that do not count
-  RowArgs R;
+  int blocks;
 };
-// Rows copied, a wave per row: 16-bit elements as they are, or binary16 (binary32 elements: in two parts) times a power of two per row
-// or per matrix.
-enum Copies { kAsTheyAre, kOwnScale, kOneScale };
-template <int TYPE, Copies HOW>
+constexpr int kCopies = 4;
+struct CopyArgs {
+  Copy copy[kCopies];
+  RowArgs R;
+  Scales* scales;
+  int found[3];                                    // how many there are; not 0: the largest are found first
+};
+template <int TYPE>
 __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
   constexpr int kParts = TYPE == QA_F32 ? 2 : 1;
+  const auto find = [&](int which) {
+    uint32_t most = 0;
+    for (int b = threadIdx.x; b < A.found[which]; b += kThreads) most = max(most, A.scales->found[which][b]);
+    return most_in_block(most);
+  };
+  if (blockIdx.x == 0 && A.found[kOfC]) {
+#pragma unroll
+    for (int w = 0; w < 3; ++w) {
+      const uint32_t most = find(w);
+      if (threadIdx.x == 0) A.scales->most[w] = most;
+    }
+  }
+  int block = blockIdx.x, at = 0;
+  while (at < kCopies && block >= A.copy[at].blocks) block -= A.copy[at++].blocks;
+  if (at == kCopies) return;
+  const Copy& C = A.copy[at];
   const int lane = threadIdx.x % kWave;
-  for (int64_t row = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; row < A.to_rows; row += (int64_t)gridDim.x * kWaves) {
-    const ElemT<TYPE>* p = (const ElemT<TYPE>*)A.from + row * A.stride;
-    _Float16* q = (_Float16*)A.to + row * A.ld;
-    const int64_t cols = row < A.rows && !(A.masked && !counts(row_of(A.R, row))) ? A.cols : 0;
-    int exp = 0;
-    if constexpr (HOW == kOwnScale) {
-      uint32_t most = 0;
-      for (int64_t c = lane * kVec; c < cols; c += kWave * kVec) {
-        float v[kVec];
-        to_f32<TYPE>(load_raw<TYPE>(p + c, (int)min((int64_t)kVec, cols - c)), v);
-        most = max(most, finite_most(v));
-      }
+  int exp = 0;
+  if (C.how == kOneScale && TYPE != QA_F16) exp = exponent_for(A.found[kOfC] ? find(C.which) : A.scales->most[C.which]);
+  for (int64_t row = (int64_t)block * kWaves + threadIdx.x / kWave; row < C.to_rows; row += (int64_t)C.blocks * kWaves) {
+    const ElemT<TYPE>* p = (const ElemT<TYPE>*)C.from + row * C.stride;
+    _Float16* q = (_Float16*)C.to + row * C.ld;
+    const int64_t cols = row < C.rows && !(C.masked && !counts(row_of(A.R, row))) ? C.cols : 0;
+    if (TYPE == QA_F32 && C.how == kOwnScale) {
+      uint32_t most = cols ? most_of_row<TYPE>(p, cols) : 0;
 #pragma unroll
       for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
       exp = exponent_for(most);
-      if (lane == 0) A.exps[row] = exp;
+      if (lane == 0) C.exps[row] = exp;
     }
-    if constexpr (HOW == kOneScale && TYPE != QA_F16) exp = exponent_for(A.scales->most[A.which]);
-    for (int64_t c = lane * kVec; c < A.ld / kParts; c += kWave * kVec) {
+    for (int64_t c = lane * kVec; c < C.ld / kParts; c += kWave * kVec) {
       const int n = (int)max((int64_t)0, min((int64_t)kVec, cols - c));
-      if constexpr (HOW == kAsTheyAre || TYPE == QA_F16) {
-        *reinterpret_cast<u32x4*>(q + c) = n ? load_raw<TYPE>(p + c, n).a : u32x4{};
-      } else {
+      bool copied = false;
+      if constexpr (TYPE != QA_F32) {
+        copied = TYPE == QA_F16 || C.how == kAsTheyAre;
+        if (copied) *reinterpret_cast<u32x4*>(q + c) = n ? load_raw<TYPE>(p + c, n).a : u32x4{};
+      }
+      if (!copied) {
         float v[kVec] = {};
         if (n) to_f32<TYPE>(load_raw<TYPE>(p + c, n), v);
 #pragma unroll
@@ -410,60 +500,6 @@ __global__ __launch_bounds__(THREADS) void output_join_kernel(ScoreArgs A, int64
 
 // ---- the gradient of the logits -------------------------------------------------------------------------------------------
 
-__global__ void output_clear_kernel(Scales* s) { s->most[threadIdx.x] = 0; }
-
-// One atomic per work-group (8192 of them, from all dies to one word, took 100 us).
-__device__ __forceinline__ void raise_most(uint32_t* to, uint32_t most) {
-  __shared__ uint32_t waves[kWaves];
-#pragma unroll
-  for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
-  if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = most;
-  __syncthreads();
-  if (threadIdx.x == 0) atomicMax(to, max(max(waves[0], waves[1]), max(waves[2], waves[3])));
-}
-
-// The largest |c| that a row can have: p <= 1, p |log p| <= 1 / e, and an entropy of at most log 2^24 < 17.
-__global__ __launch_bounds__(kThreads) void output_weights_kernel(RowArgs A, int64_t rows, Scales* scales) {
-  uint32_t most = 0;
-  for (int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x; t < rows; t += (int64_t)gridDim.x * kThreads) {
-    const Row r = row_of(A, t);
-    const uint32_t c = as_u32(fabsf(r.a) + 18.0f * fabsf(r.e));
-    if (c < 0x7F800000u) most = max(most, c);
-  }
-  raise_most(&scales->most[kOfC], most);
-}
-
-// The largest finite magnitude of rows that count.
-template <int TYPE>
-__global__ __launch_bounds__(kThreads) void output_most_kernel(const void* from, int64_t stride, int64_t rows, int64_t cols, RowArgs A, bool masked,
-                                                               Scales* scales, int which) {
-  uint32_t most = 0;
-  const int lane = threadIdx.x % kWave;
-  for (int64_t row = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; row < rows; row += (int64_t)gridDim.x * kWaves) {
-    if (masked && !counts(row_of(A, row))) continue;
-    const ElemT<TYPE>* p = (const ElemT<TYPE>*)from + row * stride;
-    constexpr int kAtOnce = 4;                     // reads that are on their way
-    int64_t c = lane * kVec;
-    for (; c + (kAtOnce - 1) * kWave * kVec + kVec <= cols; c += kAtOnce * kWave * kVec) {
-      Raw8<TYPE> raw[kAtOnce];
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) raw[k] = load_raw<TYPE>(p + c + k * kWave * kVec);
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        float v[kVec];
-        to_f32<TYPE>(raw[k], v);
-        most = max(most, finite_most(v));
-      }
-    }
-    for (; c < cols; c += kWave * kVec) {
-      float v[kVec];
-      to_f32<TYPE>(load_raw<TYPE>(p + c, (int)min((int64_t)kVec, cols - c)), v);
-      most = max(most, finite_most(v));
-    }
-  }
-  raise_most(&scales->most[which], most);
-}
-
 // c of a piece of the vocabulary, scaled, in rows of parts: zeros behind the piece, in rows that do not count, and in rows up to a whole step.
 template <bool SCALED, bool ENTROPY>
 struct LogitsGradOut {
@@ -701,20 +737,28 @@ size_t bytes_of(const qa_output_layer& L, int op, int type) {
   return std::max(plan_of(L, op, type, nullptr, nullptr).bytes, plan_of(L, op, type, aligned_place, aligned_place).bytes);
 }
 
-template <int TYPE, Copies HOW>
-int copy_launch(const CopyArgs& A, hipStream_t stream) {
-  output_copy_kernel<TYPE, HOW><<<(unsigned)std::min<int64_t>(ceil_div(A.to_rows, kWaves), 1 << 14), kThreads, 0, stream>>>(A);
-  return launch_status();
-}
+// Copies that one kernel makes.
+struct CopyList {
+  CopyArgs A = {};
+  int n = 0, blocks = 0;
+  void add(int how, const void* from, int64_t stride, int64_t rows, int64_t cols, void* to, int64_t ld, int64_t to_rows, int* exps, int which, bool masked) {
+    Copy& C = A.copy[n++];
+    C = {how, from, stride, rows, cols, to, ld, to_rows, exps, which, masked, (int)std::min<int64_t>(ceil_div(to_rows, kWaves), 1 << 14)};
+    blocks += C.blocks;
+  }
+  template <int TYPE> int launch(hipStream_t stream) {
+    if (A.found[kOfC] == 0 && n == 0) return QA_OK;
+    output_copy_kernel<TYPE><<<(unsigned)std::max(blocks, 1), kThreads, 0, stream>>>(A);
+    *this = CopyList{{.R = A.R, .scales = A.scales}};
+    return launch_status();
+  }
+};
 // Rows for the logits: where they lie, or copied.
-template <int TYPE>
-int logits_operand(const void* from, int64_t stride, int64_t rows, const qa_output_layer& L, const Plan& P, bool copy, char* to, int* exps, Operand& O,
-                   hipStream_t stream) {
-  O = {from, stride, 0, rows};
-  if (!copy) return QA_OK;
-  O = {to, P.parts * P.hp, 0, rows};
-  CopyArgs A = {from, stride, rows, L.features, to, O.ld, rows, exps, nullptr, 0, false, {}};
-  return copy_launch<TYPE, TYPE == QA_F32 ? kOwnScale : kAsTheyAre>(A, stream);
+Operand logits_operand(CopyList& copies, int type, const void* from, int64_t stride, int64_t rows, const qa_output_layer& L, const Plan& P, bool copy, char* to,
+                       int* exps) {
+  if (!copy) return {from, stride, 0, rows};
+  copies.add(type == QA_F32 ? kOwnScale : kAsTheyAre, from, stride, rows, L.features, to, P.parts * P.hp, rows, exps, 0, false);
+  return {to, P.parts * P.hp, 0, rows};
 }
 // Logits of a piece of the vocabulary: w's rows by x's.
 template <int TYPE, class Epilogue>
@@ -748,11 +792,12 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
     kernel<<<(unsigned)P.chunks, kStreamGroup, 0, stream>>>(S);
     return join_launch(A, L, P.chunks, target, logprob, entropy, stats, stream);
   }
-  Operand xo, wo;
-  if (const int rc = logits_operand<TYPE>(x, L.x_stride, L.rows, L, P, P.copy_x, ws + P.x, x_exp, xo, stream)) return rc;
+  CopyList copies;
+  const Operand xo = logits_operand(copies, TYPE, x, L.x_stride, L.rows, L, P, P.copy_x, ws + P.x, x_exp);
   for (int64_t first = 0; first < L.vocab; first += P.piece) {
     const int64_t vocab = std::min(P.piece, L.vocab - first);
-    if (const int rc = logits_operand<TYPE>((const ElemT<TYPE>*)w + first * L.w_stride, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp, wo, stream)) return rc;
+    const Operand wo = logits_operand(copies, TYPE, (const ElemT<TYPE>*)w + first * L.w_stride, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp);
+    if (const int rc = copies.launch<TYPE>(stream)) return rc;
     A.first = first;
     A.first_chunk = first / P.piece * chunks_of(P.tiles) * ceil_div(P.piece, height_of(P.tiles));
     const ScoreOut<TYPE == QA_F32> out{LayerArgs{L.rows, vocab, x_exp, w_exp, target}, A};
@@ -790,25 +835,31 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
   int* const x_exp = (int*)(ws + P.x_exp);
   int* const w_exp = (int*)(ws + P.w_exp);
   Scales* const scales = (Scales*)(ws + P.scales);
-  const auto most_blocks = [](int64_t rows) { return (unsigned)std::min<int64_t>(1024, ceil_div(rows, kWaves)); };
-  output_clear_kernel<<<1, 4, 0, stream>>>(scales);
-  output_weights_kernel<<<(unsigned)std::min<int64_t>(256, ceil_div(L.rows, kThreads)), kThreads, 0, stream>>>(G.rows, L.rows, scales);
-  if (TYPE != QA_F16 && G.dw) output_most_kernel<TYPE><<<most_blocks(L.rows), kThreads, 0, stream>>>(G.x, L.x_stride, L.rows, L.features, G.rows, true, scales, kOfX);
-  if (TYPE != QA_F16 && G.dx) output_most_kernel<TYPE><<<most_blocks(L.vocab), kThreads, 0, stream>>>(G.w, L.w_stride, L.vocab, L.features, G.rows, false, scales, kOfW);
+  const auto blocks = [](bool wanted, int64_t n, int64_t each) { return wanted ? (int)std::min<int64_t>(kMostBlocks, ceil_div(n, each)) : 0; };
+  const MostArgs most = {G.rows, L.rows, L.vocab, L.features, G.x, G.w, L.x_stride, L.w_stride, scales,
+                         {blocks(true, L.rows, kThreads), blocks(TYPE != QA_F16 && G.dw, L.rows, kWaves), blocks(TYPE != QA_F16 && G.dx, L.vocab, kWaves)}};
+  output_most_kernel<TYPE><<<(unsigned)(most.blocks[0] + most.blocks[1] + most.blocks[2]), kThreads, 0, stream>>>(most);
   if (const int rc = launch_status()) return rc;
 
   const int64_t copied = P.parts * P.hc;
-  if (G.dw) {                                      // always copied: rows that do not count may hold anything
-    const CopyArgs A = {G.x, L.x_stride, L.rows, L.features, ws + P.xc, copied, P.tp, nullptr, scales, kOfX, true, G.rows};
-    if (const int rc = copy_launch<TYPE, kOneScale>(A, stream)) return rc;
-  }
-  Operand xo, wo;
-  if (const int rc = logits_operand<TYPE>(G.x, L.x_stride, L.rows, L, P, P.copy_x, ws + P.x, x_exp, xo, stream)) return rc;
+  CopyList copies;
+  copies.A.R = G.rows;
+  copies.A.scales = scales;
+  for (int i = 0; i < 3; ++i) copies.A.found[i] = most.blocks[i];
+  // Always copied: rows that do not count may hold anything.
+  if (G.dw) copies.add(kOneScale, G.x, L.x_stride, L.rows, L.features, ws + P.xc, copied, P.tp, nullptr, kOfX, true);
+  const Operand xo = logits_operand(copies, TYPE, G.x, L.x_stride, L.rows, L, P, P.copy_x, ws + P.x, x_exp);
   constexpr Lies kColumnsOf = TYPE == QA_F32 ? kColumnsOfParts : kColumns;
   for (int64_t first = 0; first < L.vocab; first += P.piece) {
     const int64_t vocab = std::min(P.piece, L.vocab - first);
     const void* const from = (const ElemT<TYPE>*)G.w + first * L.w_stride;
-    if (const int rc = logits_operand<TYPE>(from, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp, wo, stream)) return rc;
+    const Operand wo = logits_operand(copies, TYPE, from, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp);
+    Operand wc = {from, L.w_stride, 0, L.features};
+    if (G.dx && (TYPE != QA_F16 || !in_place(from, L.w_stride) || L.features % 8 || vocab % kWholeStep)) {
+      wc = {ws + P.wc, copied, 0, L.features};
+      copies.add(kOneScale, from, L.w_stride, vocab, L.features, ws + P.wc, copied, whole(vocab, kWholeStep), nullptr, kOfW, false);
+    }
+    if (const int rc = copies.launch<TYPE>(stream)) return rc;
     _Float16* const c = (_Float16*)(ws + P.c);
     const auto logits = [&](auto entropy) {
       const LogitsGradOut<TYPE == QA_F32, decltype(entropy)::value> grad{LayerArgs{L.rows, vocab, x_exp, w_exp, nullptr}, G.rows, first, scales, c, 2 * P.vp, P.tp};
@@ -816,12 +867,6 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     };
     if (const int rc = G.rows.g_entropy ? logits(std::true_type()) : logits(std::false_type())) return rc;
     if (G.dx) {
-      Operand wc = {from, L.w_stride, 0, L.features};
-      if (TYPE != QA_F16 || !in_place(from, L.w_stride) || L.features % 8 || vocab % kWholeStep) {
-        wc = {ws + P.wc, copied, 0, L.features};
-        const CopyArgs A = {from, L.w_stride, vocab, L.features, ws + P.wc, copied, whole(vocab, kWholeStep), nullptr, scales, kOfW, false, G.rows};
-        if (const int rc = copy_launch<TYPE, kOneScale>(A, stream)) return rc;
-      }
       const bool last = first + P.piece >= L.vocab;
       const GradOut<TYPE> out{(ElemT<TYPE>*)G.dx, P.pieces > 1 || P.dx.splits > 1 ? (float*)(ws + P.sums) : nullptr, scales, G.dx_stride, L.rows, L.features,
                               TYPE == QA_F16 ? -1 : kOfW, first > 0, last && P.dx.splits == 1};
