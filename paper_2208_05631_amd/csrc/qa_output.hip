@@ -16,7 +16,7 @@ namespace {
 
 struct LayerArgs {
   int64_t rows, vocab;
-  const int *x_exp, *w_exp;                        // binary32: operands are x 2^x_exp[row], w 2^w_exp[row]
+  const int *x_exp, *w_exp;                        // scored binary32: operands are x 2^x_exp[row], w 2^w_exp[row]
   const int32_t* target;
 };
 
@@ -501,6 +501,7 @@ __global__ __launch_bounds__(THREADS) void output_join_kernel(ScoreArgs A, int64
 // ---- the gradient of the logits -------------------------------------------------------------------------------------------
 
 // c of a piece of the vocabulary, scaled, in rows of parts: zeros behind the piece, in rows that do not count, and in rows up to a whole step.
+// SCALED: of operands scaled by one power of two each.
 template <bool SCALED, bool ENTROPY>
 struct LogitsGradOut {
   LayerArgs L;                                     // vocab: of this piece
@@ -513,7 +514,8 @@ struct LogitsGradOut {
     const int exp = exponent_for(scales->most[kOfC]), lane = threadIdx.x % kWave;
     constexpr int FN = (int)(sizeof p.acc[0] / sizeof p.acc[0][0]);
     float m[FN], log_sum[FN], a[FN], e[FN], h[FN];
-    int x_exp[FN], here[FN];
+    int here[FN];
+    const int z_exp = SCALED ? -(exponent_for(scales->most[kOfX]) + exponent_for(scales->most[kOfW])) : 0;
     bool none[FN];
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
@@ -524,7 +526,6 @@ struct LogitsGradOut {
       a[j] = ldexpf(r.a, exp);
       e[j] = ldexpf(r.e, exp) * kLn2;
       h[j] = r.h * kLog2e;
-      x_exp[j] = SCALED ? L.x_exp[min(t, L.rows - 1)] : 0;
       none[j] = t >= L.rows || !counts(r);
       const int64_t at = r.at - first - v0;
       here[j] = at >= 0 && at < P::kM ? (int)at : -kVec;
@@ -535,7 +536,7 @@ struct LogitsGradOut {
       float g[kVec];
 #pragma unroll
       for (int k = 0; k < kVec; ++k) {
-        if (SCALED) z[k] = ldexpf(z[k], -(x_exp[j] + L.w_exp[min(v0 + v + k, L.vocab - 1)]));
+        if (SCALED) z[k] = ldexpf(z[k], z_exp);
         const float lp = __builtin_fmaf(z[k] - m[j], kLog2e, -log_sum[j]), q = __builtin_amdgcn_exp2f(lp);      // in powers of two
         g[k] = ENTROPY ? -q * (a[j] + e[j] * (fmaxf(lp, kFar) + h[j])) : -q * a[j];
       }
@@ -629,15 +630,22 @@ constexpr int64_t kFewRows = 64;
 // Time of a step of k beside one of three products of 16: 32 k and one product bring as much for two thirds of the matrix instructions.
 constexpr double kOneProduct = 0.75, kTwoProducts = 0.65, kThreeProducts = 1.0;
 
-// Which tiles multiply the logits, in vocabulary by rows: 256 x 64 for few rows, 256 x 256 or 128 x 128.
-enum { kTall256, kTall128, kFlat };
-int logits_tiles(int64_t rows, int64_t vocab, int64_t features, int type) {
+// Which tiles multiply the logits, in vocabulary by rows: 256 x 64 for few rows, or one of those of the other products.  Those of 256 x 256
+// have no registers to hold a binary32 product's small parts apart (1681 rows of 5248: log probabilities 1e-6 off, and 5e-7).
+enum Tall { kTall256, kTall128, kTall128Two, kTall64, kFlat };
+Tall logits_tiles(int64_t rows, int64_t vocab, int64_t features, int type) {
   if (rows <= kFewRows) return kFlat;
   const ProductShape S = {vocab, rows, ceil_div(features, type == QA_F32 ? kPartsStep : kWholeStep), 1, false, type == QA_F32 ? kThreeProducts : kOneProduct};
-  return product_plan(tiles_bit(kTiles256) | tiles_bit(kTiles128), S, 1).tiles == kTiles256 ? kTall256 : kTall128;
+  const unsigned small = tiles_bit(kTiles128) | tiles_bit(kTiles128Two) | tiles_bit(kTiles64Four);
+  switch (product_plan(type == QA_F32 ? small : small | tiles_bit(kTiles256), S, 1).tiles) {
+    case kTiles256: return kTall256;
+    case kTiles128: return kTall128;
+    case kTiles128Two: return kTall128Two;
+    default: return kTall64;
+  }
 }
-constexpr int64_t height_of(int tiles) { return tiles == kTall128 ? 128 : 256; }
-constexpr int64_t chunks_of(int tiles) { return tiles == kFlat ? 4 : 2; }         // of a tile
+constexpr int64_t height_of(Tall t) { return t == kTall64 ? 64 : t == kTall128 || t == kTall128Two ? 128 : 256; }
+constexpr int64_t chunks_of(Tall t) { return t == kFlat ? 4 : t == kTall64 ? 1 : 2; }         // of a tile
 
 // Equal pieces of n, whole tiles each, of at most `most`.
 int64_t piece_of(int64_t n, int64_t most) { return std::min(whole(n, kWholeStep), whole(ceil_div(n, ceil_div(n, most)), 256)); }
@@ -662,8 +670,9 @@ int64_t power_of_two_within(int64_t n, int64_t least) {
 struct Plan {
   bool copy_x, copy_w;                             // for the logits
   int64_t parts, hp, piece, pieces;                // a copied row's columns; vocabulary of a launch
+  bool copies;                                     // gradient: both
   bool streams;                                    // w, for few rows that would have to be copied
-  int tiles;
+  Tall tiles;
   size_t x, w, x_exp, w_exp;                       // copies and exponents
   size_t m, s, sw, given;                          // scoring
   int64_t chunks, each;                            // each: of the vocabulary per work-group, where w is streamed
@@ -700,7 +709,10 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.chunks = chunks_of(P.tiles) * ((P.pieces - 1) * ceil_div(P.piece, height_of(P.tiles)) + ceil_div(L.vocab - (P.pieces - 1) * P.piece, height_of(P.tiles)));
   } else {
     P.tp = whole(L.rows, kPartsStep);
-    P.hc = whole(L.features, 8);
+    // Where x or w have to be copied for the logits, what the products with c take serves for both.
+    P.copies = P.copy_x || P.copy_w;
+    P.copy_x = P.copy_w = false;
+    P.hc = whole(L.features, P.copies ? kWholeStep : 8);
     P.piece = even_piece_of(L.vocab, std::min(power_of_two_within(kPieceBytes / (4 * P.tp), 1024), power_of_two_within(kPieceBytes / (P.hp * 2 * P.parts), 1024)), L.rows);
     P.pieces = ceil_div(L.vocab, P.piece);
     P.tiles = logits_tiles(L.rows, std::min(P.piece, L.vocab), L.features, type);
@@ -724,8 +736,8 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.sw = room.take(4 * P.chunks * L.rows);
     P.given = room.take(4 * L.rows);
   }
-  P.x_exp = room.take(type == QA_F32 ? 4 * L.rows : 0);
-  P.w_exp = room.take(type == QA_F32 ? 4 * P.piece : 0);
+  P.x_exp = room.take(P.copy_x && type == QA_F32 ? 4 * L.rows : 0);
+  P.w_exp = room.take(P.copy_w && type == QA_F32 ? 4 * P.piece : 0);
   P.x = room.take(P.copy_x ? 2 * P.parts * L.rows * P.hp : 0);
   P.w = room.take(P.copy_w ? 2 * P.parts * P.piece * P.hp : 0);
   P.bytes = room.bytes;
@@ -761,13 +773,18 @@ Operand logits_operand(CopyList& copies, int type, const void* from, int64_t str
   return {to, P.parts * P.hp, 0, rows};
 }
 // Logits of a piece of the vocabulary: w's rows by x's.
-template <int TYPE, class Epilogue>
-int logits_launch(const Operand& w, const Operand& x, int64_t features, int tiles, const Epilogue& out, hipStream_t stream) {
-  constexpr bool kBf16 = TYPE == QA_BF16;
-  constexpr Lies kLie = TYPE == QA_F32 ? kRowsOfParts : kRows;
-  if (tiles == kTall256) return product_launch<Product256<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
-  if (tiles == kFlat) return product_launch<Product<kBf16, kLie, kLie, 4, 1, 2, 2>>(w, x, features, out, 1, stream);
-  return product_launch<Product128<kBf16, kLie, kLie>>(w, x, features, out, 1, stream);
+template <bool BF16, Lies LIE, class Epilogue>
+int logits_launch(const Operand& w, const Operand& x, int64_t features, Tall tiles, const Epilogue& out, hipStream_t stream) {
+  constexpr bool kApart = LIE == kRowsOfParts;
+  switch (tiles) {
+    case kTall128: return product_launch<Product<BF16, LIE, LIE, 2, 2, 2, 2, 1, kApart>>(w, x, features, out, 1, stream);
+    case kTall128Two: return product_launch<Product<BF16, LIE, LIE, 2, 2, 2, 2, 2, kApart>>(w, x, features, out, 1, stream);
+    case kTall64: return product_launch<Product<BF16, LIE, LIE, 1, 1, 2, 2, 4, kApart>>(w, x, features, out, 1, stream);
+    case kFlat: return product_launch<Product<BF16, LIE, LIE, 4, 1, 2, 2, 1, kApart>>(w, x, features, out, 1, stream);
+    default: break;
+  }
+  if constexpr (!kApart) return product_launch<Product256<BF16, LIE, LIE>>(w, x, features, out, 1, stream);
+  return QA_ERR_INVALID_ARG;                       // not reached: no such tiles with parts
 }
 
 int join_launch(const ScoreArgs& A, const qa_output_layer& L, int64_t chunks, const int32_t* target, float* logprob, float* entropy, float* stats, hipStream_t stream) {
@@ -801,7 +818,7 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
     A.first = first;
     A.first_chunk = first / P.piece * chunks_of(P.tiles) * ceil_div(P.piece, height_of(P.tiles));
     const ScoreOut<TYPE == QA_F32> out{LayerArgs{L.rows, vocab, x_exp, w_exp, target}, A};
-    if (const int rc = logits_launch<TYPE>(wo, xo, L.features, P.tiles, out, stream)) return rc;
+    if (const int rc = logits_launch<TYPE == QA_BF16, TYPE == QA_F32 ? kRowsOfParts : kRows>(wo, xo, L.features, P.tiles, out, stream)) return rc;
   }
   return join_launch(A, L, P.chunks, target, logprob, entropy, stats, stream);
 }
@@ -832,12 +849,11 @@ struct GradCall {
 template <int TYPE>
 int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream_t stream) {
   const Plan P = plan_of(L, QA_OP_LOGPROB_GRAD, TYPE, G.x, G.w);
-  int* const x_exp = (int*)(ws + P.x_exp);
-  int* const w_exp = (int*)(ws + P.w_exp);
   Scales* const scales = (Scales*)(ws + P.scales);
   const auto blocks = [](bool wanted, int64_t n, int64_t each) { return wanted ? (int)std::min<int64_t>(kMostBlocks, ceil_div(n, each)) : 0; };
   const MostArgs most = {G.rows, L.rows, L.vocab, L.features, G.x, G.w, L.x_stride, L.w_stride, scales,
-                         {blocks(true, L.rows, kThreads), blocks(TYPE != QA_F16 && G.dw, L.rows, kWaves), blocks(TYPE != QA_F16 && G.dx, L.vocab, kWaves)}};
+                         {blocks(true, L.rows, kThreads), blocks(TYPE != QA_F16 && (G.dw || P.copies), L.rows, kWaves),
+                          blocks(TYPE != QA_F16 && (G.dx || P.copies), L.vocab, kWaves)}};
   output_most_kernel<TYPE><<<(unsigned)(most.blocks[0] + most.blocks[1] + most.blocks[2]), kThreads, 0, stream>>>(most);
   if (const int rc = launch_status()) return rc;
 
@@ -847,23 +863,30 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
   copies.A.scales = scales;
   for (int i = 0; i < 3; ++i) copies.A.found[i] = most.blocks[i];
   // Always copied: rows that do not count may hold anything.
-  if (G.dw) copies.add(kOneScale, G.x, L.x_stride, L.rows, L.features, ws + P.xc, copied, P.tp, nullptr, kOfX, true);
-  const Operand xo = logits_operand(copies, TYPE, G.x, L.x_stride, L.rows, L, P, P.copy_x, ws + P.x, x_exp);
+  if (G.dw || P.copies) copies.add(kOneScale, G.x, L.x_stride, L.rows, L.features, ws + P.xc, copied, P.tp, nullptr, kOfX, true);
   constexpr Lies kColumnsOf = TYPE == QA_F32 ? kColumnsOfParts : kColumns;
   for (int64_t first = 0; first < L.vocab; first += P.piece) {
     const int64_t vocab = std::min(P.piece, L.vocab - first);
     const void* const from = (const ElemT<TYPE>*)G.w + first * L.w_stride;
-    const Operand wo = logits_operand(copies, TYPE, from, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp);
     Operand wc = {from, L.w_stride, 0, L.features};
-    if (G.dx && (TYPE != QA_F16 || !in_place(from, L.w_stride) || L.features % 8 || vocab % kWholeStep)) {
+    if (P.copies || (G.dx && (TYPE != QA_F16 || vocab % kWholeStep))) {
       wc = {ws + P.wc, copied, 0, L.features};
       copies.add(kOneScale, from, L.w_stride, vocab, L.features, ws + P.wc, copied, whole(vocab, kWholeStep), nullptr, kOfW, false);
     }
     if (const int rc = copies.launch<TYPE>(stream)) return rc;
     _Float16* const c = (_Float16*)(ws + P.c);
     const auto logits = [&](auto entropy) {
-      const LogitsGradOut<TYPE == QA_F32, decltype(entropy)::value> grad{LayerArgs{L.rows, vocab, x_exp, w_exp, nullptr}, G.rows, first, scales, c, 2 * P.vp, P.tp};
-      return logits_launch<TYPE>(wo, xo, L.features, P.tiles, grad, stream);
+      constexpr bool kEntropy = decltype(entropy)::value;
+      const LayerArgs piece = {L.rows, vocab, nullptr, nullptr, nullptr};
+      if (P.copies) {
+        const LogitsGradOut<true, kEntropy> grad{piece, G.rows, first, scales, c, 2 * P.vp, P.tp};
+        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xc, copied, 0, L.rows}, L.features, P.tiles, grad, stream);
+      }
+      if constexpr (TYPE != QA_F32) {              // copied always
+        const LogitsGradOut<false, kEntropy> grad{piece, G.rows, first, scales, c, 2 * P.vp, P.tp};
+        return logits_launch<TYPE == QA_BF16, kRows>(Operand{from, L.w_stride, 0, vocab}, Operand{G.x, L.x_stride, 0, L.rows}, L.features, P.tiles, grad, stream);
+      }
+      return (int)QA_ERR_INVALID_ARG;              // not reached
     };
     if (const int rc = G.rows.g_entropy ? logits(std::true_type()) : logits(std::false_type())) return rc;
     if (G.dx) {

@@ -132,9 +132,9 @@ struct Reader {
 };
 
 // WM x WN waves, FM x FN blocks of 32 x 32 each.  SHARE > 1: so many times the waves, each lot with every SHARE-th step and buffers of its own;
-// the first lot gets all sums.  Four buffers: while step s is multiplied, s + 1 is there, s + 2 on its way, and s + 3
+// the first lot gets all sums.  APART: products with a lo have sums of their own, so that a sum is rounded a third as often.  Four buffers: while step s is multiplied, s + 1 is there, s + 2 on its way, and s + 3
 // sets out for the buffer that step s - 1 had.
-template <bool BF16, Lies LA, Lies LB, int WM, int WN, int FM, int FN, int SHARE = 1>
+template <bool BF16, Lies LA, Lies LB, int WM, int WN, int FM, int FN, int SHARE = 1, bool APART = false>
 struct Product {
   static constexpr int kM = 32 * WM * FM, kN = 32 * WN * FN, kWavesHere = WM * WN, kGroup = SHARE * kWavesHere * kWave;
   static constexpr int kWavesPerSimd = FM * FN == 16 ? 1 : SHARE > 1 ? SHARE : 2;        // of registers
@@ -150,7 +150,7 @@ struct Product {
   static constexpr int kLotBytes = kWavesHere * kWave * FM * FN * 64, kShared = kBuffers * kBuffer + (SHARE - 1) * kLotBytes;
   static constexpr int kLds = SHARE * kBuffers * kBuffer > kShared ? SHARE * kBuffers * kBuffer : kShared;
 
-  f32x16 acc[FM][FN];
+  f32x16 acc[FM][FN], more[APART ? FM : 1][APART ? FN : 1];
   u32x4 a[2][FM], b[2][FN];
   BringA bring_a;
   BringB bring_b;
@@ -171,15 +171,20 @@ struct Product {
       bring_b.at += bring_b.advance & go;
     }
   }
+  template <bool MORE = false>
   __device__ __forceinline__ void multiply(const u32x4 (&x)[FM], const u32x4 (&y)[FN]) {
+    auto& to = [&]() -> auto& {
+      if constexpr (MORE && APART) return more;
+      else return acc;
+    }();
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
         if constexpr (BF16)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[i]), __builtin_bit_cast(bf16x8, y[j]), acc[i][j], 0, 0, 0);
+          to[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[i]), __builtin_bit_cast(bf16x8, y[j]), to[i][j], 0, 0, 0);
         else
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x[i]), __builtin_bit_cast(f16x8, y[j]), acc[i][j], 0, 0, 0);
+          to[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x[i]), __builtin_bit_cast(f16x8, y[j]), to[i][j], 0, 0, 0);
       }
   }
   // Waits until at most LEFT of this wave's loads are on their way, then for the other waves.  Loads into LDS are the only
@@ -213,14 +218,14 @@ struct Product {
     p.read_b.read(now + BringA::kBytes, 1, p.b[1]);
     p.template load<kLate, kLoads>(late);
     p.multiply(p.a[0], p.b[0]);
-    if constexpr (kPA == 2) p.multiply(p.a[0], p.b[1]);
+    if constexpr (kPA == 2) p.template multiply<true>(p.a[0], p.b[1]);
     interleave<kPA == 2 ? 2 * kAll : kAll, (kPA == kPB ? kReadA : 0) + kReadB, kLoads - kLate>();
     arrive<kLoads>();                              // `then` is there, and nobody reads `last` any more
     u32x4 a_next[FM], b_next[FN];
     p.read_a.read(then, 0, a_next);
     p.read_b.read(then + BringA::kBytes, 0, b_next);
     p.template load<0, kLate>(last);
-    if constexpr (kPA == 2) p.multiply(p.a[1], p.b[0]);
+    if constexpr (kPA == 2) p.template multiply<true>(p.a[1], p.b[0]);
     else if constexpr (kPB == 2) p.multiply(p.a[0], p.b[1]);
     else p.multiply(p.a[1], p.b[1]);
     interleave<kAll, kReadA + kReadB, kLate>();
@@ -241,7 +246,10 @@ struct Product {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
+      for (int j = 0; j < FN; ++j) {
+        acc[i][j] = f32x16{};
+        if constexpr (APART) more[i][j] = f32x16{};
+      }
     bring_a.begin(A.a, matrix, m0, A.a.n, begin + min(share, in_split - 1), wave);
     bring_b.begin(A.b, matrix, n0, A.b.n, begin + min(share, in_split - 1), wave);
     bring_a.advance *= SHARE;
@@ -270,6 +278,12 @@ struct Product {
     if constexpr (SHARE > 1)
       for (int s = max(steps, 0); s < all_steps; ++s) arrive<0>();
     arrive<0>();                                   // loads past the last step, before LDS is used for something else
+    if constexpr (APART) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] += more[i][j];
+    }
     if constexpr (SHARE > 1) {
       constexpr int kPieces = (int)(sizeof acc / sizeof(f32x4));
       f32x4 v[kPieces];
