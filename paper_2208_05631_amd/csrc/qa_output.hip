@@ -614,7 +614,9 @@ __global__ __launch_bounds__(kThreads) void output_zero_kernel(float* p, int64_t
 
 // ---- what a call does ------------------------------------------------------------------------------------------------------------
 
-constexpr int64_t kPieceBytes = int64_t(512) << 20;
+// Bytes of a piece's c, of its copy of w and of sums that are joined: about what the last-level cache holds.  (Gradient of 8192 rows, 32768 x 4096: 7.74 ms, 8.03
+// with half of it, 7.66 with twice and four times as much; 4096 rows, 50021 x 1024: 2.29, 2.28, 2.41, 2.20.)
+constexpr int64_t kPieceBytes = int64_t(256) << 20;
 
 struct Room {
   size_t bytes = 0;
@@ -681,10 +683,16 @@ struct Plan {
   size_t scales, xc, wc, c, sums;                  // gradient: x and w as the products with c take them
   size_t dw_sums;
   int64_t hc, tp, vp;
-  ProductPlan dx, dw;
+  ProductPlan dx;
   size_t bytes;
 };
 ProductPlan grad_plan(const ProductShape& S, int64_t most) { return product_plan(tiles_bit(kTiles256) | tiles_bit(kTiles128) | tiles_bit(kTiles128Two), S, most); }
+
+// Of a piece's dw: its tiles are few where both sides are small.
+ProductPlan dw_plan(const qa_output_layer& L, int type, int64_t vocab) {
+  return grad_plan({L.features, vocab, ceil_div(L.rows, kPartsStep), 1, false, type == QA_F32 ? kThreeProducts : kTwoProducts},
+                   std::min(std::max<int64_t>(1, kPieceBytes / (4 * vocab * L.features)), int64_t(64)));
+}
 
 bool in_place(const void* p, int64_t stride) { return stride % 8 == 0 && stride < (int64_t(1) << 22) && aligned(p, 16); }
 
@@ -717,20 +725,20 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.hc = whole(L.features, P.copies ? kWholeStep : 8);
     P.piece = even_piece_of(L.vocab, std::min(power_of_two_within(kPieceBytes / (4 * P.tp), 1024), power_of_two_within(kPieceBytes / (P.hp * 2 * P.parts), 1024)), L.rows);
     P.pieces = ceil_div(L.vocab, P.piece);
-    P.tiles = logits_tiles(L.rows, std::min(P.piece, L.vocab), L.features, type);
     P.vp = whole(P.piece, kWholeStep);
     P.scales = room.take(sizeof(Scales));
     P.xc = room.take(2 * P.parts * P.tp * P.hc);
     P.wc = room.take(2 * P.parts * P.vp * P.hc);
     P.c = room.take(2 * 2 * P.tp * P.vp);
-    // dx has few tiles and sums over the vocabulary, dw few where both sides are small.
+    // dx has few tiles and sums over the vocabulary.
     const bool one = type == QA_BF16;
     const int64_t vocab = std::min(P.piece, L.vocab), fit = std::max<int64_t>(1, kPieceBytes / (4 * L.rows * L.features));
     P.dx = grad_plan({L.features, L.rows, ceil_div(vocab, one ? kWholeStep : kPartsStep), 1, false, one ? kOneProduct : type == QA_F32 ? kThreeProducts : kTwoProducts}, std::min<int64_t>(64, fit));
-    P.dw = grad_plan({L.features, vocab, ceil_div(L.rows, kPartsStep), 1, false, type == QA_F32 ? kThreeProducts : kTwoProducts},
-                     std::min(std::max<int64_t>(1, kPieceBytes / (4 * vocab * L.features)), int64_t(64)));
     P.sums = room.take(P.pieces > 1 || P.dx.splits > 1 ? 4 * P.dx.splits * L.rows * L.features : 0);
-    P.dw_sums = room.take(P.dw.splits > 1 ? 4 * P.dw.splits * vocab * L.features : 0);
+    int64_t dw_sums = 0;
+    for (const int64_t of : {vocab, L.vocab - (P.pieces - 1) * P.piece})
+      if (const int64_t splits = dw_plan(L, type, of).splits; splits > 1) dw_sums = std::max(dw_sums, 4 * splits * of * L.features);
+    P.dw_sums = room.take(dw_sums);
   }
   if (op == QA_OP_LOGPROB) {
     P.m = room.take(4 * P.chunks * L.rows);
@@ -877,16 +885,17 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     }
     if (const int rc = copies.launch<TYPE>(stream)) return rc;
     _Float16* const c = (_Float16*)(ws + P.c);
+    const Tall tiles = logits_tiles(L.rows, vocab, L.features, TYPE);
     const auto logits = [&](auto entropy) {
       constexpr bool kEntropy = decltype(entropy)::value;
       const LayerArgs piece = {L.rows, vocab, nullptr, nullptr, nullptr};
       if (P.copies) {
         const LogitsGradOut<true, kEntropy> grad{piece, G.rows, first, scales, c, 2 * P.vp, P.tp};
-        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xc, copied, 0, L.rows}, L.features, P.tiles, grad, stream);
+        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xc, copied, 0, L.rows}, L.features, tiles, grad, stream);
       }
       if constexpr (TYPE != QA_F32) {              // copied always
         const LogitsGradOut<false, kEntropy> grad{piece, G.rows, first, scales, c, 2 * P.vp, P.tp};
-        return logits_launch<TYPE == QA_BF16, kRows>(Operand{from, L.w_stride, 0, vocab}, Operand{G.x, L.x_stride, 0, L.rows}, L.features, P.tiles, grad, stream);
+        return logits_launch<TYPE == QA_BF16, kRows>(Operand{from, L.w_stride, 0, vocab}, Operand{G.x, L.x_stride, 0, L.rows}, L.features, tiles, grad, stream);
       }
       return (int)QA_ERR_INVALID_ARG;              // not reached
     };
@@ -903,11 +912,12 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     }
     if (G.dw) {
       float* const dw = G.dw + first * G.dw_stride;
-      float* const sums = P.dw.splits > 1 ? (float*)(ws + P.dw_sums) : nullptr;
+      const ProductPlan plan = dw_plan(L, TYPE, vocab);
+      float* const sums = plan.splits > 1 ? (float*)(ws + P.dw_sums) : nullptr;
       const GradOut<QA_F32> out{dw, sums, scales, G.dw_stride, vocab, L.features, TYPE == QA_F16 ? -1 : kOfX, !sums && G.accumulate, !sums};
-      if (const int rc = grad_product<kColumnsOf, kColumnsOfParts>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, P.dw, stream)) return rc;
+      if (const int rc = grad_product<kColumnsOf, kColumnsOfParts>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, plan, stream)) return rc;
       if (sums)
-        if (const int rc = sum_launch<QA_F32>(sums, P.dw.splits, vocab, L.features, dw, G.dw_stride, G.accumulate, stream)) return rc;
+        if (const int rc = sum_launch<QA_F32>(sums, plan.splits, vocab, L.features, dw, G.dw_stride, G.accumulate, stream)) return rc;
     }
   }
   return QA_OK;
