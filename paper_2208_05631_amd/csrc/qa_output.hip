@@ -674,6 +674,7 @@ int64_t power_of_two_within(int64_t n, int64_t least) {
 struct Plan {
   bool copy_x, copy_w;                             // for the logits
   int64_t parts, hp, piece, pieces;                // a copied row's columns; vocabulary of a launch
+  int64_t rows;                                    // of a launch
   bool copies;                                     // gradient: both
   bool streams;                                    // w, for few rows that would have to be copied
   Tall tiles;
@@ -705,6 +706,7 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
   P.copy_x = !x || !rows_as_they_are || !in_place(x, L.x_stride);
   P.copy_w = !w || !rows_as_they_are || !in_place(w, L.w_stride);
   P.hp = whole(L.features, kWholeStep);
+  P.rows = L.rows;
   // Copying w takes longer than the products of few rows with it (48 rows, 100003 x 2049 binary16: 294 us, 220 from where it lies; one row,
   // 47236 x 515 binary32: 76, 57), but where it can be brought straight to LDS, that is faster (100003 x 2048: 107, 123).
   P.streams = op == QA_OP_LOGPROB && L.rows <= kFewRows && L.features >= kVec && (P.copy_x || P.copy_w);
@@ -717,6 +719,8 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.piece = P.copy_w ? piece_of(L.vocab, power_of_two_within(kPieceBytes / (P.hp * 2 * P.parts), 16384)) : L.vocab;
     P.pieces = ceil_div(L.vocab, P.piece);
     P.chunks = chunks_of(P.tiles) * ((P.pieces - 1) * ceil_div(P.piece, height_of(P.tiles)) + ceil_div(L.vocab - (P.pieces - 1) * P.piece, height_of(P.tiles)));
+    // So that the chunks' numbers stay within bounds, and the tiles within a grid's.
+    P.rows = std::min(L.rows, std::max<int64_t>(256, 4 * kPieceBytes / (12 * P.chunks) / 256 * 256));
   } else {
     P.tp = whole(L.rows, kPartsStep);
     // Where x or w have to be copied for the logits, what the products with c take serves for both.
@@ -741,14 +745,14 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.dw_sums = room.take(dw_sums);
   }
   if (op == QA_OP_LOGPROB) {
-    P.m = room.take(4 * P.chunks * L.rows);
-    P.s = room.take(4 * P.chunks * L.rows);
-    P.sw = room.take(4 * P.chunks * L.rows);
-    P.given = room.take(4 * L.rows);
+    P.m = room.take(4 * P.chunks * P.rows);
+    P.s = room.take(4 * P.chunks * P.rows);
+    P.sw = room.take(4 * P.chunks * P.rows);
+    P.given = room.take(4 * P.rows);
   }
-  P.x_exp = room.take(P.copy_x && type == QA_F32 ? 4 * L.rows : 0);
+  P.x_exp = room.take(P.copy_x && type == QA_F32 ? 4 * P.rows : 0);
   P.w_exp = room.take(P.copy_w && type == QA_F32 ? 4 * P.piece : 0);
-  P.x = room.take(P.copy_x ? 2 * P.parts * L.rows * P.hp : 0);
+  P.x = room.take(P.copy_x ? 2 * P.parts * P.rows * P.hp : 0);
   P.w = room.take(P.copy_w ? 2 * P.parts * P.piece * P.hp : 0);
   P.bytes = room.bytes;
   return P;
@@ -756,7 +760,10 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
 // At most, whatever the alignment of x and w.
 size_t bytes_of(const qa_output_layer& L, int op, int type) {
   alignas(16) static const char aligned_place[16] = {};
-  return std::max(plan_of(L, op, type, nullptr, nullptr).bytes, plan_of(L, op, type, aligned_place, aligned_place).bytes);
+  size_t most = 0;
+  for (const void* x : {(const void*)nullptr, (const void*)aligned_place})
+    for (const void* w : {(const void*)nullptr, (const void*)aligned_place}) most = std::max(most, plan_of(L, op, type, x, w).bytes);
+  return most;
 }
 
 // Copies that one kernel makes.
@@ -819,18 +826,25 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
     kernel<<<(unsigned)P.chunks, kStreamGroup, 0, stream>>>(S);
     return join_launch(A, L, P.chunks, target, logprob, entropy, stats, stream);
   }
-  CopyList copies;
-  const Operand xo = logits_operand(copies, TYPE, x, L.x_stride, L.rows, L, P, P.copy_x, ws + P.x, x_exp);
-  for (int64_t first = 0; first < L.vocab; first += P.piece) {
-    const int64_t vocab = std::min(P.piece, L.vocab - first);
-    const Operand wo = logits_operand(copies, TYPE, (const ElemT<TYPE>*)w + first * L.w_stride, L.w_stride, vocab, L, P, P.copy_w, ws + P.w, w_exp);
-    if (const int rc = copies.launch<TYPE>(stream)) return rc;
-    A.first = first;
-    A.first_chunk = first / P.piece * chunks_of(P.tiles) * ceil_div(P.piece, height_of(P.tiles));
-    const ScoreOut<TYPE == QA_F32> out{LayerArgs{L.rows, vocab, x_exp, w_exp, target}, A};
-    if (const int rc = logits_launch<TYPE == QA_BF16, TYPE == QA_F32 ? kRowsOfParts : kRows>(wo, xo, L.features, P.tiles, out, stream)) return rc;
+  const auto from = [](auto* p, int64_t n) { return p ? p + n : p; };
+  for (int64_t t = 0; t < L.rows; t += P.rows) {
+    qa_output_layer here = L;
+    here.rows = std::min(P.rows, L.rows - t);
+    const int32_t* const its_target = from(target, t);
+    CopyList copies;
+    const Operand xo = logits_operand(copies, TYPE, (const ElemT<TYPE>*)x + t * L.x_stride, L.x_stride, here.rows, here, P, P.copy_x, ws + P.x, x_exp);
+    for (int64_t first = 0; first < L.vocab; first += P.piece) {
+      const int64_t vocab = std::min(P.piece, L.vocab - first);
+      const Operand wo = logits_operand(copies, TYPE, (const ElemT<TYPE>*)w + first * L.w_stride, L.w_stride, vocab, here, P, P.copy_w, ws + P.w, w_exp);
+      if (const int rc = copies.launch<TYPE>(stream)) return rc;
+      A.first = first;
+      A.first_chunk = first / P.piece * chunks_of(P.tiles) * ceil_div(P.piece, height_of(P.tiles));
+      const ScoreOut<TYPE == QA_F32> out{LayerArgs{here.rows, vocab, x_exp, w_exp, its_target}, A};
+      if (const int rc = logits_launch<TYPE == QA_BF16, TYPE == QA_F32 ? kRowsOfParts : kRows>(wo, xo, L.features, P.tiles, out, stream)) return rc;
+    }
+    if (const int rc = join_launch(A, here, P.chunks, its_target, from(logprob, t), from(entropy, t), from(stats, 2 * t), stream)) return rc;
   }
-  return join_launch(A, L, P.chunks, target, logprob, entropy, stats, stream);
+  return QA_OK;
 }
 
 template <int TYPE>

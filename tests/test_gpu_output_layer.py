@@ -365,6 +365,22 @@ def test_dw_of_far_rows():
 
 
 @pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_pieces_of_the_rows(t):
+    """So many rows that they are scored in pieces."""
+    T, V, H = 260000, 50001, 32
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    w = (torch.randn(V, H, generator=gen, device=DEV) * (2 / math.sqrt(H))).to(TYPES[t])
+    x = torch.randn(T, H, generator=gen, device=DEV).to(TYPES[t])
+    y = torch.randint(0, V, (T,), generator=gen, device=DEV)
+    layer = qa.OutputLayer.make(T, V, H)
+    assert 4 * 3 * (V // 128) * T > qa.qa_output_workspace_bytes(layer, qa.QA_OP_LOGPROB, code_of(t))       # less than all chunks' numbers
+    b = buffers(T, V, H, t)
+    qa.qa_output_logprob(layer, code_of(t), x, w, y.to(torch.int32), b["lp"], b["h"], b["st"], room(layer, qa.QA_OP_LOGPROB, t))
+    for rows in (slice(0, 500), slice(100000, 240000, 173), slice(T - 300, T)):
+        check_score(t, x[rows].to(F64), w.to(F64), y[rows], [b[n][rows].to(F64) for n in ("lp", "h", "st")])
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
 def test_pieces_of_the_vocabulary(t):
     """So many rows that the vocabulary is taken in pieces: the sums of dx go on from piece to piece."""
     T, V, H = (20000, 20011, 32) if t == "bf16" else (9000, 20011, 20)

@@ -90,6 +90,8 @@ def test_workspaces_hold_no_logits_of_a_large_vocabulary():
     big = qa.OutputLayer.make(8192, 1 << 20, 1024)
     assert qa.qa_output_workspace_bytes(big, qa.QA_OP_LOGPROB, BF16) < 2 << 30
     assert qa.qa_output_workspace_bytes(big, qa.QA_OP_LOGPROB_GRAD, BF16) < 2 << 30
+    many = layer(rows=(1 << 24) - 1, vocab=1 << 17)
+    assert qa.qa_output_workspace_bytes(many, qa.QA_OP_LOGPROB, BF16) < 2 << 30
 
 
 @pytest.mark.parametrize("name", ["qa_orthogonalize", "qa_step_orthogonal"])
