@@ -597,10 +597,11 @@ typedef struct {
 size_t qa_output_workspace_bytes(const qa_output_layer* layer, int op, int type);
 
 /* logprob, entropy and stats of each row as qa_token_logprob gives them.  target and logprob are NULL together, entropy and
- * stats may be NULL.  16-bit elements are multiplied as they are; binary32 ones as two binary16 parts each, scaled by a power of two
- * per row (22 bits and a sign; what is below 2^-39 of a row's largest magnitude is lost).  Rows that begin on 16 bytes,
- * with strides of a multiple of 8 below 2^22 and features a multiple of 32, are read where they lie (16-bit types); others are copied
- * into the workspace first. */
+ * stats may be NULL.  16-bit elements are multiplied as they are.  binary32 ones of up to 64 rows are multiplied as three bfloat16 parts
+ * each, of more rows as two binary16 parts, scaled by a power of two per row (22 bits and a sign; what is below 2^-39 of a row's largest
+ * magnitude is lost).  16-bit x and w whose rows begin on 16 bytes, with strides of a multiple of 8 below 2^22 and features a multiple
+ * of 32, are read where they lie, and so are all of up to 64 rows (and 8 features or more); others are copied into the workspace, w a
+ * piece of the vocabulary at a time. */
 int qa_output_logprob(const qa_output_layer* layer, int type, const void* x, const void* w,
                       const int32_t* target_or_null, float* logprob_or_null, float* entropy_or_null,
                       float* stats_or_null, void* ws, size_t ws_bytes, void* stream);
@@ -611,9 +612,10 @@ int qa_output_logprob(const qa_output_layer* layer, int type, const void* x, con
  * with the logits multiplied again, a piece of the vocabulary at a time.  stats and entropy as qa_output_logprob wrote them
  * (entropy and g_entropy NULL together).  A row without target has the entropy's part alone.  A row whose g_logprob (or
  * target) and g_entropy are both none or 0 gets dx = 0 and adds nothing to dw, whatever x holds there: padding.
- * Numbers are multiplied as binary16 with one power of two per matrix as scale: c in two parts, but in one for dx of a 16-bit
- * type (a rounding by 2^-11, an eighth of a bfloat16's), binary32 x and w in two, bfloat16 ones exactly, but for magnitudes below 2^-32 of
- * their matrix's largest, which lose bits below 2^-39 of it.  dx_or_null and dw_or_null may be NULL (not both); dx does not overlap x.
+ * Numbers are multiplied as binary16 with one power of two per matrix as scale: c in two parts, but in one for dx of
+ * bfloat16 (a rounding by 2^-11, an eighth of dx's own), binary32 x and w in two, bfloat16 ones exactly, but for magnitudes below 2^-32 of
+ * their matrix's largest, which lose bits below 2^-39 of it.  The logits are multiplied from x and w as they are where
+ * qa_output_logprob would read more than 64 rows where they lie, and from these numbers elsewhere.  dx_or_null and dw_or_null may be NULL (not both); dx does not overlap x.
  * rows == 0 writes dw = 0 (kept, with accumulate). */
 int qa_output_logprob_grad(const qa_output_layer* layer, int type, const void* x, const void* w,
                            const int32_t* target_or_null, const float* stats, const float* entropy_or_null,
@@ -645,8 +647,8 @@ size_t qa_orthogonal_workspace_bytes(const qa_matrices* matrices, int type);
 /* out = X_steps, 1 <= steps <= QA_ORTHOGONAL_STEPS_MAX.  coefficients: HOST array of 3*steps floats, a, b, c of each
  * step in turn, magnitudes below 64; NULL: 3.4445, -4.7750, 2.0315 in every step, by which all but the smallest singular values end
  * between 0.7 and 1.2 after five.  A matrix of zeros gives zeros; one with an infinity or a NaN gives NaN.  ws may be NULL if 0 bytes are needed.  Numbers
- * are held in two binary16 parts, 22 bits and a sign, in fixed point below 2^-24 (X_i of a magnitude of 64 and more, which no
- * polynomial of this use has, are infinite, and NaN from there on); norms in binary64, sums in binary32.  out may be g. */
+ * are held in two binary16 parts, 22 bits and a sign, in fixed point below 2^-24 (elements of X_i, X_i X_i^T and its polynomial of
+ * a magnitude of 64 and more, which no coefficients of this use give, are infinite, and NaN from there on); norms in binary64, sums in binary32.  out may be g. */
 int qa_orthogonalize(const qa_matrices* matrices, int type, const void* g, int steps, const float* coefficients_or_null,
                      void* out, void* ws, size_t ws_bytes, void* stream);
 
