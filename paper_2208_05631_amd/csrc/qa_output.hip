@@ -61,7 +61,9 @@ enum { kOfC, kOfX, kOfW };
 constexpr int kMostBlocks = 1024;
 struct Scales {
   uint32_t most[3];
+  int rows;                                        // that count
   uint32_t found[3][kMostBlocks];
+  int counted[kMostBlocks];                        // of each share of the rows
 };
 __device__ __forceinline__ uint32_t most_in_block(uint32_t most) {
   __shared__ uint32_t waves[kWaves];
@@ -79,6 +81,8 @@ struct MostArgs {
   const void *x, *w;
   int64_t x_stride, w_stride;
   Scales* scales;
+  int* place;                                      // of a row among those of its share that count; -1: it does not
+  int64_t share;                                   // of the rows, a work-group for c
   int blocks[3];                                   // work-groups for c, for x and for w; 0: not wanted
 };
 template <int TYPE>
@@ -106,18 +110,38 @@ __device__ __forceinline__ uint32_t most_of_row(const ElemT<TYPE>* p, int64_t co
   return most;
 }
 // The largest |c| that a row can have: p <= 1, p |log p| <= 1 / e, and an entropy of at most log 2^24 < 17; the largest finite magnitudes of
-// rows of x that count, and of w.
+// rows of x that count, and of w.  And which rows count: the others take no part in the products.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void output_most_kernel(MostArgs A) {
   int block = blockIdx.x, which = 0;
   while (block >= A.blocks[which]) block -= A.blocks[which++];
   uint32_t most = 0;
   if (which == kOfC) {
-    for (int64_t t = (int64_t)block * kThreads + threadIdx.x; t < A.rows; t += (int64_t)A.blocks[which] * kThreads) {
-      const Row r = row_of(A.R, t);
-      const uint32_t c = as_u32(fabsf(r.a) + 18.0f * fabsf(r.e));
-      if (c < 0x7F800000u) most = max(most, c);
+    __shared__ int waves[kWaves];
+    const int64_t first = block * A.share, end = min(A.rows, first + A.share);
+    int counted = 0;
+    for (int64_t t0 = first; t0 < end; t0 += kThreads) {
+      const int64_t t = t0 + threadIdx.x;
+      bool here = false;
+      if (t < end) {
+        const Row r = row_of(A.R, t);
+        const uint32_t c = as_u32(fabsf(r.a) + 18.0f * fabsf(r.e));
+        if (c < 0x7F800000u) most = max(most, c);
+        here = counts(r);
+      }
+      const uint64_t all = __ballot(here);
+      if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = __popcll(all);
+      __syncthreads();
+      int before = counted + __popcll(all & ((uint64_t(1) << threadIdx.x % kWave) - 1));
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        before += w < (int)threadIdx.x / kWave ? waves[w] : 0;
+        counted += waves[w];
+      }
+      if (t < end) A.place[t] = here ? before : -1;
+      __syncthreads();
     }
+    if (threadIdx.x == 0) A.scales->counted[block] = counted;
   } else {
     const int64_t rows = which == kOfX ? A.rows : A.vocab, stride = which == kOfX ? A.x_stride : A.w_stride;
     const ElemT<TYPE>* const p = (const ElemT<TYPE>*)(which == kOfX ? A.x : A.w);
@@ -139,15 +163,19 @@ struct Copy {
   int64_t ld, to_rows;                             // zeros up to ld / parts columns, and in rows from `rows` on
   int* exps;                                       // kOwnScale: written
   int which;                                       // kOneScale
-  bool masked;                                     // zeros in rows that do not count
+  bool gather;                                     // the rows that count, one behind the other, and zeros up to a whole step of the products
   int blocks;
 };
 constexpr int kCopies = 4;
 struct CopyArgs {
   Copy copy[kCopies];
-  RowArgs R;
   Scales* scales;
   int found[3];                                    // how many there are; not 0: the largest are found first
+  const int* place;                                // of rows that are gathered, in shares; the first copy gathers, and writes which there are
+  int64_t share;
+  int* list;
+  void* zero;                                      // NULL, or zeros go to its rows that do not count
+  int64_t zero_stride;
 };
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
@@ -171,16 +199,15 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
   const int lane = threadIdx.x % kWave;
   int exp = 0;
   if (C.how == kOneScale && TYPE != QA_F16) exp = exponent_for(A.found[kOfC] ? find(C.which) : A.scales->most[C.which]);
-  for (int64_t row = (int64_t)block * kWaves + threadIdx.x / kWave; row < C.to_rows; row += (int64_t)C.blocks * kWaves) {
-    const ElemT<TYPE>* p = (const ElemT<TYPE>*)C.from + row * C.stride;
-    _Float16* q = (_Float16*)C.to + row * C.ld;
-    const int64_t cols = row < C.rows && !(C.masked && !counts(row_of(A.R, row))) ? C.cols : 0;
+  const auto copy = [&](int64_t from, int64_t to, int64_t cols) {
+    const ElemT<TYPE>* p = (const ElemT<TYPE>*)C.from + from * C.stride;
+    _Float16* q = (_Float16*)C.to + to * C.ld;
     if (TYPE == QA_F32 && C.how == kOwnScale) {
       uint32_t most = cols ? most_of_row<TYPE>(p, cols) : 0;
 #pragma unroll
       for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
       exp = exponent_for(most);
-      if (lane == 0) C.exps[row] = exp;
+      if (lane == 0) C.exps[to] = exp;
     }
     for (int64_t c = lane * kVec; c < C.ld / kParts; c += kWave * kVec) {
       const int n = (int)max((int64_t)0, min((int64_t)kVec, cols - c));
@@ -198,7 +225,53 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
         else *reinterpret_cast<u32x4*>(q + c) = from_f32<QA_F16>(v).a;
       }
     }
+  };
+  const int64_t first = (int64_t)block * kWaves + threadIdx.x / kWave, next = (int64_t)C.blocks * kWaves;
+  if (!C.gather) {
+    for (int64_t row = first; row < C.to_rows; row += next) copy(row, row, row < C.rows ? C.cols : 0);
+    return;
   }
+  __shared__ int before[kMostBlocks], waves[kWaves];           // rows that count before each share
+  constexpr int kEach = kMostBlocks / kThreads;
+  int mine[kEach], sum = 0;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int b = threadIdx.x * kEach + e;
+    mine[e] = sum;
+    sum += b < A.found[kOfC] ? A.scales->counted[b] : 0;
+  }
+  int upto = sum;
+#pragma unroll
+  for (int s = 1; s < kWave; s *= 2) {
+    const int other = __shfl_up(upto, s, kWave);
+    upto += lane >= s ? other : 0;
+  }
+  if (lane == kWave - 1) waves[threadIdx.x / kWave] = upto;
+  __syncthreads();
+  int rows = 0, ahead = upto - sum;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    ahead += w < (int)threadIdx.x / kWave ? waves[w] : 0;
+    rows += waves[w];
+  }
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) before[threadIdx.x * kEach + e] = ahead + mine[e];
+  __syncthreads();
+  if (blockIdx.x == 0 && threadIdx.x == 0) A.scales->rows = rows;
+  for (int64_t row = first; row < C.rows; row += next) {
+    const int place = A.place[row];
+    if (place >= 0) {
+      const int64_t to = before[row / A.share] + place;
+      copy(row, to, C.cols);
+      if (at == 0 && lane == 0) A.list[to] = (int)row;
+    } else if (at == 0 && A.zero) {
+      constexpr float zeros[kVec] = {};
+      for (int64_t c = lane * kVec; c < C.cols; c += kWave * kVec)
+        store_raw<TYPE>((ElemT<TYPE>*)A.zero + row * A.zero_stride + c, from_f32<TYPE>(zeros), (int)min((int64_t)kVec, C.cols - c));
+    }
+  }
+  if (block == 0)
+    for (int64_t to = rows + threadIdx.x / kWave; to < whole(max(1, rows), kPartsStep); to += kWaves) copy(0, to, 0);
 }
 
 // ---- scoring ------------------------------------------------------------------------------------------------------------------
@@ -500,16 +573,17 @@ __global__ __launch_bounds__(THREADS) void output_join_kernel(ScoreArgs A, int64
 
 // ---- the gradient of the logits -------------------------------------------------------------------------------------------
 
-// c of a piece of the vocabulary, scaled, in rows of parts: zeros behind the piece, in rows that do not count, and in rows up to a whole step.
+// c of a piece of the vocabulary, scaled, in rows of parts, for the rows that count: zeros behind the piece, and in rows up to a whole step.
 // SCALED: of operands scaled by one power of two each.
 template <bool SCALED, bool ENTROPY>
 struct LogitsGradOut {
-  LayerArgs L;                                     // vocab: of this piece
+  int64_t vocab;                                   // of this piece
   RowArgs R;
+  const int* list;                                 // rows that count
   int64_t first;                                   // of the piece
   const Scales* scales;
   _Float16* c;
-  int64_t ld, to_rows;
+  int64_t ld;
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0, char* lds) const {
     const int exp = exponent_for(scales->most[kOfC]), lane = threadIdx.x % kWave;
     constexpr int FN = (int)(sizeof p.acc[0] / sizeof p.acc[0][0]);
@@ -517,20 +591,21 @@ struct LogitsGradOut {
     int here[FN];
     const int z_exp = SCALED ? -(exponent_for(scales->most[kOfX]) + exponent_for(scales->most[kOfW])) : 0;
     bool none[FN];
+    const int64_t rows = scales->rows, to_rows = whole(max((int64_t)1, rows), kPartsStep);
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t t = t0 + 32 * j + lane % 32;
-      const Row r = row_of(R, min(t, L.rows - 1));
+      const Row r = row_of(R, rows ? list[min(t, rows - 1)] : 0);
       m[j] = r.m;
       log_sum[j] = r.log_sum * kLog2e;
       a[j] = ldexpf(r.a, exp);
       e[j] = ldexpf(r.e, exp) * kLn2;
       h[j] = r.h * kLog2e;
-      none[j] = t >= L.rows || !counts(r);
+      none[j] = t >= rows;
       const int64_t at = r.at - first - v0;
       here[j] = at >= 0 && at < P::kM ? (int)at : -kVec;
     }
-    const int left = (int)max((int64_t)0, min((int64_t)P::kM, L.vocab - v0)), wide = (int)max((int64_t)0, min((int64_t)P::kM, ld / 2 - v0));
+    const int left = (int)max((int64_t)0, min((int64_t)P::kM, vocab - v0)), wide = (int)max((int64_t)0, min((int64_t)P::kM, ld / 2 - v0));
     p.template for_runs<false>(0, 0, lds, [&](int v, int col, float (&z)[kVec]) {
       const int j = col / 32;
       float g[kVec];
@@ -563,12 +638,13 @@ struct GradOut {
   int64_t stride, rows, cols;
   int which;                                       // the scale of the other operand, -1: none
   bool add, last;                                  // to what is in sums (or, of binary32, in out); the last piece writes out
+  const int* list;                                 // NULL, or the product's rows are those that count, and where they go
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
     const int exp = -(exponent_for(scales->most[kOfC]) + (which < 0 ? 0 : exponent_for(scales->most[which])));
     p.for_runs(m0, n0, lds, [&](int64_t col, int64_t row, float (&v)[kVec]) {
-      if (row >= rows || col >= cols) return;
+      if (row >= (list ? scales->rows : rows) || col >= cols) return;
       const int n = (int)min((int64_t)kVec, cols - col);
-      ElemT<TYPE>* const at = out + row * stride + col;
+      ElemT<TYPE>* const at = out + (list ? list[row] : row) * stride + col;
       float* const s = sums + (p.split * rows + row) * cols + col;
       float before[kVec] = {};
       if (add) {
@@ -576,7 +652,7 @@ struct GradOut {
         else to_f32<TYPE>(load_raw<TYPE>(at, n), before);
       }
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) v[e] = before[e] + ldexpf(v[e], exp);
+      for (int e = 0; e < kVec; ++e) v[e] = before[e] + (p.empty ? 0.0f : ldexpf(v[e], exp));
       if (last) store_raw<TYPE>(at, from_f32<TYPE>(v), n);
       else store_raw<QA_F32>(s, from_f32<QA_F32>(v), n);
     });
@@ -585,8 +661,8 @@ struct GradOut {
 // A gradient from the splits' sums, in their order.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void output_sum_kernel(const float* sums, int splits, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride,
-                                                              int accumulate) {
-  const int64_t across = ceil_div(cols, kVec), all = rows * across;
+                                                              int accumulate, const int* list, const Scales* scales) {
+  const int64_t across = ceil_div(cols, kVec), all = (list ? scales->rows : rows) * across;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
     const int64_t row = i / across, col = i % across * kVec;
     const int n = (int)min((int64_t)kVec, cols - col);
@@ -598,13 +674,14 @@ __global__ __launch_bounds__(kThreads) void output_sum_kernel(const float* sums,
 #pragma unroll
       for (int e = 0; e < kVec; ++e) v[e] += w[e];
     }
+    ElemT<TYPE>* const at = out + (list ? list[row] : row) * stride + col;
     if (accumulate) {
       float w[kVec];
-      to_f32<TYPE>(load_raw<TYPE>(out + row * stride + col, n), w);
+      to_f32<TYPE>(load_raw<TYPE>(at, n), w);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) v[e] += w[e];
     }
-    store_raw<TYPE>(out + row * stride + col, from_f32<TYPE>(v), n);
+    store_raw<TYPE>(at, from_f32<TYPE>(v), n);
   }
 }
 __global__ __launch_bounds__(kThreads) void output_zero_kernel(float* p, int64_t stride, int64_t rows, int64_t cols) {
@@ -681,7 +758,7 @@ struct Plan {
   size_t x, w, x_exp, w_exp;                       // copies and exponents
   size_t m, s, sw, given;                          // scoring
   int64_t chunks, each;                            // each: of the vocabulary per work-group, where w is streamed
-  size_t scales, xc, wc, c, sums;                  // gradient: x and w as the products with c take them
+  size_t scales, place, list, xr, xc, wc, c, sums; // gradient: rows of x for the logits, where xc does not serve; x and w as the products with c take them
   size_t dw_sums;
   int64_t hc, tp, vp;
   ProductPlan dx;
@@ -731,6 +808,9 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.pieces = ceil_div(L.vocab, P.piece);
     P.vp = whole(P.piece, kWholeStep);
     P.scales = room.take(sizeof(Scales));
+    P.place = room.take(4 * L.rows);
+    P.list = room.take(4 * L.rows);
+    P.xr = room.take(!P.copies && type == QA_BF16 ? 2 * P.tp * P.hc : 0);
     P.xc = room.take(2 * P.parts * P.tp * P.hc);
     P.wc = room.take(2 * P.parts * P.vp * P.hc);
     P.c = room.take(2 * 2 * P.tp * P.vp);
@@ -770,15 +850,15 @@ size_t bytes_of(const qa_output_layer& L, int op, int type) {
 struct CopyList {
   CopyArgs A = {};
   int n = 0, blocks = 0;
-  void add(int how, const void* from, int64_t stride, int64_t rows, int64_t cols, void* to, int64_t ld, int64_t to_rows, int* exps, int which, bool masked) {
+  void add(int how, const void* from, int64_t stride, int64_t rows, int64_t cols, void* to, int64_t ld, int64_t to_rows, int* exps, int which, bool gather) {
     Copy& C = A.copy[n++];
-    C = {how, from, stride, rows, cols, to, ld, to_rows, exps, which, masked, (int)std::min<int64_t>(ceil_div(to_rows, kWaves), 1 << 14)};
+    C = {how, from, stride, rows, cols, to, ld, to_rows, exps, which, gather, (int)std::min<int64_t>(ceil_div(to_rows, kWaves), 1 << 14)};
     blocks += C.blocks;
   }
   template <int TYPE> int launch(hipStream_t stream) {
     if (A.found[kOfC] == 0 && n == 0) return QA_OK;
     output_copy_kernel<TYPE><<<(unsigned)std::max(blocks, 1), kThreads, 0, stream>>>(A);
-    *this = CopyList{{.R = A.R, .scales = A.scales}};
+    *this = CopyList{{.scales = A.scales}};
     return launch_status();
   }
 };
@@ -791,16 +871,16 @@ Operand logits_operand(CopyList& copies, int type, const void* from, int64_t str
 }
 // Logits of a piece of the vocabulary: w's rows by x's.
 template <bool BF16, Lies LIE, class Epilogue>
-int logits_launch(const Operand& w, const Operand& x, int64_t features, Tall tiles, const Epilogue& out, hipStream_t stream) {
+int logits_launch(const Operand& w, const Operand& x, int64_t features, Tall tiles, const Epilogue& out, hipStream_t stream, const int* fewer = nullptr) {
   constexpr bool kApart = LIE == kRowsOfParts;
   switch (tiles) {
-    case kTall128: return product_launch<Product<BF16, LIE, LIE, 2, 2, 2, 2, 1, kApart>>(w, x, features, out, 1, stream);
-    case kTall128Two: return product_launch<Product<BF16, LIE, LIE, 2, 2, 2, 2, 2, kApart>>(w, x, features, out, 1, stream);
-    case kTall64: return product_launch<Product<BF16, LIE, LIE, 1, 1, 2, 2, 4, kApart>>(w, x, features, out, 1, stream);
-    case kFlat: return product_launch<Product<BF16, LIE, LIE, 4, 1, 2, 2, 1, kApart>>(w, x, features, out, 1, stream);
+    case kTall128: return product_launch<Product<BF16, LIE, LIE, 2, 2, 2, 2, 1, kApart>>(w, x, features, out, 1, stream, 1, fewer);
+    case kTall128Two: return product_launch<Product<BF16, LIE, LIE, 2, 2, 2, 2, 2, kApart>>(w, x, features, out, 1, stream, 1, fewer);
+    case kTall64: return product_launch<Product<BF16, LIE, LIE, 1, 1, 2, 2, 4, kApart>>(w, x, features, out, 1, stream, 1, fewer);
+    case kFlat: return product_launch<Product<BF16, LIE, LIE, 4, 1, 2, 2, 1, kApart>>(w, x, features, out, 1, stream, 1, fewer);
     default: break;
   }
-  if constexpr (!kApart) return product_launch<Product256<BF16, LIE, LIE>>(w, x, features, out, 1, stream);
+  if constexpr (!kApart) return product_launch<Product256<BF16, LIE, LIE>>(w, x, features, out, 1, stream, 1, fewer);
   return QA_ERR_INVALID_ARG;                       // not reached: no such tiles with parts
 }
 
@@ -848,16 +928,17 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
 }
 
 template <int TYPE>
-int sum_launch(const float* sums, int64_t splits, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride, int accumulate, hipStream_t stream) {
+int sum_launch(const float* sums, int64_t splits, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride, int accumulate, hipStream_t stream,
+               const int* list = nullptr, const Scales* scales = nullptr) {
   const int64_t vecs = rows * ceil_div(cols, kVec);
-  output_sum_kernel<TYPE><<<(unsigned)std::min<int64_t>(ceil_div(vecs, kThreads), 4096), kThreads, 0, stream>>>(sums, (int)splits, rows, cols, out, stride, accumulate);
+  output_sum_kernel<TYPE><<<(unsigned)std::min<int64_t>(ceil_div(vecs, kThreads), 4096), kThreads, 0, stream>>>(sums, (int)splits, rows, cols, out, stride, accumulate, list, scales);
   return launch_status();
 }
 template <Lies LA, Lies LB, class Epilogue>
-int grad_product(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, const ProductPlan& plan, hipStream_t stream) {
-  if (plan.tiles == kTiles256) return product_launch<Product256<false, LA, LB>>(a, b, k, out, 1, stream, plan.splits);
-  if (plan.tiles == kTiles128) return product_launch<Product128<false, LA, LB>>(a, b, k, out, 1, stream, plan.splits);
-  return product_launch<Product<false, LA, LB, 2, 2, 2, 2, 2>>(a, b, k, out, 1, stream, plan.splits);
+int grad_product(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, const ProductPlan& plan, const int* fewer, bool fewer_of_k, hipStream_t stream) {
+  if (plan.tiles == kTiles256) return product_launch<Product256<false, LA, LB>>(a, b, k, out, 1, stream, plan.splits, fewer, fewer_of_k);
+  if (plan.tiles == kTiles128) return product_launch<Product128<false, LA, LB>>(a, b, k, out, 1, stream, plan.splits, fewer, fewer_of_k);
+  return product_launch<Product<false, LA, LB, 2, 2, 2, 2, 2>>(a, b, k, out, 1, stream, plan.splits, fewer, fewer_of_k);
 }
 
 struct GradCall {
@@ -875,19 +956,29 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
   const Plan P = plan_of(L, QA_OP_LOGPROB_GRAD, TYPE, G.x, G.w);
   Scales* const scales = (Scales*)(ws + P.scales);
   const auto blocks = [](bool wanted, int64_t n, int64_t each) { return wanted ? (int)std::min<int64_t>(kMostBlocks, ceil_div(n, each)) : 0; };
-  const MostArgs most = {G.rows, L.rows, L.vocab, L.features, G.x, G.w, L.x_stride, L.w_stride, scales,
-                         {blocks(true, L.rows, kThreads), blocks(TYPE != QA_F16 && (G.dw || P.copies), L.rows, kWaves),
+  const int64_t share = whole(ceil_div(L.rows, kMostBlocks), kThreads);
+  int* const place = (int*)(ws + P.place);
+  int* const list = (int*)(ws + P.list);
+  const int* const rows = &scales->rows;
+  const MostArgs most = {G.rows, L.rows, L.vocab, L.features, G.x, G.w, L.x_stride, L.w_stride, scales, place, share,
+                         {(int)ceil_div(L.rows, share), blocks(TYPE != QA_F16 && (G.dw || P.copies), L.rows, kWaves),
                           blocks(TYPE != QA_F16 && (G.dx || P.copies), L.vocab, kWaves)}};
   output_most_kernel<TYPE><<<(unsigned)(most.blocks[0] + most.blocks[1] + most.blocks[2]), kThreads, 0, stream>>>(most);
   if (const int rc = launch_status()) return rc;
 
   const int64_t copied = P.parts * P.hc;
   CopyList copies;
-  copies.A.R = G.rows;
   copies.A.scales = scales;
   for (int i = 0; i < 3; ++i) copies.A.found[i] = most.blocks[i];
-  // Always copied: rows that do not count may hold anything.
-  if (G.dw || P.copies) copies.add(kOneScale, G.x, L.x_stride, L.rows, L.features, ws + P.xc, copied, P.tp, nullptr, kOfX, true);
+  copies.A.place = place;
+  copies.A.share = share;
+  copies.A.list = list;
+  copies.A.zero = G.dx;
+  copies.A.zero_stride = G.dx_stride;
+  // bfloat16's own for the logits; the products with c take binary16.
+  const bool own = TYPE == QA_BF16 && !P.copies;
+  if (own) copies.add(kAsTheyAre, G.x, L.x_stride, L.rows, L.features, ws + P.xr, P.hc, L.rows, nullptr, 0, true);
+  if (G.dw || !own) copies.add(kOneScale, G.x, L.x_stride, L.rows, L.features, ws + P.xc, copied, L.rows, nullptr, kOfX, true);
   constexpr Lies kColumnsOf = TYPE == QA_F32 ? kColumnsOfParts : kColumns;
   for (int64_t first = 0; first < L.vocab; first += P.piece) {
     const int64_t vocab = std::min(P.piece, L.vocab - first);
@@ -902,14 +993,13 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     const Tall tiles = logits_tiles(L.rows, vocab, L.features, TYPE);
     const auto logits = [&](auto entropy) {
       constexpr bool kEntropy = decltype(entropy)::value;
-      const LayerArgs piece = {L.rows, vocab, nullptr, nullptr, nullptr};
       if (P.copies) {
-        const LogitsGradOut<true, kEntropy> grad{piece, G.rows, first, scales, c, 2 * P.vp, P.tp};
-        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xc, copied, 0, L.rows}, L.features, tiles, grad, stream);
+        const LogitsGradOut<true, kEntropy> grad{vocab, G.rows, list, first, scales, c, 2 * P.vp};
+        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xc, copied, 0, L.rows}, L.features, tiles, grad, stream, rows);
       }
       if constexpr (TYPE != QA_F32) {              // copied always
-        const LogitsGradOut<false, kEntropy> grad{piece, G.rows, first, scales, c, 2 * P.vp, P.tp};
-        return logits_launch<TYPE == QA_BF16, kRows>(Operand{from, L.w_stride, 0, vocab}, Operand{G.x, L.x_stride, 0, L.rows}, L.features, tiles, grad, stream);
+        const LogitsGradOut<false, kEntropy> grad{vocab, G.rows, list, first, scales, c, 2 * P.vp};
+        return logits_launch<TYPE == QA_BF16, kRows>(Operand{from, L.w_stride, 0, vocab}, Operand{ws + (own ? P.xr : P.xc), P.hc, 0, L.rows}, L.features, tiles, grad, stream, rows);
       }
       return (int)QA_ERR_INVALID_ARG;              // not reached
     };
@@ -917,19 +1007,19 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     if (G.dx) {
       const bool last = first + P.piece >= L.vocab;
       const GradOut<TYPE> out{(ElemT<TYPE>*)G.dx, P.pieces > 1 || P.dx.splits > 1 ? (float*)(ws + P.sums) : nullptr, scales, G.dx_stride, L.rows, L.features,
-                              TYPE == QA_F16 ? -1 : kOfW, first > 0, last && P.dx.splits == 1};
+                              TYPE == QA_F16 ? -1 : kOfW, first > 0, last && P.dx.splits == 1, list};
       // One part of c has 11 bits, which is little beside bfloat16's 8, but as much as binary16's own.
       constexpr Lies kC = TYPE == QA_BF16 ? kHiOfRows : kRowsOfParts;
-      if (const int rc = grad_product<kColumnsOf, kC>(wc, Operand{c, 2 * P.vp, 0, L.rows}, vocab, out, P.dx, stream)) return rc;
+      if (const int rc = grad_product<kColumnsOf, kC>(wc, Operand{c, 2 * P.vp, 0, L.rows}, vocab, out, P.dx, rows, false, stream)) return rc;
       if (last && P.dx.splits > 1)
-        if (const int rc = sum_launch<TYPE>((const float*)(ws + P.sums), P.dx.splits, L.rows, L.features, (ElemT<TYPE>*)G.dx, G.dx_stride, 0, stream)) return rc;
+        if (const int rc = sum_launch<TYPE>((const float*)(ws + P.sums), P.dx.splits, L.rows, L.features, (ElemT<TYPE>*)G.dx, G.dx_stride, 0, stream, list, scales)) return rc;
     }
     if (G.dw) {
       float* const dw = G.dw + first * G.dw_stride;
       const ProductPlan plan = dw_plan(L, TYPE, vocab);
       float* const sums = plan.splits > 1 ? (float*)(ws + P.dw_sums) : nullptr;
-      const GradOut<QA_F32> out{dw, sums, scales, G.dw_stride, vocab, L.features, TYPE == QA_F16 ? -1 : kOfX, !sums && G.accumulate, !sums};
-      if (const int rc = grad_product<kColumnsOf, kColumnsOfParts>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, plan, stream)) return rc;
+      const GradOut<QA_F32> out{dw, sums, scales, G.dw_stride, vocab, L.features, TYPE == QA_F16 ? -1 : kOfX, !sums && G.accumulate, !sums, nullptr};
+      if (const int rc = grad_product<kColumnsOf, kColumnsOfParts>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, plan, rows, true, stream)) return rc;
       if (sums)
         if (const int rc = sum_launch<QA_F32>(sums, plan.splits, vocab, L.features, dw, G.dw_stride, G.accumulate, stream)) return rc;
     }

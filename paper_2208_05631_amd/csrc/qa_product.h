@@ -38,6 +38,9 @@ struct ProductArgs {
   Operand a, b;
   int steps, split_steps;                          // of k, and of one split of them
   unsigned splits, tiles_m, tiles_n, tiles;        // tiles: of one matrix
+  unsigned batch;
+  const int* fewer;                                // NULL, or how many there are of B's, or of k; 0 counts as 1
+  bool fewer_of_k;
 };
 
 // Brings SIDE values of i and STEP of k to LDS, straight from memory, 16 bytes per lane.
@@ -159,6 +162,7 @@ struct Product {
   int to_load, wave;
   int64_t matrix, split;                           // which of the batch, and of the splits of k
   bool owns;                                       // whether this wave has the sums
+  bool empty;                                      // nothing is in this split, and what the sums hold is not meant
 
   // Instructions [FROM, TO) of a step's; behind the last one go on, past the last step to itself.
   template <int FROM, int TO>
@@ -242,7 +246,8 @@ struct Product {
     owns = share == 0;
     matrix = matrix_;
     split = split_;
-    const int begin = (int)split * A.split_steps, in_split = min(A.split_steps, A.steps - begin);
+    empty = (int)split * A.split_steps >= A.steps;
+    const int begin = empty ? 0 : (int)split * A.split_steps, in_split = min(A.split_steps, A.steps - begin);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -367,8 +372,8 @@ struct Product {
 
 // Consecutive work-groups go to the eight dies in turn.  Each die takes tiles that lie together, in bands eight tiles wide,
 // so that its cache is asked for the same rows.
-__device__ __forceinline__ unsigned on_its_die() {
-  const unsigned die = blockIdx.x % 8, each = gridDim.x / 8, more = gridDim.x % 8;
+__device__ __forceinline__ unsigned on_its_die(unsigned all) {
+  const unsigned die = blockIdx.x % 8, each = all / 8, more = all % 8;
   return die * each + min(die, more) + blockIdx.x / 8;
 }
 // LOWER: tiles on and below the diagonal only.
@@ -391,7 +396,19 @@ __device__ __forceinline__ void tile_of(const ProductArgs& A, unsigned tile, uns
 template <class P, bool LOWER, class Epilogue>
 __global__ __launch_bounds__(P::kGroup, P::kWavesPerSimd) void product_kernel(ProductArgs A, Epilogue out) {
   __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
-  const unsigned tile = on_its_die(), which = tile / A.tiles, matrix = which / A.splits;
+  if (A.fewer) {
+    const int n = max(1, *A.fewer);
+    if (A.fewer_of_k) {
+      A.steps = (n + P::kStep - 1) / P::kStep;
+      A.split_steps = (A.steps + (int)A.splits - 1) / (int)A.splits;
+    } else {
+      A.b.n = n;
+      A.tiles_n = (unsigned)(n + P::kN - 1) / P::kN;
+      A.tiles = A.tiles_m * A.tiles_n;
+    }
+    if (blockIdx.x >= A.tiles * A.batch * A.splits) return;
+  }
+  const unsigned tile = on_its_die(A.tiles * A.batch * A.splits), which = tile / A.tiles, matrix = which / A.splits;
   unsigned tm, tn;
   tile_of<LOWER>(A, tile - which * A.tiles, tm, tn);
   const int64_t m0 = (int64_t)tm * P::kM, n0 = (int64_t)tn * P::kN;
@@ -402,8 +419,9 @@ __global__ __launch_bounds__(P::kGroup, P::kWavesPerSimd) void product_kernel(Pr
 
 // Launches tiles of the given form over all of A and B; k: how many there are, zeros up to a whole step.
 template <class P, bool LOWER = false, class Epilogue>
-int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream, int64_t splits = 1) {
-  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), 0, 0, (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN), 0};
+int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream, int64_t splits = 1,
+                   const int* fewer = nullptr, bool fewer_of_k = false) {
+  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), 0, 0, (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN), 0, batch, fewer, fewer_of_k};
   A.split_steps = (int)ceil_div(A.steps, splits);
   A.splits = (unsigned)ceil_div(A.steps, A.split_steps);       // none is empty
   A.tiles = LOWER ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n;

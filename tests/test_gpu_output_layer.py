@@ -101,7 +101,7 @@ def test_logprob_in_large_tiles(t):
     check_score(t, x, w, y, score(layer, xd, wd, y, t))
 
 
-def check_grad(t, T, V, H, pad=0, lead=0, entropy=False, ignored=0.0, wants="xw", accumulate=False, seed=0):
+def check_grad(t, T, V, H, pad=0, lead=0, entropy=False, ignored=0.0, wants="xw", accumulate=False, seed=0, kept=None):
     gen = gen_of(t, T, V, H, entropy, ignored, seed)
     layer, x, xd, w, wd, y = layer_of(gen, T, V, H, t, pad, lead)
     if ignored:
@@ -110,6 +110,11 @@ def check_grad(t, T, V, H, pad=0, lead=0, entropy=False, ignored=0.0, wants="xw"
     st32, h32 = st.float(), h.float()
     a = -torch.rand(T, generator=gen) - 0.5
     e = 0.3 * torch.randn(T, generator=gen) if entropy else None
+    if kept is not None:
+        skip = torch.ones(T, dtype=torch.bool)
+        skip[kept] = False
+        a[skip] = 0.0
+        xd[skip.to(DEV)] = math.nan
     dx = torch.full((T, H + 1), 5.0, dtype=TYPES[t], device=DEV) if "x" in wants else None
     dw = torch.full((V, H + 2), 3.0, device=DEV) if "w" in wants else None
     qa.qa_output_logprob_grad(layer, code_of(t), xd, wd, y.to(torch.int32).to(DEV), st32.to(DEV), h32.to(DEV) if entropy else None, a.to(DEV),
@@ -362,6 +367,14 @@ def test_dw_of_far_rows():
     for to, s in ((dw, stride), (near, H)):
         qa.qa_output_logprob_grad(layer, qa.QA_BF16, xd, wd, y.to(torch.int32).to(DEV), st.float().to(DEV), None, a.to(DEV), None, None, H, to, s, 0, ws)
     assert torch.equal(dw[:, :H], near) and bool((dw[:, H:H + 100] == 0).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T,V,H", [(700, 300, 64), (700, 300, 50), (5000, 200, 32)])
+@pytest.mark.parametrize("kept", [(), (699,), (0, 1, 255, 256, 257, 511, 512), range(100, 116), range(37, 163), range(300, 700)])
+def test_few_of_many_rows_count(t, T, V, H, kept):
+    """The others' dx is 0, whatever x holds there.  None, one, up to a whole step of 16 and more, within one share of the rows and in several."""
+    check_grad(t, T, V, H, accumulate=True, kept=list(kept))
 
 
 @pytest.mark.parametrize("t", ["bf16", "f32"])

@@ -66,7 +66,7 @@ def test_the_others(compiled):
 def test_loops_of_products_wait_for_what_they_count(compiled, source, least):
     """The loop's barrier waits until a known number of loads is on its way: there is no other access of memory in the loop (a spill would be
     one), and no other wait for loads, which the compiler would set in front of reads of LDS if it took the buffers for one."""
-    bodies = re.findall(r"^(\S*product_kernel\S*):[^\n]*\n(.*?)\n\ts_endpgm", compiled[source][1], re.M | re.S)
+    bodies = re.findall(r"^(\S*product_kernel\S*):[^\n]*\n(.*?)\n\.Lfunc_end", compiled[source][1], re.M | re.S)
     assert len(bodies) >= least
     for name, body in bodies:
         lines = body.split("\n")
