@@ -164,6 +164,7 @@ struct Copy {
   int* exps;                                       // kOwnScale: written
   int which;                                       // kOneScale
   bool gather;                                     // the rows that count, one behind the other, and zeros up to a whole step of the products
+  bool unless_all;                                 // count
   int blocks;
 };
 constexpr int kCopies = 4;
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
     const int place = A.place[row];
     if (place >= 0) {
       const int64_t to = before[row / A.share] + place;
-      copy(row, to, C.cols);
+      if (!(C.unless_all && rows == C.rows)) copy(row, to, C.cols);
       if (at == 0 && lane == 0) A.list[to] = (int)row;
     } else if (at == 0 && A.zero) {
       constexpr float zeros[kVec] = {};
@@ -641,11 +642,14 @@ struct GradOut {
   const int* list;                                 // NULL, or the product's rows are those that count, and where they go
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
     const int exp = -(exponent_for(scales->most[kOfC]) + (which < 0 ? 0 : exponent_for(scales->most[which])));
+    const int64_t all = list ? scales->rows : rows;
+    float* const its_sums = sums + p.split * all * cols;
+    const bool writes = last || !sums;
     p.for_runs(m0, n0, lds, [&](int64_t col, int64_t row, float (&v)[kVec]) {
-      if (row >= (list ? scales->rows : rows) || col >= cols) return;
+      if (row >= all || col >= cols) return;
       const int n = (int)min((int64_t)kVec, cols - col);
-      ElemT<TYPE>* const at = out + (list ? list[row] : row) * stride + col;
-      float* const s = sums + (p.split * rows + row) * cols + col;
+      ElemT<TYPE>* const at = out + (list && writes ? list[row] : row) * stride + col;
+      float* const s = its_sums + row * cols + col;
       float before[kVec] = {};
       if (add) {
         if (sums) to_f32<QA_F32>(load_raw<QA_F32>(s, n), before);
@@ -659,10 +663,16 @@ struct GradOut {
   }
 };
 // A gradient from the splits' sums, in their order.
+struct Splits {
+  int splits, most;                                // as planned, and where few rows count
+  unsigned side;                                   // of the product's tiles, along the rows
+};
 template <int TYPE>
-__global__ __launch_bounds__(kThreads) void output_sum_kernel(const float* sums, int splits, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride,
+__global__ __launch_bounds__(kThreads) void output_sum_kernel(const float* sums, Splits of, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride,
                                                               int accumulate, const int* list, const Scales* scales) {
-  const int64_t across = ceil_div(cols, kVec), all = (list ? scales->rows : rows) * across;
+  const int splits = list ? splits_of_fewer(of.splits, of.most, of.side, (unsigned)rows, max(1, scales->rows)) : of.splits;
+  if (list) rows = scales->rows;
+  const int64_t across = ceil_div(cols, kVec), all = rows * across;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
     const int64_t row = i / across, col = i % across * kVec;
     const int n = (int)min((int64_t)kVec, cols - col);
@@ -850,9 +860,9 @@ size_t bytes_of(const qa_output_layer& L, int op, int type) {
 struct CopyList {
   CopyArgs A = {};
   int n = 0, blocks = 0;
-  void add(int how, const void* from, int64_t stride, int64_t rows, int64_t cols, void* to, int64_t ld, int64_t to_rows, int* exps, int which, bool gather) {
+  void add(int how, const void* from, int64_t stride, int64_t rows, int64_t cols, void* to, int64_t ld, int64_t to_rows, int* exps, int which, bool gather, bool unless_all = false) {
     Copy& C = A.copy[n++];
-    C = {how, from, stride, rows, cols, to, ld, to_rows, exps, which, gather, (int)std::min<int64_t>(ceil_div(to_rows, kWaves), 1 << 14)};
+    C = {how, from, stride, rows, cols, to, ld, to_rows, exps, which, gather, unless_all, (int)std::min<int64_t>(ceil_div(to_rows, kWaves), 1 << 14)};
     blocks += C.blocks;
   }
   template <int TYPE> int launch(hipStream_t stream) {
@@ -870,17 +880,17 @@ Operand logits_operand(CopyList& copies, int type, const void* from, int64_t str
   return {to, P.parts * P.hp, 0, rows};
 }
 // Logits of a piece of the vocabulary: w's rows by x's.
-template <bool BF16, Lies LIE, class Epilogue>
-int logits_launch(const Operand& w, const Operand& x, int64_t features, Tall tiles, const Epilogue& out, hipStream_t stream, const int* fewer = nullptr) {
+template <bool BF16, Lies LIE, HowMany MANY, class Epilogue>
+int logits_launch(const Operand& w, const Operand& x, int64_t features, Tall tiles, const Epilogue& out, hipStream_t stream, const Fewer& fewer = {}) {
   constexpr bool kApart = LIE == kRowsOfParts;
   switch (tiles) {
-    case kTall128: return product_launch<Product<BF16, LIE, LIE, 2, 2, 2, 2, 1, kApart>>(w, x, features, out, 1, stream, 1, fewer);
-    case kTall128Two: return product_launch<Product<BF16, LIE, LIE, 2, 2, 2, 2, 2, kApart>>(w, x, features, out, 1, stream, 1, fewer);
-    case kTall64: return product_launch<Product<BF16, LIE, LIE, 1, 1, 2, 2, 4, kApart>>(w, x, features, out, 1, stream, 1, fewer);
-    case kFlat: return product_launch<Product<BF16, LIE, LIE, 4, 1, 2, 2, 1, kApart>>(w, x, features, out, 1, stream, 1, fewer);
+    case kTall128: return product_launch<Product<BF16, LIE, LIE, 2, 2, 2, 2, 1, kApart>, false, MANY>(w, x, features, out, 1, stream, 1, fewer);
+    case kTall128Two: return product_launch<Product<BF16, LIE, LIE, 2, 2, 2, 2, 2, kApart>, false, MANY>(w, x, features, out, 1, stream, 1, fewer);
+    case kTall64: return product_launch<Product<BF16, LIE, LIE, 1, 1, 2, 2, 4, kApart>, false, MANY>(w, x, features, out, 1, stream, 1, fewer);
+    case kFlat: return product_launch<Product<BF16, LIE, LIE, 4, 1, 2, 2, 1, kApart>, false, MANY>(w, x, features, out, 1, stream, 1, fewer);
     default: break;
   }
-  if constexpr (!kApart) return product_launch<Product256<BF16, LIE, LIE>>(w, x, features, out, 1, stream, 1, fewer);
+  if constexpr (!kApart) return product_launch<Product256<BF16, LIE, LIE>, false, MANY>(w, x, features, out, 1, stream, 1, fewer);
   return QA_ERR_INVALID_ARG;                       // not reached: no such tiles with parts
 }
 
@@ -920,7 +930,7 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
       A.first = first;
       A.first_chunk = first / P.piece * chunks_of(P.tiles) * ceil_div(P.piece, height_of(P.tiles));
       const ScoreOut<TYPE == QA_F32> out{LayerArgs{here.rows, vocab, x_exp, w_exp, its_target}, A};
-      if (const int rc = logits_launch<TYPE == QA_BF16, TYPE == QA_F32 ? kRowsOfParts : kRows>(wo, xo, L.features, P.tiles, out, stream)) return rc;
+      if (const int rc = logits_launch<TYPE == QA_BF16, TYPE == QA_F32 ? kRowsOfParts : kRows, kAll>(wo, xo, L.features, P.tiles, out, stream)) return rc;
     }
     if (const int rc = join_launch(A, here, P.chunks, its_target, from(logprob, t), from(entropy, t), from(stats, 2 * t), stream)) return rc;
   }
@@ -928,17 +938,17 @@ int score_launch(const qa_output_layer& L, const void* x, const void* w, const i
 }
 
 template <int TYPE>
-int sum_launch(const float* sums, int64_t splits, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride, int accumulate, hipStream_t stream,
+int sum_launch(const float* sums, const Splits& splits, int64_t rows, int64_t cols, ElemT<TYPE>* out, int64_t stride, int accumulate, hipStream_t stream,
                const int* list = nullptr, const Scales* scales = nullptr) {
   const int64_t vecs = rows * ceil_div(cols, kVec);
-  output_sum_kernel<TYPE><<<(unsigned)std::min<int64_t>(ceil_div(vecs, kThreads), 4096), kThreads, 0, stream>>>(sums, (int)splits, rows, cols, out, stride, accumulate, list, scales);
+  output_sum_kernel<TYPE><<<(unsigned)std::min<int64_t>(ceil_div(vecs, kThreads), 4096), kThreads, 0, stream>>>(sums, splits, rows, cols, out, stride, accumulate, list, scales);
   return launch_status();
 }
-template <Lies LA, Lies LB, class Epilogue>
-int grad_product(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, const ProductPlan& plan, const int* fewer, bool fewer_of_k, hipStream_t stream) {
-  if (plan.tiles == kTiles256) return product_launch<Product256<false, LA, LB>>(a, b, k, out, 1, stream, plan.splits, fewer, fewer_of_k);
-  if (plan.tiles == kTiles128) return product_launch<Product128<false, LA, LB>>(a, b, k, out, 1, stream, plan.splits, fewer, fewer_of_k);
-  return product_launch<Product<false, LA, LB, 2, 2, 2, 2, 2>>(a, b, k, out, 1, stream, plan.splits, fewer, fewer_of_k);
+template <Lies LA, Lies LB, HowMany MANY, class Epilogue>
+int grad_product(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, const ProductPlan& plan, const Fewer& fewer, hipStream_t stream) {
+  if (plan.tiles == kTiles256) return product_launch<Product256<false, LA, LB>, false, MANY>(a, b, k, out, 1, stream, plan.splits, fewer);
+  if (plan.tiles == kTiles128) return product_launch<Product128<false, LA, LB>, false, MANY>(a, b, k, out, 1, stream, plan.splits, fewer);
+  return product_launch<Product<false, LA, LB, 2, 2, 2, 2, 2>, false, MANY>(a, b, k, out, 1, stream, plan.splits, fewer);
 }
 
 struct GradCall {
@@ -959,7 +969,7 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
   const int64_t share = whole(ceil_div(L.rows, kMostBlocks), kThreads);
   int* const place = (int*)(ws + P.place);
   int* const list = (int*)(ws + P.list);
-  const int* const rows = &scales->rows;
+  const Fewer rows = {.n = &scales->rows};
   const MostArgs most = {G.rows, L.rows, L.vocab, L.features, G.x, G.w, L.x_stride, L.w_stride, scales, place, share,
                          {(int)ceil_div(L.rows, share), blocks(TYPE != QA_F16 && (G.dw || P.copies), L.rows, kWaves),
                           blocks(TYPE != QA_F16 && (G.dx || P.copies), L.vocab, kWaves)}};
@@ -977,8 +987,14 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
   copies.A.zero_stride = G.dx_stride;
   // bfloat16's own for the logits; the products with c take binary16.
   const bool own = TYPE == QA_BF16 && !P.copies;
-  if (own) copies.add(kAsTheyAre, G.x, L.x_stride, L.rows, L.features, ws + P.xr, P.hc, L.rows, nullptr, 0, true);
+  if (own) copies.add(kAsTheyAre, G.x, L.x_stride, L.rows, L.features, ws + P.xr, P.hc, L.rows, nullptr, 0, true, true);
   if (G.dw || !own) copies.add(kOneScale, G.x, L.x_stride, L.rows, L.features, ws + P.xc, copied, L.rows, nullptr, kOfX, true);
+  // Where few rows count, dx has more splits instead of tiles, in the same room.
+  Fewer dx_rows = rows;
+  const int64_t dx_side = P.dx.tiles == kTiles256 ? 256 : 128;
+  const Splits dx_splits = {(int)P.dx.splits, (int)std::max(P.dx.splits, std::min<int64_t>(64, std::min(P.piece, L.vocab) / (8 * kWholeStep))),
+                            (unsigned)dx_side};
+  if (P.dx.splits > 1) dx_rows.most_splits = dx_splits.most;
   constexpr Lies kColumnsOf = TYPE == QA_F32 ? kColumnsOfParts : kColumns;
   for (int64_t first = 0; first < L.vocab; first += P.piece) {
     const int64_t vocab = std::min(P.piece, L.vocab - first);
@@ -995,11 +1011,16 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
       constexpr bool kEntropy = decltype(entropy)::value;
       if (P.copies) {
         const LogitsGradOut<true, kEntropy> grad{vocab, G.rows, list, first, scales, c, 2 * P.vp};
-        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xc, copied, 0, L.rows}, L.features, tiles, grad, stream, rows);
+        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows, kFewerOfB>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xc, copied, 0, L.rows}, L.features, tiles, grad, stream, rows);
       }
       if constexpr (TYPE != QA_F32) {              // copied always
         const LogitsGradOut<false, kEntropy> grad{vocab, G.rows, list, first, scales, c, 2 * P.vp};
-        return logits_launch<TYPE == QA_BF16, kRows>(Operand{from, L.w_stride, 0, vocab}, Operand{ws + (own ? P.xr : P.xc), P.hc, 0, L.rows}, L.features, tiles, grad, stream, rows);
+        Fewer or_all = rows;
+        if (own) {
+          or_all.all = G.x;
+          or_all.all_ld = L.x_stride;
+        }
+        return logits_launch<TYPE == QA_BF16, kRows, kFewerOfB>(Operand{from, L.w_stride, 0, vocab}, Operand{ws + (own ? P.xr : P.xc), P.hc, 0, L.rows}, L.features, tiles, grad, stream, or_all);
       }
       return (int)QA_ERR_INVALID_ARG;              // not reached
     };
@@ -1010,18 +1031,18 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
                               TYPE == QA_F16 ? -1 : kOfW, first > 0, last && P.dx.splits == 1, list};
       // One part of c has 11 bits, which is little beside bfloat16's 8, but as much as binary16's own.
       constexpr Lies kC = TYPE == QA_BF16 ? kHiOfRows : kRowsOfParts;
-      if (const int rc = grad_product<kColumnsOf, kC>(wc, Operand{c, 2 * P.vp, 0, L.rows}, vocab, out, P.dx, rows, false, stream)) return rc;
+      if (const int rc = grad_product<kColumnsOf, kC, kFewerOfB>(wc, Operand{c, 2 * P.vp, 0, L.rows}, vocab, out, P.dx, dx_rows, stream)) return rc;
       if (last && P.dx.splits > 1)
-        if (const int rc = sum_launch<TYPE>((const float*)(ws + P.sums), P.dx.splits, L.rows, L.features, (ElemT<TYPE>*)G.dx, G.dx_stride, 0, stream, list, scales)) return rc;
+        if (const int rc = sum_launch<TYPE>((const float*)(ws + P.sums), dx_splits, L.rows, L.features, (ElemT<TYPE>*)G.dx, G.dx_stride, 0, stream, list, scales)) return rc;
     }
     if (G.dw) {
       float* const dw = G.dw + first * G.dw_stride;
       const ProductPlan plan = dw_plan(L, TYPE, vocab);
       float* const sums = plan.splits > 1 ? (float*)(ws + P.dw_sums) : nullptr;
       const GradOut<QA_F32> out{dw, sums, scales, G.dw_stride, vocab, L.features, TYPE == QA_F16 ? -1 : kOfX, !sums && G.accumulate, !sums, nullptr};
-      if (const int rc = grad_product<kColumnsOf, kColumnsOfParts>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, plan, rows, true, stream)) return rc;
+      if (const int rc = grad_product<kColumnsOf, kColumnsOfParts, kFewerOfK>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, plan, rows, stream)) return rc;
       if (sums)
-        if (const int rc = sum_launch<QA_F32>(sums, plan.splits, vocab, L.features, dw, G.dw_stride, G.accumulate, stream)) return rc;
+        if (const int rc = sum_launch<QA_F32>(sums, Splits{(int)plan.splits}, vocab, L.features, dw, G.dw_stride, G.accumulate, stream)) return rc;
     }
   }
   return QA_OK;

@@ -34,13 +34,25 @@ struct Operand {
   int64_t batch;                                   // elements between matrices
   int64_t n;                                       // how many i there are
 };
+// A product of which the device knows how many there are of B's, or of k; 0 counts as 1.
+enum HowMany { kAll, kFewerOfB, kFewerOfK };
+struct Fewer {
+  const int* n;
+  int most_splits;                                 // of B's fewer: more splits, up to so many, in their place; 0: as planned
+  const void* all;                                 // NULL, or where B is if there are all of them
+  int64_t all_ld;
+};
+// Splits of a product in tiles of `side` along B, of whose `all` n are left: as many tiles and no more sums than with all of them.
+__host__ __device__ constexpr unsigned splits_of_fewer(unsigned splits, unsigned most, unsigned side, unsigned all, unsigned n) {
+  const unsigned tiles = splits * ((all + side - 1) / side) / ((n + side - 1) / side), sums = splits * all / n, more = tiles < sums ? tiles : sums;
+  return more < most ? more : most;
+}
 struct ProductArgs {
   Operand a, b;
   int steps, split_steps;                          // of k, and of one split of them
   unsigned splits, tiles_m, tiles_n, tiles;        // tiles: of one matrix
   unsigned batch;
-  const int* fewer;                                // NULL, or how many there are of B's, or of k; 0 counts as 1
-  bool fewer_of_k;
+  Fewer fewer;
 };
 
 // Brings SIDE values of i and STEP of k to LDS, straight from memory, 16 bytes per lane.
@@ -393,19 +405,23 @@ __device__ __forceinline__ void tile_of(const ProductArgs& A, unsigned tile, uns
 }
 
 // A work-group per tile and split.
-template <class P, bool LOWER, class Epilogue>
+template <class P, bool LOWER, HowMany MANY, class Epilogue>
 __global__ __launch_bounds__(P::kGroup, P::kWavesPerSimd) void product_kernel(ProductArgs A, Epilogue out) {
   __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
-  if (A.fewer) {
-    const int n = max(1, *A.fewer);
-    if (A.fewer_of_k) {
+  if constexpr (MANY != kAll) {
+    const int n = max(1, *A.fewer.n);
+    if constexpr (MANY == kFewerOfK) {
       A.steps = (n + P::kStep - 1) / P::kStep;
-      A.split_steps = (A.steps + (int)A.splits - 1) / (int)A.splits;
     } else {
+      const bool all = A.fewer.all && n == A.b.n;
+      A.b.p = all ? A.fewer.all : A.b.p;
+      A.b.ld = all ? A.fewer.all_ld : A.b.ld;
+      A.splits = A.fewer.most_splits ? splits_of_fewer(A.splits, A.fewer.most_splits, P::kN, (unsigned)A.b.n, n) : A.splits;
       A.b.n = n;
       A.tiles_n = (unsigned)(n + P::kN - 1) / P::kN;
       A.tiles = A.tiles_m * A.tiles_n;
     }
+    A.split_steps = (A.steps + (int)A.splits - 1) / (int)A.splits;
     if (blockIdx.x >= A.tiles * A.batch * A.splits) return;
   }
   const unsigned tile = on_its_die(A.tiles * A.batch * A.splits), which = tile / A.tiles, matrix = which / A.splits;
@@ -418,14 +434,14 @@ __global__ __launch_bounds__(P::kGroup, P::kWavesPerSimd) void product_kernel(Pr
 }
 
 // Launches tiles of the given form over all of A and B; k: how many there are, zeros up to a whole step.
-template <class P, bool LOWER = false, class Epilogue>
+template <class P, bool LOWER = false, HowMany MANY = kAll, class Epilogue>
 int product_launch(const Operand& a, const Operand& b, int64_t k, const Epilogue& out, unsigned batch, hipStream_t stream, int64_t splits = 1,
-                   const int* fewer = nullptr, bool fewer_of_k = false) {
-  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), 0, 0, (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN), 0, batch, fewer, fewer_of_k};
+                   const Fewer& fewer = {}) {
+  ProductArgs A = {a, b, (int)ceil_div(k, P::kStep), 0, 0, (unsigned)ceil_div(a.n, P::kM), (unsigned)ceil_div(b.n, P::kN), 0, batch, fewer};
   A.split_steps = (int)ceil_div(A.steps, splits);
   A.splits = (unsigned)ceil_div(A.steps, A.split_steps);       // none is empty
   A.tiles = LOWER ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n;
-  product_kernel<P, LOWER><<<A.tiles * batch * A.splits, P::kGroup, 0, stream>>>(A, out);
+  product_kernel<P, LOWER, MANY><<<A.tiles * batch * A.splits, P::kGroup, 0, stream>>>(A, out);
   return launch_status();
 }
 template <bool BF16, Lies LA, Lies LB> using Product256 = Product<BF16, LA, LB, 2, 2, 4, 4>;

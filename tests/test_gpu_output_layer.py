@@ -370,7 +370,7 @@ def test_dw_of_far_rows():
 
 
 @pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
-@pytest.mark.parametrize("T,V,H", [(700, 300, 64), (700, 300, 50), (5000, 200, 32)])
+@pytest.mark.parametrize("T,V,H", [(700, 300, 64), (700, 300, 50), (5000, 200, 32), (700, 20011, 40)])
 @pytest.mark.parametrize("kept", [(), (699,), (0, 1, 255, 256, 257, 511, 512), range(100, 116), range(37, 163), range(300, 700)])
 def test_few_of_many_rows_count(t, T, V, H, kept):
     """The others' dx is 0, whatever x holds there.  None, one, up to a whole step of 16 and more, within one share of the rows and in several."""

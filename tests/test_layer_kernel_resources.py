@@ -74,7 +74,8 @@ def test_loops_of_products_wait_for_what_they_count(compiled, source, least):
         loops = []
         for i, line in enumerate(lines):
             to = re.search(r"\bs_c?branch\w* (\.LBB\d+_\d+)", line)
-            if to and labels.get(to.group(1), i + 1) <= i:
+            # (a block may also stand behind the function's end and branch back)
+            if to and labels.get(to.group(1), i + 1) <= i and "Loop Header" in lines[labels[to.group(1)]]:
                 loop = "\n".join(lines[labels[to.group(1)]:i + 1])
                 if "v_mfma" in loop:
                     loops.append(loop)
