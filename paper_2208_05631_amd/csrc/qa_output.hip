@@ -4,6 +4,9 @@
 // many logits of one row: a tile's maximum and sums are formed in registers, and a row's numbers are joined from one triple per
 // chunk of the vocabulary.  The backward pass multiplies the logits again, a piece of the vocabulary at a time, turns them into
 // c, the gradient of the logits, which is written once, as rows of binary16 parts, and multiplies that from both sides: dx = c w, dw = c^T x.
+//
+// What bounds it: the matrix cores (8192 rows, 32768 x 4096 bfloat16: 1.75 to 1.8 ms scored, of which the softmax is a tenth, and 7.4 to 7.7 ms the gradient, four
+// times the product's operations, as c goes to dw in two parts), and for few rows w's way from memory (one row, 128000 x 4096: 183 us, 5.7 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -58,6 +61,7 @@ __device__ __forceinline__ bool counts(const Row& r) { return r.a != 0.0f || r.e
 // The gradient's operands are scaled by powers of two that follow from their largest magnitudes.  Work-groups leave theirs (bits) side by
 // side, the next kernel's find the largest of them, and its first one leaves that for the kernels behind it: no atomics, nothing to clear.
 enum { kOfC, kOfX, kOfW };
+// (One word for the maximum: 100 us for 8192 atomics.)
 constexpr int kMostBlocks = 1024;
 struct Scales {
   uint32_t most[3];
@@ -276,6 +280,9 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
 }
 
 // ---- scoring ------------------------------------------------------------------------------------------------------------------
+//
+// w's rows along the tile's height: sixteen logits of a matrix instruction in a lane are of one row of x, so that maximum and sums need one exchange
+// between the halves of a wave, and a chunk (a wave's logits of a row) leaves three numbers, 12 bytes for 64 or 128 logits.
 
 // A lane's logits of block column j, four at a time: each(the first one's place behind v0, block row, quarter, logits).
 template <bool SCALED, class P, class Each>
@@ -573,6 +580,10 @@ __global__ __launch_bounds__(THREADS) void output_join_kernel(ScoreArgs A, int64
 }
 
 // ---- the gradient of the logits -------------------------------------------------------------------------------------------
+//
+// Rows that do not count are left out before anything is multiplied: the device finds which they are, x's others are gathered, and
+// the products, launched for all rows, end early or have more splits where fewer are left (4096 rows of which half count, 50021 x 1024 binary16: 1.36 ms, 2.11
+// with all of them multiplied).
 
 // c of a piece of the vocabulary, scaled, in rows of parts, for the rows that count: zeros behind the piece, and in rows up to a whole step.
 // SCALED: of operands scaled by one power of two each.
