@@ -152,7 +152,7 @@ struct Reader {
 //
 // Four waves of 128 x 128 each on a tile of 256 x 256 read the least of LDS for a matrix instruction; eight of 128 x 64 read half as much again and are slower.
 // Large products run at 1.1 to 1.2 PFLOP/s (bfloat16, 8192 x 4096 x 32768) and, in parts, three matrix instructions for what two bring, at 1.31 to
-// 1.35 (8192 x 8192 x 2048): the card's power bounds both, at 1.75 to 1.8 GHz with the matrix cores busy in 59 to 72 % of the cycles.  Small ones are
+// 1.35 (8192 x 8192 x 2048): the card's power bounds both, at 1.4 to 1.8 GHz with the matrix cores busy in 54 to 72 % of the cycles.  Small ones are
 // bound by a tile's first loads and its results, beside 0.07 to 0.4 us per step.
 template <bool BF16, Lies LA, Lies LB, int WM, int WN, int FM, int FN, int SHARE = 1, bool APART = false>
 struct Product {

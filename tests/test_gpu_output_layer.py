@@ -317,6 +317,37 @@ def test_captured_and_replayed_among_eager_calls(t, T, V, H):
             assert torch.equal(b[k], want[k]), (i, k)
 
 
+@pytest.mark.parametrize("t,T,V,H", [("bf16", 600, 30000, 64), ("f16", 300, 2500, 128), ("f32", 270, 9000, 50)])
+def test_replayed_with_other_rows_that_count(t, T, V, H):
+    """A graph that was captured where all rows count, replayed where some do, one or none, and where all do again; and each twice, bit for bit."""
+    gen = gen_of("replayed rows", t)
+    layer, _, xd, _, wd, y = layer_of(gen, T, V, H, t)
+    y, a, b = y.to(torch.int32).to(DEV), torch.ones(T, device=DEV), buffers(T, V, H, t)
+    ws = room(layer, qa.QA_OP_LOGPROB_GRAD, t)
+    qa.qa_output_logprob(layer, code_of(t), xd, wd, y, b["lp"], b["h"], b["st"], room(layer, qa.QA_OP_LOGPROB, t))
+    call = lambda to: qa.qa_output_logprob_grad(layer, code_of(t), xd, wd, y, b["st"], None, a, None, to["dx"], H, to["dw"], H, 0, ws)  # noqa: E731
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        call(b)
+    for kept in (range(0), range(7, 8), range(0, T, 3), range(T // 2, T), range(T), range(100, 130)):
+        weights = torch.zeros(T)
+        weights[list(kept)] = torch.randn(len(kept), generator=gen)
+        for _ in range(2):
+            a.copy_(weights)
+            want = buffers(T, V, H, t)
+            call(want)
+            torch.cuda.synchronize()
+            b["dx"].fill_(7.0), b["dw"].fill_(7.0)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(b["dx"], want["dx"]) and torch.equal(b["dw"], want["dw"])
+            skip = weights == 0
+            assert bool((b["dx"].cpu()[skip] == 0).all())
+            if not len(kept):
+                assert bool((b["dw"] == 0).all())
+
+
 def test_on_another_stream():
     gen = gen_of("stream")
     T, V, H, t = 130, 4000, 64, "bf16"
