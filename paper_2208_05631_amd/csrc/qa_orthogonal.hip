@@ -11,7 +11,7 @@
 // B's diagonal, where it would swallow the sums' last bits: half of the error.
 //
 // A and B are symmetric: tiles on and below the diagonal, written twice.  Large matrices are bound by the matrix cores (4096 x 4096, five steps: 3.6 to 3.8 ms, fifteen
-// products of 208 to 340 us, 1.31 to 1.35 PFLOP/s), small ones by the launches that wait for each other (64 of 128 x 1024: 212 us in seventeen), but for those that fit LDS
+// products of 208 to 340 us, 1.31 to 1.35 PFLOP/s), small ones by the launches that wait for each other (64 of 128 x 1024: 204 to 245 us in seventeen), but for those that fit LDS
 // (96 x 96: 29 us, under 2 for a product).
 #include <algorithm>
 
