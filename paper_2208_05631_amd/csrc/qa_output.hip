@@ -587,6 +587,8 @@ __global__ __launch_bounds__(THREADS) void output_join_kernel(ScoreArgs A, int64
 
 // c of a piece of the vocabulary, scaled, in rows of parts, for the rows that count: zeros behind the piece, and in rows up to a whole step.
 // SCALED: of operands scaled by one power of two each.
+// log p is never above 0, though statistics and logits of 10^8, multiplied in another order, are tens apart: c stays within its bound, and
+// binary16 with it (NaN stays NaN).
 template <bool SCALED, bool ENTROPY>
 struct LogitsGradOut {
   int64_t vocab;                                   // of this piece
@@ -624,7 +626,7 @@ struct LogitsGradOut {
 #pragma unroll
       for (int k = 0; k < kVec; ++k) {
         if (SCALED) z[k] = ldexpf(z[k], z_exp);
-        const float lp = __builtin_fmaf(z[k] - m[j], kLog2e, -log_sum[j]), q = __builtin_amdgcn_exp2f(lp);      // in powers of two
+        const float lp = __builtin_elementwise_minimum(__builtin_fmaf(z[k] - m[j], kLog2e, -log_sum[j]), 0.0f), q = __builtin_amdgcn_exp2f(lp);  // in powers of two
         g[k] = ENTROPY ? -q * (a[j] + e[j] * (fmaxf(lp, kFar) + h[j])) : -q * a[j];
       }
       if (__any((unsigned)(here[j] - v) < kVec)) {           // few eights have a target
