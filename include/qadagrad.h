@@ -612,10 +612,11 @@ int qa_output_logprob(const qa_output_layer* layer, int type, const void* x, con
  * with the logits multiplied again, a piece of the vocabulary at a time.  stats and entropy as qa_output_logprob wrote them
  * (entropy and g_entropy NULL together).  A row without target has the entropy's part alone.  A row whose g_logprob (or
  * target) and g_entropy are both none or 0 gets dx = 0 and adds nothing to dw, whatever x holds there: padding.
- * Numbers are multiplied as binary16 with one power of two per matrix as scale: c in two parts, but in one for dx of
- * bfloat16 (a rounding by 2^-11, an eighth of dx's own), binary32 x and w in two, bfloat16 ones exactly, but for magnitudes below 2^-32 of
- * their matrix's largest, which lose bits below 2^-39 of it.  The logits are multiplied from x and w as they are where
- * qa_output_logprob would read more than 64 rows where they lie, and from these numbers elsewhere.  dx_or_null and dw_or_null may be NULL (not both); dx does not overlap x.
+ * Numbers are multiplied as binary16 times powers of two: c in two parts, but in one for dx of bfloat16 (a rounding by 2^-11, an eighth of
+ * dx's own), binary32 x and w in two (22 bits and a sign), 16-bit ones exactly; but nothing is held below 2^-39 of the largest of its kind.  With
+ * |g_t| = |g_logprob_t| + 18 |g_entropy_t| that is for dx 2^-39 |g_t| of c, the row's own, and 2^-39 of the largest magnitude in w, and for dw
+ * 2^-39 |g_t| of c and 2^-39 of the largest |g_t| |x_t| over all rows of a product.  The logits are multiplied from x and w as they are where
+ * qa_output_logprob would read more than 64 rows where they lie, and elsewhere from numbers to 2^-39 of the largest in a row of x, and in w.  dx_or_null and dw_or_null may be NULL (not both); dx does not overlap x.
  * rows == 0 writes dw = 0 (kept, with accumulate). */
 int qa_output_logprob_grad(const qa_output_layer* layer, int type, const void* x, const void* w,
                            const int32_t* target_or_null, const float* stats, const float* entropy_or_null,

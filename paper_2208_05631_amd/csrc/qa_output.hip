@@ -58,21 +58,38 @@ __device__ __forceinline__ Row row_of(const RowArgs& A, int64_t t) {
 }
 __device__ __forceinline__ bool counts(const Row& r) { return r.a != 0.0f || r.e != 0.0f; }
 
-// The gradient's operands are scaled by powers of two that follow from their largest magnitudes.  Work-groups leave theirs (bits) side by
-// side, the next kernel's find the largest of them, and its first one leaves that for the kernels behind it: no atomics, nothing to clear.
-enum { kOfC, kOfX, kOfW };
-// (One word for the maximum: 100 us for 8192 atomics.)
+// The gradient's operands are scaled by powers of two, so that binary16 holds them to 2^-39 of a largest magnitude: c of its row's bound,
+// r 2^c_exp, and x for the logits of its row's largest element.  A row's dx is as exact as if it were alone, then, whatever the others weigh.  dw is a sum
+// over rows, whose c are so scaled: x is multiplied there by 2^(x_exp - c_exp) of its row, with one x_exp by which the largest |c| |x| is
+// 2^29.  w has one scale for dx, where it is summed over, and for the logits.
+//
+// Work-groups leave their largest magnitudes side by side, the next kernel's find the largest of them, and its first one leaves
+// the exponents for the kernels behind it: no atomics, nothing to clear.  (One word for the maximum: 100 us for 8192 atomics.)
+enum { kOfRows, kOfX, kOfW };
 constexpr int kMostBlocks = 1024;
 struct Scales {
-  uint32_t most[3];
+  int x_exp, w_exp;
   int rows;                                        // that count
-  uint32_t found[3][kMostBlocks];
+  uint32_t found[3][kMostBlocks];                  // of x: key_of() rows' c and x; of w: bits; the first is unused
   int counted[kMostBlocks];                        // of each share of the rows
 };
-__device__ __forceinline__ uint32_t most_in_block(uint32_t most) {
-  __shared__ uint32_t waves[kWaves];
+// The largest |c| that a row can have: p <= 1, p |log p| <= 1 / e, and an entropy of at most log 2^24 < 17.  (The bound itself may leave binary32.)
+__device__ __forceinline__ int exponent_of_c(const Row& r) {
+  const uint32_t most = as_u32(fabsf(r.a) + 18.0f * fabsf(r.e));
+  return exponent_for(most) - (most >= 0x7F800000u ? 5 : 0);
+}
+// Of a row's largest |c| |x|: an exponent as a number that is not 0, larger for larger ones; and what x_exp follows from the largest.
+constexpr int kKeyOfOne = 1024 + 127;
+__device__ __forceinline__ uint32_t key_of(uint32_t most_x, int c_exp) { return most_x == 0 ? 0 : 1024 + max(most_x >> 23, 1u) - c_exp; }
+__device__ __forceinline__ int x_exp_for(uint32_t key) { return key == 0 ? 0 : 14 - ((int)key - kKeyOfOne); }
+__device__ __forceinline__ uint32_t most_in_wave(uint32_t most) {
 #pragma unroll
   for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
+  return most;
+}
+__device__ __forceinline__ uint32_t most_in_block(uint32_t most) {
+  __shared__ uint32_t waves[kWaves];
+  most = most_in_wave(most);
   __syncthreads();
   if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = most;
   __syncthreads();
@@ -86,8 +103,8 @@ struct MostArgs {
   int64_t x_stride, w_stride;
   Scales* scales;
   int* place;                                      // of a row among those of its share that count; -1: it does not
-  int64_t share;                                   // of the rows, a work-group for c
-  int blocks[3];                                   // work-groups for c, for x and for w; 0: not wanted
+  int64_t share;                                   // of the rows, a work-group
+  int blocks[3];                                   // work-groups for which rows count, for x and for w; 0: not wanted
 };
 template <int TYPE>
 __device__ __forceinline__ uint32_t most_of_row(const ElemT<TYPE>* p, int64_t cols) {
@@ -113,14 +130,13 @@ __device__ __forceinline__ uint32_t most_of_row(const ElemT<TYPE>* p, int64_t co
   }
   return most;
 }
-// The largest |c| that a row can have: p <= 1, p |log p| <= 1 / e, and an entropy of at most log 2^24 < 17; the largest finite magnitudes of
-// rows of x that count, and of w.  And which rows count: the others take no part in the products.
+// The largest finite magnitudes of rows of x that count, and of w.  And which rows count: the others take no part in the products.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void output_most_kernel(MostArgs A) {
   int block = blockIdx.x, which = 0;
   while (block >= A.blocks[which]) block -= A.blocks[which++];
   uint32_t most = 0;
-  if (which == kOfC) {
+  if (which == kOfRows) {
     __shared__ int waves[kWaves];
     const int64_t first = block * A.share, end = min(A.rows, first + A.share);
     int counted = 0;
@@ -128,10 +144,7 @@ __global__ __launch_bounds__(kThreads) void output_most_kernel(MostArgs A) {
       const int64_t t = t0 + threadIdx.x;
       bool here = false;
       if (t < end) {
-        const Row r = row_of(A.R, t);
-        const uint32_t c = as_u32(fabsf(r.a) + 18.0f * fabsf(r.e));
-        if (c < 0x7F800000u) most = max(most, c);
-        here = counts(r);
+        here = counts(row_of(A.R, t));
       }
       const uint64_t all = __ballot(here);
       if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = __popcll(all);
@@ -147,18 +160,23 @@ __global__ __launch_bounds__(kThreads) void output_most_kernel(MostArgs A) {
     }
     if (threadIdx.x == 0) A.scales->counted[block] = counted;
   } else {
-    const int64_t rows = which == kOfX ? A.rows : A.vocab, stride = which == kOfX ? A.x_stride : A.w_stride;
-    const ElemT<TYPE>* const p = (const ElemT<TYPE>*)(which == kOfX ? A.x : A.w);
-    for (int64_t row = (int64_t)block * kWaves + threadIdx.x / kWave; row < rows; row += (int64_t)A.blocks[which] * kWaves)
-      if (which == kOfW || counts(row_of(A.R, row))) most = max(most, most_of_row<TYPE>(p + row * stride, A.features));
+    const int64_t first = (int64_t)block * kWaves + threadIdx.x / kWave, next = (int64_t)A.blocks[which] * kWaves;
+    if (which == kOfW) {
+      for (int64_t row = first; row < A.vocab; row += next) most = max(most, most_of_row<TYPE>((const ElemT<TYPE>*)A.w + row * A.w_stride, A.features));
+    } else {
+      for (int64_t row = first; row < A.rows; row += next) {
+        const Row r = row_of(A.R, row);
+        if (counts(r)) most = max(most, key_of(most_in_wave(most_of_row<TYPE>((const ElemT<TYPE>*)A.x + row * A.x_stride, A.features)), exponent_of_c(r)));
+      }
+    }
   }
   most = most_in_block(most);
   if (threadIdx.x == 0) A.scales->found[which][block] = most;
 }
 
-// Rows copied, a wave per row: 16-bit elements as they are, or binary16 (binary32 elements: in two parts) times a power of two per row
-// or per matrix.
-enum Copies { kAsTheyAre, kOwnScale, kOneScale };
+// Rows copied, a wave per row: 16-bit elements as they are, or binary16 (binary32 elements: in two parts) times a power of two: of the row's largest
+// magnitude, one for all of w, or of x beside c.
+enum Copies { kAsTheyAre, kOwnScale, kScaleOfW, kScaleBesideC };
 struct Copy {
   int how;
   const void* from;
@@ -166,7 +184,6 @@ struct Copy {
   void* to;
   int64_t ld, to_rows;                             // zeros up to ld / parts columns, and in rows from `rows` on
   int* exps;                                       // kOwnScale: written
-  int which;                                       // kOneScale
   bool gather;                                     // the rows that count, one behind the other, and zeros up to a whole step of the products
   bool unless_all;                                 // count
   int blocks;
@@ -175,10 +192,12 @@ constexpr int kCopies = 4;
 struct CopyArgs {
   Copy copy[kCopies];
   Scales* scales;
-  int found[3];                                    // how many there are; not 0: the largest are found first
+  bool first;                                      // the largest magnitudes are found, and their exponents left
+  int found[3];                                    // how many there are of them
+  RowArgs R;
   const int* place;                                // of rows that are gathered, in shares; the first copy gathers, and writes which there are
   int64_t share;
-  int* list;
+  int *list, *c_exp;                               // c_exp: of the rows in the list
   void* zero;                                      // NULL, or zeros go to its rows that do not count
   int64_t zero_stride;
 };
@@ -190,11 +209,11 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
     for (int b = threadIdx.x; b < A.found[which]; b += kThreads) most = max(most, A.scales->found[which][b]);
     return most_in_block(most);
   };
-  if (blockIdx.x == 0 && A.found[kOfC]) {
-#pragma unroll
-    for (int w = 0; w < 3; ++w) {
-      const uint32_t most = find(w);
-      if (threadIdx.x == 0) A.scales->most[w] = most;
+  if (blockIdx.x == 0 && A.first) {
+    const uint32_t x = find(kOfX), w = find(kOfW);
+    if (threadIdx.x == 0) {
+      A.scales->x_exp = x_exp_for(x);
+      A.scales->w_exp = exponent_for(w);
     }
   }
   int block = blockIdx.x, at = 0;
@@ -202,23 +221,22 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
   if (at == kCopies) return;
   const Copy& C = A.copy[at];
   const int lane = threadIdx.x % kWave;
-  int exp = 0;
-  if (C.how == kOneScale && TYPE != QA_F16) exp = exponent_for(A.found[kOfC] ? find(C.which) : A.scales->most[C.which]);
+  int exp = 0, x_exp = 0;
+  if (C.how == kScaleOfW && TYPE != QA_F16) exp = A.first ? exponent_for(find(kOfW)) : A.scales->w_exp;
+  if (C.how == kScaleBesideC) x_exp = x_exp_for(find(kOfX));
   const auto copy = [&](int64_t from, int64_t to, int64_t cols) {
     const ElemT<TYPE>* p = (const ElemT<TYPE>*)C.from + from * C.stride;
     _Float16* q = (_Float16*)C.to + to * C.ld;
-    if (TYPE == QA_F32 && C.how == kOwnScale) {
-      uint32_t most = cols ? most_of_row<TYPE>(p, cols) : 0;
-#pragma unroll
-      for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
-      exp = exponent_for(most);
+    if (TYPE != QA_F16 && C.how == kOwnScale) {
+      exp = exponent_for(most_in_wave(cols ? most_of_row<TYPE>(p, cols) : 0));
       if (lane == 0) C.exps[to] = exp;
     }
+    if (C.how == kScaleBesideC && cols) exp = x_exp - exponent_of_c(row_of(A.R, from));
     for (int64_t c = lane * kVec; c < C.ld / kParts; c += kWave * kVec) {
       const int n = (int)max((int64_t)0, min((int64_t)kVec, cols - c));
       bool copied = false;
       if constexpr (TYPE != QA_F32) {
-        copied = TYPE == QA_F16 || C.how == kAsTheyAre;
+        copied = C.how == kAsTheyAre || (TYPE == QA_F16 && C.how != kScaleBesideC);
         if (copied) *reinterpret_cast<u32x4*>(q + c) = n ? load_raw<TYPE>(p + c, n).a : u32x4{};
       }
       if (!copied) {
@@ -243,7 +261,7 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
   for (int e = 0; e < kEach; ++e) {
     const int b = threadIdx.x * kEach + e;
     mine[e] = sum;
-    sum += b < A.found[kOfC] ? A.scales->counted[b] : 0;
+    sum += b < A.found[kOfRows] ? A.scales->counted[b] : 0;
   }
   int upto = sum;
 #pragma unroll
@@ -268,7 +286,10 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
     if (place >= 0) {
       const int64_t to = before[row / A.share] + place;
       if (!(C.unless_all && rows == C.rows)) copy(row, to, C.cols);
-      if (at == 0 && lane == 0) A.list[to] = (int)row;
+      if (at == 0 && lane == 0) {
+        A.list[to] = (int)row;
+        A.c_exp[to] = exponent_of_c(row_of(A.R, row));
+      }
     } else if (at == 0 && A.zero) {
       constexpr float zeros[kVec] = {};
       for (int64_t c = lane * kVec; c < C.cols; c += kWave * kVec)
@@ -586,30 +607,32 @@ __global__ __launch_bounds__(THREADS) void output_join_kernel(ScoreArgs A, int64
 // with all of them multiplied).
 
 // c of a piece of the vocabulary, scaled, in rows of parts, for the rows that count: zeros behind the piece, and in rows up to a whole step.
-// SCALED: of operands scaled by one power of two each.
+// SCALED: of operands scaled by a power of two per row of x, and one of w.
 // log p is never above 0, though statistics and logits of 10^8, multiplied in another order, are tens apart: c stays within its bound, and
 // binary16 with it (NaN stays NaN).
 template <bool SCALED, bool ENTROPY>
 struct LogitsGradOut {
   int64_t vocab;                                   // of this piece
   RowArgs R;
-  const int* list;                                 // rows that count
+  const int *list, *x_exp;                         // rows that count; SCALED: of each of them
   int64_t first;                                   // of the piece
   const Scales* scales;
   _Float16* c;
   int64_t ld;
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0, char* lds) const {
-    const int exp = exponent_for(scales->most[kOfC]), lane = threadIdx.x % kWave;
+    const int lane = threadIdx.x % kWave, w_exp = SCALED ? scales->w_exp : 0;
     constexpr int FN = (int)(sizeof p.acc[0] / sizeof p.acc[0][0]);
     float m[FN], log_sum[FN], a[FN], e[FN], h[FN];
-    int here[FN];
-    const int z_exp = SCALED ? -(exponent_for(scales->most[kOfX]) + exponent_for(scales->most[kOfW])) : 0;
+    int here[FN], z_exp[FN];
     bool none[FN];
     const int64_t rows = scales->rows, to_rows = whole(max((int64_t)1, rows), kPartsStep);
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t t = t0 + 32 * j + lane % 32;
-      const Row r = row_of(R, rows ? list[min(t, rows - 1)] : 0);
+      const int64_t at_most = max((int64_t)0, min(t, rows - 1));
+      const Row r = row_of(R, rows ? list[at_most] : 0);
+      const int exp = exponent_of_c(r);
+      z_exp[j] = SCALED ? -(x_exp[at_most] + w_exp) : 0;
       m[j] = r.m;
       log_sum[j] = r.log_sum * kLog2e;
       a[j] = ldexpf(r.a, exp);
@@ -625,7 +648,7 @@ struct LogitsGradOut {
       float g[kVec];
 #pragma unroll
       for (int k = 0; k < kVec; ++k) {
-        if (SCALED) z[k] = ldexpf(z[k], z_exp);
+        if (SCALED) z[k] = ldexpf(z[k], z_exp[j]);
         const float lp = __builtin_elementwise_minimum(__builtin_fmaf(z[k] - m[j], kLog2e, -log_sum[j]), 0.0f), q = __builtin_amdgcn_exp2f(lp);  // in powers of two
         g[k] = ENTROPY ? -q * (a[j] + e[j] * (fmaxf(lp, kFar) + h[j])) : -q * a[j];
       }
@@ -650,17 +673,17 @@ struct GradOut {
   float* sums;                                     // [split][rows][cols]; NULL: none before this piece, and this is the last
   const Scales* scales;
   int64_t stride, rows, cols;
-  int which;                                       // the scale of the other operand, -1: none
   bool add, last;                                  // to what is in sums (or, of binary32, in out); the last piece writes out
-  const int* list;                                 // NULL, or the product's rows are those that count, and where they go
+  const int *list, *c_exp;                         // NULL, or the product's rows are those that count, where they go, and their c's exponents
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
-    const int exp = -(exponent_for(scales->most[kOfC]) + (which < 0 ? 0 : exponent_for(scales->most[which])));
+    const int of_all = -(list ? scales->w_exp : scales->x_exp);
     const int64_t all = list ? scales->rows : rows;
     float* const its_sums = sums + p.split * all * cols;
     const bool writes = last || !sums;
     p.for_runs(m0, n0, lds, [&](int64_t col, int64_t row, float (&v)[kVec]) {
       if (row >= all || col >= cols) return;
       const int n = (int)min((int64_t)kVec, cols - col);
+      const int exp = of_all - (list ? c_exp[row] : 0);
       ElemT<TYPE>* const at = out + (list && writes ? list[row] : row) * stride + col;
       float* const s = its_sums + row * cols + col;
       float before[kVec] = {};
@@ -781,7 +804,7 @@ struct Plan {
   size_t x, w, x_exp, w_exp;                       // copies and exponents
   size_t m, s, sw, given;                          // scoring
   int64_t chunks, each;                            // each: of the vocabulary per work-group, where w is streamed
-  size_t scales, place, list, xr, xc, wc, c, sums; // gradient: rows of x for the logits, where xc does not serve; x and w as the products with c take them
+  size_t scales, place, list, c_exp, xr, xc, wc, c, sums;       // gradient: rows of x for the logits; x and w as the products with c take them
   size_t dw_sums;
   int64_t hc, tp, vp;
   ProductPlan dx;
@@ -823,7 +846,7 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.rows = std::min(L.rows, std::max<int64_t>(256, 4 * kPieceBytes / (12 * P.chunks) / 256 * 256));
   } else {
     P.tp = whole(L.rows, kPartsStep);
-    // Where x or w have to be copied for the logits, what the products with c take serves for both.
+    // Where x or w have to be copied for the logits, w as dx takes it serves for both.
     P.copies = P.copy_x || P.copy_w;
     P.copy_x = P.copy_w = false;
     P.hc = whole(L.features, P.copies ? kWholeStep : 8);
@@ -833,7 +856,9 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.scales = room.take(sizeof(Scales));
     P.place = room.take(4 * L.rows);
     P.list = room.take(4 * L.rows);
-    P.xr = room.take(!P.copies && type == QA_BF16 ? 2 * P.tp * P.hc : 0);
+    P.c_exp = room.take(4 * P.tp);
+    P.x_exp = room.take(P.copies && type != QA_F16 ? 4 * P.tp : 0);
+    P.xr = room.take(2 * P.parts * P.tp * P.hc);
     P.xc = room.take(2 * P.parts * P.tp * P.hc);
     P.wc = room.take(2 * P.parts * P.vp * P.hc);
     P.c = room.take(2 * 2 * P.tp * P.vp);
@@ -853,7 +878,7 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.sw = room.take(4 * P.chunks * P.rows);
     P.given = room.take(4 * P.rows);
   }
-  P.x_exp = room.take(P.copy_x && type == QA_F32 ? 4 * P.rows : 0);
+  if (op == QA_OP_LOGPROB) P.x_exp = room.take(P.copy_x && type == QA_F32 ? 4 * P.rows : 0);
   P.w_exp = room.take(P.copy_w && type == QA_F32 ? 4 * P.piece : 0);
   P.x = room.take(P.copy_x ? 2 * P.parts * P.rows * P.hp : 0);
   P.w = room.take(P.copy_w ? 2 * P.parts * P.piece * P.hp : 0);
@@ -873,13 +898,13 @@ size_t bytes_of(const qa_output_layer& L, int op, int type) {
 struct CopyList {
   CopyArgs A = {};
   int n = 0, blocks = 0;
-  void add(int how, const void* from, int64_t stride, int64_t rows, int64_t cols, void* to, int64_t ld, int64_t to_rows, int* exps, int which, bool gather, bool unless_all = false) {
+  void add(int how, const void* from, int64_t stride, int64_t rows, int64_t cols, void* to, int64_t ld, int64_t to_rows, int* exps, bool gather, bool unless_all = false) {
     Copy& C = A.copy[n++];
-    C = {how, from, stride, rows, cols, to, ld, to_rows, exps, which, gather, unless_all, (int)std::min<int64_t>(ceil_div(to_rows, kWaves), 1 << 14)};
+    C = {how, from, stride, rows, cols, to, ld, to_rows, exps, gather, unless_all, (int)std::min<int64_t>(ceil_div(to_rows, kWaves), 1 << 14)};
     blocks += C.blocks;
   }
   template <int TYPE> int launch(hipStream_t stream) {
-    if (A.found[kOfC] == 0 && n == 0) return QA_OK;
+    if (!A.first && n == 0) return QA_OK;
     output_copy_kernel<TYPE><<<(unsigned)std::max(blocks, 1), kThreads, 0, stream>>>(A);
     *this = CopyList{{.scales = A.scales}};
     return launch_status();
@@ -889,7 +914,7 @@ struct CopyList {
 Operand logits_operand(CopyList& copies, int type, const void* from, int64_t stride, int64_t rows, const qa_output_layer& L, const Plan& P, bool copy, char* to,
                        int* exps) {
   if (!copy) return {from, stride, 0, rows};
-  copies.add(type == QA_F32 ? kOwnScale : kAsTheyAre, from, stride, rows, L.features, to, P.parts * P.hp, rows, exps, 0, false);
+  copies.add(type == QA_F32 ? kOwnScale : kAsTheyAre, from, stride, rows, L.features, to, P.parts * P.hp, rows, exps, false);
   return {to, P.parts * P.hp, 0, rows};
 }
 // Logits of a piece of the vocabulary: w's rows by x's.
@@ -982,26 +1007,29 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
   const int64_t share = whole(ceil_div(L.rows, kMostBlocks), kThreads);
   int* const place = (int*)(ws + P.place);
   int* const list = (int*)(ws + P.list);
+  int* const c_exp = (int*)(ws + P.c_exp);
+  int* const x_exp = (int*)(ws + P.x_exp);
   const Fewer rows = {.n = &scales->rows};
   const MostArgs most = {G.rows, L.rows, L.vocab, L.features, G.x, G.w, L.x_stride, L.w_stride, scales, place, share,
-                         {(int)ceil_div(L.rows, share), blocks(TYPE != QA_F16 && (G.dw || P.copies), L.rows, kWaves),
-                          blocks(TYPE != QA_F16 && (G.dx || P.copies), L.vocab, kWaves)}};
+                         {(int)ceil_div(L.rows, share), blocks(G.dw, L.rows, kWaves), blocks(TYPE != QA_F16 && (G.dx || P.copies), L.vocab, kWaves)}};
   output_most_kernel<TYPE><<<(unsigned)(most.blocks[0] + most.blocks[1] + most.blocks[2]), kThreads, 0, stream>>>(most);
   if (const int rc = launch_status()) return rc;
 
   const int64_t copied = P.parts * P.hc;
   CopyList copies;
   copies.A.scales = scales;
+  copies.A.first = true;
   for (int i = 0; i < 3; ++i) copies.A.found[i] = most.blocks[i];
+  copies.A.R = G.rows;
   copies.A.place = place;
   copies.A.share = share;
   copies.A.list = list;
+  copies.A.c_exp = c_exp;
   copies.A.zero = G.dx;
   copies.A.zero_stride = G.dx_stride;
-  // bfloat16's own for the logits; the products with c take binary16.
-  const bool own = TYPE == QA_BF16 && !P.copies;
-  if (own) copies.add(kAsTheyAre, G.x, L.x_stride, L.rows, L.features, ws + P.xr, P.hc, L.rows, nullptr, 0, true, true);
-  if (G.dw || !own) copies.add(kOneScale, G.x, L.x_stride, L.rows, L.features, ws + P.xc, copied, L.rows, nullptr, kOfX, true);
+  // For the logits, and beside c.
+  copies.add(TYPE == QA_F16 || !P.copies ? kAsTheyAre : kOwnScale, G.x, L.x_stride, L.rows, L.features, ws + P.xr, copied, L.rows, x_exp, true, !P.copies);
+  if (G.dw) copies.add(kScaleBesideC, G.x, L.x_stride, L.rows, L.features, ws + P.xc, copied, L.rows, nullptr, true);
   // Where few rows count, dx has more splits instead of tiles, in the same room.
   Fewer dx_rows = rows;
   const int64_t dx_side = P.dx.tiles == kTiles256 ? 256 : 128;
@@ -1015,7 +1043,7 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     Operand wc = {from, L.w_stride, 0, L.features};
     if (P.copies || (G.dx && (TYPE != QA_F16 || vocab % kWholeStep))) {
       wc = {ws + P.wc, copied, 0, L.features};
-      copies.add(kOneScale, from, L.w_stride, vocab, L.features, ws + P.wc, copied, whole(vocab, kWholeStep), nullptr, kOfW, false);
+      copies.add(kScaleOfW, from, L.w_stride, vocab, L.features, ws + P.wc, copied, whole(vocab, kWholeStep), nullptr, false);
     }
     if (const int rc = copies.launch<TYPE>(stream)) return rc;
     _Float16* const c = (_Float16*)(ws + P.c);
@@ -1023,17 +1051,15 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     const auto logits = [&](auto entropy) {
       constexpr bool kEntropy = decltype(entropy)::value;
       if (P.copies) {
-        const LogitsGradOut<true, kEntropy> grad{vocab, G.rows, list, first, scales, c, 2 * P.vp};
-        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows, kFewerOfB>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xc, copied, 0, L.rows}, L.features, tiles, grad, stream, rows);
+        const LogitsGradOut<TYPE != QA_F16, kEntropy> grad{vocab, G.rows, list, x_exp, first, scales, c, 2 * P.vp};
+        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows, kFewerOfB>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xr, copied, 0, L.rows}, L.features, tiles, grad, stream, rows);
       }
       if constexpr (TYPE != QA_F32) {              // copied always
-        const LogitsGradOut<false, kEntropy> grad{vocab, G.rows, list, first, scales, c, 2 * P.vp};
+        const LogitsGradOut<false, kEntropy> grad{vocab, G.rows, list, nullptr, first, scales, c, 2 * P.vp};
         Fewer or_all = rows;
-        if (own) {
-          or_all.all = G.x;
-          or_all.all_ld = L.x_stride;
-        }
-        return logits_launch<TYPE == QA_BF16, kRows, kFewerOfB>(Operand{from, L.w_stride, 0, vocab}, Operand{ws + (own ? P.xr : P.xc), P.hc, 0, L.rows}, L.features, tiles, grad, stream, or_all);
+        or_all.all = G.x;
+        or_all.all_ld = L.x_stride;
+        return logits_launch<TYPE == QA_BF16, kRows, kFewerOfB>(Operand{from, L.w_stride, 0, vocab}, Operand{ws + P.xr, copied, 0, L.rows}, L.features, tiles, grad, stream, or_all);
       }
       return (int)QA_ERR_INVALID_ARG;              // not reached
     };
@@ -1041,7 +1067,7 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     if (G.dx) {
       const bool last = first + P.piece >= L.vocab;
       const GradOut<TYPE> out{(ElemT<TYPE>*)G.dx, P.pieces > 1 || P.dx.splits > 1 ? (float*)(ws + P.sums) : nullptr, scales, G.dx_stride, L.rows, L.features,
-                              TYPE == QA_F16 ? -1 : kOfW, first > 0, last && P.dx.splits == 1, list};
+                              first > 0, last && P.dx.splits == 1, list, c_exp};
       // One part of c has 11 bits, which is little beside bfloat16's 8, but as much as binary16's own.
       constexpr Lies kC = TYPE == QA_BF16 ? kHiOfRows : kRowsOfParts;
       if (const int rc = grad_product<kColumnsOf, kC, kFewerOfB>(wc, Operand{c, 2 * P.vp, 0, L.rows}, vocab, out, P.dx, dx_rows, stream)) return rc;
@@ -1052,7 +1078,7 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
       float* const dw = G.dw + first * G.dw_stride;
       const ProductPlan plan = dw_plan(L, TYPE, vocab);
       float* const sums = plan.splits > 1 ? (float*)(ws + P.dw_sums) : nullptr;
-      const GradOut<QA_F32> out{dw, sums, scales, G.dw_stride, vocab, L.features, TYPE == QA_F16 ? -1 : kOfX, !sums && G.accumulate, !sums, nullptr};
+      const GradOut<QA_F32> out{dw, sums, scales, G.dw_stride, vocab, L.features, !sums && G.accumulate, !sums, nullptr, nullptr};
       if (const int rc = grad_product<kColumnsOf, kColumnsOfParts, kFewerOfK>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, plan, rows, stream)) return rc;
       if (sums)
         if (const int rc = sum_launch<QA_F32>(sums, Splits{(int)plan.splits}, vocab, L.features, dw, G.dw_stride, G.accumulate, stream)) return rc;
