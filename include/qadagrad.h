@@ -616,7 +616,8 @@ int qa_output_logprob(const qa_output_layer* layer, int type, const void* x, con
  * dx's own), binary32 x and w in two (22 bits and a sign), 16-bit ones exactly; but nothing is held below 2^-39 of the largest of its kind.  With
  * |g_t| = |g_logprob_t| + 18 |g_entropy_t| that is for dx 2^-39 |g_t| of c, the row's own, and 2^-39 of the largest magnitude in w, and for dw
  * 2^-39 |g_t| of c and 2^-39 of the largest |g_t| |x_t| over all rows of a product.  The logits are multiplied from x and w as they are where
- * qa_output_logprob would read more than 64 rows where they lie, and elsewhere from numbers to 2^-39 of the largest in a row of x, and in w.  dx_or_null and dw_or_null may be NULL (not both); dx does not overlap x.
+ * qa_output_logprob would read more than 64 rows where they lie, and elsewhere from numbers to 2^-39 of the largest in a row of x, and in w
+ * (where features max|x| max|w| could be 2^22: in a row of w).  dx_or_null and dw_or_null may be NULL (not both); dx does not overlap x.
  * rows == 0 writes dw = 0 (kept, with accumulate). */
 int qa_output_logprob_grad(const qa_output_layer* layer, int type, const void* x, const void* w,
                            const int32_t* target_or_null, const float* stats, const float* entropy_or_null,

@@ -61,16 +61,18 @@ __device__ __forceinline__ bool counts(const Row& r) { return r.a != 0.0f || r.e
 // The gradient's operands are scaled by powers of two, so that binary16 holds them to 2^-39 of a largest magnitude: c of its row's bound,
 // r 2^c_exp, and x for the logits of its row's largest element.  A row's dx is as exact as if it were alone, then, whatever the others weigh.  dw is a sum
 // over rows, whose c are so scaled: x is multiplied there by 2^(x_exp - c_exp) of its row, with one x_exp by which the largest |c| |x| is
-// 2^29.  w has one scale for dx, where it is summed over, and for the logits.
+// 2^29.  w has one scale for dx, where it is summed over, and for the logits too, unless those are large.
 //
 // Work-groups leave their largest magnitudes side by side, the next kernel's find the largest of them, and its first one leaves
 // the exponents for the kernels behind it: no atomics, nothing to clear.  (One word for the maximum: 100 us for 8192 atomics.)
 enum { kOfRows, kOfX, kOfW };
+enum { kBesideC, kInX, kInW };                     // key_of() rows' c and x; bits of what is largest in x, and in w
 constexpr int kMostBlocks = 1024;
 struct Scales {
   int x_exp, w_exp;
+  int wide;                                        // w's rows have scales of their own for the logits
   int rows;                                        // that count
-  uint32_t found[3][kMostBlocks];                  // of x: key_of() rows' c and x; of w: bits; the first is unused
+  uint32_t found[3][kMostBlocks];
   int counted[kMostBlocks];                        // of each share of the rows
 };
 // The largest |c| that a row can have: p <= 1, p |log p| <= 1 / e, and an entropy of at most log 2^24 < 17.  (The bound itself may leave binary32.)
@@ -82,18 +84,29 @@ __device__ __forceinline__ int exponent_of_c(const Row& r) {
 constexpr int kKeyOfOne = 1024 + 127;
 __device__ __forceinline__ uint32_t key_of(uint32_t most_x, int c_exp) { return most_x == 0 ? 0 : 1024 + max(most_x >> 23, 1u) - c_exp; }
 __device__ __forceinline__ int x_exp_for(uint32_t key) { return key == 0 ? 0 : 14 - ((int)key - kKeyOfOne); }
+// With one scale an element of w is off by 2^-39 of the largest, and a logit by at most features max|x| max|w| 2^-38.  That is below 2^-16
+// unless it could be 2^22 (a row of w that is 2^30 times as large as the others, or so is x).  Then a second copy of w for the logits is worth its time.
+__device__ __forceinline__ bool wide_for(uint32_t most_x, uint32_t most_w, int64_t features) {
+  return (int)(most_x >> 23) - 127 + (int)(most_w >> 23) - 127 + (64 - __builtin_clzll((uint64_t)features)) > 21;
+}
 __device__ __forceinline__ uint32_t most_in_wave(uint32_t most) {
 #pragma unroll
   for (int s = 1; s < kWave; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s, kWave));
   return most;
 }
-__device__ __forceinline__ uint32_t most_in_block(uint32_t most) {
-  __shared__ uint32_t waves[kWaves];
-  most = most_in_wave(most);
+template <int N>
+__device__ __forceinline__ void most_in_block(uint32_t (&most)[N]) {
+  __shared__ uint32_t waves[N][kWaves];
+#pragma unroll
+  for (int i = 0; i < N; ++i) most[i] = most_in_wave(most[i]);
   __syncthreads();
-  if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = most;
+  if (threadIdx.x % kWave == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) waves[i][threadIdx.x / kWave] = most[i];
+  }
   __syncthreads();
-  return max(max(waves[0], waves[1]), max(waves[2], waves[3]));
+#pragma unroll
+  for (int i = 0; i < N; ++i) most[i] = max(max(waves[i][0], waves[i][1]), max(waves[i][2], waves[i][3]));
 }
 
 struct MostArgs {
@@ -135,7 +148,7 @@ template <int TYPE>
 __global__ __launch_bounds__(kThreads) void output_most_kernel(MostArgs A) {
   int block = blockIdx.x, which = 0;
   while (block >= A.blocks[which]) block -= A.blocks[which++];
-  uint32_t most = 0;
+  uint32_t most = 0, key = 0;
   if (which == kOfRows) {
     __shared__ int waves[kWaves];
     const int64_t first = block * A.share, end = min(A.rows, first + A.share);
@@ -166,12 +179,19 @@ __global__ __launch_bounds__(kThreads) void output_most_kernel(MostArgs A) {
     } else {
       for (int64_t row = first; row < A.rows; row += next) {
         const Row r = row_of(A.R, row);
-        if (counts(r)) most = max(most, key_of(most_in_wave(most_of_row<TYPE>((const ElemT<TYPE>*)A.x + row * A.x_stride, A.features)), exponent_of_c(r)));
+        if (!counts(r)) continue;
+        const uint32_t here = most_in_wave(most_of_row<TYPE>((const ElemT<TYPE>*)A.x + row * A.x_stride, A.features));
+        most = max(most, here);
+        key = max(key, key_of(here, exponent_of_c(r)));
       }
     }
   }
-  most = most_in_block(most);
-  if (threadIdx.x == 0) A.scales->found[which][block] = most;
+  if (which == kOfRows) return;
+  uint32_t both[2] = {most, key};
+  most_in_block(both);
+  if (threadIdx.x != 0) return;
+  A.scales->found[which == kOfX ? kInX : kInW][block] = both[0];
+  if (which == kOfX) A.scales->found[kBesideC][block] = both[1];
 }
 
 // Rows copied, a wave per row: 16-bit elements as they are, or binary16 (binary32 elements: in two parts) times a power of two: of the row's largest
@@ -183,7 +203,8 @@ struct Copy {
   int64_t stride, rows, cols;
   void* to;
   int64_t ld, to_rows;                             // zeros up to ld / parts columns, and in rows from `rows` on
-  int* exps;                                       // kOwnScale: written
+  int* exps;                                       // kOwnScale, and rows in wide_to: written
+  void* wide_to;                                   // NULL, or where rows go a second time, by scales of their own, if logits are large
   bool gather;                                     // the rows that count, one behind the other, and zeros up to a whole step of the products
   bool unless_all;                                 // count
   int blocks;
@@ -193,7 +214,8 @@ struct CopyArgs {
   Copy copy[kCopies];
   Scales* scales;
   bool first;                                      // the largest magnitudes are found, and their exponents left
-  int found[3];                                    // how many there are of them
+  int found[3];                                    // how many work-groups left them: for which rows count, for x, for w
+  int64_t features;
   RowArgs R;
   const int* place;                                // of rows that are gathered, in shares; the first copy gathers, and writes which there are
   int64_t share;
@@ -204,39 +226,47 @@ struct CopyArgs {
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
   constexpr int kParts = TYPE == QA_F32 ? 2 : 1;
-  const auto find = [&](int which) {
-    uint32_t most = 0;
-    for (int b = threadIdx.x; b < A.found[which]; b += kThreads) most = max(most, A.scales->found[which][b]);
-    return most_in_block(most);
-  };
-  if (blockIdx.x == 0 && A.first) {
-    const uint32_t x = find(kOfX), w = find(kOfW);
-    if (threadIdx.x == 0) {
-      A.scales->x_exp = x_exp_for(x);
-      A.scales->w_exp = exponent_for(w);
+  int x_exp = 0, w_exp = 0;
+  bool wide = false;
+  if (A.first) {
+    uint32_t most[3] = {};
+    for (int b = threadIdx.x; b < A.found[kOfX]; b += kThreads) {
+      most[kBesideC] = max(most[kBesideC], A.scales->found[kBesideC][b]);
+      most[kInX] = max(most[kInX], A.scales->found[kInX][b]);
     }
+    for (int b = threadIdx.x; b < A.found[kOfW]; b += kThreads) most[kInW] = max(most[kInW], A.scales->found[kInW][b]);
+    most_in_block(most);
+    x_exp = x_exp_for(most[kBesideC]);
+    w_exp = exponent_for(most[kInW]);
+    wide = wide_for(most[kInX], most[kInW], A.features);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      A.scales->x_exp = x_exp;
+      A.scales->w_exp = w_exp;
+      A.scales->wide = wide;
+    }
+  } else if (TYPE != QA_F16 && A.scales) {
+    w_exp = A.scales->w_exp;
+    wide = A.scales->wide;
   }
   int block = blockIdx.x, at = 0;
   while (at < kCopies && block >= A.copy[at].blocks) block -= A.copy[at++].blocks;
   if (at == kCopies) return;
   const Copy& C = A.copy[at];
   const int lane = threadIdx.x % kWave;
-  int exp = 0, x_exp = 0;
-  if (C.how == kScaleOfW && TYPE != QA_F16) exp = A.first ? exponent_for(find(kOfW)) : A.scales->w_exp;
-  if (C.how == kScaleBesideC) x_exp = x_exp_for(find(kOfX));
-  const auto copy = [&](int64_t from, int64_t to, int64_t cols) {
+  const auto copy = [&](int how, void* whereto, int64_t from, int64_t to, int64_t cols) {
     const ElemT<TYPE>* p = (const ElemT<TYPE>*)C.from + from * C.stride;
-    _Float16* q = (_Float16*)C.to + to * C.ld;
-    if (TYPE != QA_F16 && C.how == kOwnScale) {
+    _Float16* q = (_Float16*)whereto + to * C.ld;
+    int exp = w_exp;
+    if (TYPE != QA_F16 && how == kOwnScale) {
       exp = exponent_for(most_in_wave(cols ? most_of_row<TYPE>(p, cols) : 0));
       if (lane == 0) C.exps[to] = exp;
     }
-    if (C.how == kScaleBesideC && cols) exp = x_exp - exponent_of_c(row_of(A.R, from));
+    if (how == kScaleBesideC && cols) exp = x_exp - exponent_of_c(row_of(A.R, from));
     for (int64_t c = lane * kVec; c < C.ld / kParts; c += kWave * kVec) {
       const int n = (int)max((int64_t)0, min((int64_t)kVec, cols - c));
       bool copied = false;
       if constexpr (TYPE != QA_F32) {
-        copied = C.how == kAsTheyAre || (TYPE == QA_F16 && C.how != kScaleBesideC);
+        copied = how == kAsTheyAre || (TYPE == QA_F16 && how != kScaleBesideC);
         if (copied) *reinterpret_cast<u32x4*>(q + c) = n ? load_raw<TYPE>(p + c, n).a : u32x4{};
       }
       if (!copied) {
@@ -251,7 +281,9 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
   };
   const int64_t first = (int64_t)block * kWaves + threadIdx.x / kWave, next = (int64_t)C.blocks * kWaves;
   if (!C.gather) {
-    for (int64_t row = first; row < C.to_rows; row += next) copy(row, row, row < C.rows ? C.cols : 0);
+    for (int64_t row = first; row < C.to_rows; row += next) copy(C.how, C.to, row, row, row < C.rows ? C.cols : 0);
+    if (TYPE != QA_F16 && C.wide_to && wide)
+      for (int64_t row = first; row < C.to_rows; row += next) copy(kOwnScale, C.wide_to, row, row, row < C.rows ? C.cols : 0);
     return;
   }
   __shared__ int before[kMostBlocks], waves[kWaves];           // rows that count before each share
@@ -285,7 +317,7 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
     const int place = A.place[row];
     if (place >= 0) {
       const int64_t to = before[row / A.share] + place;
-      if (!(C.unless_all && rows == C.rows)) copy(row, to, C.cols);
+      if (!(C.unless_all && rows == C.rows)) copy(C.how, C.to, row, to, C.cols);
       if (at == 0 && lane == 0) {
         A.list[to] = (int)row;
         A.c_exp[to] = exponent_of_c(row_of(A.R, row));
@@ -297,7 +329,7 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
     }
   }
   if (block == 0)
-    for (int64_t to = rows + threadIdx.x / kWave; to < whole(max(1, rows), kPartsStep); to += kWaves) copy(0, to, 0);
+    for (int64_t to = rows + threadIdx.x / kWave; to < whole(max(1, rows), kPartsStep); to += kWaves) copy(C.how, C.to, 0, to, 0);
 }
 
 // ---- scoring ------------------------------------------------------------------------------------------------------------------
@@ -607,20 +639,22 @@ __global__ __launch_bounds__(THREADS) void output_join_kernel(ScoreArgs A, int64
 // with all of them multiplied).
 
 // c of a piece of the vocabulary, scaled, in rows of parts, for the rows that count: zeros behind the piece, and in rows up to a whole step.
-// SCALED: of operands scaled by a power of two per row of x, and one of w.
+// SCALED: of operands scaled by a power of two per row of x, and one of w or, if logits are large, of each of its rows.
 // log p is never above 0, though statistics and logits of 10^8, multiplied in another order, are tens apart: c stays within its bound, and
 // binary16 with it (NaN stays NaN).
 template <bool SCALED, bool ENTROPY>
 struct LogitsGradOut {
   int64_t vocab;                                   // of this piece
   RowArgs R;
-  const int *list, *x_exp;                         // rows that count; SCALED: of each of them
+  const int *list, *x_exp, *w_exps;                // rows that count; SCALED: of each of them, and of the piece's rows of w
   int64_t first;                                   // of the piece
   const Scales* scales;
   _Float16* c;
   int64_t ld;
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t v0, int64_t t0, char* lds) const {
-    const int lane = threadIdx.x % kWave, w_exp = SCALED ? scales->w_exp : 0;
+    const int lane = threadIdx.x % kWave;
+    const bool own_w = SCALED && scales->wide;
+    const int w_exp = SCALED && !own_w ? scales->w_exp : 0;
     constexpr int FN = (int)(sizeof p.acc[0] / sizeof p.acc[0][0]);
     float m[FN], log_sum[FN], a[FN], e[FN], h[FN];
     int here[FN], z_exp[FN];
@@ -646,6 +680,12 @@ struct LogitsGradOut {
     p.template for_runs<false>(0, 0, lds, [&](int v, int col, float (&z)[kVec]) {
       const int j = col / 32;
       float g[kVec];
+      if (own_w) {
+        int own[kVec];                             // (what stands there behind the vocabulary's end serves nobody)
+        __builtin_memcpy(own, __builtin_assume_aligned(w_exps + v0 + v, 16), sizeof own);
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) z[k] = ldexpf(z[k], -own[k]);
+      }
 #pragma unroll
       for (int k = 0; k < kVec; ++k) {
         if (SCALED) z[k] = ldexpf(z[k], z_exp[j]);
@@ -804,7 +844,7 @@ struct Plan {
   size_t x, w, x_exp, w_exp;                       // copies and exponents
   size_t m, s, sw, given;                          // scoring
   int64_t chunks, each;                            // each: of the vocabulary per work-group, where w is streamed
-  size_t scales, place, list, c_exp, xr, xc, wc, c, sums;       // gradient: rows of x for the logits; x and w as the products with c take them
+  size_t scales, place, list, c_exp, xr, xc, wc, wr, c, sums;   // gradient: rows of x and (if they are large) of w for the logits; x and w as the products with c take them
   size_t dw_sums;
   int64_t hc, tp, vp;
   ProductPlan dx;
@@ -861,6 +901,8 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.xr = room.take(2 * P.parts * P.tp * P.hc);
     P.xc = room.take(2 * P.parts * P.tp * P.hc);
     P.wc = room.take(2 * P.parts * P.vp * P.hc);
+    P.wr = room.take(P.copies && type != QA_F16 ? 2 * P.parts * P.vp * P.hc : 0);
+    P.w_exp = room.take(P.copies && type != QA_F16 ? 4 * whole(P.vp, 256) : 0);
     P.c = room.take(2 * 2 * P.tp * P.vp);
     // dx has few tiles and sums over the vocabulary.
     const bool one = type == QA_BF16;
@@ -878,8 +920,10 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
     P.sw = room.take(4 * P.chunks * P.rows);
     P.given = room.take(4 * P.rows);
   }
-  if (op == QA_OP_LOGPROB) P.x_exp = room.take(P.copy_x && type == QA_F32 ? 4 * P.rows : 0);
-  P.w_exp = room.take(P.copy_w && type == QA_F32 ? 4 * P.piece : 0);
+  if (op == QA_OP_LOGPROB) {
+    P.x_exp = room.take(P.copy_x && type == QA_F32 ? 4 * P.rows : 0);
+    P.w_exp = room.take(P.copy_w && type == QA_F32 ? 4 * P.piece : 0);
+  }
   P.x = room.take(P.copy_x ? 2 * P.parts * P.rows * P.hp : 0);
   P.w = room.take(P.copy_w ? 2 * P.parts * P.piece * P.hp : 0);
   P.bytes = room.bytes;
@@ -898,9 +942,12 @@ size_t bytes_of(const qa_output_layer& L, int op, int type) {
 struct CopyList {
   CopyArgs A = {};
   int n = 0, blocks = 0;
-  void add(int how, const void* from, int64_t stride, int64_t rows, int64_t cols, void* to, int64_t ld, int64_t to_rows, int* exps, bool gather, bool unless_all = false) {
+  void add(int how, const void* from, int64_t stride, int64_t rows, int64_t cols, void* to, int64_t ld, int64_t to_rows, int* exps, bool gather, bool unless_all = false, void* wide_to = nullptr) {
     Copy& C = A.copy[n++];
-    C = {how, from, stride, rows, cols, to, ld, to_rows, exps, gather, unless_all, (int)std::min<int64_t>(ceil_div(to_rows, kWaves), 1 << 14)};
+    // A gradient's first copies begin with finding the largest magnitudes: few work-groups, several rows each (333 rows, 32771 x 257 binary32: 145 us
+    // with 1024, 147.5 with 4096, 151.5 with 8368).
+    const int64_t most = A.first ? 1024 : 1 << 14;
+    C = {how, from, stride, rows, cols, to, ld, to_rows, exps, wide_to, gather, unless_all, (int)std::min<int64_t>(ceil_div(to_rows, kWaves), most)};
     blocks += C.blocks;
   }
   template <int TYPE> int launch(hipStream_t stream) {
@@ -1009,9 +1056,11 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
   int* const list = (int*)(ws + P.list);
   int* const c_exp = (int*)(ws + P.c_exp);
   int* const x_exp = (int*)(ws + P.x_exp);
+  int* const w_exp = (int*)(ws + P.w_exp);
+  const bool can_be_wide = P.copies && TYPE != QA_F16;
   const Fewer rows = {.n = &scales->rows};
   const MostArgs most = {G.rows, L.rows, L.vocab, L.features, G.x, G.w, L.x_stride, L.w_stride, scales, place, share,
-                         {(int)ceil_div(L.rows, share), blocks(G.dw, L.rows, kWaves), blocks(TYPE != QA_F16 && (G.dx || P.copies), L.vocab, kWaves)}};
+                         {(int)ceil_div(L.rows, share), blocks(G.dw || P.copies, L.rows, kWaves), blocks(TYPE != QA_F16 && (G.dx || P.copies), L.vocab, kWaves)}};
   output_most_kernel<TYPE><<<(unsigned)(most.blocks[0] + most.blocks[1] + most.blocks[2]), kThreads, 0, stream>>>(most);
   if (const int rc = launch_status()) return rc;
 
@@ -1020,6 +1069,7 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
   copies.A.scales = scales;
   copies.A.first = true;
   for (int i = 0; i < 3; ++i) copies.A.found[i] = most.blocks[i];
+  copies.A.features = L.features;
   copies.A.R = G.rows;
   copies.A.place = place;
   copies.A.share = share;
@@ -1043,7 +1093,7 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     Operand wc = {from, L.w_stride, 0, L.features};
     if (P.copies || (G.dx && (TYPE != QA_F16 || vocab % kWholeStep))) {
       wc = {ws + P.wc, copied, 0, L.features};
-      copies.add(kScaleOfW, from, L.w_stride, vocab, L.features, ws + P.wc, copied, whole(vocab, kWholeStep), nullptr, false);
+      copies.add(kScaleOfW, from, L.w_stride, vocab, L.features, ws + P.wc, copied, whole(vocab, kWholeStep), w_exp, false, false, can_be_wide ? ws + P.wr : nullptr);
     }
     if (const int rc = copies.launch<TYPE>(stream)) return rc;
     _Float16* const c = (_Float16*)(ws + P.c);
@@ -1051,11 +1101,16 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
     const auto logits = [&](auto entropy) {
       constexpr bool kEntropy = decltype(entropy)::value;
       if (P.copies) {
-        const LogitsGradOut<TYPE != QA_F16, kEntropy> grad{vocab, G.rows, list, x_exp, first, scales, c, 2 * P.vp};
-        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows, kFewerOfB>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xr, copied, 0, L.rows}, L.features, tiles, grad, stream, rows);
+        const LogitsGradOut<TYPE != QA_F16, kEntropy> grad{vocab, G.rows, list, x_exp, w_exp, first, scales, c, 2 * P.vp};
+        Fewer or_wide = rows;
+        if (can_be_wide) {
+          or_wide.wide = &scales->wide;
+          or_wide.wide_a = ws + P.wr;
+        }
+        return logits_launch<false, TYPE == QA_F32 ? kRowsOfParts : kRows, kFewerOfB>(Operand{wc.p, wc.ld, 0, vocab}, Operand{ws + P.xr, copied, 0, L.rows}, L.features, tiles, grad, stream, or_wide);
       }
       if constexpr (TYPE != QA_F32) {              // copied always
-        const LogitsGradOut<false, kEntropy> grad{vocab, G.rows, list, nullptr, first, scales, c, 2 * P.vp};
+        const LogitsGradOut<false, kEntropy> grad{vocab, G.rows, list, nullptr, nullptr, first, scales, c, 2 * P.vp};
         Fewer or_all = rows;
         or_all.all = G.x;
         or_all.all_ld = L.x_stride;

@@ -41,6 +41,8 @@ struct Fewer {
   int most_splits;                                 // of B's fewer: more splits, up to so many, in their place; 0: as planned
   const void* all;                                 // NULL, or where B is if there are all of them
   int64_t all_ld;
+  const int* wide;                                 // of B's fewer: NULL, or whether A is elsewhere
+  const void* wide_a;
 };
 // Splits of a product in tiles of `side` along B, of whose `all` n are left: as many tiles and no more sums than with all of them.
 __host__ __device__ constexpr unsigned splits_of_fewer(unsigned splits, unsigned most, unsigned side, unsigned all, unsigned n) {
@@ -421,6 +423,7 @@ __global__ __launch_bounds__(P::kGroup, P::kWavesPerSimd) void product_kernel(Pr
       const bool all = A.fewer.all && n == A.b.n;
       A.b.p = all ? A.fewer.all : A.b.p;
       A.b.ld = all ? A.fewer.all_ld : A.b.ld;
+      if (A.fewer.wide) A.a.p = *A.fewer.wide ? A.fewer.wide_a : A.a.p;
       A.splits = A.fewer.most_splits ? splits_of_fewer(A.splits, A.fewer.most_splits, P::kN, (unsigned)A.b.n, n) : A.splits;
       A.b.n = n;
       A.tiles_n = (unsigned)(n + P::kN - 1) / P::kN;

@@ -114,3 +114,18 @@ def test_a_row_of_x_beside_a_much_larger_one(t, lead, T):
     x[T // 2] *= 2.0 ** (34 if t != "f16" else 8)
     x[3] *= 2.0 ** (-34 if t != "f16" else -8)
     check(t, x, w, y, torch.rand(T, generator=gen) + 0.5, None, lead)
+
+
+@pytest.mark.parametrize("t,lead,T", [("f32", 0, 100), ("f32", 0, 40), ("bf16", 0, 100), ("bf16", 1, 100), ("f16", 1, 100)])
+@pytest.mark.parametrize("power", [10, 30, 60])
+def test_a_row_of_w_beside_a_much_larger_one(t, lead, T, power):
+    """A word whose logits are 2^30 below all others', and one with a small row: the others' logits, and dw, are as exact as without them."""
+    gen = gen_of("large word", t, T, power)
+    x, w, y = rows_of(gen, T, 300, 96)
+    power = power if t != "f16" else power // 4
+    x[:, 0] = 1.0
+    w[150] *= 2.0 ** -20 if t != "f16" else 2.0 ** -8
+    w[150, 0] = -(2.0 ** power)
+    w[7] *= 2.0 ** -30 if t != "f16" else 2.0 ** -8
+    y[y == 150] = 3
+    check(t, x, w, y, torch.rand(T, generator=gen) + 0.5, None, lead)
