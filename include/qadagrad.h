@@ -609,13 +609,13 @@ int qa_output_logprob(const qa_output_layer* layer, int type, const void* x, con
 /* Gradients of x and w from those of logprob and entropy (binary32, one per row; NULL counts as 0):
  *     c_tj = g_logprob_t ([j = target_t] - p_tj) - g_entropy_t p_tj (log p_tj + entropy_t)
  *     dx = c w (type `type`);   dw_jk = (accumulate ? dw_jk : 0) + sum_t c_tj x_tk (binary32)
- * with the logits multiplied again, a piece of the vocabulary at a time.  stats and entropy as qa_output_logprob wrote them
+ * with the logits multiplied again, a piece of the vocabulary at a time, and of the rows where there are more than 2^16 (or 2^26 / vocab).  stats and entropy as qa_output_logprob wrote them
  * (entropy and g_entropy NULL together).  A row without target has the entropy's part alone.  A row whose g_logprob (or
  * target) and g_entropy are both none or 0 gets dx = 0 and adds nothing to dw, whatever x holds there: padding.
  * Numbers are multiplied as binary16 times powers of two: c in two parts, but in one for dx of bfloat16 (a rounding by 2^-11, an eighth of
  * dx's own), binary32 x and w in two (22 bits and a sign), 16-bit ones exactly; but nothing is held below 2^-39 of the largest of its kind.  With
  * |g_t| = |g_logprob_t| + 18 |g_entropy_t| that is for dx 2^-39 |g_t| of c, the row's own, and 2^-39 of the largest magnitude in w, and for dw
- * 2^-39 |g_t| of c and 2^-39 of the largest |g_t| |x_t| over all rows of a product.  The logits are multiplied from x and w as they are where
+ * 2^-39 |g_t| of c and 2^-39 of the largest |g_t| |x_t| over all rows of a piece.  The logits are multiplied from x and w as they are where
  * qa_output_logprob would read more than 64 rows where they lie, and elsewhere from numbers to 2^-39 of the largest in a row of x, and in w
  * (where features max|x| max|w| could be 2^22: in a row of w).  dx_or_null and dw_or_null may be NULL (not both); dx does not overlap x.
  * rows == 0 writes dw = 0 (kept, with accumulate). */

@@ -777,7 +777,7 @@ __global__ __launch_bounds__(kThreads) void output_zero_kernel(float* p, int64_t
 
 // ---- what a call does ------------------------------------------------------------------------------------------------------------
 
-// Bytes of a piece's c, of its copy of w and of sums that are joined: about what the last-level cache holds.  (Gradient of 8192 rows, 32768 x 4096: 7.74 ms, 8.03
+// Bytes of a piece's c, of its copy of w and of sums that are joined (of one split at least): about what the last-level cache holds.  (Gradient of 8192 rows, 32768 x 4096: 7.74 ms, 8.03
 // with half of it, 7.66 with twice and four times as much; 4096 rows, 50021 x 1024: 2.29, 2.28, 2.41, 2.20.)
 constexpr int64_t kPieceBytes = int64_t(256) << 20;
 
@@ -929,8 +929,16 @@ Plan plan_of(const qa_output_layer& L, int op, int type, const void* x, const vo
   P.bytes = room.bytes;
   return P;
 }
+// Rows of a gradient's launches: so many that a piece of c can be 1024 wide, or the whole vocabulary.
+int64_t grad_rows_of(const qa_output_layer& L) { return piece_of(L.rows, kPieceBytes / (4 * whole(std::min<int64_t>(L.vocab, 1024), kWholeStep)) / 256 * 256); }
 // At most, whatever the alignment of x and w.
 size_t bytes_of(const qa_output_layer& L, int op, int type) {
+  if (const int64_t piece = grad_rows_of(L); op == QA_OP_LOGPROB_GRAD && piece < L.rows) {
+    qa_output_layer full = L, last = L;
+    full.rows = piece;
+    last.rows = (L.rows - 1) % piece + 1;
+    return std::max(bytes_of(full, op, type), bytes_of(last, op, type));
+  }
   alignas(16) static const char aligned_place[16] = {};
   size_t most = 0;
   for (const void* x : {(const void*)nullptr, (const void*)aligned_place})
@@ -1047,7 +1055,7 @@ struct GradCall {
 };
 
 template <int TYPE>
-int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream_t stream) {
+int grad_rows_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream_t stream) {
   const Plan P = plan_of(L, QA_OP_LOGPROB_GRAD, TYPE, G.x, G.w);
   Scales* const scales = (Scales*)(ws + P.scales);
   const auto blocks = [](bool wanted, int64_t n, int64_t each) { return wanted ? (int)std::min<int64_t>(kMostBlocks, ceil_div(n, each)) : 0; };
@@ -1138,6 +1146,27 @@ int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream
       if (sums)
         if (const int rc = sum_launch<QA_F32>(sums, Splits{(int)plan.splits}, vocab, L.features, dw, G.dw_stride, G.accumulate, stream)) return rc;
     }
+  }
+  return QA_OK;
+}
+
+template <int TYPE>
+int grad_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipStream_t stream) {
+  const auto from = [](auto* p, int64_t n) { return p ? p + n : p; };
+  const int64_t piece = grad_rows_of(L);
+  for (int64_t t = 0; t < L.rows; t += piece) {
+    qa_output_layer here = L;
+    here.rows = std::min(piece, L.rows - t);
+    GradCall its = G;
+    its.x = (const ElemT<TYPE>*)G.x + t * L.x_stride;
+    its.rows.target = from(G.rows.target, t);
+    its.rows.stats = G.rows.stats + 2 * t;
+    its.rows.entropy = from(G.rows.entropy, t);
+    its.rows.g_logprob = from(G.rows.g_logprob, t);
+    its.rows.g_entropy = from(G.rows.g_entropy, t);
+    its.dx = from((ElemT<TYPE>*)G.dx, t * G.dx_stride);
+    its.accumulate = t > 0 || G.accumulate;
+    if (const int rc = grad_rows_launch<TYPE>(here, its, ws, stream)) return rc;
   }
   return QA_OK;
 }

@@ -137,3 +137,16 @@ def test_step_orthogonal():
         assert call(name, matrices(), **bad) == INVALID, bad
     for bad in (dict(g=FAKE + 2), dict(momentum=FAKE + 2), dict(x=FAKE + 2)):
         assert call(name, matrices(), **bad) == ALIGNMENT, bad
+
+
+def test_a_gradients_workspace_does_not_grow_with_c():
+    """c of 2^20 rows would be 4 GiB for 1024 words, in pieces of the vocabulary alone; copies and sums of a piece of the rows are what is left."""
+    need = lambda rows, vocab, features, t: qa.qa_output_workspace_bytes(qa.OutputLayer.make(rows, vocab, features), qa.QA_OP_LOGPROB_GRAD, t)  # noqa: E731
+    for rows in (1 << 16, (1 << 16) + 1, 100003, 1 << 20, (1 << 24) - 1):
+        for t in (F32, BF16, F16):
+            assert need(rows, 32768, 64, t) < 1 << 30
+            assert need(rows, 50, 64, t) < 2 << 30
+    assert need(1 << 20, 32768, 1024, BF16) < 2 << 30
+    # two pieces of 35072 rows need no more than one of 65536
+    for t in (F32, BF16, F16):
+        assert need(70000, 32768, 64, t) <= need(1 << 16, 32768, 64, t)
