@@ -641,9 +641,10 @@ typedef struct {
 
 #define QA_ORTHOGONAL_STEPS_MAX 32
 
-/* Bytes of device workspace that the calls below need for matrices of `type` (QA_F32 for qa_step_orthogonal): 8 to 16 per
- * element; 0 for matrices that a compute unit holds (sides of up to some 128 x 128, 96 x 288 or 64 x 512), for
- * invalid arguments and for count == 0. */
+/* Bytes of device workspace that the calls below need for matrices of `type` (QA_F32 for qa_step_orthogonal): with n the smaller
+ * and m the larger side, and [k] for k up to a multiple of 16, 8 [n] ([m] + n) and at most 8 KiB per matrix, and at most 1280 (8 to 16 per
+ * element where both sides are long, 128 where one is 1); 0 for matrices that a compute unit holds (sides of up to some 128 x 128,
+ * 96 x 288 or 64 x 512), for invalid arguments and for count == 0. */
 size_t qa_orthogonal_workspace_bytes(const qa_matrices* matrices, int type);
 
 /* out = X_steps, 1 <= steps <= QA_ORTHOGONAL_STEPS_MAX.  coefficients: HOST array of 3*steps floats, a, b, c of each

@@ -150,3 +150,12 @@ def test_a_gradients_workspace_does_not_grow_with_c():
     # two pieces of 35072 rows need no more than one of 65536
     for t in (F32, BF16, F16):
         assert need(70000, 32768, 64, t) <= need(1 << 16, 32768, 64, t)
+
+
+def test_workspaces_of_matrices_are_what_the_header_says():
+    up = lambda k: -(-k // 16) * 16  # noqa: E731
+    for count, R, Cc in ((1, 1, 4096), (1, 4096, 1), (3, 2, 1024), (7, 17, 5000), (1, 300, 300), (2, 129, 129), (5000, 40, 600), (1, 4096, 8192)):
+        n, m = min(R, Cc), max(R, Cc)
+        least = count * 8 * up(n) * (up(m) + n)
+        for t in (F32, BF16, F16):
+            assert least <= qa.qa_orthogonal_workspace_bytes(qa.Matrices.make(count, R, Cc), t) <= least + count * 8192 + 1280
