@@ -72,7 +72,7 @@ def test_pieces_of_the_rows(t, T, V, H, entropy, accumulate):
     check(t, T, V, H, kept, entropy, accumulate)
 
 
-@pytest.mark.parametrize("t,T,V,H", [("bf16", 20000, 20011, 32), ("f16", 20000, 20011, 40), ("f32", 9000, 20011, 20)])
+@pytest.mark.parametrize("t,T,V,H", [("bf16", 20000, 20011, 32), ("bf16", 9000, 20011, 32), ("f16", 9000, 20011, 40), ("f32", 9000, 20011, 20)])
 @pytest.mark.parametrize("some", [0.0002, 0.07, 0.5])
 def test_pieces_of_the_vocabulary_where_some_rows_count(t, T, V, H, some):
     """Several pieces, the last one shorter, and dx's sums in splits, whose number the device finds for the rows that count."""
