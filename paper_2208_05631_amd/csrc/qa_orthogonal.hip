@@ -565,7 +565,16 @@ template <int TYPE, bool STEP>
 int orthogonal(const qa_matrices& M, const void* g, float* momentum, void* out, float mu, int nesterov, int steps, const float* coefficients,
                float eta, float shrink, void* ws, void* stream) {
   const auto launch = M.rows > M.cols ? orthogonal_launch<TYPE, STEP, true> : orthogonal_launch<TYPE, STEP, false>;
-  return launch(M, g, momentum, out, mu, nesterov, steps, coefficients, eta, shrink, (char*)ws, (hipStream_t)stream);
+  const int64_t most = most_side_by_side(M.rows, M.cols);
+  for (int64_t i = 0; i < M.count; i += most) {    // once, but for tens of thousands of long thin ones; each time the workspace's front
+    qa_matrices here = M;
+    here.count = std::min(most, M.count - i);
+    const int64_t at = i * M.matrix_stride;
+    const int rc = launch(here, (const ElemT<TYPE>*)g + at, momentum ? momentum + at : nullptr, (ElemT<TYPE>*)out + at, mu, nesterov, steps, coefficients, eta,
+                          shrink, (char*)ws, (hipStream_t)stream);
+    if (rc) return rc;
+  }
+  return QA_OK;
 }
 
 int check_matrices(const qa_matrices* M) {

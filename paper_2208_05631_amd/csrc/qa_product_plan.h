@@ -35,6 +35,12 @@ inline double product_us(Tiles form, const ProductShape& S, int64_t splits) {
          (splits > 1 ? 5.0 + (double)(2 * splits + 1) * (double)S.m * (double)S.n * (4.0 / 5e6) : 0.0);       // written, read and joined at 5 TB/s
 }
 
+// Products side by side in one launch, whose work-items number less than 2^32 in tiles of any form (64 x 64 by 512 are the most).
+inline int64_t most_side_by_side(int64_t m, int64_t n) {
+  const int64_t each = (m + 63) / 64 * ((n + 63) / 64) * 512, most = ((int64_t(1) << 32) - 1) / each;
+  return most > 1 ? most : 1;
+}
+
 struct ProductPlan { Tiles tiles; int64_t splits; };
 // What is estimated to take the least time, of the forms in `allowed` and up to `most` splits, each of eight steps at least and none without any.
 inline ProductPlan product_plan(unsigned allowed, const ProductShape& S, int64_t most) {
