@@ -223,12 +223,13 @@ struct CopyArgs {
   void* zero;                                      // NULL, or zeros go to its rows that do not count
   int64_t zero_stride;
 };
-template <int TYPE>
+// GRAD: a gradient's; the others find nothing and gather nothing, and have registers for more waves.
+template <int TYPE, bool GRAD>
 __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
   constexpr int kParts = TYPE == QA_F32 ? 2 : 1;
   int x_exp = 0, w_exp = 0;
   bool wide = false;
-  if (A.first) {
+  if (GRAD && A.first) {
     uint32_t most[3] = {};
     for (int b = threadIdx.x; b < A.found[kOfX]; b += kThreads) {
       most[kBesideC] = max(most[kBesideC], A.scales->found[kBesideC][b]);
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
       A.scales->w_exp = w_exp;
       A.scales->wide = wide;
     }
-  } else if (TYPE != QA_F16 && A.scales) {
+  } else if (GRAD && TYPE != QA_F16) {
     w_exp = A.scales->w_exp;
     wide = A.scales->wide;
   }
@@ -261,7 +262,7 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
       exp = exponent_for(most_in_wave(cols ? most_of_row<TYPE>(p, cols) : 0));
       if (lane == 0) C.exps[to] = exp;
     }
-    if (how == kScaleBesideC && cols) exp = x_exp - exponent_of_c(row_of(A.R, from));
+    if (GRAD && how == kScaleBesideC && cols) exp = x_exp - exponent_of_c(row_of(A.R, from));
     for (int64_t c = lane * kVec; c < C.ld / kParts; c += kWave * kVec) {
       const int n = (int)max((int64_t)0, min((int64_t)kVec, cols - c));
       bool copied = false;
@@ -280,9 +281,9 @@ __global__ __launch_bounds__(kThreads) void output_copy_kernel(CopyArgs A) {
     }
   };
   const int64_t first = (int64_t)block * kWaves + threadIdx.x / kWave, next = (int64_t)C.blocks * kWaves;
-  if (!C.gather) {
+  if (!GRAD || !C.gather) {
     for (int64_t row = first; row < C.to_rows; row += next) copy(C.how, C.to, row, row, row < C.rows ? C.cols : 0);
-    if (TYPE != QA_F16 && C.wide_to && wide)
+    if (GRAD && TYPE != QA_F16 && C.wide_to && wide)
       for (int64_t row = first; row < C.to_rows; row += next) copy(kOwnScale, C.wide_to, row, row, row < C.rows ? C.cols : 0);
     return;
   }
@@ -960,7 +961,8 @@ struct CopyList {
   }
   template <int TYPE> int launch(hipStream_t stream) {
     if (!A.first && n == 0) return QA_OK;
-    output_copy_kernel<TYPE><<<(unsigned)std::max(blocks, 1), kThreads, 0, stream>>>(A);
+    const auto kernel = A.scales ? output_copy_kernel<TYPE, true> : output_copy_kernel<TYPE, false>;
+    kernel<<<(unsigned)std::max(blocks, 1), kThreads, 0, stream>>>(A);
     *this = CopyList{{.scales = A.scales}};
     return launch_status();
   }
