@@ -129,3 +129,59 @@ def test_a_row_of_w_beside_a_much_larger_one(t, lead, T, power):
     w[7] *= 2.0 ** -30 if t != "f16" else 2.0 ** -8
     y[y == 150] = 3
     check(t, x, w, y, torch.rand(T, generator=gen) + 0.5, None, lead)
+
+
+@pytest.mark.parametrize("t,lead", [("f32", 0), ("bf16", 1)])
+def test_replayed_where_logits_become_large(t, lead):
+    """A captured gradient whose logits are small, then large, then small: each replay is what an eager call gives, bit for bit."""
+    gen = gen_of("replayed scales", t)
+    T, V, H = 100, 3000, 64
+    x, w, y = rows_of(gen, T, V, H)
+    _, xd = inside(x, t, 0, lead)
+    _, wd = inside(w, t, 0, lead)
+    y, a = y.to(torch.int32).to(DEV), torch.rand(T, generator=gen).to(DEV)
+    layer = qa.OutputLayer.make(T, V, H)
+    h, st = torch.empty(T, device=DEV), torch.empty(T, 2, device=DEV)
+    ws, ws2 = room(layer, qa.QA_OP_LOGPROB, t), room(layer, qa.QA_OP_LOGPROB_GRAD, t)
+    dx, dw = torch.empty(T, H, dtype=TYPES[t], device=DEV), torch.empty(V, H, device=DEV)
+
+    def both():
+        qa.qa_output_logprob(layer, code_of(t), xd, wd, None, None, h, st, ws)
+        qa.qa_output_logprob_grad(layer, code_of(t), xd, wd, y, st, h, a, a, dx, H, dw, H, 0, ws2)
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for power in (0, 20, 0, 30, 40, 0):
+        xd[::7] *= 2.0 ** power
+        both()
+        torch.cuda.synchronize()
+        want = dx.clone(), dw.clone()
+        dx.fill_(7.0), dw.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dx, want[0]) and torch.equal(dw, want[1]) and bool(torch.isfinite(dw).all()), power
+        xd[::7] *= 2.0 ** -power
+
+
+@pytest.mark.parametrize("t,lead", [("f32", 0), ("bf16", 1), ("bf16", 0), ("f16", 0), ("f16", 1)])
+@pytest.mark.parametrize("power", [0, 30])
+def test_one_side_is_as_both(t, lead, power):
+    """dx alone and dw alone, of small logits and large ones, are what both together are, bit for bit."""
+    gen = gen_of("one side", t)
+    T, V, H = 150, 500, 64
+    x, w, y = rows_of(gen, T, V, H)
+    w[7] *= 2.0 ** (power if t != "f16" else power // 4)
+    x64, xd = inside(x, t, 0, lead)
+    w64, wd = inside(w, t, 0, lead)
+    _, _, h, st = (v.float().to(DEV) if v.dim() <= 2 else v for v in ref.score(x64, w64, y))
+    y, a = y.to(torch.int32).to(DEV), torch.rand(T, generator=gen).to(DEV)
+    layer = qa.OutputLayer.make(T, V, H)
+    got = []
+    for wants in ("xw", "x", "w"):
+        dx = torch.full((T, H), 5.0, dtype=TYPES[t], device=DEV) if "x" in wants else None
+        dw = torch.full((V, H), 5.0, device=DEV) if "w" in wants else None
+        qa.qa_output_logprob_grad(layer, code_of(t), xd, wd, y, st, h, a, a, dx, H, dw, H, 0, room(layer, qa.QA_OP_LOGPROB_GRAD, t))
+        got.append((dx, dw))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[2][1])
