@@ -708,24 +708,25 @@ struct LogitsGradOut {
 };
 
 // Sums of a product, unscaled, rounded to the type or added in binary32; the product's columns are the rows that are written.
-template <int TYPE>
+// LISTED: dx, whose rows are those that count; else dw.
+template <int TYPE, bool LISTED>
 struct GradOut {
   ElemT<TYPE>* out;
   float* sums;                                     // [split][rows][cols]; NULL: none before this piece, and this is the last
   const Scales* scales;
   int64_t stride, rows, cols;
   bool add, last;                                  // to what is in sums (or, of binary32, in out); the last piece writes out
-  const int *list, *c_exp;                         // NULL, or the product's rows are those that count, where they go, and their c's exponents
+  const int *list, *c_exp;                         // LISTED: where the rows go, and their c's exponents
   template <class P> __device__ __forceinline__ void operator()(P& p, int64_t m0, int64_t n0, char* lds) const {
-    const int of_all = -(list ? scales->w_exp : scales->x_exp);
-    const int64_t all = list ? scales->rows : rows;
+    const int of_all = -(LISTED ? scales->w_exp : scales->x_exp);
+    const int64_t all = LISTED ? scales->rows : rows;
     float* const its_sums = sums + p.split * all * cols;
     const bool writes = last || !sums;
     p.for_runs(m0, n0, lds, [&](int64_t col, int64_t row, float (&v)[kVec]) {
       if (row >= all || col >= cols) return;
       const int n = (int)min((int64_t)kVec, cols - col);
-      const int exp = of_all - (list ? c_exp[row] : 0);
-      ElemT<TYPE>* const at = out + (list && writes ? list[row] : row) * stride + col;
+      const int exp = LISTED ? of_all - c_exp[row] : of_all;
+      ElemT<TYPE>* const at = out + (LISTED && writes ? list[row] : row) * stride + col;
       float* const s = its_sums + row * cols + col;
       float before[kVec] = {};
       if (add) {
@@ -1131,7 +1132,7 @@ int grad_rows_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipS
     if (const int rc = G.rows.g_entropy ? logits(std::true_type()) : logits(std::false_type())) return rc;
     if (G.dx) {
       const bool last = first + P.piece >= L.vocab;
-      const GradOut<TYPE> out{(ElemT<TYPE>*)G.dx, P.pieces > 1 || P.dx.splits > 1 ? (float*)(ws + P.sums) : nullptr, scales, G.dx_stride, L.rows, L.features,
+      const GradOut<TYPE, true> out{(ElemT<TYPE>*)G.dx, P.pieces > 1 || P.dx.splits > 1 ? (float*)(ws + P.sums) : nullptr, scales, G.dx_stride, L.rows, L.features,
                               first > 0, last && P.dx.splits == 1, list, c_exp};
       // One part of c has 11 bits, which is little beside bfloat16's 8, but as much as binary16's own.
       constexpr Lies kC = TYPE == QA_BF16 ? kHiOfRows : kRowsOfParts;
@@ -1143,7 +1144,7 @@ int grad_rows_launch(const qa_output_layer& L, const GradCall& G, char* ws, hipS
       float* const dw = G.dw + first * G.dw_stride;
       const ProductPlan plan = dw_plan(L, TYPE, vocab);
       float* const sums = plan.splits > 1 ? (float*)(ws + P.dw_sums) : nullptr;
-      const GradOut<QA_F32> out{dw, sums, scales, G.dw_stride, vocab, L.features, !sums && G.accumulate, !sums, nullptr, nullptr};
+      const GradOut<QA_F32, false> out{dw, sums, scales, G.dw_stride, vocab, L.features, !sums && G.accumulate, !sums, nullptr, nullptr};
       if (const int rc = grad_product<kColumnsOf, kColumnsOfParts, kFewerOfK>(Operand{ws + P.xc, copied, 0, L.features}, Operand{c, 2 * P.vp, 0, vocab}, L.rows, out, plan, rows, stream)) return rc;
       if (sums)
         if (const int rc = sum_launch<QA_F32>(sums, Splits{(int)plan.splits}, vocab, L.features, dw, G.dw_stride, G.accumulate, stream)) return rc;
