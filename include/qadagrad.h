@@ -599,9 +599,9 @@ size_t qa_output_workspace_bytes(const qa_output_layer* layer, int op, int type)
 /* logprob, entropy and stats of each row as qa_token_logprob gives them.  target and logprob are NULL together, entropy and
  * stats may be NULL.  16-bit elements are multiplied as they are.  binary32 ones of up to 64 rows are multiplied as three bfloat16 parts
  * each, of more rows as two binary16 parts, scaled by a power of two per row (22 bits and a sign; what is below 2^-39 of a row's largest
- * magnitude is lost).  16-bit x and w whose rows begin on 16 bytes, with strides of a multiple of 8 below 2^22 and features a multiple
- * of 32, are read where they lie, and so are all of up to 64 rows (and 8 features or more); others are copied into the workspace, w a
- * piece of the vocabulary at a time. */
+ * magnitude is lost); an infinity makes the logits that it takes part in NaN.  16-bit x and w whose rows begin on 16 bytes, with
+ * strides of a multiple of 8 below 2^22 and features a multiple of 32, are read where they lie, and so are all of up to 64 rows (and
+ * 8 features or more); others are copied into the workspace, w a piece of the vocabulary at a time. */
 int qa_output_logprob(const qa_output_layer* layer, int type, const void* x, const void* w,
                       const int32_t* target_or_null, float* logprob_or_null, float* entropy_or_null,
                       float* stats_or_null, void* ws, size_t ws_bytes, void* stream);

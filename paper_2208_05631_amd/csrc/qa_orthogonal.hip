@@ -331,7 +331,8 @@ __device__ __forceinline__ void small_eights(const f32x16& acc, const Each& each
   }
 }
 
-// BYTES: half of a compute unit's LDS, or all of it.
+// BYTES: half of a compute unit's LDS, or all of it, by what the matrix takes.  Registers leave room for one work-group of 1024 threads either way, and
+// both take as long (600 of 64 x 64: 55 us, of 96 x 96: 102.5, with either).
 template <int TYPE, bool STEP, bool TALL, int BYTES>
 __global__ __launch_bounds__(kSmallThreads) void orthogonal_small_kernel(SmallArgs<TYPE> A) {
   __shared__ __attribute__((aligned(16))) char lds[BYTES];

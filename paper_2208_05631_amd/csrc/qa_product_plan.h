@@ -16,7 +16,8 @@ struct TileForm {
 };
 // Measured with products of 1 x 1 to 4096 x 4096 numbers in two parts; a step of a large tile takes longer where all run, which the
 // card's power bounds.  (4096 x 4096 A = X X^T: 250 us with tiles of 256, 193 with 192, 234 with 128 shared by two, 257 with 128; 2048 x 8192:
-// 395, 242, 124, 153; 1024 x 1024: 59, 37, 19, 20, and 11.5 with 64 shared by two, 9.9 by four.)
+// 395, 242, 124, 153; 1024 x 1024: 59, 37, 19, 20, and 11.5 with 64 shared by two, 9.9 by four.)  What becomes of the sums there is a store: a tile of logits
+// takes longer behind its steps, and estimates are low for few steps (2060 rows, 16384 x 1024 in tiles of 256, with their gradient: 164 us, 106 estimated).
 constexpr TileForm kTileForms[] = {{256, 256, 0.70, 1.24, 9.0}, {192, 256, 0.38, 0.75, 6.5}, {128, 512, 0.20, 0.71, 4.5},
                                    {128, 256, 0.19, 0.37, 5.0}, {64, 512, 0.11, 0.24, 3.6}, {64, 256, 0.07, 0.115, 4.6}};
 
